@@ -377,6 +377,200 @@ DOPR_API dopr_status dopr_pack_order_noalloc(const dopr_store *store, int32_t n_
                                              void *cuda_stream);
 
 /*
+ * Paged prefix cache: operators for prefixes of any length (whole documents,
+ * prefixes that grow) beside the store of compressed ones above (the paper has
+ * no counterpart; Sec. 3.4's prefix-plus-causal attention is the same).  All
+ * memory is the caller's, on the device that is current: one layer's keys and
+ * values lie in two pools of pages, and a sequence (a table row) is a list of
+ * pages.  A sequence may name a prefix sequence; any number may name the same.
+ * A step of a program is
+ *   dopr_cache_extend           pages, slots, positions for the new tokens
+ *   dopr_shared_attention_plan  how the step's attention is split
+ *   per layer: dopr_cache_append (rotary positions, keys and values into the
+ *   pages) and dopr_shared_attention.
+ * Unlike the calls above these return once their work is on cuda_stream: they
+ * neither allocate, nor synchronise, nor read device memory on the host, and
+ * can be captured into a graph.  Calls that share buffers (a cache, a plan, a
+ * workspace) are ordered by the caller, as its own kernels would be.
+ * Arguments on the host are checked before any launch.  What lies on the
+ * device is checked there: nothing outside the stated extents is read or
+ * written, and an error is stored in *status, a device int32 (NULL: dropped),
+ * as a dopr_status, if *status is DOPR_OK; the caller clears it.  A call on no
+ * rows (n_tokens or max_tokens 0) may pass NULL for the rows' buffers.
+ */
+typedef enum { DOPR_F16 = 0, DOPR_BF16 = 1, DOPR_F32 = 2 } dopr_dtype;
+
+/*
+ * k_pool, v_pool: [n_blocks][n_kv_heads][page][head_dim] of dtype, 16-byte
+ * aligned.  block_tables: int32 [n_seqs][max_blocks]; entry p of a row is the
+ * page of its positions p*page .. p*page + page - 1.
+ * Supported: page 16, 32, 64 or 128; head_dim 64 or 128; dtype F16 or BF16;
+ * n_seqs <= 16384; max_blocks * page < 2^31;
+ * n_blocks * n_kv_heads * page < 2^31.
+ */
+typedef struct {
+    int32_t n_blocks;
+    int32_t page;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t dtype;
+    int32_t n_seqs;
+    int32_t max_blocks;
+} dopr_cache_layout;
+
+/*
+ * Block tables and slots of a step's new tokens, from lengths on the device.
+ * Row i holds seq_lens[i] tokens and gets new_lens[i] >= 0 more; new_lens[i]
+ * == -1 releases it (its pages return to the stack, its length becomes 0).
+ *   seq_lens, new_lens [n_seqs] int32, prefix [n_seqs] int32 or NULL: the row
+ *             that precedes row i's own tokens, -1 for none.  A row that is
+ *             named as a prefix names none itself.
+ *   free_blocks int32 [n_blocks], n_free [1] int32: a stack of unused pages,
+ *             the top at n_free - 1.  Released pages are pushed first, row by
+ *             row in page order; then rows in order take pages from the top,
+ *             which become their next table entries.
+ *   seq_lens_out [n_seqs], n_free_out [1]: lengths and stack height after the
+ *             call; each may be the input itself.
+ *   max_tokens extent of slots and positions; >= the new tokens in all.
+ *   tok_off   [n_seqs+1] int32: row i's new tokens are tok_off[i] .. tok_off[i+1]-1.
+ *   slots     [max_tokens] int64: page * layout->page + place of token t; -1
+ *             behind the last token.
+ *   positions [max_tokens] int32: length of the prefix row after the call +
+ *             place in the row; -1 behind the last token.
+ *   workspace dopr_cache_extend_workspace(layout) bytes, 16-byte aligned.
+ * Device errors, which leave lengths, stack and tables as they were and give
+ * no token a slot (tok_off all 0): INVALID_ARG (a length, new length or prefix
+ * out of range, more than max_tokens new tokens, a position beyond 2^31 - 1),
+ * OUT_OF_MEMORY (not enough free pages).  A page number outside the pool on
+ * the stack or in a table is INVALID_ARG too; its tokens get slot -1.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_cache_extend(const dopr_cache_layout *layout, const int32_t *seq_lens, int32_t *block_tables,
+                                       int32_t *free_blocks, const int32_t *n_free, const int32_t *prefix,
+                                       const int32_t *new_lens, int32_t max_tokens, int32_t *seq_lens_out,
+                                       int32_t *n_free_out, int32_t *tok_off, int64_t *slots, int32_t *positions,
+                                       void *workspace, int32_t *status, void *cuda_stream);
+/* Bytes of its workspace; -1 on a bad layout. */
+DOPR_API int64_t dopr_cache_extend_workspace(const dopr_cache_layout *layout);
+
+/* Rotary positions (RoPE): element pairs (x_a, x_b) of a head become
+ *   (x_a cos - x_b sin, x_b cos + x_a sin), angle = position * f_i,
+ * over the first rotary_dim = d elements; the others pass unchanged.
+ * HALF pairs (i, i + d/2), INTERLEAVED pairs (2i, 2i + 1), i < d/2.
+ * Frequencies, f_i = theta^(-2i/d) where PLAIN:
+ *   LINEAR  f_i / factor;
+ *   NTK     base theta * factor^(d / (d-2));
+ *   BANDS   with turns n_i = original_max_position f_i / 2pi: f_i where n_i >= high,
+ *           f_i / factor where n_i <= low, blended linearly in n_i between;
+ *   RAMP    (YaRN, arXiv 2309.00071) f_i (1 - r_i) + f_i / factor r_i, r_i rising
+ *           linearly from 0 to 1 between the indices floor(c(high)) and
+ *           ceil(c(low)), c(n) = d ln(original_max_position / 2pi n) / (2 ln theta),
+ *           kept within [0, d-1]; cos and sin times attention_factor (0: 0.1 ln(factor) + 1).
+ */
+typedef enum { DOPR_ROPE_HALF = 0, DOPR_ROPE_INTERLEAVED = 1 } dopr_rope_layout;
+typedef enum {
+    DOPR_ROPE_PLAIN = 0, DOPR_ROPE_LINEAR = 1, DOPR_ROPE_NTK = 2, DOPR_ROPE_BANDS = 3, DOPR_ROPE_RAMP = 4
+} dopr_rope_scaling;
+typedef struct {
+    int32_t max_position;  /* positions 0 .. max_position - 1; at most 2^22      */
+    int32_t rotary_dim;    /* even, 2 .. 256 (NTK: at least 4)                   */
+    int32_t layout;
+    int32_t scaling;
+    double theta;          /* > 1                                                */
+    double factor;         /* >= 1 (PLAIN: not used)                             */
+    int32_t original_max_position;  /* BANDS, RAMP: > 0                          */
+    double low, high;      /* BANDS, RAMP: turns, 0 < low < high                 */
+    double attention_factor;        /* RAMP: >= 0                                */
+} dopr_rope_config;
+typedef struct dopr_rope dopr_rope;
+
+/* The table of cos and sin (angles and functions in 64 bits, entries rounded
+ * to 32) on the current device: 4 * rotary_dim * max_position bytes.
+ * Synchronous.  Errors: INVALID_ARG, UNSUPPORTED, OUT_OF_MEMORY, CUDA. */
+DOPR_API dopr_status dopr_rope_create(const dopr_rope_config *cfg, dopr_rope **out);
+/* NULL is accepted.  No call that uses it may be pending. */
+DOPR_API dopr_status dopr_rope_destroy(dopr_rope *rope);
+
+/* A [tokens][n_heads][head_dim] view: strides in elements, head_dim contiguous. */
+typedef struct {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+    int32_t n_heads;
+} dopr_heads;
+
+/*
+ * q_out = rotated q, k_out = rotated k (k, k_out NULL: q alone), of dtype F16,
+ * BF16 or F32, computed in 32 bits and rounded once.  An output may be its
+ * input; otherwise outputs overlap nothing.  inverse != 0 turns back (angle
+ * -position f_i, the same attention_factor): the gradient of the rotation,
+ * from that of its output.  Rows with positions[t] < 0 are left as they were.
+ * head_dim even, rotary_dim <= head_dim <= 256.  Aligned views (data and
+ * strides multiples of 16 bytes) are faster.
+ * Device error: INVALID_ARG (a position >= max_position; its row is left).
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_rope_apply(const dopr_rope *rope, int32_t dtype, int32_t head_dim, int32_t n_tokens,
+                                     const int32_t *positions, const dopr_heads *q, const dopr_heads *q_out,
+                                     const dopr_heads *k, const dopr_heads *k_out, int32_t inverse, int32_t *status,
+                                     void *cuda_stream);
+
+/*
+ * One layer's new rows: k (rotated) and v into the pages at slots[t], and
+ * q_out = rotated q (q, q_out NULL: keys and values alone).  rope NULL: k is
+ * stored as it is, positions is not read, and q must be NULL.  Rows with
+ * slots[t] < 0 are not stored; with positions[t] < 0 nothing of a row is
+ * written.  Slots are distinct.  Device error: INVALID_ARG (a slot outside the
+ * pool, a position >= max_position; that row is left).
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_cache_append(const dopr_cache_layout *layout, const dopr_rope *rope, int32_t n_tokens,
+                                       const int32_t *positions, const int64_t *slots, const dopr_heads *q,
+                                       const dopr_heads *q_out, const dopr_heads *k, const dopr_heads *v, void *k_pool,
+                                       void *v_pool, int32_t *status, void *cuda_stream);
+
+/*
+ * How the attention of a step's tokens is split over the device: made once a
+ * step, used by every layer.  tok_off, seq_lens (after dopr_cache_extend) and
+ * prefix as there; tokens tok_off[n_seqs] .. max_tokens - 1 are behind the last.
+ *   plan  dopr_shared_attention_plan_bytes(...) bytes, 16-byte aligned.
+ * 1 <= n_q_heads / n_kv_heads <= 64, a whole number.
+ * Device error: INVALID_ARG (offsets, a length or a prefix out of range); the
+ * plan is then empty, and attention writes nothing.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_shared_attention_plan(const dopr_cache_layout *layout, int32_t n_q_heads, int32_t max_tokens,
+                                                const int32_t *tok_off, const int32_t *seq_lens, const int32_t *prefix,
+                                                void *plan, int32_t *status, void *cuda_stream);
+DOPR_API int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout *layout, int32_t n_q_heads,
+                                                  int32_t max_tokens);
+
+/*
+ * out = softmax(scale q k^T) v for every token of the plan: token j of row i's
+ * n_i tokens sees all seq_lens[prefix[i]] keys of the prefix and the row's own
+ * keys 0 .. seq_lens[i] - n_i + j.  Rows that share a prefix read its pages
+ * together, whatever their order; long keys are split and joined.  q head h
+ * reads kv head h / (n_q_heads / n_kv_heads).
+ *   q, out   views of layout->dtype, 16-byte aligned with strides multiples of
+ *            16 bytes; out overlaps nothing.  Rows behind the last token are
+ *            left as they were.
+ *   lse      [max_tokens][n_q_heads] float or NULL: log of the sum of exponentials
+ *            (natural).  A row that sees no key gives zeros and -infinity.
+ *   workspace dopr_shared_attention_workspace(...) bytes, 16-byte aligned.
+ * Keys and values past a row's end are never used, whatever the pages hold there.
+ * Products take dtype operands with 32-bit sums; probabilities are rounded to
+ * dtype, statistics and sums are 32-bit.  A row's bits depend on the plan.
+ * Device errors: INVALID_ARG (a page number outside the pool: page 0 is read
+ * for it), TIMEOUT.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_shared_attention(const dopr_cache_layout *layout, const void *plan, int32_t max_tokens,
+                                           const dopr_heads *q, const void *k_pool, const void *v_pool,
+                                           const int32_t *block_tables, float scale, const dopr_heads *out, float *lse,
+                                           void *workspace, int32_t *status, void *cuda_stream);
+DOPR_API int64_t dopr_shared_attention_workspace(const dopr_cache_layout *layout, int32_t n_q_heads,
+                                                 int32_t max_tokens);
+
+/*
  * Per-kernel accounting, for measurement.  Every dopr_score call counts its
  * kernel launches per kernel family (pack, embed, gemm_qkv, qknorm_rope,
  * attention, gemm_o, rmsnorm, gemm_gate_up, gemm_down, score, prefix_store;

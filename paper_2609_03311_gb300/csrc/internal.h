@@ -422,6 +422,89 @@ cudaError_t launch_pack_tokens(const PackArgs& a, cudaStream_t st);
 // out[0, n) = scores[0, n) unless the call's error word is set.
 cudaError_t launch_commit_scores(const int* err, const float* scores, float* out, int n, cudaStream_t st);
 
+// ---------------------------------------------------- paged prefix cache
+// Largest n_seqs of a cache layout: what the one-CTA kernels over a step's rows sort in shared memory.
+constexpr int CACHE_MAX_SEQS = 16384;
+struct CacheExtendArgs {
+  dopr_cache_layout lay;
+  const int32_t* seq_lens;
+  int32_t* tables;
+  int32_t* free_blocks;
+  const int32_t* n_free;
+  const int32_t* prefix;
+  const int32_t* new_lens;
+  int32_t max_tokens;
+  int32_t* seq_lens_out;
+  int32_t* n_free_out;
+  int32_t* tok_off;
+  int64_t* slots;
+  int32_t* positions;
+  int32_t* ws;  // CACHE_WS_HEAD ints, then three ints a row
+  int32_t* status;
+};
+constexpr int CACHE_WS_HEAD = 16;
+cudaError_t launch_cache_extend(const CacheExtendArgs& a, cudaStream_t st);
+
+// A rotary table: entry [position][i] = (cos, sin) of position * f_i.
+struct Rope {
+  dopr_rope_config cfg{};
+  int device = 0;
+  float2* table = nullptr;
+};
+// freq: device, rotary_dim / 2 doubles.
+cudaError_t launch_rope_table(const double* freq, double gain, int max_position, int half, float2* table,
+                              cudaStream_t st);
+// A view's row of heads and where it goes.
+struct RopeView {
+  const void* in;
+  void* out;
+  int64_t in_tok, in_head, out_tok, out_head;  // strides in elements
+  int n_heads;                                 // 0: no such view
+};
+struct RopeArgs {
+  int n_tokens, head_dim, rotary;  // rotary 0: nothing turns
+  bool interleaved, inverse;
+  const float2* table;
+  int max_position;
+  const int32_t* positions;
+  RopeView q, k;
+  // the cache: keys and values go to the pages at slots[t] instead (slots null: no cache, k like q)
+  RopeView v;  // in only
+  const int64_t* slots;
+  void *k_pool, *v_pool;
+  int page;
+  int64_t n_slots;
+  int32_t* status;
+};
+cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st);
+
+struct SharedAttnArgs {
+  dopr_cache_layout lay;
+  int Hq, max_tokens;
+  const void* plan;
+  const void* q;
+  int64_t q_tok, q_head;
+  const void *k_pool, *v_pool;
+  const int32_t* tables;
+  float scale;
+  void* out;
+  int64_t o_tok, o_head;
+  float* lse;
+  uint8_t* ws;
+  int32_t* status;
+};
+struct SharedPlanArgs {
+  dopr_cache_layout lay;
+  int Hq, max_tokens;
+  const int32_t *tok_off, *seq_lens, *prefix;
+  int32_t* plan;
+  int32_t* status;
+};
+int64_t shared_plan_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens);
+int64_t shared_workspace_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens, int num_sms);
+cudaError_t launch_shared_plan(const SharedPlanArgs& a, cudaStream_t st);
+cudaError_t launch_shared_attention(const SharedAttnArgs& a, cudaStream_t st);
+
 // Sets the message dopr_last_error() returns on this thread.
 void set_last_error_message(const std::string& msg);
 

@@ -1,0 +1,173 @@
+// k_rope.cu -- rotary positions on packed rows of heads (dopr_rope_apply), and the same with keys and values on
+// their way into the cache's pages (dopr_cache_append).
+//
+// A pair of elements is a point in the plane that turns by position * f_i.  Far positions times a frequency lose
+// their angle in 32 bits (at 250,000 radians a step is 0.016), so angles and their cos and sin are taken in 64 bits,
+// once, into a table; what is left for a row is four products of 32 bits a pair.
+//
+// Bound by HBM: a row is read once and written once, 24 KB of 16-bit q, k and v for 32 + 2 x 8 heads of 128.  A
+// thread takes one unit of 2 x VEC elements (16 bytes of each half of the pairs; 32 contiguous bytes where pairs are
+// interleaved) and walks over the heads with it, so that it reads its cos and sin once a row.
+#include <type_traits>
+
+#include "device_common.cuh"
+#include "internal.h"
+
+namespace dopr {
+namespace {
+
+constexpr int ROPE_THREADS = 128;
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T x) {
+  if constexpr (std::is_same_v<T, float>) return x;
+  else if constexpr (std::is_same_v<T, __half>) return __half2float(x);
+  else return __bfloat162float(x);
+}
+template <typename T>
+__device__ __forceinline__ T from_f32(float x) {
+  if constexpr (std::is_same_v<T, float>) return x;
+  else if constexpr (std::is_same_v<T, __half>) return __float2half_rn(x);
+  else return __float2bfloat16_rn(x);
+}
+
+// VEC elements, 16 bytes of them at once where VEC > 1.
+template <typename T, int VEC>
+struct alignas(VEC > 1 ? 16 : sizeof(T)) Pack {
+  T v[VEC];
+};
+
+__global__ void __launch_bounds__(256) k_rope_table(const double* freq, double gain, int max_position, int half,
+                                                    float2* table) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= static_cast<int64_t>(max_position) * half) return;
+  double s, c;
+  sincos(static_cast<double>(i / half) * freq[i % half], &s, &c);
+  table[i] = make_float2(static_cast<float>(c * gain), static_cast<float>(s * gain));
+}
+
+// (x, y) turned.  The fused steps are spelled out so that every variant gives the same bits.
+template <typename T>
+__device__ __forceinline__ void turn_pair(T& a, T& b, float c, float s) {
+  const float x = to_f32(a), y = to_f32(b);
+  a = from_f32<T>(__fmaf_rn(x, c, -__fmul_rn(y, s)));
+  b = from_f32<T>(__fmaf_rn(y, c, __fmul_rn(x, s)));
+}
+
+// One unit of one head: elements a[] and b[], VEC each, at offsets ia and ib of the head.
+template <typename T, int VEC, bool INTER>
+__device__ __forceinline__ void turn(Pack<T, VEC>& a, Pack<T, VEC>& b, const float (&c)[VEC], const float (&s)[VEC]) {
+  if constexpr (INTER && VEC > 1) {
+    // pairs (2i, 2i + 1) lie in order over a, then b
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) {
+      turn_pair(a.v[2 * i], a.v[2 * i + 1], c[i], s[i]);
+      turn_pair(b.v[2 * i], b.v[2 * i + 1], c[VEC / 2 + i], s[VEC / 2 + i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) turn_pair(a.v[i], b.v[i], c[i], s[i]);
+  }
+}
+
+template <typename T, int VEC, bool INTER>
+__global__ void __launch_bounds__(ROPE_THREADS) k_rope(RopeArgs a) {
+  const int units = a.head_dim / (2 * VEC), turning = a.rotary / (2 * VEC);
+  const int lanes = ROPE_THREADS / units;  // heads at once
+  const int u = threadIdx.x % units, h0 = threadIdx.x / units;
+  // unit u's two runs of VEC elements
+  const int ia = u < turning && !INTER ? u * VEC : u * 2 * VEC;
+  const int ib = u < turning && !INTER ? ia + a.rotary / 2 : ia + VEC;
+  const int heads = a.q.n_heads + a.k.n_heads + a.v.n_heads;
+  pdl_wait();
+  pdl_trigger();
+  if (h0 >= lanes) return;
+  for (int t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
+    float c[VEC], s[VEC];
+    if (a.rotary > 0) {
+      const int pos = a.positions[t];
+      if (pos < 0) continue;
+      if (pos >= a.max_position) {
+        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+        continue;
+      }
+      if (u < turning) {
+        const float2* cs = a.table + static_cast<int64_t>(pos) * (a.rotary / 2) + u * VEC;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          const float2 e = __ldg(cs + i);
+          c[i] = e.x;
+          s[i] = a.inverse ? -e.y : e.y;
+        }
+      }
+    }
+    int64_t slot = -1;
+    if (a.slots) {
+      slot = a.slots[t];
+      if (slot >= a.n_slots) {
+        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+        continue;
+      }
+    }
+    for (int h = h0; h < heads; h += lanes) {
+      const bool is_q = h < a.q.n_heads, is_v = h >= a.q.n_heads + a.k.n_heads;
+      if (!is_q && a.slots && slot < 0) break;  // the row is not stored; heads go up
+      const RopeView& view = is_q ? a.q : is_v ? a.v : a.k;
+      const int hh = is_q ? h : is_v ? h - a.q.n_heads - a.k.n_heads : h - a.q.n_heads;
+      const T* x = static_cast<const T*>(view.in) + t * view.in_tok + hh * view.in_head;
+      T* y;
+      if (is_q || !a.slots) {
+        y = static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head;
+      } else {
+        const int64_t row = (slot / a.page * a.k.n_heads + hh) * a.page + slot % a.page;
+        y = static_cast<T*>(is_v ? a.v_pool : a.k_pool) + row * a.head_dim;
+      }
+      Pack<T, VEC> p0 = *reinterpret_cast<const Pack<T, VEC>*>(x + ia);
+      Pack<T, VEC> p1 = *reinterpret_cast<const Pack<T, VEC>*>(x + ib);
+      if (u < turning && !is_v) turn<T, VEC, INTER>(p0, p1, c, s);
+      *reinterpret_cast<Pack<T, VEC>*>(y + ia) = p0;
+      *reinterpret_cast<Pack<T, VEC>*>(y + ib) = p1;
+    }
+  }
+}
+
+bool aligned16(const void* p, int64_t s0, int64_t s1, int size) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s0 * size % 16 == 0 && s1 * size % 16 == 0;
+}
+
+template <typename T, int VEC, bool INTER>
+cudaError_t launch(const RopeArgs& a, cudaStream_t st) {
+  return launch_dependent(k_rope<T, VEC, INTER>, dim3(a.n_tokens < 65536 ? a.n_tokens : 65536), ROPE_THREADS, 0, st, a);
+}
+template <typename T>
+cudaError_t launch_type(const RopeArgs& a, cudaStream_t st) {
+  constexpr int VEC = 16 / sizeof(T);
+  bool wide = a.rotary / 2 % VEC == 0 && (a.head_dim - a.rotary) % (2 * VEC) == 0;
+  for (const RopeView* v : {&a.q, &a.k, &a.v}) {
+    if (v->n_heads == 0) continue;
+    wide = wide && aligned16(v->in, v->in_tok, v->in_head, sizeof(T));
+    if (v->out) wide = wide && aligned16(v->out, v->out_tok, v->out_head, sizeof(T));
+  }
+  if (wide) return a.interleaved ? launch<T, VEC, true>(a, st) : launch<T, VEC, false>(a, st);
+  return a.interleaved ? launch<T, 1, true>(a, st) : launch<T, 1, false>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_rope_table(const double* freq, double gain, int max_position, int half, float2* table,
+                              cudaStream_t st) {
+  const int64_t n = static_cast<int64_t>(max_position) * half;
+  k_rope_table<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(freq, gain, max_position, half, table);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st) {
+  if (a.n_tokens == 0) return cudaSuccess;
+  switch (dtype) {
+    case DOPR_F16: return launch_type<__half>(a, st);
+    case DOPR_BF16: return launch_type<__nv_bfloat16>(a, st);
+    default: return launch_type<float>(a, st);
+  }
+}
+
+}  // namespace dopr

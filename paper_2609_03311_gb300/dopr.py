@@ -82,6 +82,16 @@ def load():
         "dopr_debug_attention_plan": ([i32, i32, i32, P, i32, P], i32),
         "dopr_select_prefix_inputs": ([P, i32, P, P, i32, i32, P, P, P, P], i32),
         "dopr_model_set_mlp_head": ([P, i32, i32, P, P, P, ctypes.c_float, i32], i32),
+        "dopr_cache_extend": ([P] * 7 + [i32] + [P] * 8, i32),
+        "dopr_cache_extend_workspace": ([P], i64),
+        "dopr_rope_create": ([P, P], i32),
+        "dopr_rope_destroy": ([P], i32),
+        "dopr_rope_apply": ([P, i32, i32, i32, P, P, P, P, P, i32, P, P], i32),
+        "dopr_cache_append": ([P, P, i32] + [P] * 10, i32),
+        "dopr_shared_attention_plan": ([P, i32, i32] + [P] * 6, i32),
+        "dopr_shared_attention_plan_bytes": ([P, i32, i32], i64),
+        "dopr_shared_attention": ([P, P, i32, P, P, P, P, ctypes.c_float] + [P] * 5, i32),
+        "dopr_shared_attention_workspace": ([P, i32, i32], i64),
         "dopr_last_error": ([], ctypes.c_char_p),
         "dopr_version": ([], ctypes.c_char_p),
     }
@@ -345,6 +355,244 @@ def pack_order_noalloc(store: Store, q_offsets: torch.Tensor, doc_ids: torch.Ten
     st = ctypes.c_void_p(stream.cuda_stream if stream is not None else torch.cuda.current_stream().cuda_stream)
     _check(load().dopr_pack_order_noalloc(store._h, n, _ptr(q_offsets), _ptr(doc_ids), _ptr(perm), _ptr(tok_off),
                                           st))
+
+
+# ------------------------------------------------------------------ paged prefix cache
+# Every call below runs on the tensors' device, on `stream` (default: that device's current stream), and returns once
+# its work is queued.  `status`: an int32 tensor of one element that keeps the first device error (a status number).
+
+class CacheLayout(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "page", "n_kv_heads", "head_dim", "dtype", "n_seqs",
+                                              "max_blocks")]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32)]
+
+
+class RopeConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("max_position", "rotary_dim", "layout", "scaling")] + \
+               [("theta", ctypes.c_double), ("factor", ctypes.c_double), ("original_max_position", ctypes.c_int32),
+                ("low", ctypes.c_double), ("high", ctypes.c_double), ("attention_factor", ctypes.c_double)]
+
+
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_RAMP = range(5)
+_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_TORCH_TYPES = (torch.float16, torch.bfloat16, torch.float32)
+
+
+class _On:
+    """The device of the call's tensors and the stream made current, where they are not, so that what the call
+    allocates belongs to the stream that uses it; enters as the stream's handle."""
+
+    def __init__(self, device, stream):
+        if device.type != "cuda":
+            raise ValueError(f"the paged cache's calls take CUDA tensors, got one on {device}")
+        if stream is not None and stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+        if stream is not None:
+            self.guard = torch.cuda.stream(stream)
+        else:
+            self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+            stream = torch.cuda.current_stream(device)
+        self.stream = stream.cuda_stream
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return self.stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _buf(name, t, dtype, n, device):
+    """Pointer of a contiguous tensor of at least n elements; None passes NULL."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: need {n} contiguous {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _heads(name, t, tokens, head_dim, dtype, device):
+    """A [tokens, heads, head_dim] tensor as the C ABI's view (strided, the last dimension contiguous)."""
+    if t is None:
+        return None
+    if t.dim() != 3 or t.shape[0] < tokens or t.shape[2] != head_dim or t.dtype != dtype or t.device != device or \
+            (head_dim > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on {device} with a contiguous last dimension, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
+    return ctypes.byref(Heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1]))
+
+
+def make_cache_layout(n_blocks: int, page: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seqs: int,
+                      max_blocks: int) -> CacheLayout:
+    """Pools of one layer's keys and values [n_blocks, n_kv_heads, page, head_dim] and tables [n_seqs, max_blocks]."""
+    return CacheLayout(n_blocks, page, n_kv_heads, head_dim, _DTYPES[dtype], n_seqs, max_blocks)
+
+
+class CacheBatch:
+    """A step's new tokens: tok_off [n_seqs + 1], slots and positions [max_tokens], seq_lens [n_seqs] and n_free [1]
+    after the step.  For a cache that is updated in place set seq_lens and n_free to the cache's own tensors."""
+
+    def __init__(self, layout: CacheLayout, max_tokens: int, device):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.max_tokens = max_tokens
+        self.tok_off = torch.empty(layout.n_seqs + 1, **i32)
+        self.slots = torch.empty(max_tokens, dtype=torch.int64, device=device)
+        self.positions = torch.empty(max_tokens, **i32)
+        self.seq_lens = torch.empty(layout.n_seqs, **i32)
+        self.n_free = torch.empty(1, **i32)
+        n = load().dopr_cache_extend_workspace(ctypes.byref(layout))
+        if n < 0:
+            raise DoprError(ERR_INVALID_ARG, load().dopr_last_error().decode())
+        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def cache_batch(layout: CacheLayout, max_tokens: int, device="cuda") -> CacheBatch:
+    return CacheBatch(layout, max_tokens, device)
+
+
+def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_free, new_lens, max_tokens: int, prefix=None,
+                 out: CacheBatch | None = None, status=None, stream=None) -> CacheBatch:
+    """Pages, slots and positions for every row's new tokens (new_lens -1: the row is released), on the device.
+    block_tables and free_blocks are updated in place, lengths and the stack's height in `out`."""
+    dev = seq_lens.device
+    n, i32 = layout.n_seqs, torch.int32
+    with _On(dev, stream) as st:
+        if out is None:
+            out = CacheBatch(layout, max_tokens, dev)
+        _check(load().dopr_cache_extend(
+            ctypes.byref(layout), _buf("seq_lens", seq_lens, i32, n, dev),
+            _buf("block_tables", block_tables, i32, n * layout.max_blocks, dev),
+            _buf("free_blocks", free_blocks, i32, layout.n_blocks, dev), _buf("n_free", n_free, i32, 1, dev),
+            _buf("prefix", prefix, i32, n, dev), _buf("new_lens", new_lens, i32, n, dev), max_tokens,
+            _buf("out.seq_lens", out.seq_lens, i32, n, dev), _buf("out.n_free", out.n_free, i32, 1, dev),
+            _buf("out.tok_off", out.tok_off, i32, n + 1, dev), _buf("out.slots", out.slots, torch.int64, max_tokens, dev),
+            _buf("out.positions", out.positions, i32, max_tokens, dev),
+            _buf("out.workspace", out.workspace, torch.uint8, 0, dev), _buf("status", status, i32, 1, dev), st))
+    return out
+
+
+class Rope:
+    """Rotary positions 0 .. max_position - 1 over the first rotary_dim elements of a head: a table on the current
+    device.  scaling and its arguments as in include/dopr.h."""
+
+    def __init__(self, max_position: int, rotary_dim: int, theta: float = 1e6, layout: int = ROPE_HALF,
+                 scaling: int = ROPE_PLAIN, factor: float = 1.0, original_max_position: int = 0, low: float = 1.0,
+                 high: float = 32.0, attention_factor: float = 0.0):
+        self.cfg = RopeConfig(max_position, rotary_dim, layout, scaling, theta, factor, original_max_position, low, high,
+                              attention_factor)
+        self._h = ctypes.c_void_p()
+        _check(load().dopr_rope_create(ctypes.byref(self.cfg), ctypes.byref(self._h)))
+
+    def close(self):
+        if self._h:
+            load().dopr_rope_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False, status=None, stream=None):
+    """Rotary positions on q and, with it, k: [tokens, heads, head_dim] views of float16, bfloat16 or float32.  Returns
+    (q_out, k_out); pass q_out=q, k_out=k to work in place.  inverse: the gradient of the rotation."""
+    T, D, dt, dev = q.shape[0], q.shape[2], q.dtype, q.device
+    if dt not in _DTYPES:
+        raise ValueError(f"rope_apply: float16, bfloat16 or float32, got {dt}")
+    with _On(dev, stream) as st:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        _check(load().dopr_rope_apply(
+            rope._h, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, dev), _heads("q", q, T, D, dt, dev),
+            _heads("q_out", q_out, T, D, dt, dev), _heads("k", k, T, D, dt, dev),
+            _heads("k_out", k_out if k is not None else None, T, D, dt, dev), int(inverse),
+            _buf("status", status, torch.int32, 1, dev), st))
+    return q_out, k_out
+
+
+def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | None = None, positions=None, q=None,
+                 q_out=None, status=None, stream=None):
+    """One layer's new rows k (rotated) and v [tokens, kv heads, head_dim] into the pages at slots; returns rotated q
+    where q is given."""
+    T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
+    pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
+    with _On(dev, stream) as st:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        _check(load().dopr_cache_append(
+            ctypes.byref(layout), rope._h if rope is not None else None, T,
+            _buf("positions", positions, torch.int32, T, dev), _buf("slots", slots, torch.int64, T, dev),
+            _heads("q", q, T, D, dt, dev), _heads("q_out", q_out if q is not None else None, T, D, dt, dev),
+            _heads("k", k, T, D, dt, dev), _heads("v", v, T, D, dt, dev), _buf("k_pool", k_pool, dt, pool, dev),
+            _buf("v_pool", v_pool, dt, pool, dev), _buf("status", status, torch.int32, 1, dev), st))
+    return q_out
+
+
+def _sized(fn, layout, n_q_heads, max_tokens):
+    n = fn(ctypes.byref(layout), n_q_heads, max_tokens)
+    if n < 0:
+        raise DoprError(ERR_INVALID_ARG, load().dopr_last_error().decode())
+    return n
+
+
+def shared_attention_plan(layout: CacheLayout, n_q_heads: int, tok_off, seq_lens, prefix, max_tokens: int, plan=None,
+                          status=None, stream=None) -> torch.Tensor:
+    """How a step's attention is split: made once a step, used by every layer (of these sizes, on this device)."""
+    dev = seq_lens.device
+    n = layout.n_seqs
+    with _On(dev, stream) as st:
+        need = _sized(load().dopr_shared_attention_plan_bytes, layout, n_q_heads, max_tokens)
+        if plan is None:
+            plan = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(load().dopr_shared_attention_plan(
+            ctypes.byref(layout), n_q_heads, max_tokens, _buf("tok_off", tok_off, torch.int32, n + 1, dev),
+            _buf("seq_lens", seq_lens, torch.int32, n, dev), _buf("prefix", prefix, torch.int32, n, dev),
+            _buf("plan", plan, torch.uint8, need, dev), _buf("status", status, torch.int32, 1, dev), st))
+    return plan
+
+
+def shared_attention_workspace(layout: CacheLayout, n_q_heads: int, max_tokens: int, device="cuda") -> torch.Tensor:
+    with torch.cuda.device(device):
+        n = _sized(load().dopr_shared_attention_workspace, layout, n_q_heads, max_tokens)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None,
+                     lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """Attention of q [max_tokens, q heads, head_dim], the plan's tokens, over their rows' prefixes and own keys.  lse:
+    float32 [max_tokens, q heads] to fill, or None."""
+    T, hq, D = q.shape
+    dt, dev = _TORCH_TYPES[layout.dtype], q.device
+    if scale is None:
+        scale = D ** -0.5
+    pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
+    lib = load()
+    with _On(dev, stream) as st:
+        if out is None:
+            out = torch.empty((T, hq, D), dtype=dt, device=dev)
+        need = _sized(lib.dopr_shared_attention_workspace, layout, hq, T)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(lib.dopr_shared_attention(
+            ctypes.byref(layout),
+            _buf("plan", plan, torch.uint8, _sized(lib.dopr_shared_attention_plan_bytes, layout, hq, T), dev), T,
+            _heads("q", q, T, layout.head_dim, dt, dev), _buf("k_pool", k_pool, dt, pool, dev),
+            _buf("v_pool", v_pool, dt, pool, dev),
+            _buf("block_tables", block_tables, torch.int32, layout.n_seqs * layout.max_blocks, dev), scale,
+            _heads("out", out, T, layout.head_dim, dt, dev), _buf("lse", lse, torch.float32, T * hq, dev),
+            _buf("workspace", workspace, torch.uint8, need, dev), _buf("status", status, torch.int32, 1, dev), st))
+    return out
 
 
 def profile_enable(model: Model, on: bool = True):

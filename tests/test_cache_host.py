@@ -1,0 +1,140 @@
+"""Refusals of the paged prefix cache's C entry points: host arguments are checked before any device work, so none of
+these needs a GPU (device pointers are never followed)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2609_03311_gb300 import build as libbuild
+from paper_2609_03311_gb300 import dopr
+
+P = ctypes.c_void_p(4096)  # stands for a device buffer
+
+
+@pytest.fixture(scope="module")
+def lib():
+    libbuild.build()
+    return dopr.load()
+
+
+def layout(**kw):
+    a = dict(n_blocks=8, page=64, n_kv_heads=2, head_dim=128, dtype=torch.bfloat16, n_seqs=3, max_blocks=4)
+    a.update(kw)
+    return dopr.make_cache_layout(**a)
+
+
+def heads(data=4096, tok=512, head=128, n=4):
+    return ctypes.byref(dopr.Heads(data, tok, head, n))
+
+
+BAD_LAYOUTS = [(dict(n_blocks=0), dopr.ERR_INVALID_ARG), (dict(n_kv_heads=-1), dopr.ERR_INVALID_ARG),
+               (dict(n_seqs=0), dopr.ERR_INVALID_ARG), (dict(max_blocks=0), dopr.ERR_INVALID_ARG),
+               (dict(page=48), dopr.ERR_UNSUPPORTED), (dict(page=256), dopr.ERR_UNSUPPORTED),
+               (dict(head_dim=96), dopr.ERR_UNSUPPORTED), (dict(dtype=torch.float32), dopr.ERR_UNSUPPORTED),
+               (dict(n_seqs=16385), dopr.ERR_UNSUPPORTED), (dict(max_blocks=2 ** 26, page=64), dopr.ERR_UNSUPPORTED),
+               (dict(n_blocks=2 ** 26, page=32), dopr.ERR_UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("kw,status", BAD_LAYOUTS)
+def test_bad_layouts_are_refused_by_every_call(lib, kw, status):
+    l = ctypes.byref(layout(**kw))
+    assert lib.dopr_cache_extend_workspace(l) == -1
+    assert lib.dopr_shared_attention_plan_bytes(l, 8, 4) == -1
+    assert lib.dopr_shared_attention_workspace(l, 8, 4) == -1
+    assert lib.dopr_cache_extend(l, P, P, P, P, None, P, 4, P, P, P, P, P, P, None, None) == status
+    assert lib.dopr_cache_append(l, None, 1, None, P, None, None, heads(n=2), heads(n=2), P, P, None, None) == status
+    assert lib.dopr_shared_attention_plan(l, 8, 4, P, P, None, P, None, None) == status
+    assert lib.dopr_shared_attention(l, P, 4, heads(), P, P, P, 0.1, heads(), None, P, None, None) == status
+    assert lib.dopr_last_error()
+
+
+def test_null_layouts_and_pointers_are_refused(lib):
+    assert lib.dopr_cache_extend_workspace(None) == -1
+    l = ctypes.byref(layout())
+    good = [l, P, P, P, P, None, P, 4, P, P, P, P, P, P, None, None]
+    for i in (0, 1, 2, 3, 4, 6, 8, 9, 10, 11, 12, 13):
+        a = list(good)
+        a[i] = None
+        assert lib.dopr_cache_extend(*a) == dopr.ERR_INVALID_ARG, i
+    a = list(good)
+    a[7] = -1
+    assert lib.dopr_cache_extend(*a) == dopr.ERR_INVALID_ARG
+    a = list(good)
+    a[13] = ctypes.c_void_p(4100)  # the workspace, not 16-byte aligned
+    assert lib.dopr_cache_extend(*a) == dopr.ERR_INVALID_ARG
+    for i in (3, 4, 6):
+        a = [l, 8, 4, P, P, None, P, None, None]
+        a[i] = None
+        assert lib.dopr_shared_attention_plan(*a) == dopr.ERR_INVALID_ARG, i
+    for i in (1, 3, 4, 5, 6, 8, 10):
+        a = [l, P, 4, heads(), P, P, P, 0.1, heads(), None, P, None, None]
+        a[i] = None
+        assert lib.dopr_shared_attention(*a) == dopr.ERR_INVALID_ARG, i
+    for i in (4, 7, 8, 9, 10):
+        a = [l, None, 1, None, P, None, None, heads(n=2), heads(n=2), P, P, None, None]
+        a[i] = None
+        assert lib.dopr_cache_append(*a) == dopr.ERR_INVALID_ARG, i
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(q=heads(n=3)), dopr.ERR_UNSUPPORTED),            # 3 q heads on 2 kv heads
+    (dict(q=heads(n=2 * 65)), dopr.ERR_UNSUPPORTED),       # 65 q heads a kv head
+    (dict(out=heads(n=2)), dopr.ERR_INVALID_ARG),          # heads differ
+    (dict(q=heads(data=4104)), dopr.ERR_INVALID_ARG),      # 8-byte aligned
+    (dict(q=heads(tok=516)), dopr.ERR_INVALID_ARG),        # a stride of 1,032 bytes
+    (dict(out=heads(head=64)), dopr.ERR_INVALID_ARG),      # heads overlap
+    (dict(out=heads(tok=-512)), dopr.ERR_INVALID_ARG),
+    (dict(scale=0.0), dopr.ERR_INVALID_ARG),
+    (dict(scale=float("nan")), dopr.ERR_INVALID_ARG),
+    (dict(scale=float("inf")), dopr.ERR_INVALID_ARG),
+    (dict(pool=ctypes.c_void_p(4104)), dopr.ERR_INVALID_ARG),
+    (dict(tokens=-1), dopr.ERR_INVALID_ARG),
+    (dict(tokens=2 ** 30), dopr.ERR_UNSUPPORTED),
+])
+def test_bad_attention_arguments_are_refused(lib, bad, status):
+    a = dict(q=heads(), out=heads(), scale=0.1, pool=P, tokens=4)
+    a.update(bad)
+    assert lib.dopr_shared_attention(ctypes.byref(layout()), P, a["tokens"], a["q"], a["pool"], P, P, a["scale"], a["out"],
+                                     None, P, None, None) == status
+    assert lib.dopr_last_error()
+
+
+@pytest.mark.parametrize("bad,status", [
+    (dict(max_position=0), dopr.ERR_INVALID_ARG), (dict(rotary_dim=0), dopr.ERR_INVALID_ARG),
+    (dict(rotary_dim=63), dopr.ERR_UNSUPPORTED), (dict(rotary_dim=258), dopr.ERR_UNSUPPORTED),
+    (dict(max_position=2 ** 22 + 1), dopr.ERR_UNSUPPORTED), (dict(layout=2), dopr.ERR_INVALID_ARG),
+    (dict(scaling=5), dopr.ERR_INVALID_ARG), (dict(theta=1.0), dopr.ERR_INVALID_ARG),
+    (dict(theta=float("nan")), dopr.ERR_INVALID_ARG), (dict(scaling=1, factor=0.5), dopr.ERR_INVALID_ARG),
+    (dict(scaling=2, factor=float("inf")), dopr.ERR_INVALID_ARG),
+    (dict(scaling=2, factor=2.0, rotary_dim=2), dopr.ERR_INVALID_ARG),
+    (dict(scaling=3, factor=2.0), dopr.ERR_INVALID_ARG),  # no original_max_position
+    (dict(scaling=4, factor=2.0, original_max_position=100, low=4.0, high=1.0), dopr.ERR_INVALID_ARG),
+    (dict(scaling=4, factor=2.0, original_max_position=100, attention_factor=-1.0), dopr.ERR_INVALID_ARG),
+])
+def test_bad_rotary_tables_are_refused(lib, bad, status):
+    a = dict(max_position=16, rotary_dim=64)
+    a.update(bad)
+    with pytest.raises(dopr.DoprError) as e:
+        dopr.Rope(**a)
+    assert e.value.status == status
+    assert lib.dopr_rope_create(None, ctypes.byref(ctypes.c_void_p())) == dopr.ERR_INVALID_ARG
+    assert lib.dopr_rope_create(ctypes.byref(dopr.RopeConfig()), None) == dopr.ERR_INVALID_ARG
+    assert lib.dopr_rope_destroy(None) == dopr.OK
+
+
+def test_the_binding_takes_device_tensors_only(lib):
+    l = layout()
+    z = torch.zeros(64, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        dopr.cache_extend(l, z, z, z, z, z, 4)
+    with pytest.raises(ValueError):
+        dopr.shared_attention_plan(l, 8, z, z, z, 4)
+    with pytest.raises(ValueError):
+        dopr.shared_attention(l, z, torch.zeros(4, 4, 128, dtype=torch.bfloat16), z, z, z)
+
+
+def test_workspace_and_plan_sizes_grow_with_their_work(lib):
+    l = ctypes.byref(layout())
+    assert lib.dopr_cache_extend_workspace(l) >= 3 * 3 * 4
+    sizes = [lib.dopr_shared_attention_plan_bytes(l, 8, t) for t in (0, 1, 64, 1000)]
+    assert sizes == sorted(sizes) and sizes[0] > 0

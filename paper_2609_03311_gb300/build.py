@@ -26,8 +26,8 @@ LIB = os.path.join(BUILD, "libdopr.so")
 BUILD_CHECKED = os.path.join(HERE, "_build_checked")
 LIB_CHECKED = os.path.join(BUILD_CHECKED, "libdopr.so")
 SOURCES = ["abi.cu", "k_gemm.cu", "k_attn.cu", "k_attn_tc.cu", "k_select.cu", "k_rows.cu", "k_pack.cu", "k_pack_noalloc.cu",
-           "abi_cache.cu", "k_cache.cu", "k_rope.cu", "k_shared_attn.cu"]
-HEADERS = [os.path.join(CSRC, "device_common.cuh"), os.path.join(CSRC, "internal.h"),
+           "abi_cache.cu", "k_cache.cu", "k_rope.cu", "k_shared_plan.cu", "k_shared_attn.cu"]
+HEADERS = [os.path.join(CSRC, "device_common.cuh"), os.path.join(CSRC, "internal.h"), os.path.join(CSRC, "shared_attn.cuh"),
            os.path.join(ROOT, "include", "dopr.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",

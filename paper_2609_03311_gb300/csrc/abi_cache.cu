@@ -327,7 +327,9 @@ dopr_status dopr_shared_attention_plan(const dopr_cache_layout* layout, int32_t 
   a.prefix = prefix;
   a.plan = static_cast<int32_t*>(plan);
   a.status = status;
-  return cuda_status(launch_shared_plan(a, static_cast<cudaStream_t>(cuda_stream)), "dopr_shared_attention_plan");
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_shared_plan(a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_shared_attention_plan");
 }
 
 int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout* layout, int32_t n_q_heads, int32_t max_tokens) {
@@ -366,7 +368,9 @@ dopr_status dopr_shared_attention(const dopr_cache_layout* layout, const void* p
   a.lse = lse;
   a.ws = static_cast<uint8_t*>(workspace);
   a.status = status;
-  return cuda_status(launch_shared_attention(a, static_cast<cudaStream_t>(cuda_stream)), "dopr_shared_attention");
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_shared_attention(a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_shared_attention");
 }
 
 int64_t dopr_shared_attention_workspace(const dopr_cache_layout* layout, int32_t n_q_heads, int32_t max_tokens) {

@@ -1,141 +1,625 @@
 // k_shared_attn.cu -- attention of a step's tokens over a paged cache (dopr_shared_attention): the keys of the row's
-// prefix, then the row's own up to the token.
+// prefix, then the row's own up to the token, on the 5th-generation tensor cores.
 //
-// softmax(scale q k^T) v in one pass over the keys: with m the running maximum of the scores and l the running sum of
-// exp(score - m), a new score s > m scales what was summed by exp(m - s).
-#include "device_common.cuh"
-#include "internal.h"
+// softmax(scale q k^T) v over any split of the keys: a part gives its maximum score m, the sum l of exp(score - m) and
+// the sum o of exp(score - m) v; parts add up as exp(m_i - m) l_i and exp(m_i - m) o_i with m the largest m_i.  A
+// part itself runs over its keys block by block the same way.
+//
+// k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh).  A segment of an
+// item of two tiles gives each block of 128 keys to both softmax groups, a tile each; of one tile, blocks go to the
+// groups in turn, so that one softmax runs beside the other's products either way.
+//   warp 0, 2  copy K and V blocks, page by page, into two rings (TMA; a page's rows of a kv head lie together)
+//   warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
+//   warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
+//   warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more
+//              than 2^8 (P stays within the type's range until then), and leaves as a partial result
+// Keys past a row's last are skipped by selection, not by arithmetic: what the page holds there cannot matter.  Their
+// values would (0 x NaN), so those of the last block's last 16 rows are cleared in shared memory.  A value that one
+// token may see and another of the same item may not would too: k_shared_join finds those rows and computes them alone.
+//
+// k_shared_join, a warp a token and q head, adds the parts up.
+#include <limits.h>
+
+#include <type_traits>
+
+#include "shared_attn.cuh"
 
 namespace dopr {
 namespace {
+using namespace shared_attn;
 
-constexpr int PLAN_THREADS = 1024, ROW_WARPS = 4;
-constexpr int PLAN_HEAD = 16;  // ints; [0]: tokens (0 where the plan is empty)
-// Then an int4 a token: own row, own keys it sees, prefix row (-1: none), prefix keys.
+constexpr int THREADS = 128 + 2 * 128;
+constexpr uint32_t TMEM_COLS = 512, S_COL = 0, O_COL = 256;  // group w: S at S_COL + 128 w, O at O_COL + 128 w
+constexpr float RESCALE_LOG2 = 8.f;
+constexpr int HALF_BYTES = 128 * 128;  // 128 rows of 64 16-bit elements
 
-__global__ void __launch_bounds__(PLAN_THREADS) k_shared_plan(SharedPlanArgs a) {
-  __shared__ int bad;
-  const int n = a.lay.n_seqs;
-  const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * a.lay.page;
-  if (threadIdx.x == 0) bad = 0;
-  pdl_wait();
-  pdl_trigger();
-  __syncthreads();
-  for (int i = threadIdx.x; i < n; i += PLAN_THREADS) {
-    const int t0 = a.tok_off[i], t1 = a.tok_off[i + 1], pre = a.prefix ? a.prefix[i] : -1;
-    if ((i == 0 && t0 != 0) || t1 < t0 || t1 > a.max_tokens || a.seq_lens[i] < 0 || a.seq_lens[i] > cap || pre < -1 || pre >= n ||
-        pre == i || (pre >= 0 && a.prefix[pre] != -1))
-      bad = 1;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    a.plan[0] = bad ? 0 : a.tok_off[n];
-    if (bad && a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-  }
-  if (bad) return;
-  int4* rec = reinterpret_cast<int4*>(a.plan + PLAN_HEAD);
-  for (int t = threadIdx.x; t < a.tok_off[n]; t += PLAN_THREADS) {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.tok_off[mid] <= t) lo = mid; else hi = mid - 1;
+template <int D>
+struct Smem {
+  static constexpr int HALVES = D / 64;
+  static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
+  static constexpr int K_STAGES = D == 128 ? 2 : 5, V_STAGES = D == 128 ? 3 : 5;
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;
+  static constexpr int OFF_V = OFF_K + K_STAGES * TILE_BYTES;
+  static constexpr int OFF_TOK = OFF_V + V_STAGES * TILE_BYTES;  // the Q gatherer's tokens
+  static constexpr int OFF_BAR = OFF_TOK + 128 * 4;
+  static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
+                       Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
+                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
+  static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
+  static_assert(BYTES <= 227 * 1024, "shared memory budget");
+};
+
+struct Ring {
+  int stage = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++stage == n) {
+      stage = 0;
+      phase ^= 1u;
     }
-    const int pre = a.prefix ? a.prefix[lo] : -1;
-    const int own = a.seq_lens[lo] - (a.tok_off[lo + 1] - a.tok_off[lo]) + (t - a.tok_off[lo]) + 1;
-    rec[t] = make_int4(lo, min(max(own, 0), a.seq_lens[lo]), pre, pre >= 0 ? a.seq_lens[pre] : 0);
   }
-}
+};
 
 template <typename T>
-__device__ __forceinline__ float2 pair_f32(uint32_t w) {
-  if constexpr (sizeof(T) && std::is_same_v<T, __half>) return __half22float2(*reinterpret_cast<const __half2*>(&w));
-  else return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
+__host__ __device__ constexpr uint32_t type_bits() {  // operand formats of the instruction descriptor: 0 f16, 1 bf16
+  return std::is_same_v<T, __half> ? 0u : (1u << 7 | 1u << 10);
 }
 template <typename T>
-__device__ __forceinline__ uint32_t pack_f32(float x, float y) {
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
   if constexpr (std::is_same_v<T, __half>) return pack_f16x2(x, y);
   else return pack_bf16x2(x, y);
 }
+template <typename T>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (std::is_same_v<T, __half>) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  else return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// A warp per token and q head, a key at a time; lane l holds elements [E l, E l + E) of the head.
+// One segment after another of this CTA's share.
+struct Segment {
+  Item it;
+  int f, h;           // flat entry, kv head
+  uint32_t b0, b1;    // its blocks here
+  uint32_t part;      // which of the entry's segments
+  bool two;           // two tiles
+};
+struct Walk {
+  const Plan& p;
+  uint32_t c0, c1, share;
+  int f, n_flat, Hkv, G;
+  __device__ __forceinline__ Walk(const Plan& plan, const SharedAttnArgs& a) : p(plan), Hkv(a.lay.n_kv_heads), G(a.Hq / a.lay.n_kv_heads) {
+    Head h = *p.head;
+    if (!made_for(h, a.lay, a.Hq, a.max_tokens, gridDim.x)) {
+      if (a.status && threadIdx.x == 0) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+      h = Head{};
+    }
+    share = h.share;
+    c0 = min(blockIdx.x * static_cast<unsigned long long>(share), static_cast<unsigned long long>(h.total));
+    c1 = min(c0 + share, h.total);
+    n_flat = h.n_flat;
+    f = c0 < c1 ? p.first[blockIdx.x] : n_flat;
+  }
+  __device__ __forceinline__ bool next(Segment& s) {
+    for (; f < n_flat; ++f) {
+      s.it = p.items[f / Hkv];
+      const uint32_t blocks = blocks_of(s.it.n_keys);
+      if (blocks == 0) continue;
+      s.h = f % Hkv;
+      const uint32_t b = keys_begin(s.it, blocks, s.h);
+      if (b - OVERHEAD >= c1) return false;
+      s.b0 = c0 > b ? c0 - b : 0;
+      s.b1 = c1 > b ? min(c1 - b, blocks) : 0;
+      if (s.b1 <= s.b0) continue;
+      s.part = (b + s.b0) / share - b / share;
+      s.two = two_tiles(s.it.n_tok, G);
+      s.f = f++;
+      return true;
+    }
+    return false;
+  }
+};
+// The groups that take a block: both, or in turn over all one-tile segments of the CTA.
+struct Turn {
+  uint32_t at = 0;
+  __device__ __forceinline__ uint32_t groups(const Segment& s) {
+    if (s.two) return 3u;
+    const uint32_t g = 1u << at;
+    at ^= 1u;
+    return g;
+  }
+};
+
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * ROW_WARPS) k_attn_rows(SharedAttnArgs a) {
-  constexpr int E = D / 32, W = E / 2;  // elements and 32-bit words a lane
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * ROW_WARPS + (threadIdx.x >> 5);
-  pdl_wait();
+__global__ void __launch_bounds__(THREADS, 1)
+    k_shared_attn(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, SharedAttnArgs a) {
+  using L = Smem<D>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ int gave_up;  // stands for the error word of the bounded waits: a CTA gives up alone
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t s0 = smem_u32(smem);
+  auto bar = [&](int i) { return s0 + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_BAR + L::N_BARS * 8);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, TT = tokens_a_tile(G);
+  int* err = &gave_up;
+
+  if (threadIdx.x == 0) {
+    gave_up = 0;
+    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
   pdl_trigger();
-  const int32_t* plan = static_cast<const int32_t*>(a.plan);
-  if (unit >= static_cast<int64_t>(plan[0]) * a.Hq) return;
-  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit % a.Hq);
-  const int4 rec = reinterpret_cast<const int4*>(plan + PLAN_HEAD)[t];
+  pdl_wait();
+  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
+  Walk walk(plan, a);
+  Segment s;
+
+  if (warp == 0 || warp == 2) {
+    // ======================= K and V blocks, page by page: a lane a page and half of the head
+    const bool is_v = warp == 2;
+    const CUtensorMap* map = is_v ? &tm_v : &tm_k;
+    const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL,
+              empty = is_v ? L::V_EMPTY : L::K_EMPTY;
+    const uint32_t ring0 = s0 + (is_v ? L::OFF_V : L::OFF_K);
+    const int page = a.lay.page;
+    const int pg = lane / L::HALVES, half = lane % L::HALVES;  // pages of a block: at most 8
+    Ring r;
+    uint32_t armed = 0, parity = 0;
+    bool ok = true;
+    while (ok && walk.next(s)) {
+      const int32_t* table = a.tables + static_cast<int64_t>(s.it.row) * a.lay.max_blocks;
+      for (uint32_t b = s.b0; b < s.b1; ++b) {
+        const int key0 = b * BLOCK, keys = min(BLOCK, s.it.n_keys - key0), pages = (keys + page - 1) / page;
+        int block = 0;
+        const bool mine = pg < pages;
+        if (mine) {
+          block = table[key0 / page + pg];
+          if (block < 0 || block >= a.lay.n_blocks) {
+            if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+            block = 0;
+          }
+        }
+        if (!mbar_wait_warp(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
+          ok = false;
+          break;
+        }
+        const uint32_t fb = bar(full + r.stage);
+        if (lane == 0) mbar_arrive_expect_tx(fb, pages * page * 128 * L::HALVES);
+        __syncwarp();
+        if (mine)
+          tma_load_2d(ring0 + r.stage * L::TILE_BYTES + half * HALF_BYTES + pg * page * 128, map, fb, half * 64,
+                      (block * Hkv + s.h) * page);
+        __syncwarp();
+        armed |= 1u << r.stage;
+        parity = (parity & ~(1u << r.stage)) | r.phase << r.stage;
+        r.next(stages);
+      }
+    }
+    if (!ok)  // copies in flight land before the CTA ends
+      for (int i = 0; i < stages; ++i)
+        if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
+  } else if (warp == 1) {
+    // ======================= MMA issuer
+    const bool one = elect_one();
+    const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
+    Ring rk, rv;
+    Turn turn;
+    bool ok = true;
+    auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
+    // products P V that wait for their softmax, oldest first; at most one a group
+    struct Pending {
+      int stage, keys;
+      uint32_t phase, flags;  // flags: 1 first of the group's segment, 2 last of it, 4 last use of the V stage, 8 its first
+    } pend0{}, pend1{};
+    int oldest = 0, next_oldest = 0, n_pend = 0;  // groups
+    uint32_t p_par = 0, q_par = 0;  // a bit a group
+    auto issue_pv = [&]() -> bool {
+      const int w = oldest;
+      const Pending x = w ? pend1 : pend0;
+      oldest = next_oldest;
+      --n_pend;
+      if (!wait(L::V_FULL + x.stage, x.phase)) return false;
+      const int steps = (x.keys + 15) / 16;
+      const uint32_t v0 = sV + x.stage * L::TILE_BYTES;
+      if ((x.flags & 8u) && (x.keys & 15)) {
+        // values of keys past the last, up to the product's step, count as zero
+        const int rows = steps * 16 - x.keys, pieces = rows * 8 * L::HALVES;
+        for (int i = lane; i < pieces; i += 32) {
+          const int row = x.keys + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
+          *reinterpret_cast<uint4*>(smem + (v0 - s0) + (c >> 3) * HALF_BYTES + row * 128 + (c & 7) * 16) = uint4{0, 0, 0, 0};
+        }
+        fence_proxy_async_shared();
+        __syncwarp();
+      }
+      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return false;
+      p_par ^= 1u << w;
+      tc_fence_after();
+      const uint64_t vd = umma_desc_sw128_mn(v0, HALF_BYTES, 1024);
+      constexpr uint32_t idesc = umma_idesc_f16_bmn(TILE, D) | type_bits<T>();
+      if (one) {
+        for (int k = 0; k < steps; ++k)
+          umma_f16_ts(tmem + O_COL + 128 * w, tmem + S_COL + 128 * w + 8 * k, vd + (k * 2048) / 16, idesc,
+                      !(x.flags & 1u) || k > 0);
+        if (x.flags & 4u) umma_commit(bar(L::V_EMPTY + x.stage));
+        if (x.flags & 2u) umma_commit(bar(L::O_FULL + w));
+      }
+      return true;
+    };
+    while (ok && walk.next(s)) {
+      uint32_t begun = 0;
+      for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
+        const uint32_t groups = turn.groups(s);
+        const int keys = min(BLOCK, s.it.n_keys - static_cast<int>(b) * BLOCK);
+        // the group's last block of the segment: two tiles' last, or one of the last two
+        const bool last = s.two ? b + 1 == s.b1 : b + 2 >= s.b1;
+        for (int w = 0; w < 2 && ok; ++w) {
+          if (!(groups >> w & 1u)) continue;
+          while (ok && ((n_pend > 0 && oldest == w) || (n_pend > 1 && next_oldest == w))) issue_pv();
+          if (!ok) break;
+          const bool first = !(begun >> w & 1u);
+          if (first) {
+            if (!wait(L::Q_FULL + w, q_par >> w & 1u)) break;
+            q_par ^= 1u << w;
+            begun |= 1u << w;
+          }
+          if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
+          tc_fence_after();
+          const bool last_use = !s.two || w == 1;
+          const uint64_t qd = umma_desc_sw128(sQ + w * L::TILE_BYTES), kd = umma_desc_sw128(sK + rk.stage * L::TILE_BYTES);
+          const uint32_t idesc = umma_idesc_f16(TILE, (keys + 15) / 16 * 16) | type_bits<T>();
+          if (one) {
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              const int off = ((k >> 2) * HALF_BYTES + (k & 3) * 32) / 16;
+              umma_f16(tmem + S_COL + 128 * w, qd + off, kd + off, idesc, k > 0);
+            }
+            umma_commit(bar(L::S_FULL + w));
+            if (last_use) umma_commit(bar(L::K_EMPTY + rk.stage));
+            if (last) umma_commit(bar(L::Q_EMPTY + w));
+          }
+          (w ? pend1 : pend0) = Pending{rv.stage, keys, rv.phase,
+                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (!s.two || w == 0 ? 8u : 0u)};
+          (n_pend++ ? next_oldest : oldest) = w;
+        }
+        rk.next(L::K_STAGES);
+        rv.next(L::V_STAGES);
+      }
+    }
+    while (ok && n_pend > 0) issue_pv();
+    if (one) umma_commit(bar(L::DRAIN));
+    mbar_wait_warp(bar(L::DRAIN), 0, err, ok ? WAIT_TIMEOUT_NS : 100000000ull);
+  } else if (warp == 3) {
+    // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
+    int* tok = reinterpret_cast<int*>(smem + L::OFF_TOK);
+    Turn turn;
+    uint32_t used = 0, par = 0;
+    bool ok = true;
+    const T* q = static_cast<const T*>(a.q);
+    while (ok && walk.next(s)) {
+      uint32_t groups = 0;
+      for (uint32_t b = s.b0; b < s.b1; ++b) groups |= turn.groups(s);
+      for (int w = 0; w < 2 && ok; ++w) {
+        if (!(groups >> w & 1u)) continue;
+        const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
+        __syncwarp();
+        for (int i = lane; i < n; i += 32) tok[i] = s.it.own ? s.it.tok + t0 + i : plan.order[s.it.tok + t0 + i];
+        __syncwarp();
+        if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
+          ok = false;
+          break;
+        }
+        if (used >> w & 1u) par ^= 1u << w;
+        used |= 1u << w;
+        constexpr int CHUNKS = D / 8;  // 16-byte pieces of a row
+        const int pieces = n * G * CHUNKS;
+        for (int i = lane; i < pieces; i += 32) {
+          const int r = i / CHUNKS, c = i % CHUNKS;
+          const T* src = q + static_cast<int64_t>(tok[r / G]) * a.q_tok + static_cast<int64_t>(s.h * G + r % G) * a.q_head + c * 8;
+          cp_async16(s0 + L::OFF_Q + w * L::TILE_BYTES + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, true);
+        }
+        cp_async_commit();
+        cp_async_wait_all();
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::Q_FULL + w));
+      }
+    }
+  } else {
+    // ======================= softmax: thread r of group w has row r of its tile
+    const int w = (warp >> 2) - 1, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
+    const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
+    const float scale_log2 = a.scale * 1.4426950408889634f;
+    float2* ml = reinterpret_cast<float2*>(a.ws);
+    float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.Hq, a.max_tokens, gridDim.x));
+    Turn turn;
+    uint32_t s_par = 0, o_par = 0;
+    bool ok = true;
+    while (ok && walk.next(s)) {
+      const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
+      const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
+      // keys that this row sees; the least of the warp's rows tells which blocks need no selection
+      const int sees = s.it.own ? min(s.it.seen + t0 + (valid ? r / G : 0), s.it.n_keys) : s.it.n_keys;
+      const int all_see = __reduce_min_sync(0xffffffffu, valid ? sees : INT_MAX);
+      const uint32_t first_group = s.two ? w : turn.at;
+      float m = -INFINITY, l = 0.f;
+      int done = 0;
+      for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
+        if (!(turn.groups(s) >> w & 1u)) continue;
+        if (!mbar_wait_warp(bar(L::S_FULL + w), s_par, err, WAIT_TIMEOUT_NS)) {
+          ok = false;
+          break;
+        }
+        s_par ^= 1u;
+        ++done;
+        if (!any) {  // none of this warp's rows is one: what its lanes of P hold reaches no other
+          if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+          continue;
+        }
+        tc_fence_after();
+        const int key0 = b * BLOCK, cols = min(BLOCK, s.it.n_keys - key0), see = sees - key0;
+        const bool whole = all_see - key0 >= BLOCK;
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(s_col + c, v);
+          tmem_ld_wait();
+          if (whole) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = c + i < see ? fmaxf(top, __uint_as_float(v[i])) : top;
+          }
+        }
+        top *= scale_log2;
+        if (m == -INFINITY) m = top;  // nothing but zeros has been summed
+        const bool grow = top > m + RESCALE_LOG2;
+        if (__any_sync(0xffffffffu, grow)) {
+          // S is complete, so every product issued before it is: O stands still
+          const float by = grow ? ex2(m - top) : 1.f;
+          if (grow) m = top;
+          l *= by;
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t v[32], x[16];
+            tmem_ld32(o_col + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int k = 0; k < 32; k += 16) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(v[k + i]) * by);
+              tmem_st16(o_col + c + k, x);
+            }
+          }
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll 1
+        for (int c = 0; c < cols; c += 32) {
+          uint32_t v[32], pk[16];
+          tmem_ld32(s_col + c, v);
+          tmem_ld_wait();
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float p = ex2(fmaf(__uint_as_float(v[i]), scale_log2, -base));
+            if (!whole) p = c + i < see ? p : 0.f;
+            sum[i & 3] += p;
+            v[i] = __float_as_uint(p);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+          tmem_st16(s_col + c / 2, pk);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+      }
+      if (!ok) break;
+      // ---- the partial result
+      const uint32_t rows = s.it.n_tok * G, copies = s.two ? 1 : 2;
+      const uint32_t copy = s.two ? 0 : (first_group == static_cast<uint32_t>(w) ? 0 : 1);
+      const int64_t row = plan.part[s.f] + static_cast<int64_t>(s.part * copies + copy) * rows + (s.two ? w * TT * G : 0) + r;
+      if (valid) ml[row] = make_float2(m, l);
+      if (done > 0) {
+        if (!mbar_wait_warp(bar(L::O_FULL + w), o_par, err, WAIT_TIMEOUT_NS)) break;
+        o_par ^= 1u;
+        tc_fence_after();
+        float* dst = part_o + row * D;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(o_col + c, v);
+          tmem_ld_wait();
+          if (valid) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + c + 4 * i) = uint4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+          }
+        }
+        tc_fence_before();
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (threadIdx.x == 0 && gave_up && a.status) atomicCAS(a.status, 0, DOPR_ERR_TIMEOUT);
+  if (warp == 1) {
+    __syncwarp();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// ------------------------------------------------------------------ joining the parts
+constexpr int JOIN_WARPS = 4;
+
+// One row alone, a key at a time, for the rows whose products took in a value they do not see; lane l holds elements
+// [E l, E l + E) of the head.
+template <typename T, int D>
+__device__ void row_alone(const SharedAttnArgs& a, const Plan& plan, const int4& rec, int t, int h, int lane, float (&o)[D / 32],
+                          float& m, float& l) {
+  constexpr int E = D / 32, W = E / 2;
   const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
   const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  float q[E];
+  m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    const float2 f = pair_f32<T>(qp[i]);
-    q[2 * i] = f.x * a.scale, q[2 * i + 1] = f.y * a.scale;
+    const float2 f = unpack2<T>(qp[i]);
+    q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
     o[2 * i] = o[2 * i + 1] = 0.f;
   }
   for (int part = 0; part < 2; ++part) {
-    const int row = part ? rec.x : rec.z, n = part ? rec.y : rec.w;
+    const int item = part ? rec.z : rec.x;
+    if (item < 0) continue;
+    const Item it = plan.items[item];
+    const int n = part ? min(it.seen + rec.w, it.n_keys) : it.n_keys;
     for (int p = 0; p < n; ++p) {
-      int block = a.tables[static_cast<int64_t>(row) * a.lay.max_blocks + p / page];
-      if (block < 0 || block >= a.lay.n_blocks) {
-        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-        block = 0;
-      }
+      int block = a.tables[static_cast<int64_t>(it.row) * a.lay.max_blocks + p / page];
+      if (block < 0 || block >= a.lay.n_blocks) block = 0;
       const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
-      const uint32_t* kp = static_cast<const uint32_t*>(a.k_pool) + at;
-      const uint32_t* vp = static_cast<const uint32_t*>(a.v_pool) + at;
+      const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
       float s = 0.f;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float2 f = pair_f32<T>(kp[i]);
+        const float2 f = unpack2<T>(kp[i]);
         s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
       }
       s = warp_sum(s);
-      const float top = fmaxf(m, s), shift = top == -INFINITY ? 0.f : top;
-      const float old = expf(m - shift), e = expf(s - shift);
+      const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+      const float old = exp2f(m - base), e = exp2f(s - base);
       m = top;
       l = l * old + e;
 #pragma unroll
       for (int i = 0; i < W; ++i) {
-        const float2 f = pair_f32<T>(vp[i]);
+        const float2 f = unpack2<T>(vp[i]);
         o[2 * i] = o[2 * i] * old + e * f.x;
         o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
       }
     }
   }
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // a NaN stays one
-  uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * W;
-#pragma unroll
-  for (int i = 0; i < W; ++i) op[i] = pack_f32<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = m + logf(l);
 }
 
 template <typename T, int D>
-cudaError_t launch_rows(const SharedAttnArgs& a, cudaStream_t st) {
+__global__ void __launch_bounds__(32 * JOIN_WARPS) k_shared_join(SharedAttnArgs a, int n_ctas) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * JOIN_WARPS + (threadIdx.x >> 5);
+  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
+  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
+  pdl_wait();
+  pdl_trigger();
+  const Head head = *plan.head;
+  if (!made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas)) return;
+  if (unit >= static_cast<int64_t>(head.tokens) * a.Hq) return;
+  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit % a.Hq), kvh = h / G;
+  const float2* ml = reinterpret_cast<const float2*>(a.ws);
+  const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.Hq, a.max_tokens, n_ctas));
+  const int4 rec = plan.rec[t];
+  float o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < E; ++i) o[i] = 0.f;
+  bool partly = false;  // the row's own item holds keys that it does not see
+  for (int part = 0; part < 2; ++part) {
+    const int item = part ? rec.z : rec.x, place = part ? rec.w : rec.y;
+    if (item < 0) continue;
+    const Item it = plan.items[item];
+    const uint32_t blocks = blocks_of(it.n_keys);
+    if (blocks == 0) continue;
+    partly |= part && it.seen + place < it.n_keys;
+    const uint32_t b = keys_begin(it, blocks, kvh), rows = it.n_tok * G;
+    const uint32_t parts = ((b + blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
+    const int64_t row0 = plan.part[static_cast<int64_t>(item) * Hkv + kvh] + place * G + h % G;
+    for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
+      const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
+      float top = x.x;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      top = fmaxf(top, m);
+      const float base = top == -INFINITY ? 0.f : top;
+      const float old = ex2(m - base), mine = ex2(x.x - base);
+      l = l * old + warp_sum(x.y * mine);
+      m = top;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] *= old;
+      const int n = min(32u, parts - p0);
+      for (int p = 0; p < n; ++p) {
+        const float wgt = __shfl_sync(0xffffffffu, mine, p), sum = __shfl_sync(0xffffffffu, x.y, p);
+        if (sum == 0.f) continue;  // no block of this part, or nothing that the row sees
+        const float* src = part_o + (row0 + static_cast<int64_t>(p0 + p) * rows) * D + lane * E;
+        if constexpr (E == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(src);
+          o[0] += wgt * v.x, o[1] += wgt * v.y, o[2] += wgt * v.z, o[3] += wgt * v.w;
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(src);
+          o[0] += wgt * v.x, o[1] += wgt * v.y;
+        }
+      }
+    }
+  }
+  if (partly) {
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
+    if (__any_sync(0xffffffffu, nan)) row_alone<T, D>(a, plan, rec, t, h, lane, o, m, l);
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // a NaN stays one
+  uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
+#pragma unroll
+  for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = (m + log2f(l)) * 0.6931471805599453f;
+}
+
+template <typename T, int D>
+cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
+  const int n_ctas = num_sms < MAX_CTAS ? num_sms : MAX_CTAS;
+  CUtensorMap tm_k, tm_v;
+  const uint64_t rows = static_cast<uint64_t>(a.lay.n_blocks) * a.lay.n_kv_heads * a.lay.page;
+  const bool half = std::is_same_v<T, __half>;
+  if (!make_tmap_16b_2d(&tm_k, a.k_pool, D, rows, D * 2, 64, a.lay.page, true, half) ||
+      !make_tmap_16b_2d(&tm_v, a.v_pool, D, rows, D * 2, 64, a.lay.page, true, half))
+    return cudaErrorInvalidValue;
+  cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_k, tm_v, a);
+  if (e != cudaSuccess) return e;
   const int64_t units = static_cast<int64_t>(a.max_tokens) * a.Hq;
-  return launch_dependent(k_attn_rows<T, D>, dim3(static_cast<unsigned>((units + ROW_WARPS - 1) / ROW_WARPS)), 32 * ROW_WARPS,
-                          0, st, a);
+  return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>((units + JOIN_WARPS - 1) / JOIN_WARPS)), 32 * JOIN_WARPS,
+                          0, st, a, n_ctas);
 }
 
 }  // namespace
 
-int64_t shared_plan_bytes(const dopr_cache_layout&, int, int max_tokens) {
-  return PLAN_HEAD * 4 + static_cast<int64_t>(max_tokens) * 16;
+int64_t shared_workspace_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens, int num_sms) {
+  return max_part_rows(Hq, max_tokens, num_sms < MAX_CTAS ? num_sms : MAX_CTAS) * (8 + 4 * static_cast<int64_t>(lay.head_dim));
 }
-int64_t shared_workspace_bytes(const dopr_cache_layout&, int, int, int) { return 16; }
 
-cudaError_t launch_shared_plan(const SharedPlanArgs& a, cudaStream_t st) {
-  return launch_dependent(k_shared_plan, dim3(1), PLAN_THREADS, 0, st, a);
-}
-cudaError_t launch_shared_attention(const SharedAttnArgs& a, cudaStream_t st) {
+cudaError_t launch_shared_attention(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   const bool half = a.lay.dtype == DOPR_F16;
-  if (a.lay.head_dim == 128) return half ? launch_rows<__half, 128>(a, st) : launch_rows<__nv_bfloat16, 128>(a, st);
-  return half ? launch_rows<__half, 64>(a, st) : launch_rows<__nv_bfloat16, 64>(a, st);
+  if (a.lay.head_dim == 128) return half ? launch<__half, 128>(a, num_sms, st) : launch<__nv_bfloat16, 128>(a, num_sms, st);
+  return half ? launch<__half, 64>(a, num_sms, st) : launch<__nv_bfloat16, 64>(a, num_sms, st);
 }
 
 }  // namespace dopr

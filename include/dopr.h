@@ -533,7 +533,9 @@ DOPR_API dopr_status dopr_cache_append(const dopr_cache_layout *layout, const do
  * How the attention of a step's tokens is split over the device: made once a
  * step, used by every layer.  tok_off, seq_lens (after dopr_cache_extend) and
  * prefix as there; tokens tok_off[n_seqs] .. max_tokens - 1 are behind the last.
- *   plan  dopr_shared_attention_plan_bytes(...) bytes, 16-byte aligned.
+ *   plan  dopr_shared_attention_plan_bytes(...) bytes, 16-byte aligned.  It serves
+ *         attention with the same layout, n_q_heads and max_tokens on the same
+ *         kind of device; with others that is INVALID_ARG and writes nothing.
  * 1 <= n_q_heads / n_kv_heads <= 64, a whole number.
  * Device error: INVALID_ARG (offsets, a length or a prefix out of range); the
  * plan is then empty, and attention writes nothing.

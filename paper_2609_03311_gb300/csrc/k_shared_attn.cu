@@ -5,17 +5,17 @@
 // the sum o of exp(score - m) v; parts add up as exp(m_i - m) l_i and exp(m_i - m) o_i with m the largest m_i.  A
 // part itself runs over its keys block by block the same way.
 //
-// k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh).  A segment of an
-// item of two tiles gives each block of 128 keys to both softmax groups, a tile each; of one tile, blocks go to the
-// groups in turn, so that one softmax runs beside the other's products either way.
+// k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh).  An item of two
+// tiles gives each block of 128 columns to the softmax groups of the tiles that it concerns, a tile each; of one tile,
+// blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
 //   warp 0, 2  copy K and V blocks, page by page, into two rings (TMA; a page's rows of a kv head lie together)
 //   warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
 //   warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
 //   warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more
 //              than 2^8 (P stays within the type's range until then), and leaves as a partial result
-// Keys past a row's last are skipped by selection, not by arithmetic: what the page holds there cannot matter.  Their
-// values would (0 x NaN), so those of the last block's last 16 rows are cleared in shared memory.  A value that one
-// token may see and another of the same item may not would too: k_shared_join finds those rows and computes them alone.
+// Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
+// Values would (0 x NaN), so rows of V past a run's keys are cleared in shared memory.  A value that one token sees and
+// another of the item does not would too: k_shared_join finds those rows and computes them alone.
 //
 // k_shared_join, a warp a token and q head, adds the parts up.
 #include <limits.h>
@@ -85,10 +85,10 @@ __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence
 // One segment after another of this CTA's share.
 struct Segment {
   Item it;
-  int f, h;           // flat entry, kv head
-  uint32_t b0, b1;    // its blocks here
-  uint32_t part;      // which of the entry's segments
-  bool two;           // two tiles
+  int f, h;         // flat entry, kv head
+  uint32_t b0, b1;  // its blocks here
+  uint32_t part;    // which of the entry's segments
+  bool two;         // two tiles
 };
 struct Walk {
   const Plan& p;
@@ -109,13 +109,12 @@ struct Walk {
   __device__ __forceinline__ bool next(Segment& s) {
     for (; f < n_flat; ++f) {
       s.it = p.items[f / Hkv];
-      const uint32_t blocks = blocks_of(s.it.n_keys);
-      if (blocks == 0) continue;
+      if (s.it.blocks == 0) continue;
       s.h = f % Hkv;
-      const uint32_t b = keys_begin(s.it, blocks, s.h);
+      const uint32_t b = blocks_begin(s.it, s.h);
       if (b - OVERHEAD >= c1) return false;
       s.b0 = c0 > b ? c0 - b : 0;
-      s.b1 = c1 > b ? min(c1 - b, blocks) : 0;
+      s.b1 = c1 > b ? min(c1 - b, s.it.blocks) : 0;
       if (s.b1 <= s.b0) continue;
       s.part = (b + s.b0) / share - b / share;
       s.two = two_tiles(s.it.n_tok, G);
@@ -125,16 +124,57 @@ struct Walk {
     return false;
   }
 };
-// The groups that take a block: both, or in turn over all one-tile segments of the CTA.
-struct Turn {
-  uint32_t at = 0;
-  __device__ __forceinline__ uint32_t groups(const Segment& s) {
-    if (s.two) return 3u;
-    const uint32_t g = 1u << at;
-    at ^= 1u;
+// The softmax groups that take a block (a bit each): those whose tile it concerns, or in turn over all one-tile
+// segments of the CTA.
+struct Groups {
+  uint32_t turn = 0;
+  __device__ __forceinline__ uint32_t of(const Segment& s, uint32_t b) {
+    if (s.two) return (b < s.it.end0 ? 1u : 0u) | (b < s.it.prefix_blocks || b >= s.it.begin1 ? 2u : 0u);
+    const uint32_t g = 1u << turn;
+    turn ^= 1u;
+    return g;
+  }
+  // The groups that take any block of the segment; goes past it.
+  __device__ __forceinline__ uint32_t any(const Segment& s) {
+    if (s.two) return (s.b0 < s.it.end0 ? 1u : 0u) | (s.b0 < s.it.prefix_blocks || s.b1 > s.it.begin1 ? 2u : 0u);
+    const uint32_t n = s.b1 - s.b0, g = n > 1 ? 3u : 1u << turn;
+    turn ^= n & 1u;
     return g;
   }
 };
+// The last block of the segment that group w takes, if it takes any (of one tile: the last but one is another's last).
+__device__ __forceinline__ bool last_block(const Segment& s, uint32_t b, int w) {
+  if (!s.two) return b + 2 >= s.b1;
+  if (w == 0) return b + 1 == min(s.b1, s.it.end0);
+  return b + 1 == (s.b1 > s.it.begin1 ? s.b1 : min(s.b1, s.it.prefix_blocks));
+}
+// A lane's page of each block and the run it lies in.
+struct PageCursor {
+  Run run;
+  int at, n_runs;
+  const Run* runs;
+  __device__ __forceinline__ void seek(const Plan& p, const Item& it, int page) {
+    runs = p.runs + it.run;
+    n_runs = it.n_runs;
+    int lo = 0, hi = n_runs - 1;
+    while (lo < hi) {  // the last run that begins at or before the page (runs without pages share their successor's place)
+      const int mid = (lo + hi + 1) >> 1;
+      if (runs[mid].off <= page) lo = mid; else hi = mid - 1;
+    }
+    at = lo;
+    run = runs[at];
+  }
+  __device__ __forceinline__ void go(int page) {
+    while (page >= run.off + run.pages && at + 1 < n_runs) run = runs[++at];
+  }
+};
+// Bits [lo, hi) of a word, the range clipped to it.
+__device__ __forceinline__ uint32_t bits_in(int lo, int hi) {
+  lo = max(lo, 0);
+  hi = min(hi, 32);
+  if (hi <= lo) return 0u;
+  return (hi >= 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
@@ -178,19 +218,21 @@ __global__ void __launch_bounds__(THREADS, 1)
     const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL,
               empty = is_v ? L::V_EMPTY : L::K_EMPTY;
     const uint32_t ring0 = s0 + (is_v ? L::OFF_V : L::OFF_K);
-    const int page = a.lay.page;
+    const int page = a.lay.page, page_blk = BLOCK / page;
     const int pg = lane / L::HALVES, half = lane % L::HALVES;  // pages of a block: at most 8
     Ring r;
     uint32_t armed = 0, parity = 0;
     bool ok = true;
     while (ok && walk.next(s)) {
-      const int32_t* table = a.tables + static_cast<int64_t>(s.it.row) * a.lay.max_blocks;
+      PageCursor cur;
+      cur.seek(plan, s.it, s.b0 * page_blk + pg);
       for (uint32_t b = s.b0; b < s.b1; ++b) {
-        const int key0 = b * BLOCK, keys = min(BLOCK, s.it.n_keys - key0), pages = (keys + page - 1) / page;
-        int block = 0;
+        const int first = b * page_blk, pages = min(page_blk, s.it.pages - first);
         const bool mine = pg < pages;
+        int block = 0;
         if (mine) {
-          block = table[key0 / page + pg];
+          cur.go(first + pg);
+          block = a.tables[static_cast<int64_t>(cur.run.row) * a.lay.max_blocks + first + pg - cur.run.off];
           if (block < 0 || block >= a.lay.n_blocks) {
             if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
             block = 0;
@@ -219,14 +261,16 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ======================= MMA issuer
     const bool one = elect_one();
     const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
+    const int page = a.lay.page, page_blk = BLOCK / page;
     Ring rk, rv;
-    Turn turn;
+    Groups groups;
     bool ok = true;
     auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
     // products P V that wait for their softmax, oldest first; at most one a group
     struct Pending {
-      int stage, keys;
+      int stage, cols;
       uint32_t phase, flags;  // flags: 1 first of the group's segment, 2 last of it, 4 last use of the V stage, 8 its first
+      int keys;               // this lane's page of the block: rows that hold keys
     } pend0{}, pend1{};
     int oldest = 0, next_oldest = 0, n_pend = 0;  // groups
     uint32_t p_par = 0, q_par = 0;  // a bit a group
@@ -236,14 +280,17 @@ __global__ void __launch_bounds__(THREADS, 1)
       oldest = next_oldest;
       --n_pend;
       if (!wait(L::V_FULL + x.stage, x.phase)) return false;
-      const int steps = (x.keys + 15) / 16;
+      const int steps = x.cols / 16;
       const uint32_t v0 = sV + x.stage * L::TILE_BYTES;
-      if ((x.flags & 8u) && (x.keys & 15)) {
-        // values of keys past the last, up to the product's step, count as zero
-        const int rows = steps * 16 - x.keys, pieces = rows * 8 * L::HALVES;
-        for (int i = lane; i < pieces; i += 32) {
-          const int row = x.keys + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
-          *reinterpret_cast<uint4*>(smem + (v0 - s0) + (c >> 3) * HALF_BYTES + row * 128 + (c & 7) * 16) = uint4{0, 0, 0, 0};
+      uint32_t ragged = __ballot_sync(0xffffffffu, x.keys < page) & ((1u << page_blk) - 1u) & ((1u << x.cols / page) - 1u);
+      if ((x.flags & 8u) && ragged) {
+        while (ragged) {  // rows past a page's keys count as zero
+          const int pg = __ffs(ragged) - 1, from = __shfl_sync(0xffffffffu, x.keys, pg);
+          ragged &= ragged - 1;
+          for (int i = lane; i < (page - from) * 8 * L::HALVES; i += 32) {
+            const int row = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
+            *reinterpret_cast<uint4*>(smem + (v0 - s0) + (c >> 3) * HALF_BYTES + row * 128 + (c & 7) * 16) = uint4{0, 0, 0, 0};
+          }
         }
         fence_proxy_async_shared();
         __syncwarp();
@@ -263,14 +310,20 @@ __global__ void __launch_bounds__(THREADS, 1)
       return true;
     };
     while (ok && walk.next(s)) {
+      PageCursor cur;
+      cur.seek(plan, s.it, s.b0 * page_blk + lane % page_blk);
       uint32_t begun = 0;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
-        const uint32_t groups = turn.groups(s);
-        const int keys = min(BLOCK, s.it.n_keys - static_cast<int>(b) * BLOCK);
-        // the group's last block of the segment: two tiles' last, or one of the last two
-        const bool last = s.two ? b + 1 == s.b1 : b + 2 >= s.b1;
+        const uint32_t takes = groups.of(s, b);
+        const int first_page = b * page_blk, cols = min(page_blk, s.it.pages - first_page) * page;
+        const int my_page = first_page + lane % page_blk;
+        int keys = page;
+        if (my_page < s.it.pages) {
+          cur.go(my_page);
+          keys = min(page, cur.run.keys - (my_page - cur.run.off) * page);
+        }
         for (int w = 0; w < 2 && ok; ++w) {
-          if (!(groups >> w & 1u)) continue;
+          if (!(takes >> w & 1u)) continue;
           while (ok && ((n_pend > 0 && oldest == w) || (n_pend > 1 && next_oldest == w))) issue_pv();
           if (!ok) break;
           const bool first = !(begun >> w & 1u);
@@ -281,9 +334,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
           tc_fence_after();
-          const bool last_use = !s.two || w == 1;
+          const bool last = last_block(s, b, w), first_use = w == 0 || takes == 2u, last_use = w == 1 || takes == 1u;
           const uint64_t qd = umma_desc_sw128(sQ + w * L::TILE_BYTES), kd = umma_desc_sw128(sK + rk.stage * L::TILE_BYTES);
-          const uint32_t idesc = umma_idesc_f16(TILE, (keys + 15) / 16 * 16) | type_bits<T>();
+          const uint32_t idesc = umma_idesc_f16(TILE, cols) | type_bits<T>();
           if (one) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
@@ -294,8 +347,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (last_use) umma_commit(bar(L::K_EMPTY + rk.stage));
             if (last) umma_commit(bar(L::Q_EMPTY + w));
           }
-          (w ? pend1 : pend0) = Pending{rv.stage, keys, rv.phase,
-                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (!s.two || w == 0 ? 8u : 0u)};
+          (w ? pend1 : pend0) = Pending{rv.stage, cols, rv.phase,
+                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (first_use ? 8u : 0u), keys};
           (n_pend++ ? next_oldest : oldest) = w;
         }
         rk.next(L::K_STAGES);
@@ -308,18 +361,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     int* tok = reinterpret_cast<int*>(smem + L::OFF_TOK);
-    Turn turn;
+    Groups groups;
     uint32_t used = 0, par = 0;
     bool ok = true;
     const T* q = static_cast<const T*>(a.q);
     while (ok && walk.next(s)) {
-      uint32_t groups = 0;
-      for (uint32_t b = s.b0; b < s.b1; ++b) groups |= turn.groups(s);
+      const uint32_t takes = groups.any(s);
       for (int w = 0; w < 2 && ok; ++w) {
-        if (!(groups >> w & 1u)) continue;
+        if (!(takes >> w & 1u)) continue;
         const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
         __syncwarp();
-        for (int i = lane; i < n; i += 32) tok[i] = s.it.own ? s.it.tok + t0 + i : plan.order[s.it.tok + t0 + i];
+        for (int i = lane; i < n; i += 32) tok[i] = plan.order[s.it.tok + t0 + i];
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
@@ -349,20 +401,24 @@ __global__ void __launch_bounds__(THREADS, 1)
     const float scale_log2 = a.scale * 1.4426950408889634f;
     float2* ml = reinterpret_cast<float2*>(a.ws);
     float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.Hq, a.max_tokens, gridDim.x));
-    Turn turn;
+    Groups groups;
     uint32_t s_par = 0, o_par = 0;
     bool ok = true;
     while (ok && walk.next(s)) {
       const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
       const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
-      // keys that this row sees; the least of the warp's rows tells which blocks need no selection
-      const int sees = s.it.own ? min(s.it.seen + t0 + (valid ? r / G : 0), s.it.n_keys) : s.it.n_keys;
-      const int all_see = __reduce_min_sync(0xffffffffu, valid ? sees : INT_MAX);
-      const uint32_t first_group = s.two ? w : turn.at;
+      // the row sees columns [0, prefix) and [own0, own1)
+      const int prefix = valid ? s.it.prefix_keys : 0;
+      int own0 = 0, own1 = 0;
+      if (valid) {
+        const int4 rec = plan.rec[plan.order[s.it.tok + t0 + r / G]];
+        own0 = rec.z, own1 = rec.z + rec.w;
+      }
+      const uint32_t first_group = s.two ? w : groups.turn;
       float m = -INFINITY, l = 0.f;
       int done = 0;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
-        if (!(turn.groups(s) >> w & 1u)) continue;
+        if (!(groups.of(s, b) >> w & 1u)) continue;
         if (!mbar_wait_warp(bar(L::S_FULL + w), s_par, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
@@ -374,8 +430,19 @@ __global__ void __launch_bounds__(THREADS, 1)
           continue;
         }
         tc_fence_after();
-        const int key0 = b * BLOCK, cols = min(BLOCK, s.it.n_keys - key0), see = sees - key0;
-        const bool whole = all_see - key0 >= BLOCK;
+        const int key0 = b * BLOCK, cols = min(BLOCK, s.it.pages * a.lay.page - key0);
+        const bool whole = s.it.prefix_keys - key0 >= BLOCK;
+        const bool sees = valid && (prefix > key0 || (own1 > key0 && own0 < key0 + cols && own1 > own0));
+        if (!__any_sync(0xffffffffu, sees)) {  // nothing here for this warp's rows
+          const uint32_t zero[16] = {};
+          for (int c = 0; c < cols; c += 32) tmem_st16(s_col + c / 2, zero);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+          continue;
+        }
+        auto seen = [&](int c) { return bits_in(-key0 - c, prefix - key0 - c) | bits_in(own0 - key0 - c, own1 - key0 - c); };
         float top = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < cols; c += 32) {
@@ -386,8 +453,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
           } else {
+            const uint32_t mask = seen(c);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = c + i < see ? fmaxf(top, __uint_as_float(v[i])) : top;
+            for (int i = 0; i < 32; ++i) top = mask >> i & 1u ? fmaxf(top, __uint_as_float(v[i])) : top;
           }
         }
         top *= scale_log2;
@@ -417,11 +485,12 @@ __global__ void __launch_bounds__(THREADS, 1)
           uint32_t v[32], pk[16];
           tmem_ld32(s_col + c, v);
           tmem_ld_wait();
+          const uint32_t mask = whole ? 0xffffffffu : seen(c);
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             float p = ex2(fmaf(__uint_as_float(v[i]), scale_log2, -base));
-            if (!whole) p = c + i < see ? p : 0.f;
+            if (!whole) p = mask >> i & 1u ? p : 0.f;
             sum[i & 3] += p;
             v[i] = __float_as_uint(p);
           }
@@ -451,7 +520,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           uint32_t v[32];
           tmem_ld32(o_col + c, v);
           tmem_ld_wait();
-          if (valid) {
+          if (valid && l != 0.f) {  // (a NaN is not)
 #pragma unroll
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + c + 4 * i) = uint4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
           }
@@ -491,13 +560,14 @@ __device__ void row_alone(const SharedAttnArgs& a, const Plan& plan, const int4&
     q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
     o[2 * i] = o[2 * i + 1] = 0.f;
   }
-  for (int part = 0; part < 2; ++part) {
-    const int item = part ? rec.z : rec.x;
-    if (item < 0) continue;
-    const Item it = plan.items[item];
-    const int n = part ? min(it.seen + rec.w, it.n_keys) : it.n_keys;
+  const Item it = plan.items[rec.x];
+  for (int k = 0; k < it.n_runs; ++k) {
+    const Run run = plan.runs[it.run + k];
+    const bool prefix = run.token < 0;
+    if (!prefix && (rec.y < run.tok0 || rec.y >= run.tok1)) continue;
+    const int n = prefix ? run.keys : rec.w;
     for (int p = 0; p < n; ++p) {
-      int block = a.tables[static_cast<int64_t>(it.row) * a.lay.max_blocks + p / page];
+      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
       if (block < 0 || block >= a.lay.n_blocks) block = 0;
       const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
       const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
@@ -541,17 +611,11 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_shared_join(SharedAttnArgs 
   float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
   for (int i = 0; i < E; ++i) o[i] = 0.f;
-  bool partly = false;  // the row's own item holds keys that it does not see
-  for (int part = 0; part < 2; ++part) {
-    const int item = part ? rec.z : rec.x, place = part ? rec.w : rec.y;
-    if (item < 0) continue;
-    const Item it = plan.items[item];
-    const uint32_t blocks = blocks_of(it.n_keys);
-    if (blocks == 0) continue;
-    partly |= part && it.seen + place < it.n_keys;
-    const uint32_t b = keys_begin(it, blocks, kvh), rows = it.n_tok * G;
-    const uint32_t parts = ((b + blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
-    const int64_t row0 = plan.part[static_cast<int64_t>(item) * Hkv + kvh] + place * G + h % G;
+  const Item it = plan.items[rec.x];
+  if (it.blocks > 0) {
+    const uint32_t b = blocks_begin(it, kvh), rows = it.n_tok * G;
+    const uint32_t parts = ((b + it.blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
+    const int64_t row0 = plan.part[static_cast<int64_t>(rec.x) * Hkv + kvh] + rec.y * G + h % G;
     for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
       const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
       float top = x.x;
@@ -579,12 +643,11 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) k_shared_join(SharedAttnArgs 
       }
     }
   }
-  if (partly) {
-    bool nan = false;
+  // scores in order, values not: perhaps a value that the row does not see
+  bool nan = false;
 #pragma unroll
-    for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
-    if (__any_sync(0xffffffffu, nan)) row_alone<T, D>(a, plan, rec, t, h, lane, o, m, l);
-  }
+  for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
+  if (l == l && __any_sync(0xffffffffu, nan)) row_alone<T, D>(a, plan, rec, t, h, lane, o, m, l);
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // a NaN stays one
   uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
 #pragma unroll

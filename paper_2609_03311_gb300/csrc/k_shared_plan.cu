@@ -4,6 +4,8 @@
 // One CTA: everything is sums over the step's rows, and the rows of a prefix brought together.  Rows usually come in
 // prefix order; those that do not are sorted (a bitonic network over (prefix, row) in shared memory; rows of a
 // prefix keep their order).  Bound by latency; made once a step and used by every layer.
+#include <limits.h>
+
 #include "shared_attn.cuh"
 
 namespace dopr {
@@ -45,16 +47,16 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   extern __shared__ uint32_t keys[];  // a power of two >= n_seqs
   __shared__ unsigned long long warp_sum[32];
   __shared__ int bad, unsorted;
-  const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
+  const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page, page_blk = BLOCK / page;
   const int tile = tokens_a_tile(G), pair = 2 * tile;
-  const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * a.lay.page;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * page;
   const Plan p = plan_view(a.plan, n, Hkv, G, a.max_tokens);
-  int* sorted = p.scratch;        // rows that read a prefix, by prefix
-  int* place = sorted + n;        // of a sorted entry: tokens of the entries before it
-  int* group = place + n + 1;     // of a prefix: tokens before its first
-  int* group_item = group + n;    // of a prefix: its first item
-  int* own_item = group_item + n; // of a row: its first item
-  int* in_group = own_item + n;   // of a row: its first token's place among its prefix's tokens; -1 if it reads none
+  int* sorted = p.scratch;          // rows with tokens, by group: their prefix, n where there are no prefix keys
+  int* place = sorted + n;          // of a sorted entry: tokens of the entries before it
+  int* group_of = place + n + 1;    // of a sorted entry
+  int* group = group_of + n;        // of a group: tokens before its first
+  int* group_item = group + n + 1;  // of a group: its first item
   if (threadIdx.x == 0) bad = 0, unsorted = 0;
   pdl_wait();
   pdl_trigger();
@@ -67,12 +69,28 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   head.max_tokens = a.max_tokens;
   head.n_ctas = n_ctas;
   head.head_dim = a.lay.head_dim;
+  head.page = page;
   auto tokens_of = [&](int i) { return a.tok_off[i + 1] - a.tok_off[i]; };
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    const int t0 = a.tok_off[i], t1 = a.tok_off[i + 1], pre = a.prefix ? a.prefix[i] : -1;
-    if ((i == 0 && t0 != 0) || t1 < t0 || t1 > a.max_tokens || a.seq_lens[i] < 0 || a.seq_lens[i] > cap || pre < -1 ||
-        pre >= n || pre == i || (pre >= 0 && a.prefix[pre] != -1))
-      bad = 1;
+
+  // checks, and the rows with tokens
+  unsigned long long total;
+  int ns = 0;
+  for (int i0 = 0; i0 < n; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    bool has = false;
+    int g = n;
+    if (i < n) {
+      const int t0 = a.tok_off[i], t1 = a.tok_off[i + 1], pre = a.prefix ? a.prefix[i] : -1, len = a.seq_lens[i];
+      if ((i == 0 && t0 != 0) || t1 < t0 || t1 > a.max_tokens || len < 0 || len > cap || pre < -1 || pre >= n || pre == i ||
+          (pre >= 0 && a.prefix[pre] != -1))
+        bad = 1;
+      else
+        has = t1 > t0;
+      if (has && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
+    }
+    const int at = ns + static_cast<int>(block_exclusive(static_cast<unsigned long long>(has), warp_sum, total));
+    if (has) sorted[at] = i, group_of[at] = g;
+    ns += static_cast<int>(total);
   }
   __syncthreads();
   if (bad) {
@@ -83,28 +101,14 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     for (int c = threadIdx.x; c < MAX_CTAS; c += THREADS) p.first[c] = 0;
     return;
   }
-
-  // rows that read a prefix
-  unsigned long long total;
-  int ns = 0;
-  for (int i0 = 0; i0 < n; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    const int pre = i < n && a.prefix ? a.prefix[i] : -1;
-    const bool reads = pre >= 0 && tokens_of(i) > 0 && a.seq_lens[pre] > 0;
-    const int at = ns + static_cast<int>(block_exclusive(static_cast<unsigned long long>(reads), warp_sum, total));
-    if (reads) sorted[at] = i;
-    if (i < n) in_group[i] = -1;
-    ns += static_cast<int>(total);
-  }
-  __syncthreads();
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
-    if (a.prefix[sorted[i]] < a.prefix[sorted[i - 1]]) unsorted = 1;
+    if (group_of[i] < group_of[i - 1]) unsorted = 1;
   __syncthreads();
   if (unsorted) {
     int m = 2;
     while (m < ns) m <<= 1;
     for (int i = threadIdx.x; i < m; i += THREADS)
-      keys[i] = i < ns ? static_cast<uint32_t>(a.prefix[sorted[i]]) << ROW_BITS | sorted[i] : 0xffffffffu;
+      keys[i] = i < ns ? static_cast<uint32_t>(group_of[i]) << ROW_BITS | sorted[i] : 0xffffffffu;
     for (int k = 2; k <= m; k <<= 1)
       for (int j = k >> 1; j > 0; j >>= 1) {
         __syncthreads();
@@ -117,7 +121,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
         }
       }
     __syncthreads();
-    for (int i = threadIdx.x; i < ns; i += THREADS) sorted[i] = keys[i] & ((1 << ROW_BITS) - 1);
+    for (int i = threadIdx.x; i < ns; i += THREADS) sorted[i] = keys[i] & ((1 << ROW_BITS) - 1), group_of[i] = keys[i] >> ROW_BITS;
     __syncthreads();
   }
   int carry = 0;
@@ -127,83 +131,118 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
     if (i < ns) {
       place[i] = at;
-      const int pre = a.prefix[sorted[i]];
-      if (i == 0 || a.prefix[sorted[i - 1]] != pre) group[pre] = at;
+      if (i == 0 || group_of[i - 1] != group_of[i]) group[group_of[i]] = at;
     }
     carry += static_cast<int>(total);
   }
   if (threadIdx.x == 0) place[ns] = carry;
   __syncthreads();
 
-  // items of prefixes, written by the last row of each; then of own keys, by their rows
+  // items, written by the last row of each group
   int n_items = 0;
   for (int i0 = 0; i0 < ns; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    const int pre = i < ns ? a.prefix[sorted[i]] : -1;
+    const int g = i < ns ? group_of[i] : 0;
     int count = 0, tok = 0;
-    if (i < ns) {
-      in_group[sorted[i]] = place[i] - group[pre];
-      if (i + 1 == ns || a.prefix[sorted[i + 1]] != pre) {
-        tok = place[i + 1] - group[pre];
-        count = (tok + pair - 1) / pair;
-      }
+    if (i < ns && (i + 1 == ns || group_of[i + 1] != g)) {
+      tok = place[i + 1] - group[g];
+      count = (tok + pair - 1) / pair;
     }
     const int at = n_items + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-    if (count > 0) group_item[pre] = at;
+    if (count > 0) group_item[g] = at;
     for (int c = 0; c < count; ++c) {
       Item it{};
-      it.tok = group[pre] + c * pair;
+      it.tok = group[g] + c * pair;
       it.n_tok = min(pair, tok - c * pair);
-      it.row = pre;
-      it.n_keys = a.seq_lens[pre];
-      p.items[at + c] = it;
-    }
-    n_items += static_cast<int>(total);
-  }
-  for (int i0 = 0; i0 < n; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    const int tok = i < n ? tokens_of(i) : 0, len = tok > 0 ? a.seq_lens[i] : 0;
-    const int count = len > 0 ? (tok + pair - 1) / pair : 0;
-    const int at = n_items + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-    if (i < n) own_item[i] = count > 0 ? at : -1;
-    for (int c = 0; c < count; ++c) {
-      Item it{};
-      it.tok = a.tok_off[i] + c * pair;
-      it.n_tok = min(pair, tok - c * pair);
-      it.row = i;
-      it.seen = len - tok + c * pair + 1;
-      it.n_keys = max(0, it.seen + it.n_tok - 1);
-      it.own = 1;
+      it.prefix_keys = g < n ? a.seq_lens[g] : 0;
       p.items[at + c] = it;
     }
     n_items += static_cast<int>(total);
   }
   __syncthreads();
 
-  // every token's items and places, a warp a row
-  for (int i = threadIdx.x >> 5; i < n; i += THREADS / 32) {
-    const int t0 = a.tok_off[i], tok = tokens_of(i), in = in_group[i], own = own_item[i];
-    const int pre = in >= 0 ? a.prefix[i] : 0;
-    for (int j = threadIdx.x & 31; j < tok; j += 32) {
-      int4 r = make_int4(-1, 0, -1, 0);
-      if (in >= 0) {
-        r.x = group_item[pre] + (in + j) / pair;
-        r.y = (in + j) % pair;
-        p.order[group[pre] + in + j] = t0 + j;
+  // runs, by their rows: a row writes its own run in each item that has tokens of it, and the prefix's in each item
+  // that begins with it
+  int n_runs = 0;
+  for (int i0 = 0; i0 < ns; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    int in = 0, tok = 0, k0 = 0, k1 = -1, begun = 0, g = 0;
+    if (i < ns) {
+      g = group_of[i];
+      in = place[i] - group[g];
+      tok = place[i + 1] - place[i];
+      k0 = in / pair;
+      k1 = (in + tok - 1) / pair;
+      begun = k1 - (in + pair - 1) / pair + 1;  // items whose first token is one of the row's
+    }
+    const int count = k1 - k0 + 1 + (g < n ? begun : 0);
+    int at = n_runs + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
+    for (int k = k0; k <= k1; ++k) {
+      Item& it = p.items[group_item[g] + k];
+      const int lo = max(in, k * pair), hi = min(in + tok, (k + 1) * pair);  // places in the group
+      if (lo == k * pair) {
+        it.run = at;
+        if (g < n) {
+          const int keys_ = a.seq_lens[g];
+          p.runs[at++] = Run{g, 0, (keys_ + page - 1) / page, keys_, 0, it.n_tok, -1, 0};
+        }
       }
-      if (own >= 0) {
-        r.z = own + j / pair;
-        r.w = j % pair;
+      const int row = sorted[i], len = a.seq_lens[row];
+      const int seen = max(0, len - (in + tok - hi));  // own keys of its last token here: each token behind it sees one more
+      p.runs[at++] = Run{row, 0, (seen + page - 1) / page, seen, lo - k * pair, hi - k * pair, a.tok_off[row] + lo - in, 0};
+    }
+    n_runs += static_cast<int>(total);
+  }
+  __syncthreads();
+
+  // a warp an item: where its runs' pages begin, and the tokens' records
+  for (int k = warp; k < n_items; k += THREADS / 32) {
+    Item it = p.items[k];
+    it.n_runs = (k + 1 < n_items ? p.items[k + 1].run : n_runs) - it.run;
+    int pages = 0, end0 = 0, begin1 = INT_MAX;
+    for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
+      const int r = r0 + lane;
+      Run run{};
+      if (r < it.n_runs) run = p.runs[it.run + r];
+      int inc = run.pages;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += u;
       }
-      p.rec[t0 + j] = r;
+      const int off = pages + inc - run.pages;
+      if (r < it.n_runs) {
+        p.runs[it.run + r].off = off;
+        if (run.tok0 < tile) end0 = max(end0, off + run.pages);
+        if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
+        const int seen1 = run.keys - (run.tok1 - run.tok0);  // + 1 for the first token, and so on
+        for (int x = run.tok0; run.token >= 0 && x < run.tok1; ++x) {
+          const int t = run.token + x - run.tok0;
+          p.order[it.tok + x] = t;
+          // a row with more new tokens than keys: its first tokens see none, however many those of its last are
+          p.rec[t] = make_int4(k, x, off * page, max(0, run.keys > 0 ? seen1 + x - run.tok0 + 1 : 0));
+        }
+      }
+      pages += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    end0 = __reduce_max_sync(0xffffffffu, end0);
+    begin1 = __reduce_min_sync(0xffffffffu, begin1);
+    if (lane == 0) {
+      it.pages = pages;
+      it.blocks = (pages + page_blk - 1) / page_blk;
+      it.end0 = (end0 + page_blk - 1) / page_blk;
+      it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
+      it.begin1 = begin1 / page_blk;
+      p.items[k] = it;
     }
   }
+  __syncthreads();
 
   // the line
   unsigned long long line = 0;
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    const uint32_t blocks = i < n_items ? blocks_of(p.items[i].n_keys) : 0;
+    const uint32_t blocks = i < n_items ? p.items[i].blocks : 0;
     const unsigned long long cost = blocks > 0 ? static_cast<unsigned long long>(Hkv) * (blocks + OVERHEAD) : 0;
     const unsigned long long at = line + block_exclusive(cost, warp_sum, total);
     if (i < n_items) p.items[i].cost = static_cast<uint32_t>(at);
@@ -232,9 +271,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     unsigned long long count = 0;
     if (f < n_flat) {
       const Item it = p.items[f / Hkv];
-      const uint32_t blocks = blocks_of(it.n_keys);
-      if (blocks > 0) {
-        const uint32_t b = keys_begin(it, blocks, f % Hkv), e = b + blocks, start = b - OVERHEAD;
+      if (it.blocks > 0) {
+        const uint32_t b = blocks_begin(it, f % Hkv), e = b + it.blocks, start = b - OVERHEAD;
         const uint32_t segs = (e - 1) / share - b / share + 1;
         count = static_cast<unsigned long long>(segs) * it.n_tok * G * (two_tiles(it.n_tok, G) ? 1 : 2);
         for (uint32_t c = (start + share - 1) / share; static_cast<unsigned long long>(c) * share < e; ++c)

@@ -483,6 +483,36 @@ def test_attention_of_infinite_and_nan_inputs_stays_in_its_rows():
     assert not bool(torch.isnan(got[0][2]).any())
 
 
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_rows_are_not_touched_by_values_that_only_others_see(bad, d):
+    # the last own value of one row is bad: its last token alone sees it, not its others, nor rows beside it
+    b = Batch(4, 2, d, BF, 16, [50], [(0, 20, 5), (0, 30, 2), (0, 9, 9)], seed=6)
+    want = b.run()
+    b.check(want)
+    at = 19
+    b.v[int(b.tables[1, at // 16]), 1, at % 16] = bad
+    got = b.run()
+    other = torch.ones(b.T, dtype=torch.bool, device=DEV)
+    other[4] = False
+    u = torch.finfo(BF).eps / 2
+    # the rows beside are computed alone, in another order and without rounded probabilities
+    assert bool(((got[0] - want[0]).double().abs()[other] <= (3 * u + 2.0 ** -10) * b.exact()[2][other] + 2.0 ** -24).all())
+    assert torch.equal(got[0][4, :2], want[0][4, :2]) and not bool(torch.isfinite(got[0][4, 2:]).any())
+    assert bool(((got[1] - want[1]).abs() <= 2.0 ** -11).all())
+
+
+def test_attention_refuses_a_plan_of_other_sizes():
+    b = Batch(4, 2, 64, HF, 16, [20], [(0, 5, 2), (0, 6, 1)], seed=1)
+    plan = dopr.shared_attention_plan(b.layout, b.hq, *b.args())
+    room = torch.zeros(plan.numel() * 4, dtype=torch.uint8, device=DEV)
+    room[:plan.numel()] = plan
+    st, q = word(), torch.cat([b.q, b.q])
+    out = torch.full_like(q, 7.0)
+    dopr.shared_attention(b.layout, room, q, b.k, b.v, i32(b.tables), out=out, status=st)
+    assert st.item() == dopr.ERR_INVALID_ARG and bool((out == 7).all())
+
+
 def test_attention_scale_and_strided_views():
     b = Batch(8, 2, 64, HF, 32, [400], [(0, 20, 7), (0, 9, 9)], seed=4)
     want = b.run(scale=0.31)

@@ -29,7 +29,8 @@ namespace {
 using namespace shared_attn;
 
 constexpr int THREADS = 128 + 2 * 128;
-constexpr uint32_t TMEM_COLS = 512, S_COL = 0, O_COL = 256;  // group w: S at S_COL + 128 w, O at O_COL + 128 w
+// group w: S at S_COL + 128 w, P over its upper half, O at O_COL + 128 w
+constexpr uint32_t TMEM_COLS = 512, S_COL = 0, P_COL = 64, O_COL = 256;
 constexpr float RESCALE_LOG2 = 8.f;
 constexpr int HALF_BYTES = 128 * 128;  // 128 rows of 64 16-bit elements
 
@@ -41,8 +42,8 @@ struct Smem {
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;
   static constexpr int OFF_V = OFF_K + K_STAGES * TILE_BYTES;
-  static constexpr int OFF_TOK = OFF_V + V_STAGES * TILE_BYTES;  // the Q gatherer's tokens
-  static constexpr int OFF_BAR = OFF_TOK + 128 * 4;
+  static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // where the Q gatherer's rows lie
+  static constexpr int OFF_BAR = OFF_ROW + 128 * 8;
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
                        O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
@@ -79,6 +80,18 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// Two at once: a * b + c, a + b.
+__device__ __forceinline__ void fma2(float& x, float& y, float ax, float ay, float b, float c) {
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%5, %5};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(x), "=f"(y)
+      : "f"(ax), "f"(ay), "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float bx, float by) {
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "+f"(x), "+f"(y)
+      : "f"(bx), "f"(by));
 }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -168,6 +181,40 @@ struct PageCursor {
     while (page >= run.off + run.pages && at + 1 < n_runs) run = runs[++at];
   }
 };
+// Waits for the loads from tensor memory before it; the values pass through, so that nothing that uses them moves ahead.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]),
+                 "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]),
+                 "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
+                 "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
+// 32 columns of S, those that the row does not see at -inf; the columns' maximum joins top.
+template <bool WHOLE>
+__device__ __forceinline__ void mask_max(uint32_t (&v)[32], uint32_t seen, float& top) {
+  float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    if (!WHOLE && !(seen >> i & 1u)) v[i] = __float_as_uint(-INFINITY);
+    t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
+  }
+  top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+}
+// 2^(s scale - base) of 32 columns as pairs of T, their sum in sum.
+template <typename T, bool MASK>
+__device__ __forceinline__ void exp_pack(const uint32_t (&v)[32], uint32_t seen, float scale_log2, float base, float (&sum)[4],
+                                         uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    float x = __uint_as_float(v[i]), y = __uint_as_float(v[i + 1]);
+    if (MASK) x = seen >> i & 1u ? x : -INFINITY, y = seen >> (i + 1) & 1u ? y : -INFINITY;
+    fma2(x, y, x, y, scale_log2, -base);
+    x = ex2(x), y = ex2(y);  // unseen: 2^-inf, nothing
+    add2(sum[i & 2], sum[(i & 2) + 1], x, y);
+    pk[i / 2] = pack2<T>(x, y);
+  }
+}
+
 // Bits [lo, hi) of a word, the range clipped to it.
 __device__ __forceinline__ uint32_t bits_in(int lo, int hi) {
   lo = max(lo, 0);
@@ -271,39 +318,46 @@ __global__ void __launch_bounds__(THREADS, 1)
       int stage, cols;
       uint32_t phase, flags;  // flags: 1 first of the group's segment, 2 last of it, 4 last use of the V stage, 8 its first
       int keys;               // this lane's page of the block: rows that hold keys
+      bool there;             // V has been seen to be
     } pend0{}, pend1{};
     int oldest = 0, next_oldest = 0, n_pend = 0;  // groups
-    uint32_t p_par = 0, q_par = 0;  // a bit a group
+    uint32_t p_par = 0, q_par = 0;                // a bit a group
+    constexpr uint32_t idesc_o = umma_idesc_f16_bmn(TILE, D) | type_bits<T>();
+    const uint64_t v_desc0 = umma_desc_sw128_mn(sV, HALF_BYTES, 1024), k_desc0 = umma_desc_sw128(sK), q_desc0 = umma_desc_sw128(sQ);
     auto issue_pv = [&]() -> bool {
       const int w = oldest;
       const Pending x = w ? pend1 : pend0;
       oldest = next_oldest;
       --n_pend;
-      if (!wait(L::V_FULL + x.stage, x.phase)) return false;
-      const int steps = x.cols / 16;
-      const uint32_t v0 = sV + x.stage * L::TILE_BYTES;
-      uint32_t ragged = __ballot_sync(0xffffffffu, x.keys < page) & ((1u << page_blk) - 1u) & ((1u << x.cols / page) - 1u);
-      if ((x.flags & 8u) && ragged) {
-        while (ragged) {  // rows past a page's keys count as zero
-          const int pg = __ffs(ragged) - 1, from = __shfl_sync(0xffffffffu, x.keys, pg);
-          ragged &= ragged - 1;
-          for (int i = lane; i < (page - from) * 8 * L::HALVES; i += 32) {
-            const int row = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
-            *reinterpret_cast<uint4*>(smem + (v0 - s0) + (c >> 3) * HALF_BYTES + row * 128 + (c & 7) * 16) = uint4{0, 0, 0, 0};
+      if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) return false;
+      if (x.flags & 8u) {
+        if (__any_sync(0xffffffffu, x.keys < page)) {
+          uint32_t ragged = __ballot_sync(0xffffffffu, x.keys < page) & ((1u << page_blk) - 1u) & ((1u << x.cols / page) - 1u);
+          while (ragged) {  // rows past a page's keys count as zero
+            const int pg = __ffs(ragged) - 1, from = __shfl_sync(0xffffffffu, x.keys, pg);
+            ragged &= ragged - 1;
+            for (int i = lane; i < (page - from) * 8 * L::HALVES; i += 32) {
+              const int row = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
+              *reinterpret_cast<uint4*>(smem + L::OFF_V + x.stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + row * 128 +
+                                        (c & 7) * 16) = uint4{0, 0, 0, 0};
+            }
           }
+          fence_proxy_async_shared();
+          __syncwarp();
         }
-        fence_proxy_async_shared();
-        __syncwarp();
       }
+      const uint64_t vd = v_desc0 + x.stage * (L::TILE_BYTES / 16);
+      const uint32_t o = tmem + O_COL + 128 * w, pc = tmem + P_COL + 128 * w;
       if (!wait(L::P_FULL + w, p_par >> w & 1u)) return false;
       p_par ^= 1u << w;
       tc_fence_after();
-      const uint64_t vd = umma_desc_sw128_mn(v0, HALF_BYTES, 1024);
-      constexpr uint32_t idesc = umma_idesc_f16_bmn(TILE, D) | type_bits<T>();
       if (one) {
-        for (int k = 0; k < steps; ++k)
-          umma_f16_ts(tmem + O_COL + 128 * w, tmem + S_COL + 128 * w + 8 * k, vd + (k * 2048) / 16, idesc,
-                      !(x.flags & 1u) || k > 0);
+        if (x.cols == BLOCK) {
+#pragma unroll
+          for (int k = 0; k < BLOCK / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & 1u));
+        } else {
+          for (int k = 0; k < x.cols / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & 1u));
+        }
         if (x.flags & 4u) umma_commit(bar(L::V_EMPTY + x.stage));
         if (x.flags & 2u) umma_commit(bar(L::O_FULL + w));
       }
@@ -318,37 +372,44 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int first_page = b * page_blk, cols = min(page_blk, s.it.pages - first_page) * page;
         const int my_page = first_page + lane % page_blk;
         int keys = page;
-        if (my_page < s.it.pages) {
+        if (static_cast<int>(b + 1) * BLOCK > s.it.prefix_keys && my_page < s.it.pages) {
           cur.go(my_page);
           keys = min(page, cur.run.keys - (my_page - cur.run.off) * page);
         }
+        const uint32_t idesc = umma_idesc_f16(TILE, cols) | type_bits<T>();
+        const uint64_t kd = k_desc0 + rk.stage * (L::TILE_BYTES / 16);
         for (int w = 0; w < 2 && ok; ++w) {
           if (!(takes >> w & 1u)) continue;
+          const bool first = !(begun >> w & 1u);
+          const bool last = last_block(s, b, w), first_use = w == 0 || takes == 2u, last_use = w == 1 || takes == 1u;
+          const uint64_t qd = q_desc0 + w * (L::TILE_BYTES / 16);
+          const uint32_t sd = tmem + S_COL + 128 * w;
+          // whether operands are there is asked while products run, not between them: K here, ahead of the wait for the
+          // softmax, V after S has been issued
+          bool there = !first_use || mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
+          if (first) there = there && mbar_test_warp(bar(L::Q_FULL + w), q_par >> w & 1u);
           while (ok && ((n_pend > 0 && oldest == w) || (n_pend > 1 && next_oldest == w))) issue_pv();
           if (!ok) break;
-          const bool first = !(begun >> w & 1u);
-          if (first) {
-            if (!wait(L::Q_FULL + w, q_par >> w & 1u)) break;
-            q_par ^= 1u << w;
-            begun |= 1u << w;
+          if (!there) {
+            if (first && !wait(L::Q_FULL + w, q_par >> w & 1u)) break;
+            if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
           }
-          if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
+          if (first) q_par ^= 1u << w;
+          begun |= 1u << w;
           tc_fence_after();
-          const bool last = last_block(s, b, w), first_use = w == 0 || takes == 2u, last_use = w == 1 || takes == 1u;
-          const uint64_t qd = umma_desc_sw128(sQ + w * L::TILE_BYTES), kd = umma_desc_sw128(sK + rk.stage * L::TILE_BYTES);
-          const uint32_t idesc = umma_idesc_f16(TILE, cols) | type_bits<T>();
           if (one) {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
               const int off = ((k >> 2) * HALF_BYTES + (k & 3) * 32) / 16;
-              umma_f16(tmem + S_COL + 128 * w, qd + off, kd + off, idesc, k > 0);
+              umma_f16(sd, qd + off, kd + off, idesc, k > 0);
             }
             umma_commit(bar(L::S_FULL + w));
             if (last_use) umma_commit(bar(L::K_EMPTY + rk.stage));
             if (last) umma_commit(bar(L::Q_EMPTY + w));
           }
           (w ? pend1 : pend0) = Pending{rv.stage, cols, rv.phase,
-                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (first_use ? 8u : 0u), keys};
+                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (first_use ? 8u : 0u), keys,
+                                        mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase)};
           (n_pend++ ? next_oldest : oldest) = w;
         }
         rk.next(L::K_STAGES);
@@ -360,7 +421,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     mbar_wait_warp(bar(L::DRAIN), 0, err, ok ? WAIT_TIMEOUT_NS : 100000000ull);
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
-    int* tok = reinterpret_cast<int*>(smem + L::OFF_TOK);
+    const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);
     Groups groups;
     uint32_t used = 0, par = 0;
     bool ok = true;
@@ -369,9 +430,11 @@ __global__ void __launch_bounds__(THREADS, 1)
       const uint32_t takes = groups.any(s);
       for (int w = 0; w < 2 && ok; ++w) {
         if (!(takes >> w & 1u)) continue;
-        const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
+        const int t0 = s.two ? w * TT : 0, rows = min(TT, s.it.n_tok - t0) * G;
         __syncwarp();
-        for (int i = lane; i < n; i += 32) tok[i] = plan.order[s.it.tok + t0 + i];
+        for (int r = lane; r < rows; r += 32)
+          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(plan.order[s.it.tok + t0 + r / G]) * a.q_tok +
+                                                  static_cast<int64_t>(s.h * G + r % G) * a.q_head);
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
@@ -379,12 +442,19 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (used >> w & 1u) par ^= 1u << w;
         used |= 1u << w;
-        constexpr int CHUNKS = D / 8;  // 16-byte pieces of a row
-        const int pieces = n * G * CHUNKS;
-        for (int i = lane; i < pieces; i += 32) {
-          const int r = i / CHUNKS, c = i % CHUNKS;
-          const T* src = q + static_cast<int64_t>(tok[r / G]) * a.q_tok + static_cast<int64_t>(s.h * G + r % G) * a.q_head + c * 8;
-          cp_async16(s0 + L::OFF_Q + w * L::TILE_BYTES + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, true);
+        // a lane a 16-byte piece of the row, 32 / CHUNKS rows at once
+        constexpr int CHUNKS = D / 8, STEP = 32 / CHUNKS;
+        const int c = lane % CHUNKS;
+        const uint32_t dst = s0 + L::OFF_Q + w * L::TILE_BYTES + (c >> 3) * HALF_BYTES;
+        for (int r0 = lane / CHUNKS; r0 < rows; r0 += 8 * STEP) {
+          const uint4* src[8];  // eight addresses before the first copy: a copy is not waited for, an address is
+#pragma unroll
+          for (int i = 0; i < 8; ++i) src[i] = r0 + i * STEP < rows ? row[r0 + i * STEP] : nullptr;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = r0 + i * STEP;
+            if (r < rows) cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), src[i] + c, true);
+          }
         }
         cp_async_commit();
         cp_async_wait_all();
@@ -435,29 +505,38 @@ __global__ void __launch_bounds__(THREADS, 1)
         const bool sees = valid && (prefix > key0 || (own1 > key0 && own0 < key0 + cols && own1 > own0));
         if (!__any_sync(0xffffffffu, sees)) {  // nothing here for this warp's rows
           const uint32_t zero[16] = {};
-          for (int c = 0; c < cols; c += 32) tmem_st16(s_col + c / 2, zero);
+          for (int c = 0; c < 64; c += 16) tmem_st16(s_col + 64 + c, zero);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
           continue;
         }
-        auto seen = [&](int c) { return bits_in(-key0 - c, prefix - key0 - c) | bits_in(own0 - key0 - c, own1 - key0 - c); };
+        // S is read twice, 32 columns at a time with the next ones on their way: first for the maximum, upwards, then
+        // for P, downwards, where the last 64 are still held.  P of columns [32 c, 32 c + 32) goes to 64 + 16 c, over
+        // columns that are read by then.  (Columns past the block's last hold anything; no row sees them.)
+        uint32_t va[32], vb[32], pk[16];
+        auto seen = [&](int c) {
+          const int at = key0 + 32 * c;
+          return bits_in(-at, prefix - at) | bits_in(own0 - at, own1 - at);
+        };
         float top = -INFINITY;
-#pragma unroll 1
-        for (int c = 0; c < cols; c += 32) {
-          uint32_t v[32];
-          tmem_ld32(s_col + c, v);
-          tmem_ld_wait();
-          if (whole) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
-          } else {
-            const uint32_t mask = seen(c);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = mask >> i & 1u ? fmaxf(top, __uint_as_float(v[i])) : top;
-          }
-        }
+        auto maximum = [&](auto w_) {
+          constexpr bool W = decltype(w_)::value;
+          tmem_ld32(s_col, va);
+          tmem_ld_wait_for(va);
+          tmem_ld32(s_col + 32, vb);
+          mask_max<W>(va, W ? 0 : seen(0), top);
+          tmem_ld_wait_for(vb);
+          tmem_ld32(s_col + 64, va);
+          mask_max<W>(vb, W ? 0 : seen(1), top);
+          tmem_ld_wait_for(va);
+          tmem_ld32(s_col + 96, vb);
+          mask_max<W>(va, W ? 0 : seen(2), top);
+          tmem_ld_wait_for(vb);
+          mask_max<W>(vb, W ? 0 : seen(3), top);
+        };
+        if (whole) maximum(std::true_type{}); else maximum(std::false_type{});
         top *= scale_log2;
         if (m == -INFINITY) m = top;  // nothing but zeros has been summed
         const bool grow = top > m + RESCALE_LOG2;
@@ -470,7 +549,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int c = 0; c < D; c += 32) {
             uint32_t v[32], x[16];
             tmem_ld32(o_col + c, v);
-            tmem_ld_wait();
+            tmem_ld_wait_for(v);
 #pragma unroll
             for (int k = 0; k < 32; k += 16) {
 #pragma unroll
@@ -480,25 +559,24 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
         const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 1
-        for (int c = 0; c < cols; c += 32) {
-          uint32_t v[32], pk[16];
-          tmem_ld32(s_col + c, v);
-          tmem_ld_wait();
-          const uint32_t mask = whole ? 0xffffffffu : seen(c);
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float p = ex2(fmaf(__uint_as_float(v[i]), scale_log2, -base));
-            if (!whole) p = mask >> i & 1u ? p : 0.f;
-            sum[i & 3] += p;
-            v[i] = __float_as_uint(p);
-          }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-#pragma unroll
-          for (int i = 0; i < 16; ++i) pk[i] = pack2<T>(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-          tmem_st16(s_col + c / 2, pk);
-        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        auto powers = [&](auto m_) {
+          constexpr bool M = decltype(m_)::value;
+          exp_pack<T, false>(vb, 0, scale_log2, base, sum, pk);
+          tmem_ld32(s_col + 32, vb);
+          tmem_st16(s_col + 112, pk);
+          exp_pack<T, false>(va, 0, scale_log2, base, sum, pk);
+          tmem_ld_wait_for(vb);
+          tmem_ld32(s_col, va);
+          tmem_st16(s_col + 96, pk);
+          exp_pack<T, M>(vb, M ? seen(1) : 0, scale_log2, base, sum, pk);
+          tmem_ld_wait_for(va);
+          tmem_st16(s_col + 80, pk);
+          exp_pack<T, M>(va, M ? seen(0) : 0, scale_log2, base, sum, pk);
+          tmem_st16(s_col + 64, pk);
+        };
+        if (whole) powers(std::false_type{}); else powers(std::true_type{});
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -519,7 +597,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         for (int c = 0; c < D; c += 32) {
           uint32_t v[32];
           tmem_ld32(o_col + c, v);
-          tmem_ld_wait();
+          tmem_ld_wait_for(v);
           if (valid && l != 0.f) {  // (a NaN is not)
 #pragma unroll
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + c + 4 * i) = uint4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};

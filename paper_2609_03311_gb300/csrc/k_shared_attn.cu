@@ -363,11 +363,79 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       return true;
     };
+    // One group's P V of an earlier block and S of a later one, all columns whole, the products back to back: the issuing
+    // warp has few instruction slots beside the softmax, and a commit returns when the products before it are under way,
+    // so what can be found out about the next step is, before the commits (`ahead`).
+    auto step = [&](uint32_t w, int v_stage, bool acc, int k_stage, bool k_there, uint32_t k_phase, bool free_v, bool free_k, auto ahead) {
+      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
+      p_par ^= 1u << w;
+      tc_fence_after();
+      const uint32_t o = tmem + O_COL + 128 * w, sd = tmem + S_COL + 128 * w;
+      const uint64_t vd = v_desc0 + v_stage * (L::TILE_BYTES / 16), kd = k_desc0 + k_stage * (L::TILE_BYTES / 16),
+                     qd = q_desc0 + w * (L::TILE_BYTES / 16);
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < BLOCK / 16; ++k) umma_f16_ts(o, sd + (P_COL - S_COL) + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || acc);
+      }
+      if (!k_there) {
+        if (!wait(L::K_FULL + k_stage, k_phase)) return;
+        tc_fence_after();
+      }
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const int off = ((k >> 2) * HALF_BYTES + (k & 3) * 32) / 16;
+          umma_f16(sd, qd + off, kd + off, umma_idesc_f16(TILE, BLOCK) | type_bits<T>(), k > 0);
+        }
+      }
+      ahead();
+      if (one) {
+        umma_commit(bar(L::S_FULL + w));
+        if (free_v) umma_commit(bar(L::V_EMPTY + v_stage));
+        if (free_k) umma_commit(bar(L::K_EMPTY + k_stage));
+      }
+    };
     while (ok && walk.next(s)) {
       PageCursor cur;
       cur.seek(plan, s.it, s.b0 * page_blk + lane % page_blk);
       uint32_t begun = 0;
+      // whole blocks of the prefix, but for each group's first and last, which the general steps take
+      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.it.prefix_keys) / BLOCK), margin = s.two ? 1 : 2, head = s.b0 + margin;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
+        if (b == head && b + margin < whole) {
+          Pending x = oldest ? pend1 : pend0, y = oldest ? pend0 : pend1;  // of two tiles: the same block
+          bool k_there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
+          for (; b + margin < whole && ok; ++b) {
+            bool v_there = false;
+            auto ahead = [&] { v_there = mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase); };
+            if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) break;
+            if (s.two) {
+              step(0, x.stage, !(x.flags & 1u), rk.stage, k_there, rk.phase, false, false, [] {});
+              if (ok) step(1, x.stage, !(x.flags & 1u), rk.stage, true, 0, true, true, ahead);
+              x = Pending{rv.stage, BLOCK, rv.phase, 0, page, v_there};
+            } else {
+              step(oldest, x.stage, !(x.flags & 1u), rk.stage, k_there, rk.phase, true, true, ahead);
+              x = y;
+              y = Pending{rv.stage, BLOCK, rv.phase, 12u, page, v_there};
+              oldest ^= 1;
+              groups.turn ^= 1u;
+            }
+            rk.next(L::K_STAGES);
+            rv.next(L::V_STAGES);
+            k_there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
+          }
+          if (!ok) break;
+          if (s.two) {
+            x.flags &= 1u;
+            pend0 = pend1 = x;
+            pend0.flags |= 8u;
+            pend1.flags |= 4u;
+          } else {
+            (oldest ? pend1 : pend0) = x;
+            (oldest ? pend0 : pend1) = y;
+            next_oldest = oldest ^ 1;
+          }
+        }
         const uint32_t takes = groups.of(s, b);
         const int first_page = b * page_blk, cols = min(page_blk, s.it.pages - first_page) * page;
         const int my_page = first_page + lane % page_blk;

@@ -43,11 +43,13 @@ struct Smem {
   static constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;
   static constexpr int OFF_V = OFF_K + K_STAGES * TILE_BYTES;
   static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // where the Q gatherer's rows lie
-  static constexpr int OFF_BAR = OFF_ROW + 128 * 8;
+  static constexpr int OFF_KEYS = OFF_ROW + 128 * 8;  // of each page of a V stage: rows that hold keys
+  static constexpr int OFF_BAR = OFF_KEYS + 64;
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
                        O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
   static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
+  static_assert(V_STAGES * 8 <= 64, "a byte a page");
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
@@ -93,6 +95,12 @@ __device__ __forceinline__ void add2(float& x, float& y, float bx, float by) {
       : "+f"(x), "+f"(y)
       : "f"(bx), "f"(by));
 }
+// Shares of the launch's registers (384 threads x 168): little for the warps that copy and issue, more where rows of S
+// are held.
+constexpr int REGS_FEW = 152, REGS_MANY = 176;
+static_assert(128 * REGS_FEW + 256 * REGS_MANY <= 384 * 168, "more registers than the launch has are waited for without end");
+__device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW)); }
+__device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY)); }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // One segment after another of this CTA's share.
@@ -189,27 +197,20 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
                  "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]),
                  "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
 }
-// 32 columns of S, those that the row does not see at -inf; the columns' maximum joins top.
-template <bool WHOLE>
-__device__ __forceinline__ void mask_max(uint32_t (&v)[32], uint32_t seen, float& top) {
+__device__ __forceinline__ void max32(const uint32_t (&v)[32], float& top) {
   float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    if (!WHOLE && !(seen >> i & 1u)) v[i] = __float_as_uint(-INFINITY);
-    t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
-  }
+  for (int i = 0; i < 32; ++i) t[i & 3] = fmaxf(t[i & 3], __uint_as_float(v[i]));
   top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
 }
 // 2^(s scale - base) of 32 columns as pairs of T, their sum in sum.
-template <typename T, bool MASK>
-__device__ __forceinline__ void exp_pack(const uint32_t (&v)[32], uint32_t seen, float scale_log2, float base, float (&sum)[4],
-                                         uint32_t (&pk)[16]) {
+template <typename T>
+__device__ __forceinline__ void exp_pack(const uint32_t (&v)[32], float scale_log2, float base, float (&sum)[4], uint32_t (&pk)[16]) {
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    float x = __uint_as_float(v[i]), y = __uint_as_float(v[i + 1]);
-    if (MASK) x = seen >> i & 1u ? x : -INFINITY, y = seen >> (i + 1) & 1u ? y : -INFINITY;
-    fma2(x, y, x, y, scale_log2, -base);
-    x = ex2(x), y = ex2(y);  // unseen: 2^-inf, nothing
+    float x, y;
+    fma2(x, y, __uint_as_float(v[i]), __uint_as_float(v[i + 1]), scale_log2, -base);
+    x = ex2(x), y = ex2(y);
     add2(sum[i & 2], sum[(i & 2) + 1], x, y);
     pk[i / 2] = pack2<T>(x, y);
   }
@@ -260,6 +261,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (warp == 0 || warp == 2) {
     // ======================= K and V blocks, page by page: a lane a page and half of the head
+    regs_few();
     const bool is_v = warp == 2;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
     const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL,
@@ -290,6 +292,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           break;
         }
         const uint32_t fb = bar(full + r.stage);
+        if (is_v && mine && half == 0)
+          smem[L::OFF_KEYS + r.stage * 8 + pg] = static_cast<uint8_t>(min(page, cur.run.keys - (first + pg - cur.run.off) * page));
+        __syncwarp();
         if (lane == 0) mbar_arrive_expect_tx(fb, pages * page * 128 * L::HALVES);
         __syncwarp();
         if (mine)
@@ -306,67 +311,92 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
   } else if (warp == 1) {
     // ======================= MMA issuer
+    regs_few();
     const bool one = elect_one();
     const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
     const int page = a.lay.page, page_blk = BLOCK / page;
-    Ring rk, rv;
     Groups groups;
     bool ok = true;
     auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
-    // products P V that wait for their softmax, oldest first; at most one a group
-    struct Pending {
-      int stage, cols;
-      uint32_t phase, flags;  // flags: 1 first of the group's segment, 2 last of it, 4 last use of the V stage, 8 its first
-      int keys;               // this lane's page of the block: rows that hold keys
-      bool there;             // V has been seen to be
-    } pend0{}, pend1{};
-    int oldest = 0, next_oldest = 0, n_pend = 0;  // groups
-    uint32_t p_par = 0, q_par = 0;                // a bit a group
     constexpr uint32_t idesc_o = umma_idesc_f16_bmn(TILE, D) | type_bits<T>();
     const uint64_t v_desc0 = umma_desc_sw128_mn(sV, HALF_BYTES, 1024), k_desc0 = umma_desc_sw128(sK), q_desc0 = umma_desc_sw128(sQ);
-    auto issue_pv = [&]() -> bool {
-      const int w = oldest;
+    uint32_t p_par = 0, q_par = 0;  // a bit a group
+
+    // products P V that wait for their softmax, oldest first; at most one a group
+    enum : uint32_t { FIRST = 1, LAST = 2, FREE_V = 4, FREE_K = 8 };
+    struct Pending {
+      int stage, cols;
+      uint32_t phase, flags;  // FIRST, LAST of the group's segment, FREE_V: last use of the stage
+      bool there;             // V has been seen to be
+    } pend0{}, pend1{};
+    uint32_t oldest = 0;
+    int n_pend = 0;
+    // what the oldest frees: committed with the S behind it
+    int freed[2] = {-1, -1}, ended = 0;  // V stages; a bit a group whose O is whole
+    auto issue_pv = [&] {
+      const uint32_t w = oldest;
       const Pending x = w ? pend1 : pend0;
-      oldest = next_oldest;
+      oldest ^= 1u;
       --n_pend;
-      if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) return false;
-      if (x.flags & 8u) {
-        if (__any_sync(0xffffffffu, x.keys < page)) {
-          uint32_t ragged = __ballot_sync(0xffffffffu, x.keys < page) & ((1u << page_blk) - 1u) & ((1u << x.cols / page) - 1u);
-          while (ragged) {  // rows past a page's keys count as zero
-            const int pg = __ffs(ragged) - 1, from = __shfl_sync(0xffffffffu, x.keys, pg);
-            ragged &= ragged - 1;
-            for (int i = lane; i < (page - from) * 8 * L::HALVES; i += 32) {
-              const int row = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
-              *reinterpret_cast<uint4*>(smem + L::OFF_V + x.stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + row * 128 +
-                                        (c & 7) * 16) = uint4{0, 0, 0, 0};
-            }
-          }
-          fence_proxy_async_shared();
-          __syncwarp();
-        }
-      }
-      const uint64_t vd = v_desc0 + x.stage * (L::TILE_BYTES / 16);
-      const uint32_t o = tmem + O_COL + 128 * w, pc = tmem + P_COL + 128 * w;
-      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return false;
+      if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) return;
+      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
       p_par ^= 1u << w;
       tc_fence_after();
+      const uint64_t vd = v_desc0 + x.stage * (L::TILE_BYTES / 16);
+      const uint32_t o = tmem + O_COL + 128 * w, pc = tmem + P_COL + 128 * w;
+      if (one)
+        for (int k = 0; k < x.cols / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & FIRST));
+      if (x.flags & FREE_V) freed[freed[0] >= 0] = x.stage;
+      if (x.flags & LAST) ended |= 1 << w;
+    };
+    auto commit_pv = [&] {
       if (one) {
-        if (x.cols == BLOCK) {
-#pragma unroll
-          for (int k = 0; k < BLOCK / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & 1u));
-        } else {
-          for (int k = 0; k < x.cols / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & 1u));
-        }
-        if (x.flags & 4u) umma_commit(bar(L::V_EMPTY + x.stage));
-        if (x.flags & 2u) umma_commit(bar(L::O_FULL + w));
+        if (ended & 1) umma_commit(bar(L::O_FULL));
+        if (ended & 2) umma_commit(bar(L::O_FULL + 1));
+        if (freed[0] >= 0) umma_commit(bar(L::V_EMPTY + freed[0]));
+        if (freed[1] >= 0) umma_commit(bar(L::V_EMPTY + freed[1]));
       }
-      return true;
+      freed[0] = freed[1] = -1;
+      ended = 0;
+    };
+    // the next S: a block and a group that takes it
+    Ring rk, rv;
+    uint32_t b = 0, takes = 0, begun = 0;
+    struct Next {
+      uint32_t w, flags;
+      int cols;
+      bool valid, there;  // there: K, and Q where it is the first, have been seen to be
+    } n{};
+    bool in_segment = false, any_block = false;
+    auto look = [&] {
+      if (takes == 0) {
+        if (!in_segment || ++b == s.b1) {
+          n.valid = in_segment = walk.next(s);
+          if (!n.valid) return;
+          b = s.b0;
+          begun = 0;
+        }
+        if (any_block) {
+          rk.next(L::K_STAGES);
+          rv.next(L::V_STAGES);
+        }
+        any_block = true;
+        takes = groups.of(s, b);
+        n.cols = min(page_blk, s.it.pages - static_cast<int>(b) * page_blk) * page;
+      }
+      n.w = takes & 1u ? 0 : 1;
+      takes &= ~(1u << n.w);
+      n.flags = (begun >> n.w & 1u ? 0 : FIRST) | (last_block(s, b, n.w) ? LAST : 0) | (takes == 0 ? FREE_V | FREE_K : 0);
+      begun |= 1u << n.w;
+      n.there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
+      if (n.there && (n.flags & FIRST)) n.there = mbar_test_warp(bar(L::Q_FULL + n.w), q_par >> n.w & 1u);
+      n.valid = true;
     };
     // One group's P V of an earlier block and S of a later one, all columns whole, the products back to back: the issuing
     // warp has few instruction slots beside the softmax, and a commit returns when the products before it are under way,
-    // so what can be found out about the next step is, before the commits (`ahead`).
-    auto step = [&](uint32_t w, int v_stage, bool acc, int k_stage, bool k_there, uint32_t k_phase, bool free_v, bool free_k, auto ahead) {
+    // so what can be found out about the next step is, before the commits.
+    bool v_there = false;
+    auto step = [&](uint32_t w, int v_stage, bool acc, int k_stage, bool k_there, uint32_t k_phase, bool frees) {
       if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
       p_par ^= 1u << w;
       tc_fence_after();
@@ -388,107 +418,94 @@ __global__ void __launch_bounds__(THREADS, 1)
           umma_f16(sd, qd + off, kd + off, umma_idesc_f16(TILE, BLOCK) | type_bits<T>(), k > 0);
         }
       }
-      ahead();
+      v_there = mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase);
       if (one) {
         umma_commit(bar(L::S_FULL + w));
-        if (free_v) umma_commit(bar(L::V_EMPTY + v_stage));
-        if (free_k) umma_commit(bar(L::K_EMPTY + k_stage));
+        if (frees) {
+          umma_commit(bar(L::V_EMPTY + v_stage));
+          umma_commit(bar(L::K_EMPTY + k_stage));
+        }
       }
     };
-    while (ok && walk.next(s)) {
-      PageCursor cur;
-      cur.seek(plan, s.it, s.b0 * page_blk + lane % page_blk);
-      uint32_t begun = 0;
-      // whole blocks of the prefix, but for each group's first and last, which the general steps take
-      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.it.prefix_keys) / BLOCK), margin = s.two ? 1 : 2, head = s.b0 + margin;
-      for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
-        if (b == head && b + margin < whole) {
-          Pending x = oldest ? pend1 : pend0, y = oldest ? pend0 : pend1;  // of two tiles: the same block
-          bool k_there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
-          for (; b + margin < whole && ok; ++b) {
-            bool v_there = false;
-            auto ahead = [&] { v_there = mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase); };
-            if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) break;
-            if (s.two) {
-              step(0, x.stage, !(x.flags & 1u), rk.stage, k_there, rk.phase, false, false, [] {});
-              if (ok) step(1, x.stage, !(x.flags & 1u), rk.stage, true, 0, true, true, ahead);
-              x = Pending{rv.stage, BLOCK, rv.phase, 0, page, v_there};
-            } else {
-              step(oldest, x.stage, !(x.flags & 1u), rk.stage, k_there, rk.phase, true, true, ahead);
-              x = y;
-              y = Pending{rv.stage, BLOCK, rv.phase, 12u, page, v_there};
-              oldest ^= 1;
-              groups.turn ^= 1u;
-            }
-            rk.next(L::K_STAGES);
-            rv.next(L::V_STAGES);
-            k_there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
-          }
-          if (!ok) break;
-          if (s.two) {
-            x.flags &= 1u;
-            pend0 = pend1 = x;
-            pend0.flags |= 8u;
-            pend1.flags |= 4u;
-          } else {
-            (oldest ? pend1 : pend0) = x;
-            (oldest ? pend0 : pend1) = y;
-            next_oldest = oldest ^ 1;
-          }
+    Next m{};
+    int k_stage = -1;  // >= 0: S of m has been issued and not committed
+    while (ok) {
+      look();
+      if (k_stage >= 0) {
+        if (one) {
+          umma_commit(bar(L::S_FULL + m.w));
+          if (m.flags & FREE_K) umma_commit(bar(L::K_EMPTY + k_stage));
+          if (m.flags & LAST) umma_commit(bar(L::Q_EMPTY + m.w));
         }
-        const uint32_t takes = groups.of(s, b);
-        const int first_page = b * page_blk, cols = min(page_blk, s.it.pages - first_page) * page;
-        const int my_page = first_page + lane % page_blk;
-        int keys = page;
-        if (static_cast<int>(b + 1) * BLOCK > s.it.prefix_keys && my_page < s.it.pages) {
-          cur.go(my_page);
-          keys = min(page, cur.run.keys - (my_page - cur.run.off) * page);
-        }
-        const uint32_t idesc = umma_idesc_f16(TILE, cols) | type_bits<T>();
-        const uint64_t kd = k_desc0 + rk.stage * (L::TILE_BYTES / 16);
-        for (int w = 0; w < 2 && ok; ++w) {
-          if (!(takes >> w & 1u)) continue;
-          const bool first = !(begun >> w & 1u);
-          const bool last = last_block(s, b, w), first_use = w == 0 || takes == 2u, last_use = w == 1 || takes == 1u;
-          const uint64_t qd = q_desc0 + w * (L::TILE_BYTES / 16);
-          const uint32_t sd = tmem + S_COL + 128 * w;
-          // whether operands are there is asked while products run, not between them: K here, ahead of the wait for the
-          // softmax, V after S has been issued
-          bool there = !first_use || mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
-          if (first) there = there && mbar_test_warp(bar(L::Q_FULL + w), q_par >> w & 1u);
-          while (ok && ((n_pend > 0 && oldest == w) || (n_pend > 1 && next_oldest == w))) issue_pv();
-          if (!ok) break;
-          if (!there) {
-            if (first && !wait(L::Q_FULL + w, q_par >> w & 1u)) break;
-            if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
-          }
-          if (first) q_par ^= 1u << w;
-          begun |= 1u << w;
-          tc_fence_after();
-          if (one) {
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const int off = ((k >> 2) * HALF_BYTES + (k & 3) * 32) / 16;
-              umma_f16(sd, qd + off, kd + off, idesc, k > 0);
-            }
-            umma_commit(bar(L::S_FULL + w));
-            if (last_use) umma_commit(bar(L::K_EMPTY + rk.stage));
-            if (last) umma_commit(bar(L::Q_EMPTY + w));
-          }
-          (w ? pend1 : pend0) = Pending{rv.stage, cols, rv.phase,
-                                        (first ? 1u : 0u) | (last ? 2u : 0u) | (last_use ? 4u : 0u) | (first_use ? 8u : 0u), keys,
-                                        mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase)};
-          (n_pend++ ? next_oldest : oldest) = w;
-        }
-        rk.next(L::K_STAGES);
-        rv.next(L::V_STAGES);
+        k_stage = -1;
+        commit_pv();
       }
+      // whole blocks of the prefix, but for each group's first and last, which the general steps take
+      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.it.prefix_keys) / BLOCK), margin = s.two ? 1 : 2;
+      if (n.valid && b == s.b0 + margin && b + margin < whole && (!s.two || n.w == 0)) {
+        Pending x = oldest ? pend1 : pend0, y = oldest ? pend0 : pend1;  // of two tiles: the same block
+        bool k_there = n.there;
+        if (!s.two) groups.turn ^= 1u;  // back to before the block
+        for (;;) {
+          if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) break;
+          if (s.two) {
+            step(0, x.stage, !(x.flags & FIRST), rk.stage, k_there, rk.phase, false);
+            if (ok) step(1, x.stage, !(x.flags & FIRST), rk.stage, true, 0, true);
+          } else {
+            step(oldest, x.stage, !(x.flags & FIRST), rk.stage, k_there, rk.phase, true);
+          }
+          if (!ok) break;
+          const Pending z{rv.stage, BLOCK, rv.phase, FREE_V, v_there};
+          x = s.two ? z : y;
+          y = z;
+          if (!s.two) {
+            oldest ^= 1u;
+            groups.turn ^= 1u;
+          }
+          if (b + 1 + margin >= whole) break;
+          ++b;
+          rk.next(L::K_STAGES);
+          rv.next(L::V_STAGES);
+          k_there = mbar_test_warp(bar(L::K_FULL + rk.stage), rk.phase);
+        }
+        if (!ok) break;
+        (oldest ? pend1 : pend0) = x;
+        (oldest ? pend0 : pend1) = y;
+        if (s.two) pend0.flags &= ~FREE_V;
+        takes = 0;
+        continue;
+      }
+      // S of a group goes over its P: the product with it, and those before that, first
+      while (ok && n_pend > 0 && (!n.valid || oldest == n.w || n_pend == 2)) issue_pv();
+      if (!ok || !n.valid) break;
+      m = n;
+      if (!m.there) {
+        commit_pv();
+        if (m.flags & FIRST) wait(L::Q_FULL + m.w, q_par >> m.w & 1u);
+        if (!wait(L::K_FULL + rk.stage, rk.phase)) break;
+      }
+      if (m.flags & FIRST) q_par ^= 1u << m.w;
+      tc_fence_after();
+      k_stage = rk.stage;
+      if (one) {
+        const uint64_t qd = q_desc0 + m.w * (L::TILE_BYTES / 16), kd = k_desc0 + k_stage * (L::TILE_BYTES / 16);
+        const uint32_t idesc = umma_idesc_f16(TILE, m.cols) | type_bits<T>(), sd = tmem + S_COL + 128 * m.w;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          const int off = ((k >> 2) * HALF_BYTES + (k & 3) * 32) / 16;
+          umma_f16(sd, qd + off, kd + off, idesc, k > 0);
+        }
+      }
+      const Pending x{rv.stage, m.cols, rv.phase, m.flags, mbar_test_warp(bar(L::V_FULL + rv.stage), rv.phase)};
+      (m.w ? pend1 : pend0) = x;
+      if (n_pend++ == 0) oldest = m.w;
     }
-    while (ok && n_pend > 0) issue_pv();
+    commit_pv();
     if (one) umma_commit(bar(L::DRAIN));
     mbar_wait_warp(bar(L::DRAIN), 0, err, ok ? WAIT_TIMEOUT_NS : 100000000ull);
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
+    regs_few();
     const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);
     Groups groups;
     uint32_t used = 0, par = 0;
@@ -533,6 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
   } else {
     // ======================= softmax: thread r of group w has row r of its tile
+    regs_many();
     const int w = (warp >> 2) - 1, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
@@ -540,8 +558,30 @@ __global__ void __launch_bounds__(THREADS, 1)
     float2* ml = reinterpret_cast<float2*>(a.ws);
     float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.Hq, a.max_tokens, gridDim.x));
     Groups groups;
+    Ring rv;
     uint32_t s_par = 0, o_par = 0;
     bool ok = true;
+    // P of a block is there, and (the first group that takes it) rows of V past a page's keys count as zero
+    auto done_with = [&](int stage, uint32_t phase, int cols, bool ragged) {
+      if (ragged) {
+        if (!mbar_wait_warp(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
+        const int page = a.lay.page;
+        for (int pg = 0; pg * page < cols; ++pg) {
+          const int from = smem[L::OFF_KEYS + stage * 8 + pg];
+          for (int i = r; i < (page - from) * 8 * L::HALVES; i += 128) {
+            const int at = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
+            *reinterpret_cast<uint4*>(smem + L::OFF_V + stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + at * 128 + (c & 7) * 16) =
+                uint4{0, 0, 0, 0};
+          }
+        }
+        fence_proxy_async_shared();
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+      return true;
+    };
     while (ok && walk.next(s)) {
       const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
       const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
@@ -549,62 +589,70 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int prefix = valid ? s.it.prefix_keys : 0;
       int own0 = 0, own1 = 0;
       if (valid) {
-        const int4 rec = plan.rec[plan.order[s.it.tok + t0 + r / G]];
-        own0 = rec.z, own1 = rec.z + rec.w;
+        const int2 own = plan.own[s.it.tok + t0 + r / G];
+        own0 = own.x, own1 = own.y;
       }
       const uint32_t first_group = s.two ? w : groups.turn;
       float m = -INFINITY, l = 0.f;
       int done = 0;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
-        if (!(groups.of(s, b) >> w & 1u)) continue;
+        const uint32_t takes = groups.of(s, b);
+        const int v_stage = rv.stage;
+        const uint32_t v_phase = rv.phase;
+        rv.next(L::V_STAGES);
+        if (!(takes >> w & 1u)) continue;
         if (!mbar_wait_warp(bar(L::S_FULL + w), s_par, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
         }
         s_par ^= 1u;
         ++done;
-        if (!any) {  // none of this warp's rows is one: what its lanes of P hold reaches no other
-          if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
-          continue;
-        }
         tc_fence_after();
         const int key0 = b * BLOCK, cols = min(BLOCK, s.it.pages * a.lay.page - key0);
-        const bool whole = s.it.prefix_keys - key0 >= BLOCK;
+        const bool whole = s.it.prefix_keys - key0 >= BLOCK, ragged = !whole && !(s.two && w == 1 && (takes & 1u));
         const bool sees = valid && (prefix > key0 || (own1 > key0 && own0 < key0 + cols && own1 > own0));
-        if (!__any_sync(0xffffffffu, sees)) {  // nothing here for this warp's rows
+        if (!__any_sync(0xffffffffu, sees)) {  // nothing here for this warp's rows; lanes that are no rows reach none
           const uint32_t zero[16] = {};
-          for (int c = 0; c < 64; c += 16) tmem_st16(s_col + 64 + c, zero);
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+          if (any)
+            for (int c = 0; c < 64; c += 16) tmem_st16(s_col + 64 + c, zero);
+          if (!(ok = done_with(v_stage, v_phase, cols, ragged))) break;
           continue;
+        }
+        uint32_t va[32], vb[32], pk[16];
+        if (!whole) {
+          // columns that a row does not see: -inf in their place (also past the block's last, where S holds anything)
+#pragma unroll 1
+          for (int c = 0; c < BLOCK; c += 32) {
+            const int at = key0 + c;
+            const uint32_t seen = bits_in(-at, prefix - at) | bits_in(own0 - at, own1 - at);
+            if (__all_sync(0xffffffffu, seen == 0xffffffffu)) continue;
+            tmem_ld32(s_col + c, va);
+            tmem_ld_wait_for(va);
+#pragma unroll
+            for (int k = 0; k < 32; k += 16) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) pk[i] = seen >> (k + i) & 1u ? va[k + i] : 0xff800000u;
+              tmem_st16(s_col + c + k, pk);
+            }
+          }
+          tmem_st_wait();
         }
         // S is read twice, 32 columns at a time with the next ones on their way: first for the maximum, upwards, then
         // for P, downwards, where the last 64 are still held.  P of columns [32 c, 32 c + 32) goes to 64 + 16 c, over
-        // columns that are read by then.  (Columns past the block's last hold anything; no row sees them.)
-        uint32_t va[32], vb[32], pk[16];
-        auto seen = [&](int c) {
-          const int at = key0 + 32 * c;
-          return bits_in(-at, prefix - at) | bits_in(own0 - at, own1 - at);
-        };
+        // columns that are read by then.
         float top = -INFINITY;
-        auto maximum = [&](auto w_) {
-          constexpr bool W = decltype(w_)::value;
-          tmem_ld32(s_col, va);
-          tmem_ld_wait_for(va);
-          tmem_ld32(s_col + 32, vb);
-          mask_max<W>(va, W ? 0 : seen(0), top);
-          tmem_ld_wait_for(vb);
-          tmem_ld32(s_col + 64, va);
-          mask_max<W>(vb, W ? 0 : seen(1), top);
-          tmem_ld_wait_for(va);
-          tmem_ld32(s_col + 96, vb);
-          mask_max<W>(va, W ? 0 : seen(2), top);
-          tmem_ld_wait_for(vb);
-          mask_max<W>(vb, W ? 0 : seen(3), top);
-        };
-        if (whole) maximum(std::true_type{}); else maximum(std::false_type{});
+        tmem_ld32(s_col, va);
+        tmem_ld_wait_for(va);
+        tmem_ld32(s_col + 32, vb);
+        max32(va, top);
+        tmem_ld_wait_for(vb);
+        tmem_ld32(s_col + 64, va);
+        max32(vb, top);
+        tmem_ld_wait_for(va);
+        tmem_ld32(s_col + 96, vb);
+        max32(va, top);
+        tmem_ld_wait_for(vb);
+        max32(vb, top);
         top *= scale_log2;
         if (m == -INFINITY) m = top;  // nothing but zeros has been summed
         const bool grow = top > m + RESCALE_LOG2;
@@ -628,27 +676,20 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         const float base = m == -INFINITY ? 0.f : m;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        auto powers = [&](auto m_) {
-          constexpr bool M = decltype(m_)::value;
-          exp_pack<T, false>(vb, 0, scale_log2, base, sum, pk);
-          tmem_ld32(s_col + 32, vb);
-          tmem_st16(s_col + 112, pk);
-          exp_pack<T, false>(va, 0, scale_log2, base, sum, pk);
-          tmem_ld_wait_for(vb);
-          tmem_ld32(s_col, va);
-          tmem_st16(s_col + 96, pk);
-          exp_pack<T, M>(vb, M ? seen(1) : 0, scale_log2, base, sum, pk);
-          tmem_ld_wait_for(va);
-          tmem_st16(s_col + 80, pk);
-          exp_pack<T, M>(va, M ? seen(0) : 0, scale_log2, base, sum, pk);
-          tmem_st16(s_col + 64, pk);
-        };
-        if (whole) powers(std::false_type{}); else powers(std::true_type{});
+        exp_pack<T>(vb, scale_log2, base, sum, pk);
+        tmem_ld32(s_col + 32, vb);
+        tmem_st16(s_col + 112, pk);
+        exp_pack<T>(va, scale_log2, base, sum, pk);
+        tmem_ld_wait_for(vb);
+        tmem_ld32(s_col, va);
+        tmem_st16(s_col + 96, pk);
+        exp_pack<T>(vb, scale_log2, base, sum, pk);
+        tmem_ld_wait_for(va);
+        tmem_st16(s_col + 80, pk);
+        exp_pack<T>(va, scale_log2, base, sum, pk);
+        tmem_st16(s_col + 64, pk);
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
+        if (!(ok = done_with(v_stage, v_phase, cols, ragged))) break;
       }
       if (!ok) break;
       // ---- the partial result

@@ -220,7 +220,9 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
           const int t = run.token + x - run.tok0;
           p.order[it.tok + x] = t;
           // a row with more new tokens than keys: its first tokens see none, however many those of its last are
-          p.rec[t] = make_int4(k, x, off * page, max(0, run.keys > 0 ? seen1 + x - run.tok0 + 1 : 0));
+          const int own = max(0, run.keys > 0 ? seen1 + x - run.tok0 + 1 : 0);
+          p.rec[t] = make_int4(k, x, off * page, own);
+          p.own[it.tok + x] = make_int2(off * page, off * page + own);
         }
       }
       pages += __shfl_sync(0xffffffffu, inc, 31);

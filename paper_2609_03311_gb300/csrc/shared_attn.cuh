@@ -60,6 +60,7 @@ struct Plan {
   Run* runs;
   uint32_t* part;  // [flat entry] first row of its partial results
   int* order;      // [tokens]
+  int2* own;       // [tokens, in that order] columns of its own keys, from and to
   int* scratch;    // 5 * n_seqs + 5, of the plan kernel
   int64_t bytes;
 };
@@ -86,6 +87,7 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   p.runs = static_cast<Run*>(take((2 * items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));
   p.part = static_cast<uint32_t*>(take(4 * items * n_kv_heads));
   p.order = static_cast<int*>(take(4 * static_cast<int64_t>(max_tokens)));
+  p.own = static_cast<int2*>(take(8 * static_cast<int64_t>(max_tokens)));
   p.scratch = static_cast<int*>(take(4 * (5 * static_cast<int64_t>(n_seqs) + 5)));
   p.bytes = at;
   return p;

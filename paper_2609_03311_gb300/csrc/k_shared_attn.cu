@@ -15,9 +15,9 @@
 //              than 2^8 (P stays within the type's range until then), and leaves as a partial result
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
 // Values would (0 x NaN), so rows of V past a run's keys are cleared in shared memory.  A value that one token sees and
-// another of the item does not would too: k_shared_join finds those rows and computes them alone.
+// another of the item does not would too: rows that end with a NaN though their scores have none are computed alone.
 //
-// k_shared_join, a warp a token and q head, adds the parts up.
+// k_shared_join, a warp a row, adds the parts up.
 #include <limits.h>
 
 #include <type_traits>
@@ -224,9 +224,67 @@ __device__ __forceinline__ uint32_t bits_in(int lo, int hi) {
   return (hi >= 32 ? 0xffffffffu : (1u << hi) - 1u) & ~((1u << lo) - 1u);
 }
 
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }  // a NaN stays one
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
+
+// One row alone by a warp, a key at a time, for rows whose products took in a value that they do not see; lane l holds
+// elements [E l, E l + E) of the head.
+template <typename T, int D>
+__device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, int lane) {
+  constexpr int E = D / 32, W = E / 2;
+  const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
+  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, a.Hq / Hkv, a.max_tokens);
+  const int4 rec = plan.rec[t];
+  const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  float q[E], o[E], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const float2 f = unpack2<T>(qp[i]);
+    q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
+    o[2 * i] = o[2 * i + 1] = 0.f;
+  }
+  const Item it = plan.items[rec.x];
+  for (int k = 0; k < it.n_runs; ++k) {
+    const Run run = plan.runs[it.run + k];
+    const bool prefix = run.token < 0;
+    if (!prefix && (rec.y < run.tok0 || rec.y >= run.tok1)) continue;
+    const int n = prefix ? run.keys : rec.w;
+    for (int p = 0; p < n; ++p) {
+      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
+      if (block < 0 || block >= a.lay.n_blocks) block = 0;
+      const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
+      const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float2 f = unpack2<T>(kp[i]);
+        s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
+      }
+      s = warp_sum(s);
+      const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+      const float old = exp2f(m - base), e = exp2f(s - base);
+      m = top;
+      l = l * old + e;
+#pragma unroll
+      for (int i = 0; i < W; ++i) {
+        const float2 f = unpack2<T>(vp[i]);
+        o[2 * i] = o[2 * i] * old + e * f.x;
+        o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
+      }
+    }
+  }
+  const float inv = inverse(l);
+  uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * W;
+#pragma unroll
+  for (int i = 0; i < W; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
+  if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_shared_attn(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, SharedAttnArgs a) {
+    k_shared_attn(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                  const __grid_constant__ SharedAttnArgs a) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int gave_up;  // stands for the error word of the bounded waits: a CTA gives up alone
@@ -555,8 +613,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    float2* ml = reinterpret_cast<float2*>(a.ws);
-    float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.Hq, a.max_tokens, gridDim.x));
     Groups groups;
     Ring rv;
     uint32_t s_par = 0, o_par = 0;
@@ -692,18 +748,64 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!(ok = done_with(v_stage, v_phase, cols, ragged))) break;
       }
       if (!ok) break;
-      // ---- the partial result
-      const uint32_t rows = s.it.n_tok * G, copies = s.two ? 1 : 2;
-      const uint32_t copy = s.two ? 0 : (first_group == static_cast<uint32_t>(w) ? 0 : 1);
-      const int64_t row = plan.part[s.f] + static_cast<int64_t>(s.part * copies + copy) * rows + (s.two ? w * TT * G : 0) + r;
-      if (valid) ml[row] = make_float2(m, l);
       if (done > 0) {
         if (!mbar_wait_warp(bar(L::O_FULL + w), o_par, err, WAIT_TIMEOUT_NS)) break;
         o_par ^= 1u;
         tc_fence_after();
-        float* dst = part_o + row * D;
+      }
+      // what only the end of a segment needs is found out again here, not held in registers over its blocks
+      const Plan ends = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
+      const Item it = ends.items[s.f / Hkv];
+      if (s.two && s.b1 - s.b0 == it.blocks) {
+        // ---- the whole entry: the rows' results
+        const int t = valid ? ends.order[it.tok + w * TT + r / G] : 0, h = s.f % Hkv * G + r % G;
+        const float inv = inverse(l);
+        T* dst = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+        bool nan = false;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
+          uint32_t v[32] = {};
+          if (done > 0) {
+            tmem_ld32(o_col + c, v);
+            tmem_ld_wait_for(v);
+          }
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            const float x = l == 0.f ? 0.f : __uint_as_float(v[i]) * inv;
+            nan |= x != x;
+            v[i] = __float_as_uint(x);
+          }
+          if (valid) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              uint4 x;
+              x.x = pack2<T>(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+              x.y = pack2<T>(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+              x.z = pack2<T>(__uint_as_float(v[i + 4]), __uint_as_float(v[i + 5]));
+              x.w = pack2<T>(__uint_as_float(v[i + 6]), __uint_as_float(v[i + 7]));
+              *reinterpret_cast<uint4*>(dst + c + i) = x;
+            }
+          }
+        }
+        if (valid && a.lse) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
+        // scores in order, values not: perhaps a value that the row does not see
+        uint32_t odd = __ballot_sync(0xffffffffu, valid && nan && l == l);
+        while (odd) {
+          const int from = __ffs(odd) - 1;
+          odd &= odd - 1;
+          row_alone<T, D>(a, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
+        }
+      } else {
+        // ---- a partial result
+        float2* ml = reinterpret_cast<float2*>(a.ws);
+        float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
+        const uint32_t rows = it.n_tok * G, copies = s.two ? 1 : 2;
+        const uint32_t copy = s.two || first_group == static_cast<uint32_t>(w) ? 0 : 1;
+        const int64_t row = ends.part[s.f] + static_cast<int64_t>(s.part * copies + copy) * rows + (s.two ? w * TT * G : 0) + r;
+        if (valid) ml[row] = make_float2(m, l);
+        float* dst = part_o + row * D;
+#pragma unroll 1
+        for (int c = 0; c < D && done > 0; c += 32) {
           uint32_t v[32];
           tmem_ld32(o_col + c, v);
           tmem_ld_wait_for(v);
@@ -712,8 +814,8 @@ __global__ void __launch_bounds__(THREADS, 1)
             for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + c + 4 * i) = uint4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
           }
         }
-        tc_fence_before();
       }
+      tc_fence_before();
     }
   }
 
@@ -728,118 +830,82 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // ------------------------------------------------------------------ joining the parts
-constexpr int JOIN_WARPS = 4;
-
-// One row alone, a key at a time, for the rows whose products took in a value they do not see; lane l holds elements
-// [E l, E l + E) of the head.
+// A warp a row, JOIN_ROWS rows of an entry at a time.
 template <typename T, int D>
-__device__ void row_alone(const SharedAttnArgs& a, const Plan& plan, const int4& rec, int t, int h, int lane, float (&o)[D / 32],
-                          float& m, float& l) {
-  constexpr int E = D / 32, W = E / 2;
-  const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
-  const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
-  const float scale_log2 = a.scale * 1.4426950408889634f;
-  float q[E];
-  m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const float2 f = unpack2<T>(qp[i]);
-    q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
-    o[2 * i] = o[2 * i + 1] = 0.f;
-  }
-  const Item it = plan.items[rec.x];
-  for (int k = 0; k < it.n_runs; ++k) {
-    const Run run = plan.runs[it.run + k];
-    const bool prefix = run.token < 0;
-    if (!prefix && (rec.y < run.tok0 || rec.y >= run.tok1)) continue;
-    const int n = prefix ? run.keys : rec.w;
-    for (int p = 0; p < n; ++p) {
-      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
-      if (block < 0 || block >= a.lay.n_blocks) block = 0;
-      const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
-      const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float2 f = unpack2<T>(kp[i]);
-        s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
-      }
-      s = warp_sum(s);
-      const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-      const float old = exp2f(m - base), e = exp2f(s - base);
-      m = top;
-      l = l * old + e;
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float2 f = unpack2<T>(vp[i]);
-        o[2 * i] = o[2 * i] * old + e * f.x;
-        o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
-      }
-    }
-  }
-}
-
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * JOIN_WARPS) k_shared_join(SharedAttnArgs a, int n_ctas) {
+__global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_constant__ SharedAttnArgs a, int n_ctas) {
   constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * JOIN_WARPS + (threadIdx.x >> 5);
-  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
+  const int lane = threadIdx.x & 31, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
   const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
+  const float2* ml = reinterpret_cast<const float2*>(a.ws);
+  const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas));
   pdl_wait();
   pdl_trigger();
   const Head head = *plan.head;
   if (!made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas)) return;
-  if (unit >= static_cast<int64_t>(head.tokens) * a.Hq) return;
-  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit % a.Hq), kvh = h / G;
-  const float2* ml = reinterpret_cast<const float2*>(a.ws);
-  const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.Hq, a.max_tokens, n_ctas));
-  const int4 rec = plan.rec[t];
-  float o[E], m = -INFINITY, l = 0.f;
+  for (int j = blockIdx.x; j < head.n_join; j += gridDim.x) {
+    const int2 piece = plan.join[j];
+    const int f = piece.x, row = piece.y + (threadIdx.x >> 5);
+    const Item it = plan.items[f / Hkv];
+    if (row >= it.n_tok * G) continue;
+    const int t = plan.order[it.tok + row / G], h = f % Hkv * G + row % G;
+    float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < E; ++i) o[i] = 0.f;
-  const Item it = plan.items[rec.x];
-  if (it.blocks > 0) {
-    const uint32_t b = blocks_begin(it, kvh), rows = it.n_tok * G;
-    const uint32_t parts = ((b + it.blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
-    const int64_t row0 = plan.part[static_cast<int64_t>(rec.x) * Hkv + kvh] + rec.y * G + h % G;
-    for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
-      const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
-      float top = x.x;
+    for (int i = 0; i < E; ++i) o[i] = 0.f;
+    if (it.blocks > 0) {
+      const uint32_t b = blocks_begin(it, f % Hkv), rows = it.n_tok * G;
+      const uint32_t parts = ((b + it.blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
+      const int64_t row0 = plan.part[f] + static_cast<int64_t>(row);
+      for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
+        const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
+        float top = x.x;
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-      top = fmaxf(top, m);
-      const float base = top == -INFINITY ? 0.f : top;
-      const float old = ex2(m - base), mine = ex2(x.x - base);
-      l = l * old + warp_sum(x.y * mine);
-      m = top;
+        for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        top = fmaxf(top, m);
+        const float base = top == -INFINITY ? 0.f : top;
+        const float old = ex2(m - base), mine = ex2(x.x - base);
+        l = l * old + warp_sum(x.y * mine);
+        m = top;
 #pragma unroll
-      for (int i = 0; i < E; ++i) o[i] *= old;
-      const int n = min(32u, parts - p0);
-      for (int p = 0; p < n; ++p) {
-        const float wgt = __shfl_sync(0xffffffffu, mine, p), sum = __shfl_sync(0xffffffffu, x.y, p);
-        if (sum == 0.f) continue;  // no block of this part, or nothing that the row sees
-        const float* src = part_o + (row0 + static_cast<int64_t>(p0 + p) * rows) * D + lane * E;
-        if constexpr (E == 4) {
-          const float4 v = *reinterpret_cast<const float4*>(src);
-          o[0] += wgt * v.x, o[1] += wgt * v.y, o[2] += wgt * v.z, o[3] += wgt * v.w;
-        } else {
-          const float2 v = *reinterpret_cast<const float2*>(src);
-          o[0] += wgt * v.x, o[1] += wgt * v.y;
+        for (int i = 0; i < E; ++i) o[i] *= old;
+        // parts with no block, or nothing that the row sees, left no values; four at a time on their way
+        unsigned todo = __ballot_sync(0xffffffffu, x.y != 0.f);
+        while (todo) {
+          float wgt[4], v[4][E];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int p = todo ? __ffs(todo) - 1 : -1;
+            todo &= todo - 1;
+            wgt[k] = __shfl_sync(0xffffffffu, mine, p < 0 ? 0 : p);
+            if (p < 0) wgt[k] = 0.f;
+            const float* src = part_o + (row0 + static_cast<int64_t>(p0 + (p < 0 ? 0 : p)) * rows) * D + lane * E;
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[k][i] = 0.f;
+            if (p >= 0) {
+              if constexpr (E == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(src);
+              else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(src);
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int i = 0; i < E; ++i) o[i] += wgt[k] * v[k][i];
         }
       }
     }
+    // scores in order, values not: perhaps a value that the row does not see
+    bool nan = false;
+#pragma unroll
+    for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
+    if (l == l && __any_sync(0xffffffffu, nan)) {
+      row_alone<T, D>(a, t, h, lane);
+      continue;
+    }
+    const float inv = inverse(l);
+    uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
+    if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
   }
-  // scores in order, values not: perhaps a value that the row does not see
-  bool nan = false;
-#pragma unroll
-  for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
-  if (l == l && __any_sync(0xffffffffu, nan)) row_alone<T, D>(a, plan, rec, t, h, lane, o, m, l);
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // a NaN stays one
-  uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
-#pragma unroll
-  for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D>
@@ -855,15 +921,19 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_k, tm_v, a);
   if (e != cudaSuccess) return e;
-  const int64_t units = static_cast<int64_t>(a.max_tokens) * a.Hq;
-  return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>((units + JOIN_WARPS - 1) / JOIN_WARPS)), 32 * JOIN_WARPS,
-                          0, st, a, n_ctas);
+  // as many blocks as could have work, up to what the SMs hold at once
+  const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +
+                         static_cast<int64_t>(a.max_tokens) * a.Hq / JOIN_ROWS;
+  const int64_t held = 6 * static_cast<int64_t>(num_sms);
+  return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>(pieces < held ? pieces : held)), 32 * JOIN_ROWS, 0, st, a,
+                          n_ctas);
 }
 
 }  // namespace
 
 int64_t shared_workspace_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens, int num_sms) {
-  return max_part_rows(Hq, max_tokens, num_sms < MAX_CTAS ? num_sms : MAX_CTAS) * (8 + 4 * static_cast<int64_t>(lay.head_dim));
+  const int n_ctas = num_sms < MAX_CTAS ? num_sms : MAX_CTAS;
+  return max_part_rows(lay.n_seqs, lay.n_kv_heads, Hq / lay.n_kv_heads, max_tokens, n_ctas) * (8 + 4 * static_cast<int64_t>(lay.head_dim));
 }
 
 cudaError_t launch_shared_attention(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {

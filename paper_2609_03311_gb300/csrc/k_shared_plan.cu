@@ -267,24 +267,33 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   }
   __syncthreads();
   if (!fits) return;
-  unsigned long long rows = 0;
+  unsigned long long rows = 0;  // of partial results; in the upper half pieces of the join's list
   for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
     const int f = f0 + threadIdx.x;
     unsigned long long count = 0;
+    int entry_rows = 0;
     if (f < n_flat) {
       const Item it = p.items[f / Hkv];
+      const bool two = two_tiles(it.n_tok, G);
+      uint32_t segs = 0;
       if (it.blocks > 0) {
         const uint32_t b = blocks_begin(it, f % Hkv), e = b + it.blocks, start = b - OVERHEAD;
-        const uint32_t segs = (e - 1) / share - b / share + 1;
-        count = static_cast<unsigned long long>(segs) * it.n_tok * G * (two_tiles(it.n_tok, G) ? 1 : 2);
+        segs = (e - 1) / share - b / share + 1;
         for (uint32_t c = (start + share - 1) / share; static_cast<unsigned long long>(c) * share < e; ++c)
           if (c < MAX_CTAS) p.first[c] = f;
+      }
+      if (!two || segs != 1) {  // also where there is no key at all
+        entry_rows = it.n_tok * G;
+        count = static_cast<unsigned long long>(segs) * entry_rows * (two ? 1 : 2) |
+                static_cast<unsigned long long>((entry_rows + JOIN_ROWS - 1) / JOIN_ROWS) << 32;
       }
     }
     const unsigned long long at = rows + block_exclusive(count, warp_sum, total);
     if (f < n_flat) p.part[f] = static_cast<uint32_t>(at);
+    for (int r = 0; r < entry_rows; r += JOIN_ROWS) p.join[(at >> 32) + r / JOIN_ROWS] = make_int2(f, r);
     rows += total;
   }
+  if (threadIdx.x == 0) p.head->n_join = static_cast<int>(rows >> 32);
 }
 
 }  // namespace

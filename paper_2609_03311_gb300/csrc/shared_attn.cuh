@@ -9,7 +9,8 @@
 //
 // An item and a kv head are a flat entry.  The flat entries' blocks lie one after another on a line on which each entry
 // also takes OVERHEAD steps, and every CTA takes an equal share of the line.  What a CTA has of an entry is a segment; it
-// leaves partial softmax results (maximum, sum, weighted values), which the joining kernel adds up by token.
+// leaves partial softmax results (maximum, sum, weighted values), which the joining kernel adds up by row; only an entry
+// of two tiles that is whole in one CTA gives its rows' results right away.
 #pragma once
 
 #include "device_common.cuh"
@@ -22,6 +23,7 @@ constexpr int TILE = 128;   // rows of a tile
 constexpr int BLOCK = 128;  // columns of a block
 constexpr uint32_t OVERHEAD = 2;
 constexpr int MAX_CTAS = 256;
+constexpr int JOIN_ROWS = 8;
 
 struct alignas(16) Run {
   int row;    // table row
@@ -44,7 +46,7 @@ struct alignas(16) Item {
   int pad;
 };
 struct alignas(16) Head {
-  int tokens, n_items, n_flat;
+  int tokens, n_items, n_flat, n_join;
   uint32_t share, total;  // of the line: a CTA's part, all of it
   int n_seqs, n_kv_heads, Hq, max_tokens, n_ctas, head_dim, page;  // what the plan was made for
 };
@@ -59,6 +61,7 @@ struct Plan {
   Item* items;
   Run* runs;
   uint32_t* part;  // [flat entry] first row of its partial results
+  int2* join;      // flat entry, first of up to JOIN_ROWS rows that are to be added up from partial results
   int* order;      // [tokens]
   int2* own;       // [tokens, in that order] columns of its own keys, from and to
   int* scratch;    // 5 * n_seqs + 5, of the plan kernel
@@ -86,16 +89,19 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   // a run for every row, one more wherever an item ends within a row, and the prefixes'
   p.runs = static_cast<Run*>(take((2 * items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));
   p.part = static_cast<uint32_t*>(take(4 * items * n_kv_heads));
+  p.join = static_cast<int2*>(take(8 * (items * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / JOIN_ROWS)));
   p.order = static_cast<int*>(take(4 * static_cast<int64_t>(max_tokens)));
   p.own = static_cast<int2*>(take(8 * static_cast<int64_t>(max_tokens)));
   p.scratch = static_cast<int*>(take(4 * (5 * static_cast<int64_t>(n_seqs) + 5)));
   p.bytes = at;
   return p;
 }
-// Rows of partial results at most: an item of one tile leaves two for a segment (its two halves of the blocks), one of
-// two tiles one; every boundary between CTAs adds a segment.
-__host__ __device__ inline int64_t max_part_rows(int Hq, int max_tokens, int n_ctas) {
-  return 2 * static_cast<int64_t>(max_tokens) * Hq + 2 * TILE * static_cast<int64_t>(n_ctas);
+// Rows of partial results at most.  An entry of two tiles leaves some only where it is split: a boundary between CTAs
+// makes two segments of at most 256 rows.  An item of one tile (at most one for every prefix, hence for every row) leaves
+// two for each segment, its two halves of the blocks.
+__host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int G, int max_tokens, int n_ctas) {
+  const int64_t all = static_cast<int64_t>(max_tokens) * G, single = static_cast<int64_t>(TILE) * n_seqs;
+  return 2 * n_kv_heads * (all < single ? all : single) + 4 * TILE * static_cast<int64_t>(n_ctas);
 }
 
 __host__ __device__ inline bool two_tiles(int n_tok, int G) { return n_tok > tokens_a_tile(G); }

@@ -5,14 +5,17 @@
 // the sum o of exp(score - m) v; parts add up as exp(m_i - m) l_i and exp(m_i - m) o_i with m the largest m_i.  A
 // part itself runs over its keys block by block the same way.
 //
-// k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh).  An item of two
-// tiles gives each block of 128 columns to the softmax groups of the tiles that it concerns, a tile each; of one tile,
-// blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
-//   warp 0, 2  copy K and V blocks, page by page, into two rings (TMA; a page's rows of a kv head lie together)
-//   warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
-//   warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
-//   warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more
-//              than 2^8 (P stays within the type's range until then), and leaves as a partial result
+// k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh), which holds either
+// tiles or few items.  In both, warps 0 and 2 copy K and V blocks, page by page, into two rings (TMA; a page's rows of a kv
+// head lie together).
+//   Tiles: an item of two tiles gives each block of 128 columns to the softmax groups of the tiles that it concerns, a tile
+//   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
+//     warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
+//     warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
+//     warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more than
+//                2^8 (P stays within the type's range until then)
+//   Few items: warps 4-11 do 16-row warp-level products, 16 columns of each block a warp, and add their eight results up
+//   at the end of a segment; the room of Q goes to the rings.
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
 // Values would (0 x NaN), so rows of V past a run's keys are cleared in shared memory.  A value that one token sees and
 // another of the item does not would too: rows that end with a NaN though their scores have none are computed alone.
@@ -45,11 +48,15 @@ struct Smem {
   static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // where the Q gatherer's rows lie
   static constexpr int OFF_KEYS = OFF_ROW + 128 * 8;  // of each page of a V stage: rows that hold keys
   static constexpr int OFF_BAR = OFF_KEYS + 64;
+  // few items: the rings begin at 0
+  static constexpr int FK_STAGES = D == 128 ? 3 : 6, FV_STAGES = D == 128 ? 4 : 6;
+  static_assert((FK_STAGES + FV_STAGES) * TILE_BYTES <= OFF_ROW, "the few items' rings");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
-                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
+                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, FK_FULL = DRAIN + 1, FK_EMPTY = FK_FULL + FK_STAGES,
+                       FV_FULL = FK_EMPTY + FK_STAGES, FV_EMPTY = FV_FULL + FV_STAGES, N_BARS = FV_EMPTY + FV_STAGES;
   static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
-  static_assert(V_STAGES * 8 <= 64, "a byte a page");
+  static_assert(V_STAGES * 8 <= 64 && FV_STAGES * 8 <= 64, "a byte a page");
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
@@ -63,6 +70,10 @@ struct Ring {
     }
   }
 };
+
+__device__ __forceinline__ Plan plan_of(const SharedAttnArgs& a) {
+  return plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, a.lay.n_kv_heads, a.Hq / a.lay.n_kv_heads, a.max_tokens);
+}
 
 template <typename T>
 __host__ __device__ constexpr uint32_t type_bits() {  // operand formats of the instruction descriptor: 0 f16, 1 bf16
@@ -103,46 +114,49 @@ __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.a
 __device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY)); }
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// One segment after another of this CTA's share.
-struct Segment {
-  Item it;
-  int f, h;         // flat entry, kv head
-  uint32_t b0, b1;  // its blocks here
-  uint32_t part;    // which of the entry's segments
-  bool two;         // two tiles
-};
-struct Walk {
-  const Plan& p;
-  uint32_t c0, c1, share;
-  int f, n_flat, Hkv, G;
-  __device__ __forceinline__ Walk(const Plan& plan, const SharedAttnArgs& a) : p(plan), Hkv(a.lay.n_kv_heads), G(a.Hq / a.lay.n_kv_heads) {
-    Head h = *p.head;
-    if (!made_for(h, a.lay, a.Hq, a.max_tokens, gridDim.x)) {
-      if (a.status && threadIdx.x == 0) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-      h = Head{};
-    }
-    share = h.share;
-    c0 = min(blockIdx.x * static_cast<unsigned long long>(share), static_cast<unsigned long long>(h.total));
-    c1 = min(c0 + share, h.total);
-    n_flat = h.n_flat;
-    f = c0 < c1 ? p.first[blockIdx.x] : n_flat;
+// D (16 x 8, 32-bit) += A (16 x 16) B (16 x 8) of T by a warp.
+template <typename T>
+__device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same_v<T, __half>) {
+    mma_f16_16816(d, a, b0, b1);
+  } else {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
-  __device__ __forceinline__ bool next(Segment& s) {
-    for (; f < n_flat; ++f) {
-      s.it = p.items[f / Hkv];
-      if (s.it.blocks == 0) continue;
-      s.h = f % Hkv;
-      const uint32_t b = blocks_begin(s.it, s.h);
-      if (b - OVERHEAD >= c1) return false;
-      s.b0 = c0 > b ? c0 - b : 0;
-      s.b1 = c1 > b ? min(c1 - b, s.it.blocks) : 0;
-      if (s.b1 <= s.b0) continue;
-      s.part = (b + s.b0) / share - b / share;
-      s.two = two_tiles(s.it.n_tok, G);
-      s.f = f++;
-      return true;
+}
+// A barrier of warps 4-11; true in all of them when `x` is in any.
+__device__ __forceinline__ bool eight_any(bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"(static_cast<uint32_t>(x))
+      : "memory");
+  return r != 0;
+}
+
+// One segment after another of this CTA's share.
+struct Walk {
+  const Segment* segs;
+  int at, end;
+  __device__ __forceinline__ explicit Walk(const SharedAttnArgs& a) {
+    const Plan p = plan_of(a);
+    segs = p.segs;
+    at = p.first[blockIdx.x];
+    end = p.first[blockIdx.x + 1];
+    if (!made_for(*p.head, a.lay, a.Hq, a.max_tokens, gridDim.x)) {
+      if (a.status && threadIdx.x == 0) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+      at = end = 0;
     }
-    return false;
+  }
+  __device__ __forceinline__ bool few() const { return at < end && (segs[at].flags & SEG_FEW); }  // at the start
+  __device__ __forceinline__ bool next(Segment& s) {
+    if (at >= end) return false;
+    s = segs[at++];
+    return true;
   }
 };
 // The softmax groups that take a block (a bit each): those whose tile it concerns, or in turn over all one-tile
@@ -150,14 +164,14 @@ struct Walk {
 struct Groups {
   uint32_t turn = 0;
   __device__ __forceinline__ uint32_t of(const Segment& s, uint32_t b) {
-    if (s.two) return (b < s.it.end0 ? 1u : 0u) | (b < s.it.prefix_blocks || b >= s.it.begin1 ? 2u : 0u);
+    if (s.flags & SEG_TWO) return (b < s.end0 ? 1u : 0u) | (b < s.prefix_blocks || b >= s.begin1 ? 2u : 0u);
     const uint32_t g = 1u << turn;
     turn ^= 1u;
     return g;
   }
   // The groups that take any block of the segment; goes past it.
   __device__ __forceinline__ uint32_t any(const Segment& s) {
-    if (s.two) return (s.b0 < s.it.end0 ? 1u : 0u) | (s.b0 < s.it.prefix_blocks || s.b1 > s.it.begin1 ? 2u : 0u);
+    if (s.flags & SEG_TWO) return (s.b0 < s.end0 ? 1u : 0u) | (s.b0 < s.prefix_blocks || s.b1 > s.begin1 ? 2u : 0u);
     const uint32_t n = s.b1 - s.b0, g = n > 1 ? 3u : 1u << turn;
     turn ^= n & 1u;
     return g;
@@ -165,18 +179,18 @@ struct Groups {
 };
 // The last block of the segment that group w takes, if it takes any (of one tile: the last but one is another's last).
 __device__ __forceinline__ bool last_block(const Segment& s, uint32_t b, int w) {
-  if (!s.two) return b + 2 >= s.b1;
-  if (w == 0) return b + 1 == min(s.b1, s.it.end0);
-  return b + 1 == (s.b1 > s.it.begin1 ? s.b1 : min(s.b1, s.it.prefix_blocks));
+  if (!(s.flags & SEG_TWO)) return b + 2 >= s.b1;
+  if (w == 0) return b + 1 == min(s.b1, s.end0);
+  return b + 1 == (s.b1 > s.begin1 ? s.b1 : min(s.b1, s.prefix_blocks));
 }
 // A lane's page of each block and the run it lies in.
 struct PageCursor {
   Run run;
   int at, n_runs;
   const Run* runs;
-  __device__ __forceinline__ void seek(const Plan& p, const Item& it, int page) {
-    runs = p.runs + it.run;
-    n_runs = it.n_runs;
+  __device__ __forceinline__ void seek(const Plan& p, const Segment& s, int page) {
+    runs = p.runs + s.run;
+    n_runs = s.n_runs;
     int lo = 0, hi = n_runs - 1;
     while (lo < hi) {  // the last run that begins at or before the page (runs without pages share their successor's place)
       const int mid = (lo + hi + 1) >> 1;
@@ -233,7 +247,7 @@ template <typename T, int D>
 __device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, int lane) {
   constexpr int E = D / 32, W = E / 2;
   const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
-  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, a.Hq / Hkv, a.max_tokens);
+  const Plan plan = plan_of(a);
   const int4 rec = plan.rec[t];
   const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
   const float scale_log2 = a.scale * 1.4426950408889634f;
@@ -244,33 +258,37 @@ __device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, in
     q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
     o[2 * i] = o[2 * i + 1] = 0.f;
   }
-  const Item it = plan.items[rec.x];
-  for (int k = 0; k < it.n_runs; ++k) {
-    const Run run = plan.runs[it.run + k];
-    const bool prefix = run.token < 0;
-    if (!prefix && (rec.y < run.tok0 || rec.y >= run.tok1)) continue;
-    const int n = prefix ? run.keys : rec.w;
-    for (int p = 0; p < n; ++p) {
-      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
-      if (block < 0 || block >= a.lay.n_blocks) block = 0;
-      const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
-      const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
-      float s = 0.f;
+  for (int k = 0; k < 2; ++k) {
+    // the prefix, by whichever item reads it; the row's own keys likewise
+    const int item = k ? rec.z : rec.x, place = k ? rec.w : rec.y;
+    if (item < 0) continue;
+    const Item it = plan.items[item];
+    for (int j = 0; j < it.n_runs; ++j) {
+      const Run run = plan.runs[it.run + j];
+      if (place < run.tok0 || place >= run.tok1) continue;
+      const int n = run.token < 0 ? run.keys : max(0, run.keys - (run.tok1 - 1 - place));
+      for (int p = 0; p < n; ++p) {
+        int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
+        if (block < 0 || block >= a.lay.n_blocks) block = 0;
+        const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
+        const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
+        float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float2 f = unpack2<T>(kp[i]);
-        s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
-      }
-      s = warp_sum(s);
-      const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-      const float old = exp2f(m - base), e = exp2f(s - base);
-      m = top;
-      l = l * old + e;
+        for (int i = 0; i < W; ++i) {
+          const float2 f = unpack2<T>(kp[i]);
+          s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
+        }
+        s = warp_sum(s);
+        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
+        const float old = exp2f(m - base), e = exp2f(s - base);
+        m = top;
+        l = l * old + e;
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float2 f = unpack2<T>(vp[i]);
-        o[2 * i] = o[2 * i] * old + e * f.x;
-        o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
+        for (int i = 0; i < W; ++i) {
+          const float2 f = unpack2<T>(vp[i]);
+          o[2 * i] = o[2 * i] * old + e * f.x;
+          o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
+        }
       }
     }
   }
@@ -279,6 +297,204 @@ __device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, in
 #pragma unroll
   for (int i = 0; i < W; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
   if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
+}
+
+// A share of few items by warps 4-11: warp `wi` takes columns 16 wi .. + 15 of each block.  Fragments of the products: a
+// thread has rows lane / 4 and lane / 4 + 8 of the item, and of each 8 columns two from 2 (lane % 4).  Bound by the copies
+// of K and V (64 KB a block of head size 128: 1.5 us of an SM's part of the memory's rate).
+template <typename T, int D>
+__device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint8_t* smem, uint32_t s0, int wi, int lane, int* err) {
+  using L = Smem<D>;
+  auto bar = [&](int i) { return s0 + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
+  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  const int quad = lane >> 2, in_quad = lane & 3;
+  const Plan plan = plan_of(a);
+  Walk walk(a);
+  Ring rk, rv;
+  Segment s;
+  while (walk.next(s)) {
+    const int rows = s.n_tok * G;
+    uint32_t q[D / 16][4];
+    int own0[2], own1[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = quad + 8 * i;
+      const bool valid = r < rows;
+      const int o = s.tok + (valid ? r / G : 0);
+      const int2 own = plan.own[o];
+      own0[i] = valid ? own.x : 0, own1[i] = valid ? own.y : 0;
+      const uint32_t* src = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + plan.order[o] * a.q_tok +
+                                                              static_cast<int64_t>(s.h * G + (valid ? r % G : 0)) * a.q_head) + in_quad;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        q[k][i] = valid ? src[8 * k] : 0u;
+        q[k][2 + i] = valid ? src[8 * k + 4] : 0u;
+      }
+    }
+    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    bool ok = true;
+    uint32_t k0 = 0, v0 = 0;
+    for (uint32_t b = s.b0; b < s.b1; ++b) {
+      k0 = L::TILE_BYTES * rk.stage;
+      v0 = L::TILE_BYTES * (L::FK_STAGES + rv.stage);
+      const int col0 = b * BLOCK + 16 * wi;
+      const bool mine = col0 < s.pages * page, part = s.prefix_keys < col0 + 16;  // a page is 16 columns or more
+      if (!(ok = mbar_wait_warp(bar(L::FK_FULL + rk.stage), rk.phase, err, WAIT_TIMEOUT_NS))) break;
+      uint32_t p[4] = {0, 0, 0, 0};
+      if (mine) {
+        float sc[2][4];
+        const int row = 16 * wi + (lane & 7);
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+#pragma unroll
+          for (int k = 0; k < D / 16; k += 2) {
+            const int c = 2 * k + (lane >> 3);  // 16-byte piece of the key's row
+            uint32_t x[4];
+            ldmatrix_x4(s0 + k0 + (c >> 3) * HALF_BYTES + (row + 8 * t) * 128 + (((c & 7) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
+            mma16<T>(sc[t], q[k], x[0], x[1]);
+            mma16<T>(sc[t], q[k + 1], x[2], x[3]);
+          }
+        }
+        if (b + 1 < s.b1) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::FK_EMPTY + rk.stage));
+        }
+        if (part) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int c = col0 + 8 * t + 2 * in_quad + (e & 1), i = e >> 1;
+              if (!(c < s.prefix_keys || (c >= own0[i] && c < own1[i]))) sc[t][e] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2;
+          if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
+          const bool grow = top > m[i] + RESCALE_LOG2;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float by = grow ? ex2(m[i] - top) : 1.f;
+            if (grow) m[i] = top;
+            l[i] *= by;
+#pragma unroll
+            for (int d = 0; d < D / 8; ++d) o[d][2 * i] *= by, o[d][2 * i + 1] *= by;
+          }
+          const float base = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const float x = ex2(fmaf(sc[t][2 * i], scale_log2, -base)), y = ex2(fmaf(sc[t][2 * i + 1], scale_log2, -base));
+            l[i] += x + y;  // this thread's columns: the quad's four sums are added up at the end
+            p[2 * t + i] = pack2<T>(x, y);
+          }
+        }
+      } else if (b + 1 < s.b1 && lane == 0) {
+        mbar_arrive(bar(L::FK_EMPTY + rk.stage));
+      }
+      if (!(ok = mbar_wait_warp(bar(L::FV_FULL + rv.stage), rv.phase, err, WAIT_TIMEOUT_NS))) break;
+      if (mine) {
+        const int row = 16 * wi + (lane & 15);
+        if (part) {
+          // rows of V past a page's keys count as zero
+          const bool clear = row % page >= smem[L::OFF_KEYS + rv.stage * 8 + row / page];
+          if (__any_sync(0xffffffffu, clear)) {
+            if (clear)
+#pragma unroll 1
+              for (int c = lane >> 4; c < 8 * L::HALVES; c += 2)
+                *reinterpret_cast<uint4*>(smem + v0 + (c >> 3) * HALF_BYTES + row * 128 + ((c & 7) << 4)) = uint4{0, 0, 0, 0};
+            fence_proxy_async_shared();  // ahead of the copies that follow
+            __syncwarp();
+          }
+        }
+#pragma unroll
+        for (int d = 0; d < D / 8; d += 2) {
+          const int c = d + (lane >> 4);
+          uint32_t x[4];
+          ldmatrix_x4_trans(s0 + v0 + (c >> 3) * HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
+          mma16<T>(o[d], p, x[0], x[1]);
+          mma16<T>(o[d + 1], p, x[2], x[3]);
+        }
+      }
+      if (b + 1 < s.b1) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(L::FV_EMPTY + rv.stage));
+        rk.next(L::FK_STAGES);
+        rv.next(L::FV_STAGES);
+      }
+    }
+    // The eight warps' results, by way of the last block's stages, which are not handed back before: four in K's, four in
+    // V's.  The barrier also tells every warp whether one gave up, so that none waits for it.
+    if (eight_any(!ok)) return;
+    float2* stats = reinterpret_cast<float2*>(smem + L::OFF_ROW);  // [warp][row] maximum and sum
+    auto sums = [&](int k, int r) { return reinterpret_cast<float*>(smem + (k < 4 ? k0 : v0)) + ((k & 3) * FEW + r) * D; };
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = quad + 8 * i;
+      float sum = l[i] + __shfl_xor_sync(0xffffffffu, l[i], 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      if (in_quad == 0) stats[wi * FEW + r] = make_float2(m[i], sum);
+      // a row begins 8 further round than the one before: the quads' stores go to different banks
+#pragma unroll
+      for (int d = 0; d < D / 8; ++d)
+        *reinterpret_cast<float2*>(sums(wi, r) + (8 * (d + quad) + 2 * in_quad) % D) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
+    }
+    eight_any(false);
+    float2* ml = reinterpret_cast<float2*>(a.ws);
+    float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
+    constexpr int E = D / 32;
+    for (int r = wi; r < rows; r += 8) {  // a warp a row
+      float top = -INFINITY, sum = 0.f, x[E] = {};
+      float2 st[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        st[k] = stats[k * FEW + r];
+        top = fmaxf(top, st[k].x);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (st[k].y == 0.f) continue;  // nothing that the row sees, whatever its values
+        const float by = ex2(st[k].x - top);
+        sum += st[k].y * by;
+        const float* src = sums(k, r) + (lane * E + 8 * (r & 7)) % D;
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] += src[i] * by;
+      }
+      if (s.flags & SEG_WHOLE) {
+        const int t = plan.order[s.tok + r / G], h = s.h * G + r % G;
+        const float inv = inverse(sum);
+        bool nan = false;
+        uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] *= inv, nan |= x[i] != x[i];
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+        if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(top, sum);
+        // scores in order, values not: perhaps a value that the row does not see
+        if (sum == sum && __any_sync(0xffffffffu, nan)) row_alone<T, D>(a, t, h, lane);
+      } else {
+        const int64_t row = static_cast<int64_t>(s.part_row) + r;
+        if (lane == 0) ml[row] = make_float2(top, sum);
+        if (sum != 0.f) {
+#pragma unroll
+          for (int i = 0; i < E; i += 2) *reinterpret_cast<float2*>(part_o + row * D + lane * E + i) = make_float2(x[i], x[i + 1]);
+        }
+      }
+    }
+    fence_proxy_async_shared();
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive(bar(L::FK_EMPTY + rk.stage));
+      mbar_arrive(bar(L::FV_EMPTY + rv.stage));
+    }
+    rk.next(L::FK_STAGES);
+    rv.next(L::FV_STAGES);
+  }
 }
 
 template <typename T, int D>
@@ -298,7 +514,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (threadIdx.x == 0) {
     gave_up = 0;
-    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
+    for (int i = 0; i < L::N_BARS; ++i) {
+      const bool by_eight = (i >= L::FK_EMPTY && i < L::FV_FULL) || i >= L::FV_EMPTY;
+      mbar_init(bar(i), by_eight ? 8 : i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
+    }
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -313,8 +532,8 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem = *tmem_slot;
   pdl_trigger();
   pdl_wait();
-  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
-  Walk walk(plan, a);
+  // each role finds its way by itself: little is held in registers where their shares change
+  const bool few = Walk(a).few();
   Segment s;
 
   if (warp == 0 || warp == 2) {
@@ -322,9 +541,11 @@ __global__ void __launch_bounds__(THREADS, 1)
     regs_few();
     const bool is_v = warp == 2;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
-    const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL,
-              empty = is_v ? L::V_EMPTY : L::K_EMPTY;
-    const uint32_t ring0 = s0 + (is_v ? L::OFF_V : L::OFF_K);
+    Walk walk(a);
+    const Plan plan = plan_of(a);
+    const int stages = few ? (is_v ? L::FV_STAGES : L::FK_STAGES) : is_v ? L::V_STAGES : L::K_STAGES;
+    const int full = few ? (is_v ? L::FV_FULL : L::FK_FULL) : is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
+    const uint32_t ring0 = s0 + (few ? (is_v ? L::FK_STAGES * L::TILE_BYTES : 0) : is_v ? L::OFF_V : L::OFF_K);
     const int page = a.lay.page, page_blk = BLOCK / page;
     const int pg = lane / L::HALVES, half = lane % L::HALVES;  // pages of a block: at most 8
     Ring r;
@@ -332,9 +553,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     bool ok = true;
     while (ok && walk.next(s)) {
       PageCursor cur;
-      cur.seek(plan, s.it, s.b0 * page_blk + pg);
+      cur.seek(plan, s, s.b0 * page_blk + pg);
       for (uint32_t b = s.b0; b < s.b1; ++b) {
-        const int first = b * page_blk, pages = min(page_blk, s.it.pages - first);
+        const int first = b * page_blk, pages = min(page_blk, s.pages - first);
         const bool mine = pg < pages;
         int block = 0;
         if (mine) {
@@ -367,12 +588,20 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (!ok)  // copies in flight land before the CTA ends
       for (int i = 0; i < stages; ++i)
         if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
+  } else if (few) {
+    if (warp >= 4) {
+      regs_many();
+      few_items<T, D>(a, smem, s0, warp - 4, lane, err);
+    } else {
+      regs_few();
+    }
   } else if (warp == 1) {
     // ======================= MMA issuer
     regs_few();
     const bool one = elect_one();
     const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
     const int page = a.lay.page, page_blk = BLOCK / page;
+    Walk walk(a);
     Groups groups;
     bool ok = true;
     auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
@@ -440,7 +669,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         any_block = true;
         takes = groups.of(s, b);
-        n.cols = min(page_blk, s.it.pages - static_cast<int>(b) * page_blk) * page;
+        n.cols = min(page_blk, s.pages - static_cast<int>(b) * page_blk) * page;
       }
       n.w = takes & 1u ? 0 : 1;
       takes &= ~(1u << n.w);
@@ -499,14 +728,14 @@ __global__ void __launch_bounds__(THREADS, 1)
         commit_pv();
       }
       // whole blocks of the prefix, but for each group's first and last, which the general steps take
-      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.it.prefix_keys) / BLOCK), margin = s.two ? 1 : 2;
-      if (n.valid && b == s.b0 + margin && b + margin < whole && (!s.two || n.w == 0)) {
+      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.prefix_keys) / BLOCK), margin = s.flags & SEG_TWO ? 1 : 2;
+      if (n.valid && b == s.b0 + margin && b + margin < whole && (!(s.flags & SEG_TWO) || n.w == 0)) {
         Pending x = oldest ? pend1 : pend0, y = oldest ? pend0 : pend1;  // of two tiles: the same block
         bool k_there = n.there;
-        if (!s.two) groups.turn ^= 1u;  // back to before the block
+        if (!(s.flags & SEG_TWO)) groups.turn ^= 1u;  // back to before the block
         for (;;) {
           if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) break;
-          if (s.two) {
+          if (s.flags & SEG_TWO) {
             step(0, x.stage, !(x.flags & FIRST), rk.stage, k_there, rk.phase, false);
             if (ok) step(1, x.stage, !(x.flags & FIRST), rk.stage, true, 0, true);
           } else {
@@ -514,9 +743,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           if (!ok) break;
           const Pending z{rv.stage, BLOCK, rv.phase, FREE_V, v_there};
-          x = s.two ? z : y;
+          x = s.flags & SEG_TWO ? z : y;
           y = z;
-          if (!s.two) {
+          if (!(s.flags & SEG_TWO)) {
             oldest ^= 1u;
             groups.turn ^= 1u;
           }
@@ -529,7 +758,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!ok) break;
         (oldest ? pend1 : pend0) = x;
         (oldest ? pend0 : pend1) = y;
-        if (s.two) pend0.flags &= ~FREE_V;
+        if (s.flags & SEG_TWO) pend0.flags &= ~FREE_V;
         takes = 0;
         continue;
       }
@@ -565,6 +794,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few();
     const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);
+    const int* order = plan_of(a).order;
+    Walk walk(a);
     Groups groups;
     uint32_t used = 0, par = 0;
     bool ok = true;
@@ -573,10 +804,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       const uint32_t takes = groups.any(s);
       for (int w = 0; w < 2 && ok; ++w) {
         if (!(takes >> w & 1u)) continue;
-        const int t0 = s.two ? w * TT : 0, rows = min(TT, s.it.n_tok - t0) * G;
+        const int t0 = s.flags & SEG_TWO ? w * TT : 0, rows = min(TT, s.n_tok - t0) * G;
         __syncwarp();
         for (int r = lane; r < rows; r += 32)
-          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(plan.order[s.it.tok + t0 + r / G]) * a.q_tok +
+          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(order[s.tok + t0 + r / G]) * a.q_tok +
                                                   static_cast<int64_t>(s.h * G + r % G) * a.q_head);
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
@@ -613,6 +844,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
     const float scale_log2 = a.scale * 1.4426950408889634f;
+    const int2* own_columns = plan_of(a).own;
+    Walk walk(a);
     Groups groups;
     Ring rv;
     uint32_t s_par = 0, o_par = 0;
@@ -639,16 +872,16 @@ __global__ void __launch_bounds__(THREADS, 1)
       return true;
     };
     while (ok && walk.next(s)) {
-      const int t0 = s.two ? w * TT : 0, n = min(TT, s.it.n_tok - t0);
+      const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0);
       const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
       // the row sees columns [0, prefix) and [own0, own1)
-      const int prefix = valid ? s.it.prefix_keys : 0;
+      const int prefix = valid ? s.prefix_keys : 0;
       int own0 = 0, own1 = 0;
       if (valid) {
-        const int2 own = plan.own[s.it.tok + t0 + r / G];
+        const int2 own = own_columns[s.tok + t0 + r / G];
         own0 = own.x, own1 = own.y;
       }
-      const uint32_t first_group = s.two ? w : groups.turn;
+      const uint32_t first_group = s.flags & SEG_TWO ? w : groups.turn;
       float m = -INFINITY, l = 0.f;
       int done = 0;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
@@ -664,8 +897,8 @@ __global__ void __launch_bounds__(THREADS, 1)
         s_par ^= 1u;
         ++done;
         tc_fence_after();
-        const int key0 = b * BLOCK, cols = min(BLOCK, s.it.pages * a.lay.page - key0);
-        const bool whole = s.it.prefix_keys - key0 >= BLOCK, ragged = !whole && !(s.two && w == 1 && (takes & 1u));
+        const int key0 = b * BLOCK, cols = min(BLOCK, s.pages * a.lay.page - key0);
+        const bool whole = s.prefix_keys - key0 >= BLOCK, ragged = !whole && !((s.flags & SEG_TWO) && w == 1 && (takes & 1u));
         const bool sees = valid && (prefix > key0 || (own1 > key0 && own0 < key0 + cols && own1 > own0));
         if (!__any_sync(0xffffffffu, sees)) {  // nothing here for this warp's rows; lanes that are no rows reach none
           const uint32_t zero[16] = {};
@@ -753,12 +986,11 @@ __global__ void __launch_bounds__(THREADS, 1)
         o_par ^= 1u;
         tc_fence_after();
       }
-      // what only the end of a segment needs is found out again here, not held in registers over its blocks
-      const Plan ends = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
-      const Item it = ends.items[s.f / Hkv];
-      if (s.two && s.b1 - s.b0 == it.blocks) {
+      // what only the end of a segment needs is read again here, not held in registers over its blocks
+      const Segment& e = walk.segs[walk.at - 1];
+      if (e.flags & SEG_WHOLE) {
         // ---- the whole entry: the rows' results
-        const int t = valid ? ends.order[it.tok + w * TT + r / G] : 0, h = s.f % Hkv * G + r % G;
+        const int t = valid ? plan_of(a).order[e.tok + w * TT + r / G] : 0, h = e.h * G + r % G;
         const float inv = inverse(l);
         T* dst = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
         bool nan = false;
@@ -799,9 +1031,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         // ---- a partial result
         float2* ml = reinterpret_cast<float2*>(a.ws);
         float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
-        const uint32_t rows = it.n_tok * G, copies = s.two ? 1 : 2;
-        const uint32_t copy = s.two || first_group == static_cast<uint32_t>(w) ? 0 : 1;
-        const int64_t row = ends.part[s.f] + static_cast<int64_t>(s.part * copies + copy) * rows + (s.two ? w * TT * G : 0) + r;
+        const bool two = e.flags & SEG_TWO;
+        const uint32_t second = !two && first_group != static_cast<uint32_t>(w) ? e.n_tok * G : 0;
+        const int64_t row = static_cast<int64_t>(e.part_row) + second + (two ? w * TT * G : 0) + r;
         if (valid) ml[row] = make_float2(m, l);
         float* dst = part_o + row * D;
 #pragma unroll 1
@@ -835,7 +1067,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_constant__ SharedAttnArgs a, int n_ctas) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
-  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, Hkv, G, a.max_tokens);
+  const Plan plan = plan_of(a);
   const float2* ml = reinterpret_cast<const float2*>(a.ws);
   const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas));
   pdl_wait();
@@ -851,10 +1083,15 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_con
     float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = 0.f;
-    if (it.blocks > 0) {
-      const uint32_t b = blocks_begin(it, f % Hkv), rows = it.n_tok * G;
-      const uint32_t parts = ((b + it.blocks - 1) / head.share - b / head.share + 1) * (two_tiles(it.n_tok, G) ? 1 : 2);
-      const int64_t row0 = plan.part[f] + static_cast<int64_t>(row);
+    // the piece's own entry, then the few entry that has a row's own keys beside tiles
+    const int4 rec = plan.rec[t];
+    const bool beside = !(it.flags & ITEM_FEW) && rec.z >= 0;
+    for (int k = 0; k <= static_cast<int>(beside); ++k) {
+      const int e = k ? rec.z * Hkv + f % Hkv : f, place = k ? rec.w * G + h % G : row;
+      const Item x_it = k ? plan.items[rec.z] : it;
+      const uint32_t rows = x_it.n_tok * G;
+      const uint32_t parts = on_line(x_it, f % Hkv, G).segments(x_it.blocks, head.share) * copies_of(x_it, G);
+      const int64_t row0 = plan.part[e] + static_cast<int64_t>(place);
       for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
         const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
         float top = x.x;

@@ -48,15 +48,18 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   __shared__ unsigned long long warp_sum[32];
   __shared__ int bad, unsorted;
   const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page, page_blk = BLOCK / page;
-  const int tile = tokens_a_tile(G), pair = 2 * tile;
+  const int tile = tokens_a_tile(G), few = tokens_a_few(G);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * page;
   const Plan p = plan_view(a.plan, n, Hkv, G, a.max_tokens);
   int* sorted = p.scratch;          // rows with tokens, by group: their prefix, n where there are no prefix keys
-  int* place = sorted + n;          // of a sorted entry: tokens of the entries before it
-  int* group_of = place + n + 1;    // of a sorted entry
-  int* group = group_of + n;        // of a group: tokens before its first
-  int* group_item = group + n + 1;  // of a group: its first item
+  int* group_of = sorted + n;       // of a sorted entry
+  int* group_tok = group_of + n;    // of a group: its tokens
+  int* list = group_tok + n + 1;    // the rows of a kind of items, by key
+  int* key = list + n;              // of a listed row: its prefix; n and n + 1 where the items hold no prefix keys
+  int* place = key + n;             // of a listed row: tokens of those before it
+  int* first_tok = place + n + 1;   // of a key: tokens before its first
+  int* first_item = first_tok + n + 2;
   if (threadIdx.x == 0) bad = 0, unsorted = 0;
   pdl_wait();
   pdl_trigger();
@@ -98,7 +101,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       *p.head = head;
       if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
     }
-    for (int c = threadIdx.x; c < MAX_CTAS; c += THREADS) p.first[c] = 0;
+    for (int c = threadIdx.x; c <= MAX_CTAS; c += THREADS) p.first[c] = 0;
     return;
   }
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
@@ -124,176 +127,296 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     for (int i = threadIdx.x; i < ns; i += THREADS) sorted[i] = keys[i] & ((1 << ROW_BITS) - 1), group_of[i] = keys[i] >> ROW_BITS;
     __syncthreads();
   }
-  int carry = 0;
-  for (int i0 = 0; i0 < ns; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    const int tok = i < ns ? tokens_of(sorted[i]) : 0;
-    const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
-    if (i < ns) {
-      place[i] = at;
-      if (i == 0 || group_of[i - 1] != group_of[i]) group[group_of[i]] = at;
-    }
-    carry += static_cast<int>(total);
-  }
-  if (threadIdx.x == 0) place[ns] = carry;
-  __syncthreads();
-
-  // items, written by the last row of each group
-  int n_items = 0;
-  for (int i0 = 0; i0 < ns; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    const int g = i < ns ? group_of[i] : 0;
-    int count = 0, tok = 0;
-    if (i < ns && (i + 1 == ns || group_of[i + 1] != g)) {
-      tok = place[i + 1] - group[g];
-      count = (tok + pair - 1) / pair;
-    }
-    const int at = n_items + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-    if (count > 0) group_item[g] = at;
-    for (int c = 0; c < count; ++c) {
-      Item it{};
-      it.tok = group[g] + c * pair;
-      it.n_tok = min(pair, tok - c * pair);
-      it.prefix_keys = g < n ? a.seq_lens[g] : 0;
-      p.items[at + c] = it;
-    }
-    n_items += static_cast<int>(total);
-  }
-  __syncthreads();
-
-  // runs, by their rows: a row writes its own run in each item that has tokens of it, and the prefix's in each item
-  // that begins with it
-  int n_runs = 0;
-  for (int i0 = 0; i0 < ns; i0 += THREADS) {
-    const int i = i0 + threadIdx.x;
-    int in = 0, tok = 0, k0 = 0, k1 = -1, begun = 0, g = 0;
-    if (i < ns) {
-      g = group_of[i];
-      in = place[i] - group[g];
-      tok = place[i + 1] - place[i];
-      k0 = in / pair;
-      k1 = (in + tok - 1) / pair;
-      begun = k1 - (in + pair - 1) / pair + 1;  // items whose first token is one of the row's
-    }
-    const int count = k1 - k0 + 1 + (g < n ? begun : 0);
-    int at = n_runs + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-    for (int k = k0; k <= k1; ++k) {
-      Item& it = p.items[group_item[g] + k];
-      const int lo = max(in, k * pair), hi = min(in + tok, (k + 1) * pair);  // places in the group
-      if (lo == k * pair) {
-        it.run = at;
-        if (g < n) {
-          const int keys_ = a.seq_lens[g];
-          p.runs[at++] = Run{g, 0, (keys_ + page - 1) / page, keys_, 0, it.n_tok, -1, 0};
-        }
+  // a group's tokens: its rows stand together
+  {
+    int carry = 0;
+    for (int i0 = 0; i0 < ns; i0 += THREADS) {
+      const int i = i0 + threadIdx.x;
+      const int tok = i < ns ? tokens_of(sorted[i]) : 0;
+      const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
+      if (i < ns) {
+        place[i] = at;
+        if (i == 0 || group_of[i - 1] != group_of[i]) first_tok[group_of[i]] = at;
       }
-      const int row = sorted[i], len = a.seq_lens[row];
-      const int seen = max(0, len - (in + tok - hi));  // own keys of its last token here: each token behind it sees one more
-      p.runs[at++] = Run{row, 0, (seen + page - 1) / page, seen, lo - k * pair, hi - k * pair, a.tok_off[row] + lo - in, 0};
+      carry += static_cast<int>(total);
     }
-    n_runs += static_cast<int>(total);
+    if (threadIdx.x == 0) place[ns] = carry;
+    __syncthreads();
+    for (int i = threadIdx.x; i < ns; i += THREADS)
+      if (i + 1 == ns || group_of[i + 1] != group_of[i]) group_tok[group_of[i]] = place[i + 1] - first_tok[group_of[i]];
+    __syncthreads();
   }
-  __syncthreads();
+  auto small = [&](int row) { return tokens_of(row) <= few; };
+  auto few_group = [&](int g) { return g < n && group_tok[g] <= few; };
+  for (int t = threadIdx.x; t < a.tok_off[n]; t += THREADS) p.rec[t] = make_int4(-1, 0, -1, 0);
 
-  // a warp an item: where its runs' pages begin, and the tokens' records
-  for (int k = warp; k < n_items; k += THREADS / 32) {
-    Item it = p.items[k];
-    it.n_runs = (k + 1 < n_items ? p.items[k + 1].run : n_runs) - it.run;
-    int pages = 0, end0 = 0, begin1 = INT_MAX;
-    for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
-      const int r = r0 + lane;
-      Run run{};
-      if (r < it.n_runs) run = p.runs[it.run + r];
-      int inc = run.pages;
+  // Both kinds are laid out alike: rows in the order of their keys, their tokens cut into items.
+  int n_items = 0, n_runs = 0, n_tok = 0;
+  for (int kind = 0; kind < 2; ++kind) {
+    const int cut = kind ? few : 2 * tile;
+    int nl = 0;
+    // tiles: all but the prefixes that have few rows, and rows with few tokens that read no prefix.  few: those prefixes'
+    // rows; rows with few tokens whose prefix tiles read; and those that read none
+    for (int part = 0; part < (kind ? (few > 0 ? 3 : 0) : 1); ++part) {
+      for (int i0 = 0; i0 < ns; i0 += THREADS) {
+        const int i = i0 + threadIdx.x;
+        bool in = false;
+        int row = 0, k = 0;
+        if (i < ns) {
+          row = sorted[i];
+          k = group_of[i];
+          const bool fg = few_group(k);
+          if (kind == 0) {
+            in = !fg && (k < n || !small(row));
+          } else if (part == 0) {
+            in = fg;
+          } else {
+            in = !fg && small(row) && (part == 1 ? k < n && a.seq_lens[row] > 0 : k == n);
+            k = n + part - 1;
+          }
+        }
+        const int at = nl + static_cast<int>(block_exclusive(static_cast<unsigned long long>(in), warp_sum, total));
+        if (in) list[at] = row, key[at] = k;
+        nl += static_cast<int>(total);
+      }
+    }
+    __syncthreads();
+    int carry = 0;
+    for (int i0 = 0; i0 < nl; i0 += THREADS) {
+      const int i = i0 + threadIdx.x;
+      const int tok = i < nl ? tokens_of(list[i]) : 0;
+      const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
+      if (i < nl) {
+        place[i] = at;
+        if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = at;
+      }
+      carry += static_cast<int>(total);
+    }
+    if (threadIdx.x == 0) place[nl] = carry;
+    __syncthreads();
+
+    // items, written by the last row of each key
+    const int items0 = n_items;
+    for (int i0 = 0; i0 < nl; i0 += THREADS) {
+      const int i = i0 + threadIdx.x;
+      const int k = i < nl ? key[i] : 0;
+      int count = 0, tok = 0;
+      if (i < nl && (i + 1 == nl || key[i + 1] != k)) {
+        tok = place[i + 1] - first_tok[k];
+        count = (tok + cut - 1) / cut;
+      }
+      const int at = n_items + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
+      if (count > 0) first_item[k] = at;
+      for (int c = 0; c < count; ++c) {
+        Item it{};
+        it.tok = n_tok + first_tok[k] + c * cut;
+        it.n_tok = min(cut, tok - c * cut);
+        it.prefix_keys = k < n ? a.seq_lens[k] : 0;
+        it.flags = kind == 0 ? ITEM_ALONE : ITEM_FEW | (k == n ? 0u : ITEM_ALONE);
+        p.items[at + c] = it;
+      }
+      n_items += static_cast<int>(total);
+    }
+    __syncthreads();
+
+    // runs, by their rows: a row writes its own run in each item that has tokens of it (of tiles: unless a few item has
+    // its own keys), and the prefix's in each item that begins with it
+    for (int i0 = 0; i0 < nl; i0 += THREADS) {
+      const int i = i0 + threadIdx.x;
+      int in = 0, tok = 0, k0 = 0, k1 = -1, begun = 0, k = 0;
+      bool own = false;
+      if (i < nl) {
+        k = key[i];
+        in = place[i] - first_tok[k];
+        tok = place[i + 1] - place[i];
+        k0 = in / cut;
+        k1 = (in + tok - 1) / cut;
+        begun = k1 - (in + cut - 1) / cut + 1;  // items whose first token is one of the row's
+        own = kind == 1 || !small(list[i]);
+      }
+      const int count = (own ? k1 - k0 + 1 : 0) + (k < n ? begun : 0);
+      int at = n_runs + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
+      for (int c = k0; c <= k1; ++c) {
+        Item& it = p.items[first_item[k] + c];
+        const int lo = max(in, c * cut), hi = min(in + tok, (c + 1) * cut);  // places among the key's tokens
+        if (lo == c * cut) {
+          it.run = at;
+          if (k < n) {
+            const int keys_ = a.seq_lens[k];
+            p.runs[at++] = Run{k, 0, (keys_ + page - 1) / page, keys_, 0, it.n_tok, -1, 0};
+          }
+        }
+        if (!own) continue;
+        const int row = list[i];
+        const int seen = max(0, a.seq_lens[row] - (in + tok - hi));  // own keys of its last token here
+        p.runs[at++] = Run{row, 0, (seen + page - 1) / page, seen, lo - c * cut, hi - c * cut, a.tok_off[row] + lo - in, 0};
+      }
+      n_runs += static_cast<int>(total);
+    }
+    __syncthreads();
+
+    // a warp a row: its tokens' items; a token with a few item beside its tiles spoils the tiles' being alone
+    for (int i = warp; i < nl; i += THREADS / 32) {
+      const int row = list[i], k = key[i], in = place[i] - first_tok[k], tok = place[i + 1] - place[i], t0 = a.tok_off[row];
+      const bool beside = kind == 0 && k < n && small(row) && a.seq_lens[row] > 0;
+      for (int j = lane; j < tok; j += 32) {
+        const int item = first_item[k] + (in + j) / cut, at = (in + j) % cut;
+        const int o = n_tok + place[i] + j;
+        p.order[o] = t0 + j;
+        p.own[o] = make_int2(0, 0);
+        int2* rec = reinterpret_cast<int2*>(p.rec + t0 + j) + kind;
+        *rec = make_int2(item, at);
+        if (beside) p.items[item].flags = 0;
+      }
+    }
+    __syncthreads();
+
+    // a warp an item: where its runs' pages begin, and its tokens' own columns
+    for (int c = items0 + warp; c < n_items; c += THREADS / 32) {
+      Item it = p.items[c];
+      it.n_runs = (c + 1 < n_items ? p.items[c + 1].run : n_runs) - it.run;
+      int pages = 0, end0 = 0, begin1 = INT_MAX;
+      for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
+        const int r = r0 + lane;
+        Run run{};
+        if (r < it.n_runs) run = p.runs[it.run + r];
+        int inc = run.pages;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int u = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += u;
-      }
-      const int off = pages + inc - run.pages;
-      if (r < it.n_runs) {
-        p.runs[it.run + r].off = off;
-        if (run.tok0 < tile) end0 = max(end0, off + run.pages);
-        if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
-        const int seen1 = run.keys - (run.tok1 - run.tok0);  // + 1 for the first token, and so on
-        for (int x = run.tok0; run.token >= 0 && x < run.tok1; ++x) {
-          const int t = run.token + x - run.tok0;
-          p.order[it.tok + x] = t;
-          // a row with more new tokens than keys: its first tokens see none, however many those of its last are
-          const int own = max(0, run.keys > 0 ? seen1 + x - run.tok0 + 1 : 0);
-          p.rec[t] = make_int4(k, x, off * page, own);
-          p.own[it.tok + x] = make_int2(off * page, off * page + own);
+        for (int o = 1; o < 32; o <<= 1) {
+          const int u = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += u;
         }
+        const int off = pages + inc - run.pages;
+        if (r < it.n_runs) {
+          p.runs[it.run + r].off = off;
+          if (run.tok0 < tile) end0 = max(end0, off + run.pages);
+          if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
+          // the last token sees the run's keys, each before it one less
+          for (int x = run.tok0; run.token >= 0 && x < run.tok1; ++x)
+            p.own[it.tok + x] = make_int2(off * page, off * page + max(0, run.keys - (run.tok1 - 1 - x)));
+        }
+        pages += __shfl_sync(0xffffffffu, inc, 31);
       }
-      pages += __shfl_sync(0xffffffffu, inc, 31);
+      end0 = __reduce_max_sync(0xffffffffu, end0);
+      begin1 = __reduce_min_sync(0xffffffffu, begin1);
+      if (lane == 0) {
+        it.pages = pages;
+        it.blocks = (pages + page_blk - 1) / page_blk;
+        it.end0 = (end0 + page_blk - 1) / page_blk;
+        it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
+        it.begin1 = begin1 / page_blk;
+        p.items[c] = it;
+      }
     }
-    end0 = __reduce_max_sync(0xffffffffu, end0);
-    begin1 = __reduce_min_sync(0xffffffffu, begin1);
-    if (lane == 0) {
-      it.pages = pages;
-      it.blocks = (pages + page_blk - 1) / page_blk;
-      it.end0 = (end0 + page_blk - 1) / page_blk;
-      it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
-      it.begin1 = begin1 / page_blk;
-      p.items[k] = it;
-    }
+    n_tok += carry;
+    __syncthreads();
   }
-  __syncthreads();
 
   // the line
-  unsigned long long line = 0;
+  unsigned long long line = 0, tiles_line = 0;
+  int longest = 1;  // of a block: a share holds one at least
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    const uint32_t blocks = i < n_items ? p.items[i].blocks : 0;
-    const unsigned long long cost = blocks > 0 ? static_cast<unsigned long long>(Hkv) * (blocks + OVERHEAD) : 0;
-    const unsigned long long at = line + block_exclusive(cost, warp_sum, total);
-    if (i < n_items) p.items[i].cost = static_cast<uint32_t>(at);
+    unsigned long long length = 0, tiles = 0;
+    if (i < n_items) {
+      const Item it = p.items[i];
+      length = static_cast<unsigned long long>(Hkv) * length_of(it, G);
+      if (!(it.flags & ITEM_FEW)) tiles = length;
+      if (it.blocks > 0) longest = max(longest, static_cast<int>(block_length(it.flags & ITEM_FEW, two_tiles(it, G))));
+    }
+    const unsigned long long at = line + block_exclusive(length, warp_sum, total);
+    if (i < n_items) p.items[i].start = static_cast<uint32_t>(at);
     line += total;
+    block_exclusive(tiles, warp_sum, total);
+    tiles_line += total;
   }
-  const bool fits = line < 0x80000000ull;
-  const uint32_t share = fits ? max(1u, static_cast<uint32_t>((line + n_ctas - 1) / n_ctas)) : 1;
-  const int n_flat = n_items * Hkv;
-  for (int c = threadIdx.x; c < MAX_CTAS; c += THREADS) p.first[c] = n_flat;
+  if (threadIdx.x == 0) unsorted = 1;
+  __syncthreads();
+  atomicMax(&unsorted, longest);
+  __syncthreads();
+  longest = unsorted;
+  const bool fits = line < 0x20000000ull;
+  uint32_t share = 1;
+  if (fits) {
+    // the few items begin with a CTA's share: the least share with which both kinds' CTAs are there
+    const uint32_t tiles = static_cast<uint32_t>(tiles_line), rest = static_cast<uint32_t>(line - tiles_line), ctas = n_ctas;
+    share = max(static_cast<uint32_t>(longest), static_cast<uint32_t>((line + ctas - 1) / ctas));
+    while (ctas > 1 && (tiles + share - 1) / share + (rest + share - 1) / share > ctas) share += 1 + share / 256;
+    const uint32_t shift = (tiles + share - 1) / share * share - tiles;
+    for (int i = threadIdx.x; i < n_items; i += THREADS)
+      if (p.items[i].flags & ITEM_FEW) p.items[i].start += shift;
+    line += shift;
+  }
+  __syncthreads();
+  const int n_flat = fits ? n_items * Hkv : 0;
+  // the CTAs' segments, rows of partial results, pieces of the join's list
+  unsigned long long segments = 0, rows = 0;  // in the upper half of rows: pieces
+  for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
+    const int f = f0 + threadIdx.x;
+    unsigned long long count = 0;
+    uint32_t segs = 0;
+    int entry_rows = 0;
+    bool right_away = false;
+    Item it{};
+    OnLine on{0, 1};
+    if (f < n_flat) {
+      it = p.items[f / Hkv];
+      on = on_line(it, f % Hkv, G);
+      segs = on.segments(it.blocks, share);
+      right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
+      if (!right_away) {
+        entry_rows = it.n_tok * G;
+        count = static_cast<unsigned long long>(segs) * entry_rows * copies_of(it, G);
+        // rows of a few item beside tiles are joined by the tiles' pieces
+        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) == ITEM_FEW) entry_rows = 0;
+        count |= static_cast<unsigned long long>((entry_rows + JOIN_ROWS - 1) / JOIN_ROWS) << 32;
+      }
+    }
+    const unsigned long long at = rows + block_exclusive(count, warp_sum, total);
+    rows += total;
+    if (f < n_flat) p.part[f] = static_cast<uint32_t>(at);
+    for (int r = 0; r < entry_rows; r += JOIN_ROWS) p.join[(at >> 32) + r / JOIN_ROWS] = make_int2(f, r);
+    const uint32_t seg0 = static_cast<uint32_t>(segments + block_exclusive(static_cast<unsigned long long>(segs), warp_sum, total));
+    segments += total;
+    for (uint32_t i = 0; i < segs; ++i) {
+      const uint32_t c = on.cta_of(0, share) + i;
+      Segment sg{};
+      sg.f = f;
+      sg.h = f % Hkv;
+      sg.b0 = on.block_from(c * share, it.blocks);
+      sg.b1 = on.block_from((c + 1) * share, it.blocks);
+      sg.tok = it.tok, sg.n_tok = it.n_tok, sg.run = it.run, sg.n_runs = it.n_runs;
+      sg.prefix_keys = it.prefix_keys, sg.pages = it.pages;
+      sg.end0 = it.end0, sg.begin1 = it.begin1, sg.prefix_blocks = it.prefix_blocks;
+      sg.flags = (two_tiles(it, G) ? SEG_TWO : 0u) | (it.flags & ITEM_FEW ? SEG_FEW : 0u) | (right_away ? SEG_WHOLE : 0u);
+      sg.part_row = static_cast<uint32_t>(at) + i * copies_of(it, G) * it.n_tok * G;
+      p.segs[seg0 + i] = sg;
+    }
+  }
+  // a CTA's first segment: the entry in which its share begins tells which
+  __syncthreads();
+  for (int c = threadIdx.x; c <= MAX_CTAS; c += THREADS) {
+    int lo = 0, hi = static_cast<int>(segments);
+    while (lo < hi) {  // the first segment of this CTA or a later one
+      const int mid = (lo + hi) >> 1;
+      const Segment& sg = p.segs[mid];
+      const Item it = p.items[sg.f / Hkv];
+      if (on_line(it, sg.h, G).cta_of(sg.b0, share) < static_cast<uint32_t>(c)) lo = mid + 1; else hi = mid;
+    }
+    p.first[c] = lo;
+  }
   if (threadIdx.x == 0) {
     if (fits) {
       head.tokens = a.tok_off[n];
       head.n_items = n_items;
       head.n_flat = n_flat;
+      head.n_join = static_cast<int>(rows >> 32);
       head.share = share;
       head.total = static_cast<uint32_t>(line);
     }
     *p.head = head;
     if (!fits && a.status) atomicCAS(a.status, 0, DOPR_ERR_UNSUPPORTED);
   }
-  __syncthreads();
-  if (!fits) return;
-  unsigned long long rows = 0;  // of partial results; in the upper half pieces of the join's list
-  for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
-    const int f = f0 + threadIdx.x;
-    unsigned long long count = 0;
-    int entry_rows = 0;
-    if (f < n_flat) {
-      const Item it = p.items[f / Hkv];
-      const bool two = two_tiles(it.n_tok, G);
-      uint32_t segs = 0;
-      if (it.blocks > 0) {
-        const uint32_t b = blocks_begin(it, f % Hkv), e = b + it.blocks, start = b - OVERHEAD;
-        segs = (e - 1) / share - b / share + 1;
-        for (uint32_t c = (start + share - 1) / share; static_cast<unsigned long long>(c) * share < e; ++c)
-          if (c < MAX_CTAS) p.first[c] = f;
-      }
-      if (!two || segs != 1) {  // also where there is no key at all
-        entry_rows = it.n_tok * G;
-        count = static_cast<unsigned long long>(segs) * entry_rows * (two ? 1 : 2) |
-                static_cast<unsigned long long>((entry_rows + JOIN_ROWS - 1) / JOIN_ROWS) << 32;
-      }
-    }
-    const unsigned long long at = rows + block_exclusive(count, warp_sum, total);
-    if (f < n_flat) p.part[f] = static_cast<uint32_t>(at);
-    for (int r = 0; r < entry_rows; r += JOIN_ROWS) p.join[(at >> 32) + r / JOIN_ROWS] = make_int2(f, r);
-    rows += total;
-  }
-  if (threadIdx.x == 0) p.head->n_join = static_cast<int>(rows >> 32);
 }
 
 }  // namespace

@@ -1,16 +1,21 @@
 // shared_attn.cuh -- how a step's attention over the paged cache is split: what k_shared_plan.cu lays down and
 // k_shared_attn.cu walks through.
 //
-// Tokens of rows with one prefix (or of rows without) stand in one order, cut into items of up to two tiles of 128 rows
-// (G = q heads a kv head rows a token).  An item's keys are a list of pages, as runs: the prefix's pages, which all its
-// tokens see, then for each of its rows the row's own pages, as far as its last token in the item sees them; a token
-// sees its own run's keys up to itself.  A page's place in the list is its place in the columns of S, so a token's keys
-// are two intervals of columns.  128 columns are a block.
+// Tokens that read the same keys stand together in an item.  There are two kinds, by the rows (G = q heads a kv head rows
+// a token) that share the keys:
+//   tiles  up to two tiles of 128 rows for the 5th-generation tensor cores: the tokens of rows with one prefix, or
+//          without, cut into items;
+//   few    up to 16 rows for warp-level products: all tokens of a prefix that has no more; and the own keys of rows with
+//          few new tokens, beside the tiles that read their prefix (a step of one token a row: the prefix is read by
+//          tiles of many rows, each row's own keys by its own few) or by themselves where there is no prefix.
+// An item's keys are a list of pages, as runs: the prefix's pages, which all its tokens see, then the own pages of its rows,
+// as far as their last token in the item sees them; a token sees its own run's keys up to itself.  A page's place in the
+// list is its place in the columns of the scores, so a token's keys are two intervals of columns.  128 columns are a block.
 //
-// An item and a kv head are a flat entry.  The flat entries' blocks lie one after another on a line on which each entry
-// also takes OVERHEAD steps, and every CTA takes an equal share of the line.  What a CTA has of an entry is a segment; it
-// leaves partial softmax results (maximum, sum, weighted values), which the joining kernel adds up by row; only an entry
-// of two tiles that is whole in one CTA gives its rows' results right away.
+// An item and a kv head are a flat entry.  The flat entries lie one after another on a line, on which an entry takes a
+// length for its start and end and one for each block, and every CTA takes the blocks that begin in an equal share of the
+// line, of tiles or of few items.  What a CTA has of an entry is a segment; it leaves partial softmax results (maximum, sum, weighted values), which
+// the joining kernel adds up by row, unless they are all that its rows have: then it gives the rows' results right away.
 #pragma once
 
 #include "device_common.cuh"
@@ -20,10 +25,13 @@ namespace dopr {
 namespace shared_attn {
 
 constexpr int TILE = 128;   // rows of a tile
+constexpr int FEW = 16;     // rows of a few item
 constexpr int BLOCK = 128;  // columns of a block
-constexpr uint32_t OVERHEAD = 2;
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
+// Lengths on the line, about 0.3 us each: a block of two tiles, of one, of a few item; an entry's start and end.
+__host__ __device__ constexpr uint32_t block_length(bool few, bool two) { return few ? 4 : two ? 6 : 4; }
+__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 : 10; }
 
 struct alignas(16) Run {
   int row;    // table row
@@ -39,11 +47,31 @@ struct alignas(16) Item {
   int run, n_runs;
   int prefix_keys;
   int pages;
-  uint32_t cost;     // where its first entry begins on the line
+  uint32_t start;    // where its first entry begins on the line
   uint32_t blocks;
-  // blocks that concern the first tile's rows: [0, end0); the second's: [0, prefix_blocks) and from begin1 on
+  // tiles: blocks that concern the first tile's rows: [0, end0); the second's: [0, prefix_blocks) and from begin1 on
   uint32_t end0, begin1, prefix_blocks;
+  uint32_t flags;
+};
+enum : uint32_t {
+  ITEM_FEW = 1,    // a few item
+  ITEM_ALONE = 2,  // its tokens are in no other item
+};
+// What a CTA has of a flat entry, with what its warps need to know of the item.
+struct alignas(16) Segment {
+  int f, h;           // flat entry, kv head
+  uint32_t b0, b1;    // its blocks here
+  int tok, n_tok, run, n_runs;
+  int prefix_keys, pages;
+  uint32_t end0, begin1, prefix_blocks;
+  uint32_t flags;
+  uint32_t part_row;  // first row of its partial results
   int pad;
+};
+enum : uint32_t {
+  SEG_TWO = 1,    // two tiles
+  SEG_FEW = 2,
+  SEG_WHOLE = 4,  // gives its rows' results right away
 };
 struct alignas(16) Head {
   int tokens, n_items, n_flat, n_join;
@@ -56,21 +84,29 @@ __host__ __device__ inline bool made_for(const Head& h, const dopr_cache_layout&
 }
 struct Plan {
   Head* head;
-  int* first;      // [MAX_CTAS] flat entry in which a CTA's share begins
-  int4* rec;       // [tokens] item, place in it, first column of its own keys, own keys seen
+  int* first;      // [MAX_CTAS + 1] a CTA's first segment
+  Segment* segs;   // in the CTAs' order
+  int4* rec;       // [tokens] item of tiles and place in it, few item and place in it (-1: none)
   Item* items;
   Run* runs;
   uint32_t* part;  // [flat entry] first row of its partial results
   int2* join;      // flat entry, first of up to JOIN_ROWS rows that are to be added up from partial results
-  int* order;      // [tokens]
-  int2* own;       // [tokens, in that order] columns of its own keys, from and to
-  int* scratch;    // 5 * n_seqs + 5, of the plan kernel
+  int* order;      // [2 * tokens] the items' tokens
+  int2* own;       // [2 * tokens, in that order] columns of its own keys, from and to
+  int* scratch;    // 8 * n_seqs + 8, of the plan kernel
   int64_t bytes;
 };
 __host__ __device__ inline int tokens_a_tile(int G) { return TILE / G; }
+__host__ __device__ inline int tokens_a_few(int G) { return FEW / G; }  // 0: no few items
 __host__ __device__ inline int64_t max_items(int n_seqs, int G, int max_tokens) {
-  const int pair = 2 * tokens_a_tile(G);
-  return (static_cast<int64_t>(max_tokens) + pair - 1) / pair + (n_seqs < max_tokens ? n_seqs : max_tokens);
+  const int pair = 2 * tokens_a_tile(G), few = tokens_a_few(G);
+  const int64_t rows = n_seqs < max_tokens ? n_seqs : max_tokens;
+  // whole items and a last one a prefix, of each kind
+  return (static_cast<int64_t>(max_tokens) + pair - 1) / pair + rows +
+         (few > 0 ? (static_cast<int64_t>(max_tokens) + few - 1) / few + rows + 2 : 0);
+}
+__host__ __device__ inline int64_t max_pieces(int n_seqs, int n_kv_heads, int G, int max_tokens) {
+  return max_items(n_seqs, G, max_tokens) * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / JOIN_ROWS;
 }
 __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads, int G, int max_tokens) {
   uint8_t* b = static_cast<uint8_t*>(base);
@@ -83,31 +119,52 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   const int64_t items = max_items(n_seqs, G, max_tokens);
   Plan p;
   p.head = static_cast<Head*>(take(sizeof(Head)));
-  p.first = static_cast<int*>(take(MAX_CTAS * 4));
+  p.first = static_cast<int*>(take((MAX_CTAS + 1) * 4));
   p.rec = static_cast<int4*>(take(16 * static_cast<int64_t>(max_tokens)));
+  p.segs = static_cast<Segment*>(take((items * n_kv_heads + MAX_CTAS) * static_cast<int64_t>(sizeof(Segment))));
   p.items = static_cast<Item*>(take(items * static_cast<int64_t>(sizeof(Item))));
   // a run for every row, one more wherever an item ends within a row, and the prefixes'
-  p.runs = static_cast<Run*>(take((2 * items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));
+  p.runs = static_cast<Run*>(take(2 * (items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));
   p.part = static_cast<uint32_t*>(take(4 * items * n_kv_heads));
-  p.join = static_cast<int2*>(take(8 * (items * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / JOIN_ROWS)));
-  p.order = static_cast<int*>(take(4 * static_cast<int64_t>(max_tokens)));
-  p.own = static_cast<int2*>(take(8 * static_cast<int64_t>(max_tokens)));
-  p.scratch = static_cast<int*>(take(4 * (5 * static_cast<int64_t>(n_seqs) + 5)));
+  p.join = static_cast<int2*>(take(8 * max_pieces(n_seqs, n_kv_heads, G, max_tokens)));
+  p.order = static_cast<int*>(take(8 * static_cast<int64_t>(max_tokens)));
+  p.own = static_cast<int2*>(take(16 * static_cast<int64_t>(max_tokens)));
+  p.scratch = static_cast<int*>(take(4 * (8 * static_cast<int64_t>(n_seqs) + 8)));
   p.bytes = at;
   return p;
 }
-// Rows of partial results at most.  An entry of two tiles leaves some only where it is split: a boundary between CTAs
-// makes two segments of at most 256 rows.  An item of one tile (at most one for every prefix, hence for every row) leaves
-// two for each segment, its two halves of the blocks.
+// Rows of partial results at most.  Of tiles, a token's rows are left once where they have a few item too, or twice where
+// the item has one tile (its two halves of the blocks); of few items once.  Either kind of tiles holds the tokens of some
+// row with few tokens or ends a prefix, so there is at most one for every row.  A boundary between CTAs makes one segment
+// more, of at most 256 rows, or two of what would have given its rows' results right away.
 __host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int G, int max_tokens, int n_ctas) {
-  const int64_t all = static_cast<int64_t>(max_tokens) * G, single = static_cast<int64_t>(TILE) * n_seqs;
-  return 2 * n_kv_heads * (all < single ? all : single) + 4 * TILE * static_cast<int64_t>(n_ctas);
+  const int64_t all = static_cast<int64_t>(max_tokens) * G, n = n_seqs;
+  const int64_t tiles = 2 * all < 4 * TILE * n ? 2 * all : 4 * TILE * n, few = all < FEW * n ? all : FEW * n;
+  // even, so that the values behind the maxima and sums begin on 16 bytes
+  return (n_kv_heads * (tiles + few) + 1) / 2 * 2 + 4 * TILE * static_cast<int64_t>(n_ctas);
 }
 
-__host__ __device__ inline bool two_tiles(int n_tok, int G) { return n_tok > tokens_a_tile(G); }
-// Where the blocks of kv head h of an item begin on the line.
-__device__ __forceinline__ uint32_t blocks_begin(const Item& it, int h) {
-  return it.cost + h * (it.blocks + OVERHEAD) + OVERHEAD;
+__host__ __device__ inline bool two_tiles(const Item& it, int G) { return !(it.flags & ITEM_FEW) && it.n_tok > tokens_a_tile(G); }
+__host__ __device__ inline uint32_t copies_of(const Item& it, int G) { return (it.flags & ITEM_FEW) || two_tiles(it, G) ? 1 : 2; }
+// The blocks of kv head h's entry on the line: where the first begins and the length of one.
+struct OnLine {
+  uint32_t begin, length;
+  // first block that begins at or behind a place on the line
+  __host__ __device__ uint32_t block_from(uint32_t at, uint32_t blocks) const {
+    if (at <= begin) return 0;
+    const uint32_t b = (at - begin + length - 1) / length;
+    return b < blocks ? b : blocks;
+  }
+  __host__ __device__ uint32_t cta_of(uint32_t block, uint32_t share) const { return (begin + block * length) / share; }
+  __host__ __device__ uint32_t segments(uint32_t blocks, uint32_t share) const {
+    return blocks > 0 ? cta_of(blocks - 1, share) - cta_of(0, share) + 1 : 0;
+  }
+};
+__host__ __device__ inline uint32_t length_of(const Item& it, int G) {
+  return it.blocks > 0 ? entry_length(it.flags & ITEM_FEW) + it.blocks * block_length(it.flags & ITEM_FEW, two_tiles(it, G)) : 0;
+}
+__host__ __device__ inline OnLine on_line(const Item& it, int h, int G) {
+  return OnLine{it.start + h * length_of(it, G) + entry_length(it.flags & ITEM_FEW), block_length(it.flags & ITEM_FEW, two_tiles(it, G))};
 }
 
 }  // namespace shared_attn

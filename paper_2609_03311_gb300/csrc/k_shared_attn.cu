@@ -6,18 +6,18 @@
 // part itself runs over its keys block by block the same way.
 //
 // k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh), which holds either
-// tiles or few items.  In both, warps 0 and 2 copy K and V blocks, page by page, into two rings (TMA; a page's rows of a kv
-// head lie together).
+// tiles or few items.
 //   Tiles: an item of two tiles gives each block of 128 columns to the softmax groups of the tiles that it concerns, a tile
 //   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
+//     warp 0, 2  copy K and V blocks into two rings, page by page (TMA; a page's rows of a kv head lie together)
 //     warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
 //     warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
 //     warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more than
 //                2^8 (P stays within the type's range until then)
-//   Few items: warps 4-11 do 16-row warp-level products, 16 columns of each block a warp, and add their eight results up
-//   at the end of a segment; the room of Q goes to the rings.
+//   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
+//   box by TMA takes about 80 ns of an SM (the rate of ragged documents in pages of 16 was 2 KB a box, 73 us for 63).
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
-// Values would (0 x NaN), so rows of V past a run's keys are cleared in shared memory.  A value that one token sees and
+// Values would (0 x NaN), so rows of V past a run's keys are zero in shared memory.  A value that one token sees and
 // another of the item does not would too: rows that end with a NaN though their scores have none are computed alone.
 //
 // k_shared_join, a warp a row, adds the parts up.
@@ -48,15 +48,14 @@ struct Smem {
   static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // where the Q gatherer's rows lie
   static constexpr int OFF_KEYS = OFF_ROW + 128 * 8;  // of each page of a V stage: rows that hold keys
   static constexpr int OFF_BAR = OFF_KEYS + 64;
-  // few items: the rings begin at 0
-  static constexpr int FK_STAGES = D == 128 ? 3 : 6, FV_STAGES = D == 128 ? 4 : 6;
-  static_assert((FK_STAGES + FV_STAGES) * TILE_BYTES <= OFF_ROW, "the few items' rings");
+  // few items: from 0 on, pieces of 16 columns of K and V, F_STAGES of them a warp
+  static constexpr int F_STAGES = D == 128 ? 3 : 6;
+  static_assert(WORKERS * F_STAGES * 2 * HALVES * PIECE * 128 <= OFF_ROW, "the few items' pieces");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
-                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, FK_FULL = DRAIN + 1, FK_EMPTY = FK_FULL + FK_STAGES,
-                       FV_FULL = FK_EMPTY + FK_STAGES, FV_EMPTY = FV_FULL + FV_STAGES, N_BARS = FV_EMPTY + FV_STAGES;
+                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
   static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
-  static_assert(V_STAGES * 8 <= 64 && FV_STAGES * 8 <= 64, "a byte a page");
+  static_assert(V_STAGES * 8 <= 64, "a byte a page");
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
@@ -126,33 +125,16 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 }
-// A barrier of warps 4-11; true in all of them when `x` is in any.
-__device__ __forceinline__ bool eight_any(bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
-      "barrier.cta.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(r)
-      : "r"(static_cast<uint32_t>(x))
-      : "memory");
-  return r != 0;
-}
-
-// One segment after another of this CTA's share.
+// One segment after another of a share: of tiles a CTA's, of few items a warp's.
 struct Walk {
   const Segment* segs;
   int at, end;
-  __device__ __forceinline__ explicit Walk(const SharedAttnArgs& a) {
+  __device__ __forceinline__ Walk(const SharedAttnArgs& a, int share) {
     const Plan p = plan_of(a);
     segs = p.segs;
-    at = p.first[blockIdx.x];
-    end = p.first[blockIdx.x + 1];
-    if (!made_for(*p.head, a.lay, a.Hq, a.max_tokens, gridDim.x)) {
-      if (a.status && threadIdx.x == 0) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-      at = end = 0;
-    }
+    at = p.first[share];
+    end = p.first[share + 1];
   }
-  __device__ __forceinline__ bool few() const { return at < end && (segs[at].flags & SEG_FEW); }  // at the start
   __device__ __forceinline__ bool next(Segment& s) {
     if (at >= end) return false;
     s = segs[at++];
@@ -299,21 +281,71 @@ __device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, in
   if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
 }
 
-// A share of few items by warps 4-11: warp `wi` takes columns 16 wi .. + 15 of each block.  Fragments of the products: a
-// thread has rows lane / 4 and lane / 4 + 8 of the item, and of each 8 columns two from 2 (lane % 4).  Bound by the copies
-// of K and V (64 KB a block of head size 128: 1.5 us of an SM's part of the memory's rate).
+// A share of few items by one warp, a piece of 16 columns at a time, three or six of them on their way in shared memory of
+// its own: what a warp waits for, the others do not.  Fragments of the products: a thread has rows lane / 4 and lane / 4 + 8
+// of the item, and of each 8 columns two from 2 (lane % 4).  Bound by the copies of K and V: 8 KB a piece of head size 128,
+// 1.5 us of an eighth of an SM's part of the memory's rate, of which the products and the softmax take a third.
 template <typename T, int D>
-__device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint8_t* smem, uint32_t s0, int wi, int lane, int* err) {
+__device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint32_t s0, int wi, int share, int lane) {
   using L = Smem<D>;
-  auto bar = [&](int i) { return s0 + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
+  constexpr int HALF = PIECE * 128, KV = L::HALVES * HALF;  // 64 elements a row; K or V of a piece
+  constexpr int CHUNKS = D / 8;                             // 16-byte chunks of a row
+  const uint32_t base = s0 + wi * L::F_STAGES * 2 * KV;
+  const Plan plan = plan_of(a);
   const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
   const float scale_log2 = a.scale * 1.4426950408889634f;
   const int quad = lane >> 2, in_quad = lane & 3;
-  const Plan plan = plan_of(a);
-  Walk walk(a);
-  Ring rk, rv;
+  Walk walk(a, share);
   Segment s;
   while (walk.next(s)) {
+    // where the next 32 pieces lie: a lane a piece
+    int row_at = 0, valid_at = 0;
+    auto find = [&](uint32_t b) {
+      if (b >= s.b1) return;
+      const Run* runs = plan.runs + s.run;
+      int lo = 0, hi = s.n_runs - 1;
+      while (lo < hi) {  // the last run that begins at or before the piece (runs without keys share their successor's place)
+        const int mid = (lo + hi + 1) >> 1;
+        if (runs[mid].off <= static_cast<int>(b)) lo = mid; else hi = mid - 1;
+      }
+      const Run run = runs[lo];
+      const int key = (static_cast<int>(b) - run.off) * PIECE;
+      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
+      if (block < 0 || block >= a.lay.n_blocks) {
+        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+        block = 0;
+      }
+      row_at = (block * Hkv + s.h) * page + key % page;
+      valid_at = min(PIECE, run.keys - key);
+    };
+    uint32_t next = s.b0;
+    int stage = 0, ahead = 0;  // of the piece at hand, of the next one to be copied
+    // rows past the run's keys come as zeros; a group of copies also where there is no piece left
+    auto copy = [&] {
+      if (next < s.b1) {
+        const int at = (next - s.b0) & 31;
+        if (at == 0) find(next + lane);
+        const int64_t row = __shfl_sync(0xffffffffu, row_at, at);
+        const int valid = __shfl_sync(0xffffffffu, valid_at, at);
+        const uint4* k = static_cast<const uint4*>(a.k_pool) + row * CHUNKS + lane;
+        const uint4* v = static_cast<const uint4*>(a.v_pool) + row * CHUNKS + lane;
+        const int c = lane % CHUNKS;
+        const uint32_t dst = base + ahead * 2 * KV + (c >> 3) * HALF;
+#pragma unroll
+        for (int i = 0; i < PIECE * CHUNKS / 32; ++i) {
+          const int r = lane / CHUNKS + i * (32 / CHUNKS);
+          const uint32_t at_row = dst + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+          cp_async16(at_row, k + 32 * i, r < valid);
+          cp_async16(at_row + KV, v + 32 * i, r < valid);
+        }
+        ++next;
+      }
+      cp_async_commit();
+      ahead = ahead + 1 == L::F_STAGES ? 0 : ahead + 1;
+    };
+#pragma unroll 1
+    for (int i = 0; i + 1 < L::F_STAGES; ++i) copy();
+
     const int rows = s.n_tok * G;
     uint32_t q[D / 16][4];
     int own0[2], own1[2];
@@ -335,165 +367,104 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint8_t* smem
     float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    bool ok = true;
-    uint32_t k0 = 0, v0 = 0;
     for (uint32_t b = s.b0; b < s.b1; ++b) {
-      k0 = L::TILE_BYTES * rk.stage;
-      v0 = L::TILE_BYTES * (L::FK_STAGES + rv.stage);
-      const int col0 = b * BLOCK + 16 * wi;
-      const bool mine = col0 < s.pages * page, part = s.prefix_keys < col0 + 16;  // a page is 16 columns or more
-      if (!(ok = mbar_wait_warp(bar(L::FK_FULL + rk.stage), rk.phase, err, WAIT_TIMEOUT_NS))) break;
-      uint32_t p[4] = {0, 0, 0, 0};
-      if (mine) {
-        float sc[2][4];
-        const int row = 16 * wi + (lane & 7);
+      copy();
+      asm volatile("cp.async.wait_group %0;" ::"n"(L::F_STAGES - 1) : "memory");
+      __syncwarp();
+      const uint32_t k0 = base + stage * 2 * KV, v0 = k0 + KV;
+      const int col0 = b * PIECE, row8 = lane & 7;
+      float sc[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+#pragma unroll
+        for (int k = 0; k < D / 16; k += 2) {
+          const int c = 2 * k + (lane >> 3);  // 16-byte piece of the key's row
+          uint32_t x[4];
+          ldmatrix_x4(k0 + (c >> 3) * HALF + (row8 + 8 * t) * 128 + (((c & 7) ^ row8) << 4), x[0], x[1], x[2], x[3]);
+          mma16<T>(sc[t], q[k], x[0], x[1]);
+          mma16<T>(sc[t], q[k + 1], x[2], x[3]);
+        }
+      }
+      if (s.prefix_keys < col0 + PIECE) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int c = col0 + 8 * t + 2 * in_quad + (e & 1), i = e >> 1;
+            if (!(c < s.prefix_keys || (c >= own0[i] && c < own1[i]))) sc[t][e] = -INFINITY;
+          }
+      }
+      uint32_t p[4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2;
+        if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
+        const bool grow = top > m[i] + RESCALE_LOG2;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float by = grow ? ex2(m[i] - top) : 1.f;
+          if (grow) m[i] = top;
+          l[i] *= by;
+#pragma unroll
+          for (int d = 0; d < D / 8; ++d) o[d][2 * i] *= by, o[d][2 * i + 1] *= by;
+        }
+        const float at_m = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
-#pragma unroll
-          for (int k = 0; k < D / 16; k += 2) {
-            const int c = 2 * k + (lane >> 3);  // 16-byte piece of the key's row
-            uint32_t x[4];
-            ldmatrix_x4(s0 + k0 + (c >> 3) * HALF_BYTES + (row + 8 * t) * 128 + (((c & 7) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
-            mma16<T>(sc[t], q[k], x[0], x[1]);
-            mma16<T>(sc[t], q[k + 1], x[2], x[3]);
-          }
-        }
-        if (b + 1 < s.b1) {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(L::FK_EMPTY + rk.stage));
-        }
-        if (part) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int c = col0 + 8 * t + 2 * in_quad + (e & 1), i = e >> 1;
-              if (!(c < s.prefix_keys || (c >= own0[i] && c < own1[i]))) sc[t][e] = -INFINITY;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2;
-          if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
-          const bool grow = top > m[i] + RESCALE_LOG2;
-          if (__any_sync(0xffffffffu, grow)) {
-            const float by = grow ? ex2(m[i] - top) : 1.f;
-            if (grow) m[i] = top;
-            l[i] *= by;
-#pragma unroll
-            for (int d = 0; d < D / 8; ++d) o[d][2 * i] *= by, o[d][2 * i + 1] *= by;
-          }
-          const float base = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const float x = ex2(fmaf(sc[t][2 * i], scale_log2, -base)), y = ex2(fmaf(sc[t][2 * i + 1], scale_log2, -base));
-            l[i] += x + y;  // this thread's columns: the quad's four sums are added up at the end
-            p[2 * t + i] = pack2<T>(x, y);
-          }
-        }
-      } else if (b + 1 < s.b1 && lane == 0) {
-        mbar_arrive(bar(L::FK_EMPTY + rk.stage));
-      }
-      if (!(ok = mbar_wait_warp(bar(L::FV_FULL + rv.stage), rv.phase, err, WAIT_TIMEOUT_NS))) break;
-      if (mine) {
-        const int row = 16 * wi + (lane & 15);
-        if (part) {
-          // rows of V past a page's keys count as zero
-          const bool clear = row % page >= smem[L::OFF_KEYS + rv.stage * 8 + row / page];
-          if (__any_sync(0xffffffffu, clear)) {
-            if (clear)
-#pragma unroll 1
-              for (int c = lane >> 4; c < 8 * L::HALVES; c += 2)
-                *reinterpret_cast<uint4*>(smem + v0 + (c >> 3) * HALF_BYTES + row * 128 + ((c & 7) << 4)) = uint4{0, 0, 0, 0};
-            fence_proxy_async_shared();  // ahead of the copies that follow
-            __syncwarp();
-          }
-        }
-#pragma unroll
-        for (int d = 0; d < D / 8; d += 2) {
-          const int c = d + (lane >> 4);
-          uint32_t x[4];
-          ldmatrix_x4_trans(s0 + v0 + (c >> 3) * HALF_BYTES + row * 128 + (((c & 7) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
-          mma16<T>(o[d], p, x[0], x[1]);
-          mma16<T>(o[d + 1], p, x[2], x[3]);
+          const float x = ex2(fmaf(sc[t][2 * i], scale_log2, -at_m)), y = ex2(fmaf(sc[t][2 * i + 1], scale_log2, -at_m));
+          l[i] += x + y;  // this thread's columns: the quad's four sums are added up at the end
+          p[2 * t + i] = pack2<T>(x, y);
         }
       }
-      if (b + 1 < s.b1) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(L::FV_EMPTY + rv.stage));
-        rk.next(L::FK_STAGES);
-        rv.next(L::FV_STAGES);
+#pragma unroll
+      for (int d = 0; d < D / 8; d += 2) {
+        const int c = d + (lane >> 4), row = lane & 15;
+        uint32_t x[4];
+        ldmatrix_x4_trans(v0 + (c >> 3) * HALF + row * 128 + (((c & 7) ^ (row & 7)) << 4), x[0], x[1], x[2], x[3]);
+        mma16<T>(o[d], p, x[0], x[1]);
+        mma16<T>(o[d + 1], p, x[2], x[3]);
       }
+      __syncwarp();  // every lane has read the stage
+      if (++stage == L::F_STAGES) stage = 0;
     }
-    // The eight warps' results, by way of the last block's stages, which are not handed back before: four in K's, four in
-    // V's.  The barrier also tells every warp whether one gave up, so that none waits for it.
-    if (eight_any(!ok)) return;
-    float2* stats = reinterpret_cast<float2*>(smem + L::OFF_ROW);  // [warp][row] maximum and sum
-    auto sums = [&](int k, int r) { return reinterpret_cast<float*>(smem + (k < 4 ? k0 : v0)) + ((k & 3) * FEW + r) * D; };
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = quad + 8 * i;
       float sum = l[i] + __shfl_xor_sync(0xffffffffu, l[i], 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (in_quad == 0) stats[wi * FEW + r] = make_float2(m[i], sum);
-      // a row begins 8 further round than the one before: the quads' stores go to different banks
-#pragma unroll
-      for (int d = 0; d < D / 8; ++d)
-        *reinterpret_cast<float2*>(sums(wi, r) + (8 * (d + quad) + 2 * in_quad) % D) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
-    }
-    eight_any(false);
-    float2* ml = reinterpret_cast<float2*>(a.ws);
-    float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
-    constexpr int E = D / 32;
-    for (int r = wi; r < rows; r += 8) {  // a warp a row
-      float top = -INFINITY, sum = 0.f, x[E] = {};
-      float2 st[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        st[k] = stats[k * FEW + r];
-        top = fmaxf(top, st[k].x);
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if (st[k].y == 0.f) continue;  // nothing that the row sees, whatever its values
-        const float by = ex2(st[k].x - top);
-        sum += st[k].y * by;
-        const float* src = sums(k, r) + (lane * E + 8 * (r & 7)) % D;
-#pragma unroll
-        for (int i = 0; i < E; ++i) x[i] += src[i] * by;
-      }
       if (s.flags & SEG_WHOLE) {
-        const int t = plan.order[s.tok + r / G], h = s.h * G + r % G;
-        const float inv = inverse(sum);
         bool nan = false;
-        uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);
+        const int t = r < rows ? plan.order[s.tok + r / G] : 0, h = s.h * G + r % G;
+        const float inv = inverse(sum);
+        uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + in_quad;
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] *= inv, nan |= x[i] != x[i];
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-        if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(top, sum);
+        for (int d = 0; d < D / 8; ++d) {
+          const float x = sum == 0.f ? 0.f : o[d][2 * i] * inv, y = sum == 0.f ? 0.f : o[d][2 * i + 1] * inv;
+          nan |= x != x || y != y;
+          if (r < rows) dst[4 * d] = pack2<T>(x, y);
+        }
+        if (r < rows && a.lse && in_quad == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m[i], sum);
         // scores in order, values not: perhaps a value that the row does not see
-        if (sum == sum && __any_sync(0xffffffffu, nan)) row_alone<T, D>(a, t, h, lane);
-      } else {
+        uint32_t odd = __ballot_sync(0xffffffffu, r < rows && nan && sum == sum);
+        while (odd) {
+          const int from = __ffs(odd) - 1;
+          odd &= ~(0xfu << (from & ~3));
+          row_alone<T, D>(a, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
+        }
+      } else if (r < rows) {
+        float2* ml = reinterpret_cast<float2*>(a.ws);
+        float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
         const int64_t row = static_cast<int64_t>(s.part_row) + r;
-        if (lane == 0) ml[row] = make_float2(top, sum);
+        if (in_quad == 0) ml[row] = make_float2(m[i], sum);
         if (sum != 0.f) {
 #pragma unroll
-          for (int i = 0; i < E; i += 2) *reinterpret_cast<float2*>(part_o + row * D + lane * E + i) = make_float2(x[i], x[i + 1]);
+          for (int d = 0; d < D / 8; ++d)
+            *reinterpret_cast<float2*>(part_o + row * D + 8 * d + 2 * in_quad) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
         }
       }
     }
-    fence_proxy_async_shared();
-    __syncwarp();
-    if (lane == 0) {
-      mbar_arrive(bar(L::FK_EMPTY + rk.stage));
-      mbar_arrive(bar(L::FV_EMPTY + rv.stage));
-    }
-    rk.next(L::FK_STAGES);
-    rv.next(L::FV_STAGES);
   }
 }
 
@@ -514,10 +485,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (threadIdx.x == 0) {
     gave_up = 0;
-    for (int i = 0; i < L::N_BARS; ++i) {
-      const bool by_eight = (i >= L::FK_EMPTY && i < L::FV_FULL) || i >= L::FV_EMPTY;
-      mbar_init(bar(i), by_eight ? 8 : i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
-    }
+    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -532,20 +500,31 @@ __global__ void __launch_bounds__(THREADS, 1)
   const uint32_t tmem = *tmem_slot;
   pdl_trigger();
   pdl_wait();
-  // each role finds its way by itself: little is held in registers where their shares change
-  const bool few = Walk(a).few();
   Segment s;
+  const Head head = *plan_of(a).head;
+  const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, gridDim.x);
+  const bool few = static_cast<int>(blockIdx.x) >= head.tile_ctas;
+  if (!good && threadIdx.x == 0 && a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
 
-  if (warp == 0 || warp == 2) {
+  if (!good) {
+  } else if (few) {
+    // the CTAs' first warps before their second ones: few shares are spread over many SMs
+    if (warp >= 4) {
+      const int ctas = gridDim.x - head.tile_ctas;
+      regs_many();
+      few_items<T, D>(a, s0, warp - 4, head.tile_ctas + 1 + (warp - 4) * ctas + static_cast<int>(blockIdx.x) - head.tile_ctas, lane);
+    } else {
+      regs_few();
+    }
+  } else if (warp == 0 || warp == 2) {
     // ======================= K and V blocks, page by page: a lane a page and half of the head
     regs_few();
     const bool is_v = warp == 2;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
-    Walk walk(a);
+    Walk walk(a, blockIdx.x);
     const Plan plan = plan_of(a);
-    const int stages = few ? (is_v ? L::FV_STAGES : L::FK_STAGES) : is_v ? L::V_STAGES : L::K_STAGES;
-    const int full = few ? (is_v ? L::FV_FULL : L::FK_FULL) : is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
-    const uint32_t ring0 = s0 + (few ? (is_v ? L::FK_STAGES * L::TILE_BYTES : 0) : is_v ? L::OFF_V : L::OFF_K);
+    const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
+    const uint32_t ring0 = s0 + (is_v ? L::OFF_V : L::OFF_K);
     const int page = a.lay.page, page_blk = BLOCK / page;
     const int pg = lane / L::HALVES, half = lane % L::HALVES;  // pages of a block: at most 8
     Ring r;
@@ -588,20 +567,13 @@ __global__ void __launch_bounds__(THREADS, 1)
     if (!ok)  // copies in flight land before the CTA ends
       for (int i = 0; i < stages; ++i)
         if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
-  } else if (few) {
-    if (warp >= 4) {
-      regs_many();
-      few_items<T, D>(a, smem, s0, warp - 4, lane, err);
-    } else {
-      regs_few();
-    }
   } else if (warp == 1) {
     // ======================= MMA issuer
     regs_few();
     const bool one = elect_one();
     const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
     const int page = a.lay.page, page_blk = BLOCK / page;
-    Walk walk(a);
+    Walk walk(a, blockIdx.x);
     Groups groups;
     bool ok = true;
     auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
@@ -795,7 +767,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     regs_few();
     const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);
     const int* order = plan_of(a).order;
-    Walk walk(a);
+    Walk walk(a, blockIdx.x);
     Groups groups;
     uint32_t used = 0, par = 0;
     bool ok = true;
@@ -845,7 +817,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
     const float scale_log2 = a.scale * 1.4426950408889634f;
     const int2* own_columns = plan_of(a).own;
-    Walk walk(a);
+    Walk walk(a, blockIdx.x);
     Groups groups;
     Ring rv;
     uint32_t s_par = 0, o_par = 0;
@@ -1090,7 +1062,8 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_con
       const int e = k ? rec.z * Hkv + f % Hkv : f, place = k ? rec.w * G + h % G : row;
       const Item x_it = k ? plan.items[rec.z] : it;
       const uint32_t rows = x_it.n_tok * G;
-      const uint32_t parts = on_line(x_it, f % Hkv, G).segments(x_it.blocks, head.share) * copies_of(x_it, G);
+      const uint32_t share = x_it.flags & ITEM_FEW ? head.few_share : head.share;
+      const uint32_t parts = on_line(x_it, f % Hkv, G).segments(x_it.blocks, share) * copies_of(x_it, G);
       const int64_t row0 = plan.part[e] + static_cast<int64_t>(place);
       for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
         const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   pdl_trigger();
   __syncthreads();
   Head head{};
-  head.share = 1;
+  head.share = head.few_share = 1;
   head.n_seqs = n;
   head.n_kv_heads = Hkv;
   head.Hq = a.Hq;
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       *p.head = head;
       if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
     }
-    for (int c = threadIdx.x; c <= MAX_CTAS; c += THREADS) p.first[c] = 0;
+    for (int c = threadIdx.x; c < SHARES; c += THREADS) p.first[c] = 0;
     return;
   }
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   // Both kinds are laid out alike: rows in the order of their keys, their tokens cut into items.
   int n_items = 0, n_runs = 0, n_tok = 0;
   for (int kind = 0; kind < 2; ++kind) {
-    const int cut = kind ? few : 2 * tile;
+    const int cut = kind ? few : 2 * tile, unit = kind ? PIECE : page, block_units = kind ? 1 : page_blk;
     int nl = 0;
     // tiles: all but the prefixes that have few rows, and rows with few tokens that read no prefix.  few: those prefixes'
     // rows; rows with few tokens whose prefix tiles read; and those that read none
@@ -243,13 +243,13 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
           it.run = at;
           if (k < n) {
             const int keys_ = a.seq_lens[k];
-            p.runs[at++] = Run{k, 0, (keys_ + page - 1) / page, keys_, 0, it.n_tok, -1, 0};
+            p.runs[at++] = Run{k, 0, (keys_ + unit - 1) / unit, keys_, 0, it.n_tok, -1, 0};
           }
         }
         if (!own) continue;
         const int row = list[i];
         const int seen = max(0, a.seq_lens[row] - (in + tok - hi));  // own keys of its last token here
-        p.runs[at++] = Run{row, 0, (seen + page - 1) / page, seen, lo - c * cut, hi - c * cut, a.tok_off[row] + lo - in, 0};
+        p.runs[at++] = Run{row, 0, (seen + unit - 1) / unit, seen, lo - c * cut, hi - c * cut, a.tok_off[row] + lo - in, 0};
       }
       n_runs += static_cast<int>(total);
     }
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
           if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
           // the last token sees the run's keys, each before it one less
           for (int x = run.tok0; run.token >= 0 && x < run.tok1; ++x)
-            p.own[it.tok + x] = make_int2(off * page, off * page + max(0, run.keys - (run.tok1 - 1 - x)));
+            p.own[it.tok + x] = make_int2(off * unit, off * unit + max(0, run.keys - (run.tok1 - 1 - x)));
         }
         pages += __shfl_sync(0xffffffffu, inc, 31);
       }
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       begin1 = __reduce_min_sync(0xffffffffu, begin1);
       if (lane == 0) {
         it.pages = pages;
-        it.blocks = (pages + page_blk - 1) / page_blk;
+        it.blocks = (pages + block_units - 1) / block_units;
         it.end0 = (end0 + page_blk - 1) / page_blk;
         it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
         it.begin1 = begin1 / page_blk;
@@ -313,48 +313,42 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   }
 
   // the line
-  unsigned long long line = 0, tiles_line = 0;
-  int longest = 1;  // of a block: a share holds one at least
+  unsigned long long tiles_line = 0, few_line = 0;
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    unsigned long long length = 0, tiles = 0;
+    unsigned long long length = 0;
+    bool is_few = false;
     if (i < n_items) {
       const Item it = p.items[i];
       length = static_cast<unsigned long long>(Hkv) * length_of(it, G);
-      if (!(it.flags & ITEM_FEW)) tiles = length;
-      if (it.blocks > 0) longest = max(longest, static_cast<int>(block_length(it.flags & ITEM_FEW, two_tiles(it, G))));
+      is_few = it.flags & ITEM_FEW;
     }
-    const unsigned long long at = line + block_exclusive(length, warp_sum, total);
-    if (i < n_items) p.items[i].start = static_cast<uint32_t>(at);
-    line += total;
-    block_exclusive(tiles, warp_sum, total);
+    const unsigned long long at_tiles = tiles_line + block_exclusive(is_few ? 0ull : length, warp_sum, total);
     tiles_line += total;
+    const unsigned long long at_few = few_line + block_exclusive(is_few ? length : 0ull, warp_sum, total);
+    few_line += total;
+    if (i < n_items) p.items[i].start = static_cast<uint32_t>(is_few ? at_few : at_tiles);
   }
-  if (threadIdx.x == 0) unsorted = 1;
-  __syncthreads();
-  atomicMax(&unsorted, longest);
-  __syncthreads();
-  longest = unsorted;
-  const bool fits = line < 0x20000000ull;
-  uint32_t share = 1;
-  if (fits) {
-    // the few items begin with a CTA's share: the least share with which both kinds' CTAs are there
-    const uint32_t tiles = static_cast<uint32_t>(tiles_line), rest = static_cast<uint32_t>(line - tiles_line), ctas = n_ctas;
-    share = max(static_cast<uint32_t>(longest), static_cast<uint32_t>((line + ctas - 1) / ctas));
-    while (ctas > 1 && (tiles + share - 1) / share + (rest + share - 1) / share > ctas) share += 1 + share / 256;
-    const uint32_t shift = (tiles + share - 1) / share * share - tiles;
-    for (int i = threadIdx.x; i < n_items; i += THREADS)
-      if (p.items[i].flags & ITEM_FEW) p.items[i].start += shift;
-    line += shift;
+  // CTAs for each kind by what they take, one at least
+  const bool both = tiles_line > 0 && few_line > 0, fits = tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
+  int tile_ctas = few_line > 0 ? 0 : n_ctas;
+  if (both) {
+    const unsigned long long few_cost = few_line * FEW_PER_TILES / WORKERS;
+    tile_ctas = min(n_ctas - 1, max(1, static_cast<int>((n_ctas * tiles_line + (tiles_line + few_cost) / 2) / (tiles_line + few_cost))));
   }
+  const uint32_t few_ctas = n_ctas - tile_ctas;
+  // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up
+  uint32_t share = block_length(false, true), few_share = MIN_FEW_SHARE;
+  if (fits && tile_ctas > 0) share = max(share, static_cast<uint32_t>((tiles_line + tile_ctas - 1) / tile_ctas));
+  if (fits && few_ctas > 0) few_share = max(few_share, static_cast<uint32_t>((few_line + few_ctas * WORKERS - 1) / (few_ctas * WORKERS)));
   __syncthreads();
   const int n_flat = fits ? n_items * Hkv : 0;
   // the CTAs' segments, rows of partial results, pieces of the join's list
-  unsigned long long segments = 0, rows = 0;  // in the upper half of rows: pieces
+  unsigned long long segments = 0, tile_segments = 0, rows = 0;  // in the upper half of rows: pieces
   for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
     const int f = f0 + threadIdx.x;
     unsigned long long count = 0;
-    uint32_t segs = 0;
+    uint32_t segs = 0, few_segs = 0, entry_share = 1;
     int entry_rows = 0;
     bool right_away = false;
     Item it{};
@@ -362,7 +356,9 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     if (f < n_flat) {
       it = p.items[f / Hkv];
       on = on_line(it, f % Hkv, G);
-      segs = on.segments(it.blocks, share);
+      entry_share = it.flags & ITEM_FEW ? few_share : share;
+      segs = on.segments(it.blocks, entry_share);
+      if (it.flags & ITEM_FEW) few_segs = segs;
       right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
       if (!right_away) {
         entry_rows = it.n_tok * G;
@@ -378,13 +374,15 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     for (int r = 0; r < entry_rows; r += JOIN_ROWS) p.join[(at >> 32) + r / JOIN_ROWS] = make_int2(f, r);
     const uint32_t seg0 = static_cast<uint32_t>(segments + block_exclusive(static_cast<unsigned long long>(segs), warp_sum, total));
     segments += total;
+    block_exclusive(static_cast<unsigned long long>(segs - few_segs), warp_sum, total);
+    tile_segments += total;
     for (uint32_t i = 0; i < segs; ++i) {
-      const uint32_t c = on.cta_of(0, share) + i;
+      const uint32_t c = on.cta_of(0, entry_share) + i;
       Segment sg{};
       sg.f = f;
       sg.h = f % Hkv;
-      sg.b0 = on.block_from(c * share, it.blocks);
-      sg.b1 = on.block_from((c + 1) * share, it.blocks);
+      sg.b0 = on.block_from(c * entry_share, it.blocks);
+      sg.b1 = on.block_from((c + 1) * entry_share, it.blocks);
       sg.tok = it.tok, sg.n_tok = it.n_tok, sg.run = it.run, sg.n_runs = it.n_runs;
       sg.prefix_keys = it.prefix_keys, sg.pages = it.pages;
       sg.end0 = it.end0, sg.begin1 = it.begin1, sg.prefix_blocks = it.prefix_blocks;
@@ -393,15 +391,16 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       p.segs[seg0 + i] = sg;
     }
   }
-  // a CTA's first segment: the entry in which its share begins tells which
+  // the shares' first segments
   __syncthreads();
-  for (int c = threadIdx.x; c <= MAX_CTAS; c += THREADS) {
-    int lo = 0, hi = static_cast<int>(segments);
-    while (lo < hi) {  // the first segment of this CTA or a later one
+  for (int c = threadIdx.x; c < SHARES; c += THREADS) {
+    const bool of_few = c > tile_ctas;
+    const uint32_t mine = of_few ? c - tile_ctas - 1 : c, kind_share = of_few ? few_share : share;
+    int lo = of_few ? static_cast<int>(tile_segments) : 0, hi = static_cast<int>(of_few ? segments : tile_segments);
+    while (lo < hi) {  // the first segment of this share or a later one
       const int mid = (lo + hi) >> 1;
       const Segment& sg = p.segs[mid];
-      const Item it = p.items[sg.f / Hkv];
-      if (on_line(it, sg.h, G).cta_of(sg.b0, share) < static_cast<uint32_t>(c)) lo = mid + 1; else hi = mid;
+      if (on_line(p.items[sg.f / Hkv], sg.h, G).cta_of(sg.b0, kind_share) < mine) lo = mid + 1; else hi = mid;
     }
     p.first[c] = lo;
   }
@@ -412,7 +411,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       head.n_flat = n_flat;
       head.n_join = static_cast<int>(rows >> 32);
       head.share = share;
-      head.total = static_cast<uint32_t>(line);
+      head.few_share = few_share;
+      head.tile_ctas = tile_ctas;
     }
     *p.head = head;
     if (!fits && a.status) atomicCAS(a.status, 0, DOPR_ERR_UNSUPPORTED);

@@ -12,9 +12,12 @@
 // as far as their last token in the item sees them; a token sees its own run's keys up to itself.  A page's place in the
 // list is its place in the columns of the scores, so a token's keys are two intervals of columns.  128 columns are a block.
 //
-// An item and a kv head are a flat entry.  The flat entries lie one after another on a line, on which an entry takes a
-// length for its start and end and one for each block, and every CTA takes the blocks that begin in an equal share of the
-// line, of tiles or of few items.  What a CTA has of an entry is a segment; it leaves partial softmax results (maximum, sum, weighted values), which
+// Of few items a block is a piece of 16 columns, and a run's last piece is its last one with keys.
+//
+// An item and a kv head are a flat entry.  The flat entries of each kind lie one after another on a line, on which an entry
+// takes a length for its start and end and one for each block.  Some CTAs take the tiles, the others the few items; a CTA
+// of the former, a warp of the latter takes the blocks that begin in an equal share of its line.  What it has of an entry is
+// a segment; it leaves partial softmax results (maximum, sum, weighted values), which
 // the joining kernel adds up by row, unless they are all that its rows have: then it gives the rows' results right away.
 #pragma once
 
@@ -26,12 +29,17 @@ namespace shared_attn {
 
 constexpr int TILE = 128;   // rows of a tile
 constexpr int FEW = 16;     // rows of a few item
-constexpr int BLOCK = 128;  // columns of a block
+constexpr int BLOCK = 128;  // columns of a block of tiles
+constexpr int PIECE = 16;   // of few items
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
-// Lengths on the line, about 0.3 us each: a block of two tiles, of one, of a few item; an entry's start and end.
-__host__ __device__ constexpr uint32_t block_length(bool few, bool two) { return few ? 4 : two ? 6 : 4; }
-__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 : 10; }
+constexpr int WORKERS = 8;  // warps of a CTA that take few items
+// Lengths on the lines.  Tiles, about 0.3 us each: a block of two tiles, of one; an entry's start and end.  Few items, about
+// 1.5 us of a warp each (a CTA's eight share the SM's part of the memory's rate): a piece; an entry's start and end.
+__host__ __device__ constexpr uint32_t block_length(bool few, bool two) { return few ? 1 : two ? 6 : 4; }
+__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 10; }
+constexpr uint32_t FEW_PER_TILES = 5;  // a length of few items in those of tiles
+constexpr uint32_t MIN_FEW_SHARE = 6;
 
 struct alignas(16) Run {
   int row;    // table row
@@ -75,16 +83,19 @@ enum : uint32_t {
 };
 struct alignas(16) Head {
   int tokens, n_items, n_flat, n_join;
-  uint32_t share, total;  // of the line: a CTA's part, all of it
+  uint32_t share, few_share;  // of the lines: a CTA's part of tiles, a warp's of few items
+  int tile_ctas;              // the CTAs that take tiles
   int n_seqs, n_kv_heads, Hq, max_tokens, n_ctas, head_dim, page;  // what the plan was made for
+  int pad[2];
 };
 __host__ __device__ inline bool made_for(const Head& h, const dopr_cache_layout& lay, int Hq, int max_tokens, int n_ctas) {
   return h.n_seqs == lay.n_seqs && h.n_kv_heads == lay.n_kv_heads && h.Hq == Hq && h.max_tokens == max_tokens &&
          h.n_ctas == n_ctas && h.head_dim == lay.head_dim && h.page == lay.page;
 }
+constexpr int SHARES = MAX_CTAS * WORKERS + 2;  // at most: a CTA has one or WORKERS
 struct Plan {
   Head* head;
-  int* first;      // [MAX_CTAS + 1] a CTA's first segment
+  int* first;      // [SHARES] the shares' first segments: the tiles' CTAs' and the end, the few items' warps' and the end
   Segment* segs;   // in the CTAs' order
   int4* rec;       // [tokens] item of tiles and place in it, few item and place in it (-1: none)
   Item* items;
@@ -119,9 +130,9 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   const int64_t items = max_items(n_seqs, G, max_tokens);
   Plan p;
   p.head = static_cast<Head*>(take(sizeof(Head)));
-  p.first = static_cast<int*>(take((MAX_CTAS + 1) * 4));
+  p.first = static_cast<int*>(take(SHARES * 4));
   p.rec = static_cast<int4*>(take(16 * static_cast<int64_t>(max_tokens)));
-  p.segs = static_cast<Segment*>(take((items * n_kv_heads + MAX_CTAS) * static_cast<int64_t>(sizeof(Segment))));
+  p.segs = static_cast<Segment*>(take((items * n_kv_heads + SHARES) * static_cast<int64_t>(sizeof(Segment))));
   p.items = static_cast<Item*>(take(items * static_cast<int64_t>(sizeof(Item))));
   // a run for every row, one more wherever an item ends within a row, and the prefixes'
   p.runs = static_cast<Run*>(take(2 * (items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));

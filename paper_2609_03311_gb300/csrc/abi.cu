@@ -1030,6 +1030,20 @@ bool make_gemm_operand_b(GemmOperandB* b, const void* base, uint64_t k, uint64_t
 // The Q columns of a packed QKV buffer [rows][cols] as a 3-D tensor: 128 elements of a head
 // (innermost), rows, heads (256 bytes apart); the box takes 64 elements of box_heads heads over
 // box_rows rows, stored head after head (fp16, 128-byte swizzle).
+bool make_tmap_rows_of_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t heads, uint64_t tokens, int64_t head_stride,
+                             int64_t token_stride, uint32_t box_heads, uint32_t box_tokens, bool half) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[3] = {cols, heads, tokens};
+  // a stride that is never taken, of a single head or token, is any valid one
+  cuuint64_t strides[2] = {2 * (heads > 1 ? (cuuint64_t)head_stride : cols), 2 * (tokens > 1 ? (cuuint64_t)token_stride : cols)};
+  cuuint32_t box[3] = {64, box_heads, box_tokens};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+            box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_tmap_q_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint32_t box_rows,
                        uint32_t box_heads) {
   auto fn = encode_fn();

@@ -256,6 +256,10 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, unsigned block, si
 // 2-D map over 16-bit elements (fp16 when `half` is set, else bf16).
 bool make_tmap_16b_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t row_stride_bytes,
                       uint32_t box_cols, uint32_t box_rows, bool swizzle128, bool half);
+// 3-D map over 16-bit elements of [tokens][heads][cols] with strides in elements: boxes of 64 columns x box_heads x
+// box_tokens, 128-byte swizzle.
+bool make_tmap_rows_of_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t heads, uint64_t tokens, int64_t head_stride,
+                             int64_t token_stride, uint32_t box_heads, uint32_t box_tokens, bool half);
 bool make_tmap_q_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint32_t box_rows,
                        uint32_t box_heads);
 
@@ -484,6 +488,7 @@ struct SharedAttnArgs {
   const void* plan;
   const void* q;
   int64_t q_tok, q_head;
+  bool q_boxes;  // set by the launcher: eight tokens of Q that follow one another come by TMA
   const void *k_pool, *v_pool;
   const int32_t* tables;
   float scale;

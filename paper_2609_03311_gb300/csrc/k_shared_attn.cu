@@ -11,7 +11,8 @@
 //   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
 //     warp 0, 2  copy K and V blocks into two rings, page by page (TMA; a page's rows of a kv head lie together)
 //     warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
-//     warp 3     gathers the rows of Q (they lie anywhere) with 16-byte asynchronous copies
+//     warp 3     brings the rows of Q: eight tokens that follow one another by TMA (the rows of a token and kv head are the
+//                heads of a box), others with 16-byte copies
 //     warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more than
 //                2^8 (P stays within the type's range until then)
 //   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
@@ -111,6 +112,9 @@ constexpr int REGS_FEW = 152, REGS_MANY = 176;
 static_assert(128 * REGS_FEW + 256 * REGS_MANY <= 384 * 168, "more registers than the launch has are waited for without end");
 __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW)); }
 __device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY)); }
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void fence_proxy_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // D (16 x 8, 32-bit) += A (16 x 16) B (16 x 8) of T by a warp.
@@ -164,6 +168,12 @@ __device__ __forceinline__ bool last_block(const Segment& s, uint32_t b, int w) 
   if (!(s.flags & SEG_TWO)) return b + 2 >= s.b1;
   if (w == 0) return b + 1 == min(s.b1, s.end0);
   return b + 1 == (s.b1 > s.begin1 ? s.b1 : min(s.b1, s.prefix_blocks));
+}
+// The first block of the segment that is some group's last.
+__device__ __forceinline__ uint32_t first_last(const Segment& s) {
+  if (!(s.flags & SEG_TWO)) return s.b1 < 2 ? 0 : s.b1 - 2;
+  const uint32_t last0 = min(s.b1, s.end0), last1 = s.b1 > s.begin1 ? s.b1 : min(s.b1, s.prefix_blocks);
+  return min(last0, last1) - 1;  // (of a group that takes none: at most the other's)
 }
 // A lane's page of each block and the run it lies in.
 struct PageCursor {
@@ -470,7 +480,7 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint32_t s0, 
 
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_shared_attn(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+    k_shared_attn(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ SharedAttnArgs a) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -487,6 +497,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     gave_up = 0;
     for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
     fence_mbar_init();
+    tma_prefetch_desc(&tm_q);
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
@@ -700,8 +711,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         commit_pv();
       }
       // whole blocks of the prefix, but for each group's first and last, which the general steps take
-      const uint32_t whole = min(s.b1, static_cast<uint32_t>(s.prefix_keys) / BLOCK), margin = s.flags & SEG_TWO ? 1 : 2;
-      if (n.valid && b == s.b0 + margin && b + margin < whole && (!(s.flags & SEG_TWO) || n.w == 0)) {
+      const uint32_t margin = s.flags & SEG_TWO ? 1 : 2;
+      const uint32_t hot = min(static_cast<uint32_t>(s.prefix_keys) / BLOCK, first_last(s));
+      if (n.valid && b == s.b0 + margin && b < hot && (!(s.flags & SEG_TWO) || n.w == 0)) {
         Pending x = oldest ? pend1 : pend0, y = oldest ? pend0 : pend1;  // of two tiles: the same block
         bool k_there = n.there;
         if (!(s.flags & SEG_TWO)) groups.turn ^= 1u;  // back to before the block
@@ -721,7 +733,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             oldest ^= 1u;
             groups.turn ^= 1u;
           }
-          if (b + 1 + margin >= whole) break;
+          if (b + 1 >= hot) break;
           ++b;
           rk.next(L::K_STAGES);
           rv.next(L::V_STAGES);
@@ -765,22 +777,36 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few();
-    const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);
+    const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);  // where the rows of other tokens lie
     const int* order = plan_of(a).order;
     Walk walk(a, blockIdx.x);
     Groups groups;
-    uint32_t used = 0, par = 0;
+    uint32_t used = 0, par = 0, filled = 0;  // a bit a group
     bool ok = true;
     const T* q = static_cast<const T*>(a.q);
     while (ok && walk.next(s)) {
       const uint32_t takes = groups.any(s);
       for (int w = 0; w < 2 && ok; ++w) {
         if (!(takes >> w & 1u)) continue;
-        const int t0 = s.flags & SEG_TWO ? w * TT : 0, rows = min(TT, s.n_tok - t0) * G;
+        const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0), rows = n * G;
+        // tokens 8 i .. 8 i + 7 of the tile, a lane an i: whether they follow one another
+        const int* tok = order + s.tok + t0;
+        int first = 0;
+        bool run = a.q_boxes && 8 * lane + 8 <= n;
+        if (run) {
+          first = tok[8 * lane];
+#pragma unroll
+          for (int i = 1; i < 8; ++i) run = run && tok[8 * lane + i] == first + i;
+        }
+        const uint32_t runs = __ballot_sync(0xffffffffu, run);
         __syncwarp();
-        for (int r = lane; r < rows; r += 32)
-          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(order[s.tok + t0 + r / G]) * a.q_tok +
-                                                  static_cast<int64_t>(s.h * G + r % G) * a.q_head);
+        const bool others = __popc(runs) * 8 < n;
+        for (int r = lane; others && r < rows; r += 32) {
+          const int i = r / G;
+          row[r] = runs >> (i / 8) & 1u ? nullptr
+                                        : reinterpret_cast<const uint4*>(q + static_cast<int64_t>(tok[i]) * a.q_tok +
+                                                                         static_cast<int64_t>(s.h * G + r - i * G) * a.q_head);
+        }
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
@@ -788,27 +814,43 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (used >> w & 1u) par ^= 1u << w;
         used |= 1u << w;
-        // a lane a 16-byte piece of the row, 32 / CHUNKS rows at once
-        constexpr int CHUNKS = D / 8, STEP = 32 / CHUNKS;
-        const int c = lane % CHUNKS;
-        const uint32_t dst = s0 + L::OFF_Q + w * L::TILE_BYTES + (c >> 3) * HALF_BYTES;
-        for (int r0 = lane / CHUNKS; r0 < rows; r0 += 8 * STEP) {
-          const uint4* src[8];  // eight addresses before the first copy: a copy is not waited for, an address is
-#pragma unroll
-          for (int i = 0; i < 8; ++i) src[i] = r0 + i * STEP < rows ? row[r0 + i * STEP] : nullptr;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = r0 + i * STEP;
-            if (r < rows) cp_async16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), src[i] + c, true);
-          }
-        }
-        cp_async_commit();
-        cp_async_wait_all();
-        fence_proxy_async_shared();
+        const uint32_t dst = s0 + L::OFF_Q + w * L::TILE_BYTES, bytes = __popc(runs) * 8 * G * 128 * L::HALVES;
+        if (lane == 0 && bytes > 0) mbar_expect_tx(bar(L::Q_FULL + w), bytes);
         __syncwarp();
+        if (run)
+#pragma unroll
+          for (int h = 0; h < L::HALVES; ++h)
+            tma_load_3d(dst + h * HALF_BYTES + lane * 8 * G * 128, &tm_q, bar(L::Q_FULL + w), 64 * h, s.h * G, first);
+        __syncwarp();
+        if (others) {
+          // a lane a 16-byte piece of the row, 32 / CHUNKS rows at once
+          constexpr int CHUNKS = D / 8, STEP = 32 / CHUNKS;
+          const int c = lane % CHUNKS;
+          for (int r0 = lane / CHUNKS; r0 < rows; r0 += 8 * STEP) {
+            const uint4* src[8];  // eight addresses before the first copy: a copy is not waited for, an address is
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = r0 + i * STEP;
+              src[i] = r < rows ? row[r] : nullptr;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = r0 + i * STEP;
+              if (src[i]) cp_async16(dst + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src[i] + c, true);
+            }
+          }
+          cp_async_commit();
+          cp_async_wait_all();
+          fence_proxy_async_shared();
+          __syncwarp();
+        }
         if (lane == 0) mbar_arrive(bar(L::Q_FULL + w));
+        filled ^= 1u << w;
       }
     }
+    if (ld_volatile(err))  // copies in flight land before the CTA ends
+      for (int w = 0; w < 2; ++w)
+        if (used >> w & 1u) mbar_wait_warp(bar(L::Q_FULL + w), (filled >> w & 1u) ^ 1u, err, 100000000ull);
   } else {
     // ======================= softmax: thread r of group w has row r of its tile
     regs_many();
@@ -965,7 +1007,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int t = valid ? plan_of(a).order[e.tok + w * TT + r / G] : 0, h = e.h * G + r % G;
         const float inv = inverse(l);
         T* dst = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
-        bool nan = false;
+        float all = 0.f;  // the values' sum: a NaN where one of them is (or they are infinite both ways: no harm)
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t v[32] = {};
@@ -976,7 +1018,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const float x = l == 0.f ? 0.f : __uint_as_float(v[i]) * inv;
-            nan |= x != x;
+            all += x;
             v[i] = __float_as_uint(x);
           }
           if (valid) {
@@ -991,6 +1033,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
           }
         }
+        const bool nan = all != all;
         if (valid && a.lse) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
         // scores in order, values not: perhaps a value that the row does not see
         uint32_t odd = __ballot_sync(0xffffffffu, valid && nan && l == l);
@@ -1121,15 +1164,21 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_con
 template <typename T, int D>
 cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   const int n_ctas = num_sms < MAX_CTAS ? num_sms : MAX_CTAS;
-  CUtensorMap tm_k, tm_v;
+  CUtensorMap tm_q, tm_k, tm_v;
+  const int G = a.Hq / a.lay.n_kv_heads;
   const uint64_t rows = static_cast<uint64_t>(a.lay.n_blocks) * a.lay.n_kv_heads * a.lay.page;
   const bool half = std::is_same_v<T, __half>;
   if (!make_tmap_16b_2d(&tm_k, a.k_pool, D, rows, D * 2, 64, a.lay.page, true, half) ||
       !make_tmap_16b_2d(&tm_v, a.v_pool, D, rows, D * 2, 64, a.lay.page, true, half))
     return cudaErrorInvalidValue;
+  // Q of eight tokens at once, where a tile holds as many; views that a tensor map does not take (one row for all tokens)
+  // are gathered
+  SharedAttnArgs args = a;
+  args.q_boxes = tokens_a_tile(G) >= 8 && make_tmap_rows_of_heads(&tm_q, a.q, D, a.Hq, a.max_tokens, a.q_head, a.q_tok, G, 8, half);
+  if (!args.q_boxes) tm_q = tm_k;
   cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_k, tm_v, a);
+  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q, tm_k, tm_v, args);
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +

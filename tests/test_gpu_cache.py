@@ -526,6 +526,13 @@ def test_attention_scale_and_strided_views():
     assert torch.equal(out, want[0])
 
 
+def test_attention_of_one_query_for_all_tokens():
+    # a broadcast view: the same row for every token
+    b = Batch(8, 2, 64, HF, 32, [400], [(0, 20, 7), (0, 9, 9)], seed=4)
+    b.q = b.q[:1].expand(b.T, -1, -1)
+    b.check(b.run())
+
+
 def test_attention_plan_refuses_bad_device_values_and_attention_then_writes_nothing():
     b = Batch(4, 2, 64, HF, 16, [20], [(0, 5, 2), (0, 6, 1)], seed=1)
     for off, lens, prefix in (([0, 0, 2, 1], b.lens, b.prefix), ([1, 1, 2, 3], b.lens, b.prefix),

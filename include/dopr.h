@@ -558,7 +558,7 @@ DOPR_API int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout *layou
  *            left as they were.
  *   lse      [max_tokens][n_q_heads] float or NULL: log of the sum of exponentials
  *            (natural).  A row that sees no key gives zeros and -infinity.
- *   workspace dopr_shared_attention_workspace(...) bytes, 16-byte aligned.
+ *   workspace dopr_shared_attention_workspace(...) bytes, 32-byte aligned.
  * Keys and values past a row's end are never used, whatever the pages hold there.
  * Products take dtype operands with 32-bit sums; probabilities are rounded to
  * dtype, statistics and sums are 32-bit.  A row's bits depend on the plan.

@@ -345,8 +345,8 @@ dopr_status dopr_shared_attention(const dopr_cache_layout* layout, const void* p
   if (max_tokens == 0) return DOPR_OK;  // views of no rows have no data
   if (!plan || !k_pool || !v_pool || !block_tables || !workspace)
     return fail(DOPR_ERR_INVALID_ARG, "plan, k_pool, v_pool, block_tables or workspace is NULL");
-  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(workspace, 16))
-    return fail(DOPR_ERR_INVALID_ARG, "plan, pools and workspace must be 16-byte aligned");
+  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(workspace, 32))
+    return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned, the workspace 32-byte");
   if (!(scale > 0.f) || !isfinite(scale)) return fail(DOPR_ERR_INVALID_ARG, "scale must be positive");
   STATUS_TRY(check_view(q, "q", layout->head_dim, 2, true, 0));
   STATUS_TRY(check_view(out, "out", layout->head_dim, 2, true, q->n_heads));

@@ -112,6 +112,11 @@ constexpr int REGS_FEW = 152, REGS_MANY = 176;
 static_assert(128 * REGS_FEW + 256 * REGS_MANY <= 384 * 168, "more registers than the launch has are waited for without end");
 __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW)); }
 __device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY)); }
+__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+               "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
@@ -142,6 +147,7 @@ struct Walk {
   __device__ __forceinline__ bool next(Segment& s) {
     if (at >= end) return false;
     s = segs[at++];
+    if (at < end) asm volatile("prefetch.global.L1 [%0];" ::"l"(segs + at));
     return true;
   }
 };
@@ -601,8 +607,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     } pend0{}, pend1{};
     uint32_t oldest = 0;
     int n_pend = 0;
-    // what the oldest frees: committed with the S behind it
-    int freed[2] = {-1, -1}, ended = 0;  // V stages; a bit a group whose O is whole
+    int freed[2] = {-1, -1};  // V stages that are free after the products issued: committed with the S behind them
     auto issue_pv = [&] {
       const uint32_t w = oldest;
       const Pending x = w ? pend1 : pend0;
@@ -614,20 +619,21 @@ __global__ void __launch_bounds__(THREADS, 1)
       tc_fence_after();
       const uint64_t vd = v_desc0 + x.stage * (L::TILE_BYTES / 16);
       const uint32_t o = tmem + O_COL + 128 * w, pc = tmem + P_COL + 128 * w;
-      if (one)
-        for (int k = 0; k < x.cols / 16; ++k) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & FIRST));
+      if (one) {
+        // (a loop of unknown length takes 115 clocks a product, one spelled out 26)
+#pragma unroll
+        for (int k = 0; k < BLOCK / 16; ++k)
+          if (16 * k < x.cols) umma_f16_ts(o, pc + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || !(x.flags & FIRST));
+        if (x.flags & LAST) umma_commit(bar(L::O_FULL + w));
+      }
       if (x.flags & FREE_V) freed[freed[0] >= 0] = x.stage;
-      if (x.flags & LAST) ended |= 1 << w;
     };
     auto commit_pv = [&] {
       if (one) {
-        if (ended & 1) umma_commit(bar(L::O_FULL));
-        if (ended & 2) umma_commit(bar(L::O_FULL + 1));
         if (freed[0] >= 0) umma_commit(bar(L::V_EMPTY + freed[0]));
         if (freed[1] >= 0) umma_commit(bar(L::V_EMPTY + freed[1]));
       }
       freed[0] = freed[1] = -1;
-      ended = 0;
     };
     // the next S: a block and a group that takes it
     Ring rk, rv;
@@ -859,6 +865,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
     const float scale_log2 = a.scale * 1.4426950408889634f;
     const int2* own_columns = plan_of(a).own;
+    const int* order = plan_of(a).order;
     Walk walk(a, blockIdx.x);
     Groups groups;
     Ring rv;
@@ -890,8 +897,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
       // the row sees columns [0, prefix) and [own0, own1)
       const int prefix = valid ? s.prefix_keys : 0;
-      int own0 = 0, own1 = 0;
+      int own0 = 0, own1 = 0, token = 0;
       if (valid) {
+        token = order[s.tok + t0 + r / G];
         const int2 own = own_columns[s.tok + t0 + r / G];
         own0 = own.x, own1 = own.y;
       }
@@ -1004,9 +1012,10 @@ __global__ void __launch_bounds__(THREADS, 1)
       const Segment& e = walk.segs[walk.at - 1];
       if (e.flags & SEG_WHOLE) {
         // ---- the whole entry: the rows' results
-        const int t = valid ? plan_of(a).order[e.tok + w * TT + r / G] : 0, h = e.h * G + r % G;
+        const int t = token, h = e.h * G + r % G;
         const float inv = inverse(l);
         T* dst = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
+        const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | a.o_tok * 2 | a.o_head * 2) & 31) == 0;  // a store a sector
         float all = 0.f;  // the values' sum: a NaN where one of them is (or they are infinite both ways: no harm)
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
@@ -1023,13 +1032,16 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
           if (valid) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8) {
-              uint4 x;
-              x.x = pack2<T>(__uint_as_float(v[i]), __uint_as_float(v[i + 1]));
-              x.y = pack2<T>(__uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
-              x.z = pack2<T>(__uint_as_float(v[i + 4]), __uint_as_float(v[i + 5]));
-              x.w = pack2<T>(__uint_as_float(v[i + 6]), __uint_as_float(v[i + 7]));
-              *reinterpret_cast<uint4*>(dst + c + i) = x;
+            for (int i = 0; i < 32; i += 16) {
+              uint32_t x[8];
+#pragma unroll
+              for (int k = 0; k < 8; ++k) x[k] = pack2<T>(__uint_as_float(v[i + 2 * k]), __uint_as_float(v[i + 2 * k + 1]));
+              if (wide) {
+                st_global32(dst + c + i, x);
+              } else {
+                *reinterpret_cast<uint4*>(dst + c + i) = uint4{x[0], x[1], x[2], x[3]};
+                *reinterpret_cast<uint4*>(dst + c + i + 8) = uint4{x[4], x[5], x[6], x[7]};
+              }
             }
           }
         }
@@ -1058,7 +1070,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           tmem_ld_wait_for(v);
           if (valid && l != 0.f) {  // (a NaN is not)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4*>(dst + c + 4 * i) = uint4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+            for (int i = 0; i < 32; i += 8) {
+              const uint32_t x[8] = {v[i], v[i + 1], v[i + 2], v[i + 3], v[i + 4], v[i + 5], v[i + 6], v[i + 7]};
+              st_global32(dst + c + i, x);
+            }
           }
         }
       }

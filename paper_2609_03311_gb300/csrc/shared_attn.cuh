@@ -151,8 +151,8 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
 __host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int G, int max_tokens, int n_ctas) {
   const int64_t all = static_cast<int64_t>(max_tokens) * G, n = n_seqs;
   const int64_t tiles = 2 * all < 4 * TILE * n ? 2 * all : 4 * TILE * n, few = all < FEW * n ? all : FEW * n;
-  // even, so that the values behind the maxima and sums begin on 16 bytes
-  return (n_kv_heads * (tiles + few) + 1) / 2 * 2 + 4 * TILE * static_cast<int64_t>(n_ctas);
+  // so that the values behind the maxima and sums begin on 32 bytes where the workspace does
+  return (n_kv_heads * (tiles + few) + 3) / 4 * 4 + 4 * TILE * static_cast<int64_t>(n_ctas);
 }
 
 __host__ __device__ inline bool two_tiles(const Item& it, int G) { return !(it.flags & ITEM_FEW) && it.n_tok > tokens_a_tile(G); }

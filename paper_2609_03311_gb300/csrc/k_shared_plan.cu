@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   }
   const uint32_t few_ctas = n_ctas - tile_ctas;
   // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up
-  uint32_t share = block_length(false, true), few_share = MIN_FEW_SHARE;
+  uint32_t share = block_length(false), few_share = MIN_FEW_SHARE;
   if (fits && tile_ctas > 0) share = max(share, static_cast<uint32_t>((tiles_line + tile_ctas - 1) / tile_ctas));
   if (fits && few_ctas > 0) few_share = max(few_share, static_cast<uint32_t>((few_line + few_ctas * WORKERS - 1) / (few_ctas * WORKERS)));
   __syncthreads();

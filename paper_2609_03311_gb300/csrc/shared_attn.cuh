@@ -34,11 +34,13 @@ constexpr int PIECE = 16;   // of few items
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
 constexpr int WORKERS = 8;  // warps of a CTA that take few items
-// Lengths on the lines.  Tiles, about 0.3 us each: a block of two tiles, of one; an entry's start and end.  Few items, about
-// 1.5 us of a warp each (a CTA's eight share the SM's part of the memory's rate): a piece; an entry's start and end.
-__host__ __device__ constexpr uint32_t block_length(bool few, bool two) { return few ? 1 : two ? 6 : 4; }
-__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 10; }
-constexpr uint32_t FEW_PER_TILES = 5;  // a length of few items in those of tiles
+// Lengths on the lines.  Tiles, about 0.3 us each: a block; an entry's start and end.  Few items, about 1.5 us of a warp each
+// (a CTA's eight share the SM's part of the memory's rate): a piece; an entry's start and end.  Measured over ragged documents
+// / queries of 16 documents: an entry of tiles at 10 and a block of one tile at 4, 69 / 192 us; 22 and 6, 61 / 180; a length of
+// few items at 3, 4, 5 of tiles, 59.2 / 58.8 / 61.6 us for the former.
+__host__ __device__ constexpr uint32_t block_length(bool few) { return few ? 1 : 6; }
+__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 26; }
+constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
 constexpr uint32_t MIN_FEW_SHARE = 6;
 
 struct alignas(16) Run {
@@ -172,10 +174,10 @@ struct OnLine {
   }
 };
 __host__ __device__ inline uint32_t length_of(const Item& it, int G) {
-  return it.blocks > 0 ? entry_length(it.flags & ITEM_FEW) + it.blocks * block_length(it.flags & ITEM_FEW, two_tiles(it, G)) : 0;
+  return it.blocks > 0 ? entry_length(it.flags & ITEM_FEW) + it.blocks * block_length(it.flags & ITEM_FEW) : 0;
 }
 __host__ __device__ inline OnLine on_line(const Item& it, int h, int G) {
-  return OnLine{it.start + h * length_of(it, G) + entry_length(it.flags & ITEM_FEW), block_length(it.flags & ITEM_FEW, two_tiles(it, G))};
+  return OnLine{it.start + h * length_of(it, G) + entry_length(it.flags & ITEM_FEW), block_length(it.flags & ITEM_FEW)};
 }
 
 }  // namespace shared_attn

@@ -3,7 +3,9 @@
 //
 // One CTA: everything is sums over the step's rows, and the rows of a prefix brought together.  Rows usually come in
 // prefix order; those that do not are sorted (a bitonic network over (prefix, row) in shared memory; rows of a
-// prefix keep their order).  Bound by latency; made once a step and used by every layer.
+// prefix keep their order).  Made once a step and used by every layer.  Bound by the latency of some twenty short phases:
+// lists, items and runs stay in shared memory where they fit, a sum over the block takes one barrier, and what rows, items
+// and entries hold several of (items, runs, tokens, segments) is spread over a warp's lanes.
 #include <limits.h>
 
 #include "shared_attn.cuh"
@@ -12,55 +14,133 @@ namespace dopr {
 namespace {
 using namespace shared_attn;
 
-constexpr int THREADS = 1024;
+constexpr int THREADS = 1024, WARPS = THREADS / 32;
 constexpr int ROW_BITS = 14;
+constexpr int MAX_SHARED = 200 * 1024;
 static_assert(CACHE_MAX_SEQS == 1 << ROW_BITS, "a sort key holds two row numbers");
+static_assert(CACHE_MAX_SEQS * 4 <= MAX_SHARED, "the sort's keys");
+enum { LISTS_SHARED = 1, ITEMS_SHARED = 2, RUNS_SHARED = 4 };
 
-// Exclusive sums over the block's threads in order; the block's total through `total`.
-template <typename T>
-__device__ T block_exclusive(T v, T* warp_sum, T& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  T inc = v;
+__device__ int warp_inclusive(int v) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const T u = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += u;
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += u;
   }
-  __syncthreads();  // the last use of warp_sum is over
-  if (lane == 31) warp_sum[warp] = inc;
-  __syncthreads();
-  if (warp == 0) {
-    T w = warp_sum[lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const T u = __shfl_up_sync(0xffffffffu, w, o);
-      if (lane >= o) w += u;
-    }
-    warp_sum[lane] = w;
-  }
-  __syncthreads();
-  total = warp_sum[31];
-  return (warp > 0 ? warp_sum[warp - 1] : T(0)) + inc - v;
+  return v;
 }
 
-__global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n_ctas) {
-  extern __shared__ uint32_t keys[];  // a power of two >= n_seqs
-  __shared__ unsigned long long warp_sum[32];
+// Exclusive sums of N values over the block's threads in order; the block's totals through `total`.  One barrier: the warps'
+// sums lie in one of two places by turns, and who writes one has passed the barrier behind its last readers.
+template <int N>
+struct BlockSums {
+  int (*sums)[WARPS];  // [2 * N] in shared memory
+  int turn = 0;
+  __device__ void operator()(int (&v)[N], int (&total)[N]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int inc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      inc[i] = warp_inclusive(v[i]);
+      if (lane == 31) sums[turn * N + i][warp] = inc[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int w = warp_inclusive(sums[turn * N + i][lane]);
+      const int before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
+      total[i] = __shfl_sync(0xffffffffu, w, 31);
+      v[i] = (warp > 0 ? before : 0) + inc[i] - v[i];
+    }
+    turn ^= 1;
+  }
+};
+
+// f(whether there is one, lane, i) for i below each lane's count, 32 at a time over the warp's lanes.
+template <typename F>
+__device__ void spread(int count, F f) {
+  const int inc = warp_inclusive(count), total = __shfl_sync(0xffffffffu, inc, 31);
+  for (int s = threadIdx.x & 31; s < (total + 31) / 32 * 32; s += 32) {
+    int src = 0;  // lanes whose counts end at or before s
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      if (__shfl_sync(0xffffffffu, inc, src + o - 1) <= s) src += o;
+    f(s < total, src, s - __shfl_sync(0xffffffffu, inc - count, src));
+  }
+}
+__device__ __forceinline__ int of_lane(int v, int src) { return __shfl_sync(0xffffffffu, v, src); }
+
+// Ascending; m, a power of two, 32 at least.  Steps within 32 keys by shuffles; the warps that have keys meet for the others.
+__device__ void sort_keys(uint32_t* keys, int m) {
+  const int threads = min(m, THREADS), tid = threadIdx.x;
+  if (tid >= threads) return;
+  for (int k = 2; k <= m; k <<= 1) {
+    int j = k >> 1;
+    for (; j >= 32; j >>= 1) {
+      for (int i = tid; i < m; i += threads) {
+        const int o = i ^ j;
+        if (o > i) {
+          const uint32_t x = keys[i], y = keys[o];
+          if ((x > y) == ((i & k) == 0)) keys[i] = y, keys[o] = x;
+        }
+      }
+      asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+    }
+    for (int i = tid; i < m; i += threads) {
+      uint32_t x = keys[i];
+      for (int l = j; l > 0; l >>= 1) {
+        const uint32_t y = __shfl_xor_sync(0xffffffffu, x, l);
+        x = ((i & l) == 0) == ((i & k) == 0) ? min(x, y) : max(x, y);
+      }
+      keys[i] = x;
+    }
+    if (k >= 32) asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
+  }
+}
+
+// Runs that a row has in the items before the c-th of those with tokens of it: one each if it has its own, and the prefix's in
+// each that begins with it (all but the first, and that too where `first` says so).
+__device__ __forceinline__ int run_before(int c, bool first, bool own, bool prefix) {
+  return (own ? c : 0) + (prefix && c > 0 ? c - !first : 0);
+}
+
+__global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n_ctas, int n_keys, int in_shared) {
+  extern __shared__ __align__(16) uint32_t keys[];  // a power of two >= n_seqs, then what in_shared says
+  __shared__ int sums_memory[2 * 8][WARPS];
+  __shared__ int first_of[SHARES];
   __shared__ int bad, unsorted;
+  __shared__ unsigned long long lines[2][WARPS];
   const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page, page_blk = BLOCK / page;
   const int tile = tokens_a_tile(G), few = tokens_a_few(G);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * page;
   const Plan p = plan_view(a.plan, n, Hkv, G, a.max_tokens);
-  int* sorted = p.scratch;          // rows with tokens, by group: their prefix, n where there are no prefix keys
-  int* group_of = sorted + n;       // of a sorted entry
-  int* group_tok = group_of + n;    // of a group: its tokens
-  int* list = group_tok + n + 1;    // the rows of a kind of items, by key
-  int* key = list + n;              // of a listed row: its prefix; n and n + 1 where the items hold no prefix keys
-  int* place = key + n;             // of a listed row: tokens of those before it
-  int* first_tok = place + n + 1;   // of a key: tokens before its first
-  int* first_item = first_tok + n + 2;
+  uint8_t* at_shared = reinterpret_cast<uint8_t*>(keys + n_keys);
+  auto shared = [&](int what, auto* global, int64_t count) {
+    if (!(in_shared & what)) return global;
+    auto* q = reinterpret_cast<decltype(global)>(at_shared);
+    at_shared += (count * static_cast<int64_t>(sizeof(*global)) + 15) / 16 * 16;
+    return q;
+  };
+  int* sorted = shared(LISTS_SHARED, p.scratch, plan_scratch_ints(n));  // rows with tokens, by group: their prefix, n where there are no prefix keys
+  Item* items = shared(ITEMS_SHARED, p.items, max_items(n, G, a.max_tokens));
+  Run* runs = shared(RUNS_SHARED, p.runs, max_runs(n, G, a.max_tokens));
+  int* group_of = sorted + n;        // of a sorted entry
+  int* group_tok = group_of + n;     // of a group: its tokens
+  // rows listed for tiles, then for few items, by key: the prefix, or n where the items hold no prefix keys; of few items
+  // n + 1 more, and one key more (own keys beside tiles, then without a prefix)
+  int* list = group_tok + n + 1;
+  int* key = list + 2 * n;
+  int* place = key + 2 * n;            // tokens of those before it
+  int* row_run = place + 2 * n + 1;    // its first run
+  int* first_tok = row_run + 2 * n;    // of a key: tokens before its first
+  int* first_item = first_tok + 2 * n + 3;
   if (threadIdx.x == 0) bad = 0, unsorted = 0;
+  for (int c = threadIdx.x; c < SHARES; c += THREADS) first_of[c] = INT_MAX;
+  BlockSums<1> sum1{sums_memory};
+  BlockSums<2> sum2{sums_memory};
+  BlockSums<4> sum4{sums_memory};
+  BlockSums<8> sum8{sums_memory};
   pdl_wait();
   pdl_trigger();
   __syncthreads();
@@ -76,24 +156,24 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   auto tokens_of = [&](int i) { return a.tok_off[i + 1] - a.tok_off[i]; };
 
   // checks, and the rows with tokens
-  unsigned long long total;
-  int ns = 0;
+  int ns = 0, n_sorted_tok = 0;
   for (int i0 = 0; i0 < n; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    bool has = false;
-    int g = n;
+    int v[2] = {0, 0}, total[2], g = n;
     if (i < n) {
       const int t0 = a.tok_off[i], t1 = a.tok_off[i + 1], pre = a.prefix ? a.prefix[i] : -1, len = a.seq_lens[i];
-      if ((i == 0 && t0 != 0) || t1 < t0 || t1 > a.max_tokens || len < 0 || len > cap || pre < -1 || pre >= n || pre == i ||
+      if ((i == 0 && t0 != 0) || t0 < 0 || t1 < t0 || t1 > a.max_tokens || len < 0 || len > cap || pre < -1 || pre >= n || pre == i ||
           (pre >= 0 && a.prefix[pre] != -1))
         bad = 1;
       else
-        has = t1 > t0;
-      if (has && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
+        v[0] = t1 > t0, v[1] = t1 - t0;
+      if (v[0] && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
     }
-    const int at = ns + static_cast<int>(block_exclusive(static_cast<unsigned long long>(has), warp_sum, total));
-    if (has) sorted[at] = i, group_of[at] = g;
-    ns += static_cast<int>(total);
+    const bool has = v[0];
+    sum2(v, total);
+    if (has) sorted[ns + v[0]] = i, group_of[ns + v[0]] = g, place[ns + v[0]] = n_sorted_tok + v[1];
+    ns += total[0];
+    n_sorted_tok += total[1];
   }
   __syncthreads();
   if (bad) {
@@ -104,231 +184,277 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     for (int c = threadIdx.x; c < SHARES; c += THREADS) p.first[c] = 0;
     return;
   }
+  for (int t = threadIdx.x; t < n_sorted_tok; t += THREADS) p.rec[t] = make_int4(-1, 0, -1, 0);
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
     if (group_of[i] < group_of[i - 1]) unsorted = 1;
   __syncthreads();
   if (unsorted) {
-    int m = 2;
+    int m = 32;
     while (m < ns) m <<= 1;
     for (int i = threadIdx.x; i < m; i += THREADS)
       keys[i] = i < ns ? static_cast<uint32_t>(group_of[i]) << ROW_BITS | sorted[i] : 0xffffffffu;
-    for (int k = 2; k <= m; k <<= 1)
-      for (int j = k >> 1; j > 0; j >>= 1) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < m; i += THREADS) {
-          const int o = i ^ j;
-          if (o > i) {
-            const uint32_t x = keys[i], y = keys[o];
-            if ((x > y) == ((i & k) == 0)) keys[i] = y, keys[o] = x;
-          }
-        }
-      }
     __syncthreads();
-    for (int i = threadIdx.x; i < ns; i += THREADS) sorted[i] = keys[i] & ((1 << ROW_BITS) - 1), group_of[i] = keys[i] >> ROW_BITS;
+    sort_keys(keys, m);
     __syncthreads();
-  }
-  // a group's tokens: its rows stand together
-  {
     int carry = 0;
     for (int i0 = 0; i0 < ns; i0 += THREADS) {
       const int i = i0 + threadIdx.x;
-      const int tok = i < ns ? tokens_of(sorted[i]) : 0;
-      const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
+      int v[1] = {0}, total[1];
       if (i < ns) {
-        place[i] = at;
-        if (i == 0 || group_of[i - 1] != group_of[i]) first_tok[group_of[i]] = at;
+        sorted[i] = keys[i] & ((1 << ROW_BITS) - 1);
+        group_of[i] = keys[i] >> ROW_BITS;
+        v[0] = tokens_of(sorted[i]);
       }
-      carry += static_cast<int>(total);
+      sum1(v, total);
+      if (i < ns) place[i] = carry + v[0];
+      carry += total[0];
     }
-    if (threadIdx.x == 0) place[ns] = carry;
-    __syncthreads();
-    for (int i = threadIdx.x; i < ns; i += THREADS)
-      if (i + 1 == ns || group_of[i + 1] != group_of[i]) group_tok[group_of[i]] = place[i + 1] - first_tok[group_of[i]];
-    __syncthreads();
   }
+  if (threadIdx.x == 0) place[ns] = n_sorted_tok;
+  __syncthreads();
+  // a group's tokens: its rows stand together
+  for (int i = threadIdx.x; i < ns; i += THREADS)
+    if (i == 0 || group_of[i - 1] != group_of[i]) first_tok[group_of[i]] = place[i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < ns; i += THREADS)
+    if (i + 1 == ns || group_of[i + 1] != group_of[i]) group_tok[group_of[i]] = place[i + 1] - first_tok[group_of[i]];
+  __syncthreads();
   auto small = [&](int row) { return tokens_of(row) <= few; };
   auto few_group = [&](int g) { return g < n && group_tok[g] <= few; };
-  for (int t = threadIdx.x; t < a.tok_off[n]; t += THREADS) p.rec[t] = make_int4(-1, 0, -1, 0);
 
-  // Both kinds are laid out alike: rows in the order of their keys, their tokens cut into items.
-  int n_items = 0, n_runs = 0, n_tok = 0;
-  for (int kind = 0; kind < 2; ++kind) {
-    const int cut = kind ? few : 2 * tile, unit = kind ? PIECE : page, block_units = kind ? 1 : page_blk;
-    int nl = 0;
-    // tiles: all but the prefixes that have few rows, and rows with few tokens that read no prefix.  few: those prefixes'
-    // rows; rows with few tokens whose prefix tiles read; and those that read none
-    for (int part = 0; part < (kind ? (few > 0 ? 3 : 0) : 1); ++part) {
-      for (int i0 = 0; i0 < ns; i0 += THREADS) {
-        const int i = i0 + threadIdx.x;
-        bool in = false;
-        int row = 0, k = 0;
-        if (i < ns) {
-          row = sorted[i];
-          k = group_of[i];
-          const bool fg = few_group(k);
-          if (kind == 0) {
-            in = !fg && (k < n || !small(row));
-          } else if (part == 0) {
-            in = fg;
-          } else {
-            in = !fg && small(row) && (part == 1 ? k < n && a.seq_lens[row] > 0 : k == n);
-            k = n + part - 1;
-          }
-        }
-        const int at = nl + static_cast<int>(block_exclusive(static_cast<unsigned long long>(in), warp_sum, total));
-        if (in) list[at] = row, key[at] = k;
-        nl += static_cast<int>(total);
-      }
-    }
-    __syncthreads();
-    int carry = 0;
-    for (int i0 = 0; i0 < nl; i0 += THREADS) {
+  // the lists: tiles: all but the prefixes that have few rows, and rows with few tokens that read no prefix.  few: those
+  // prefixes' rows; rows with few tokens whose prefix tiles read; and those that read none
+  int base[8] = {}, nl = 0;
+  for (int pass = ns > THREADS ? 0 : 1; pass < 2; ++pass) {  // with more rows than threads: first the lists' lengths
+    int seen[8] = {};
+    for (int i0 = 0; i0 < ns; i0 += THREADS) {
       const int i = i0 + threadIdx.x;
-      const int tok = i < nl ? tokens_of(list[i]) : 0;
-      const int at = carry + static_cast<int>(block_exclusive(static_cast<unsigned long long>(tok), warp_sum, total));
-      if (i < nl) {
-        place[i] = at;
-        if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = at;
-      }
-      carry += static_cast<int>(total);
-    }
-    if (threadIdx.x == 0) place[nl] = carry;
-    __syncthreads();
-
-    // items, written by the last row of each key
-    const int items0 = n_items;
-    for (int i0 = 0; i0 < nl; i0 += THREADS) {
-      const int i = i0 + threadIdx.x;
-      const int k = i < nl ? key[i] : 0;
-      int count = 0, tok = 0;
-      if (i < nl && (i + 1 == nl || key[i + 1] != k)) {
-        tok = place[i + 1] - first_tok[k];
-        count = (tok + cut - 1) / cut;
-      }
-      const int at = n_items + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-      if (count > 0) first_item[k] = at;
-      for (int c = 0; c < count; ++c) {
-        Item it{};
-        it.tok = n_tok + first_tok[k] + c * cut;
-        it.n_tok = min(cut, tok - c * cut);
-        it.prefix_keys = k < n ? a.seq_lens[k] : 0;
-        it.flags = kind == 0 ? ITEM_ALONE : ITEM_FEW | (k == n ? 0u : ITEM_ALONE);
-        p.items[at + c] = it;
-      }
-      n_items += static_cast<int>(total);
-    }
-    __syncthreads();
-
-    // runs, by their rows: a row writes its own run in each item that has tokens of it (of tiles: unless a few item has
-    // its own keys), and the prefix's in each item that begins with it
-    for (int i0 = 0; i0 < nl; i0 += THREADS) {
-      const int i = i0 + threadIdx.x;
-      int in = 0, tok = 0, k0 = 0, k1 = -1, begun = 0, k = 0;
-      bool own = false;
-      if (i < nl) {
-        k = key[i];
-        in = place[i] - first_tok[k];
-        tok = place[i + 1] - place[i];
-        k0 = in / cut;
-        k1 = (in + tok - 1) / cut;
-        begun = k1 - (in + cut - 1) / cut + 1;  // items whose first token is one of the row's
-        own = kind == 1 || !small(list[i]);
-      }
-      const int count = (own ? k1 - k0 + 1 : 0) + (k < n ? begun : 0);
-      int at = n_runs + static_cast<int>(block_exclusive(static_cast<unsigned long long>(count), warp_sum, total));
-      for (int c = k0; c <= k1; ++c) {
-        Item& it = p.items[first_item[k] + c];
-        const int lo = max(in, c * cut), hi = min(in + tok, (c + 1) * cut);  // places among the key's tokens
-        if (lo == c * cut) {
-          it.run = at;
-          if (k < n) {
-            const int keys_ = a.seq_lens[k];
-            p.runs[at++] = Run{k, 0, (keys_ + unit - 1) / unit, keys_, 0, it.n_tok, -1, 0};
-          }
-        }
-        if (!own) continue;
-        const int row = list[i];
-        const int seen = max(0, a.seq_lens[row] - (in + tok - hi));  // own keys of its last token here
-        p.runs[at++] = Run{row, 0, (seen + unit - 1) / unit, seen, lo - c * cut, hi - c * cut, a.tok_off[row] + lo - in, 0};
-      }
-      n_runs += static_cast<int>(total);
-    }
-    __syncthreads();
-
-    // a warp a row: its tokens' items; a token with a few item beside its tiles spoils the tiles' being alone
-    for (int i = warp; i < nl; i += THREADS / 32) {
-      const int row = list[i], k = key[i], in = place[i] - first_tok[k], tok = place[i + 1] - place[i], t0 = a.tok_off[row];
-      const bool beside = kind == 0 && k < n && small(row) && a.seq_lens[row] > 0;
-      for (int j = lane; j < tok; j += 32) {
-        const int item = first_item[k] + (in + j) / cut, at = (in + j) % cut;
-        const int o = n_tok + place[i] + j;
-        p.order[o] = t0 + j;
-        p.own[o] = make_int2(0, 0);
-        int2* rec = reinterpret_cast<int2*>(p.rec + t0 + j) + kind;
-        *rec = make_int2(item, at);
-        if (beside) p.items[item].flags = 0;
-      }
-    }
-    __syncthreads();
-
-    // a warp an item: where its runs' pages begin, and its tokens' own columns
-    for (int c = items0 + warp; c < n_items; c += THREADS / 32) {
-      Item it = p.items[c];
-      it.n_runs = (c + 1 < n_items ? p.items[c + 1].run : n_runs) - it.run;
-      int pages = 0, end0 = 0, begin1 = INT_MAX;
-      for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
-        const int r = r0 + lane;
-        Run run{};
-        if (r < it.n_runs) run = p.runs[it.run + r];
-        int inc = run.pages;
+      int v[8] = {}, total[8], row = 0, k = 0;
+      if (i < ns) {
+        row = sorted[i];
+        k = group_of[i];
+        const int tok = tokens_of(row);
+        const bool fg = few_group(k), sm = tok <= few;
+        v[0] = !fg && (k < n || !sm);
+        v[1] = fg;
+        v[2] = !fg && sm && k < n && a.seq_lens[row] > 0;
+        v[3] = !fg && sm && k == n;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int u = __shfl_up_sync(0xffffffffu, inc, o);
-          if (lane >= o) inc += u;
-        }
-        const int off = pages + inc - run.pages;
-        if (r < it.n_runs) {
-          p.runs[it.run + r].off = off;
-          if (run.tok0 < tile) end0 = max(end0, off + run.pages);
-          if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
-          // the last token sees the run's keys, each before it one less
-          for (int x = run.tok0; run.token >= 0 && x < run.tok1; ++x)
-            p.own[it.tok + x] = make_int2(off * unit, off * unit + max(0, run.keys - (run.tok1 - 1 - x)));
-        }
-        pages += __shfl_sync(0xffffffffu, inc, 31);
+        for (int l = 0; l < 4; ++l) v[4 + l] = v[l] ? tok : 0;
       }
-      end0 = __reduce_max_sync(0xffffffffu, end0);
-      begin1 = __reduce_min_sync(0xffffffffu, begin1);
-      if (lane == 0) {
-        it.pages = pages;
-        it.blocks = (pages + block_units - 1) / block_units;
-        it.end0 = (end0 + page_blk - 1) / page_blk;
-        it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
-        it.begin1 = begin1 / page_blk;
-        p.items[c] = it;
+      const bool in[4] = {v[0] != 0, v[1] != 0, v[2] != 0, v[3] != 0};
+      sum8(v, total);
+      if (ns <= THREADS) {
+#pragma unroll
+        for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + total[l - 1], base[4 + l] = base[3 + l] + total[3 + l];
       }
+#pragma unroll
+      for (int l = 0; l < 4; ++l)
+        if (pass == 1 && in[l]) {
+          const int at = base[l] + seen[l] + v[l];
+          list[at] = row;
+          key[at] = l == 0 ? k : l == 1 ? n + 1 + k : 2 * n - 1 + l;  // the last two keys: 2 n + 1, 2 n + 2
+          place[at] = base[4 + l] + seen[4 + l] + v[4 + l];
+        }
+#pragma unroll
+      for (int l = 0; l < 8; ++l) seen[l] += total[l];
     }
-    n_tok += carry;
-    __syncthreads();
+    if (pass == 0) {
+#pragma unroll
+      for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + seen[l - 1], base[4 + l] = base[3 + l] + seen[3 + l];
+    } else {
+      nl = base[3] + seen[3];
+      if (threadIdx.x == 0) place[nl] = base[7] + seen[7];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < nl; i += THREADS)
+    if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = place[i];
+  __syncthreads();
+  auto is_few = [&](int k) { return k > n; };
+  auto cut_of = [&](int k) { return is_few(k) ? few : 2 * tile; };
+  auto prefix_of = [&](int k) { return k < n ? k : k > n && k <= 2 * n ? k - n - 1 : -1; };
+
+  // items, by the last row of each key
+  int n_items = 0, n_runs = 0;
+  for (int i0 = 0; i0 < nl; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    const int k = i < nl ? key[i] : 0;
+    int v[1] = {0}, total[1], tok = 0;
+    if (i < nl && (i + 1 == nl || key[i + 1] != k)) {
+      tok = place[i + 1] - first_tok[k];
+      v[0] = (tok + cut_of(k) - 1) / cut_of(k);
+    }
+    const int count = v[0];
+    sum1(v, total);
+    const int at = n_items + v[0];
+    if (count > 0) first_item[k] = at;
+    spread(count, [&](bool on, int src, int c) {
+      const int k_ = of_lane(k, src), at_ = of_lane(at, src), tok_ = of_lane(tok, src);
+      if (!on) return;
+      const int pre = prefix_of(k_), cut = cut_of(k_);
+      Item it{};
+      it.tok = first_tok[k_] + c * cut;
+      it.n_tok = min(cut, tok_ - c * cut);
+      it.prefix_keys = pre >= 0 ? a.seq_lens[pre] : 0;
+      it.flags = is_few(k_) ? ITEM_FEW | (k_ == 2 * n + 1 ? 0u : ITEM_ALONE) : ITEM_ALONE;
+      items[at_ + c] = it;
+    });
+    n_items += total[0];
+  }
+  __syncthreads();
+
+  // runs, by their rows: a row has its own run in each item that has tokens of it (of tiles: unless a few item has its own
+  // keys), and writes the prefix's in each item that begins with it.  A token with a few item beside its tiles spoils the
+  // tiles' being alone.
+  for (int i0 = 0; i0 < nl; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    int v[1] = {0}, total[1], in = 0, tok = 0, k0 = 0, n_in = 0, k = 0, row = 0;
+    bool own = false, beside = false;
+    if (i < nl) {
+      k = key[i], row = list[i];
+      in = place[i] - first_tok[k];
+      tok = place[i + 1] - place[i];
+      const int cut = cut_of(k);
+      k0 = in / cut;
+      const int k1 = (in + tok - 1) / cut;
+      n_in = k1 - k0 + 1;
+      own = is_few(k) || !small(row);
+      beside = k < n && small(row) && a.seq_lens[row] > 0;
+      // items whose first token is one of the row's: k1 - (in + cut - 1) / cut + 1
+      v[0] = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - (in + cut - 1) / cut + 1 : 0);
+    }
+    sum1(v, total);
+    const int at = n_runs + v[0];
+    if (i < nl) row_run[i] = at;
+    spread(n_in, [&](bool on, int src, int c) {
+      const int k_ = of_lane(k, src), in_ = of_lane(in, src), tok_ = of_lane(tok, src), row_ = of_lane(row, src);
+      const int own_ = of_lane(own, src), beside_ = of_lane(beside, src);
+      int at_ = of_lane(at, src);
+      const int item = c + of_lane(k0, src);
+      if (!on) return;
+      const int cut = cut_of(k_), unit = is_few(k_) ? PIECE : page, pre = prefix_of(k_);
+      Item& it = items[first_item[k_] + item];
+      const int lo = max(in_, item * cut), hi = min(in_ + tok_, (item + 1) * cut);  // places among the key's tokens
+      at_ += run_before(c, in_ % cut == 0, own_, pre >= 0);
+      if (lo == item * cut) {
+        it.run = at_;
+        if (pre >= 0) runs[at_++] = Run{pre, 0, (it.prefix_keys + unit - 1) / unit, it.prefix_keys, 0, it.n_tok, -1, 0};
+      }
+      if (beside_) it.flags = 0;
+      if (!own_) return;
+      const int seen = max(0, a.seq_lens[row_] - (in_ + tok_ - hi));  // own keys of its last token here
+      runs[at_] = Run{row_, 0, (seen + unit - 1) / unit, seen, lo - item * cut, hi - item * cut, a.tok_off[row_] + lo - in_, 0};
+    });
+    n_runs += total[0];
+  }
+  __syncthreads();
+
+  // a warp an item: where its runs' pages begin
+  for (int c = warp; c < n_items; c += WARPS) {
+    Item it = items[c];
+    it.n_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - it.run;
+    int pages = 0, end0 = 0, begin1 = INT_MAX;
+    for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
+      const int r = r0 + lane;
+      Run run{};
+      if (r < it.n_runs) run = runs[it.run + r];
+      const int inc = warp_inclusive(run.pages);
+      const int off = pages + inc - run.pages;
+      if (r < it.n_runs) {
+        runs[it.run + r].off = off;
+        if (run.tok0 < tile) end0 = max(end0, off + run.pages);
+        if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
+      }
+      pages += of_lane(inc, 31);
+    }
+    end0 = __reduce_max_sync(0xffffffffu, end0);
+    begin1 = __reduce_min_sync(0xffffffffu, begin1);
+    const int block_units = it.flags & ITEM_FEW ? 1 : page_blk;
+    if (lane == 0) {
+      it.pages = pages;
+      it.blocks = (pages + block_units - 1) / block_units;
+      it.end0 = (end0 + page_blk - 1) / page_blk;
+      it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
+      it.begin1 = begin1 / page_blk;
+      items[c] = it;
+    }
+  }
+  __syncthreads();
+
+  // a warp some rows: their tokens' items and own columns
+  {
+    const int rows_a_warp = (nl + WARPS - 1) / WARPS, end = min(nl, (warp + 1) * rows_a_warp);
+    for (int i0 = warp * rows_a_warp; i0 < end; i0 += 32) {
+      const int i = i0 + lane;
+      int k = 0, in = 0, tok = 0, t0 = 0, own = 0, o0 = 0, run0 = 0;
+      if (i < end) {
+        k = key[i], o0 = place[i], run0 = row_run[i];
+        in = o0 - first_tok[k];
+        tok = place[i + 1] - o0;
+        t0 = a.tok_off[list[i]];
+        own = is_few(k) || !small(list[i]);
+      }
+      spread(tok, [&](bool on, int src, int j) {
+        const int k_ = of_lane(k, src), in_ = of_lane(in, src), t = of_lane(t0, src) + j, o = of_lane(o0, src) + j;
+        const int own_ = of_lane(own, src), run0_ = of_lane(run0, src);
+        if (!on) return;
+        const int cut = cut_of(k_), item = (in_ + j) / cut, at = (in_ + j) % cut;
+        p.order[o] = t;
+        reinterpret_cast<int2*>(p.rec + t)[is_few(k_)] = make_int2(first_item[k_] + item, at);
+        int2 cols = make_int2(0, 0);
+        if (own_) {
+          const bool pre = prefix_of(k_) >= 0;
+          const int c = item - in_ / cut;
+          const bool begins = c > 0 || in_ % cut == 0;
+          const Run run = runs[run0_ + run_before(c, in_ % cut == 0, true, pre) + (begins && pre)];
+          // the last token sees the run's keys, each before it one less
+          const int from = run.off * (is_few(k_) ? PIECE : page);
+          cols = make_int2(from, from + max(0, run.keys - (run.tok1 - 1 - at)));
+        }
+        p.own[o] = cols;
+      });
+    }
   }
 
-  // the line
-  unsigned long long tiles_line = 0, few_line = 0;
+  // the lines
+  unsigned long long line[2] = {0, 0};  // of tiles, of few items
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    unsigned long long length = 0;
-    bool is_few = false;
+    unsigned long long v[2] = {0, 0}, inc[2];
+    bool of_few = false;
     if (i < n_items) {
-      const Item it = p.items[i];
-      length = static_cast<unsigned long long>(Hkv) * length_of(it, G);
-      is_few = it.flags & ITEM_FEW;
+      const Item& it = items[i];
+      of_few = it.flags & ITEM_FEW;
+      v[of_few] = static_cast<unsigned long long>(Hkv) * length_of(it, G);
     }
-    const unsigned long long at_tiles = tiles_line + block_exclusive(is_few ? 0ull : length, warp_sum, total);
-    tiles_line += total;
-    const unsigned long long at_few = few_line + block_exclusive(is_few ? length : 0ull, warp_sum, total);
-    few_line += total;
-    if (i < n_items) p.items[i].start = static_cast<uint32_t>(is_few ? at_few : at_tiles);
+#pragma unroll
+    for (int l = 0; l < 2; ++l) {
+      inc[l] = v[l];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long u = __shfl_up_sync(0xffffffffu, inc[l], o);
+        if (lane >= o) inc[l] += u;
+      }
+    }
+    __syncthreads();
+    if (lane == 31) lines[0][warp] = inc[0], lines[1][warp] = inc[1];
+    __syncthreads();
+    unsigned long long before[2];
+#pragma unroll
+    for (int l = 0; l < 2; ++l) {
+      unsigned long long w = lines[l][lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long u = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += u;
+      }
+      before[l] = line[l] + (warp > 0 ? __shfl_sync(0xffffffffu, w, warp - 1) : 0ull) + inc[l] - v[l];
+      line[l] += __shfl_sync(0xffffffffu, w, 31);
+    }
+    if (i < n_items) items[i].start = static_cast<uint32_t>(before[of_few]);
   }
+  const unsigned long long tiles_line = line[0], few_line = line[1];
   // CTAs for each kind by what they take, one at least
   const bool both = tiles_line > 0 && few_line > 0, fits = tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
   int tile_ctas = few_line > 0 ? 0 : n_ctas;
@@ -343,73 +469,102 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   if (fits && few_ctas > 0) few_share = max(few_share, static_cast<uint32_t>((few_line + few_ctas * WORKERS - 1) / (few_ctas * WORKERS)));
   __syncthreads();
   const int n_flat = fits ? n_items * Hkv : 0;
-  // the CTAs' segments, rows of partial results, pieces of the join's list
-  unsigned long long segments = 0, tile_segments = 0, rows = 0;  // in the upper half of rows: pieces
+  // the shares' segments, rows of partial results, pieces of the join's list
+  int done[4] = {0, 0, 0, 0};  // segments, those of tiles, rows, pieces
   for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
     const int f = f0 + threadIdx.x;
-    unsigned long long count = 0;
-    uint32_t segs = 0, few_segs = 0, entry_share = 1;
-    int entry_rows = 0;
-    bool right_away = false;
-    Item it{};
-    OnLine on{0, 1};
+    int v[4] = {0, 0, 0, 0}, total[4];
+    int segs = 0, entry_rows = 0, cta0 = 0, right_away = 0;
     if (f < n_flat) {
-      it = p.items[f / Hkv];
-      on = on_line(it, f % Hkv, G);
-      entry_share = it.flags & ITEM_FEW ? few_share : share;
-      segs = on.segments(it.blocks, entry_share);
-      if (it.flags & ITEM_FEW) few_segs = segs;
+      const Item& it = items[f / Hkv];
+      const OnLine on = on_line(it, f % Hkv, G);
+      const uint32_t entry_share = it.flags & ITEM_FEW ? few_share : share;
+      v[0] = segs = on.segments(it.blocks, entry_share);
+      v[1] = it.flags & ITEM_FEW ? 0 : segs;
+      cta0 = on.cta_of(0, entry_share);
       right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
       if (!right_away) {
         entry_rows = it.n_tok * G;
-        count = static_cast<unsigned long long>(segs) * entry_rows * copies_of(it, G);
+        v[2] = segs * entry_rows * copies_of(it, G);
         // rows of a few item beside tiles are joined by the tiles' pieces
         if ((it.flags & (ITEM_FEW | ITEM_ALONE)) == ITEM_FEW) entry_rows = 0;
-        count |= static_cast<unsigned long long>((entry_rows + JOIN_ROWS - 1) / JOIN_ROWS) << 32;
+        v[3] = (entry_rows + JOIN_ROWS - 1) / JOIN_ROWS;
       }
     }
-    const unsigned long long at = rows + block_exclusive(count, warp_sum, total);
-    rows += total;
-    if (f < n_flat) p.part[f] = static_cast<uint32_t>(at);
-    for (int r = 0; r < entry_rows; r += JOIN_ROWS) p.join[(at >> 32) + r / JOIN_ROWS] = make_int2(f, r);
-    const uint32_t seg0 = static_cast<uint32_t>(segments + block_exclusive(static_cast<unsigned long long>(segs), warp_sum, total));
-    segments += total;
-    block_exclusive(static_cast<unsigned long long>(segs - few_segs), warp_sum, total);
-    tile_segments += total;
-    for (uint32_t i = 0; i < segs; ++i) {
-      const uint32_t c = on.cta_of(0, entry_share) + i;
+    const int n_pieces = v[3];
+    sum4(v, total);
+    const int seg0 = done[0] + v[0], part_row = done[2] + v[2], piece0 = done[3] + v[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) done[i] += total[i];
+    if (f < n_flat) p.part[f] = part_row;
+    spread(n_pieces, [&](bool on, int src, int i) {
+      const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i;
+      if (on) p.join[piece] = make_int2(f_, i * JOIN_ROWS);
+    });
+    spread(segs, [&](bool on_, int src, int i) {
+      const int f_ = of_lane(f, src), at = of_lane(seg0, src) + i, whole = of_lane(right_away, src), row0 = of_lane(part_row, src);
+      const uint32_t c = of_lane(cta0, src) + i;
+      if (!on_) return;
+      const Item it = items[f_ / Hkv];
+      const OnLine on = on_line(it, f_ % Hkv, G);
+      const bool of_few = it.flags & ITEM_FEW;
+      const uint32_t entry_share = of_few ? few_share : share;
       Segment sg{};
-      sg.f = f;
-      sg.h = f % Hkv;
+      sg.f = f_;
+      sg.h = f_ % Hkv;
       sg.b0 = on.block_from(c * entry_share, it.blocks);
       sg.b1 = on.block_from((c + 1) * entry_share, it.blocks);
       sg.tok = it.tok, sg.n_tok = it.n_tok, sg.run = it.run, sg.n_runs = it.n_runs;
       sg.prefix_keys = it.prefix_keys, sg.pages = it.pages;
       sg.end0 = it.end0, sg.begin1 = it.begin1, sg.prefix_blocks = it.prefix_blocks;
-      sg.flags = (two_tiles(it, G) ? SEG_TWO : 0u) | (it.flags & ITEM_FEW ? SEG_FEW : 0u) | (right_away ? SEG_WHOLE : 0u);
-      sg.part_row = static_cast<uint32_t>(at) + i * copies_of(it, G) * it.n_tok * G;
-      p.segs[seg0 + i] = sg;
-    }
+      sg.flags = (two_tiles(it, G) ? SEG_TWO : 0u) | (of_few ? SEG_FEW : 0u) | (whole ? SEG_WHOLE : 0u);
+      sg.part_row = static_cast<uint32_t>(row0) + i * copies_of(it, G) * it.n_tok * G;
+      p.segs[at] = sg;
+      atomicMin(&first_of[of_few ? tile_ctas + 1 + c : c], at);
+    });
   }
-  // the shares' first segments
+  if (threadIdx.x == 0) atomicMin(&first_of[tile_ctas], done[1]);
+  // what the shares' kernel and the joining one read of items and runs
+  if (in_shared & ITEMS_SHARED)
+    for (int i = threadIdx.x; i < n_items * static_cast<int>(sizeof(Item) / 16); i += THREADS)
+      reinterpret_cast<int4*>(p.items)[i] = reinterpret_cast<const int4*>(items)[i];
+  if (in_shared & RUNS_SHARED)
+    for (int i = threadIdx.x; i < n_runs * static_cast<int>(sizeof(Run) / 16); i += THREADS)
+      reinterpret_cast<int4*>(p.runs)[i] = reinterpret_cast<const int4*>(runs)[i];
   __syncthreads();
-  for (int c = threadIdx.x; c < SHARES; c += THREADS) {
-    const bool of_few = c > tile_ctas;
-    const uint32_t mine = of_few ? c - tile_ctas - 1 : c, kind_share = of_few ? few_share : share;
-    int lo = of_few ? static_cast<int>(tile_segments) : 0, hi = static_cast<int>(of_few ? segments : tile_segments);
-    while (lo < hi) {  // the first segment of this share or a later one
-      const int mid = (lo + hi) >> 1;
-      const Segment& sg = p.segs[mid];
-      if (on_line(p.items[sg.f / Hkv], sg.h, G).cta_of(sg.b0, kind_share) < mine) lo = mid + 1; else hi = mid;
+  // the shares' first segments; one without gets the next one's, the last the end
+  {
+    constexpr int EACH = (SHARES + THREADS - 1) / THREADS;
+    int low[EACH], least = done[0];
+#pragma unroll
+    for (int i = EACH - 1; i >= 0; --i) {
+      const int c = threadIdx.x * EACH + i;
+      if (c < SHARES) least = min(least, first_of[c]);
+      low[i] = least;
     }
-    p.first[c] = lo;
+    int after = least;  // of this thread and those behind it in the warp
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_down_sync(0xffffffffu, after, o);
+      if (lane + o < 32) after = min(after, u);
+    }
+    if (lane == 0) sums_memory[0][warp] = after;
+    __syncthreads();
+    const int behind = __reduce_min_sync(0xffffffffu, lane > warp ? sums_memory[0][lane] : INT_MAX);
+    const int next = __shfl_down_sync(0xffffffffu, after, 1);
+    const int rest = min(behind, lane < 31 ? next : INT_MAX);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int c = threadIdx.x * EACH + i;
+      if (c < SHARES) p.first[c] = min(low[i], rest);
+    }
   }
   if (threadIdx.x == 0) {
     if (fits) {
-      head.tokens = a.tok_off[n];
+      head.tokens = n_sorted_tok;
       head.n_items = n_items;
       head.n_flat = n_flat;
-      head.n_join = static_cast<int>(rows >> 32);
+      head.n_join = done[3];
       head.share = share;
       head.few_share = few_share;
       head.tile_ctas = tile_ctas;
@@ -426,12 +581,23 @@ int64_t shared_plan_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens) 
 }
 
 cudaError_t launch_shared_plan(const SharedPlanArgs& a, int num_sms, cudaStream_t st) {
-  int keys = 2;
-  while (keys < a.lay.n_seqs) keys <<= 1;
-  static_assert(CACHE_MAX_SEQS * 4 <= 65536, "shared memory of the sort");
-  const cudaError_t e = cudaFuncSetAttribute(k_shared_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, 65536);
+  const int n = a.lay.n_seqs, G = a.Hq / a.lay.n_kv_heads;
+  int n_keys = 32, in_shared = 0;
+  while (n_keys < n) n_keys <<= 1;
+  int64_t bytes = 4 * static_cast<int64_t>(n_keys);
+  auto take = [&](int what, int64_t more) {
+    more = (more + 15) / 16 * 16;
+    if (bytes + more > MAX_SHARED) return;
+    bytes += more;
+    in_shared |= what;
+  };
+  take(LISTS_SHARED, 4 * plan_scratch_ints(n));
+  take(ITEMS_SHARED, max_items(n, G, a.max_tokens) * static_cast<int64_t>(sizeof(Item)));
+  take(RUNS_SHARED, max_runs(n, G, a.max_tokens) * static_cast<int64_t>(sizeof(Run)));
+  const cudaError_t e = cudaFuncSetAttribute(k_shared_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SHARED);
   if (e != cudaSuccess) return e;
-  return launch_dependent(k_shared_plan, dim3(1), THREADS, keys * 4, st, a, num_sms < MAX_CTAS ? num_sms : MAX_CTAS);
+  return launch_dependent(k_shared_plan, dim3(1), THREADS, static_cast<int>(bytes), st, a, num_sms < MAX_CTAS ? num_sms : MAX_CTAS, n_keys,
+                          in_shared);
 }
 
 }  // namespace dopr

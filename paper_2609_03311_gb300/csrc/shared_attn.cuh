@@ -106,7 +106,7 @@ struct Plan {
   int2* join;      // flat entry, first of up to JOIN_ROWS rows that are to be added up from partial results
   int* order;      // [2 * tokens] the items' tokens
   int2* own;       // [2 * tokens, in that order] columns of its own keys, from and to
-  int* scratch;    // 8 * n_seqs + 8, of the plan kernel
+  int* scratch;    // plan_scratch_ints(n_seqs), of the plan kernel where its shared memory does not hold them
   int64_t bytes;
 };
 __host__ __device__ inline int tokens_a_tile(int G) { return TILE / G; }
@@ -118,6 +118,11 @@ __host__ __device__ inline int64_t max_items(int n_seqs, int G, int max_tokens) 
   return (static_cast<int64_t>(max_tokens) + pair - 1) / pair + rows +
          (few > 0 ? (static_cast<int64_t>(max_tokens) + few - 1) / few + rows + 2 : 0);
 }
+// a run for every row, one more wherever an item ends within a row, and the prefixes'
+__host__ __device__ inline int64_t max_runs(int n_seqs, int G, int max_tokens) {
+  return 2 * (max_items(n_seqs, G, max_tokens) + (n_seqs < max_tokens ? n_seqs : max_tokens));
+}
+__host__ __device__ inline int64_t plan_scratch_ints(int64_t n_seqs) { return 15 * n_seqs + 8; }
 __host__ __device__ inline int64_t max_pieces(int n_seqs, int n_kv_heads, int G, int max_tokens) {
   return max_items(n_seqs, G, max_tokens) * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / JOIN_ROWS;
 }
@@ -136,13 +141,12 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   p.rec = static_cast<int4*>(take(16 * static_cast<int64_t>(max_tokens)));
   p.segs = static_cast<Segment*>(take((items * n_kv_heads + SHARES) * static_cast<int64_t>(sizeof(Segment))));
   p.items = static_cast<Item*>(take(items * static_cast<int64_t>(sizeof(Item))));
-  // a run for every row, one more wherever an item ends within a row, and the prefixes'
-  p.runs = static_cast<Run*>(take(2 * (items + (n_seqs < max_tokens ? n_seqs : max_tokens)) * static_cast<int64_t>(sizeof(Run))));
+  p.runs = static_cast<Run*>(take(max_runs(n_seqs, G, max_tokens) * static_cast<int64_t>(sizeof(Run))));
   p.part = static_cast<uint32_t*>(take(4 * items * n_kv_heads));
   p.join = static_cast<int2*>(take(8 * max_pieces(n_seqs, n_kv_heads, G, max_tokens)));
   p.order = static_cast<int*>(take(8 * static_cast<int64_t>(max_tokens)));
   p.own = static_cast<int2*>(take(16 * static_cast<int64_t>(max_tokens)));
-  p.scratch = static_cast<int*>(take(4 * (8 * static_cast<int64_t>(n_seqs) + 8)));
+  p.scratch = static_cast<int*>(take(4 * plan_scratch_ints(n_seqs)));
   p.bytes = at;
   return p;
 }

@@ -30,29 +30,41 @@ __device__ int warp_inclusive(int v) {
   return v;
 }
 
-// Exclusive sums of N values over the block's threads in order; the block's totals through `total`.  One barrier: the warps'
-// sums lie in one of two places by turns, and who writes one has passed the barrier behind its last readers.
+// Exclusive sums of N values over the block's threads in order, of which the first `count` have some; the block's totals
+// through `total`.  One barrier: the warps' sums lie in one of two places by turns, and who writes one has passed the barrier
+// behind its last readers.  With 32 warps on one SM it is the number of shuffles that counts, so warps without values only
+// add up the others' sums, with a reducing instruction (all 32 warps scanning: 5,000 cycles for the eight sums of the lists).
 template <int N>
 struct BlockSums {
   int (*sums)[WARPS];  // [2 * N] in shared memory
   int turn = 0;
-  __device__ void operator()(int (&v)[N], int (&total)[N]) {
+  __device__ void operator()(int (&v)[N], int (&total)[N], int count) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool any = warp * 32 < count;
     int inc[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      inc[i] = warp_inclusive(v[i]);
+      inc[i] = any ? warp_inclusive(v[i]) : 0;
       if (lane == 31) sums[turn * N + i][warp] = inc[i];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int w = warp_inclusive(sums[turn * N + i][lane]);
-      const int before = __shfl_sync(0xffffffffu, w, warp > 0 ? warp - 1 : 0);
-      total[i] = __shfl_sync(0xffffffffu, w, 31);
-      v[i] = (warp > 0 ? before : 0) + inc[i] - v[i];
+      const int w = sums[turn * N + i][lane];
+      total[i] = __reduce_add_sync(0xffffffffu, w);
+      if (any) v[i] = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + inc[i] - v[i];
     }
     turn ^= 1;
+  }
+};
+
+// Division by a number that stays: m is 2^32 / d or up to one less, so the product's upper half is the quotient or one less.
+struct Divisor {
+  uint32_t d, m;
+  __device__ explicit Divisor(uint32_t divisor) : d(divisor), m(divisor ? 0xffffffffu / divisor : 0) {}
+  __device__ uint32_t of(uint32_t x) const {
+    const uint32_t q = __umulhi(x, m);
+    return x - q * d >= d ? q + 1 : q;
   }
 };
 
@@ -109,7 +121,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   __shared__ int sums_memory[2 * 8][WARPS];
   __shared__ int first_of[SHARES];
   __shared__ int bad, unsorted;
-  __shared__ unsigned long long lines[2][WARPS];
+  __shared__ unsigned long long lines[WARPS], tiles_line, both_lines;
+  __shared__ int first_few;
   const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page, page_blk = BLOCK / page;
   const int tile = tokens_a_tile(G), few = tokens_a_few(G);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -135,7 +148,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   int* row_run = place + 2 * n + 1;    // its first run
   int* first_tok = row_run + 2 * n;    // of a key: tokens before its first
   int* first_item = first_tok + 2 * n + 3;
-  if (threadIdx.x == 0) bad = 0, unsorted = 0;
+  if (threadIdx.x == 0) bad = 0, unsorted = 0, tiles_line = both_lines = 0, first_few = 0;
   for (int c = threadIdx.x; c < SHARES; c += THREADS) first_of[c] = INT_MAX;
   BlockSums<1> sum1{sums_memory};
   BlockSums<2> sum2{sums_memory};
@@ -170,7 +183,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       if (v[0] && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
     }
     const bool has = v[0];
-    sum2(v, total);
+    sum2(v, total, n - i0);
     if (has) sorted[ns + v[0]] = i, group_of[ns + v[0]] = g, place[ns + v[0]] = n_sorted_tok + v[1];
     ns += total[0];
     n_sorted_tok += total[1];
@@ -205,7 +218,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
         group_of[i] = keys[i] >> ROW_BITS;
         v[0] = tokens_of(sorted[i]);
       }
-      sum1(v, total);
+      sum1(v, total, ns - i0);
       if (i < ns) place[i] = carry + v[0];
       carry += total[0];
     }
@@ -243,7 +256,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
         for (int l = 0; l < 4; ++l) v[4 + l] = v[l] ? tok : 0;
       }
       const bool in[4] = {v[0] != 0, v[1] != 0, v[2] != 0, v[3] != 0};
-      sum8(v, total);
+      sum8(v, total, ns - i0);
       if (ns <= THREADS) {
 #pragma unroll
         for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + total[l - 1], base[4 + l] = base[3 + l] + total[3 + l];
@@ -272,7 +285,12 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = place[i];
   __syncthreads();
   auto is_few = [&](int k) { return k > n; };
+  const Divisor by_pair(2 * tile), by_few(few), by_heads(Hkv);
+  const int page_bits = __ffs(page) - 1, page_blk_bits = __ffs(page_blk) - 1;  // powers of two
   auto cut_of = [&](int k) { return is_few(k) ? few : 2 * tile; };
+  auto in_cuts = [&](int k, int x) { return static_cast<int>(is_few(k) ? by_few.of(x) : by_pair.of(x)); };
+  auto in_units = [&](bool of_few, int x) { return of_few ? (x + PIECE - 1) / PIECE : (x + page - 1) >> page_bits; };
+  auto in_blocks = [&](int pages) { return (pages + page_blk - 1) >> page_blk_bits; };
   auto prefix_of = [&](int k) { return k < n ? k : k > n && k <= 2 * n ? k - n - 1 : -1; };
 
   // items, by the last row of each key
@@ -283,10 +301,10 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     int v[1] = {0}, total[1], tok = 0;
     if (i < nl && (i + 1 == nl || key[i + 1] != k)) {
       tok = place[i + 1] - first_tok[k];
-      v[0] = (tok + cut_of(k) - 1) / cut_of(k);
+      v[0] = in_cuts(k, tok + cut_of(k) - 1);
     }
     const int count = v[0];
-    sum1(v, total);
+    sum1(v, total, nl - i0);
     const int at = n_items + v[0];
     if (count > 0) first_item[k] = at;
     spread(count, [&](bool on, int src, int c) {
@@ -316,68 +334,77 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       in = place[i] - first_tok[k];
       tok = place[i + 1] - place[i];
       const int cut = cut_of(k);
-      k0 = in / cut;
-      const int k1 = (in + tok - 1) / cut;
+      k0 = in_cuts(k, in);
+      const int k1 = in_cuts(k, in + tok - 1);
       n_in = k1 - k0 + 1;
       own = is_few(k) || !small(row);
       beside = k < n && small(row) && a.seq_lens[row] > 0;
-      // items whose first token is one of the row's: k1 - (in + cut - 1) / cut + 1
-      v[0] = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - (in + cut - 1) / cut + 1 : 0);
+      // items whose first token is one of the row's: those up to k1 from the first that begins at or behind `in`
+      v[0] = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - in_cuts(k, in + cut - 1) + 1 : 0);
     }
-    sum1(v, total);
+    sum1(v, total, nl - i0);
     const int at = n_runs + v[0];
     if (i < nl) row_run[i] = at;
     spread(n_in, [&](bool on, int src, int c) {
       const int k_ = of_lane(k, src), in_ = of_lane(in, src), tok_ = of_lane(tok, src), row_ = of_lane(row, src);
       const int own_ = of_lane(own, src), beside_ = of_lane(beside, src);
       int at_ = of_lane(at, src);
-      const int item = c + of_lane(k0, src);
+      const int k0_ = of_lane(k0, src), item = c + k0_;
       if (!on) return;
-      const int cut = cut_of(k_), unit = is_few(k_) ? PIECE : page, pre = prefix_of(k_);
+      const int cut = cut_of(k_), pre = prefix_of(k_);
       Item& it = items[first_item[k_] + item];
       const int lo = max(in_, item * cut), hi = min(in_ + tok_, (item + 1) * cut);  // places among the key's tokens
-      at_ += run_before(c, in_ % cut == 0, own_, pre >= 0);
+      at_ += run_before(c, in_ == k0_ * cut, own_, pre >= 0);
       if (lo == item * cut) {
         it.run = at_;
-        if (pre >= 0) runs[at_++] = Run{pre, 0, (it.prefix_keys + unit - 1) / unit, it.prefix_keys, 0, it.n_tok, -1, 0};
+        if (pre >= 0) runs[at_++] = Run{pre, 0, in_units(is_few(k_), it.prefix_keys), it.prefix_keys, 0, it.n_tok, -1, 0};
       }
       if (beside_) it.flags = 0;
       if (!own_) return;
       const int seen = max(0, a.seq_lens[row_] - (in_ + tok_ - hi));  // own keys of its last token here
-      runs[at_] = Run{row_, 0, (seen + unit - 1) / unit, seen, lo - item * cut, hi - item * cut, a.tok_off[row_] + lo - in_, 0};
+      runs[at_] = Run{row_, 0, in_units(is_few(k_), seen), seen, lo - item * cut, hi - item * cut, a.tok_off[row_] + lo - in_, 0};
     });
     n_runs += total[0];
   }
   __syncthreads();
 
-  // a warp an item: where its runs' pages begin
-  for (int c = warp; c < n_items; c += WARPS) {
-    Item it = items[c];
-    it.n_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - it.run;
+  // eight lanes an item: where its runs' pages begin
+  for (int c = threadIdx.x / 8; c < n_items; c += THREADS / 8) {
+    const int part = threadIdx.x & 7;
+    const uint32_t mask = 0xffu << (lane & 24);
+    Item& it = items[c];
+    const int run0 = it.run, it_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - run0;
     int pages = 0, end0 = 0, begin1 = INT_MAX;
-    for (int r0 = 0; r0 < it.n_runs; r0 += 32) {
-      const int r = r0 + lane;
-      Run run{};
-      if (r < it.n_runs) run = runs[it.run + r];
-      const int inc = warp_inclusive(run.pages);
-      const int off = pages + inc - run.pages;
-      if (r < it.n_runs) {
-        runs[it.run + r].off = off;
-        if (run.tok0 < tile) end0 = max(end0, off + run.pages);
-        if (run.token >= 0 && run.tok1 > tile) begin1 = min(begin1, off);
+    for (int r0 = 0; r0 < it_runs; r0 += 8) {
+      Run* run = runs + run0 + r0 + part;
+      const bool on = r0 + part < it_runs;
+      const int mine = on ? run->pages : 0;
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 8; o <<= 1) {
+        const int u = __shfl_up_sync(mask, inc, o, 8);
+        if (part >= o) inc += u;
       }
-      pages += of_lane(inc, 31);
+      if (on) {
+        const int off = pages + inc - mine;
+        run->off = off;
+        if (run->tok0 < tile) end0 = max(end0, off + mine);
+        if (run->token >= 0 && run->tok1 > tile) begin1 = min(begin1, off);
+      }
+      pages += __shfl_sync(mask, inc, 7, 8);
     }
-    end0 = __reduce_max_sync(0xffffffffu, end0);
-    begin1 = __reduce_min_sync(0xffffffffu, begin1);
-    const int block_units = it.flags & ITEM_FEW ? 1 : page_blk;
-    if (lane == 0) {
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      end0 = max(end0, __shfl_xor_sync(mask, end0, o));
+      begin1 = min(begin1, __shfl_xor_sync(mask, begin1, o));
+    }
+    if (part == 0) {
+      it.n_runs = it_runs;
       it.pages = pages;
-      it.blocks = (pages + block_units - 1) / block_units;
-      it.end0 = (end0 + page_blk - 1) / page_blk;
-      it.prefix_blocks = ((it.prefix_keys + page - 1) / page + page_blk - 1) / page_blk;
-      it.begin1 = begin1 / page_blk;
-      items[c] = it;
+      it.blocks = it.flags & ITEM_FEW ? pages : in_blocks(pages);
+      it.end0 = in_blocks(end0);
+      it.prefix_blocks = in_blocks(in_units(false, it.prefix_keys));
+      it.begin1 = begin1 >> page_blk_bits;
     }
   }
   __syncthreads();
@@ -387,27 +414,28 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     const int rows_a_warp = (nl + WARPS - 1) / WARPS, end = min(nl, (warp + 1) * rows_a_warp);
     for (int i0 = warp * rows_a_warp; i0 < end; i0 += 32) {
       const int i = i0 + lane;
-      int k = 0, in = 0, tok = 0, t0 = 0, own = 0, o0 = 0, run0 = 0;
+      int k = 0, in = 0, tok = 0, t0 = 0, own = 0, o0 = 0, run0 = 0, k0 = 0;
       if (i < end) {
         k = key[i], o0 = place[i], run0 = row_run[i];
         in = o0 - first_tok[k];
         tok = place[i + 1] - o0;
+        k0 = in_cuts(k, in);
         t0 = a.tok_off[list[i]];
         own = is_few(k) || !small(list[i]);
       }
       spread(tok, [&](bool on, int src, int j) {
         const int k_ = of_lane(k, src), in_ = of_lane(in, src), t = of_lane(t0, src) + j, o = of_lane(o0, src) + j;
-        const int own_ = of_lane(own, src), run0_ = of_lane(run0, src);
+        const int own_ = of_lane(own, src), run0_ = of_lane(run0, src), k0_ = of_lane(k0, src);
         if (!on) return;
-        const int cut = cut_of(k_), item = (in_ + j) / cut, at = (in_ + j) % cut;
+        const int cut = cut_of(k_), item = in_cuts(k_, in_ + j), at = in_ + j - item * cut;
         p.order[o] = t;
         reinterpret_cast<int2*>(p.rec + t)[is_few(k_)] = make_int2(first_item[k_] + item, at);
         int2 cols = make_int2(0, 0);
         if (own_) {
           const bool pre = prefix_of(k_) >= 0;
-          const int c = item - in_ / cut;
-          const bool begins = c > 0 || in_ % cut == 0;
-          const Run run = runs[run0_ + run_before(c, in_ % cut == 0, true, pre) + (begins && pre)];
+          const int c = item - k0_;
+          const bool first = in_ == k0_ * cut;
+          const Run& run = runs[run0_ + run_before(c, first, true, pre) + (pre && (c > 0 || first))];
           // the last token sees the run's keys, each before it one less
           const int from = run.off * (is_few(k_) ? PIECE : page);
           cols = make_int2(from, from + max(0, run.keys - (run.tok1 - 1 - at)));
@@ -417,44 +445,39 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     }
   }
 
-  // the lines
-  unsigned long long line[2] = {0, 0};  // of tiles, of few items
+  // the lines: the items of tiles come first
+  unsigned long long line = 0;
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    unsigned long long v[2] = {0, 0}, inc[2];
-    bool of_few = false;
+    const unsigned long long v = i < n_items ? static_cast<unsigned long long>(Hkv) * length_of(items[i], G) : 0;
+    unsigned long long inc = v;
+    if (warp * 32 < n_items - i0) {
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long u = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += u;
+      }
+    }
+    if (lane == 31) lines[warp] = inc;
+    __syncthreads();
+    unsigned long long before = line;
+    for (int w = 0; w < warp && w * 32 < n_items - i0; ++w) before += lines[w];
+    before += inc - v;
     if (i < n_items) {
-      const Item& it = items[i];
-      of_few = it.flags & ITEM_FEW;
-      v[of_few] = static_cast<unsigned long long>(Hkv) * length_of(it, G);
-    }
-#pragma unroll
-    for (int l = 0; l < 2; ++l) {
-      inc[l] = v[l];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long u = __shfl_up_sync(0xffffffffu, inc[l], o);
-        if (lane >= o) inc[l] += u;
+      items[i].start = static_cast<uint32_t>(before);  // of few items: the tiles' line before it too, for now
+      if ((items[i].flags & ITEM_FEW) && (i == 0 || !(items[i - 1].flags & ITEM_FEW))) tiles_line = before, first_few = i;
+      if (i == n_items - 1) {
+        both_lines = before + v;
+        if (!(items[i].flags & ITEM_FEW)) tiles_line = before + v, first_few = n_items;
       }
     }
-    __syncthreads();
-    if (lane == 31) lines[0][warp] = inc[0], lines[1][warp] = inc[1];
-    __syncthreads();
-    unsigned long long before[2];
-#pragma unroll
-    for (int l = 0; l < 2; ++l) {
-      unsigned long long w = lines[l][lane];
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned long long u = __shfl_up_sync(0xffffffffu, w, o);
-        if (lane >= o) w += u;
-      }
-      before[l] = line[l] + (warp > 0 ? __shfl_sync(0xffffffffu, w, warp - 1) : 0ull) + inc[l] - v[l];
-      line[l] += __shfl_sync(0xffffffffu, w, 31);
+    if (i0 + THREADS < n_items) {
+      for (int w = 0; w < WARPS; ++w) line += lines[w];
+      __syncthreads();
     }
-    if (i < n_items) items[i].start = static_cast<uint32_t>(before[of_few]);
   }
-  const unsigned long long tiles_line = line[0], few_line = line[1];
+  __syncthreads();
+  const unsigned long long few_line = both_lines - tiles_line;
   // CTAs for each kind by what they take, one at least
   const bool both = tiles_line > 0 && few_line > 0, fits = tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
   int tile_ctas = few_line > 0 ? 0 : n_ctas;
@@ -467,6 +490,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   uint32_t share = block_length(false), few_share = MIN_FEW_SHARE;
   if (fits && tile_ctas > 0) share = max(share, static_cast<uint32_t>((tiles_line + tile_ctas - 1) / tile_ctas));
   if (fits && few_ctas > 0) few_share = max(few_share, static_cast<uint32_t>((few_line + few_ctas * WORKERS - 1) / (few_ctas * WORKERS)));
+  const Divisor by_share(share), by_few_share(few_share);
+  for (int i = first_few + threadIdx.x; i < n_items; i += THREADS) items[i].start -= static_cast<uint32_t>(tiles_line);
   __syncthreads();
   const int n_flat = fits ? n_items * Hkv : 0;
   // the shares' segments, rows of partial results, pieces of the join's list
@@ -476,12 +501,13 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     int v[4] = {0, 0, 0, 0}, total[4];
     int segs = 0, entry_rows = 0, cta0 = 0, right_away = 0;
     if (f < n_flat) {
-      const Item& it = items[f / Hkv];
-      const OnLine on = on_line(it, f % Hkv, G);
-      const uint32_t entry_share = it.flags & ITEM_FEW ? few_share : share;
-      v[0] = segs = on.segments(it.blocks, entry_share);
+      const int i = by_heads.of(f);
+      const Item& it = items[i];
+      const OnLine on = on_line(it, f - i * Hkv, G);
+      const Divisor& by = it.flags & ITEM_FEW ? by_few_share : by_share;
+      cta0 = by.of(on.begin);
+      if (it.blocks > 0) v[0] = segs = by.of(on.begin + (it.blocks - 1) * on.length) - cta0 + 1;
       v[1] = it.flags & ITEM_FEW ? 0 : segs;
-      cta0 = on.cta_of(0, entry_share);
       right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
       if (!right_away) {
         entry_rows = it.n_tok * G;
@@ -492,7 +518,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       }
     }
     const int n_pieces = v[3];
-    sum4(v, total);
+    sum4(v, total, n_flat - f0);
     const int seg0 = done[0] + v[0], part_row = done[2] + v[2], piece0 = done[3] + v[3];
 #pragma unroll
     for (int i = 0; i < 4; ++i) done[i] += total[i];
@@ -505,13 +531,14 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       const int f_ = of_lane(f, src), at = of_lane(seg0, src) + i, whole = of_lane(right_away, src), row0 = of_lane(part_row, src);
       const uint32_t c = of_lane(cta0, src) + i;
       if (!on_) return;
-      const Item it = items[f_ / Hkv];
-      const OnLine on = on_line(it, f_ % Hkv, G);
+      const int item = by_heads.of(f_), h = f_ - item * Hkv;
+      const Item& it = items[item];
+      const OnLine on = on_line(it, h, G);
       const bool of_few = it.flags & ITEM_FEW;
       const uint32_t entry_share = of_few ? few_share : share;
       Segment sg{};
       sg.f = f_;
-      sg.h = f_ % Hkv;
+      sg.h = h;
       sg.b0 = on.block_from(c * entry_share, it.blocks);
       sg.b1 = on.block_from((c + 1) * entry_share, it.blocks);
       sg.tok = it.tok, sg.n_tok = it.n_tok, sg.run = it.run, sg.n_runs = it.n_runs;

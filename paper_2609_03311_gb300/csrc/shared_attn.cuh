@@ -169,7 +169,7 @@ struct OnLine {
   // first block that begins at or behind a place on the line
   __host__ __device__ uint32_t block_from(uint32_t at, uint32_t blocks) const {
     if (at <= begin) return 0;
-    const uint32_t b = (at - begin + length - 1) / length;
+    const uint32_t b = length == 1 ? at - begin : (at - begin + block_length(false) - 1) / block_length(false);
     return b < blocks ? b : blocks;
   }
   __host__ __device__ uint32_t cta_of(uint32_t block, uint32_t share) const { return (begin + block * length) / share; }

@@ -4,8 +4,11 @@
 // One CTA: everything is sums over the step's rows, and the rows of a prefix brought together.  Rows usually come in
 // prefix order; those that do not are sorted (a bitonic network over (prefix, row) in shared memory; rows of a
 // prefix keep their order).  Made once a step and used by every layer.  Bound by the latency of some twenty short phases:
-// lists, items and runs stay in shared memory where they fit, a sum over the block takes one barrier, and what rows, items
-// and entries hold several of (items, runs, tokens, segments) is spread over a warp's lanes.
+// lists, items and runs stay in shared memory where they fit, a sum over the block takes one barrier and two counts where
+// they fit, and what rows, items and entries hold several of (items, runs, tokens, segments) is spread over a warp's lanes.
+// 512 threads: 10.9 us for one token, 14.1 for 64 queries of one document, 20.9 for 256 of 64 documents, 28.7 for 5,000 tokens
+// of 200 queries; 1024: 12.1, 15.7, 20.8, 26.4 (a barrier and a sum cost more the more warps there are); 256: 10.7, 13.6, 25.9,
+// 37.5.
 #include <limits.h>
 
 #include "shared_attn.cuh"
@@ -14,7 +17,7 @@ namespace dopr {
 namespace {
 using namespace shared_attn;
 
-constexpr int THREADS = 1024, WARPS = THREADS / 32;
+constexpr int THREADS = 512, WARPS = THREADS / 32;
 constexpr int ROW_BITS = 14;
 constexpr int MAX_SHARED = 200 * 1024;
 static_assert(CACHE_MAX_SEQS == 1 << ROW_BITS, "a sort key holds two row numbers");
@@ -30,33 +33,19 @@ __device__ int warp_inclusive(int v) {
   return v;
 }
 
-// Exclusive sums of N values over the block's threads in order, of which the first `count` have some; the block's totals
-// through `total`.  One barrier: the warps' sums lie in one of two places by turns, and who writes one has passed the barrier
-// behind its last readers.  With 32 warps on one SM it is the number of shuffles that counts, so warps without values only
-// add up the others' sums, with a reducing instruction (all 32 warps scanning: 5,000 cycles for the eight sums of the lists).
-template <int N>
-struct BlockSums {
-  int (*sums)[WARPS];  // [2 * N] in shared memory
-  int turn = 0;
-  __device__ void operator()(int (&v)[N], int (&total)[N], int count) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool any = warp * 32 < count;
-    int inc[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      inc[i] = any ? warp_inclusive(v[i]) : 0;
-      if (lane == 31) sums[turn * N + i][warp] = inc[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int w = sums[turn * N + i][lane];
-      total[i] = __reduce_add_sync(0xffffffffu, w);
-      if (any) v[i] = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) + inc[i] - v[i];
-    }
-    turn ^= 1;
-  }
-};
+// Exclusive sums over the block's threads in order, of which the first `count` have values; x: a thread's sum, y: all.  One
+// barrier: the warps' sums lie in one of two places by turns, and who writes one has passed the barrier behind its last
+// readers.  Warps without values only add up the others' sums.
+__device__ __noinline__ int2 block_sum(int v, int count, int* sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const bool any = warp * 32 < count;
+  int inc = any ? warp_inclusive(v) : 0;
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  const int w = sums[lane];
+  if (any) inc += __reduce_add_sync(0xffffffffu, lane < warp ? w : 0) - v;
+  return make_int2(inc, __reduce_add_sync(0xffffffffu, w));
+}
 
 // Division by a number that stays: m is 2^32 / d or up to one less, so the product's upper half is the quotient or one less.
 struct Divisor {
@@ -72,6 +61,7 @@ struct Divisor {
 template <typename F>
 __device__ void spread(int count, F f) {
   const int inc = warp_inclusive(count), total = __shfl_sync(0xffffffffu, inc, 31);
+  #pragma unroll 1
   for (int s = threadIdx.x & 31; s < (total + 31) / 32 * 32; s += 32) {
     int src = 0;  // lanes whose counts end at or before s
 #pragma unroll
@@ -86,9 +76,12 @@ __device__ __forceinline__ int of_lane(int v, int src) { return __shfl_sync(0xff
 __device__ void sort_keys(uint32_t* keys, int m) {
   const int threads = min(m, THREADS), tid = threadIdx.x;
   if (tid >= threads) return;
+  #pragma unroll 1
   for (int k = 2; k <= m; k <<= 1) {
     int j = k >> 1;
+    #pragma unroll 1
     for (; j >= 32; j >>= 1) {
+      #pragma unroll 1
       for (int i = tid; i < m; i += threads) {
         const int o = i ^ j;
         if (o > i) {
@@ -98,8 +91,10 @@ __device__ void sort_keys(uint32_t* keys, int m) {
       }
       asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
     }
+    #pragma unroll 1
     for (int i = tid; i < m; i += threads) {
       uint32_t x = keys[i];
+      #pragma unroll 1
       for (int l = j; l > 0; l >>= 1) {
         const uint32_t y = __shfl_xor_sync(0xffffffffu, x, l);
         x = ((i & l) == 0) == ((i & k) == 0) ? min(x, y) : max(x, y);
@@ -116,9 +111,9 @@ __device__ __forceinline__ int run_before(int c, bool first, bool own, bool pref
   return (own ? c : 0) + (prefix && c > 0 ? c - !first : 0);
 }
 
-__global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n_ctas, int n_keys, int in_shared) {
+__global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan p, int n_ctas, int n_keys, int in_shared) {
   extern __shared__ __align__(16) uint32_t keys[];  // a power of two >= n_seqs, then what in_shared says
-  __shared__ int sums_memory[2 * 8][WARPS];
+  __shared__ int sums_memory[2][32];
   __shared__ int first_of[SHARES];
   __shared__ int bad, unsorted;
   __shared__ unsigned long long lines[WARPS], tiles_line, both_lines;
@@ -127,7 +122,6 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   const int tile = tokens_a_tile(G), few = tokens_a_few(G);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t cap = static_cast<int64_t>(a.lay.max_blocks) * page;
-  const Plan p = plan_view(a.plan, n, Hkv, G, a.max_tokens);
   uint8_t* at_shared = reinterpret_cast<uint8_t*>(keys + n_keys);
   auto shared = [&](int what, auto* global, int64_t count) {
     if (!(in_shared & what)) return global;
@@ -149,11 +143,15 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   int* first_tok = row_run + 2 * n;    // of a key: tokens before its first
   int* first_item = first_tok + 2 * n + 3;
   if (threadIdx.x == 0) bad = 0, unsorted = 0, tiles_line = both_lines = 0, first_few = 0;
+  if (threadIdx.x < 64) sums_memory[threadIdx.x >> 5][lane] = 0;
+#pragma unroll 1
   for (int c = threadIdx.x; c < SHARES; c += THREADS) first_of[c] = INT_MAX;
-  BlockSums<1> sum1{sums_memory};
-  BlockSums<2> sum2{sums_memory};
-  BlockSums<4> sum4{sums_memory};
-  BlockSums<8> sum8{sums_memory};
+  int turn = 0;
+  auto sum = [&](int v, int count, int& total) {
+    const int2 r = block_sum(v, count, sums_memory[turn ^= 1]);
+    total = r.y;
+    return r.x;
+  };
   pdl_wait();
   pdl_trigger();
   __syncthreads();
@@ -170,6 +168,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
 
   // checks, and the rows with tokens
   int ns = 0, n_sorted_tok = 0;
+  #pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     int v[2] = {0, 0}, total[2], g = n;
@@ -183,7 +182,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       if (v[0] && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
     }
     const bool has = v[0];
-    sum2(v, total, n - i0);
+    for (int l = 0; l < 2; ++l) v[l] = sum(v[l], n - i0, total[l]);
     if (has) sorted[ns + v[0]] = i, group_of[ns + v[0]] = g, place[ns + v[0]] = n_sorted_tok + v[1];
     ns += total[0];
     n_sorted_tok += total[1];
@@ -194,22 +193,28 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       *p.head = head;
       if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
     }
+    #pragma unroll 1
     for (int c = threadIdx.x; c < SHARES; c += THREADS) p.first[c] = 0;
     return;
   }
+  #pragma unroll 1
   for (int t = threadIdx.x; t < n_sorted_tok; t += THREADS) p.rec[t] = make_int4(-1, 0, -1, 0);
+  #pragma unroll 1
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
     if (group_of[i] < group_of[i - 1]) unsorted = 1;
   __syncthreads();
   if (unsorted) {
     int m = 32;
+    #pragma unroll 1
     while (m < ns) m <<= 1;
+    #pragma unroll 1
     for (int i = threadIdx.x; i < m; i += THREADS)
       keys[i] = i < ns ? static_cast<uint32_t>(group_of[i]) << ROW_BITS | sorted[i] : 0xffffffffu;
     __syncthreads();
     sort_keys(keys, m);
     __syncthreads();
     int carry = 0;
+    #pragma unroll 1
     for (int i0 = 0; i0 < ns; i0 += THREADS) {
       const int i = i0 + threadIdx.x;
       int v[1] = {0}, total[1];
@@ -218,7 +223,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
         group_of[i] = keys[i] >> ROW_BITS;
         v[0] = tokens_of(sorted[i]);
       }
-      sum1(v, total, ns - i0);
+      v[0] = sum(v[0], ns - i0, total[0]);
       if (i < ns) place[i] = carry + v[0];
       carry += total[0];
     }
@@ -226,9 +231,11 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   if (threadIdx.x == 0) place[ns] = n_sorted_tok;
   __syncthreads();
   // a group's tokens: its rows stand together
+  #pragma unroll 1
   for (int i = threadIdx.x; i < ns; i += THREADS)
     if (i == 0 || group_of[i - 1] != group_of[i]) first_tok[group_of[i]] = place[i];
   __syncthreads();
+  #pragma unroll 1
   for (int i = threadIdx.x; i < ns; i += THREADS)
     if (i + 1 == ns || group_of[i + 1] != group_of[i]) group_tok[group_of[i]] = place[i + 1] - first_tok[group_of[i]];
   __syncthreads();
@@ -237,52 +244,65 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
 
   // the lists: tiles: all but the prefixes that have few rows, and rows with few tokens that read no prefix.  few: those
   // prefixes' rows; rows with few tokens whose prefix tiles read; and those that read none
-  int base[8] = {}, nl = 0;
+  int base[4] = {}, nl = 0;
+#pragma unroll 1
   for (int pass = ns > THREADS ? 0 : 1; pass < 2; ++pass) {  // with more rows than threads: first the lists' lengths
-    int seen[8] = {};
+    int seen[4] = {};
+#pragma unroll 1
     for (int i0 = 0; i0 < ns; i0 += THREADS) {
       const int i = i0 + threadIdx.x;
-      int v[8] = {}, total[8], row = 0, k = 0;
+      int row = 0, k = 0;
+      bool in[4] = {};
       if (i < ns) {
         row = sorted[i];
         k = group_of[i];
-        const int tok = tokens_of(row);
-        const bool fg = few_group(k), sm = tok <= few;
-        v[0] = !fg && (k < n || !sm);
-        v[1] = fg;
-        v[2] = !fg && sm && k < n && a.seq_lens[row] > 0;
-        v[3] = !fg && sm && k == n;
-#pragma unroll
-        for (int l = 0; l < 4; ++l) v[4 + l] = v[l] ? tok : 0;
+        const bool fg = few_group(k), sm = small(row);
+        in[0] = !fg && (k < n || !sm);
+        in[1] = fg;
+        in[2] = !fg && sm && k < n && a.seq_lens[row] > 0;
+        in[3] = !fg && sm && k == n;
       }
-      const bool in[4] = {v[0] != 0, v[1] != 0, v[2] != 0, v[3] != 0};
-      sum8(v, total, ns - i0);
-      if (ns <= THREADS) {
+      int v[4], total[4];
 #pragma unroll
-        for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + total[l - 1], base[4 + l] = base[3 + l] + total[3 + l];
+      for (int l = 0; l < 4; l += 2) {  // two counts a sum
+        static_assert(THREADS < 1 << 15, "a count takes 16 bits");
+        int both = 0;
+        const int x = sum(in[l] | in[l + 1] << 16, ns - i0, both);
+        v[l] = x & 0xffff, v[l + 1] = x >> 16;
+        total[l] = both & 0xffff, total[l + 1] = both >> 16;
       }
+      if (ns <= THREADS)
+        for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + total[l - 1];
 #pragma unroll
-      for (int l = 0; l < 4; ++l)
+      for (int l = 0; l < 4; ++l) {
         if (pass == 1 && in[l]) {
           const int at = base[l] + seen[l] + v[l];
           list[at] = row;
           key[at] = l == 0 ? k : l == 1 ? n + 1 + k : 2 * n - 1 + l;  // the last two keys: 2 n + 1, 2 n + 2
-          place[at] = base[4 + l] + seen[4 + l] + v[4 + l];
         }
-#pragma unroll
-      for (int l = 0; l < 8; ++l) seen[l] += total[l];
+        seen[l] += total[l];
+      }
     }
     if (pass == 0) {
-#pragma unroll
-      for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + seen[l - 1], base[4 + l] = base[3 + l] + seen[3 + l];
+      for (int l = 1; l < 4; ++l) base[l] = base[l - 1] + seen[l - 1];
     } else {
       nl = base[3] + seen[3];
-      if (threadIdx.x == 0) place[nl] = base[7] + seen[7];
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < nl; i += THREADS)
-    if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = place[i];
+  int n_listed_tok = 0;
+#pragma unroll 1
+  for (int i0 = 0; i0 < nl; i0 += THREADS) {
+    const int i = i0 + threadIdx.x;
+    int total;
+    const int at = n_listed_tok + sum(i < nl ? tokens_of(list[i]) : 0, nl - i0, total);
+    if (i < nl) {
+      place[i] = at;
+      if (i == 0 || key[i - 1] != key[i]) first_tok[key[i]] = at;
+    }
+    n_listed_tok += total;
+  }
+  if (threadIdx.x == 0) place[nl] = n_listed_tok;
   __syncthreads();
   auto is_few = [&](int k) { return k > n; };
   const Divisor by_pair(2 * tile), by_few(few), by_heads(Hkv);
@@ -295,6 +315,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
 
   // items, by the last row of each key
   int n_items = 0, n_runs = 0;
+  #pragma unroll 1
   for (int i0 = 0; i0 < nl; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     const int k = i < nl ? key[i] : 0;
@@ -304,7 +325,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       v[0] = in_cuts(k, tok + cut_of(k) - 1);
     }
     const int count = v[0];
-    sum1(v, total, nl - i0);
+    v[0] = sum(v[0], nl - i0, total[0]);
     const int at = n_items + v[0];
     if (count > 0) first_item[k] = at;
     spread(count, [&](bool on, int src, int c) {
@@ -325,6 +346,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   // runs, by their rows: a row has its own run in each item that has tokens of it (of tiles: unless a few item has its own
   // keys), and writes the prefix's in each item that begins with it.  A token with a few item beside its tiles spoils the
   // tiles' being alone.
+  #pragma unroll 1
   for (int i0 = 0; i0 < nl; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     int v[1] = {0}, total[1], in = 0, tok = 0, k0 = 0, n_in = 0, k = 0, row = 0;
@@ -342,7 +364,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       // items whose first token is one of the row's: those up to k1 from the first that begins at or behind `in`
       v[0] = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - in_cuts(k, in + cut - 1) + 1 : 0);
     }
-    sum1(v, total, nl - i0);
+    v[0] = sum(v[0], nl - i0, total[0]);
     const int at = n_runs + v[0];
     if (i < nl) row_run[i] = at;
     spread(n_in, [&](bool on, int src, int c) {
@@ -369,12 +391,14 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   __syncthreads();
 
   // eight lanes an item: where its runs' pages begin
+  #pragma unroll 1
   for (int c = threadIdx.x / 8; c < n_items; c += THREADS / 8) {
     const int part = threadIdx.x & 7;
     const uint32_t mask = 0xffu << (lane & 24);
     Item& it = items[c];
     const int run0 = it.run, it_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - run0;
     int pages = 0, end0 = 0, begin1 = INT_MAX;
+    #pragma unroll 1
     for (int r0 = 0; r0 < it_runs; r0 += 8) {
       Run* run = runs + run0 + r0 + part;
       const bool on = r0 + part < it_runs;
@@ -412,6 +436,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   // a warp some rows: their tokens' items and own columns
   {
     const int rows_a_warp = (nl + WARPS - 1) / WARPS, end = min(nl, (warp + 1) * rows_a_warp);
+    #pragma unroll 1
     for (int i0 = warp * rows_a_warp; i0 < end; i0 += 32) {
       const int i = i0 + lane;
       int k = 0, in = 0, tok = 0, t0 = 0, own = 0, o0 = 0, run0 = 0, k0 = 0;
@@ -447,6 +472,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
 
   // the lines: the items of tiles come first
   unsigned long long line = 0;
+  #pragma unroll 1
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     const unsigned long long v = i < n_items ? static_cast<unsigned long long>(Hkv) * length_of(items[i], G) : 0;
@@ -461,6 +487,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     if (lane == 31) lines[warp] = inc;
     __syncthreads();
     unsigned long long before = line;
+    #pragma unroll 1
     for (int w = 0; w < warp && w * 32 < n_items - i0; ++w) before += lines[w];
     before += inc - v;
     if (i < n_items) {
@@ -472,6 +499,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       }
     }
     if (i0 + THREADS < n_items) {
+      #pragma unroll 1
       for (int w = 0; w < WARPS; ++w) line += lines[w];
       __syncthreads();
     }
@@ -482,48 +510,49 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
   const bool both = tiles_line > 0 && few_line > 0, fits = tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
   int tile_ctas = few_line > 0 ? 0 : n_ctas;
   if (both) {
-    const unsigned long long few_cost = few_line * FEW_PER_TILES / WORKERS;
-    tile_ctas = min(n_ctas - 1, max(1, static_cast<int>((n_ctas * tiles_line + (tiles_line + few_cost) / 2) / (tiles_line + few_cost))));
+    const float tiles_cost = static_cast<float>(tiles_line), few_cost = static_cast<float>(few_line) * FEW_PER_TILES / WORKERS;
+    tile_ctas = min(n_ctas - 1, max(1, __float2int_rn(n_ctas * tiles_cost / (tiles_cost + few_cost))));
   }
   const uint32_t few_ctas = n_ctas - tile_ctas;
   // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up
   uint32_t share = block_length(false), few_share = MIN_FEW_SHARE;
-  if (fits && tile_ctas > 0) share = max(share, static_cast<uint32_t>((tiles_line + tile_ctas - 1) / tile_ctas));
-  if (fits && few_ctas > 0) few_share = max(few_share, static_cast<uint32_t>((few_line + few_ctas * WORKERS - 1) / (few_ctas * WORKERS)));
+  if (fits && tile_ctas > 0) share = max(share, (static_cast<uint32_t>(tiles_line) + tile_ctas - 1) / tile_ctas);
+  if (fits && few_ctas > 0) few_share = max(few_share, (static_cast<uint32_t>(few_line) + few_ctas * WORKERS - 1) / (few_ctas * WORKERS));
   const Divisor by_share(share), by_few_share(few_share);
+  #pragma unroll 1
   for (int i = first_few + threadIdx.x; i < n_items; i += THREADS) items[i].start -= static_cast<uint32_t>(tiles_line);
   __syncthreads();
   const int n_flat = fits ? n_items * Hkv : 0;
   // the shares' segments, rows of partial results, pieces of the join's list
-  int done[4] = {0, 0, 0, 0};  // segments, those of tiles, rows, pieces
+  int n_segs = 0, n_rows = 0, n_join = 0;
+#pragma unroll 1
   for (int f0 = 0; f0 < n_flat; f0 += THREADS) {
     const int f = f0 + threadIdx.x;
-    int v[4] = {0, 0, 0, 0}, total[4];
-    int segs = 0, entry_rows = 0, cta0 = 0, right_away = 0;
+    int segs = 0, rows = 0, pieces = 0, cta0 = 0, right_away = 0;
     if (f < n_flat) {
       const int i = by_heads.of(f);
       const Item& it = items[i];
       const OnLine on = on_line(it, f - i * Hkv, G);
       const Divisor& by = it.flags & ITEM_FEW ? by_few_share : by_share;
       cta0 = by.of(on.begin);
-      if (it.blocks > 0) v[0] = segs = by.of(on.begin + (it.blocks - 1) * on.length) - cta0 + 1;
-      v[1] = it.flags & ITEM_FEW ? 0 : segs;
+      if (it.blocks > 0) segs = by.of(on.begin + (it.blocks - 1) * on.length) - cta0 + 1;
       right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
       if (!right_away) {
-        entry_rows = it.n_tok * G;
-        v[2] = segs * entry_rows * copies_of(it, G);
+        rows = segs * it.n_tok * G * copies_of(it, G);
         // rows of a few item beside tiles are joined by the tiles' pieces
-        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) == ITEM_FEW) entry_rows = 0;
-        v[3] = (entry_rows + JOIN_ROWS - 1) / JOIN_ROWS;
+        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) != ITEM_FEW) pieces = (it.n_tok * G + JOIN_ROWS - 1) / JOIN_ROWS;
       }
     }
-    const int n_pieces = v[3];
-    sum4(v, total, n_flat - f0);
-    const int seg0 = done[0] + v[0], part_row = done[2] + v[2], piece0 = done[3] + v[3];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) done[i] += total[i];
+    // two counts a sum: no more segments than entries and shares, 32 pieces an entry at most
+    static_assert(2 * TILE / JOIN_ROWS * THREADS < 1 << 16 && THREADS + SHARES < 1 << 15, "a count takes 16 bits");
+    int both, total;
+    const uint32_t at = sum(segs << 16 | pieces, n_flat - f0, both);
+    const int seg0 = n_segs + (at >> 16), piece0 = n_join + (at & 0xffff);
+    const int part_row = n_rows + sum(rows, n_flat - f0, total);
+    n_segs += static_cast<uint32_t>(both) >> 16, n_join += both & 0xffff, n_rows += total;
+    if (f < n_flat && f == first_few * Hkv) first_of[tile_ctas] = seg0;  // the end of tiles
     if (f < n_flat) p.part[f] = part_row;
-    spread(n_pieces, [&](bool on, int src, int i) {
+    spread(pieces, [&](bool on, int src, int i) {
       const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i;
       if (on) p.join[piece] = make_int2(f_, i * JOIN_ROWS);
     });
@@ -550,19 +579,20 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       atomicMin(&first_of[of_few ? tile_ctas + 1 + c : c], at);
     });
   }
-  if (threadIdx.x == 0) atomicMin(&first_of[tile_ctas], done[1]);
   // what the shares' kernel and the joining one read of items and runs
   if (in_shared & ITEMS_SHARED)
+    #pragma unroll 1
     for (int i = threadIdx.x; i < n_items * static_cast<int>(sizeof(Item) / 16); i += THREADS)
       reinterpret_cast<int4*>(p.items)[i] = reinterpret_cast<const int4*>(items)[i];
   if (in_shared & RUNS_SHARED)
+    #pragma unroll 1
     for (int i = threadIdx.x; i < n_runs * static_cast<int>(sizeof(Run) / 16); i += THREADS)
       reinterpret_cast<int4*>(p.runs)[i] = reinterpret_cast<const int4*>(runs)[i];
   __syncthreads();
   // the shares' first segments; one without gets the next one's, the last the end
   {
     constexpr int EACH = (SHARES + THREADS - 1) / THREADS;
-    int low[EACH], least = done[0];
+    int low[EACH], least = n_segs;
 #pragma unroll
     for (int i = EACH - 1; i >= 0; --i) {
       const int c = threadIdx.x * EACH + i;
@@ -577,7 +607,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
     }
     if (lane == 0) sums_memory[0][warp] = after;
     __syncthreads();
-    const int behind = __reduce_min_sync(0xffffffffu, lane > warp ? sums_memory[0][lane] : INT_MAX);
+    const int behind = __reduce_min_sync(0xffffffffu, lane > warp && lane < WARPS ? sums_memory[0][lane] : INT_MAX);
     const int next = __shfl_down_sync(0xffffffffu, after, 1);
     const int rest = min(behind, lane < 31 ? next : INT_MAX);
 #pragma unroll
@@ -591,7 +621,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, int n
       head.tokens = n_sorted_tok;
       head.n_items = n_items;
       head.n_flat = n_flat;
-      head.n_join = done[3];
+      head.n_join = n_join;
       head.share = share;
       head.few_share = few_share;
       head.tile_ctas = tile_ctas;
@@ -610,6 +640,7 @@ int64_t shared_plan_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens) 
 cudaError_t launch_shared_plan(const SharedPlanArgs& a, int num_sms, cudaStream_t st) {
   const int n = a.lay.n_seqs, G = a.Hq / a.lay.n_kv_heads;
   int n_keys = 32, in_shared = 0;
+  #pragma unroll 1
   while (n_keys < n) n_keys <<= 1;
   int64_t bytes = 4 * static_cast<int64_t>(n_keys);
   auto take = [&](int what, int64_t more) {
@@ -623,7 +654,8 @@ cudaError_t launch_shared_plan(const SharedPlanArgs& a, int num_sms, cudaStream_
   take(RUNS_SHARED, max_runs(n, G, a.max_tokens) * static_cast<int64_t>(sizeof(Run)));
   const cudaError_t e = cudaFuncSetAttribute(k_shared_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, MAX_SHARED);
   if (e != cudaSuccess) return e;
-  return launch_dependent(k_shared_plan, dim3(1), THREADS, static_cast<int>(bytes), st, a, num_sms < MAX_CTAS ? num_sms : MAX_CTAS, n_keys,
+  return launch_dependent(k_shared_plan, dim3(1), THREADS, static_cast<int>(bytes), st, a,
+                          plan_view(a.plan, n, a.lay.n_kv_heads, G, a.max_tokens), num_sms < MAX_CTAS ? num_sms : MAX_CTAS, n_keys,
                           in_shared);
 }
 

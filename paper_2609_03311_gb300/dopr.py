@@ -383,38 +383,33 @@ _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH_TYPES = (torch.float16, torch.bfloat16, torch.float32)
 
 
-class _On:
+# Calls of a few microseconds on the device are bound by what is done here: device and stream are asked for as numbers, and
+# a device or stream guard is made only where the current one is another.
+def _on(device, stream):
     """The device of the call's tensors and the stream made current, where they are not, so that what the call
-    allocates belongs to the stream that uses it; enters as the stream's handle."""
-
-    def __init__(self, device, stream):
-        if device.type != "cuda":
-            raise ValueError(f"the paged cache's calls take CUDA tensors, got one on {device}")
-        if stream is not None and stream.device != device:
+    allocates belongs to the stream that uses it.  (stream's handle, entered guard or None, device's number)"""
+    if device.type != "cuda":
+        raise ValueError(f"the paged cache's calls take CUDA tensors, got one on {device}")
+    index = device.index
+    if stream is not None:
+        if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        if stream is not None:
-            self.guard = torch.cuda.stream(stream)
-        else:
-            self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-            stream = torch.cuda.current_stream(device)
-        self.stream = stream.cuda_stream
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        guard = torch.cuda.stream(stream)
+        guard.__enter__()
+        return stream.cuda_stream, guard, index
+    guard = None
+    if torch._C._cuda_getDevice() != index:
+        guard = torch.cuda.device(device)
+        guard.__enter__()
+    return torch._C._cuda_getCurrentRawStream(index), guard, index
 
 
 def _buf(name, t, dtype, n, device):
-    """Pointer of a contiguous tensor of at least n elements; None passes NULL."""
+    """Pointer of a contiguous tensor of at least n elements on the numbered device; None passes NULL."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{name}: need {n} contiguous {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.dtype != dtype or t.get_device() != device or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: need {n} contiguous {dtype} on cuda:{device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -422,11 +417,12 @@ def _heads(name, t, tokens, head_dim, dtype, device):
     """A [tokens, heads, head_dim] tensor as the C ABI's view (strided, the last dimension contiguous)."""
     if t is None:
         return None
-    if t.dim() != 3 or t.shape[0] < tokens or t.shape[2] != head_dim or t.dtype != dtype or t.device != device or \
-            (head_dim > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on {device} with a contiguous last dimension, "
-                         f"got {tuple(t.shape)} {t.dtype} on {t.device}, strides {t.stride()}")
-    return ctypes.byref(Heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1]))
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] < tokens or shape[2] != head_dim or t.dtype != dtype or t.get_device() != device or \
+            (head_dim > 1 and strides[2] != 1):
+        raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on cuda:{device} with a contiguous last "
+                         f"dimension, got {tuple(shape)} {t.dtype} on {t.device}, strides {strides}")
+    return ctypes.byref(Heads(t.data_ptr(), strides[0], strides[1], shape[1]))
 
 
 def make_cache_layout(n_blocks: int, page: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seqs: int,
@@ -463,18 +459,22 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
     block_tables and free_blocks are updated in place, lengths and the stack's height in `out`."""
     dev = seq_lens.device
     n, i32 = layout.n_seqs, torch.int32
-    with _On(dev, stream) as st:
+    st, guard, on = _on(dev, stream)
+    try:
         if out is None:
             out = CacheBatch(layout, max_tokens, dev)
         _check(load().dopr_cache_extend(
-            ctypes.byref(layout), _buf("seq_lens", seq_lens, i32, n, dev),
-            _buf("block_tables", block_tables, i32, n * layout.max_blocks, dev),
-            _buf("free_blocks", free_blocks, i32, layout.n_blocks, dev), _buf("n_free", n_free, i32, 1, dev),
-            _buf("prefix", prefix, i32, n, dev), _buf("new_lens", new_lens, i32, n, dev), max_tokens,
-            _buf("out.seq_lens", out.seq_lens, i32, n, dev), _buf("out.n_free", out.n_free, i32, 1, dev),
-            _buf("out.tok_off", out.tok_off, i32, n + 1, dev), _buf("out.slots", out.slots, torch.int64, max_tokens, dev),
-            _buf("out.positions", out.positions, i32, max_tokens, dev),
-            _buf("out.workspace", out.workspace, torch.uint8, 0, dev), _buf("status", status, i32, 1, dev), st))
+            ctypes.byref(layout), _buf("seq_lens", seq_lens, i32, n, on),
+            _buf("block_tables", block_tables, i32, n * layout.max_blocks, on),
+            _buf("free_blocks", free_blocks, i32, layout.n_blocks, on), _buf("n_free", n_free, i32, 1, on),
+            _buf("prefix", prefix, i32, n, on), _buf("new_lens", new_lens, i32, n, on), max_tokens,
+            _buf("out.seq_lens", out.seq_lens, i32, n, on), _buf("out.n_free", out.n_free, i32, 1, on),
+            _buf("out.tok_off", out.tok_off, i32, n + 1, on), _buf("out.slots", out.slots, torch.int64, max_tokens, on),
+            _buf("out.positions", out.positions, i32, max_tokens, on),
+            _buf("out.workspace", out.workspace, torch.uint8, 0, on), _buf("status", status, i32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
     return out
 
 
@@ -508,16 +508,20 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse
     T, D, dt, dev = q.shape[0], q.shape[2], q.dtype, q.device
     if dt not in _DTYPES:
         raise ValueError(f"rope_apply: float16, bfloat16 or float32, got {dt}")
-    with _On(dev, stream) as st:
+    st, guard, on = _on(dev, stream)
+    try:
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=dev)
         if k is not None and k_out is None:
             k_out = torch.empty(k.shape, dtype=dt, device=dev)
         _check(load().dopr_rope_apply(
-            rope._h, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, dev), _heads("q", q, T, D, dt, dev),
-            _heads("q_out", q_out, T, D, dt, dev), _heads("k", k, T, D, dt, dev),
-            _heads("k_out", k_out if k is not None else None, T, D, dt, dev), int(inverse),
-            _buf("status", status, torch.int32, 1, dev), st))
+            rope._h, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, on), _heads("q", q, T, D, dt, on),
+            _heads("q_out", q_out, T, D, dt, on), _heads("k", k, T, D, dt, on),
+            _heads("k_out", k_out if k is not None else None, T, D, dt, on), int(inverse),
+            _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
     return q_out, k_out
 
 
@@ -527,15 +531,19 @@ def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | 
     where q is given."""
     T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
     pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
-    with _On(dev, stream) as st:
+    st, guard, on = _on(dev, stream)
+    try:
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=dev)
         _check(load().dopr_cache_append(
             ctypes.byref(layout), rope._h if rope is not None else None, T,
-            _buf("positions", positions, torch.int32, T, dev), _buf("slots", slots, torch.int64, T, dev),
-            _heads("q", q, T, D, dt, dev), _heads("q_out", q_out if q is not None else None, T, D, dt, dev),
-            _heads("k", k, T, D, dt, dev), _heads("v", v, T, D, dt, dev), _buf("k_pool", k_pool, dt, pool, dev),
-            _buf("v_pool", v_pool, dt, pool, dev), _buf("status", status, torch.int32, 1, dev), st))
+            _buf("positions", positions, torch.int32, T, on), _buf("slots", slots, torch.int64, T, on),
+            _heads("q", q, T, D, dt, on), _heads("q_out", q_out if q is not None else None, T, D, dt, on),
+            _heads("k", k, T, D, dt, on), _heads("v", v, T, D, dt, on), _buf("k_pool", k_pool, dt, pool, on),
+            _buf("v_pool", v_pool, dt, pool, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
     return q_out
 
 
@@ -551,14 +559,18 @@ def shared_attention_plan(layout: CacheLayout, n_q_heads: int, tok_off, seq_lens
     """How a step's attention is split: made once a step, used by every layer (of these sizes, on this device)."""
     dev = seq_lens.device
     n = layout.n_seqs
-    with _On(dev, stream) as st:
+    st, guard, on = _on(dev, stream)
+    try:
         need = _sized(load().dopr_shared_attention_plan_bytes, layout, n_q_heads, max_tokens)
         if plan is None:
             plan = torch.empty(need, dtype=torch.uint8, device=dev)
         _check(load().dopr_shared_attention_plan(
-            ctypes.byref(layout), n_q_heads, max_tokens, _buf("tok_off", tok_off, torch.int32, n + 1, dev),
-            _buf("seq_lens", seq_lens, torch.int32, n, dev), _buf("prefix", prefix, torch.int32, n, dev),
-            _buf("plan", plan, torch.uint8, need, dev), _buf("status", status, torch.int32, 1, dev), st))
+            ctypes.byref(layout), n_q_heads, max_tokens, _buf("tok_off", tok_off, torch.int32, n + 1, on),
+            _buf("seq_lens", seq_lens, torch.int32, n, on), _buf("prefix", prefix, torch.int32, n, on),
+            _buf("plan", plan, torch.uint8, need, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
     return plan
 
 
@@ -578,7 +590,8 @@ def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables,
         scale = D ** -0.5
     pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
     lib = load()
-    with _On(dev, stream) as st:
+    st, guard, on = _on(dev, stream)
+    try:
         if out is None:
             out = torch.empty((T, hq, D), dtype=dt, device=dev)
         need = _sized(lib.dopr_shared_attention_workspace, layout, hq, T)
@@ -586,12 +599,15 @@ def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables,
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
         _check(lib.dopr_shared_attention(
             ctypes.byref(layout),
-            _buf("plan", plan, torch.uint8, _sized(lib.dopr_shared_attention_plan_bytes, layout, hq, T), dev), T,
-            _heads("q", q, T, layout.head_dim, dt, dev), _buf("k_pool", k_pool, dt, pool, dev),
-            _buf("v_pool", v_pool, dt, pool, dev),
-            _buf("block_tables", block_tables, torch.int32, layout.n_seqs * layout.max_blocks, dev), scale,
-            _heads("out", out, T, layout.head_dim, dt, dev), _buf("lse", lse, torch.float32, T * hq, dev),
-            _buf("workspace", workspace, torch.uint8, need, dev), _buf("status", status, torch.int32, 1, dev), st))
+            _buf("plan", plan, torch.uint8, _sized(lib.dopr_shared_attention_plan_bytes, layout, hq, T), on), T,
+            _heads("q", q, T, layout.head_dim, dt, on), _buf("k_pool", k_pool, dt, pool, on),
+            _buf("v_pool", v_pool, dt, pool, on),
+            _buf("block_tables", block_tables, torch.int32, layout.n_seqs * layout.max_blocks, on), scale,
+            _heads("out", out, T, layout.head_dim, dt, on), _buf("lse", lse, torch.float32, T * hq, on),
+            _buf("workspace", workspace, torch.uint8, need, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
     return out
 
 

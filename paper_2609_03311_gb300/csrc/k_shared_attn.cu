@@ -71,10 +71,6 @@ struct Ring {
   }
 };
 
-__device__ __forceinline__ Plan plan_of(const SharedAttnArgs& a) {
-  return plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, a.lay.n_kv_heads, a.Hq / a.lay.n_kv_heads, a.max_tokens);
-}
-
 template <typename T>
 __host__ __device__ constexpr uint32_t type_bits() {  // operand formats of the instruction descriptor: 0 f16, 1 bf16
   return std::is_same_v<T, __half> ? 0u : (1u << 7 | 1u << 10);
@@ -138,12 +134,7 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
 struct Walk {
   const Segment* segs;
   int at, end;
-  __device__ __forceinline__ Walk(const SharedAttnArgs& a, int share) {
-    const Plan p = plan_of(a);
-    segs = p.segs;
-    at = p.first[share];
-    end = p.first[share + 1];
-  }
+  __device__ __forceinline__ Walk(const Plan& p, int2 work) : segs(p.segs), at(work.x), end(work.y) {}
   __device__ __forceinline__ bool next(Segment& s) {
     if (at >= end) return false;
     s = segs[at++];
@@ -186,16 +177,8 @@ struct PageCursor {
   Run run;
   int at, n_runs;
   const Run* runs;
-  __device__ __forceinline__ void seek(const Plan& p, const Segment& s, int page) {
-    runs = p.runs + s.run;
-    n_runs = s.n_runs;
-    int lo = 0, hi = n_runs - 1;
-    while (lo < hi) {  // the last run that begins at or before the page (runs without pages share their successor's place)
-      const int mid = (lo + hi + 1) >> 1;
-      if (runs[mid].off <= page) lo = mid; else hi = mid - 1;
-    }
-    at = lo;
-    run = runs[at];
+  __device__ __forceinline__ PageCursor(const Plan& p, const Segment& s) : at(s.run_at), n_runs(s.n_runs), runs(p.runs + s.run) {
+    run.row = s.run_row, run.off = s.run_off, run.pages = s.run_pages, run.keys = s.run_keys;
   }
   __device__ __forceinline__ void go(int page) {
     while (page >= run.off + run.pages && at + 1 < n_runs) run = runs[++at];
@@ -242,10 +225,9 @@ __device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)
 // One row alone by a warp, a key at a time, for rows whose products took in a value that they do not see; lane l holds
 // elements [E l, E l + E) of the head.
 template <typename T, int D>
-__device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, int lane) {
+__device__ __noinline__ void row_alone(const SharedAttnArgs& a, const Plan& plan, int t, int h, int lane) {
   constexpr int E = D / 32, W = E / 2;
   const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
-  const Plan plan = plan_of(a);
   const int4 rec = plan.rec[t];
   const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
   const float scale_log2 = a.scale * 1.4426950408889634f;
@@ -302,29 +284,24 @@ __device__ __noinline__ void row_alone(const SharedAttnArgs& a, int t, int h, in
 // of the item, and of each 8 columns two from 2 (lane % 4).  Bound by the copies of K and V: 8 KB a piece of head size 128,
 // 1.5 us of an eighth of an SM's part of the memory's rate, of which the products and the softmax take a third.
 template <typename T, int D>
-__device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint32_t s0, int wi, int share, int lane) {
+__device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int wi, int2 work, int lane) {
   using L = Smem<D>;
   constexpr int HALF = PIECE * 128, KV = L::HALVES * HALF;  // 64 elements a row; K or V of a piece
   constexpr int CHUNKS = D / 8;                             // 16-byte chunks of a row
   const uint32_t base = s0 + wi * L::F_STAGES * 2 * KV;
-  const Plan plan = plan_of(a);
   const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
   const float scale_log2 = a.scale * 1.4426950408889634f;
   const int quad = lane >> 2, in_quad = lane & 3;
-  Walk walk(a, share);
+  Walk walk(plan, work);
   Segment s;
   while (walk.next(s)) {
     // where the next 32 pieces lie: a lane a piece
     int row_at = 0, valid_at = 0;
     auto find = [&](uint32_t b) {
       if (b >= s.b1) return;
-      const Run* runs = plan.runs + s.run;
-      int lo = 0, hi = s.n_runs - 1;
-      while (lo < hi) {  // the last run that begins at or before the piece (runs without keys share their successor's place)
-        const int mid = (lo + hi + 1) >> 1;
-        if (runs[mid].off <= static_cast<int>(b)) lo = mid; else hi = mid - 1;
-      }
-      const Run run = runs[lo];
+      PageCursor cur(plan, s);
+      cur.go(b);
+      const Run& run = cur.run;
       const int key = (static_cast<int>(b) - run.off) * PIECE;
       int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
       if (block < 0 || block >= a.lay.n_blocks) {
@@ -467,7 +444,7 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint32_t s0, 
         while (odd) {
           const int from = __ffs(odd) - 1;
           odd &= ~(0xfu << (from & ~3));
-          row_alone<T, D>(a, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
+          row_alone<T, D>(a, plan, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
         }
       } else if (r < rows) {
         float2* ml = reinterpret_cast<float2*>(a.ws);
@@ -487,7 +464,7 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, uint32_t s0, 
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
     k_shared_attn(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                  const __grid_constant__ SharedAttnArgs a) {
+                  const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int gave_up;  // stands for the error word of the bounded waits: a CTA gives up alone
@@ -518,18 +495,17 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_trigger();
   pdl_wait();
   Segment s;
-  const Head head = *plan_of(a).head;
+  const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];  // beside the head: what begins the chain of loads
+  const Head head = *plan.head;
   const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, gridDim.x);
   const bool few = static_cast<int>(blockIdx.x) >= head.tile_ctas;
   if (!good && threadIdx.x == 0 && a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
 
   if (!good) {
   } else if (few) {
-    // the CTAs' first warps before their second ones: few shares are spread over many SMs
     if (warp >= 4) {
-      const int ctas = gridDim.x - head.tile_ctas;
       regs_many();
-      few_items<T, D>(a, s0, warp - 4, head.tile_ctas + 1 + (warp - 4) * ctas + static_cast<int>(blockIdx.x) - head.tile_ctas, lane);
+      few_items<T, D>(a, plan, s0, warp - 4, work, lane);
     } else {
       regs_few();
     }
@@ -538,9 +514,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     regs_few();
     const bool is_v = warp == 2;
     const CUtensorMap* map = is_v ? &tm_v : &tm_k;
-    Walk walk(a, blockIdx.x);
-    const Plan plan = plan_of(a);
-    const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
+    Walk walk(plan, work);
+      const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
     const uint32_t ring0 = s0 + (is_v ? L::OFF_V : L::OFF_K);
     const int page = a.lay.page, page_blk = BLOCK / page;
     const int pg = lane / L::HALVES, half = lane % L::HALVES;  // pages of a block: at most 8
@@ -548,8 +523,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     uint32_t armed = 0, parity = 0;
     bool ok = true;
     while (ok && walk.next(s)) {
-      PageCursor cur;
-      cur.seek(plan, s, s.b0 * page_blk + pg);
+      PageCursor cur(plan, s);
       for (uint32_t b = s.b0; b < s.b1; ++b) {
         const int first = b * page_blk, pages = min(page_blk, s.pages - first);
         const bool mine = pg < pages;
@@ -590,7 +564,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const bool one = elect_one();
     const uint32_t sQ = s0 + L::OFF_Q, sK = s0 + L::OFF_K, sV = s0 + L::OFF_V;
     const int page = a.lay.page, page_blk = BLOCK / page;
-    Walk walk(a, blockIdx.x);
+    Walk walk(plan, work);
     Groups groups;
     bool ok = true;
     auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
@@ -784,8 +758,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few();
     const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);  // where the rows of other tokens lie
-    const int* order = plan_of(a).order;
-    Walk walk(a, blockIdx.x);
+    const int* order = plan.order;
+    Walk walk(plan, work);
     Groups groups;
     uint32_t used = 0, par = 0, filled = 0;  // a bit a group
     bool ok = true;
@@ -802,7 +776,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (run) {
           first = tok[8 * lane];
 #pragma unroll
-          for (int i = 1; i < 8; ++i) run = run && tok[8 * lane + i] == first + i;
+          for (int i = 1; i < 8; ++i) run = run & (tok[8 * lane + i] == first + i);
         }
         const uint32_t runs = __ballot_sync(0xffffffffu, run);
         __syncwarp();
@@ -864,9 +838,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t lane_base = tmem + (static_cast<uint32_t>(quarter * 32) << 16);
     const uint32_t s_col = lane_base + S_COL + 128 * w, o_col = lane_base + O_COL + 128 * w;
     const float scale_log2 = a.scale * 1.4426950408889634f;
-    const int2* own_columns = plan_of(a).own;
-    const int* order = plan_of(a).order;
-    Walk walk(a, blockIdx.x);
+    const int2* own_columns = plan.own;
+    const int* order = plan.order;
+    Walk walk(plan, work);
     Groups groups;
     Ring rv;
     uint32_t s_par = 0, o_par = 0;
@@ -1052,7 +1026,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         while (odd) {
           const int from = __ffs(odd) - 1;
           odd &= odd - 1;
-          row_alone<T, D>(a, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
+          row_alone<T, D>(a, plan, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
         }
       } else {
         // ---- a partial result
@@ -1094,35 +1068,40 @@ __global__ void __launch_bounds__(THREADS, 1)
 // ------------------------------------------------------------------ joining the parts
 // A warp a row, JOIN_ROWS rows of an entry at a time.
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_constant__ SharedAttnArgs a, int n_ctas) {
+__global__ void __launch_bounds__(32 * JOIN_ROWS)
+    k_shared_join(const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan, int n_ctas) {
   constexpr int E = D / 32;
   const int lane = threadIdx.x & 31, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
-  const Plan plan = plan_of(a);
   const float2* ml = reinterpret_cast<const float2*>(a.ws);
   const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas));
   pdl_wait();
   pdl_trigger();
+  Piece piece = plan.join[blockIdx.x];  // there may be none, but there is room for it; read beside the head
   const Head head = *plan.head;
   if (!made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas)) return;
+#pragma unroll 1
   for (int j = blockIdx.x; j < head.n_join; j += gridDim.x) {
-    const int2 piece = plan.join[j];
-    const int f = piece.x, row = piece.y + (threadIdx.x >> 5);
-    const Item it = plan.items[f / Hkv];
-    if (row >= it.n_tok * G) continue;
-    const int t = plan.order[it.tok + row / G], h = f % Hkv * G + row % G;
+    if (j != static_cast<int>(blockIdx.x)) piece = plan.join[j];
+    const int row = piece.row + (threadIdx.x >> 5);
+    if (row >= piece.rows) continue;
+    const int t = plan.order[piece.tok + row / G], h = piece.h * G + row % G;
     float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = 0.f;
+    uint32_t parts = piece.parts, rows = piece.rows;
+    int64_t row0 = piece.part_row + static_cast<int64_t>(row);
     // the piece's own entry, then the few entry that has a row's own keys beside tiles
-    const int4 rec = plan.rec[t];
-    const bool beside = !(it.flags & ITEM_FEW) && rec.z >= 0;
-    for (int k = 0; k <= static_cast<int>(beside); ++k) {
-      const int e = k ? rec.z * Hkv + f % Hkv : f, place = k ? rec.w * G + h % G : row;
-      const Item x_it = k ? plan.items[rec.z] : it;
-      const uint32_t rows = x_it.n_tok * G;
-      const uint32_t share = x_it.flags & ITEM_FEW ? head.few_share : head.share;
-      const uint32_t parts = on_line(x_it, f % Hkv, G).segments(x_it.blocks, share) * copies_of(x_it, G);
-      const int64_t row0 = plan.part[e] + static_cast<int64_t>(place);
+#pragma unroll 1
+    for (int k = 0; k <= piece.beside; ++k) {
+      if (k) {
+        const int4 rec = plan.rec[t];
+        if (rec.z < 0) break;
+        const Item it = plan.items[rec.z];
+        parts = on_line(it, piece.h, G).segments(it.blocks, head.few_share);
+        rows = it.n_tok * G;
+        row0 = plan.part[rec.z * Hkv + piece.h] + static_cast<int64_t>(rec.w * G + h % G);
+      }
+#pragma unroll 1
       for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
         const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
         float top = x.x;
@@ -1165,7 +1144,7 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS) k_shared_join(const __grid_con
 #pragma unroll
     for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
     if (l == l && __any_sync(0xffffffffu, nan)) {
-      row_alone<T, D>(a, t, h, lane);
+      row_alone<T, D>(a, plan, t, h, lane);
       continue;
     }
     const float inv = inverse(l);
@@ -1181,6 +1160,7 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   const int n_ctas = num_sms < MAX_CTAS ? num_sms : MAX_CTAS;
   CUtensorMap tm_q, tm_k, tm_v;
   const int G = a.Hq / a.lay.n_kv_heads;
+  const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, a.lay.n_kv_heads, G, a.max_tokens);
   const uint64_t rows = static_cast<uint64_t>(a.lay.n_blocks) * a.lay.n_kv_heads * a.lay.page;
   const bool half = std::is_same_v<T, __half>;
   if (!make_tmap_16b_2d(&tm_k, a.k_pool, D, rows, D * 2, 64, a.lay.page, true, half) ||
@@ -1193,14 +1173,14 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   if (!args.q_boxes) tm_q = tm_k;
   cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q, tm_k, tm_v, args);
+  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q, tm_k, tm_v, args, plan);
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +
                          static_cast<int64_t>(a.max_tokens) * a.Hq / JOIN_ROWS;
   const int64_t held = 6 * static_cast<int64_t>(num_sms);
   return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>(pieces < held ? pieces : held)), 32 * JOIN_ROWS, 0, st, a,
-                          n_ctas);
+                          plan, n_ctas);
 }
 
 }  // namespace

@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
     }
     #pragma unroll 1
-    for (int c = threadIdx.x; c < SHARES; c += THREADS) p.first[c] = 0;
+    for (int c = threadIdx.x; c < MAX_CTAS * WORKERS; c += THREADS) p.work[c] = make_int2(0, 0);
     return;
   }
   #pragma unroll 1
@@ -553,8 +553,12 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     if (f < n_flat && f == first_few * Hkv) first_of[tile_ctas] = seg0;  // the end of tiles
     if (f < n_flat) p.part[f] = part_row;
     spread(pieces, [&](bool on, int src, int i) {
-      const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i;
-      if (on) p.join[piece] = make_int2(f_, i * JOIN_ROWS);
+      const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i, row0 = of_lane(part_row, src), n = of_lane(segs, src);
+      if (!on) return;
+      const int item = by_heads.of(f_);
+      const Item& it = items[item];
+      p.join[piece] = Piece{it.tok, i * JOIN_ROWS, it.n_tok * G, f_ - item * Hkv, static_cast<uint32_t>(row0),
+                            n * static_cast<int>(copies_of(it, G)), !(it.flags & (ITEM_FEW | ITEM_ALONE)), 0};
     });
     spread(segs, [&](bool on_, int src, int i) {
       const int f_ = of_lane(f, src), at = of_lane(seg0, src) + i, whole = of_lane(right_away, src), row0 = of_lane(part_row, src);
@@ -575,11 +579,19 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       sg.end0 = it.end0, sg.begin1 = it.begin1, sg.prefix_blocks = it.prefix_blocks;
       sg.flags = (two_tiles(it, G) ? SEG_TWO : 0u) | (of_few ? SEG_FEW : 0u) | (whole ? SEG_WHOLE : 0u);
       sg.part_row = static_cast<uint32_t>(row0) + i * copies_of(it, G) * it.n_tok * G;
+      const int page0 = sg.b0 * (of_few ? 1 : page_blk);
+      int lo = 0, hi = it.n_runs - 1;
+      while (lo < hi) {  // the last run that begins at or before the page (runs without pages share their successor's place)
+        const int mid = (lo + hi + 1) >> 1;
+        if (runs[it.run + mid].off <= page0) lo = mid; else hi = mid - 1;
+      }
+      const Run& run = runs[it.run + lo];
+      sg.run_at = lo, sg.run_row = run.row, sg.run_off = run.off, sg.run_pages = run.pages, sg.run_keys = run.keys;
       p.segs[at] = sg;
       atomicMin(&first_of[of_few ? tile_ctas + 1 + c : c], at);
     });
   }
-  // what the shares' kernel and the joining one read of items and runs
+  // what the attention's kernels read of items and runs
   if (in_shared & ITEMS_SHARED)
     #pragma unroll 1
     for (int i = threadIdx.x; i < n_items * static_cast<int>(sizeof(Item) / 16); i += THREADS)
@@ -613,8 +625,15 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       const int c = threadIdx.x * EACH + i;
-      if (c < SHARES) p.first[c] = min(low[i], rest);
+      if (c < SHARES) first_of[c] = min(low[i], rest);
     }
+  }
+  __syncthreads();
+  // the few items' shares are dealt to the CTAs' first warps, then to their second ones: few shares are spread over many SMs
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n_ctas * WORKERS; i += THREADS) {
+    const int cta = i / WORKERS, slot = cta < tile_ctas ? cta : tile_ctas + 1 + i % WORKERS * few_ctas + cta - tile_ctas;
+    p.work[i] = make_int2(first_of[slot], first_of[slot + 1]);
   }
   if (threadIdx.x == 0) {
     if (fits) {

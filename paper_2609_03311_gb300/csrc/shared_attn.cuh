@@ -67,7 +67,8 @@ enum : uint32_t {
   ITEM_FEW = 1,    // a few item
   ITEM_ALONE = 2,  // its tokens are in no other item
 };
-// What a CTA has of a flat entry, with what its warps need to know of the item.
+// What a CTA has of a flat entry, with what its warps need to know of the item and of the run that its first page lies in: a
+// load each from here to the block table and to the rows.
 struct alignas(16) Segment {
   int f, h;           // flat entry, kv head
   uint32_t b0, b1;    // its blocks here
@@ -76,12 +77,23 @@ struct alignas(16) Segment {
   uint32_t end0, begin1, prefix_blocks;
   uint32_t flags;
   uint32_t part_row;  // first row of its partial results
-  int pad;
+  int run_at;         // of the item's: the run of its first page (few items: piece), and what is needed of it
+  int run_row, run_off, run_pages, run_keys;
 };
 enum : uint32_t {
   SEG_TWO = 1,    // two tiles
   SEG_FEW = 2,
   SEG_WHOLE = 4,  // gives its rows' results right away
+};
+// Up to JOIN_ROWS rows of an entry that are to be added up from partial results.
+struct alignas(16) Piece {
+  int tok;            // of the entry's item
+  int row, rows;      // the first of them, and all of the item's
+  int h;              // kv head
+  uint32_t part_row;  // of the item's first row
+  int parts;          // an item's rows after another
+  int beside;         // the rows' own keys may be in a few item
+  int pad;
 };
 struct alignas(16) Head {
   int tokens, n_items, n_flat, n_join;
@@ -97,13 +109,13 @@ __host__ __device__ inline bool made_for(const Head& h, const dopr_cache_layout&
 constexpr int SHARES = MAX_CTAS * WORKERS + 2;  // at most: a CTA has one or WORKERS
 struct Plan {
   Head* head;
-  int* first;      // [SHARES] the shares' first segments: the tiles' CTAs' and the end, the few items' warps' and the end
+  int2* work;      // [CTA][WORKERS] segments of a CTA of tiles (WORKERS times), of a few items' CTA's warps: from and to
   Segment* segs;   // in the CTAs' order
   int4* rec;       // [tokens] item of tiles and place in it, few item and place in it (-1: none)
   Item* items;
   Run* runs;
   uint32_t* part;  // [flat entry] first row of its partial results
-  int2* join;      // flat entry, first of up to JOIN_ROWS rows that are to be added up from partial results
+  Piece* join;
   int* order;      // [2 * tokens] the items' tokens
   int2* own;       // [2 * tokens, in that order] columns of its own keys, from and to
   int* scratch;    // plan_scratch_ints(n_seqs), of the plan kernel where its shared memory does not hold them
@@ -137,13 +149,13 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   const int64_t items = max_items(n_seqs, G, max_tokens);
   Plan p;
   p.head = static_cast<Head*>(take(sizeof(Head)));
-  p.first = static_cast<int*>(take(SHARES * 4));
+  p.work = static_cast<int2*>(take(MAX_CTAS * WORKERS * 8));
   p.rec = static_cast<int4*>(take(16 * static_cast<int64_t>(max_tokens)));
   p.segs = static_cast<Segment*>(take((items * n_kv_heads + SHARES) * static_cast<int64_t>(sizeof(Segment))));
   p.items = static_cast<Item*>(take(items * static_cast<int64_t>(sizeof(Item))));
   p.runs = static_cast<Run*>(take(max_runs(n_seqs, G, max_tokens) * static_cast<int64_t>(sizeof(Run))));
   p.part = static_cast<uint32_t*>(take(4 * items * n_kv_heads));
-  p.join = static_cast<int2*>(take(8 * max_pieces(n_seqs, n_kv_heads, G, max_tokens)));
+  p.join = static_cast<Piece*>(take(max_pieces(n_seqs, n_kv_heads, G, max_tokens) * static_cast<int64_t>(sizeof(Piece))));
   p.order = static_cast<int*>(take(8 * static_cast<int64_t>(max_tokens)));
   p.own = static_cast<int2*>(take(16 * static_cast<int64_t>(max_tokens)));
   p.scratch = static_cast<int*>(take(4 * plan_scratch_ints(n_seqs)));

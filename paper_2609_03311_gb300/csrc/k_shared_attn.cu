@@ -130,6 +130,15 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 }
+// What the chains of loads at the start run through, brought into L2 while the kernel before ends: it may still write there,
+// and L2 shows what it wrote.  A line a thread of the grid; of larger calls, whose work is long, a part.
+__device__ __forceinline__ void prefetch_l2(const SharedAttnArgs& a, const Plan& plan) {
+  const int64_t at = (static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x) * 128;
+  const char* from = static_cast<const char*>(a.plan);
+  if (at < reinterpret_cast<const char*>(plan.scratch) - from) asm volatile("prefetch.global.L2 [%0];" ::"l"(from + at));
+  if (at < static_cast<int64_t>(a.lay.n_seqs) * a.lay.max_blocks * 4)
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(reinterpret_cast<const char*>(a.tables) + at));
+}
 // One segment after another of a share: of tiles a CTA's, of few items a warp's.
 struct Walk {
   const Segment* segs;
@@ -493,6 +502,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_trigger();
+  prefetch_l2(a, plan);
   pdl_wait();
   Segment s;
   const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];  // beside the head: what begins the chain of loads

@@ -488,7 +488,7 @@ struct SharedAttnArgs {
   const void* plan;
   const void* q;
   int64_t q_tok, q_head;
-  bool q_boxes;  // set by the launcher: eight tokens of Q that follow one another come by TMA
+  bool q_boxes;  // set by the launcher: Q comes by TMA
   const void *k_pool, *v_pool;
   const int32_t* tables;
   float scale;

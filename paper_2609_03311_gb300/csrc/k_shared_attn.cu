@@ -54,7 +54,7 @@ struct Smem {
   static_assert(WORKERS * F_STAGES * 2 * HALVES * PIECE * 128 <= OFF_ROW, "the few items' pieces");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
-                       O_FULL = P_FULL + 2, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
+                       O_FULL = P_FULL + 4, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
   static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
   static_assert(V_STAGES * 8 <= 64, "a byte a page");
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
@@ -472,7 +472,7 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
 
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_shared_attn(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+    k_shared_attn(const __grid_constant__ CUtensorMap tm_q8, const __grid_constant__ CUtensorMap tm_q1, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -487,9 +487,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (threadIdx.x == 0) {
     gave_up = 0;
-    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 2 ? 4 : 1);
+    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 4 ? 4 : 1);
     fence_mbar_init();
-    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_q8);
+    tma_prefetch_desc(&tm_q1);
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
@@ -598,7 +599,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       oldest ^= 1u;
       --n_pend;
       if (!x.there && !wait(L::V_FULL + x.stage, x.phase)) return;
-      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
+      if (!wait(L::P_FULL + 2 + w, p_par >> w & 1u) || !wait(L::P_FULL + w, p_par >> w & 1u)) return;
       p_par ^= 1u << w;
       tc_fence_after();
       const uint64_t vd = v_desc0 + x.stage * (L::TILE_BYTES / 16);
@@ -657,15 +658,21 @@ __global__ void __launch_bounds__(THREADS, 1)
     // so what can be found out about the next step is, before the commits.
     bool v_there = false;
     auto step = [&](uint32_t w, int v_stage, bool acc, int k_stage, bool k_there, uint32_t k_phase, bool frees) {
-      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
-      p_par ^= 1u << w;
+      if (!wait(L::P_FULL + 2 + w, p_par >> w & 1u)) return;
       tc_fence_after();
       const uint32_t o = tmem + O_COL + 128 * w, sd = tmem + S_COL + 128 * w;
       const uint64_t vd = v_desc0 + v_stage * (L::TILE_BYTES / 16), kd = k_desc0 + k_stage * (L::TILE_BYTES / 16),
                      qd = q_desc0 + w * (L::TILE_BYTES / 16);
       if (one) {
 #pragma unroll
-        for (int k = 0; k < BLOCK / 16; ++k) umma_f16_ts(o, sd + (P_COL - S_COL) + 8 * k, vd + k * (2048 / 16), idesc_o, k > 0 || acc);
+        for (int k = 4; k < 8; ++k) umma_f16_ts(o, sd + (P_COL - S_COL) + 8 * k, vd + k * (2048 / 16), idesc_o, k > 4 || acc);
+      }
+      if (!wait(L::P_FULL + w, p_par >> w & 1u)) return;
+      p_par ^= 1u << w;
+      tc_fence_after();
+      if (one) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) umma_f16_ts(o, sd + (P_COL - S_COL) + 8 * k, vd + k * (2048 / 16), idesc_o, true);
       }
       if (!k_there) {
         if (!wait(L::K_FULL + k_stage, k_phase)) return;
@@ -768,7 +775,6 @@ __global__ void __launch_bounds__(THREADS, 1)
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few();
     const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);  // where the rows of other tokens lie
-    const int* order = plan.order;
     Walk walk(plan, work);
     Groups groups;
     uint32_t used = 0, par = 0, filled = 0;  // a bit a group
@@ -780,7 +786,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (!(takes >> w & 1u)) continue;
         const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0), rows = n * G;
         // tokens 8 i .. 8 i + 7 of the tile, a lane an i: whether they follow one another
-        const int* tok = order + s.tok + t0;
+        const int* tok = plan.order + s.tok + t0;
         int first = 0;
         bool run = a.q_boxes && 8 * lane + 8 <= n;
         if (run) {
@@ -789,13 +795,10 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int i = 1; i < 8; ++i) run = run & (tok[8 * lane + i] == first + i);
         }
         const uint32_t runs = __ballot_sync(0xffffffffu, run);
-        __syncwarp();
-        const bool others = __popc(runs) * 8 < n;
-        for (int r = lane; others && r < rows; r += 32) {
+        for (int r = lane; !a.q_boxes && r < rows; r += 32) {
           const int i = r / G;
-          row[r] = runs >> (i / 8) & 1u ? nullptr
-                                        : reinterpret_cast<const uint4*>(q + static_cast<int64_t>(tok[i]) * a.q_tok +
-                                                                         static_cast<int64_t>(s.h * G + r - i * G) * a.q_head);
+          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(tok[i]) * a.q_tok +
+                                                  static_cast<int64_t>(s.h * G + r - i * G) * a.q_head);
         }
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
@@ -804,29 +807,33 @@ __global__ void __launch_bounds__(THREADS, 1)
         }
         if (used >> w & 1u) par ^= 1u << w;
         used |= 1u << w;
-        const uint32_t dst = s0 + L::OFF_Q + w * L::TILE_BYTES, bytes = __popc(runs) * 8 * G * 128 * L::HALVES;
-        if (lane == 0 && bytes > 0) mbar_expect_tx(bar(L::Q_FULL + w), bytes);
-        __syncwarp();
-        if (run)
+        const uint32_t dst = s0 + L::OFF_Q + w * L::TILE_BYTES;
+        if (a.q_boxes) {
+          if (lane == 0) mbar_expect_tx(bar(L::Q_FULL + w), rows * 128 * L::HALVES);
+          __syncwarp();
+          if (run)
 #pragma unroll
-          for (int h = 0; h < L::HALVES; ++h)
-            tma_load_3d(dst + h * HALF_BYTES + lane * 8 * G * 128, &tm_q, bar(L::Q_FULL + w), 64 * h, s.h * G, first);
-        __syncwarp();
-        if (others) {
+            for (int h = 0; h < L::HALVES; ++h)
+              tma_load_3d(dst + h * HALF_BYTES + lane * 8 * G * 128, &tm_q8, bar(L::Q_FULL + w), 64 * h, s.h * G, first);
+          // the others one by one (the swizzle goes by the address, so a box may begin at any row)
+#pragma unroll 1
+          for (int i = lane; i < n; i += 32) {
+            if (runs >> (i / 8) & 1u) continue;
+            const int t = tok[i];
+#pragma unroll
+            for (int h = 0; h < L::HALVES; ++h)
+              tma_load_3d(dst + h * HALF_BYTES + i * G * 128, &tm_q1, bar(L::Q_FULL + w), 64 * h, s.h * G, t);
+          }
+          __syncwarp();
+        } else {
           // a lane a 16-byte piece of the row, 32 / CHUNKS rows at once
           constexpr int CHUNKS = D / 8, STEP = 32 / CHUNKS;
           const int c = lane % CHUNKS;
           for (int r0 = lane / CHUNKS; r0 < rows; r0 += 8 * STEP) {
-            const uint4* src[8];  // eight addresses before the first copy: a copy is not waited for, an address is
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int r = r0 + i * STEP;
-              src[i] = r < rows ? row[r] : nullptr;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = r0 + i * STEP;
-              if (src[i]) cp_async16(dst + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), src[i] + c, true);
+              if (r < rows) cp_async16(dst + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), row[r] + c, true);
             }
           }
           cp_async_commit();
@@ -855,26 +862,28 @@ __global__ void __launch_bounds__(THREADS, 1)
     Ring rv;
     uint32_t s_par = 0, o_par = 0;
     bool ok = true;
-    // P of a block is there, and (the first group that takes it) rows of V past a page's keys count as zero
-    auto done_with = [&](int stage, uint32_t phase, int cols, bool ragged) {
-      if (ragged) {
-        if (!mbar_wait_warp(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
-        const int page = a.lay.page;
-        for (int pg = 0; pg * page < cols; ++pg) {
-          const int from = smem[L::OFF_KEYS + stage * 8 + pg];
-          for (int i = r; i < (page - from) * 8 * L::HALVES; i += 128) {
-            const int at = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
-            *reinterpret_cast<uint4*>(smem + L::OFF_V + stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + at * 128 + (c & 7) * 16) =
-                uint4{0, 0, 0, 0};
-          }
+    // (the first group that takes a block) rows of V past a page's keys count as zero: before any of P is given
+    auto ready_v = [&](int stage, uint32_t phase, int cols) {
+      if (!mbar_wait_warp(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
+      const int page = a.lay.page;
+      for (int pg = 0; pg * page < cols; ++pg) {
+        const int from = smem[L::OFF_KEYS + stage * 8 + pg];
+        for (int i = r; i < (page - from) * 8 * L::HALVES; i += 128) {
+          const int at = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
+          *reinterpret_cast<uint4*>(smem + L::OFF_V + stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + at * 128 + (c & 7) * 16) =
+              uint4{0, 0, 0, 0};
         }
-        fence_proxy_async_shared();
       }
+      fence_proxy_async_shared();
+      return true;
+    };
+    // P is given in halves, the upper first: the products with it run while the other is made.  A barrier each: a warp may
+    // give its second half before another gives its first.
+    auto give = [&](int half) {
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(L::P_FULL + w));
-      return true;
+      if (lane == 0) mbar_arrive(bar(L::P_FULL + 2 * half + w));
     };
     while (ok && walk.next(s)) {
       const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0);
@@ -910,7 +919,9 @@ __global__ void __launch_bounds__(THREADS, 1)
           const uint32_t zero[16] = {};
           if (any)
             for (int c = 0; c < 64; c += 16) tmem_st16(s_col + 64 + c, zero);
-          if (!(ok = done_with(v_stage, v_phase, cols, ragged))) break;
+          if (ragged && !(ok = ready_v(v_stage, v_phase, cols))) break;
+          give(1);
+          give(0);
           continue;
         }
         uint32_t va[32], vb[32], pk[16];
@@ -978,13 +989,15 @@ __global__ void __launch_bounds__(THREADS, 1)
         tmem_ld_wait_for(vb);
         tmem_ld32(s_col, va);
         tmem_st16(s_col + 96, pk);
+        if (ragged && !(ok = ready_v(v_stage, v_phase, cols))) break;
+        give(1);
         exp_pack<T>(vb, scale_log2, base, sum, pk);
         tmem_ld_wait_for(va);
         tmem_st16(s_col + 80, pk);
         exp_pack<T>(va, scale_log2, base, sum, pk);
         tmem_st16(s_col + 64, pk);
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (!(ok = done_with(v_stage, v_phase, cols, ragged))) break;
+        give(0);
       }
       if (!ok) break;
       if (done > 0) {
@@ -1168,7 +1181,7 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS)
 template <typename T, int D>
 cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   const int n_ctas = num_sms < MAX_CTAS ? num_sms : MAX_CTAS;
-  CUtensorMap tm_q, tm_k, tm_v;
+  CUtensorMap tm_q8, tm_q1, tm_k, tm_v;
   const int G = a.Hq / a.lay.n_kv_heads;
   const Plan plan = plan_view(const_cast<void*>(a.plan), a.lay.n_seqs, a.lay.n_kv_heads, G, a.max_tokens);
   const uint64_t rows = static_cast<uint64_t>(a.lay.n_blocks) * a.lay.n_kv_heads * a.lay.page;
@@ -1176,14 +1189,16 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   if (!make_tmap_16b_2d(&tm_k, a.k_pool, D, rows, D * 2, 64, a.lay.page, true, half) ||
       !make_tmap_16b_2d(&tm_v, a.v_pool, D, rows, D * 2, 64, a.lay.page, true, half))
     return cudaErrorInvalidValue;
-  // Q of eight tokens at once, where a tile holds as many; views that a tensor map does not take (one row for all tokens)
-  // are gathered
+  // Q by boxes of eight tokens that follow one another and of one; views that a tensor map does not take (one row for all
+  // tokens) are gathered
   SharedAttnArgs args = a;
-  args.q_boxes = tokens_a_tile(G) >= 8 && make_tmap_rows_of_heads(&tm_q, a.q, D, a.Hq, a.max_tokens, a.q_head, a.q_tok, G, 8, half);
-  if (!args.q_boxes) tm_q = tm_k;
+  args.q_boxes = make_tmap_rows_of_heads(&tm_q1, a.q, D, a.Hq, a.max_tokens, a.q_head, a.q_tok, G, 1, half);
+  if (!args.q_boxes) tm_q1 = tm_k;
+  if (!args.q_boxes || tokens_a_tile(G) < 8) tm_q8 = tm_q1;
+  else if (!make_tmap_rows_of_heads(&tm_q8, a.q, D, a.Hq, a.max_tokens, a.q_head, a.q_tok, G, 8, half)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q, tm_k, tm_v, args, plan);
+  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q8, tm_q1, tm_k, tm_v, args, plan);
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +

@@ -1120,7 +1120,7 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS)
         const int4 rec = plan.rec[t];
         if (rec.z < 0) break;
         const Item it = plan.items[rec.z];
-        parts = on_line(it, piece.h, G).segments(it.blocks, head.few_share);
+        parts = on_line(it, piece.h).segments(it.blocks, head.few_share);
         rows = it.n_tok * G;
         row0 = plan.part[rec.z * Hkv + piece.h] + static_cast<int64_t>(rec.w * G + h % G);
       }

@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   #pragma unroll 1
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    const unsigned long long v = i < n_items ? static_cast<unsigned long long>(Hkv) * length_of(items[i], G) : 0;
+    const unsigned long long v = i < n_items ? static_cast<unsigned long long>(Hkv) * length_of(items[i]) : 0;
     unsigned long long inc = v;
     if (warp * 32 < n_items - i0) {
 #pragma unroll
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   }
   const uint32_t few_ctas = n_ctas - tile_ctas;
   // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up
-  uint32_t share = block_length(false), few_share = MIN_FEW_SHARE;
+  uint32_t share = OTHER_BLOCK, few_share = MIN_FEW_SHARE;
   if (fits && tile_ctas > 0) share = max(share, (static_cast<uint32_t>(tiles_line) + tile_ctas - 1) / tile_ctas);
   if (fits && few_ctas > 0) few_share = max(few_share, (static_cast<uint32_t>(few_line) + few_ctas * WORKERS - 1) / (few_ctas * WORKERS));
   const Divisor by_share(share), by_few_share(few_share);
@@ -532,10 +532,10 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     if (f < n_flat) {
       const int i = by_heads.of(f);
       const Item& it = items[i];
-      const OnLine on = on_line(it, f - i * Hkv, G);
+      const OnLine on = on_line(it, f - i * Hkv);
       const Divisor& by = it.flags & ITEM_FEW ? by_few_share : by_share;
       cta0 = by.of(on.begin);
-      if (it.blocks > 0) segs = by.of(on.begin + (it.blocks - 1) * on.length) - cta0 + 1;
+      if (it.blocks > 0) segs = by.of(on.begin_of(it.blocks - 1)) - cta0 + 1;
       right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
       if (!right_away) {
         rows = segs * it.n_tok * G * copies_of(it, G);
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       if (!on_) return;
       const int item = by_heads.of(f_), h = f_ - item * Hkv;
       const Item& it = items[item];
-      const OnLine on = on_line(it, h, G);
+      const OnLine on = on_line(it, h);
       const bool of_few = it.flags & ITEM_FEW;
       const uint32_t entry_share = of_few ? few_share : share;
       Segment sg{};

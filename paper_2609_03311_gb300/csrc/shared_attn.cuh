@@ -15,7 +15,7 @@
 // Of few items a block is a piece of 16 columns, and a run's last piece is its last one with keys.
 //
 // An item and a kv head are a flat entry.  The flat entries of each kind lie one after another on a line, on which an entry
-// takes a length for its start and end and one for each block.  Some CTAs take the tiles, the others the few items; a CTA
+// takes a length for its start and end and one for each block, longer where rows see a part of it.  Some CTAs take the tiles, the others the few items; a CTA
 // of the former, a warp of the latter takes the blocks that begin in an equal share of its line.  What it has of an entry is
 // a segment; it leaves partial softmax results (maximum, sum, weighted values), which
 // the joining kernel adds up by row, unless they are all that its rows have: then it gives the rows' results right away.
@@ -34,12 +34,12 @@ constexpr int PIECE = 16;   // of few items
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
 constexpr int WORKERS = 8;  // warps of a CTA that take few items
-// Lengths on the lines.  Tiles, about 0.3 us each: a block; an entry's start and end.  Few items, about 1.5 us of a warp each
-// (a CTA's eight share the SM's part of the memory's rate): a piece; an entry's start and end.  Measured over ragged documents
-// / queries of 16 documents: an entry of tiles at 10 and a block of one tile at 4, 69 / 192 us; 22 and 6, 61 / 180; a length of
-// few items at 3, 4, 5 of tiles, 59.2 / 58.8 / 61.6 us for the former.
-__host__ __device__ constexpr uint32_t block_length(bool few) { return few ? 1 : 6; }
-__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 26; }
+// Lengths on the lines.  Tiles, about 480 clocks each: a block of keys that all rows see, another block (masked, and often of
+// one tile), an entry's start and end.  Few items, about 1.5 us of a warp each (a CTA's eight share the SM's part of the
+// memory's rate): a piece; an entry's start and end.  Fitted to the CTAs' times: 2,880 clocks a whole block, 5,200 to 6,900
+// another, 10,200 to 12,200 an entry.
+constexpr uint32_t WHOLE_BLOCK = 6, OTHER_BLOCK = 12, FEW_PIECE = 1;
+__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 20; }
 constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
 constexpr uint32_t MIN_FEW_SHARE = 6;
 
@@ -175,25 +175,36 @@ __host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int
 
 __host__ __device__ inline bool two_tiles(const Item& it, int G) { return !(it.flags & ITEM_FEW) && it.n_tok > tokens_a_tile(G); }
 __host__ __device__ inline uint32_t copies_of(const Item& it, int G) { return (it.flags & ITEM_FEW) || two_tiles(it, G) ? 1 : 2; }
-// The blocks of kv head h's entry on the line: where the first begins and the length of one.
+// The blocks of kv head h's entry on the line: where the first begins, how many are whole, and where those end.
 struct OnLine {
-  uint32_t begin, length;
+  uint32_t begin, whole, whole_end;
+  bool few;
+  __host__ __device__ uint32_t begin_of(uint32_t b) const {
+    if (few) return begin + b * FEW_PIECE;
+    return b <= whole ? begin + b * WHOLE_BLOCK : whole_end + (b - whole) * OTHER_BLOCK;
+  }
   // first block that begins at or behind a place on the line
   __host__ __device__ uint32_t block_from(uint32_t at, uint32_t blocks) const {
     if (at <= begin) return 0;
-    const uint32_t b = length == 1 ? at - begin : (at - begin + block_length(false) - 1) / block_length(false);
+    const uint32_t b = few ? (at - begin + FEW_PIECE - 1) / FEW_PIECE
+                       : at <= whole_end ? (at - begin + WHOLE_BLOCK - 1) / WHOLE_BLOCK
+                                         : whole + (at - whole_end + OTHER_BLOCK - 1) / OTHER_BLOCK;
     return b < blocks ? b : blocks;
   }
-  __host__ __device__ uint32_t cta_of(uint32_t block, uint32_t share) const { return (begin + block * length) / share; }
+  __host__ __device__ uint32_t cta_of(uint32_t block, uint32_t share) const { return begin_of(block) / share; }
   __host__ __device__ uint32_t segments(uint32_t blocks, uint32_t share) const {
     return blocks > 0 ? cta_of(blocks - 1, share) - cta_of(0, share) + 1 : 0;
   }
 };
-__host__ __device__ inline uint32_t length_of(const Item& it, int G) {
-  return it.blocks > 0 ? entry_length(it.flags & ITEM_FEW) + it.blocks * block_length(it.flags & ITEM_FEW) : 0;
+__host__ __device__ inline OnLine blocks_from(const Item& it, uint32_t begin) {
+  const uint32_t all = it.prefix_keys / BLOCK, whole = all < it.blocks ? all : it.blocks;
+  return OnLine{begin, whole, begin + whole * WHOLE_BLOCK, (it.flags & ITEM_FEW) != 0};
 }
-__host__ __device__ inline OnLine on_line(const Item& it, int h, int G) {
-  return OnLine{it.start + h * length_of(it, G) + entry_length(it.flags & ITEM_FEW), block_length(it.flags & ITEM_FEW)};
+__host__ __device__ inline uint32_t length_of(const Item& it) {
+  return it.blocks > 0 ? blocks_from(it, entry_length(it.flags & ITEM_FEW)).begin_of(it.blocks) : 0;
+}
+__host__ __device__ inline OnLine on_line(const Item& it, int h) {
+  return blocks_from(it, it.start + h * length_of(it) + entry_length(it.flags & ITEM_FEW));
 }
 
 }  // namespace shared_attn

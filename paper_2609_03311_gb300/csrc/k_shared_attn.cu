@@ -36,6 +36,7 @@ constexpr int THREADS = 128 + 2 * 128;
 // group w: S at S_COL + 128 w, P over its upper half, O at O_COL + 128 w
 constexpr uint32_t TMEM_COLS = 512, S_COL = 0, P_COL = 64, O_COL = 256;
 constexpr float RESCALE_LOG2 = 8.f;
+constexpr int JOIN_CTAS = 4;  // of the joining kernel on an SM
 constexpr int HALF_BYTES = 128 * 128;  // 128 rows of 64 16-bit elements
 
 template <int D>
@@ -502,9 +503,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_trigger();
   prefetch_l2(a, plan);
   pdl_wait();
+  pdl_trigger();  // behind the wait: the joining kernel reads the plan before its own (and finds no room earlier anyway)
   Segment s;
   const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];  // beside the head: what begins the chain of loads
   const Head head = *plan.head;
@@ -1089,44 +1090,66 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // ------------------------------------------------------------------ joining the parts
-// A warp a row, JOIN_ROWS rows of an entry at a time.
+// A warp a row, JOIN_ROWS rows of an entry at a time.  Bound by latency where few rows have many parts, so what the plan says
+// of a CTA's first piece is read while the attention ends (it was complete before that began), the first values are asked for
+// beside the maxima and sums, and eight parts are on their way at once.
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * JOIN_ROWS)
+__global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
     k_shared_join(const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan, int n_ctas) {
-  constexpr int E = D / 32;
+  constexpr int E = D / 32, AHEAD = 4;
   const int lane = threadIdx.x & 31, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv;
   const float2* ml = reinterpret_cast<const float2*>(a.ws);
-  const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas));
-  pdl_wait();
-  pdl_trigger();
-  Piece piece = plan.join[blockIdx.x];  // there may be none, but there is room for it; read beside the head
+  const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas)) + lane * E;
   const Head head = *plan.head;
-  if (!made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas)) return;
+  const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas);
+  bool waited = false;
+  auto wait_once = [&] {
+    if (!waited) pdl_wait(), pdl_trigger();
+    waited = true;
+  };
+  Piece next{};
+  if (good && static_cast<int>(blockIdx.x) < head.n_join) next = plan.join[blockIdx.x];
 #pragma unroll 1
-  for (int j = blockIdx.x; j < head.n_join; j += gridDim.x) {
-    if (j != static_cast<int>(blockIdx.x)) piece = plan.join[j];
+  for (int j = blockIdx.x; good && j < head.n_join; j += gridDim.x) {
+    const Piece piece = next;
+    if (j + static_cast<int>(gridDim.x) < head.n_join) next = plan.join[j + gridDim.x];
     const int row = piece.row + (threadIdx.x >> 5);
     if (row >= piece.rows) continue;
     const int t = plan.order[piece.tok + row / G], h = piece.h * G + row % G;
     float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = 0.f;
-    uint32_t parts = piece.parts, rows = piece.rows;
-    int64_t row0 = piece.part_row + static_cast<int64_t>(row);
     // the piece's own entry, then the few entry that has a row's own keys beside tiles
-#pragma unroll 1
-    for (int k = 0; k <= piece.beside; ++k) {
-      if (k) {
-        const int4 rec = plan.rec[t];
-        if (rec.z < 0) break;
+    uint32_t parts = piece.parts, rows = piece.rows, beside_parts = 0, beside_rows = 0;
+    int64_t row0 = piece.part_row + static_cast<int64_t>(row), beside_row0 = 0;
+    if (piece.beside) {
+      const int4 rec = plan.rec[t];
+      if (rec.z >= 0) {
         const Item it = plan.items[rec.z];
-        parts = on_line(it, piece.h).segments(it.blocks, head.few_share);
-        rows = it.n_tok * G;
-        row0 = plan.part[rec.z * Hkv + piece.h] + static_cast<int64_t>(rec.w * G + h % G);
+        beside_parts = on_line(it, piece.h).segments(it.blocks, head.few_share);
+        beside_rows = it.n_tok * G;
+        beside_row0 = plan.part[rec.z * Hkv + piece.h] + static_cast<int64_t>(rec.w * G + h % G);
       }
+    }
+    wait_once();
+#pragma unroll 1
+    for (int k = 0; k < (beside_parts > 0 ? 2 : 1); ++k) {
+      if (k) parts = beside_parts, rows = beside_rows, row0 = beside_row0;
 #pragma unroll 1
       for (uint32_t p0 = 0; p0 < parts; p0 += 32) {
-        const float2 x = p0 + lane < parts ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
+        const uint32_t n = min(32u, parts - p0);
+        float v[AHEAD][E];
+        auto load = [&](uint32_t from) {
+#pragma unroll
+          for (uint32_t i = 0; i < AHEAD; ++i) {
+            if (from + i >= n) continue;
+            const float* src = part_o + (row0 + static_cast<int64_t>(p0 + from + i) * rows) * D;
+            if constexpr (E == 4) *reinterpret_cast<float4*>(v[i]) = *reinterpret_cast<const float4*>(src);
+            else *reinterpret_cast<float2*>(v[i]) = *reinterpret_cast<const float2*>(src);
+          }
+        };
+        const float2 x = lane < n ? ml[row0 + static_cast<int64_t>(p0 + lane) * rows] : make_float2(-INFINITY, 0.f);
+        load(0);
         float top = x.x;
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -1137,28 +1160,19 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS)
         m = top;
 #pragma unroll
         for (int i = 0; i < E; ++i) o[i] *= old;
-        // parts with no block, or nothing that the row sees, left no values; four at a time on their way
-        unsigned todo = __ballot_sync(0xffffffffu, x.y != 0.f);
-        while (todo) {
-          float wgt[4], v[4][E];
+        // parts with no block, or nothing that the row sees, left no values
+        const unsigned there = __ballot_sync(0xffffffffu, x.y != 0.f);
+#pragma unroll 1
+        for (uint32_t from = 0; from < n; from += AHEAD) {
+          if (from > 0) load(from);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int p = todo ? __ffs(todo) - 1 : -1;
-            todo &= todo - 1;
-            wgt[k] = __shfl_sync(0xffffffffu, mine, p < 0 ? 0 : p);
-            if (p < 0) wgt[k] = 0.f;
-            const float* src = part_o + (row0 + static_cast<int64_t>(p0 + (p < 0 ? 0 : p)) * rows) * D + lane * E;
+          for (uint32_t i = 0; i < AHEAD; ++i) {
+            const float wgt = __shfl_sync(0xffffffffu, mine, (from + i) & 31);
+            if (from + i < n && (there >> (from + i) & 1u)) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[k][i] = 0.f;
-            if (p >= 0) {
-              if constexpr (E == 4) *reinterpret_cast<float4*>(v[k]) = *reinterpret_cast<const float4*>(src);
-              else *reinterpret_cast<float2*>(v[k]) = *reinterpret_cast<const float2*>(src);
+              for (int e = 0; e < E; ++e) o[e] += wgt * v[i][e];
             }
           }
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int i = 0; i < E; ++i) o[i] += wgt[k] * v[k][i];
         }
       }
     }
@@ -1176,6 +1190,7 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS)
     for (int i = 0; i < E / 2; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
     if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
   }
+  wait_once();
 }
 
 template <typename T, int D>
@@ -1203,7 +1218,7 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +
                          static_cast<int64_t>(a.max_tokens) * a.Hq / JOIN_ROWS;
-  const int64_t held = 6 * static_cast<int64_t>(num_sms);
+  const int64_t held = JOIN_CTAS * static_cast<int64_t>(num_sms);
   return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>(pieces < held ? pieces : held)), 32 * JOIN_ROWS, 0, st, a,
                           plan, n_ctas);
 }

@@ -15,8 +15,9 @@
 namespace dopr {
 namespace {
 
-constexpr int SUM_THREADS = 1024, FILL_THREADS = 256;
+constexpr int FILL_THREADS = 256;
 constexpr int FILL_HERE = 4096;
+constexpr int FEW_THREADS = 128, MANY_THREADS = 1024;  // of the CTA that takes the sums
 
 // Workspace header: whether the call goes ahead, the stack's height once released pages are back, new tokens.
 enum { WS_OK = 0, WS_TOP = 1, WS_TOKENS = 2 };
@@ -36,6 +37,7 @@ __device__ __forceinline__ Sums shfl_up(Sums v, int o) {
   return v;
 }
 // Exclusive sums over the block's threads in order; the block's totals through `total`.
+template <int WARPS>
 __device__ Sums block_exclusive(Sums v, Sums* warp_sum, Sums& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Sums inc = v;
@@ -47,18 +49,28 @@ __device__ Sums block_exclusive(Sums v, Sums* warp_sum, Sums& total) {
   __syncthreads();  // the last use of warp_sum is over
   if (lane == 31) warp_sum[warp] = inc;
   __syncthreads();
-  if (warp == 0) {
-    Sums w = warp_sum[lane];
+  Sums base{0, 0};
+  if constexpr (WARPS <= 8) {
+    total = Sums{0, 0};
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const Sums u = shfl_up(w, o);
-      if (lane >= o) w.tokens += u.tokens, w.pages += u.pages;
+    for (int w = 0; w < WARPS; ++w) {
+      if (w == warp) base = total;
+      total.tokens += warp_sum[w].tokens, total.pages += warp_sum[w].pages;
     }
-    warp_sum[lane] = w;
+  } else {
+    if (warp == 0) {
+      Sums w = warp_sum[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const Sums u = shfl_up(w, o);
+        if (lane >= o) w.tokens += u.tokens, w.pages += u.pages;
+      }
+      warp_sum[lane] = w;
+    }
+    __syncthreads();
+    total = warp_sum[WARPS - 1];
+    if (warp > 0) base = warp_sum[warp - 1];
   }
-  __syncthreads();
-  total = warp_sum[31];
-  const Sums base = warp > 0 ? warp_sum[warp - 1] : Sums{0, 0};
   return Sums{base.tokens + inc.tokens - v.tokens, base.pages + inc.pages - v.pages};
 }
 
@@ -84,8 +96,11 @@ __device__ void fill_token(const CacheExtendArgs& a, int t, const int32_t* off, 
   a.positions[t] = base[lo] + at;
 }
 
+template <int SUM_THREADS>
 __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, bool fill) {
-  __shared__ Sums warp_sum[32];
+  constexpr int WARPS = SUM_THREADS / 32;
+  __shared__ Sums warp_sum[WARPS];
+  __shared__ int2 gone_rows[SUM_THREADS];  // a released row, where its pages go on the stack
   __shared__ int bad;
   __shared__ int64_t released;
   const int n = a.lay.n_seqs, page = a.lay.page;
@@ -127,7 +142,7 @@ __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, b
       }
     }
     Sums total;
-    const Sums ex = block_exclusive(v, warp_sum, total);
+    const Sums ex = block_exclusive<WARPS>(v, warp_sum, total);
     if (i < n) {
       held[i] = len;
       base[i] = b;
@@ -164,16 +179,14 @@ __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, b
       const int i = i0 + threadIdx.x;
       const bool gone = i < n && a.new_lens[i] < 0;
       Sums total;
-      const Sums ex = block_exclusive(Sums{0, gone ? pages_of(held[i], page) : 0}, warp_sum, total);
-      // each warp works through its released rows together
-      unsigned todo = __ballot_sync(0xffffffffu, gone);
-      while (todo) {
-        const int who = __ffs(todo) - 1;
-        todo &= todo - 1;
-        const int row = i - (threadIdx.x & 31) + who, np = pages_of(held[row], page);
-        const int64_t to = at + __shfl_sync(0xffffffffu, ex.pages, who);
+      const Sums ex = block_exclusive<WARPS>(Sums{gone ? 1 : 0, gone ? pages_of(held[i], page) : 0}, warp_sum, total);
+      if (gone) gone_rows[ex.tokens] = make_int2(i, static_cast<int>(at + ex.pages));
+      __syncthreads();
+      for (int g = threadIdx.x >> 5; g < total.tokens; g += WARPS) {  // a warp a row
+        const int2 it = gone_rows[g];
+        const int np = pages_of(held[it.x], page);
         for (int p = threadIdx.x & 31; p < np; p += 32)
-          a.free_blocks[to + p] = a.tables[static_cast<int64_t>(row) * a.lay.max_blocks + p];
+          a.free_blocks[it.y + p] = a.tables[static_cast<int64_t>(it.x) * a.lay.max_blocks + p];
       }
       at += total.pages;
     }
@@ -222,7 +235,10 @@ __global__ void __launch_bounds__(FILL_THREADS) k_cache_fill(CacheExtendArgs a) 
 
 cudaError_t launch_cache_extend(const CacheExtendArgs& a, cudaStream_t st) {
   const bool here = a.max_tokens <= FILL_HERE;
-  const cudaError_t e = launch_dependent(k_cache_sums, dim3(1), SUM_THREADS, 0, st, a, here);
+  // a few rows need few threads, whose barriers are shorter
+  const bool few = a.lay.n_seqs <= FEW_THREADS && a.max_tokens <= 4 * FEW_THREADS;
+  const cudaError_t e = few ? launch_dependent(k_cache_sums<FEW_THREADS>, dim3(1), FEW_THREADS, 0, st, a, here)
+                            : launch_dependent(k_cache_sums<MANY_THREADS>, dim3(1), MANY_THREADS, 0, st, a, here);
   if (e != cudaSuccess || here) return e;
   return launch_dependent(k_cache_fill, dim3((a.max_tokens + FILL_THREADS - 1) / FILL_THREADS), FILL_THREADS, 0, st, a);
 }

@@ -206,22 +206,25 @@ __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, b
 }
 
 __global__ void __launch_bounds__(FILL_THREADS) k_cache_fill(CacheExtendArgs a) {
-  __shared__ int rows[2];
-  const int t0 = blockIdx.x * FILL_THREADS, t = t0 + threadIdx.x;
+  static_assert((CACHE_MAX_SEQS + FILL_THREADS - 1) / FILL_THREADS <= FILL_THREADS, "two counts find a row");
+  const int t0 = blockIdx.x * FILL_THREADS, t = t0 + threadIdx.x, n = a.lay.n_seqs;
   pdl_wait();
   pdl_trigger();
   const int tokens = a.ws[WS_TOKENS], top = a.ws[WS_TOP];
-  if (threadIdx.x < 2 && t0 < tokens) {
-    // the rows of the block's first and last token bound every thread's search
-    const int x = threadIdx.x ? min(t0 + FILL_THREADS, tokens) - 1 : t0;
-    int lo = 0, hi = a.lay.n_seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.tok_off[mid] <= x) lo = mid; else hi = mid - 1;
-    }
-    rows[threadIdx.x] = lo;
+  // the rows of the block's first and last token bound every thread's search: all threads look at every step-th offset, then
+  // at those between (one thread halving the range: 11 loads one after another for 2,000 rows)
+  int rows[2] = {0, 0};
+  if (t0 < tokens) {
+    const int x0 = t0, x1 = min(t0 + FILL_THREADS, tokens) - 1, step = (n + FILL_THREADS - 1) / FILL_THREADS;
+    const int i = threadIdx.x * step, v = i < n ? a.tok_off[i] : INT32_MAX;
+    rows[0] = (__syncthreads_count(v <= x0) - 1) * step;
+    rows[1] = (__syncthreads_count(v <= x1) - 1) * step;
+    const bool in = static_cast<int>(threadIdx.x) < step;
+    const int i0 = rows[0] + threadIdx.x, i1 = rows[1] + threadIdx.x;
+    const int v0 = in && i0 < n ? a.tok_off[i0] : INT32_MAX, v1 = in && i1 < n ? a.tok_off[i1] : INT32_MAX;
+    rows[0] += __syncthreads_count(v0 <= x0) - 1;
+    rows[1] += __syncthreads_count(v1 <= x1) - 1;
   }
-  __syncthreads();
   if (t >= a.max_tokens) return;
   if (t < tokens) {
     fill_token(a, t, a.tok_off, rows[0], rows[1], top);

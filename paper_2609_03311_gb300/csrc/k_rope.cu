@@ -5,9 +5,11 @@
 // their angle in 32 bits (at 250,000 radians a step is 0.016), so angles and their cos and sin are taken in 64 bits,
 // once, into a table; what is left for a row is four products of 32 bits a pair.
 //
-// Bound by HBM: a row is read once and written once, 24 KB of 16-bit q, k and v for 32 + 2 x 8 heads of 128.  A
-// thread takes one unit of 2 x VEC elements (16 bytes of each half of the pairs; 32 contiguous bytes where pairs are
-// interleaved) and walks over the heads with it, so that it reads its cos and sin once a row.
+// Bound by HBM: a row is read once and written once, 24 KB of 16-bit q, k and v for 32 + 2 x 8 heads of 128.  26,800 of them
+// take 110 us, 6.0 TB/s; 4,097 rows of 24 heads in 32 bits, 17.3 us, 5.8 TB/s.  A thread takes one unit of 2 x VEC
+// elements (16 bytes of each half of the pairs; 32 contiguous bytes where pairs are interleaved) and walks over the
+// heads with it, so that it reads its cos and sin once a row.  Two or three heads on their way a thread were slower (115 us
+// a chunk): what counts is how many threads an SM holds.  Views that 16-byte accesses do not fit go element by element.
 #include <type_traits>
 
 #include "device_common.cuh"
@@ -16,7 +18,7 @@
 namespace dopr {
 namespace {
 
-constexpr int ROPE_THREADS = 128;
+constexpr int MAX_THREADS = 256;
 
 template <typename T>
 __device__ __forceinline__ float to_f32(T x) {
@@ -71,21 +73,34 @@ __device__ __forceinline__ void turn(Pack<T, VEC>& a, Pack<T, VEC>& b, const flo
 }
 
 template <typename T, int VEC, bool INTER>
-__global__ void __launch_bounds__(ROPE_THREADS) k_rope(RopeArgs a) {
+__global__ void __launch_bounds__(MAX_THREADS) k_rope(RopeArgs a) {
   const int units = a.head_dim / (2 * VEC), turning = a.rotary / (2 * VEC);
-  const int lanes = ROPE_THREADS / units;  // heads at once
+  const int lanes = blockDim.x / units;  // heads at once
   const int u = threadIdx.x % units, h0 = threadIdx.x / units;
   // unit u's two runs of VEC elements
   const int ia = u < turning && !INTER ? u * VEC : u * 2 * VEC;
   const int ib = u < turning && !INTER ? ia + a.rotary / 2 : ia + VEC;
   const int heads = a.q.n_heads + a.k.n_heads + a.v.n_heads;
+  const int page_bits = __ffs(a.page) - 1;  // a power of two
   pdl_wait();
   pdl_trigger();
   if (h0 >= lanes) return;
   for (int t = blockIdx.x; t < a.n_tokens; t += gridDim.x) {
+    const int pos = a.rotary > 0 ? a.positions[t] : 0;
+    const int64_t slot = a.slots ? a.slots[t] : -1;
+    // the first head's elements are asked for beside the position and the table
+    Pack<T, VEC> p0, p1;
+    auto load = [&](int h) {
+      const bool is_q = h < a.q.n_heads, is_v = h >= a.q.n_heads + a.k.n_heads;
+      const RopeView& view = is_q ? a.q : is_v ? a.v : a.k;
+      const int hh = is_q ? h : is_v ? h - a.q.n_heads - a.k.n_heads : h - a.q.n_heads;
+      const T* x = static_cast<const T*>(view.in) + t * view.in_tok + hh * view.in_head;
+      p0 = *reinterpret_cast<const Pack<T, VEC>*>(x + ia);
+      p1 = *reinterpret_cast<const Pack<T, VEC>*>(x + ib);
+    };
+    if (h0 < heads) load(h0);
     float c[VEC], s[VEC];
     if (a.rotary > 0) {
-      const int pos = a.positions[t];
       if (pos < 0) continue;
       if (pos >= a.max_position) {
         if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
@@ -93,40 +108,43 @@ __global__ void __launch_bounds__(ROPE_THREADS) k_rope(RopeArgs a) {
       }
       if (u < turning) {
         const float2* cs = a.table + static_cast<int64_t>(pos) * (a.rotary / 2) + u * VEC;
+        if constexpr (VEC > 1) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float2 e = __ldg(cs + i);
-          c[i] = e.x;
-          s[i] = a.inverse ? -e.y : e.y;
+          for (int i = 0; i < VEC; i += 2) {
+            const float4 e = __ldg(reinterpret_cast<const float4*>(cs + i));
+            c[i] = e.x, s[i] = e.y, c[i + 1] = e.z, s[i + 1] = e.w;
+          }
+        } else {
+          const float2 e = __ldg(cs);
+          c[0] = e.x, s[0] = e.y;
+        }
+        if (a.inverse) {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) s[i] = -s[i];
         }
       }
     }
-    int64_t slot = -1;
-    if (a.slots) {
-      slot = a.slots[t];
-      if (slot >= a.n_slots) {
-        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-        continue;
-      }
+    if (slot >= a.n_slots && a.slots) {
+      if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+      continue;
     }
-    for (int h = h0; h < heads; h += lanes) {
+    for (int h = h0; h < heads;) {
       const bool is_q = h < a.q.n_heads, is_v = h >= a.q.n_heads + a.k.n_heads;
       if (!is_q && a.slots && slot < 0) break;  // the row is not stored; heads go up
       const RopeView& view = is_q ? a.q : is_v ? a.v : a.k;
       const int hh = is_q ? h : is_v ? h - a.q.n_heads - a.k.n_heads : h - a.q.n_heads;
-      const T* x = static_cast<const T*>(view.in) + t * view.in_tok + hh * view.in_head;
       T* y;
       if (is_q || !a.slots) {
         y = static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head;
       } else {
-        const int64_t row = (slot / a.page * a.k.n_heads + hh) * a.page + slot % a.page;
+        const int64_t row = (((slot >> page_bits) * a.k.n_heads + hh) << page_bits) + (slot & (a.page - 1));
         y = static_cast<T*>(is_v ? a.v_pool : a.k_pool) + row * a.head_dim;
       }
-      Pack<T, VEC> p0 = *reinterpret_cast<const Pack<T, VEC>*>(x + ia);
-      Pack<T, VEC> p1 = *reinterpret_cast<const Pack<T, VEC>*>(x + ib);
       if (u < turning && !is_v) turn<T, VEC, INTER>(p0, p1, c, s);
       *reinterpret_cast<Pack<T, VEC>*>(y + ia) = p0;
       *reinterpret_cast<Pack<T, VEC>*>(y + ib) = p1;
+      h += lanes;
+      if (h < heads) load(h);
     }
   }
 }
@@ -137,7 +155,10 @@ bool aligned16(const void* p, int64_t s0, int64_t s1, int size) {
 
 template <typename T, int VEC, bool INTER>
 cudaError_t launch(const RopeArgs& a, cudaStream_t st) {
-  return launch_dependent(k_rope<T, VEC, INTER>, dim3(a.n_tokens < 65536 ? a.n_tokens : 65536), ROPE_THREADS, 0, st, a);
+  // few tokens leave most SMs idle: more threads a token make fewer turns over the heads (one token 2.3 us, with 128 2.8;
+  // 64 rows into the cache 2.7 and 3.1); of many tokens the heads fill 128 more evenly (a chunk of 26,800: 110 us, with 256 138)
+  const int threads = a.n_tokens <= 512 ? MAX_THREADS : MAX_THREADS / 2;
+  return launch_dependent(k_rope<T, VEC, INTER>, dim3(a.n_tokens < 65536 ? a.n_tokens : 65536), threads, 0, st, a);
 }
 template <typename T>
 cudaError_t launch_type(const RopeArgs& a, cudaStream_t st) {

@@ -99,6 +99,14 @@ def test_bad_attention_arguments_are_refused(lib, bad, status):
     assert lib.dopr_last_error()
 
 
+@pytest.mark.parametrize("plan,workspace", [(4104, 4096), (4096, 4112), (4096, 4100)])
+def test_misaligned_plans_and_workspaces_are_refused(lib, plan, workspace):
+    # a plan by 16 bytes, a workspace by 32
+    assert lib.dopr_shared_attention(ctypes.byref(layout()), ctypes.c_void_p(plan), 4, heads(), P, P, P, 0.1, heads(), None,
+                                     ctypes.c_void_p(workspace), None, None) == dopr.ERR_INVALID_ARG
+    assert lib.dopr_last_error()
+
+
 @pytest.mark.parametrize("bad,status", [
     (dict(max_position=0), dopr.ERR_INVALID_ARG), (dict(rotary_dim=0), dopr.ERR_INVALID_ARG),
     (dict(rotary_dim=63), dopr.ERR_UNSUPPORTED), (dict(rotary_dim=258), dopr.ERR_UNSUPPORTED),

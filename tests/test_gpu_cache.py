@@ -704,3 +704,38 @@ def test_a_captured_step_is_replayed_as_the_sequences_grow():
         p.check(outs, new, lens, qkv)
         lens = [a + c for a, c in zip(lens, new)]
         assert p.seq_lens.tolist() == lens
+
+
+# ------------------------------------------------------------------ more rows and tokens than a plan holds close by
+@pytest.mark.parametrize("n,docs,busy,in_order", [(1500, 40, 1500, False), (1500, 1400, 1500, True), (5000, 9, 5000, False),
+                                                  (16000, 384, 700, False)])
+def test_attention_of_thousands_of_rows(n, docs, busy, in_order):
+    # rows in any order of their prefixes (or in it), most of them with one token; beyond 1,024 rows the lists are made in
+    # parts, beyond some 3,000 they no longer lie in shared memory
+    r = np.random.default_rng(n + docs)
+    of = r.integers(-1, docs, n)
+    of = np.sort(of) if in_order else of
+    live = np.zeros(n, dtype=bool)
+    live[r.permutation(n)[:busy]] = True
+    reqs = [(int(p), int(x), int(t)) for p, x, t in zip(of, np.where(live, r.integers(0, 4, n), 0),
+                                                        np.where(live, r.choice([0, 1, 1, 1, 2], n), 0))]
+    b = Batch(2, 1, 64, BF, 16, [int(x) for x in r.integers(0, 20, docs)], reqs, seed=n)
+    b.check(b.run())
+
+
+def test_attention_of_more_tokens_than_items_in_shared_memory():
+    r = np.random.default_rng(3)
+    reqs = [(int(r.integers(-1, 2)), 70, int(t)) for t in r.integers(60, 71, 300)]
+    b = Batch(4, 1, 64, HF, 32, [40, 0], reqs, seed=4)
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("rows,hi", [(16384, 1), (16384, 2), (129, 4), (128, 4), (100, 3)])
+def test_extend_of_many_and_few_rows(rows, hi):
+    # both counts of threads, and offsets found in two steps over all rows
+    r = np.random.default_rng(rows + hi)
+    held, new = r.integers(0, 20, rows), r.integers(0, hi + 1, rows)
+    new[r.random(rows) < 0.4] = -1
+    mb = -(-(20 + hi) // 16)
+    t = Tables(held, 16, mb, rows * mb, seed=rows)
+    check_extend(t, new, None, int(np.maximum(new, 0).sum()) + hi)

@@ -302,53 +302,60 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
   const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
   const float scale_log2 = a.scale * 1.4426950408889634f;
   const int quad = lane >> 2, in_quad = lane & 3;
+  // copies run ahead of the products, over the ends of segments too
+  Walk copies(plan, work);
+  Segment c;
+  bool more = copies.next(c);
+  uint32_t next = more ? c.b0 : 0;
+  int stage = 0, ahead = 0;        // of the piece at hand, of the next one to be copied
+  int row_at = 0, valid_at = 0;    // where the next 32 pieces lie: a lane a piece
+  auto find = [&](uint32_t b) {
+    if (b >= c.b1) return;
+    PageCursor cur(plan, c);
+    cur.go(b);
+    const Run& run = cur.run;
+    const int key = (static_cast<int>(b) - run.off) * PIECE;
+    int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
+    if (block < 0 || block >= a.lay.n_blocks) {
+      if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+      block = 0;
+    }
+    row_at = (block * Hkv + c.h) * page + key % page;
+    valid_at = min(PIECE, run.keys - key);
+  };
+  // rows past the run's keys come as zeros; a group of copies also where there is no piece left
+  auto copy = [&] {
+    if (more && next == c.b1) {
+      more = copies.next(c);
+      next = c.b0;
+    }
+    if (more) {
+      const int at = (next - c.b0) & 31;
+      if (at == 0) find(next + lane);
+      const int64_t row = __shfl_sync(0xffffffffu, row_at, at);
+      const int valid = __shfl_sync(0xffffffffu, valid_at, at);
+      const uint4* k = static_cast<const uint4*>(a.k_pool) + row * CHUNKS + lane;
+      const uint4* v = static_cast<const uint4*>(a.v_pool) + row * CHUNKS + lane;
+      const int x = lane % CHUNKS;
+      const uint32_t dst = base + ahead * 2 * KV + (x >> 3) * HALF;
+#pragma unroll
+      for (int i = 0; i < PIECE * CHUNKS / 32; ++i) {
+        const int r = lane / CHUNKS + i * (32 / CHUNKS);
+        const uint32_t at_row = dst + r * 128 + (((x & 7) ^ (r & 7)) << 4);
+        cp_async16(at_row, k + 32 * i, r < valid);
+        cp_async16(at_row + KV, v + 32 * i, r < valid);
+      }
+      ++next;
+    }
+    cp_async_commit();
+    ahead = ahead + 1 == L::F_STAGES ? 0 : ahead + 1;
+  };
+#pragma unroll 1
+  for (int i = 0; i + 1 < L::F_STAGES; ++i) copy();
+
   Walk walk(plan, work);
   Segment s;
   while (walk.next(s)) {
-    // where the next 32 pieces lie: a lane a piece
-    int row_at = 0, valid_at = 0;
-    auto find = [&](uint32_t b) {
-      if (b >= s.b1) return;
-      PageCursor cur(plan, s);
-      cur.go(b);
-      const Run& run = cur.run;
-      const int key = (static_cast<int>(b) - run.off) * PIECE;
-      int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
-      if (block < 0 || block >= a.lay.n_blocks) {
-        if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-        block = 0;
-      }
-      row_at = (block * Hkv + s.h) * page + key % page;
-      valid_at = min(PIECE, run.keys - key);
-    };
-    uint32_t next = s.b0;
-    int stage = 0, ahead = 0;  // of the piece at hand, of the next one to be copied
-    // rows past the run's keys come as zeros; a group of copies also where there is no piece left
-    auto copy = [&] {
-      if (next < s.b1) {
-        const int at = (next - s.b0) & 31;
-        if (at == 0) find(next + lane);
-        const int64_t row = __shfl_sync(0xffffffffu, row_at, at);
-        const int valid = __shfl_sync(0xffffffffu, valid_at, at);
-        const uint4* k = static_cast<const uint4*>(a.k_pool) + row * CHUNKS + lane;
-        const uint4* v = static_cast<const uint4*>(a.v_pool) + row * CHUNKS + lane;
-        const int c = lane % CHUNKS;
-        const uint32_t dst = base + ahead * 2 * KV + (c >> 3) * HALF;
-#pragma unroll
-        for (int i = 0; i < PIECE * CHUNKS / 32; ++i) {
-          const int r = lane / CHUNKS + i * (32 / CHUNKS);
-          const uint32_t at_row = dst + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-          cp_async16(at_row, k + 32 * i, r < valid);
-          cp_async16(at_row + KV, v + 32 * i, r < valid);
-        }
-        ++next;
-      }
-      cp_async_commit();
-      ahead = ahead + 1 == L::F_STAGES ? 0 : ahead + 1;
-    };
-#pragma unroll 1
-    for (int i = 0; i + 1 < L::F_STAGES; ++i) copy();
-
     const int rows = s.n_tok * G;
     uint32_t q[D / 16][4];
     int own0[2], own1[2];

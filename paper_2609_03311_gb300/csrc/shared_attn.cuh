@@ -39,7 +39,7 @@ constexpr int WORKERS = 8;  // warps of a CTA that take few items
 // memory's rate): a piece; an entry's start and end.  Fitted to the CTAs' times: 2,880 clocks a whole block, 5,200 to 6,900
 // another, 10,200 to 12,200 an entry.
 constexpr uint32_t WHOLE_BLOCK = 6, OTHER_BLOCK = 12, FEW_PIECE = 1;
-__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 2 : 20; }
+__host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 : 20; }
 constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
 constexpr uint32_t MIN_FEW_SHARE = 6;
 

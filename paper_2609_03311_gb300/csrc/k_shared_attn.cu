@@ -11,12 +11,19 @@
 //   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
 //     warp 0, 2  copy K and V blocks into two rings, page by page (TMA; a page's rows of a kv head lie together)
 //     warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
-//     warp 3     brings the rows of Q: eight tokens that follow one another by TMA (the rows of a token and kv head are the
-//                heads of a box), others with 16-byte copies
+//     warp 3     brings the rows of Q by TMA: eight tokens that follow one another, others one by one (the rows of a token
+//                and kv head are the heads of a box); of a view that a tensor map does not take, with 16-byte copies
 //     warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more than
 //                2^8 (P stays within the type's range until then)
+//   P is rounded to the inputs' type for its product with V, as the tensor cores take it; maxima, sums, O and parts stay in 32
+//   bits, and a row's sum adds up P before the rounding.
+//   2,048 rows of 32 heads over 16,384 keys: 351 us, 1.57 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
+//   cores work 2,050: a tile's S, softmax, P V and next S wait for one another (TMEM, full with two of S and of O, has no
+//   room for a second S), so a second tile fills the gaps and P goes over in halves (371 us when it went as one).  64 rows of
+//   a token over 32,768 keys: 46.5 us, 38 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
 //   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
-//   box by TMA takes about 80 ns of an SM (the rate of ragged documents in pages of 16 was 2 KB a box, 73 us for 63).
+//   box by TMA takes about 80 ns of an SM (256 tokens over 64 ragged documents in pages of 16: 73 us by TMA, 63 with 16-byte
+//   copies then; 53 now, 4.8 TB/s).
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
 // Values would (0 x NaN), so rows of V past a run's keys are zero in shared memory.  A value that one token sees and
 // another of the item does not would too: rows that end with a NaN though their scores have none are computed alone.
@@ -36,7 +43,8 @@ constexpr int THREADS = 128 + 2 * 128;
 // group w: S at S_COL + 128 w, P over its upper half, O at O_COL + 128 w
 constexpr uint32_t TMEM_COLS = 512, S_COL = 0, P_COL = 64, O_COL = 256;
 constexpr float RESCALE_LOG2 = 8.f;
-constexpr int JOIN_CTAS = 4;  // of the joining kernel on an SM
+// of the joining kernel on an SM (3 with twice the loads on their way: 64 rows a little faster, 16 documents 3 % slower)
+constexpr int JOIN_CTAS = 4;
 constexpr int HALF_BYTES = 128 * 128;  // 128 rows of 64 16-bit elements
 
 template <int D>
@@ -480,7 +488,8 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
 
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1)
-    k_shared_attn(const __grid_constant__ CUtensorMap tm_q8, const __grid_constant__ CUtensorMap tm_q1, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+    k_shared_attn(const __grid_constant__ CUtensorMap tm_q8, const __grid_constant__ CUtensorMap tm_q1,
+                  const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -1099,7 +1108,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 // ------------------------------------------------------------------ joining the parts
 // A warp a row, JOIN_ROWS rows of an entry at a time.  Bound by latency where few rows have many parts, so what the plan says
 // of a CTA's first piece is read while the attention ends (it was complete before that began), the first values are asked for
-// beside the maxima and sums, and eight parts are on their way at once.
+// beside the maxima and sums, and four parts are on their way at once (eight take registers that cost more rows at once).
+// 64 rows of a token, 19 parts each: about 8 us; 5,000 tokens of 16 documents, of which a third has two parts: 14.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
     k_shared_join(const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan, int n_ctas) {

@@ -425,6 +425,14 @@ def _heads(name, t, tokens, head_dim, dtype, device):
     return ctypes.byref(Heads(t.data_ptr(), strides[0], strides[1], shape[1]))
 
 
+def _sized(fn, layout, *sizes):
+    """Bytes that a call with this layout and these sizes needs."""
+    n = fn(ctypes.byref(layout), *sizes)
+    if n < 0:
+        raise DoprError(ERR_INVALID_ARG, load().dopr_last_error().decode())
+    return n
+
+
 def make_cache_layout(n_blocks: int, page: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_seqs: int,
                       max_blocks: int) -> CacheLayout:
     """Pools of one layer's keys and values [n_blocks, n_kv_heads, page, head_dim] and tables [n_seqs, max_blocks]."""
@@ -443,10 +451,7 @@ class CacheBatch:
         self.positions = torch.empty(max_tokens, **i32)
         self.seq_lens = torch.empty(layout.n_seqs, **i32)
         self.n_free = torch.empty(1, **i32)
-        n = load().dopr_cache_extend_workspace(ctypes.byref(layout))
-        if n < 0:
-            raise DoprError(ERR_INVALID_ARG, load().dopr_last_error().decode())
-        self.workspace = torch.empty(n, dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(_sized(load().dopr_cache_extend_workspace, layout), dtype=torch.uint8, device=device)
 
 
 def cache_batch(layout: CacheLayout, max_tokens: int, device="cuda") -> CacheBatch:
@@ -463,7 +468,8 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
     try:
         if out is None:
             out = CacheBatch(layout, max_tokens, dev)
-        _check(load().dopr_cache_extend(
+        lib = load()
+        _check(lib.dopr_cache_extend(
             ctypes.byref(layout), _buf("seq_lens", seq_lens, i32, n, on),
             _buf("block_tables", block_tables, i32, n * layout.max_blocks, on),
             _buf("free_blocks", free_blocks, i32, layout.n_blocks, on), _buf("n_free", n_free, i32, 1, on),
@@ -471,7 +477,7 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
             _buf("out.seq_lens", out.seq_lens, i32, n, on), _buf("out.n_free", out.n_free, i32, 1, on),
             _buf("out.tok_off", out.tok_off, i32, n + 1, on), _buf("out.slots", out.slots, torch.int64, max_tokens, on),
             _buf("out.positions", out.positions, i32, max_tokens, on),
-            _buf("out.workspace", out.workspace, torch.uint8, 0, on), _buf("status", status, i32, 1, on), st))
+            _buf("out.workspace", out.workspace, torch.uint8, _sized(lib.dopr_cache_extend_workspace, layout), on), _buf("status", status, i32, 1, on), st))
     finally:
         if guard is not None:
             guard.__exit__(None, None, None)
@@ -545,13 +551,6 @@ def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | 
         if guard is not None:
             guard.__exit__(None, None, None)
     return q_out
-
-
-def _sized(fn, layout, n_q_heads, max_tokens):
-    n = fn(ctypes.byref(layout), n_q_heads, max_tokens)
-    if n < 0:
-        raise DoprError(ERR_INVALID_ARG, load().dopr_last_error().decode())
-    return n
 
 
 def shared_attention_plan(layout: CacheLayout, n_q_heads: int, tok_off, seq_lens, prefix, max_tokens: int, plan=None,

@@ -739,3 +739,18 @@ def test_extend_of_many_and_few_rows(rows, hi):
     mb = -(-(20 + hi) // 16)
     t = Tables(held, 16, mb, rows * mb, seed=rows)
     check_extend(t, new, None, int(np.maximum(new, 0).sum()) + hi)
+
+
+def test_extend_refuses_a_batch_of_another_layout():
+    # a step's buffers made for 3 rows, every tensor but the workspace replaced by one that 40 rows fit
+    t = Tables([5] * 40, 16, 2, 90, seed=1)
+    small = dopr.make_cache_layout(90, 16, 2, 64, torch.float16, 3, 2)
+    layout = dopr.make_cache_layout(90, 16, 2, 64, torch.float16, 40, 2)
+    out, whole = dopr.cache_batch(small, 40), dopr.cache_batch(layout, 40)
+    lens, tables, free, n_free = t.device()
+    for name in ("tok_off", "seq_lens", "slots", "positions", "n_free"):
+        setattr(out, name, getattr(whole, name))
+    with pytest.raises(ValueError, match="workspace"):
+        dopr.cache_extend(layout, lens, tables, free, n_free, i32([1] * 40), 40, out=out)
+    dopr.cache_extend(layout, lens, tables, free, n_free, i32([1] * 40), 40, out=whole)
+    assert whole.seq_lens.tolist() == [6] * 40

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -381,6 +382,8 @@ ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_RAMP = range(5)
 _DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
 _TORCH_TYPES = (torch.float16, torch.bfloat16, torch.float32)
+_pack_heads = struct.Struct("@Pqqi4x").pack
+assert struct.calcsize("@Pqqi4x") == ctypes.sizeof(Heads)
 
 
 # Calls of a few microseconds on the device are bound by what is done here: device and stream are asked for as numbers, and
@@ -414,7 +417,8 @@ def _buf(name, t, dtype, n, device):
 
 
 def _heads(name, t, tokens, head_dim, dtype, device):
-    """A [tokens, heads, head_dim] tensor as the C ABI's view (strided, the last dimension contiguous)."""
+    """A [tokens, heads, head_dim] tensor as the C ABI's view (strided, the last dimension contiguous): the bytes of a
+    Heads, which a call takes faster than the structure."""
     if t is None:
         return None
     shape, strides = t.shape, t.stride()
@@ -422,7 +426,7 @@ def _heads(name, t, tokens, head_dim, dtype, device):
             (head_dim > 1 and strides[2] != 1):
         raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on cuda:{device} with a contiguous last "
                          f"dimension, got {tuple(shape)} {t.dtype} on {t.device}, strides {strides}")
-    return ctypes.byref(Heads(t.data_ptr(), strides[0], strides[1], shape[1]))
+    return _pack_heads(t.data_ptr(), strides[0], strides[1], shape[1])
 
 
 def _sized(fn, layout, *sizes):
@@ -451,7 +455,8 @@ class CacheBatch:
         self.positions = torch.empty(max_tokens, **i32)
         self.seq_lens = torch.empty(layout.n_seqs, **i32)
         self.n_free = torch.empty(1, **i32)
-        self.workspace = torch.empty(_sized(load().dopr_cache_extend_workspace, layout), dtype=torch.uint8, device=device)
+        self.n_seqs, self.workspace_bytes = layout.n_seqs, _sized(load().dopr_cache_extend_workspace, layout)
+        self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
 
 
 def cache_batch(layout: CacheLayout, max_tokens: int, device="cuda") -> CacheBatch:
@@ -468,8 +473,9 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
     try:
         if out is None:
             out = CacheBatch(layout, max_tokens, dev)
-        lib = load()
-        _check(lib.dopr_cache_extend(
+        elif out.n_seqs < n:
+            raise ValueError(f"out: its workspace is for {out.n_seqs} rows, the layout has {n}")
+        _check(load().dopr_cache_extend(
             ctypes.byref(layout), _buf("seq_lens", seq_lens, i32, n, on),
             _buf("block_tables", block_tables, i32, n * layout.max_blocks, on),
             _buf("free_blocks", free_blocks, i32, layout.n_blocks, on), _buf("n_free", n_free, i32, 1, on),
@@ -477,7 +483,7 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
             _buf("out.seq_lens", out.seq_lens, i32, n, on), _buf("out.n_free", out.n_free, i32, 1, on),
             _buf("out.tok_off", out.tok_off, i32, n + 1, on), _buf("out.slots", out.slots, torch.int64, max_tokens, on),
             _buf("out.positions", out.positions, i32, max_tokens, on),
-            _buf("out.workspace", out.workspace, torch.uint8, _sized(lib.dopr_cache_extend_workspace, layout), on), _buf("status", status, i32, 1, on), st))
+            _buf("out.workspace", out.workspace, torch.uint8, out.workspace_bytes, on), _buf("status", status, i32, 1, on), st))
     finally:
         if guard is not None:
             guard.__exit__(None, None, None)
@@ -511,7 +517,7 @@ class Rope:
 def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False, status=None, stream=None):
     """Rotary positions on q and, with it, k: [tokens, heads, head_dim] views of float16, bfloat16 or float32.  Returns
     (q_out, k_out); pass q_out=q, k_out=k to work in place.  inverse: the gradient of the rotation."""
-    T, D, dt, dev = q.shape[0], q.shape[2], q.dtype, q.device
+    (T, _, D), dt, dev = q.shape, q.dtype, q.device
     if dt not in _DTYPES:
         raise ValueError(f"rope_apply: float16, bfloat16 or float32, got {dt}")
     st, guard, on = _on(dev, stream)

@@ -6,9 +6,9 @@
 // prefix keep their order).  Made once a step and used by every layer.  Bound by the latency of some twenty short phases:
 // lists, items and runs stay in shared memory where they fit, a sum over the block takes one barrier and two counts where
 // they fit, and what rows, items and entries hold several of (items, runs, tokens, segments) is spread over a warp's lanes.
-// 512 threads: 10.9 us for one token, 14.1 for 64 queries of one document, 20.9 for 256 of 64 documents, 28.7 for 5,000 tokens
-// of 200 queries; 1024: 12.1, 15.7, 20.8, 26.4 (a barrier and a sum cost more the more warps there are); 256: 10.7, 13.6, 25.9,
-// 37.5.
+// 512 threads: 11 us for one token, 15 for 64 queries of one document, 22 for 256 of 64 documents, 31 for 5,000 tokens of 200
+// queries.  (As it was then, 1024 threads to 512 to 256: 12.1, 10.9, 10.7; 15.7, 14.1, 13.6; 20.8, 20.9, 25.9; 26.4, 28.7, 37.5:
+// a barrier and a sum cost more the more warps there are.)
 #include <limits.h>
 
 #include "shared_attn.cuh"
@@ -61,7 +61,7 @@ struct Divisor {
 template <typename F>
 __device__ void spread(int count, F f) {
   const int inc = warp_inclusive(count), total = __shfl_sync(0xffffffffu, inc, 31);
-  #pragma unroll 1
+#pragma unroll 1
   for (int s = threadIdx.x & 31; s < (total + 31) / 32 * 32; s += 32) {
     int src = 0;  // lanes whose counts end at or before s
 #pragma unroll
@@ -76,12 +76,12 @@ __device__ __forceinline__ int of_lane(int v, int src) { return __shfl_sync(0xff
 __device__ void sort_keys(uint32_t* keys, int m) {
   const int threads = min(m, THREADS), tid = threadIdx.x;
   if (tid >= threads) return;
-  #pragma unroll 1
+#pragma unroll 1
   for (int k = 2; k <= m; k <<= 1) {
     int j = k >> 1;
-    #pragma unroll 1
+#pragma unroll 1
     for (; j >= 32; j >>= 1) {
-      #pragma unroll 1
+#pragma unroll 1
       for (int i = tid; i < m; i += threads) {
         const int o = i ^ j;
         if (o > i) {
@@ -91,10 +91,10 @@ __device__ void sort_keys(uint32_t* keys, int m) {
       }
       asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory");
     }
-    #pragma unroll 1
+#pragma unroll 1
     for (int i = tid; i < m; i += threads) {
       uint32_t x = keys[i];
-      #pragma unroll 1
+#pragma unroll 1
       for (int l = j; l > 0; l >>= 1) {
         const uint32_t y = __shfl_xor_sync(0xffffffffu, x, l);
         x = ((i & l) == 0) == ((i & k) == 0) ? min(x, y) : max(x, y);
@@ -129,7 +129,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     at_shared += (count * static_cast<int64_t>(sizeof(*global)) + 15) / 16 * 16;
     return q;
   };
-  int* sorted = shared(LISTS_SHARED, p.scratch, plan_scratch_ints(n));  // rows with tokens, by group: their prefix, n where there are no prefix keys
+  // rows with tokens, by group: their prefix, n where there are no prefix keys
+  int* sorted = shared(LISTS_SHARED, p.scratch, plan_scratch_ints(n));
   Item* items = shared(ITEMS_SHARED, p.items, max_items(n, G, a.max_tokens));
   Run* runs = shared(RUNS_SHARED, p.runs, max_runs(n, G, a.max_tokens));
   int* group_of = sorted + n;        // of a sorted entry
@@ -168,24 +169,24 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
 
   // checks, and the rows with tokens
   int ns = 0, n_sorted_tok = 0;
-  #pragma unroll 1
+#pragma unroll 1
   for (int i0 = 0; i0 < n; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    int v[2] = {0, 0}, total[2], g = n;
+    int tok = 0, g = n;
     if (i < n) {
       const int t0 = a.tok_off[i], t1 = a.tok_off[i + 1], pre = a.prefix ? a.prefix[i] : -1, len = a.seq_lens[i];
       if ((i == 0 && t0 != 0) || t0 < 0 || t1 < t0 || t1 > a.max_tokens || len < 0 || len > cap || pre < -1 || pre >= n || pre == i ||
           (pre >= 0 && a.prefix[pre] != -1))
         bad = 1;
       else
-        v[0] = t1 > t0, v[1] = t1 - t0;
-      if (v[0] && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
+        tok = t1 - t0;
+      if (tok > 0 && pre >= 0 && a.seq_lens[pre] > 0) g = pre;
     }
-    const bool has = v[0];
-    for (int l = 0; l < 2; ++l) v[l] = sum(v[l], n - i0, total[l]);
-    if (has) sorted[ns + v[0]] = i, group_of[ns + v[0]] = g, place[ns + v[0]] = n_sorted_tok + v[1];
-    ns += total[0];
-    n_sorted_tok += total[1];
+    int rows, toks;
+    const int at = ns + sum(tok > 0, n - i0, rows), before = n_sorted_tok + sum(tok, n - i0, toks);
+    if (tok > 0) sorted[at] = i, group_of[at] = g, place[at] = before;
+    ns += rows;
+    n_sorted_tok += toks;
   }
   __syncthreads();
   if (bad) {
@@ -193,49 +194,49 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       *p.head = head;
       if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
     }
-    #pragma unroll 1
+#pragma unroll 1
     for (int c = threadIdx.x; c < MAX_CTAS * WORKERS; c += THREADS) p.work[c] = make_int2(0, 0);
     return;
   }
-  #pragma unroll 1
+#pragma unroll 1
   for (int t = threadIdx.x; t < n_sorted_tok; t += THREADS) p.rec[t] = make_int4(-1, 0, -1, 0);
-  #pragma unroll 1
+#pragma unroll 1
   for (int i = threadIdx.x + 1; i < ns; i += THREADS)
     if (group_of[i] < group_of[i - 1]) unsorted = 1;
   __syncthreads();
   if (unsorted) {
     int m = 32;
-    #pragma unroll 1
+#pragma unroll 1
     while (m < ns) m <<= 1;
-    #pragma unroll 1
+#pragma unroll 1
     for (int i = threadIdx.x; i < m; i += THREADS)
       keys[i] = i < ns ? static_cast<uint32_t>(group_of[i]) << ROW_BITS | sorted[i] : 0xffffffffu;
     __syncthreads();
     sort_keys(keys, m);
     __syncthreads();
     int carry = 0;
-    #pragma unroll 1
+#pragma unroll 1
     for (int i0 = 0; i0 < ns; i0 += THREADS) {
       const int i = i0 + threadIdx.x;
-      int v[1] = {0}, total[1];
+      int tok = 0, total;
       if (i < ns) {
         sorted[i] = keys[i] & ((1 << ROW_BITS) - 1);
         group_of[i] = keys[i] >> ROW_BITS;
-        v[0] = tokens_of(sorted[i]);
+        tok = tokens_of(sorted[i]);
       }
-      v[0] = sum(v[0], ns - i0, total[0]);
-      if (i < ns) place[i] = carry + v[0];
-      carry += total[0];
+      const int before = carry + sum(tok, ns - i0, total);
+      if (i < ns) place[i] = before;
+      carry += total;
     }
   }
   if (threadIdx.x == 0) place[ns] = n_sorted_tok;
   __syncthreads();
   // a group's tokens: its rows stand together
-  #pragma unroll 1
+#pragma unroll 1
   for (int i = threadIdx.x; i < ns; i += THREADS)
     if (i == 0 || group_of[i - 1] != group_of[i]) first_tok[group_of[i]] = place[i];
   __syncthreads();
-  #pragma unroll 1
+#pragma unroll 1
   for (int i = threadIdx.x; i < ns; i += THREADS)
     if (i + 1 == ns || group_of[i + 1] != group_of[i]) group_tok[group_of[i]] = place[i + 1] - first_tok[group_of[i]];
   __syncthreads();
@@ -315,18 +316,16 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
 
   // items, by the last row of each key
   int n_items = 0, n_runs = 0;
-  #pragma unroll 1
+#pragma unroll 1
   for (int i0 = 0; i0 < nl; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     const int k = i < nl ? key[i] : 0;
-    int v[1] = {0}, total[1], tok = 0;
+    int count = 0, total, tok = 0;
     if (i < nl && (i + 1 == nl || key[i + 1] != k)) {
       tok = place[i + 1] - first_tok[k];
-      v[0] = in_cuts(k, tok + cut_of(k) - 1);
+      count = in_cuts(k, tok + cut_of(k) - 1);
     }
-    const int count = v[0];
-    v[0] = sum(v[0], nl - i0, total[0]);
-    const int at = n_items + v[0];
+    const int at = n_items + sum(count, nl - i0, total);
     if (count > 0) first_item[k] = at;
     spread(count, [&](bool on, int src, int c) {
       const int k_ = of_lane(k, src), at_ = of_lane(at, src), tok_ = of_lane(tok, src);
@@ -339,17 +338,17 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       it.flags = is_few(k_) ? ITEM_FEW | (k_ == 2 * n + 1 ? 0u : ITEM_ALONE) : ITEM_ALONE;
       items[at_ + c] = it;
     });
-    n_items += total[0];
+    n_items += total;
   }
   __syncthreads();
 
   // runs, by their rows: a row has its own run in each item that has tokens of it (of tiles: unless a few item has its own
   // keys), and writes the prefix's in each item that begins with it.  A token with a few item beside its tiles spoils the
   // tiles' being alone.
-  #pragma unroll 1
+#pragma unroll 1
   for (int i0 = 0; i0 < nl; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
-    int v[1] = {0}, total[1], in = 0, tok = 0, k0 = 0, n_in = 0, k = 0, row = 0;
+    int count = 0, total, in = 0, tok = 0, k0 = 0, n_in = 0, k = 0, row = 0;
     bool own = false, beside = false;
     if (i < nl) {
       k = key[i], row = list[i];
@@ -362,10 +361,9 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       own = is_few(k) || !small(row);
       beside = k < n && small(row) && a.seq_lens[row] > 0;
       // items whose first token is one of the row's: those up to k1 from the first that begins at or behind `in`
-      v[0] = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - in_cuts(k, in + cut - 1) + 1 : 0);
+      count = (own ? n_in : 0) + (prefix_of(k) >= 0 ? k1 - in_cuts(k, in + cut - 1) + 1 : 0);
     }
-    v[0] = sum(v[0], nl - i0, total[0]);
-    const int at = n_runs + v[0];
+    const int at = n_runs + sum(count, nl - i0, total);
     if (i < nl) row_run[i] = at;
     spread(n_in, [&](bool on, int src, int c) {
       const int k_ = of_lane(k, src), in_ = of_lane(in, src), tok_ = of_lane(tok, src), row_ = of_lane(row, src);
@@ -386,19 +384,19 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       const int seen = max(0, a.seq_lens[row_] - (in_ + tok_ - hi));  // own keys of its last token here
       runs[at_] = Run{row_, 0, in_units(is_few(k_), seen), seen, lo - item * cut, hi - item * cut, a.tok_off[row_] + lo - in_, 0};
     });
-    n_runs += total[0];
+    n_runs += total;
   }
   __syncthreads();
 
   // eight lanes an item: where its runs' pages begin
-  #pragma unroll 1
+#pragma unroll 1
   for (int c = threadIdx.x / 8; c < n_items; c += THREADS / 8) {
     const int part = threadIdx.x & 7;
     const uint32_t mask = 0xffu << (lane & 24);
     Item& it = items[c];
     const int run0 = it.run, it_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - run0;
     int pages = 0, end0 = 0, begin1 = INT_MAX;
-    #pragma unroll 1
+#pragma unroll 1
     for (int r0 = 0; r0 < it_runs; r0 += 8) {
       Run* run = runs + run0 + r0 + part;
       const bool on = r0 + part < it_runs;
@@ -436,7 +434,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   // a warp some rows: their tokens' items and own columns
   {
     const int rows_a_warp = (nl + WARPS - 1) / WARPS, end = min(nl, (warp + 1) * rows_a_warp);
-    #pragma unroll 1
+#pragma unroll 1
     for (int i0 = warp * rows_a_warp; i0 < end; i0 += 32) {
       const int i = i0 + lane;
       int k = 0, in = 0, tok = 0, t0 = 0, own = 0, o0 = 0, run0 = 0, k0 = 0;
@@ -472,7 +470,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
 
   // the lines: the items of tiles come first
   unsigned long long line = 0;
-  #pragma unroll 1
+#pragma unroll 1
   for (int i0 = 0; i0 < n_items; i0 += THREADS) {
     const int i = i0 + threadIdx.x;
     const unsigned long long v = i < n_items ? static_cast<unsigned long long>(Hkv) * length_of(items[i]) : 0;
@@ -487,7 +485,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     if (lane == 31) lines[warp] = inc;
     __syncthreads();
     unsigned long long before = line;
-    #pragma unroll 1
+#pragma unroll 1
     for (int w = 0; w < warp && w * 32 < n_items - i0; ++w) before += lines[w];
     before += inc - v;
     if (i < n_items) {
@@ -499,7 +497,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       }
     }
     if (i0 + THREADS < n_items) {
-      #pragma unroll 1
+#pragma unroll 1
       for (int w = 0; w < WARPS; ++w) line += lines[w];
       __syncthreads();
     }
@@ -519,7 +517,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   if (fits && tile_ctas > 0) share = max(share, (static_cast<uint32_t>(tiles_line) + tile_ctas - 1) / tile_ctas);
   if (fits && few_ctas > 0) few_share = max(few_share, (static_cast<uint32_t>(few_line) + few_ctas * WORKERS - 1) / (few_ctas * WORKERS));
   const Divisor by_share(share), by_few_share(few_share);
-  #pragma unroll 1
+#pragma unroll 1
   for (int i = first_few + threadIdx.x; i < n_items; i += THREADS) items[i].start -= static_cast<uint32_t>(tiles_line);
   __syncthreads();
   const int n_flat = fits ? n_items * Hkv : 0;
@@ -593,11 +591,11 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   }
   // what the attention's kernels read of items and runs
   if (in_shared & ITEMS_SHARED)
-    #pragma unroll 1
+#pragma unroll 1
     for (int i = threadIdx.x; i < n_items * static_cast<int>(sizeof(Item) / 16); i += THREADS)
       reinterpret_cast<int4*>(p.items)[i] = reinterpret_cast<const int4*>(items)[i];
   if (in_shared & RUNS_SHARED)
-    #pragma unroll 1
+#pragma unroll 1
     for (int i = threadIdx.x; i < n_runs * static_cast<int>(sizeof(Run) / 16); i += THREADS)
       reinterpret_cast<int4*>(p.runs)[i] = reinterpret_cast<const int4*>(runs)[i];
   __syncthreads();
@@ -659,7 +657,7 @@ int64_t shared_plan_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens) 
 cudaError_t launch_shared_plan(const SharedPlanArgs& a, int num_sms, cudaStream_t st) {
   const int n = a.lay.n_seqs, G = a.Hq / a.lay.n_kv_heads;
   int n_keys = 32, in_shared = 0;
-  #pragma unroll 1
+#pragma unroll 1
   while (n_keys < n) n_keys <<= 1;
   int64_t bytes = 4 * static_cast<int64_t>(n_keys);
   auto take = [&](int what, int64_t more) {

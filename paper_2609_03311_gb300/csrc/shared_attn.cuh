@@ -37,11 +37,12 @@ constexpr int WORKERS = 8;  // warps of a CTA that take few items
 // Lengths on the lines.  Tiles, about 480 clocks each: a block of keys that all rows see, another block (masked, and often of
 // one tile), an entry's start and end.  Few items, about 1.5 us of a warp each (a CTA's eight share the SM's part of the
 // memory's rate): a piece; an entry's start and end.  Fitted to the CTAs' times: 2,880 clocks a whole block, 5,200 to 6,900
-// another, 10,200 to 12,200 an entry.
+// another, 10,200 to 12,200 an entry.  Queries of 16 documents: 163 us; other blocks at 10: 164.5, 14: 168; entries at 14:
+// 165, 26: 167.  Ragged documents: a few entry at 4 53.0 us, at 2 53.4.
 constexpr uint32_t WHOLE_BLOCK = 6, OTHER_BLOCK = 12, FEW_PIECE = 1;
 __host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 : 20; }
 constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
-constexpr uint32_t MIN_FEW_SHARE = 6;
+constexpr uint32_t MIN_FEW_SHARE = 3;  // one token on 536 keys: 8.2 us; 2: 8.5 (more parts to join), 4: 8.9, 6: 9.5
 
 struct alignas(16) Run {
   int row;    // table row

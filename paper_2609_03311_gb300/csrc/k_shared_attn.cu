@@ -20,7 +20,7 @@
 //   2,048 rows of 32 heads over 16,384 keys: 351 us, 1.57 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
 //   cores work 2,050: a tile's S, softmax, P V and next S wait for one another (TMEM, full with two of S and of O, has no
 //   room for a second S), so a second tile fills the gaps and P goes over in halves (371 us when it went as one).  64 rows of
-//   a token over 32,768 keys: 46.5 us, 38 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
+//   a token over 32,768 keys: 45 us, 38 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
 //   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
 //   box by TMA takes about 80 ns of an SM (256 tokens over 64 ragged documents in pages of 16: 73 us by TMA, 63 with 16-byte
 //   copies then; 53 now, 4.8 TB/s).
@@ -1106,10 +1106,10 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // ------------------------------------------------------------------ joining the parts
-// A warp a row, JOIN_ROWS rows of an entry at a time.  Bound by latency where few rows have many parts, so what the plan says
+// A warp a row, JOIN_ROWS rows of an entry at a time, or two warps a row of many parts.  Bound by latency where few rows have many parts, so what the plan says
 // of a CTA's first piece is read while the attention ends (it was complete before that began), the first values are asked for
 // beside the maxima and sums, and four parts are on their way at once (eight take registers that cost more rows at once).
-// 64 rows of a token, 19 parts each: about 8 us; 5,000 tokens of 16 documents, of which a third has two parts: 14.
+// 64 rows of a token, 19 parts each: about 7 us; 5,000 tokens of 16 documents, of which a third has two parts: 14.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
     k_shared_join(const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan, int n_ctas) {
@@ -1119,6 +1119,9 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
   const float* part_o = reinterpret_cast<const float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, n_ctas)) + lane * E;
   const Head head = *plan.head;
   const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, n_ctas);
+  __shared__ float halves[2][JOIN_ROWS / 2][D];
+  __shared__ float2 halves_ml[2][JOIN_ROWS / 2];
+  int turn = 0;
   bool waited = false;
   auto wait_once = [&] {
     if (!waited) pdl_wait(), pdl_trigger();
@@ -1130,16 +1133,19 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
   for (int j = blockIdx.x; good && j < head.n_join; j += gridDim.x) {
     const Piece piece = next;
     if (j + static_cast<int>(gridDim.x) < head.n_join) next = plan.join[j + gridDim.x];
-    const int row = piece.row + (threadIdx.x >> 5);
+    // two warps a row, half of the parts each, where there are many
+    const bool two = piece.parts > PARTS_A_WARP;
+    const int warp = threadIdx.x >> 5, second = two ? warp & 1 : 0, row = piece.row + (two ? warp >> 1 : warp);
     if (row >= piece.rows) continue;
     const int t = plan.order[piece.tok + row / G], h = piece.h * G + row % G;
     float o[E], m = -INFINITY, l = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) o[i] = 0.f;
     // the piece's own entry, then the few entry that has a row's own keys beside tiles
-    uint32_t parts = piece.parts, rows = piece.rows, beside_parts = 0, beside_rows = 0;
-    int64_t row0 = piece.part_row + static_cast<int64_t>(row), beside_row0 = 0;
-    if (piece.beside) {
+    const uint32_t half = (piece.parts + 1) / 2;
+    uint32_t parts = !two ? piece.parts : second ? piece.parts - half : half, rows = piece.rows, beside_parts = 0, beside_rows = 0;
+    int64_t row0 = piece.part_row + row + static_cast<int64_t>(second ? half : 0) * rows, beside_row0 = 0;
+    if (piece.beside && second == static_cast<int>(two)) {
       const int4 rec = plan.rec[t];
       if (rec.z >= 0) {
         const Item it = plan.items[rec.z];
@@ -1193,6 +1199,25 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
         }
       }
     }
+    if (two) {
+      // the second warp's half to the first; the places are used by turns, so that one barrier is enough
+      turn ^= 1;
+      float* at = halves[turn][warp >> 1] + lane * E;
+      if (second) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) at[i] = o[i];
+        if (lane == 0) halves_ml[turn][warp >> 1] = make_float2(m, l);
+      }
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp >> 1)) : "memory");
+      if (second) continue;
+      const float2 x = halves_ml[turn][warp >> 1];
+      const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
+      const float mine = ex2(m - base), other = ex2(x.x - base);
+      l = l * mine + x.y * other;
+      m = top;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] = o[i] * mine + at[i] * other;
+    }
     // scores in order, values not: perhaps a value that the row does not see
     bool nan = false;
 #pragma unroll
@@ -1234,7 +1259,7 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +
-                         static_cast<int64_t>(a.max_tokens) * a.Hq / JOIN_ROWS;
+                         static_cast<int64_t>(a.max_tokens) * a.Hq / (JOIN_ROWS / 2);
   const int64_t held = JOIN_CTAS * static_cast<int64_t>(num_sms);
   return launch_dependent(k_shared_join<T, D>, dim3(static_cast<unsigned>(pieces < held ? pieces : held)), 32 * JOIN_ROWS, 0, st, a,
                           plan, n_ctas);

@@ -538,11 +538,11 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       if (!right_away) {
         rows = segs * it.n_tok * G * copies_of(it, G);
         // rows of a few item beside tiles are joined by the tiles' pieces
-        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) != ITEM_FEW) pieces = (it.n_tok * G + JOIN_ROWS - 1) / JOIN_ROWS;
+        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) != ITEM_FEW) pieces = (it.n_tok * G + rows_a_piece(segs * copies_of(it, G)) - 1) / rows_a_piece(segs * copies_of(it, G));
       }
     }
-    // two counts a sum: no more segments than entries and shares, 32 pieces an entry at most
-    static_assert(2 * TILE / JOIN_ROWS * THREADS < 1 << 16 && THREADS + SHARES < 1 << 15, "a count takes 16 bits");
+    // two counts a sum: no more segments than entries and shares, 64 pieces an entry at most
+    static_assert(4 * TILE / JOIN_ROWS * THREADS < 1 << 16 && THREADS + SHARES < 1 << 15, "a count takes 16 bits");
     int both, total;
     const uint32_t at = sum(segs << 16 | pieces, n_flat - f0, both);
     const int seg0 = n_segs + (at >> 16), piece0 = n_join + (at & 0xffff);
@@ -555,8 +555,9 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       if (!on) return;
       const int item = by_heads.of(f_);
       const Item& it = items[item];
-      p.join[piece] = Piece{it.tok, i * JOIN_ROWS, it.n_tok * G, f_ - item * Hkv, static_cast<uint32_t>(row0),
-                            n * static_cast<int>(copies_of(it, G)), !(it.flags & (ITEM_FEW | ITEM_ALONE)), 0};
+      const int parts = n * static_cast<int>(copies_of(it, G));
+      p.join[piece] = Piece{it.tok, i * rows_a_piece(parts), it.n_tok * G, f_ - item * Hkv, static_cast<uint32_t>(row0), parts,
+                            !(it.flags & (ITEM_FEW | ITEM_ALONE)), 0};
     });
     spread(segs, [&](bool on_, int src, int i) {
       const int f_ = of_lane(f, src), at = of_lane(seg0, src) + i, whole = of_lane(right_away, src), row0 = of_lane(part_row, src);

@@ -33,6 +33,10 @@ constexpr int BLOCK = 128;  // columns of a block of tiles
 constexpr int PIECE = 16;   // of few items
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
+// Rows of more parts than this are joined by two warps each, JOIN_ROWS / 2 of them at a time: 64 queries of one document, 19
+// parts a row, 46.3 us with one warp, 45.0 with two; one token, 12 parts, 8.1 with one, 8.6 with two.
+constexpr int PARTS_A_WARP = 12;
+__host__ __device__ inline int rows_a_piece(int parts) { return parts > PARTS_A_WARP ? JOIN_ROWS / 2 : JOIN_ROWS; }
 constexpr int WORKERS = 8;  // warps of a CTA that take few items
 // Lengths on the lines.  Tiles, about 480 clocks each: a block of keys that all rows see, another block (masked, and often of
 // one tile), an entry's start and end.  Few items, about 1.5 us of a warp each (a CTA's eight share the SM's part of the
@@ -86,7 +90,7 @@ enum : uint32_t {
   SEG_FEW = 2,
   SEG_WHOLE = 4,  // gives its rows' results right away
 };
-// Up to JOIN_ROWS rows of an entry that are to be added up from partial results.
+// Up to rows_a_piece rows of an entry that are to be added up from partial results.
 struct alignas(16) Piece {
   int tok;            // of the entry's item
   int row, rows;      // the first of them, and all of the item's
@@ -137,7 +141,7 @@ __host__ __device__ inline int64_t max_runs(int n_seqs, int G, int max_tokens) {
 }
 __host__ __device__ inline int64_t plan_scratch_ints(int64_t n_seqs) { return 15 * n_seqs + 8; }
 __host__ __device__ inline int64_t max_pieces(int n_seqs, int n_kv_heads, int G, int max_tokens) {
-  return max_items(n_seqs, G, max_tokens) * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / JOIN_ROWS;
+  return max_items(n_seqs, G, max_tokens) * n_kv_heads + static_cast<int64_t>(max_tokens) * G * n_kv_heads / (JOIN_ROWS / 2);
 }
 __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads, int G, int max_tokens) {
   uint8_t* b = static_cast<uint8_t*>(base);

@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   __shared__ int bad, unsorted;
   __shared__ unsigned long long lines[WARPS], tiles_line, both_lines;
   __shared__ int first_few;
+  __shared__ uint32_t longest[2];  // entry of tiles, of few items
   const int n = a.lay.n_seqs, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page, page_blk = BLOCK / page;
   const int tile = tokens_a_tile(G), few = tokens_a_few(G);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   int* row_run = place + 2 * n + 1;    // its first run
   int* first_tok = row_run + 2 * n;    // of a key: tokens before its first
   int* first_item = first_tok + 2 * n + 3;
-  if (threadIdx.x == 0) bad = 0, unsorted = 0, tiles_line = both_lines = 0, first_few = 0;
+  if (threadIdx.x == 0) bad = 0, unsorted = 0, tiles_line = both_lines = 0, first_few = 0, longest[0] = longest[1] = 0;
   if (threadIdx.x < 64) sums_memory[threadIdx.x >> 5][lane] = 0;
 #pragma unroll 1
   for (int c = threadIdx.x; c < SHARES; c += THREADS) first_of[c] = INT_MAX;
@@ -490,6 +491,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     before += inc - v;
     if (i < n_items) {
       items[i].start = static_cast<uint32_t>(before);  // of few items: the tiles' line before it too, for now
+      atomicMax(&longest[items[i].flags & ITEM_FEW ? 1 : 0], length_of(items[i]));
       if ((items[i].flags & ITEM_FEW) && (i == 0 || !(items[i - 1].flags & ITEM_FEW))) tiles_line = before, first_few = i;
       if (i == n_items - 1) {
         both_lines = before + v;
@@ -512,8 +514,10 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     tile_ctas = min(n_ctas - 1, max(1, __float2int_rn(n_ctas * tiles_cost / (tiles_cost + few_cost))));
   }
   const uint32_t few_ctas = n_ctas - tile_ctas;
-  // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up
-  uint32_t share = OTHER_BLOCK, few_share = MIN_FEW_SHARE;
+  // a share of tiles holds a block at least, one of few items a few pieces: each share more is a part more to be added up; of
+  // long entries more, where a share's time and that of joining the longest entry's parts meet
+  uint32_t share = max(OTHER_BLOCK, (static_cast<uint32_t>(sqrtf(TILES_JOIN * longest[0])) / WHOLE_BLOCK + 1) * WHOLE_BLOCK);
+  uint32_t few_share = max(MIN_FEW_SHARE, static_cast<uint32_t>(sqrtf(FEW_JOIN * longest[1])));
   if (fits && tile_ctas > 0) share = max(share, (static_cast<uint32_t>(tiles_line) + tile_ctas - 1) / tile_ctas);
   if (fits && few_ctas > 0) few_share = max(few_share, (static_cast<uint32_t>(few_line) + few_ctas * WORKERS - 1) / (few_ctas * WORKERS));
   const Divisor by_share(share), by_few_share(few_share);

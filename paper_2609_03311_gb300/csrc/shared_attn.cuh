@@ -48,6 +48,10 @@ __host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 :
 constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
 constexpr uint32_t MIN_FEW_SHARE = 3;  // one token on 536 keys: 8.2 us; 2: 8.5 (more parts to join), 4: 8.9, 6: 9.5
 
+// Time of joining a part by that of a length, of tiles and of few items: 20 rows over 13,295 keys, cut into 104 parts or 52: 21.0
+// and 16.5 us; 120 rows over 7,994 keys: 22.8 and 20.
+constexpr float TILES_JOIN = 0.8f, FEW_JOIN = 0.14f;
+
 struct alignas(16) Run {
   int row;    // table row
   int off;    // pages of the item before it

@@ -43,7 +43,9 @@ constexpr int WORKERS = 8;  // warps of a CTA that take few items
 // memory's rate): a piece; an entry's start and end.  Fitted to the CTAs' times: 2,880 clocks a whole block, 5,200 to 6,900
 // another, 10,200 to 12,200 an entry.  Queries of 16 documents: 163 us; other blocks at 10: 164.5, 14: 168; entries at 14:
 // 165, 26: 167.  Ragged documents: a few entry at 4 53.0 us, at 2 53.4.
-constexpr uint32_t WHOLE_BLOCK = 6, OTHER_BLOCK = 12, FEW_PIECE = 1;
+// An entry of no more than UNCUT behind its start goes whole to the CTA that it begins in: 290 tokens of six queries on 55 keys 19.0
+// us cut, 17.0 whole; at 36 ten entries of four blocks keep too many CTAs idle (15.5 to 19).
+constexpr uint32_t WHOLE_BLOCK = 6, OTHER_BLOCK = 12, FEW_PIECE = 1, UNCUT = 24;
 __host__ __device__ constexpr uint32_t entry_length(bool few) { return few ? 4 : 20; }
 constexpr uint32_t FEW_PER_TILES = 4;  // a length of few items in those of tiles
 constexpr uint32_t MIN_FEW_SHARE = 3;  // one token on 536 keys: 8.2 us; 2: 8.5 (more parts to join), 4: 8.9, 6: 9.5
@@ -187,14 +189,16 @@ __host__ __device__ inline uint32_t copies_of(const Item& it, int G) { return (i
 // The blocks of kv head h's entry on the line: where the first begins, how many are whole, and where those end.
 struct OnLine {
   uint32_t begin, whole, whole_end;
-  bool few;
+  bool few, uncut;  // uncut: all blocks count as where the first begins
   __host__ __device__ uint32_t begin_of(uint32_t b) const {
     if (few) return begin + b * FEW_PIECE;
+    if (uncut) return begin;
     return b <= whole ? begin + b * WHOLE_BLOCK : whole_end + (b - whole) * OTHER_BLOCK;
   }
   // first block that begins at or behind a place on the line
   __host__ __device__ uint32_t block_from(uint32_t at, uint32_t blocks) const {
     if (at <= begin) return 0;
+    if (uncut) return blocks;
     const uint32_t b = few ? (at - begin + FEW_PIECE - 1) / FEW_PIECE
                        : at <= whole_end ? (at - begin + WHOLE_BLOCK - 1) / WHOLE_BLOCK
                                          : whole + (at - whole_end + OTHER_BLOCK - 1) / OTHER_BLOCK;
@@ -207,13 +211,16 @@ struct OnLine {
 };
 __host__ __device__ inline OnLine blocks_from(const Item& it, uint32_t begin) {
   const uint32_t all = it.prefix_keys / BLOCK, whole = all < it.blocks ? all : it.blocks;
-  return OnLine{begin, whole, begin + whole * WHOLE_BLOCK, (it.flags & ITEM_FEW) != 0};
+  return OnLine{begin, whole, begin + whole * WHOLE_BLOCK, (it.flags & ITEM_FEW) != 0, false};
 }
 __host__ __device__ inline uint32_t length_of(const Item& it) {
   return it.blocks > 0 ? blocks_from(it, entry_length(it.flags & ITEM_FEW)).begin_of(it.blocks) : 0;
 }
 __host__ __device__ inline OnLine on_line(const Item& it, int h) {
-  return blocks_from(it, it.start + h * length_of(it) + entry_length(it.flags & ITEM_FEW));
+  const uint32_t length = length_of(it), head = entry_length(it.flags & ITEM_FEW);
+  OnLine on = blocks_from(it, it.start + h * length + head);
+  on.uncut = !on.few && length <= head + UNCUT;
+  return on;
 }
 
 }  // namespace shared_attn

@@ -8,7 +8,9 @@
 // k_shared_attn, a persistent CTA an SM, walks over its share of the plan's line (shared_attn.cuh), which holds either
 // tiles or few items.
 //   Tiles: an item of two tiles gives each block of 128 columns to the softmax groups of the tiles that it concerns, a tile
-//   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way.
+//   each; of one tile, blocks go to the groups in turn, so that one softmax runs beside the other's products either way, and
+//   the group of the last block adds the other's O to its own (left to the joining kernel as two parts, 120 rows over 7,994
+//   keys took 20.4 us for 17.4, 47 documents' queries 31.9 for 28.3).
 //     warp 0, 2  copy K and V blocks into two rings, page by page (TMA; a page's rows of a kv head lie together)
 //     warp 1     issues S = Q K^T (128 x 128, 32-bit, in TMEM) and O += P V (P in TMEM over the S it came from)
 //     warp 3     brings the rows of Q by TMA: eight tokens that follow one another, others one by one (the rows of a token
@@ -55,15 +57,16 @@ struct Smem {
   static constexpr int OFF_Q = 0;
   static constexpr int OFF_K = OFF_Q + 2 * TILE_BYTES;
   static constexpr int OFF_V = OFF_K + K_STAGES * TILE_BYTES;
-  static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // where the Q gatherer's rows lie
-  static constexpr int OFF_KEYS = OFF_ROW + 128 * 8;  // of each page of a V stage: rows that hold keys
+  static constexpr int OFF_ROW = OFF_V + V_STAGES * TILE_BYTES;  // the Q gatherer's rows' tokens
+  static constexpr int OFF_ML = OFF_ROW + 128 * 4;      // maxima and sums that one softmax group leaves to the other
+  static constexpr int OFF_KEYS = OFF_ML + 128 * 8;     // of each page of a V stage: rows that hold keys
   static constexpr int OFF_BAR = OFF_KEYS + 64;
   // few items: from 0 on, pieces of 16 columns of K and V, F_STAGES of them a warp
   static constexpr int F_STAGES = D == 128 ? 3 : 6;
   static_assert(WORKERS * F_STAGES * 2 * HALVES * PIECE * 128 <= OFF_ROW, "the few items' pieces");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
-                       O_FULL = P_FULL + 4, DRAIN = O_FULL + 2, N_BARS = DRAIN + 1;
+                       O_FULL = P_FULL + 4, ML_FULL = O_FULL + 2, ML_EMPTY = ML_FULL + 1, DRAIN = ML_EMPTY + 1, N_BARS = DRAIN + 1;
   static constexpr int BYTES = 1024 + OFF_BAR + N_BARS * 8 + 16;
   static_assert(V_STAGES * 8 <= 64, "a byte a page");
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
@@ -113,7 +116,7 @@ __device__ __forceinline__ void add2(float& x, float& y, float bx, float by) {
 }
 // Shares of the launch's registers (384 threads x 168): little for the warps that copy and issue, more where rows of S
 // are held.
-constexpr int REGS_FEW = 152, REGS_MANY = 176;
+constexpr int REGS_FEW = 136, REGS_MANY = 184;
 static_assert(128 * REGS_FEW + 256 * REGS_MANY <= 384 * 168, "more registers than the launch has are waited for without end");
 __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW)); }
 __device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY)); }
@@ -239,6 +242,29 @@ __device__ __forceinline__ uint32_t bits_in(int lo, int hi) {
 
 __device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }  // a NaN stays one
 __device__ __forceinline__ float lse_of(float m, float l) { return (m + log2f(l)) * 0.6931471805599453f; }
+
+// O of the softmax group at o_col += O of the other one; the groups' maxima and sums before, theirs together after.  Not inlined,
+// as what is rare should not stand between the blocks' loop and its instructions: with this and the loops over V's tails
+// unrolled, queries of 16 documents took 169 us, so 160.
+template <int D>
+__device__ __noinline__ float2 add_other(uint32_t o_col, float2 mine, float2 other) {
+  const float top = fmaxf(mine.x, other.x), base = top == -INFINITY ? 0.f : top;
+  const float by = ex2(mine.x - base), other_by = ex2(other.x - base);
+#pragma unroll 1
+  for (int c = 0; c < D; c += 16) {
+    uint32_t v[32], x[16];
+    tmem_ld16x2(o_col + c, (o_col ^ 128u) + c, v);
+    tmem_ld_wait_for(v);
+    // a group that summed nothing up leaves no values
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      x[i] = __float_as_uint((mine.y != 0.f ? __uint_as_float(v[i]) * by : 0.f) +
+                             (other.y != 0.f ? __uint_as_float(v[16 + i]) * other_by : 0.f));
+    tmem_st16(o_col + c, x);
+  }
+  tmem_st_wait();
+  return make_float2(top, mine.y * by + other.y * other_by);
+}
 
 // One row alone by a warp, a key at a time, for rows whose products took in a value that they do not see; lane l holds
 // elements [E l, E l + E) of the head.
@@ -504,7 +530,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (threadIdx.x == 0) {
     gave_up = 0;
-    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), i >= L::P_FULL && i < L::P_FULL + 4 ? 4 : 1);
+    for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), (i >= L::P_FULL && i < L::P_FULL + 4) || i == L::ML_FULL || i == L::ML_EMPTY ? 4 : 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q8);
     tma_prefetch_desc(&tm_q1);
@@ -791,7 +817,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few();
-    const uint4** row = reinterpret_cast<const uint4**>(smem + L::OFF_ROW);  // where the rows of other tokens lie
+    int* row = reinterpret_cast<int*>(smem + L::OFF_ROW);  // tokens of the rows
     Walk walk(plan, work);
     Groups groups;
     uint32_t used = 0, par = 0, filled = 0;  // a bit a group
@@ -812,11 +838,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int i = 1; i < 8; ++i) run = run & (tok[8 * lane + i] == first + i);
         }
         const uint32_t runs = __ballot_sync(0xffffffffu, run);
-        for (int r = lane; !a.q_boxes && r < rows; r += 32) {
-          const int i = r / G;
-          row[r] = reinterpret_cast<const uint4*>(q + static_cast<int64_t>(tok[i]) * a.q_tok +
-                                                  static_cast<int64_t>(s.h * G + r - i * G) * a.q_head);
-        }
+        for (int r = lane; !a.q_boxes && r < rows; r += 32) row[r] = tok[r / G];
         __syncwarp();
         if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
@@ -850,7 +872,9 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int r = r0 + i * STEP;
-              if (r < rows) cp_async16(dst + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4), row[r] + c, true);
+              if (r < rows)
+                cp_async16(dst + (c >> 3) * HALF_BYTES + r * 128 + (((c & 7) ^ (r & 7)) << 4),
+                           q + row[r] * a.q_tok + static_cast<int64_t>(s.h * G + r % G) * a.q_head + 8 * c, true);
             }
           }
           cp_async_commit();
@@ -883,8 +907,10 @@ __global__ void __launch_bounds__(THREADS, 1)
     auto ready_v = [&](int stage, uint32_t phase, int cols) {
       if (!mbar_wait_warp(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
       const int page = a.lay.page;
+#pragma unroll 1
       for (int pg = 0; pg * page < cols; ++pg) {
         const int from = smem[L::OFF_KEYS + stage * 8 + pg];
+#pragma unroll 1
         for (int i = r; i < (page - from) * 8 * L::HALVES; i += 128) {
           const int at = pg * page + from + i / (8 * L::HALVES), c = i % (8 * L::HALVES);
           *reinterpret_cast<uint4*>(smem + L::OFF_V + stage * L::TILE_BYTES + (c >> 3) * HALF_BYTES + at * 128 + (c & 7) * 16) =
@@ -902,7 +928,15 @@ __global__ void __launch_bounds__(THREADS, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(L::P_FULL + 2 * half + w));
     };
+    // The group that took the last block of a segment of one tile adds the other's O to its own; the other begins a new one
+    // when that is done.  In o_par beside O's parity, where the blocks' loop has no register to spare: that of such sums, and
+    // whether this group left its O to the other.
+    constexpr uint32_t SUMS = 2, LEFT = 4;
     while (ok && walk.next(s)) {
+      if (o_par & LEFT) {
+        if (!mbar_wait_warp(bar(L::ML_EMPTY), (o_par & SUMS) == 0, err, WAIT_TIMEOUT_NS)) break;
+        o_par &= ~LEFT;
+      }
       const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0);
       const bool valid = r < n * G, any = __any_sync(0xffffffffu, valid);
       // the row sees columns [0, prefix) and [own0, own1)
@@ -913,7 +947,6 @@ __global__ void __launch_bounds__(THREADS, 1)
         const int2 own = own_columns[s.tok + t0 + r / G];
         own0 = own.x, own1 = own.y;
       }
-      const uint32_t first_group = s.flags & SEG_TWO ? w : groups.turn;
       float m = -INFINITY, l = 0.f;
       int done = 0;
       for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
@@ -1018,12 +1051,33 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       if (!ok) break;
       if (done > 0) {
-        if (!mbar_wait_warp(bar(L::O_FULL + w), o_par, err, WAIT_TIMEOUT_NS)) break;
+        if (!mbar_wait_warp(bar(L::O_FULL + w), o_par & 1u, err, WAIT_TIMEOUT_NS)) break;
         o_par ^= 1u;
         tc_fence_after();
       }
       // what only the end of a segment needs is read again here, not held in registers over its blocks
       const Segment& e = walk.segs[walk.at - 1];
+      if (!(e.flags & SEG_TWO)) {
+        float2* ml = reinterpret_cast<float2*>(smem + L::OFF_ML);
+        const bool last = groups.turn != static_cast<uint32_t>(w), both = e.b1 - e.b0 > 1;
+        if (both && !last) {
+          ml[r] = make_float2(m, l);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::ML_FULL));
+          o_par |= LEFT;
+        } else if (both) {
+          if (!mbar_wait_warp(bar(L::ML_FULL), (o_par & SUMS) != 0, err, WAIT_TIMEOUT_NS)) break;
+          tc_fence_after();
+          const float2 sum = add_other<D>(o_col, make_float2(m, l), ml[r]);
+          m = sum.x, l = sum.y;
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(L::ML_EMPTY));
+        }
+        if (both) o_par ^= SUMS;
+        if (!last) continue;
+      }
       if (e.flags & SEG_WHOLE) {
         // ---- the whole entry: the rows' results
         const int t = token, h = e.h * G + r % G;
@@ -1073,8 +1127,7 @@ __global__ void __launch_bounds__(THREADS, 1)
         float2* ml = reinterpret_cast<float2*>(a.ws);
         float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
         const bool two = e.flags & SEG_TWO;
-        const uint32_t second = !two && first_group != static_cast<uint32_t>(w) ? e.n_tok * G : 0;
-        const int64_t row = static_cast<int64_t>(e.part_row) + second + (two ? w * TT * G : 0) + r;
+        const int64_t row = static_cast<int64_t>(e.part_row) + (two ? w * TT * G : 0) + r;
         if (valid) ml[row] = make_float2(m, l);
         float* dst = part_o + row * D;
 #pragma unroll 1

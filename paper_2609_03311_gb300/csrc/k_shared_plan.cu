@@ -538,11 +538,11 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       const Divisor& by = it.flags & ITEM_FEW ? by_few_share : by_share;
       cta0 = by.of(on.begin);
       if (it.blocks > 0) segs = by.of(on.begin_of(it.blocks - 1)) - cta0 + 1;
-      right_away = segs == 1 && (it.flags & ITEM_ALONE) && copies_of(it, G) == 1;
+      right_away = segs == 1 && (it.flags & ITEM_ALONE);
       if (!right_away) {
-        rows = segs * it.n_tok * G * copies_of(it, G);
+        rows = segs * it.n_tok * G;
         // rows of a few item beside tiles are joined by the tiles' pieces
-        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) != ITEM_FEW) pieces = (it.n_tok * G + rows_a_piece(segs * copies_of(it, G)) - 1) / rows_a_piece(segs * copies_of(it, G));
+        if ((it.flags & (ITEM_FEW | ITEM_ALONE)) != ITEM_FEW) pieces = (it.n_tok * G + rows_a_piece(segs) - 1) / rows_a_piece(segs);
       }
     }
     // two counts a sum: no more segments than entries and shares, 64 pieces an entry at most
@@ -555,11 +555,10 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     if (f < n_flat && f == first_few * Hkv) first_of[tile_ctas] = seg0;  // the end of tiles
     if (f < n_flat) p.part[f] = part_row;
     spread(pieces, [&](bool on, int src, int i) {
-      const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i, row0 = of_lane(part_row, src), n = of_lane(segs, src);
+      const int f_ = of_lane(f, src), piece = of_lane(piece0, src) + i, row0 = of_lane(part_row, src), parts = of_lane(segs, src);
       if (!on) return;
       const int item = by_heads.of(f_);
       const Item& it = items[item];
-      const int parts = n * static_cast<int>(copies_of(it, G));
       p.join[piece] = Piece{it.tok, i * rows_a_piece(parts), it.n_tok * G, f_ - item * Hkv, static_cast<uint32_t>(row0), parts,
                             !(it.flags & (ITEM_FEW | ITEM_ALONE)), 0};
     });
@@ -581,7 +580,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       sg.prefix_keys = it.prefix_keys, sg.pages = it.pages;
       sg.end0 = it.end0, sg.begin1 = it.begin1, sg.prefix_blocks = it.prefix_blocks;
       sg.flags = (two_tiles(it, G) ? SEG_TWO : 0u) | (of_few ? SEG_FEW : 0u) | (whole ? SEG_WHOLE : 0u);
-      sg.part_row = static_cast<uint32_t>(row0) + i * copies_of(it, G) * it.n_tok * G;
+      sg.part_row = static_cast<uint32_t>(row0) + i * it.n_tok * G;
       const int page0 = sg.b0 * (of_few ? 1 : page_blk);
       int lo = 0, hi = it.n_runs - 1;
       while (lo < hi) {  // the last run that begins at or before the page (runs without pages share their successor's place)

@@ -173,10 +173,10 @@ __host__ __device__ inline Plan plan_view(void* base, int n_seqs, int n_kv_heads
   p.bytes = at;
   return p;
 }
-// Rows of partial results at most.  Of tiles, a token's rows are left once where they have a few item too, or twice where
-// the item has one tile (its two halves of the blocks); of few items once.  Either kind of tiles holds the tokens of some
-// row with few tokens or ends a prefix, so there is at most one for every row.  A boundary between CTAs makes one segment
-// more, of at most 256 rows, or two of what would have given its rows' results right away.
+// Rows of partial results, at most and with room to spare.  Of tiles, a token's rows are left once where they have a few item
+// too (counted twice here), of few items once; a tile item holds the tokens of some row with few tokens or ends a prefix, so
+// there is at most one for every row.  A boundary between CTAs makes one segment more, of at most 256 rows, or two of what would
+// have given its rows' results right away.
 __host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int G, int max_tokens, int n_ctas) {
   const int64_t all = static_cast<int64_t>(max_tokens) * G, n = n_seqs;
   const int64_t tiles = 2 * all < 4 * TILE * n ? 2 * all : 4 * TILE * n, few = all < FEW * n ? all : FEW * n;
@@ -185,7 +185,6 @@ __host__ __device__ inline int64_t max_part_rows(int n_seqs, int n_kv_heads, int
 }
 
 __host__ __device__ inline bool two_tiles(const Item& it, int G) { return !(it.flags & ITEM_FEW) && it.n_tok > tokens_a_tile(G); }
-__host__ __device__ inline uint32_t copies_of(const Item& it, int G) { return (it.flags & ITEM_FEW) || two_tiles(it, G) ? 1 : 2; }
 // The blocks of kv head h's entry on the line: where the first begins, how many are whole, and where those end.
 struct OnLine {
   uint32_t begin, whole, whole_end;

@@ -19,10 +19,10 @@
 //                2^8 (P stays within the type's range until then)
 //   P is rounded to the inputs' type for its product with V, as the tensor cores take it; maxima, sums, O and parts stay in 32
 //   bits, and a row's sum adds up P before the rounding.
-//   2,048 rows of 32 heads over 16,384 keys: 351 us, 1.57 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
+//   2,048 rows of 32 heads over 16,384 keys: 352 us, 1.56 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
 //   cores work 2,050: a tile's S, softmax, P V and next S wait for one another (TMEM, full with two of S and of O, has no
 //   room for a second S), so a second tile fills the gaps and P goes over in halves (371 us when it went as one).  64 rows of
-//   a token over 32,768 keys: 45 us, 38 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
+//   a token over 32,768 keys: 44 us, 37 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
 //   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
 //   box by TMA takes about 80 ns of an SM (256 tokens over 64 ragged documents in pages of 16: 73 us by TMA, 63 with 16-byte
 //   copies then; 53 now, 4.8 TB/s).
@@ -115,7 +115,7 @@ __device__ __forceinline__ void add2(float& x, float& y, float bx, float by) {
       : "f"(bx), "f"(by));
 }
 // Shares of the launch's registers (384 threads x 168): little for the warps that copy and issue, more where rows of S
-// are held.
+// are held (152 and 176: 2,048 rows 353 us for 351.7).
 constexpr int REGS_FEW = 136, REGS_MANY = 184;
 static_assert(128 * REGS_FEW + 256 * REGS_MANY <= 384 * 168, "more registers than the launch has are waited for without end");
 __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW)); }

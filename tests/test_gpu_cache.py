@@ -754,3 +754,12 @@ def test_extend_refuses_a_batch_of_another_layout():
         dopr.cache_extend(layout, lens, tables, free, n_free, i32([1] * 40), 40, out=out)
     dopr.cache_extend(layout, lens, tables, free, n_free, i32([1] * 40), 40, out=whole)
     assert whole.seq_lens.tolist() == [6] * 40
+
+
+@pytest.mark.parametrize("m", [0, 100, 128, 129, 256, 300, 1000, 4100])
+@pytest.mark.parametrize("d,page,own,new", [(128, 64, 90, 20), (64, 16, 300, 9), (128, 32, 5, 5)])
+def test_attention_of_one_tile_with_blocks_in_turn(d, page, own, new, m):
+    # 17 to 128 rows a kv head: two groups take the blocks in turn, and one adds up both; of one block, of rows that see the
+    # keys of one group alone, behind another document's tile and before a tile of its own
+    b = Batch(8, 2, d, BF, page, [m, 150], [(0, own, new), (1, 40, 25), (0, 3, 6), (-1, 70, 30)], seed=m + d, dirt=math.inf)
+    b.check(b.run())

@@ -159,13 +159,10 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   __syncthreads();
   Head head{};
   head.share = head.few_share = 1;
-  head.n_seqs = n;
-  head.n_kv_heads = Hkv;
   head.Hq = a.Hq;
   head.max_tokens = a.max_tokens;
   head.n_ctas = n_ctas;
-  head.head_dim = a.lay.head_dim;
-  head.page = page;
+  head.lay = a.lay;
   auto tokens_of = [&](int i) { return a.tok_off[i + 1] - a.tok_off[i]; };
 
   // checks, and the rows with tokens

@@ -110,12 +110,14 @@ struct alignas(16) Head {
   int tokens, n_items, n_flat, n_join;
   uint32_t share, few_share;  // of the lines: a CTA's part of tiles, a warp's of few items
   int tile_ctas;              // the CTAs that take tiles
-  int n_seqs, n_kv_heads, Hq, max_tokens, n_ctas, head_dim, page;  // what the plan was made for
-  int pad[2];
+  // what the plan was made for: its runs' pages lie in tables of max_blocks entries a row
+  int Hq, max_tokens, n_ctas;
+  dopr_cache_layout lay;
 };
 __host__ __device__ inline bool made_for(const Head& h, const dopr_cache_layout& lay, int Hq, int max_tokens, int n_ctas) {
-  return h.n_seqs == lay.n_seqs && h.n_kv_heads == lay.n_kv_heads && h.Hq == Hq && h.max_tokens == max_tokens &&
-         h.n_ctas == n_ctas && h.head_dim == lay.head_dim && h.page == lay.page;
+  return h.lay.n_blocks == lay.n_blocks && h.lay.page == lay.page && h.lay.n_kv_heads == lay.n_kv_heads &&
+         h.lay.head_dim == lay.head_dim && h.lay.dtype == lay.dtype && h.lay.n_seqs == lay.n_seqs &&
+         h.lay.max_blocks == lay.max_blocks && h.Hq == Hq && h.max_tokens == max_tokens && h.n_ctas == n_ctas;
 }
 constexpr int SHARES = MAX_CTAS * WORKERS + 2;  // at most: a CTA has one or WORKERS
 struct Plan {

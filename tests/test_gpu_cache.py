@@ -763,3 +763,28 @@ def test_attention_of_one_tile_with_blocks_in_turn(d, page, own, new, m):
     # keys of one group alone, behind another document's tile and before a tile of its own
     b = Batch(8, 2, d, BF, page, [m, 150], [(0, own, new), (1, 40, 25), (0, 3, 6), (-1, 70, 30)], seed=m + d, dirt=math.inf)
     b.check(b.run())
+
+
+# ------------------------------------------------------------------ calls that the documentation speaks of
+@pytest.mark.parametrize("change", [dict(n_blocks=11), dict(n_blocks=20), dict(page=32), dict(n_kv_heads=1), dict(n_kv_heads=4),
+                                    dict(head_dim=128), dict(dtype=BF), dict(n_seqs=2), dict(n_seqs=4), dict(max_blocks=1),
+                                    dict(max_blocks=6), dict(max_blocks=8), dict(hq=8), dict()])
+def test_attention_refuses_a_plan_of_another_layout(change):
+    # every field by itself; tables, pools and the plan's room are large enough for any of them
+    b = Batch(4, 2, 64, HF, 16, [100], [(0, 5, 2), (0, 6, 1)], seed=1)
+    a = dict(n_blocks=b.layout.n_blocks, page=16, n_kv_heads=2, head_dim=64, dtype=HF, n_seqs=3, max_blocks=b.mb, hq=4)
+    assert (a["n_blocks"], a["max_blocks"]) == (12, 7)
+    plan = dopr.shared_attention_plan(b.layout, b.hq, *b.args())
+    a.update(change)
+    hq = a.pop("hq")
+    layout = dopr.make_cache_layout(**a)
+    room = torch.zeros(plan.numel() * 8, dtype=torch.uint8, device=DEV)
+    room[:plan.numel()] = plan
+    pool = torch.zeros(2 * b.k.numel() * 8, dtype=a["dtype"], device=DEV)
+    q = torch.ones(b.T, hq, a["head_dim"], dtype=a["dtype"], device=DEV)
+    st, out, lse = word(), torch.full_like(q, 7.0), torch.full((b.T, hq), 7.0, device=DEV)
+    dopr.shared_attention(layout, room, q, pool, pool, i32(np.zeros(64)), out=out, lse=lse, status=st)
+    if change:
+        assert st.item() == dopr.ERR_INVALID_ARG and bool((out == 7).all()) and bool((lse == 7).all())
+    else:
+        assert st.item() == 0 and bool((out == 0).all())

@@ -422,6 +422,8 @@ def _heads(name, t, tokens, head_dim, dtype, device):
     if t is None:
         return None
     shape, strides = t.shape, t.stride()
+    if tokens > 0x7fffffff:
+        raise ValueError(f"{name}: {tokens} tokens, a call takes at most 2^31 - 1")
     if len(shape) != 3 or shape[0] < tokens or shape[2] != head_dim or t.dtype != dtype or t.get_device() != device or \
             (head_dim > 1 and strides[2] != 1):
         raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on cuda:{device} with a contiguous last "

@@ -788,3 +788,23 @@ def test_attention_refuses_a_plan_of_another_layout(change):
         assert st.item() == dopr.ERR_INVALID_ARG and bool((out == 7).all()) and bool((lse == 7).all())
     else:
         assert st.item() == 0 and bool((out == 0).all())
+
+
+def test_rotary_positions_of_the_largest_number_of_tokens():
+    # 2^31 - 1 rows of one pair: the kernel's step behind the last of them passes 31 bits
+    T = 2 ** 31 - 1
+    rope = dopr.Rope(4, 2)
+    x = torch.empty(T, 1, 2, dtype=HF, device=DEV).normal_()
+    pos = torch.zeros(T, dtype=torch.int32, device=DEV)
+    ends = torch.cat([torch.arange(100, device=DEV), torch.arange(T - 70000, T, device=DEV)])
+    pos[ends] = 3
+    out, st = torch.full_like(x, 7.0), word()
+    dopr.rope_apply(rope, pos, x, q_out=out, status=st)
+    assert st.item() == 0
+    assert_turned(out[ends], x[ends], pos[ends], *frequencies(2, 1e6, 0, 1, 0, 0, 0, 0), 2, False, False)
+    out[ends] = x[ends]  # the rows between are at position 0, which turns nothing
+    assert all(torch.equal(out[i:i + 2 ** 28], x[i:i + 2 ** 28]) for i in range(0, T, 2 ** 28))
+    del x, out
+    with pytest.raises(ValueError, match="at most"):
+        wide = torch.zeros(1, dtype=HF, device=DEV).expand(2 ** 31, 1, 2)
+        dopr.rope_apply(rope, torch.zeros(2 ** 31, dtype=torch.int32, device=DEV), wide, q_out=wide)

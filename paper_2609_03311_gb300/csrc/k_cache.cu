@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(FILL_THREADS) k_cache_fill(CacheExtendArgs a) 
   // at those between (one thread halving the range: 11 loads one after another for 2,000 rows)
   int rows[2] = {0, 0};
   if (t0 < tokens) {
-    const int x0 = t0, x1 = min(t0 + FILL_THREADS, tokens) - 1, step = (n + FILL_THREADS - 1) / FILL_THREADS;
+    const int x0 = t0, x1 = t0 + min(FILL_THREADS, tokens - t0) - 1, step = (n + FILL_THREADS - 1) / FILL_THREADS;
     const int i = threadIdx.x * step, v = i < n ? a.tok_off[i] : INT32_MAX;
     rows[0] = (__syncthreads_count(v <= x0) - 1) * step;
     rows[1] = (__syncthreads_count(v <= x1) - 1) * step;
@@ -243,7 +243,7 @@ cudaError_t launch_cache_extend(const CacheExtendArgs& a, cudaStream_t st) {
   const cudaError_t e = few ? launch_dependent(k_cache_sums<FEW_THREADS>, dim3(1), FEW_THREADS, 0, st, a, here)
                             : launch_dependent(k_cache_sums<MANY_THREADS>, dim3(1), MANY_THREADS, 0, st, a, here);
   if (e != cudaSuccess || here) return e;
-  return launch_dependent(k_cache_fill, dim3((a.max_tokens + FILL_THREADS - 1) / FILL_THREADS), FILL_THREADS, 0, st, a);
+  return launch_dependent(k_cache_fill, dim3((a.max_tokens - 1) / FILL_THREADS + 1), FILL_THREADS, 0, st, a);
 }
 
 }  // namespace dopr

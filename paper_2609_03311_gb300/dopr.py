@@ -451,6 +451,8 @@ class CacheBatch:
 
     def __init__(self, layout: CacheLayout, max_tokens: int, device):
         i32 = dict(dtype=torch.int32, device=device)
+        if max_tokens > 0x7fffffff:
+            raise ValueError(f"{max_tokens} tokens, a step takes at most 2^31 - 1")
         self.max_tokens = max_tokens
         self.tok_off = torch.empty(layout.n_seqs + 1, **i32)
         self.slots = torch.empty(max_tokens, dtype=torch.int64, device=device)
@@ -471,6 +473,8 @@ def cache_extend(layout: CacheLayout, seq_lens, block_tables, free_blocks, n_fre
     block_tables and free_blocks are updated in place, lengths and the stack's height in `out`."""
     dev = seq_lens.device
     n, i32 = layout.n_seqs, torch.int32
+    if max_tokens > 0x7fffffff:
+        raise ValueError(f"{max_tokens} tokens, a step takes at most 2^31 - 1")
     st, guard, on = _on(dev, stream)
     try:
         if out is None:

@@ -808,3 +808,22 @@ def test_rotary_positions_of_the_largest_number_of_tokens():
     with pytest.raises(ValueError, match="at most"):
         wide = torch.zeros(1, dtype=HF, device=DEV).expand(2 ** 31, 1, 2)
         dopr.rope_apply(rope, torch.zeros(2 ** 31, dtype=torch.int32, device=DEV), wide, q_out=wide)
+
+
+def test_extend_by_the_largest_number_of_tokens():
+    # one row takes every page of the largest pool; the step's extent is the largest, 127 places longer
+    n = 2 ** 24 - 1
+    layout = dopr.make_cache_layout(n, 128, 1, 64, HF, 2, n)
+    free = torch.arange(n, dtype=torch.int32, device=DEV)
+    tables = torch.zeros(2, n, dtype=torch.int32, device=DEV)
+    st, T = word(), 2 ** 31 - 1
+    b = dopr.cache_extend(layout, i32([0, 0]), tables, free, i32([n]), i32([0, n * 128]), T, status=st)
+    assert st.item() == 0 and b.tok_off.tolist() == [0, 0, n * 128] and b.seq_lens.tolist() == [0, n * 128]
+    assert b.n_free.item() == 0 and torch.equal(tables[1], free.flip(0))
+    for i in range(0, n * 128, 2 ** 28):
+        t = torch.arange(i, min(i + 2 ** 28, n * 128), device=DEV)
+        assert torch.equal(b.slots[i:i + t.numel()], (n - 1 - t // 128) * 128 + t % 128)
+        assert torch.equal(b.positions[i:i + t.numel()], t.int())
+    assert b.slots[n * 128:].tolist() == [-1] * 127 and b.positions[n * 128:].tolist() == [-1] * 127
+    with pytest.raises(ValueError, match="at most"):
+        dopr.cache_extend(layout, i32([0, 0]), tables, free, i32([n]), i32([0, 1]), 2 ** 32 + 4, out=b)

@@ -537,8 +537,12 @@ DOPR_API dopr_status dopr_cache_append(const dopr_cache_layout *layout, const do
  *         attention with the same layout, n_q_heads and max_tokens on the same
  *         kind of device; with others that is INVALID_ARG and writes nothing.
  * 1 <= n_q_heads / n_kv_heads <= 64, a whole number.
- * Device error: INVALID_ARG (offsets, a length or a prefix out of range); the
- * plan is then empty, and attention writes nothing.
+ * Device errors: INVALID_ARG (offsets, a length or a prefix out of range),
+ * UNSUPPORTED (2^29 units of work or more: for every kv head and group of up to
+ * 256 rows that share keys, 6 a block of 128 keys that all of them see and 12
+ * another; where 16 rows or fewer share them, 1 for every 16 keys.  90,000 tokens
+ * of 32 heads on 8 over 2^20 keys are that many); the plan is then empty, and
+ * attention writes nothing.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 DOPR_API dopr_status dopr_shared_attention_plan(const dopr_cache_layout *layout, int32_t n_q_heads, int32_t max_tokens,

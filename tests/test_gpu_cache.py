@@ -827,3 +827,22 @@ def test_extend_by_the_largest_number_of_tokens():
     assert b.slots[n * 128:].tolist() == [-1] * 127 and b.positions[n * 128:].tolist() == [-1] * 127
     with pytest.raises(ValueError, match="at most"):
         dopr.cache_extend(layout, i32([0, 0]), tables, free, i32([n]), i32([0, 1]), 2 ** 32 + 4, out=b)
+
+
+def refused_by_the_plan(layout, hq, off, lens, prefix, tables):
+    T = int(off[-1])
+    st = word()
+    plan = dopr.shared_attention_plan(layout, hq, i32(off), i32(lens), i32(prefix), T, status=st)
+    assert st.item() == dopr.ERR_UNSUPPORTED
+    pool = torch.zeros(layout.n_blocks, layout.n_kv_heads, layout.page, layout.head_dim, dtype=HF, device=DEV)
+    q, st = torch.ones(T, hq, layout.head_dim, dtype=HF, device=DEV), word()
+    out, lse = torch.full_like(q, 7.0), torch.full((T, hq), 7.0, device=DEV)
+    dopr.shared_attention(layout, plan, q, pool, pool, tables, out=out, lse=lse, status=st)
+    assert st.item() == 0 and bool((out == 7).all()) and bool((lse == 7).all())
+
+
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_plan_refuses_more_work_than_it_counts(tokens):
+    # 2^30 keys for each of 16 kv heads: 2^30 units for a single row a head, 48 * 2^24 for forty
+    layout = dopr.make_cache_layout(1, 128, 16, 64, HF, 2, 2 ** 23)
+    refused_by_the_plan(layout, 16, [0, 0, tokens], [2 ** 30, 0], [-1, 0], torch.zeros(2, 2 ** 23, dtype=torch.int32, device=DEV))

@@ -541,8 +541,9 @@ DOPR_API dopr_status dopr_cache_append(const dopr_cache_layout *layout, const do
  * UNSUPPORTED (2^29 units of work or more: for every kv head and group of up to
  * 256 rows that share keys, 6 a block of 128 keys that all of them see and 12
  * another; where 16 rows or fewer share them, 1 for every 16 keys.  90,000 tokens
- * of 32 heads on 8 over 2^20 keys are that many); the plan is then empty, and
- * attention writes nothing.
+ * of 32 heads on 8 over 2^20 keys are that many; or keys of such a group, its
+ * rows' own together, beyond 2^31 - 129); the plan is then empty, and attention
+ * writes nothing.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 DOPR_API dopr_status dopr_shared_attention_plan(const dopr_cache_layout *layout, int32_t n_q_heads, int32_t max_tokens,

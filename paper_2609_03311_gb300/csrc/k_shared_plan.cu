@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   extern __shared__ __align__(16) uint32_t keys[];  // a power of two >= n_seqs, then what in_shared says
   __shared__ int sums_memory[2][32];
   __shared__ int first_of[SHARES];
-  __shared__ int bad, unsorted;
+  __shared__ int bad, unsorted, too_long;
   __shared__ unsigned long long lines[WARPS], tiles_line, both_lines;
   __shared__ int first_few;
   __shared__ uint32_t longest[2];  // entry of tiles, of few items
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   int* row_run = place + 2 * n + 1;    // its first run
   int* first_tok = row_run + 2 * n;    // of a key: tokens before its first
   int* first_item = first_tok + 2 * n + 3;
-  if (threadIdx.x == 0) bad = 0, unsorted = 0, tiles_line = both_lines = 0, first_few = 0, longest[0] = longest[1] = 0;
+  if (threadIdx.x == 0) bad = 0, unsorted = 0, too_long = 0, tiles_line = both_lines = 0, first_few = 0, longest[0] = longest[1] = 0;
   if (threadIdx.x < 64) sums_memory[threadIdx.x >> 5][lane] = 0;
 #pragma unroll 1
   for (int c = threadIdx.x; c < SHARES; c += THREADS) first_of[c] = INT_MAX;
@@ -394,6 +394,8 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
     Item& it = items[c];
     const int run0 = it.run, it_runs = (c + 1 < n_items ? items[c + 1].run : n_runs) - run0;
     int pages = 0, end0 = 0, begin1 = INT_MAX;
+    const int most = (INT_MAX - BLOCK) / (it.flags & ITEM_FEW ? PIECE : page);  // columns are counted in 31 bits
+    bool fit = true;
 #pragma unroll 1
     for (int r0 = 0; r0 < it_runs; r0 += 8) {
       Run* run = runs + run0 + r0 + part;
@@ -411,8 +413,11 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
         if (run->tok0 < tile) end0 = max(end0, off + mine);
         if (run->token >= 0 && run->tok1 > tile) begin1 = min(begin1, off);
       }
-      pages += __shfl_sync(mask, inc, 7, 8);
+      inc = __shfl_sync(mask, inc, 7, 8);  // (a run has 2^27 pages at most, eight have 2^30)
+      fit = fit && inc <= most - pages;
+      pages = fit ? pages + inc : 0;
     }
+    if (!fit) too_long = 1;
 #pragma unroll
     for (int o = 1; o < 8; o <<= 1) {
       end0 = max(end0, __shfl_xor_sync(mask, end0, o));
@@ -504,7 +509,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   __syncthreads();
   const unsigned long long few_line = both_lines - tiles_line;
   // CTAs for each kind by what they take, one at least
-  const bool both = tiles_line > 0 && few_line > 0, fits = tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
+  const bool both = tiles_line > 0 && few_line > 0, fits = !too_long && tiles_line < 0x20000000ull && few_line < 0x20000000ull && (!both || n_ctas > 1);
   int tile_ctas = few_line > 0 ? 0 : n_ctas;
   if (both) {
     const float tiles_cost = static_cast<float>(tiles_line), few_cost = static_cast<float>(few_line) * FEW_PER_TILES / WORKERS;

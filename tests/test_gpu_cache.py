@@ -846,3 +846,20 @@ def test_plan_refuses_more_work_than_it_counts(tokens):
     # 2^30 keys for each of 16 kv heads: 2^30 units for a single row a head, 48 * 2^24 for forty
     layout = dopr.make_cache_layout(1, 128, 16, 64, HF, 2, 2 ** 23)
     refused_by_the_plan(layout, 16, [0, 0, tokens], [2 ** 30, 0], [-1, 0], torch.zeros(2, 2 ** 23, dtype=torch.int32, device=DEV))
+
+
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_plan_refuses_keys_that_31_bits_do_not_count(tokens):
+    # tables may name a page more than once: a prefix of 2^30 keys and as many own ones, by pieces of 16 and by tiles
+    layout = dopr.make_cache_layout(1, 128, 1, 64, HF, 3, 2 ** 23)
+    refused_by_the_plan(layout, 1, [0, 0, tokens, tokens], [2 ** 30, 2 ** 30, 0], [-1, 0, -1],
+                        torch.zeros(3, 2 ** 23, dtype=torch.int32, device=DEV))
+    # rows of a tile whose own keys alone are too many
+    if tokens > 1:
+        refused_by_the_plan(layout, 1, [0, tokens, 2 * tokens, 3 * tokens], [2 ** 30, 2 ** 30, 2 ** 30], [-1] * 3,
+                            torch.zeros(3, 2 ** 23, dtype=torch.int32, device=DEV))
+    # a page less is planned
+    st = word()
+    dopr.shared_attention_plan(layout, 1, i32([0, 0, tokens, tokens]), i32([2 ** 30, 2 ** 30 - 256, 0]), i32([-1, 0, -1]), tokens,
+                               status=st)
+    assert st.item() == 0

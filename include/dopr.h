@@ -558,6 +558,7 @@ DOPR_API int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout *layou
  * keys 0 .. seq_lens[i] - n_i + j.  Rows that share a prefix read its pages
  * together, whatever their order; long keys are split and joined.  q head h
  * reads kv head h / (n_q_heads / n_kv_heads).
+ *   plan     dopr_shared_attention_plan_bytes(...) bytes, of this call's sizes.
  *   q, out   views of layout->dtype, 16-byte aligned with strides multiples of
  *            16 bytes; out overlaps nothing.  Rows behind the last token are
  *            left as they were.

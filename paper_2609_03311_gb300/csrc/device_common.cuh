@@ -77,6 +77,9 @@ __device__ __forceinline__ int ld_volatile(const int* p) { return *reinterpret_c
 // plain pointers (never __ldg or const __restrict__, whose loads may go through the non-coherent
 // path and be moved above the wait); those are for weights, gains, the RoPE table and whatever
 // was copied or finished before the first dependent launch.
+// A launch of the ordinary kind begins when all before it on the stream is complete and visible.
+// So a dependent launch right behind it may read before its own wait what was written before the
+// ordinary one (the attention over the paged cache and its join: the plan).
 //
 // One kernel does not wait so at its start: the few-row GEMM that runs beside the wide one of the
 // same product (GemmParams::beside) would wait for that launch to end.  It reads only what the

@@ -142,8 +142,8 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 }
-// What the chains of loads at the start run through, brought into L2 while the kernel before ends: it may still write there,
-// and L2 shows what it wrote.  A line a thread of the grid; of larger calls, whose work is long, a part.
+// What the chains of loads at the start run through, brought into L2 while the CTA sets up.  A line a thread of the grid; of
+// larger calls, whose work is long, a part.
 __device__ __forceinline__ void prefetch_l2(const SharedAttnArgs& a, const Plan& plan) {
   const int64_t at = (static_cast<int64_t>(threadIdx.x) * gridDim.x + blockIdx.x) * 128;
   const char* from = static_cast<const char*>(a.plan);
@@ -528,6 +528,11 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, TT = tokens_a_tile(G);
   int* err = &gave_up;
 
+  // An ordinary launch: everything before it is complete.  What begins the chain of loads comes while the CTA sets up.
+  pdl_trigger();
+  const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];
+  const Head head = *plan.head;
+  prefetch_l2(a, plan);
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), (i >= L::P_FULL && i < L::P_FULL + 4) || i == L::ML_FULL || i == L::ML_EMPTY ? 4 : 1);
@@ -545,12 +550,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  prefetch_l2(a, plan);
-  pdl_wait();
-  pdl_trigger();  // behind the wait: the joining kernel reads the plan before its own (and finds no room earlier anyway)
   Segment s;
-  const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];  // beside the head: what begins the chain of loads
-  const Head head = *plan.head;
   const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, gridDim.x);
   const bool few = static_cast<int>(blockIdx.x) >= head.tile_ctas;
   if (!good && threadIdx.x == 0 && a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
@@ -1159,9 +1159,12 @@ __global__ void __launch_bounds__(THREADS, 1)
 }
 
 // ------------------------------------------------------------------ joining the parts
-// A warp a row, JOIN_ROWS rows of an entry at a time, or two warps a row of many parts.  Bound by latency where few rows have many parts, so what the plan says
-// of a CTA's first piece is read while the attention ends (it was complete before that began), the first values are asked for
+// A warp a row, JOIN_ROWS rows of an entry at a time, or two warps a row of many parts.  Bound by latency where few rows have
+// many parts, so what the plan says of a CTA's first piece is read while the attention ends, the first values are asked for
 // beside the maxima and sums, and four parts are on their way at once (eight take registers that cost more rows at once).
+// The plan may be read before this kernel's wait because the attention's launch is an ordinary one, which begins when the plan
+// is complete, and this one begins behind it.  (The attention as a dependent launch and the plan read behind the wait: one
+// token 9.2 us, 64 queries 46.1, ragged documents 54.7, 16 documents 161; so 8.9, 44.9, 53.9, 158.)
 // 64 rows of a token, 19 parts each: about 7 us; 5,000 tokens of 16 documents, of which a third has two parts: 14.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
@@ -1308,7 +1311,9 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   else if (!make_tmap_rows_of_heads(&tm_q8, a.q, D, a.Hq, a.max_tokens, a.q_head, a.q_tok, G, 8, half)) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
   if (e != cudaSuccess) return e;
-  e = launch_dependent(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q8, tm_q1, tm_k, tm_v, args, plan);
+  // not a dependent launch: the joining kernel relies on that
+  k_shared_attn<T, D><<<n_ctas, THREADS, Smem<D>::BYTES, st>>>(tm_q8, tm_q1, tm_k, tm_v, args, plan);
+  e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +

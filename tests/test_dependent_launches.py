@@ -96,3 +96,32 @@ def test_the_few_row_launch_beside_a_wide_one_passes_its_gate_before_it_reads():
     # without a gate every warp waits for the kernel before, and a launch beside does so at its end
     assert few.count("if (!p.beside) pdl_wait();") == 1 and few.count("if (warp != 0 && !p.beside) pdl_wait();") == 1
     assert few.index("if (p.beside) pdl_wait();") > few.index("epilogue_tile<") and few.count("pdl_wait()") == 3
+
+
+def test_the_paged_caches_kernels_wait_before_they_read_what_others_write():
+    # Every dependent launch of the paged cache waits once, and nothing that another kernel writes is read ahead of that.
+    # The attention is an ordinary launch, which begins when all before it is complete; so the joining kernel, the dependent
+    # launch behind it, may read the plan (and that alone) ahead of its wait.
+    kernels = {k: body for s in ("k_cache.cu", "k_rope.cu", "k_shared_plan.cu", "k_shared_attn.cu")
+               for k, _, body in _kernels(_source(s)) if k != "k_rope_table"}
+    assert set(kernels) == {"k_cache_sums", "k_cache_fill", "k_rope", "k_shared_plan", "k_shared_attn", "k_shared_join"}
+    launches = _source("k_shared_attn.cu")
+    assert len(re.findall(r"\bk_shared_attn<T, D><<<", launches)) == 1 and "launch_dependent(k_shared_attn" not in launches
+    order = [launches.index("k_shared_attn<T, D><<<"), launches.index("launch_dependent(k_shared_join<T, D>")]
+    assert order == sorted(order)
+    attention = kernels.pop("k_shared_attn")
+    assert "pdl_wait()" not in attention and attention.count("pdl_trigger()") == 1
+    of_plan, others = r"\b(plan|p)(\.\w+)+\s*\[|\*\s*(plan|p)\.\w+", r"\ba(\.\w+)+\s*\[|\*\s*a\.\w+|\b(ml|part_o|src)\s*\["
+    for name, body in kernels.items():
+        assert body.count("pdl_wait()") == 1 and body.count("pdl_trigger()") == 1, name
+        if name == "k_shared_join":
+            # the wait is made once, at the first row's parts or at the end
+            assert body.count("wait_once();") == 2 and body.rstrip("}\n ").endswith("wait_once();")
+            ahead, read = body[:body.index("    wait_once();")], others
+        else:
+            ahead, read = body[:body.index("pdl_wait()")], of_plan + "|" + others
+            # at the outermost level of the kernel, not in a branch that some threads may not take
+            assert ahead.count("{") - ahead.count("}") == 1, name
+        # (functions defined ahead of the wait run behind it)
+        ahead = re.sub(r"auto \w+ = \[&\]\([^)]*\) \{[^{}]*\};", "", ahead)
+        assert not re.search(read, ahead), (name, re.search(read, ahead).group())

@@ -28,7 +28,8 @@
 //   copies then; 53 now, 4.8 TB/s).
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
 // Values would (0 x NaN), so rows of V past a run's keys are zero in shared memory.  A value that one token sees and
-// another of the item does not would too: rows that end with a NaN though their scores have none are computed alone.
+// another of the item does not would too: rows that end with a NaN though their scores have none are looked at when the CTA has
+// done everything else.
 //
 // k_shared_join, a warp a row, adds the parts up.
 #include <limits.h>
@@ -266,61 +267,141 @@ __device__ __noinline__ float2 add_other(uint32_t o_col, float2 mine, float2 oth
   return make_float2(top, mine.y * by + other.y * other_by);
 }
 
-// One row alone by a warp, a key at a time, for rows whose products took in a value that they do not see; lane l holds
-// elements [E l, E l + E) of the head.
+// A row of a segment whose values hold a NaN though its scores have none, by a warp; lane l holds elements [E l, E l + E) of the
+// head.  The NaN stands where it came from a value that the row sees.  It may also be of one that only other rows of the item
+// see: the products take in all columns of a block, at a weight of zero, and zero times a NaN or an infinity is not zero.
+// Prefix columns are seen by all rows, so only the other rows' own keys are looked through; where a value there is not finite, in
+// an element that holds a NaN, those elements are summed up again over the row's columns alone, 32 at a time: a lane a key's
+// score, then the values row by row.  That ends early where they are all NaN again.  Rare and slow, so nobody waits for it.
+// place: of the row's token in `order`; part: the row of its partial result, -1: the results themselves.
 template <typename T, int D>
-__device__ __noinline__ void row_alone(const SharedAttnArgs& a, const Plan& plan, int t, int h, int lane) {
-  constexpr int E = D / 32, W = E / 2;
-  const int page = a.lay.page, Hkv = a.lay.n_kv_heads, kvh = h / (a.Hq / Hkv);
-  const int4 rec = plan.rec[t];
-  const uint32_t* qp = reinterpret_cast<const uint32_t*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head) + lane * W;
-  const float scale_log2 = a.scale * 1.4426950408889634f;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+__device__ __noinline__ void mend_row(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int place, int h, int64_t part, int lane) {
+  constexpr int E = D / 32, W = E / 2, AHEAD = 8;
+  const int page = a.lay.page, Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, t = plan.order[place];
+  const float2* ml = reinterpret_cast<const float2*>(a.ws);
+  float2* part_o = reinterpret_cast<float2*>(a.ws + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x) * 8 + part * (4 * D)) + lane * W;
+  uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * W;
+  // a part that summed nothing up left no values; a NaN among the scores makes all of them NaN
+  if (part >= 0 && !(ml[part].y > 0.f)) return;
+  float2 o[W];
+  bool nan = false;
 #pragma unroll
   for (int i = 0; i < W; ++i) {
-    const float2 f = unpack2<T>(qp[i]);
-    q[2 * i] = f.x * scale_log2, q[2 * i + 1] = f.y * scale_log2;
-    o[2 * i] = o[2 * i + 1] = 0.f;
+    o[i] = part < 0 ? unpack2<T>(out[i]) : part_o[i];
+    nan |= o[i].x != o[i].x || o[i].y != o[i].y;
   }
-  for (int k = 0; k < 2; ++k) {
-    // the prefix, by whichever item reads it; the row's own keys likewise
-    const int item = k ? rec.z : rec.x, place = k ? rec.w : rec.y;
-    if (item < 0) continue;
-    const Item it = plan.items[item];
-    for (int j = 0; j < it.n_runs; ++j) {
-      const Run run = plan.runs[it.run + j];
-      if (place < run.tok0 || place >= run.tok1) continue;
-      const int n = run.token < 0 ? run.keys : max(0, run.keys - (run.tok1 - 1 - place));
-      for (int p = 0; p < n; ++p) {
-        int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + p / page];
-        if (block < 0 || block >= a.lay.n_blocks) block = 0;
-        const int64_t at = ((static_cast<int64_t>(block) * Hkv + kvh) * page + p % page) * (D / 2) + lane * W;
-        const uint32_t *kp = static_cast<const uint32_t*>(a.k_pool) + at, *vp = static_cast<const uint32_t*>(a.v_pool) + at;
-        float s = 0.f;
+  if (!__any_sync(0xffffffffu, nan)) return;
+  const int unit = s.flags & SEG_FEW ? PIECE : page, block = s.flags & SEG_FEW ? PIECE : BLOCK;
+  const int c0 = s.b0 * block, c1 = s.b1 * block;  // the segment's columns
+  const int2 own = plan.own[place];
+  // of the table row's key p: its row among the pool's [pages][kv heads][page]
+  auto row_of = [&](int row, int p) {
+    int block = a.tables[static_cast<int64_t>(row) * a.lay.max_blocks + p / page];
+    if (block < 0 || block >= a.lay.n_blocks) block = 0;
+    return (block * Hkv + s.h) * page + p % page;
+  };
+  auto value = [&](int at, int i) {
+    return unpack2<T>((static_cast<const uint32_t*>(a.v_pool) + static_cast<int64_t>(at) * (D / 2) + lane * W)[i]);
+  };
+  bool unseen = false;
+  for (int j = 0; j < s.n_runs && !unseen; ++j) {
+    const Run run = plan.runs[s.run + j];
+    if (run.token < 0) continue;
+    const int from = run.off * unit, end = min(run.keys, c1 - from);
+    for (int p = max(0, c0 - from); p < end && !unseen; p += AHEAD) {
+      bool bad = false;
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const float2 f = unpack2<T>(kp[i]);
-          s += q[2 * i] * f.x + q[2 * i + 1] * f.y;
-        }
-        s = warp_sum(s);
-        const float top = fmaxf(m, s), base = top == -INFINITY ? 0.f : top;
-        const float old = exp2f(m - base), e = exp2f(s - base);
-        m = top;
-        l = l * old + e;
+      for (int i = 0; i < AHEAD; ++i) {
+        if (p + i >= end || (from + p + i >= own.x && from + p + i < own.y)) continue;
+        const int at = row_of(run.row, p + i);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const float2 f = unpack2<T>(vp[i]);
-          o[2 * i] = o[2 * i] * old + e * f.x;
-          o[2 * i + 1] = o[2 * i + 1] * old + e * f.y;
+        for (int e = 0; e < W; ++e) {
+          const float2 v = value(at, e);
+          bad |= (o[e].x != o[e].x && !isfinite(v.x)) || (o[e].y != o[e].y && !isfinite(v.y));
         }
       }
+      unseen = __any_sync(0xffffffffu, bad);
     }
   }
-  const float inv = inverse(l);
-  uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * W;
+  if (!unseen) return;
+  const uint4* qp = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + t * a.q_tok + h * a.q_head);
+  const float scale_log2 = a.scale * 1.4426950408889634f;
+  float2 x[W];
 #pragma unroll
-  for (int i = 0; i < W; ++i) op[i] = pack2<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
-  if (a.lse && lane == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
+  for (int i = 0; i < W; ++i) x[i] = make_float2(0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+  for (int j = 0; j < s.n_runs; ++j) {
+    const Run run = plan.runs[s.run + j];
+    const int from = run.off * unit;
+    if (run.token >= 0 && (own.x >= own.y || from != own.x || run.keys == 0)) continue;
+    const int end = min(run.token < 0 ? s.prefix_keys : own.y - own.x, c1 - from);
+    for (int p0 = max(0, c0 - from); p0 < end; p0 += 32) {
+      const int here = min(32, end - p0);
+      const int at = row_of(run.row, p0 + min(lane, here - 1));
+      const uint4* kp = reinterpret_cast<const uint4*>(static_cast<const T*>(a.k_pool) + static_cast<int64_t>(at) * D);
+      float sc = 0.f;
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        const uint4 w = kp[c], u = qp[c];
+        const uint32_t ks[4] = {w.x, w.y, w.z, w.w}, qs[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = unpack2<T>(ks[i]), g = unpack2<T>(qs[i]);
+          sc += f.x * g.x + f.y * g.y;
+        }
+      }
+      sc = lane < here ? sc * scale_log2 : -INFINITY;
+      float top = sc;
+#pragma unroll
+      for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      top = fmaxf(top, m);
+      const float base = top == -INFINITY ? 0.f : top, old = exp2f(m - base), e = exp2f(sc - base);
+      m = top;
+      l = l * old + warp_sum(e);
+#pragma unroll
+      for (int i = 0; i < W; ++i) x[i].x *= old, x[i].y *= old;
+#pragma unroll 8
+      for (int i = 0; i < here; ++i) {
+        const float by = __shfl_sync(0xffffffffu, e, i);
+        const int row = __shfl_sync(0xffffffffu, at, i);
+#pragma unroll
+        for (int c = 0; c < W; ++c) {
+          const float2 v = value(row, c);
+          x[c].x += by * v.x;
+          x[c].y += by * v.y;
+        }
+      }
+      bool open = false;
+#pragma unroll
+      for (int i = 0; i < W; ++i) open |= (o[i].x != o[i].x && x[i].x == x[i].x) || (o[i].y != o[i].y && x[i].y == x[i].y);
+      if (!__any_sync(0xffffffffu, open)) return;
+    }
+  }
+  // parts are relative to the maximum that they were left with
+  const float by = part < 0 ? inverse(l) : exp2f(m - ml[part].x);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    if (o[i].x == o[i].x && o[i].y == o[i].y) continue;
+    const float2 y = make_float2(o[i].x != o[i].x ? x[i].x * by : o[i].x, o[i].y != o[i].y ? x[i].y * by : o[i].y);
+    if (part < 0) out[i] = pack2<T>(y.x, y.y);
+    else part_o[i] = y;
+  }
+}
+
+// The marked segments of a softmax group's warp (quarter 32 rows of group w's tile) or of a few items' warp.
+template <typename T, int D>
+__device__ __noinline__ void mend_segments(const SharedAttnArgs& a, const Plan& plan, uint32_t marked, int worker, int lane) {
+  const int G = a.Hq / a.lay.n_kv_heads, TT = tokens_a_tile(G);
+  const int2 work = plan.work[blockIdx.x * WORKERS + worker];
+  for (int at = work.x; at < work.y; ++at) {
+    if (!(marked >> (at & 31) & 1u)) continue;
+    const Segment& s = plan.segs[at];
+    const int t0 = s.flags & SEG_TWO ? worker / 4 * TT : 0, rows = min(TT, s.n_tok - t0) * G;
+    const int first = s.flags & SEG_FEW ? 0 : worker % 4 * 32;
+    for (int r = first; r < min(rows, first + 32); ++r)
+      mend_row<T, D>(a, plan, s, s.tok + t0 + r / G, s.h * G + r % G,
+                     s.flags & SEG_WHOLE ? -1 : static_cast<int64_t>(s.part_row) + t0 * G + r, lane);
+  }
 }
 
 // A share of few items by one warp, a piece of 16 columns at a time, three or six of them on their way in shared memory of
@@ -328,7 +409,7 @@ __device__ __noinline__ void row_alone(const SharedAttnArgs& a, const Plan& plan
 // of the item, and of each 8 columns two from 2 (lane % 4).  Bound by the copies of K and V: 8 KB a piece of head size 128,
 // 1.5 us of an eighth of an SM's part of the memory's rate, of which the products and the softmax take a third.
 template <typename T, int D>
-__device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int wi, int2 work, int lane) {
+__device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int wi, int2 work, uint32_t* marked, int lane) {
   using L = Smem<D>;
   constexpr int HALF = PIECE * 128, KV = L::HALVES * HALF;  // 64 elements a row; K or V of a piece
   constexpr int CHUNKS = D / 8;                             // 16-byte chunks of a row
@@ -473,30 +554,24 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
       __syncwarp();  // every lane has read the stage
       if (++stage == L::F_STAGES) stage = 0;
     }
+    bool odd = false;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = quad + 8 * i;
       float sum = l[i] + __shfl_xor_sync(0xffffffffu, l[i], 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      float all = 0.f;  // a NaN where one of the values is (or they are infinite both ways: no harm)
       if (s.flags & SEG_WHOLE) {
-        bool nan = false;
         const int t = r < rows ? plan.order[s.tok + r / G] : 0, h = s.h * G + r % G;
         const float inv = inverse(sum);
         uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + in_quad;
 #pragma unroll
         for (int d = 0; d < D / 8; ++d) {
           const float x = sum == 0.f ? 0.f : o[d][2 * i] * inv, y = sum == 0.f ? 0.f : o[d][2 * i + 1] * inv;
-          nan |= x != x || y != y;
+          all += x + y;
           if (r < rows) dst[4 * d] = pack2<T>(x, y);
         }
         if (r < rows && a.lse && in_quad == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m[i], sum);
-        // scores in order, values not: perhaps a value that the row does not see
-        uint32_t odd = __ballot_sync(0xffffffffu, r < rows && nan && sum == sum);
-        while (odd) {
-          const int from = __ffs(odd) - 1;
-          odd &= ~(0xfu << (from & ~3));
-          row_alone<T, D>(a, plan, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
-        }
       } else if (r < rows) {
         float2* ml = reinterpret_cast<float2*>(a.ws);
         float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
@@ -504,11 +579,16 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
         if (in_quad == 0) ml[row] = make_float2(m[i], sum);
         if (sum != 0.f) {
 #pragma unroll
-          for (int d = 0; d < D / 8; ++d)
+          for (int d = 0; d < D / 8; ++d) {
+            all += o[d][2 * i] + o[d][2 * i + 1];
             *reinterpret_cast<float2*>(part_o + row * D + 8 * d + 2 * in_quad) = make_float2(o[d][2 * i], o[d][2 * i + 1]);
+          }
         }
       }
+      odd |= r < rows && all != all && sum > 0.f;
     }
+    // scores in order, values not: perhaps a value that the row does not see
+    if (__any_sync(0xffffffffu, odd) && lane == 0) *marked |= 1u << (walk.at - 1 & 31);
   }
 }
 
@@ -519,6 +599,7 @@ __global__ void __launch_bounds__(THREADS, 1)
                   const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan) {
   using L = Smem<D>;
   extern __shared__ uint8_t smem_raw[];
+  __shared__ uint32_t marked[WORKERS];  // of each of the warps 4-11: segments (modulo 32) that hold rows to be mended
   __shared__ int gave_up;  // stands for the error word of the bounded waits: a CTA gives up alone
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t s0 = smem_u32(smem);
@@ -533,6 +614,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   const int2 work = plan.work[blockIdx.x * WORKERS + (warp >= 4 ? warp - 4 : 0)];
   const Head head = *plan.head;
   prefetch_l2(a, plan);
+  if (threadIdx.x < WORKERS) marked[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
     gave_up = 0;
     for (int i = 0; i < L::N_BARS; ++i) mbar_init(bar(i), (i >= L::P_FULL && i < L::P_FULL + 4) || i == L::ML_FULL || i == L::ML_EMPTY ? 4 : 1);
@@ -559,7 +641,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else if (few) {
     if (warp >= 4) {
       regs_many();
-      few_items<T, D>(a, plan, s0, warp - 4, work, lane);
+      few_items<T, D>(a, plan, s0, warp - 4, work, &marked[warp - 4], lane);
     } else {
       regs_few();
     }
@@ -1078,13 +1160,13 @@ __global__ void __launch_bounds__(THREADS, 1)
         if (both) o_par ^= SUMS;
         if (!last) continue;
       }
+      float all = 0.f;  // the values' sum: a NaN where one of them is (or they are infinite both ways: no harm)
       if (e.flags & SEG_WHOLE) {
         // ---- the whole entry: the rows' results
         const int t = token, h = e.h * G + r % G;
         const float inv = inverse(l);
         T* dst = static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head;
         const bool wide = ((reinterpret_cast<uintptr_t>(a.out) | a.o_tok * 2 | a.o_head * 2) & 31) == 0;  // a store a sector
-        float all = 0.f;  // the values' sum: a NaN where one of them is (or they are infinite both ways: no harm)
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t v[32] = {};
@@ -1113,15 +1195,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             }
           }
         }
-        const bool nan = all != all;
         if (valid && a.lse) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m, l);
-        // scores in order, values not: perhaps a value that the row does not see
-        uint32_t odd = __ballot_sync(0xffffffffu, valid && nan && l == l);
-        while (odd) {
-          const int from = __ffs(odd) - 1;
-          odd &= odd - 1;
-          row_alone<T, D>(a, plan, __shfl_sync(0xffffffffu, t, from), __shfl_sync(0xffffffffu, h, from), lane);
-        }
       } else {
         // ---- a partial result
         float2* ml = reinterpret_cast<float2*>(a.ws);
@@ -1137,6 +1211,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           tmem_ld_wait_for(v);
           if (valid && l != 0.f) {  // (a NaN is not)
 #pragma unroll
+            for (int i = 0; i < 32; ++i) all += __uint_as_float(v[i]);
+#pragma unroll
             for (int i = 0; i < 32; i += 8) {
               const uint32_t x[8] = {v[i], v[i + 1], v[i + 2], v[i + 3], v[i + 4], v[i + 5], v[i + 6], v[i + 7]};
               st_global32(dst + c + i, x);
@@ -1144,6 +1220,8 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
       }
+      // scores in order, values not: perhaps a value that the row does not see
+      if (__any_sync(0xffffffffu, valid && all != all && l > 0.f) && lane == 0) marked[warp - 4] |= 1u << (walk.at - 1 & 31);
       tc_fence_before();
     }
   }
@@ -1156,6 +1234,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     __syncwarp();
     tmem_dealloc(tmem, TMEM_COLS);
   }
+  // nobody waits for anybody any more
+  if (warp >= 4 && marked[warp - 4] != 0) mend_segments<T, D>(a, plan, marked[warp - 4], warp - 4, lane);
 }
 
 // ------------------------------------------------------------------ joining the parts
@@ -1273,14 +1353,6 @@ __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
       m = top;
 #pragma unroll
       for (int i = 0; i < E; ++i) o[i] = o[i] * mine + at[i] * other;
-    }
-    // scores in order, values not: perhaps a value that the row does not see
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < E; ++i) nan |= !(o[i] == o[i]);
-    if (l == l && __any_sync(0xffffffffu, nan)) {
-      row_alone<T, D>(a, plan, t, h, lane);
-      continue;
     }
     const float inv = inverse(l);
     uint32_t* op = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head) + lane * (E / 2);

@@ -863,3 +863,66 @@ def test_plan_refuses_keys_that_31_bits_do_not_count(tokens):
     dopr.shared_attention_plan(layout, 1, i32([0, 0, tokens, tokens]), i32([2 ** 30, 2 ** 30 - 256, 0]), i32([-1, 0, -1]), tokens,
                                status=st)
     assert st.item() == 0
+
+
+MIXED = {  # documents and requests whose rows share items in every way: (hq, docs, reqs)
+    "one tile": (4, [20 + 3 * i for i in range(40)], [(i % 40, 20 - i % 7, 9) for i in range(80)]),
+    "two tiles": (8, [20 + 5 * i for i in range(30)], [(i % 30, 30 - i % 4, 20) for i in range(60)]),
+    "few rows": (4, [5 + 11 * i for i in range(30)], [(i % 30, 3 + i % 40, 1 + i % 2) for i in range(60)]),
+    "own keys beside tiles": (4, [3000], [(0, 5 + i, 1) for i in range(50)]),
+    "few rows, cut": (4, [9000, 700], [(0, 30, 1), (0, 17, 2), (1, 40, 1), (1, 33, 1)]),
+    "cut": (8, [20000], [(0, 9 + i, 9) for i in range(3)]),
+    "no prefix": (8, [10], [(-1, 50 + i, 1 + 13 * (i % 3)) for i in range(20)]),
+}
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", list(MIXED))
+def test_attention_of_values_that_other_rows_of_an_item_see(kind, d, bad):
+    # one element of the last own value of every third request is bad: its last token sees it, nobody else
+    hq, docs, reqs = MIXED[kind]
+    b = Batch(hq, 2, d, BF, 16, docs, reqs, seed=len(reqs) + d)
+    want = b.run()
+    b.check(want)
+    sees = torch.zeros(b.T, dtype=torch.bool, device=DEV)
+    for i in range(len(docs), len(b.lens), 3):
+        at = b.lens[i] - 1
+        b.v[int(b.tables[i, at // 16]), 1, at % 16, 5] = bad
+        sees[b.off[i + 1] - 1] = True
+    got = b.run()
+    G = hq // 2
+    same = torch.ones_like(want[0], dtype=torch.bool)
+    same[:, G:, 5] = False
+    assert torch.equal(got[0][same], want[0][same]) and torch.equal(got[1], want[1])
+    mine = got[0][:, G:, 5]
+    assert not bool(torch.isfinite(mine[sees]).any())
+    if not math.isnan(bad):
+        assert bool((mine[sees] == bad).all())
+    out, _, avg = (x[:, G:, 5] if x.dim() == 3 else x for x in b.exact())
+    u = torch.finfo(BF).eps / 2
+    err, tol = (mine.double() - out).abs(), (u + 2.0 ** -11) * avg + u * out.abs() + 2.0 ** -24
+    assert bool((err <= tol)[~sees].all()), float((err / tol)[~sees].max())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_attention_of_a_bad_value_in_a_long_document(bad):
+    # every row sees it: the results hold it at once, in its element alone, and nothing runs into a limit
+    b = Batch(32, 8, 128, BF, 64, [131072, 200], [(0, 20 + i, 4) for i in range(64)] + [(1, 9, 9), (1, 30, 1)], seed=5)
+    want = b.run()
+    b.v[int(b.tables[0, 700 // 64]), 1, 700 % 64, 5] = bad
+    got = b.run()
+    T = 64 * 4
+    assert bool(torch.isnan(got[0][:T, 4:8, 5]).all() if math.isnan(bad) else (got[0][:T, 4:8, 5] == bad).all())
+    same = torch.ones_like(want[0], dtype=torch.bool)
+    same[:T, 4:8, 5] = False
+    assert torch.equal(got[0][same], want[0][same]) and torch.equal(got[1], want[1])
+    # no longer than a few times what it takes without (a walk over the document by a warp a row takes hundreds of times that)
+    plan, tables = dopr.shared_attention_plan(b.layout, b.hq, *b.args()), i32(b.tables)
+    ws = dopr.shared_attention_workspace(b.layout, b.hq, b.T)
+    a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    dopr.shared_attention(b.layout, plan, b.q, b.k, b.v, tables, workspace=ws)
+    z.record()
+    z.synchronize()
+    assert a.elapsed_time(z) < 20

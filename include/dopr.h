@@ -567,7 +567,8 @@ DOPR_API int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout *layou
  *   workspace dopr_shared_attention_workspace(...) bytes, 32-byte aligned.
  * Keys and values past a row's end are never used, whatever the pages hold there.
  * Products take dtype operands with 32-bit sums; probabilities are rounded to
- * dtype, statistics and sums are 32-bit.  A row's bits depend on the plan.
+ * dtype (F16: those below 2^-25 of a row's largest to steps of 2^-35 of it),
+ * statistics and sums are 32-bit.  A row's bits depend on the plan.
  * Device errors: INVALID_ARG (a page number outside the pool: page 0 is read
  * for it), TIMEOUT.  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */

@@ -16,7 +16,7 @@
 //     warp 3     brings the rows of Q by TMA: eight tokens that follow one another, others one by one (the rows of a token
 //                and kv head are the heads of a box); of a view that a tensor map does not take, with 16-byte copies
 //     warps 4-7, 8-11  softmax, a thread a row: the maximum, then P; O is scaled only when the maximum grew by more than
-//                2^8 (P stays within the type's range until then)
+//                2^8 (f16: 2^4; P stays within the type's range until then)
 //   P is rounded to the inputs' type for its product with V, as the tensor cores take it; maxima, sums, O and parts stay in 32
 //   bits, and a row's sum adds up P before the rounding.
 //   2,048 rows of 32 heads over 16,384 keys: 352 us, 1.56 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
@@ -45,7 +45,14 @@ using namespace shared_attn;
 constexpr int THREADS = 128 + 2 * 128;
 // group w: S at S_COL + 128 w, P over its upper half, O at O_COL + 128 w
 constexpr uint32_t TMEM_COLS = 512, S_COL = 0, P_COL = 64, O_COL = 256;
-constexpr float RESCALE_LOG2 = 8.f;
+// P = 2^(score - m), and O is scaled when m falls behind the maximum by more than RESCALE.  bf16 has the range of 32 bits: m is a
+// maximum.  f16 reaches from 2^-24 to 2^16: m is BELOW a maximum by 11, so that P takes the whole range up to 2^15 and a row's
+// smallest probabilities are rounded to steps of 2^-35 of its largest (with m the maximum, 2^-24: 131,071 keys of 2^-26 of one
+// other, which make up 0.2 % of the sum, counted as nothing).
+template <typename T>
+constexpr float RESCALE = std::is_same_v<T, __half> ? 4.f : 8.f;
+template <typename T>
+constexpr float BELOW = std::is_same_v<T, __half> ? 11.f : 0.f;
 // of the joining kernel on an SM (3 with twice the loads on their way: 64 rows a little faster, 16 documents 3 % slower)
 constexpr int JOIN_CTAS = 4;
 constexpr int HALF_BYTES = 128 * 128;  // 128 rows of 64 16-bit elements
@@ -525,9 +532,9 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
       for (int i = 0; i < 2; ++i) {
         float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2;
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2 - BELOW<T>;
         if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
-        const bool grow = top > m[i] + RESCALE_LOG2;
+        const bool grow = top > m[i] + RESCALE<T>;
         if (__any_sync(0xffffffffu, grow)) {
           const float by = grow ? ex2(m[i] - top) : 1.f;
           if (grow) m[i] = top;
@@ -1091,9 +1098,9 @@ __global__ void __launch_bounds__(THREADS, 1)
         max32(va, top);
         tmem_ld_wait_for(vb);
         max32(vb, top);
-        top *= scale_log2;
+        top = top * scale_log2 - BELOW<T>;
         if (m == -INFINITY) m = top;  // nothing but zeros has been summed
-        const bool grow = top > m + RESCALE_LOG2;
+        const bool grow = top > m + RESCALE<T>;
         if (__any_sync(0xffffffffu, grow)) {
           // S is complete, so every product issued before it is: O stands still
           const float by = grow ? ex2(m - top) : 1.f;

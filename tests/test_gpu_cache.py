@@ -926,3 +926,32 @@ def test_attention_of_a_bad_value_in_a_long_document(bad):
     z.record()
     z.synchronize()
     assert a.elapsed_time(z) < 20
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tokens", [1, 3, 40, 200])
+@pytest.mark.parametrize("m", [1000, 131072])
+def test_attention_of_one_heavy_key_among_many_light_ones(m, tokens, d, dt):
+    # one key has 2^26 times the weight of each other: together they matter, and each is below the steps of fp16 near one.
+    # Its place is late, so that the maximum grows over sums of the others, or first.
+    for at in (0, m - 1, m // 2):
+        b = Batch(1, 1, d, dt, 64, [m], [(0, tokens + 2, tokens)], seed=3)
+        b.q.zero_()
+        b.q[:, :, 0] = 16.0
+        k, v = b.rows[0]
+        k.zero_()
+        k[at, :, 0] = 26 * math.log(2) * d ** 0.5 / 16
+        v.copy_(1 + torch.rand_like(v.float()) / 2)
+        v[at] = 0.0
+        t = torch.arange(m, device=DEV)
+        blk = torch.from_numpy(b.tables[0]).to(DEV).long()[t // 64]
+        b.k[blk, :, t % 64], b.v[blk, :, t % 64] = k, v
+        out, lse, avg = b.exact()
+        got = b.run()
+        # beside the roundings above, probabilities of fp16 lie on steps of 2^-35 of the largest: off by 2^-36 a key at most
+        u = torch.finfo(dt).eps / 2
+        tol = (u + 2.0 ** -11) * avg + u * out.abs() + 2.0 ** -24 + (m * 2.0 ** -36 * 1.5 if dt == HF else 0)
+        err = (got[0].double() - out).abs()
+        assert bool((err <= tol).all()), (at, float((err / tol).max()), float(out.abs().max()))
+        assert bool(((got[1].double() - lse).abs() <= 2.0 ** -12 + 2.0 ** -22 * lse.abs()).all())

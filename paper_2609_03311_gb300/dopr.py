@@ -508,6 +508,12 @@ class Rope:
         self._h = ctypes.c_void_p()
         _check(load().dopr_rope_create(ctypes.byref(self.cfg), ctypes.byref(self._h)))
 
+    def handle(self):
+        """The table's handle: a closed one's is NULL, which the library takes for no rotation."""
+        if not self._h:
+            raise ValueError("the rotary table is closed")
+        return self._h
+
     def close(self):
         if self._h:
             load().dopr_rope_destroy(self._h)
@@ -526,6 +532,7 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse
     (T, _, D), dt, dev = q.shape, q.dtype, q.device
     if dt not in _DTYPES:
         raise ValueError(f"rope_apply: float16, bfloat16 or float32, got {dt}")
+    handle = rope.handle()
     st, guard, on = _on(dev, stream)
     try:
         if q_out is None:
@@ -533,7 +540,7 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse
         if k is not None and k_out is None:
             k_out = torch.empty(k.shape, dtype=dt, device=dev)
         _check(load().dopr_rope_apply(
-            rope._h, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, on), _heads("q", q, T, D, dt, on),
+            handle, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, on), _heads("q", q, T, D, dt, on),
             _heads("q_out", q_out, T, D, dt, on), _heads("k", k, T, D, dt, on),
             _heads("k_out", k_out if k is not None else None, T, D, dt, on), int(inverse),
             _buf("status", status, torch.int32, 1, on), st))
@@ -548,13 +555,14 @@ def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | 
     """One layer's new rows k (rotated) and v [tokens, kv heads, head_dim] into the pages at slots; returns rotated q
     where q is given."""
     T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
+    handle = rope.handle() if rope is not None else None
     pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
     st, guard, on = _on(dev, stream)
     try:
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=dt, device=dev)
         _check(load().dopr_cache_append(
-            ctypes.byref(layout), rope._h if rope is not None else None, T,
+            ctypes.byref(layout), handle, T,
             _buf("positions", positions, torch.int32, T, on), _buf("slots", slots, torch.int64, T, on),
             _heads("q", q, T, D, dt, on), _heads("q_out", q_out if q is not None else None, T, D, dt, on),
             _heads("k", k, T, D, dt, on), _heads("v", v, T, D, dt, on), _buf("k_pool", k_pool, dt, pool, on),

@@ -146,3 +146,16 @@ def test_workspace_and_plan_sizes_grow_with_their_work(lib):
     assert lib.dopr_cache_extend_workspace(l) >= 3 * 3 * 4
     sizes = [lib.dopr_shared_attention_plan_bytes(l, 8, t) for t in (0, 1, 64, 1000)]
     assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+def test_the_binding_refuses_a_closed_rotary_table(lib):
+    # its handle is NULL, with which the library would store keys as they are
+    rope = dopr.Rope.__new__(dopr.Rope)
+    rope._h = ctypes.c_void_p()
+    x, pos = torch.zeros(4, 2, 128, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
+    pool = torch.zeros(8, 2, 64, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="closed"):
+        dopr.cache_append(layout(), pos.long(), x, x, pool, pool, rope=rope, positions=pos)
+    with pytest.raises(ValueError, match="closed"):
+        dopr.rope_apply(rope, pos, x)
+    rope.close()

@@ -955,3 +955,13 @@ def test_attention_of_one_heavy_key_among_many_light_ones(m, tokens, d, dt):
         err = (got[0].double() - out).abs()
         assert bool((err <= tol).all()), (at, float((err / tol).max()), float(out.abs().max()))
         assert bool(((got[1].double() - lse).abs() <= 2.0 ** -12 + 2.0 ** -22 * lse.abs()).all())
+
+
+def test_append_refuses_a_closed_rotary_table():
+    layout = dopr.make_cache_layout(2, 16, 1, 64, HF, 1, 2)
+    rope, x = dopr.Rope(8, 64), torch.ones(3, 1, 64, dtype=HF, device=DEV)
+    pools = [torch.zeros(2, 1, 16, 64, dtype=HF, device=DEV) for _ in range(2)]
+    rope.close()
+    with pytest.raises(ValueError, match="closed"):
+        dopr.cache_append(layout, torch.arange(3, device=DEV), x, x, *pools, rope=rope, positions=i32([1, 2, 3]))
+    assert not bool(pools[0].any()) and not bool(pools[1].any())

@@ -416,6 +416,13 @@ def _buf(name, t, dtype, n, device):
     return t.data_ptr()
 
 
+def _no_grad(name, t):
+    """The calls are not recorded for autograd: a tensor whose gradient would be lost is refused."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{name} requires a gradient, which this call does not record: use torch.no_grad() (the gradient of a "
+                         "rotation is rope_apply with inverse=True)")
+
+
 def _heads(name, t, tokens, head_dim, dtype, device):
     """A [tokens, heads, head_dim] tensor as the C ABI's view (strided, the last dimension contiguous): the bytes of a
     Heads, which a call takes faster than the structure."""
@@ -424,6 +431,7 @@ def _heads(name, t, tokens, head_dim, dtype, device):
     shape, strides = t.shape, t.stride()
     if tokens > 0x7fffffff:
         raise ValueError(f"{name}: {tokens} tokens, a call takes at most 2^31 - 1")
+    _no_grad(name, t)
     if len(shape) != 3 or shape[0] < tokens or shape[2] != head_dim or t.dtype != dtype or t.get_device() != device or \
             (head_dim > 1 and strides[2] != 1):
         raise ValueError(f"{name}: need [{tokens}, heads, {head_dim}] {dtype} on cuda:{device} with a contiguous last "
@@ -528,7 +536,8 @@ class Rope:
 
 def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse: bool = False, status=None, stream=None):
     """Rotary positions on q and, with it, k: [tokens, heads, head_dim] views of float16, bfloat16 or float32.  Returns
-    (q_out, k_out); pass q_out=q, k_out=k to work in place.  inverse: the gradient of the rotation."""
+    (q_out, k_out); pass q_out=q, k_out=k to work in place.  inverse: the gradient of the rotation, for a backward pass of the
+    caller's own (tensors that require a gradient are refused unless gradients are off)."""
     (T, _, D), dt, dev = q.shape, q.dtype, q.device
     if dt not in _DTYPES:
         raise ValueError(f"rope_apply: float16, bfloat16 or float32, got {dt}")
@@ -553,7 +562,9 @@ def rope_apply(rope: Rope, positions, q, k=None, q_out=None, k_out=None, inverse
 def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | None = None, positions=None, q=None,
                  q_out=None, status=None, stream=None):
     """One layer's new rows k (rotated) and v [tokens, kv heads, head_dim] into the pages at slots; returns rotated q
-    where q is given."""
+    where q is given.  Not recorded for autograd."""
+    _no_grad("k_pool", k_pool)
+    _no_grad("v_pool", v_pool)
     T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
     handle = rope.handle() if rope is not None else None
     pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
@@ -602,7 +613,9 @@ def shared_attention_workspace(layout: CacheLayout, n_q_heads: int, max_tokens: 
 def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None,
                      lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
     """Attention of q [max_tokens, q heads, head_dim], the plan's tokens, over their rows' prefixes and own keys.  lse:
-    float32 [max_tokens, q heads] to fill, or None."""
+    float32 [max_tokens, q heads] to fill, or None.  Not recorded for autograd: it has no backward pass."""
+    _no_grad("k_pool", k_pool)
+    _no_grad("v_pool", v_pool)
     T, hq, D = q.shape
     dt, dev = _TORCH_TYPES[layout.dtype], q.device
     if scale is None:

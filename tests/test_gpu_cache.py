@@ -965,3 +965,42 @@ def test_append_refuses_a_closed_rotary_table():
     with pytest.raises(ValueError, match="closed"):
         dopr.cache_append(layout, torch.arange(3, device=DEV), x, x, *pools, rope=rope, positions=i32([1, 2, 3]))
     assert not bool(pools[0].any()) and not bool(pools[1].any())
+
+
+def test_tensors_that_require_a_gradient_are_refused_unless_gradients_are_off():
+    b = Batch(4, 2, 64, HF, 16, [20], [(0, 5, 2)], seed=1)
+    rope, pos, x = dopr.Rope(64, 64), i32([1, 2]), b.q.clone().requires_grad_()
+    y = torch.zeros(2, 2, 64, dtype=HF, device=DEV, requires_grad=True)
+    plan, tables, z = dopr.shared_attention_plan(b.layout, 4, *b.args()), i32(b.tables), y.detach()
+    pools = [p.clone().requires_grad_() for p in (b.k, b.v)]
+    slots = torch.tensor([3, 4], device=DEV)
+    calls = [lambda: dopr.rope_apply(rope, pos, x), lambda: dopr.rope_apply(rope, pos, b.q, y),
+             lambda: dopr.rope_apply(rope, pos, b.q, q_out=x),
+             lambda: dopr.cache_append(b.layout, slots, y, z, b.k, b.v), lambda: dopr.cache_append(b.layout, slots, z, y, b.k, b.v),
+             lambda: dopr.cache_append(b.layout, slots, z, z, pools[0], b.v),
+             lambda: dopr.cache_append(b.layout, slots, z, z, b.k, b.v, rope=rope, positions=pos, q=x),
+             lambda: dopr.shared_attention(b.layout, plan, x, b.k, b.v, tables),
+             lambda: dopr.shared_attention(b.layout, plan, b.q, b.k, pools[1], tables)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+
+
+def test_a_rotation_in_a_graph_of_autograd_by_its_inverse():
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, rope, pos):
+            ctx.more = rope, pos
+            return dopr.rope_apply(rope, pos, x)[0]
+
+        @staticmethod
+        def backward(ctx, g):
+            return dopr.rope_apply(*ctx.more, g.contiguous(), inverse=True)[0], None, None
+
+    rope, pos = dopr.Rope(64, 32), i32([1, 2, 3])
+    x = torch.randn(3, 2, 64, device=DEV, requires_grad=True)
+    w = torch.randn(3, 2, 64, device=DEV)
+    (Turn.apply(x, rope, pos) * w).sum().backward()
+    assert torch.equal(x.grad, dopr.rope_apply(rope, pos, w, inverse=True)[0])

@@ -442,7 +442,8 @@ typedef struct {
  * no token a slot (tok_off all 0): INVALID_ARG (a length, new length or prefix
  * out of range, more than max_tokens new tokens, a position beyond 2^31 - 1),
  * OUT_OF_MEMORY (not enough free pages).  A page number outside the pool on
- * the stack or in a table is INVALID_ARG too; its tokens get slot -1.
+ * the stack or in a table is INVALID_ARG too: its tokens get slot -1, and that of
+ * a released row goes onto the stack as it is.
  * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
  */
 DOPR_API dopr_status dopr_cache_extend(const dopr_cache_layout *layout, const int32_t *seq_lens, int32_t *block_tables,

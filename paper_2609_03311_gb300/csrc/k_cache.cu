@@ -185,8 +185,11 @@ __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, b
       for (int g = threadIdx.x >> 5; g < total.tokens; g += WARPS) {  // a warp a row
         const int2 it = gone_rows[g];
         const int np = pages_of(held[it.x], page);
-        for (int p = threadIdx.x & 31; p < np; p += 32)
-          a.free_blocks[it.y + p] = a.tables[static_cast<int64_t>(it.x) * a.lay.max_blocks + p];
+        for (int p = threadIdx.x & 31; p < np; p += 32) {
+          const int block = a.tables[static_cast<int64_t>(it.x) * a.lay.max_blocks + p];
+          if (block < 0 || block >= a.lay.n_blocks) set_status(a.status, DOPR_ERR_INVALID_ARG);
+          a.free_blocks[it.y + p] = block;
+        }
       }
       at += total.pages;
     }

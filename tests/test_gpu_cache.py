@@ -1004,3 +1004,16 @@ def test_a_rotation_in_a_graph_of_autograd_by_its_inverse():
     w = torch.randn(3, 2, 64, device=DEV)
     (Turn.apply(x, rope, pos) * w).sum().backward()
     assert torch.equal(x.grad, dopr.rope_apply(rope, pos, w, inverse=True)[0])
+
+
+@pytest.mark.parametrize("rows", [2, 300])
+@pytest.mark.parametrize("bad", [-1, 6, 2 ** 31 - 1])
+def test_extend_says_so_when_a_released_page_is_outside_the_pool(bad, rows):
+    layout = dopr.make_cache_layout(6, 16, 2, 64, torch.float16, rows, 4)
+    tables, lens, new = np.zeros((rows, 4)), np.zeros(rows), np.zeros(rows)
+    tables[rows - 1, :2] = 3, bad
+    lens[rows - 1], new[rows - 1] = 20, -1
+    st, free = word(), i32([1, 2, 0, 0, 0, 0])
+    b = dopr.cache_extend(layout, i32(lens), i32(tables), free, i32([2]), i32(new), 20, status=st)
+    assert st.item() == dopr.ERR_INVALID_ARG and b.n_free.item() == 4 and free.tolist()[:4] == [1, 2, 3, bad]
+    assert not any(b.seq_lens.tolist())

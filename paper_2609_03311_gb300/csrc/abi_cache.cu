@@ -5,6 +5,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <initializer_list>
 #include <new>
 
 #include "device_common.cuh"
@@ -37,6 +38,12 @@ dopr_status cuda_status(cudaError_t e, const char* what) {
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+// Pointers to 32-bit numbers (NULL is aligned), which the kernels read and write whole.
+dopr_status check_words(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!aligned(p, 4)) return fail(DOPR_ERR_INVALID_ARG, "a pointer to 32-bit numbers is not aligned to 4 bytes");
+  return DOPR_OK;
+}
 
 dopr_status check_layout(const dopr_cache_layout* l) {
   if (!l) return fail(DOPR_ERR_INVALID_ARG, "layout is NULL");
@@ -193,6 +200,9 @@ dopr_status dopr_cache_extend(const dopr_cache_layout* layout, const int32_t* se
       (max_tokens > 0 && (!slots || !positions)) || !workspace)
     return fail(DOPR_ERR_INVALID_ARG, "a pointer is NULL");
   if (!aligned(workspace, 16)) return fail(DOPR_ERR_INVALID_ARG, "the workspace must be 16-byte aligned");
+  if (!aligned(slots, 8)) return fail(DOPR_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+  STATUS_TRY(check_words({seq_lens, block_tables, free_blocks, n_free, prefix, new_lens, seq_lens_out, n_free_out, tok_off, positions,
+                          status}));
   CacheExtendArgs a{};
   a.lay = *layout;
   a.seq_lens = seq_lens;
@@ -267,6 +277,7 @@ dopr_status dopr_rope_apply(const dopr_rope* rope, int32_t dtype, int32_t head_d
   if (!k != !k_out) return fail(DOPR_ERR_INVALID_ARG, "k and k_out belong together");
   if (n_tokens == 0) return DOPR_OK;  // views of no rows have no data
   STATUS_TRY(check_rope_use(rope, head_dim, positions));
+  STATUS_TRY(check_words({positions, status}));
   const int size = type_size(dtype);
   STATUS_TRY(check_view(q, "q", head_dim, size, false, 0));
   STATUS_TRY(check_view(q_out, "q_out", head_dim, size, false, q->n_heads));
@@ -290,6 +301,8 @@ dopr_status dopr_cache_append(const dopr_cache_layout* layout, const dopr_rope* 
   if (n_tokens == 0) return DOPR_OK;  // views of no rows have no data
   if (!slots || !k_pool || !v_pool) return fail(DOPR_ERR_INVALID_ARG, "slots, k_pool or v_pool is NULL");
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16)) return fail(DOPR_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+  if (!aligned(slots, 8)) return fail(DOPR_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+  STATUS_TRY(check_words({rope ? positions : nullptr, status}));
   if (!q != !q_out) return fail(DOPR_ERR_INVALID_ARG, "q and q_out belong together");
   if (q && !rope) return fail(DOPR_ERR_INVALID_ARG, "q without a rotary table");
   if (rope) STATUS_TRY(check_rope_use(rope, layout->head_dim, positions));
@@ -318,6 +331,7 @@ dopr_status dopr_shared_attention_plan(const dopr_cache_layout* layout, int32_t 
   STATUS_TRY(check_attention(layout, n_q_heads, max_tokens));
   if (!tok_off || !seq_lens || !plan) return fail(DOPR_ERR_INVALID_ARG, "tok_off, seq_lens or plan is NULL");
   if (!aligned(plan, 16)) return fail(DOPR_ERR_INVALID_ARG, "the plan must be 16-byte aligned");
+  STATUS_TRY(check_words({tok_off, seq_lens, prefix, status}));
   SharedPlanArgs a{};
   a.lay = *layout;
   a.Hq = n_q_heads;
@@ -347,6 +361,7 @@ dopr_status dopr_shared_attention(const dopr_cache_layout* layout, const void* p
     return fail(DOPR_ERR_INVALID_ARG, "plan, k_pool, v_pool, block_tables or workspace is NULL");
   if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(workspace, 32))
     return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned, the workspace 32-byte");
+  STATUS_TRY(check_words({block_tables, lse, status}));
   if (!(scale > 0.f) || !isfinite(scale)) return fail(DOPR_ERR_INVALID_ARG, "scale must be positive");
   STATUS_TRY(check_view(q, "q", layout->head_dim, 2, true, 0));
   STATUS_TRY(check_view(out, "out", layout->head_dim, 2, true, q->n_heads));

@@ -159,3 +159,29 @@ def test_the_binding_refuses_a_closed_rotary_table(lib):
     with pytest.raises(ValueError, match="closed"):
         dopr.rope_apply(rope, pos, x)
     rope.close()
+
+
+def test_buffers_that_are_not_aligned_to_their_type_are_refused(lib):
+    # a kernel's access to one would fault
+    l, odd, four = ctypes.byref(layout()), ctypes.c_void_p(4098), ctypes.c_void_p(4100)
+    good = [l, P, P, P, P, None, P, 4, P, P, P, P, P, P, None, None]
+    for i in (1, 2, 3, 4, 5, 6, 8, 9, 10, 11, 12, 13, 14):
+        a = list(good)
+        a[i] = odd
+        assert lib.dopr_cache_extend(*a) == dopr.ERR_INVALID_ARG, i
+    a = list(good)
+    a[11] = four  # slots, 64-bit
+    assert lib.dopr_cache_extend(*a) == dopr.ERR_INVALID_ARG
+    for i in (3, 4, 5, 6, 7):
+        a = [l, 8, 4, P, P, None, P, None, None]
+        a[i] = odd
+        assert lib.dopr_shared_attention_plan(*a) == dopr.ERR_INVALID_ARG, i
+    for i in (6, 9, 11):
+        a = [l, P, 4, heads(), P, P, P, 0.1, heads(), None, P, None, None]
+        a[i] = odd
+        assert lib.dopr_shared_attention(*a) == dopr.ERR_INVALID_ARG, i
+    for i, p in ((4, odd), (4, four), (11, odd)):
+        a = [l, None, 1, None, P, None, None, heads(n=2), heads(n=2), P, P, None, None]
+        a[i] = p
+        assert lib.dopr_cache_append(*a) == dopr.ERR_INVALID_ARG, i
+    assert b"aligned" in lib.dopr_last_error()

@@ -492,7 +492,9 @@ DOPR_API dopr_status dopr_rope_create(const dopr_rope_config *cfg, dopr_rope **o
 /* NULL is accepted.  No call that uses it may be pending. */
 DOPR_API dopr_status dopr_rope_destroy(dopr_rope *rope);
 
-/* A [tokens][n_heads][head_dim] view: strides in elements, head_dim contiguous. */
+/* A [tokens][n_heads][head_dim] view: strides in elements, head_dim contiguous.
+ * Inputs may repeat a row for all tokens (token_stride 0); of an output all of a
+ * token's heads, or all of a head's tokens, lie before those of the next. */
 typedef struct {
     void *data;
     int64_t token_stride;

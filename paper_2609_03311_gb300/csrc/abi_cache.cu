@@ -75,6 +75,18 @@ dopr_status check_view(const dopr_heads* v, const char* name, int head_dim, int 
   return DOPR_OK;
 }
 
+// A view that is written: no two of its rows share elements.
+dopr_status check_output(const dopr_heads* v, const char* name, int head_dim, int size, bool vectors, int heads, int tokens) {
+  STATUS_TRY(check_view(v, name, head_dim, size, vectors, heads));
+  if (tokens <= 1) return DOPR_OK;
+  const bool heads_inside = v->n_heads == 1 || v->head_stride <= v->token_stride;
+  const int64_t inner = v->n_heads == 1 ? head_dim : heads_inside ? v->head_stride : v->token_stride;
+  const int64_t outer = heads_inside ? v->token_stride : v->head_stride, n = heads_inside ? v->n_heads : tokens;
+  if (inner < head_dim || (outer - head_dim) / (n > 1 ? n - 1 : 1) < (n > 1 ? inner : 0) || outer < head_dim)
+    return fail(DOPR_ERR_INVALID_ARG, "%s: rows of an output overlap or interleave", name);
+  return DOPR_OK;
+}
+
 int type_size(int dtype) { return dtype == DOPR_F32 ? 4 : 2; }
 
 dopr_status check_rope_use(const dopr_rope* r, int head_dim, const int32_t* positions) {
@@ -280,13 +292,13 @@ dopr_status dopr_rope_apply(const dopr_rope* rope, int32_t dtype, int32_t head_d
   STATUS_TRY(check_words({positions, status}));
   const int size = type_size(dtype);
   STATUS_TRY(check_view(q, "q", head_dim, size, false, 0));
-  STATUS_TRY(check_view(q_out, "q_out", head_dim, size, false, q->n_heads));
+  STATUS_TRY(check_output(q_out, "q_out", head_dim, size, false, q->n_heads, n_tokens));
   RopeArgs a = rope_args(rope, n_tokens, head_dim, positions, status);
   a.inverse = inverse != 0;
   a.q = rope_view(q, q_out);
   if (k) {
     STATUS_TRY(check_view(k, "k", head_dim, size, false, 0));
-    STATUS_TRY(check_view(k_out, "k_out", head_dim, size, false, k->n_heads));
+    STATUS_TRY(check_output(k_out, "k_out", head_dim, size, false, k->n_heads, n_tokens));
     a.k = rope_view(k, k_out);
   }
   return cuda_status(launch_rope(dtype, a, static_cast<cudaStream_t>(cuda_stream)), "dopr_rope_apply");
@@ -312,7 +324,7 @@ dopr_status dopr_cache_append(const dopr_cache_layout* layout, const dopr_rope* 
   RopeArgs a = rope_args(rope, n_tokens, D, positions, status);
   if (q) {
     STATUS_TRY(check_view(q, "q", D, size, false, 0));
-    STATUS_TRY(check_view(q_out, "q_out", D, size, false, q->n_heads));
+    STATUS_TRY(check_output(q_out, "q_out", D, size, false, q->n_heads, n_tokens));
     a.q = rope_view(q, q_out);
   }
   a.k = rope_view(k, nullptr);
@@ -359,12 +371,13 @@ dopr_status dopr_shared_attention(const dopr_cache_layout* layout, const void* p
   if (max_tokens == 0) return DOPR_OK;  // views of no rows have no data
   if (!plan || !k_pool || !v_pool || !block_tables || !workspace)
     return fail(DOPR_ERR_INVALID_ARG, "plan, k_pool, v_pool, block_tables or workspace is NULL");
-  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16) || !aligned(workspace, 32))
-    return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned, the workspace 32-byte");
+  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16))
+    return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned");
   STATUS_TRY(check_words({block_tables, lse, status}));
   if (!(scale > 0.f) || !isfinite(scale)) return fail(DOPR_ERR_INVALID_ARG, "scale must be positive");
   STATUS_TRY(check_view(q, "q", layout->head_dim, 2, true, 0));
-  STATUS_TRY(check_view(out, "out", layout->head_dim, 2, true, q->n_heads));
+  STATUS_TRY(check_output(out, "out", layout->head_dim, 2, true, q->n_heads, max_tokens));
+  if (!aligned(workspace, 32)) return fail(DOPR_ERR_INVALID_ARG, "the workspace must be 32-byte aligned");
   SharedAttnArgs a{};
   a.lay = *layout;
   a.Hq = q->n_heads;

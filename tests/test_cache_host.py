@@ -185,3 +185,16 @@ def test_buffers_that_are_not_aligned_to_their_type_are_refused(lib):
         a[i] = p
         assert lib.dopr_cache_append(*a) == dopr.ERR_INVALID_ARG, i
     assert b"aligned" in lib.dopr_last_error()
+
+
+@pytest.mark.parametrize("tok,head,n,tokens,good", [
+    (512, 128, 4, 4, True), (128, 512, 4, 4, True), (128, 520, 4, 4, True), (640, 160, 4, 9, True), (512, 0, 1, 4, True), (128, 0, 1, 4, True), (0, 0, 1, 4, False),
+    (0, 128, 4, 4, False), (0, 128, 4, 1, True), (128, 128, 4, 4, False), (384, 128, 4, 4, False), (504, 128, 4, 4, False),
+    (128, 504, 4, 4, False), (128, 512, 4, 5, False), (64, 512, 4, 2, False), (120, 512, 4, 2, False), (2 ** 40, 2 ** 60, 4, 4, True),
+    (2 ** 40, 2 ** 40, 4, 4, False)])
+def test_outputs_whose_rows_overlap_are_refused(lib, tok, head, n, tokens, good):
+    # rows of 128 elements.  The workspace is misaligned, which is looked at last: nothing gets as far as a launch
+    l, q = layout(n_kv_heads=1), heads(n=n)
+    assert lib.dopr_shared_attention(ctypes.byref(l), P, tokens, q, P, P, P, 0.1, heads(tok=tok, head=head, n=n), None,
+                                     ctypes.c_void_p(4096 + 16), None, None) == dopr.ERR_INVALID_ARG
+    assert (b"workspace" if good else b"overlap") in lib.dopr_last_error()

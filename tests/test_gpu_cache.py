@@ -1017,3 +1017,20 @@ def test_extend_says_so_when_a_released_page_is_outside_the_pool(bad, rows):
     b = dopr.cache_extend(layout, i32(lens), i32(tables), free, i32([2]), i32(new), 20, status=st)
     assert st.item() == dopr.ERR_INVALID_ARG and b.n_free.item() == 4 and free.tolist()[:4] == [1, 2, 3, bad]
     assert not any(b.seq_lens.tolist())
+
+
+def test_outputs_whose_rows_overlap_are_refused():
+    b = Batch(4, 2, 64, HF, 16, [20], [(0, 5, 3)], seed=1)
+    rope, pos = dopr.Rope(64, 64), i32([1, 2, 3])
+    one = torch.zeros(1, 4, 64, dtype=HF, device=DEV).expand(3, 4, 64)
+    sliding = torch.zeros(1000, dtype=HF, device=DEV).as_strided((3, 4, 64), (128, 64, 1))
+    plan, tables, kv = dopr.shared_attention_plan(b.layout, 4, *b.args()), i32(b.tables), b.q[:, :2].contiguous()
+    for out in (one, sliding):
+        for call in (lambda: dopr.rope_apply(rope, pos, b.q, q_out=out), lambda: dopr.rope_apply(rope, pos, b.q, b.q, k_out=out),
+                     lambda: dopr.rope_apply(rope, pos, out, q_out=out),
+                     lambda: dopr.cache_append(b.layout, torch.arange(3, device=DEV), kv, kv, b.k, b.v, rope=rope, positions=pos, q=b.q,
+                                               q_out=out),
+                     lambda: dopr.shared_attention(b.layout, plan, b.q, b.k, b.v, tables, out=out)):
+            with pytest.raises(dopr.DoprError, match="overlap"):
+                call()
+    assert torch.equal(dopr.rope_apply(rope, pos, one)[0], torch.zeros(3, 4, 64, dtype=HF, device=DEV))

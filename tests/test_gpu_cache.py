@@ -1034,3 +1034,53 @@ def test_outputs_whose_rows_overlap_are_refused():
             with pytest.raises(dopr.DoprError, match="overlap"):
                 call()
     assert torch.equal(dopr.rope_apply(rope, pos, one)[0], torch.zeros(3, 4, 64, dtype=HF, device=DEV))
+
+
+def test_attention_of_two_streams_at_the_same_time():
+    # calls of two streams queue up behind a short wait of each, so that they run beside one another: tiles that fill tensor
+    # memory, few items and joins of both, with plans, workspaces and outputs of their own
+    bs = [Batch(8, 2, 128, BF, 64, [3000, 500], [(i % 2, 50, 1 + i) for i in range(20)], seed=1),
+          Batch(4, 2, 64, HF, 16, [700] * 9, [(i % 9, 9 + i, 1 + i % 2) for i in range(40)], seed=2)]
+    want = [b.run() for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    rounds, jobs = 12, []
+    for b, s in zip(bs, streams):
+        args, tables = b.args(), i32(b.tables)
+        plan = torch.empty(dopr.shared_attention_plan(b.layout, b.hq, *args).numel(), dtype=torch.uint8, device=DEV)
+        outs = [torch.full_like(b.q, 7.0) for _ in range(rounds)]
+        lses = [torch.zeros(b.T, b.hq, device=DEV) for _ in range(rounds)]
+        jobs.append((b, s, args, tables, plan, dopr.shared_attention_workspace(b.layout, b.hq, b.T), outs, lses, word()))
+    torch.cuda.synchronize()
+
+    def queue(i):
+        for b, s, args, tables, plan, ws, outs, lses, st in jobs:
+            dopr.shared_attention_plan(b.layout, b.hq, *args, plan=plan, status=st, stream=s)
+            dopr.shared_attention(b.layout, plan, b.q, b.k, b.v, tables, out=outs[i], lse=lses[i], workspace=ws, status=st, stream=s)
+
+    def check():
+        torch.cuda.synchronize()
+        for (b, _, _, _, _, _, outs, lses, st), (out, lse) in zip(jobs, want):
+            assert st.item() == 0
+            assert all(torch.equal(x, out) for x in outs) and all(torch.equal(x, lse) for x in lses)
+            for x in outs + lses:
+                x.fill_(7.0)
+        torch.cuda.synchronize()
+
+    for s in streams:
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(3000000)  # about 2 ms, in which everything is queued
+    for i in range(rounds):
+        queue(i)
+    check()
+    # the same as two branches of one graph
+    graph, fork = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=fork):
+        for s in streams:
+            s.wait_stream(fork)
+        for i in range(rounds):
+            queue(i)
+        for s in streams:
+            fork.wait_stream(s)
+    for _ in range(3):
+        graph.replay()
+        check()

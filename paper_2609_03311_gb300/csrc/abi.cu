@@ -1027,9 +1027,6 @@ bool make_gemm_operand_b(GemmOperandB* b, const void* base, uint64_t k, uint64_t
   return ok;
 }
 
-// The Q columns of a packed QKV buffer [rows][cols] as a 3-D tensor: 128 elements of a head
-// (innermost), rows, heads (256 bytes apart); the box takes 64 elements of box_heads heads over
-// box_rows rows, stored head after head (fp16, 128-byte swizzle).
 bool make_tmap_rows_of_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t heads, uint64_t tokens, int64_t head_stride,
                              int64_t token_stride, uint32_t box_heads, uint32_t box_tokens, bool half) {
   auto fn = encode_fn();
@@ -1044,6 +1041,9 @@ bool make_tmap_rows_of_heads(CUtensorMap* map, const void* base, uint64_t cols, 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The Q columns of a packed QKV buffer [rows][cols] as a 3-D tensor: 128 elements of a head
+// (innermost), rows, heads (256 bytes apart); the box takes 64 elements of box_heads heads over
+// box_rows rows, stored head after head (fp16, 128-byte swizzle).
 bool make_tmap_q_heads(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint32_t box_rows,
                        uint32_t box_heads) {
   auto fn = encode_fn();

@@ -19,8 +19,8 @@ constexpr int FILL_THREADS = 256;
 constexpr int FILL_HERE = 4096;
 constexpr int FEW_THREADS = 128, MANY_THREADS = 1024;  // of the CTA that takes the sums
 
-// Workspace header: whether the call goes ahead, the stack's height once released pages are back, new tokens.
-enum { WS_OK = 0, WS_TOP = 1, WS_TOKENS = 2 };
+// Workspace header: the stack's height once released pages are back, new tokens (0 where the call does not go ahead).
+enum { WS_TOP = 0, WS_TOKENS = 1 };
 
 __device__ __forceinline__ void set_status(int32_t* status, int code) {
   if (status) atomicCAS(status, 0, code);
@@ -167,7 +167,6 @@ __global__ void __launch_bounds__(SUM_THREADS) k_cache_sums(CacheExtendArgs a, b
   }
   if (threadIdx.x == 0) {
     a.tok_off[n] = static_cast<int32_t>(carry.tokens);
-    a.ws[WS_OK] = err == 0;
     a.ws[WS_TOP] = static_cast<int32_t>(top);
     a.ws[WS_TOKENS] = static_cast<int32_t>(carry.tokens);
     *a.n_free_out = static_cast<int32_t>(err ? stack : top - carry.pages);

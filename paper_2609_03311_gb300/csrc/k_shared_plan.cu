@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   pdl_trigger();
   __syncthreads();
   Head head{};
-  head.share = head.few_share = 1;
+  head.few_share = 1;
   head.Hq = a.Hq;
   head.max_tokens = a.max_tokens;
   head.n_ctas = n_ctas;
@@ -574,7 +574,6 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
       const bool of_few = it.flags & ITEM_FEW;
       const uint32_t entry_share = of_few ? few_share : share;
       Segment sg{};
-      sg.f = f_;
       sg.h = h;
       sg.b0 = on.block_from(c * entry_share, it.blocks);
       sg.b1 = on.block_from((c + 1) * entry_share, it.blocks);
@@ -641,11 +640,7 @@ __global__ void __launch_bounds__(THREADS) k_shared_plan(SharedPlanArgs a, Plan 
   }
   if (threadIdx.x == 0) {
     if (fits) {
-      head.tokens = n_sorted_tok;
-      head.n_items = n_items;
-      head.n_flat = n_flat;
       head.n_join = n_join;
-      head.share = share;
       head.few_share = few_share;
       head.tile_ctas = tile_ctas;
     }

@@ -81,7 +81,7 @@ enum : uint32_t {
 // What a CTA has of a flat entry, with what its warps need to know of the item and of the run that its first page lies in: a
 // load each from here to the block table and to the rows.
 struct alignas(16) Segment {
-  int f, h;           // flat entry, kv head
+  int h;              // kv head
   uint32_t b0, b1;    // its blocks here
   int tok, n_tok, run, n_runs;
   int prefix_keys, pages;
@@ -107,8 +107,8 @@ struct alignas(16) Piece {
   int pad;
 };
 struct alignas(16) Head {
-  int tokens, n_items, n_flat, n_join;
-  uint32_t share, few_share;  // of the lines: a CTA's part of tiles, a warp's of few items
+  int n_join;
+  uint32_t few_share;  // of the few items' line: a warp's part
   int tile_ctas;              // the CTAs that take tiles
   // what the plan was made for: its runs' pages lie in tables of max_blocks entries a row
   int Hq, max_tokens, n_ctas;

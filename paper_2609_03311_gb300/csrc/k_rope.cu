@@ -156,9 +156,11 @@ bool aligned16(const void* p, int64_t s0, int64_t s1, int size) {
 
 template <typename T, int VEC, bool INTER>
 cudaError_t launch(const RopeArgs& a, cudaStream_t st) {
-  // few tokens leave most SMs idle: more threads a token make fewer turns over the heads (one token 2.3 us, with 128 2.8;
-  // 64 rows into the cache 2.7 and 3.1); of many tokens the heads fill 128 more evenly (a chunk of 26,800: 110 us, with 256 138)
-  const int threads = a.n_tokens <= 512 ? MAX_THREADS : MAX_THREADS / 2;
+  // few tokens leave most SMs idle: more threads a token make fewer turns over the heads; of many tokens the heads fill 128 more
+  // evenly.  40 heads of 128 in bf16, with 256 threads and with 128: one token 2.5 and 2.8 us, 128 2.6 and 2.9, 256 3.0 and 3.2,
+  // 384 3.7 and 3.4, 640 5.6 and 4.0; a chunk of 26,800 into the cache 138 and 110.  (24 heads in 32 bits: 384 2.8 and 3.0, 512
+  // 3.6 and 3.2; 10 heads of 64: the same to 256, 384 2.4 and 2.0.)
+  const int threads = a.n_tokens <= 256 ? MAX_THREADS : MAX_THREADS / 2;
   return launch_dependent(k_rope<T, VEC, INTER>, dim3(a.n_tokens < 65536 ? a.n_tokens : 65536), threads, 0, st, a);
 }
 template <typename T>

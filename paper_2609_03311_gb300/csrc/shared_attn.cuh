@@ -33,9 +33,11 @@ constexpr int BLOCK = 128;  // columns of a block of tiles
 constexpr int PIECE = 16;   // of few items
 constexpr int MAX_CTAS = 256;
 constexpr int JOIN_ROWS = 8;
-// Rows of more parts than this are joined by two warps each, JOIN_ROWS / 2 of them at a time: 64 queries of one document, 19
-// parts a row, 46.3 us with one warp, 45.0 with two; one token, 12 parts, 8.1 with one, 8.6 with two.
-constexpr int PARTS_A_WARP = 12;
+// Rows of more parts than this are joined by two warps each, JOIN_ROWS / 2 of them at a time.  Attention of n queries of one
+// document, with one warp and with two: 11 to 13 parts a row: n = 1 9.3 and 9.0 us, 16 15.6 and 14.6, 64 20.4 and 19.8; 9 or 10:
+// 1 8.8 and 9.0, 64 20.2 and 19.4, but 100 39.0 and 41.2, 128 41.8 and 43.5 (more rows than the SMs hold at once, two warps each);
+// 19: 64 46.1 and 44.1.
+constexpr int PARTS_A_WARP = 10;
 __host__ __device__ inline int rows_a_piece(int parts) { return parts > PARTS_A_WARP ? JOIN_ROWS / 2 : JOIN_ROWS; }
 constexpr int WORKERS = 8;  // warps of a CTA that take few items
 // Lengths on the lines.  Tiles, about 480 clocks each: a block of keys that all rows see, another block (masked, and often of

@@ -1084,3 +1084,43 @@ def test_attention_of_two_streams_at_the_same_time():
     for _ in range(3):
         graph.replay()
         check()
+
+
+@pytest.mark.parametrize("d,dt", [(128, BF), (64, HF)])
+def test_pages_beyond_32_bits_of_elements(d, dt):
+    # pools of more than 2^32 elements, of which the last pages are used: append, few rows and tiles
+    hkv, page, blocks = 8, 128, 2 ** 32 // (8 * 128 * d) + 700
+    layout = dopr.make_cache_layout(blocks, page, hkv, d, dt, 4, 40)
+    pools = [torch.empty(blocks, hkv, page, d, dtype=dt, device=DEV) for _ in range(2)]
+    lens, new, prefix = [3000, 20, 50, 9], [0, 1, 30, 9], [-1, 0, 0, -1]
+    tables = np.zeros((4, 40))
+    tables[0, :24], tables[1, 0], tables[2, 0], tables[3, 0] = blocks - 1 - 20 * np.arange(24), blocks - 2, blocks - 3, blocks - 4
+    tables, g = i32(tables), torch.Generator(DEV).manual_seed(d)
+    rows = []
+    for i, n in enumerate(lens):
+        k, v = (torch.randn(n, hkv, d, generator=g, device=DEV).to(dt) for _ in range(2))
+        t = torch.arange(n, device=DEV)
+        dopr.cache_append(layout, tables[i].long()[t // page] * page + t % page, k, v, *pools)
+        rows.append((k, v))
+        b, at = int(tables[i, (n - 1) // page]), (n - 1) % page
+        assert torch.equal(pools[0][b, :, at], k[-1]) and torch.equal(pools[1][b, :, at], v[-1])
+    b = Batch(16, hkv, d, dt, page, lens[:1], [(0, 20, 1), (0, 50, 30), (-1, 9, 9)], seed=1)
+    b.rows, b.layout, b.tables, b.k, b.v = rows, layout, tables.cpu().numpy(), *pools
+    assert b.lens == lens and b.new == new and b.prefix == prefix
+    b.check(b.run())
+
+
+def test_a_step_of_no_tokens():
+    b = Batch(4, 2, 64, HF, 16, [40], [(0, 5, 1), (-1, 3, 0)], seed=1)
+    none, st, off = b.q[:0], word(), i32([0, 0, 0, 0])
+    for T in (0, 7):
+        plan = dopr.shared_attention_plan(b.layout, b.hq, off, i32(b.lens), i32(b.prefix), T, status=st)
+        q, out = (torch.full((T, 4, 64), x, dtype=HF, device=DEV) for x in (1.0, 7.0))
+        dopr.shared_attention(b.layout, plan, q, b.k, b.v, i32(b.tables), out=out, status=st)
+        assert bool((out == 7).all())
+        e = dopr.cache_extend(b.layout, i32(b.lens), i32(b.tables), i32([0] * 8), i32([0]), i32([0, 0, 0]), T, status=st)
+        assert e.seq_lens.tolist() == b.lens and e.tok_off.tolist() == [0] * 4 and e.slots.tolist() == [-1] * T
+    rope = dopr.Rope(8, 64)
+    dopr.cache_append(b.layout, torch.empty(0, dtype=torch.int64, device=DEV), none[:, :2], none[:, :2], b.k, b.v, rope=rope,
+                      positions=i32([]), q=none)
+    assert st.item() == 0

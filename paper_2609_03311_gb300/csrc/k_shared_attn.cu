@@ -337,7 +337,8 @@ __device__ __noinline__ void mend_row(const SharedAttnArgs& a, const Plan& plan,
 #pragma unroll
   for (int i = 0; i < W; ++i) x[i] = make_float2(0.f, 0.f);
   float m = -INFINITY, l = 0.f;
-  for (int j = 0; j < s.n_runs; ++j) {
+  // (the row's own keys first, the prefix last: where a step's new values are bad, all of its rows end at once)
+  for (int j = s.n_runs - 1; j >= 0; --j) {
     const Run run = plan.runs[s.run + j];
     const int from = run.off * unit;
     if (run.token >= 0 && (own.x >= own.y || from != own.x || run.keys == 0)) continue;

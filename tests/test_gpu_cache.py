@@ -1124,3 +1124,27 @@ def test_a_step_of_no_tokens():
     dopr.cache_append(b.layout, torch.empty(0, dtype=torch.int64, device=DEV), none[:, :2], none[:, :2], b.k, b.v, rope=rope,
                       positions=i32([]), q=none)
     assert st.item() == 0
+
+
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+def test_attention_of_a_step_whose_new_rows_are_all_bad(what):
+    # a model that has come apart: queries, new keys or new values are NaN, on a long document and beside a good request
+    b = Batch(32, 8, 128, BF, 64, [131072, 200], [(0, 4, 4) for i in range(64)] + [(1, 9, 9)], seed=5)
+    want = b.run()
+    T = 64 * 4
+    if what == "q":
+        b.q[:T] = math.nan
+    else:
+        pool = b.k if what == "k" else b.v
+        for i in range(2, 66):
+            pool[int(b.tables[i, 0]), :, :4] = math.nan
+    plan, tables = dopr.shared_attention_plan(b.layout, b.hq, *b.args()), i32(b.tables)
+    ws, st = dopr.shared_attention_workspace(b.layout, b.hq, b.T), word()
+    dopr.shared_attention(b.layout, plan, b.q, b.k, b.v, tables, workspace=ws)
+    a, z = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    a.record()
+    got = dopr.shared_attention(b.layout, plan, b.q, b.k, b.v, tables, workspace=ws, status=st)
+    z.record()
+    z.synchronize()
+    assert st.item() == 0 and bool(torch.isnan(got[:T]).all()) and torch.equal(got[T:], want[0][T:])
+    assert a.elapsed_time(z) < 20

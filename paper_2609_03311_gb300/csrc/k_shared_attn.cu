@@ -19,13 +19,14 @@
 //                2^8 (f16: 2^4; P stays within the type's range until then)
 //   P is rounded to the inputs' type for its product with V, as the tensor cores take it; maxima, sums, O and parts stay in 32
 //   bits, and a row's sum adds up P before the rounding.
-//   2,048 rows of 32 heads over 16,384 keys: 352 us, 1.56 PFLOP/s.  A block of two tiles takes 2,700 clocks of which the tensor
+//   2,048 rows of 32 heads over 16,384 keys: 346 us, 1.59 PFLOP/s (1.46 in calls that follow one another for seconds, under the
+//   power limit).  A block of two tiles takes 2,700 clocks of which the tensor
 //   cores work 2,050: a tile's S, softmax, P V and next S wait for one another (TMEM, full with two of S and of O, has no
 //   room for a second S), so a second tile fills the gaps and P goes over in halves (371 us when it went as one).  64 rows of
-//   a token over 32,768 keys: 44 us, 37 of them here, 26 of those in the blocks; the rest is start, partial results, joining.
+//   a token over 32,768 keys: 43 us, 26 of them in the blocks; the rest is start, partial results, joining.
 //   Few items: warps 4-11 each walk over a share of their own, with 16-row warp-level products and 16-byte copies: a 16-row
 //   box by TMA takes about 80 ns of an SM (256 tokens over 64 ragged documents in pages of 16: 73 us by TMA, 63 with 16-byte
-//   copies then; 53 now, 4.8 TB/s).
+//   copies then; 51 now, 5.0 TB/s).
 // Columns that a row does not see are left out by selection, not by arithmetic: what a page holds there cannot matter.
 // Values would (0 x NaN), so rows of V past a run's keys are zero in shared memory.  A value that one token sees and
 // another of the item does not would too: rows that end with a NaN though their scores have none are looked at when the CTA has
@@ -1253,7 +1254,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 // The plan may be read before this kernel's wait because the attention's launch is an ordinary one, which begins when the plan
 // is complete, and this one begins behind it.  (The attention as a dependent launch and the plan read behind the wait: one
 // token 9.2 us, 64 queries 46.1, ragged documents 54.7, 16 documents 161; so 8.9, 44.9, 53.9, 158.)
-// 64 rows of a token, 19 parts each: about 7 us; 5,000 tokens of 16 documents, of which a third has two parts: 14.
+// With cold caches: 64 rows of a token, 19 parts each, 11.7 us; 6,784 tokens of 16 documents, a third of them in two parts, 15.3.
 template <typename T, int D>
 __global__ void __launch_bounds__(32 * JOIN_ROWS, JOIN_CTAS)
     k_shared_join(const __grid_constant__ SharedAttnArgs a, const __grid_constant__ Plan plan, int n_ctas) {

@@ -6,7 +6,7 @@
 // prefix keep their order).  Made once a step and used by every layer.  Bound by the latency of some twenty short phases:
 // lists, items and runs stay in shared memory where they fit, a sum over the block takes one barrier and two counts where
 // they fit, and what rows, items and entries hold several of (items, runs, tokens, segments) is spread over a warp's lanes.
-// 512 threads: 11 us for one token, 15 for 64 queries of one document, 22 for 256 of 64 documents, 31 for 5,000 tokens of 200
+// 512 threads: 12 us for one token, 18 for 64 queries of one document, 24 for 256 of 64 documents, 32 for 6,784 tokens of 200
 // queries.  (As it was then, 1024 threads to 512 to 256: 12.1, 10.9, 10.7; 15.7, 14.1, 13.6; 20.8, 20.9, 25.9; 26.4, 28.7, 37.5:
 // a barrier and a sum cost more the more warps there are.)
 #include <limits.h>

@@ -360,7 +360,9 @@ def pack_order_noalloc(store: Store, q_offsets: torch.Tensor, doc_ids: torch.Ten
 
 # ------------------------------------------------------------------ paged prefix cache
 # Every call below runs on the tensors' device, on `stream` (default: that device's current stream), and returns once
-# its work is queued.  `status`: an int32 tensor of one element that keeps the first device error (a status number).
+# its work is queued.  `status`: an int32 tensor of one element that keeps the first device error (a status number); without
+# it device errors go unnoticed.  Rows that a call leaves as they were (a position that is negative or beyond the table, places
+# behind the last token) are undefined in outputs that the binding allocates.
 
 class CacheLayout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_blocks", "page", "n_kv_heads", "head_dim", "dtype", "n_seqs",
@@ -586,7 +588,8 @@ def cache_append(layout: CacheLayout, slots, k, v, k_pool, v_pool, rope: Rope | 
 
 def shared_attention_plan(layout: CacheLayout, n_q_heads: int, tok_off, seq_lens, prefix, max_tokens: int, plan=None,
                           status=None, stream=None) -> torch.Tensor:
-    """How a step's attention is split: made once a step, used by every layer (of these sizes, on this device)."""
+    """How a step's attention is split: made once a step, used by every layer (of this very layout, n_q_heads and max_tokens,
+    on this device)."""
     dev = seq_lens.device
     n = layout.n_seqs
     st, guard, on = _on(dev, stream)
@@ -613,7 +616,9 @@ def shared_attention_workspace(layout: CacheLayout, n_q_heads: int, max_tokens: 
 def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None,
                      lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
     """Attention of q [max_tokens, q heads, head_dim], the plan's tokens, over their rows' prefixes and own keys.  lse:
-    float32 [max_tokens, q heads] to fill, or None.  Not recorded for autograd: it has no backward pass."""
+    float32 [max_tokens, q heads] to fill, or None.  workspace: shared_attention_workspace(...), for all layers; without
+    it each call allocates one, hundreds of megabytes for thousands of tokens.  Not recorded for autograd: it has no
+    backward pass."""
     _no_grad("k_pool", k_pool)
     _no_grad("v_pool", v_pool)
     T, hq, D = q.shape

@@ -252,6 +252,17 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, unsigned block, si
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
+// An ordinary launch, whose status is its own (not an error that an earlier call left behind, as cudaGetLastError's may be).
+template <typename... P, typename... A>
+cudaError_t launch_ordinary(void (*kernel)(P...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // Tensor map helper (driver entry point resolved at run time).
 // 2-D map over 16-bit elements (fp16 when `half` is set, else bf16).
 bool make_tmap_16b_2d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t row_stride_bytes,

@@ -181,8 +181,7 @@ cudaError_t launch_type(const RopeArgs& a, cudaStream_t st) {
 cudaError_t launch_rope_table(const double* freq, double gain, int max_position, int half, float2* table,
                               cudaStream_t st) {
   const int64_t n = static_cast<int64_t>(max_position) * half;
-  k_rope_table<<<static_cast<unsigned>((n + 255) / 256), 256, 0, st>>>(freq, gain, max_position, half, table);
-  return cudaGetLastError();
+  return launch_ordinary(k_rope_table, dim3(static_cast<unsigned>((n + 255) / 256)), 256, 0, st, freq, gain, max_position, half, table);
 }
 
 cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st) {

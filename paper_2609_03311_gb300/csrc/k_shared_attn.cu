@@ -1393,8 +1393,7 @@ cudaError_t launch(const SharedAttnArgs& a, int num_sms, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(k_shared_attn<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::BYTES);
   if (e != cudaSuccess) return e;
   // not a dependent launch: the joining kernel relies on that
-  k_shared_attn<T, D><<<n_ctas, THREADS, Smem<D>::BYTES, st>>>(tm_q8, tm_q1, tm_k, tm_v, args, plan);
-  e = cudaGetLastError();
+  e = launch_ordinary(k_shared_attn<T, D>, dim3(n_ctas), THREADS, Smem<D>::BYTES, st, tm_q8, tm_q1, tm_k, tm_v, args, plan);
   if (e != cudaSuccess) return e;
   // as many blocks as could have work, up to what the SMs hold at once
   const int64_t pieces = max_items(a.lay.n_seqs, a.Hq / a.lay.n_kv_heads, a.max_tokens) * a.lay.n_kv_heads +

@@ -106,8 +106,8 @@ def test_the_paged_caches_kernels_wait_before_they_read_what_others_write():
                for k, _, body in _kernels(_source(s)) if k != "k_rope_table"}
     assert set(kernels) == {"k_cache_sums", "k_cache_fill", "k_rope", "k_shared_plan", "k_shared_attn", "k_shared_join"}
     launches = _source("k_shared_attn.cu")
-    assert len(re.findall(r"\bk_shared_attn<T, D><<<", launches)) == 1 and "launch_dependent(k_shared_attn" not in launches
-    order = [launches.index("k_shared_attn<T, D><<<"), launches.index("launch_dependent(k_shared_join<T, D>")]
+    assert "launch_dependent(k_shared_attn" not in launches
+    order = [launches.index("launch_ordinary(k_shared_attn<T, D>"), launches.index("launch_dependent(k_shared_join<T, D>")]
     assert order == sorted(order)
     attention = kernels.pop("k_shared_attn")
     assert "pdl_wait()" not in attention and attention.count("pdl_trigger()") == 1

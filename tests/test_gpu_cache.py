@@ -1148,3 +1148,17 @@ def test_attention_of_a_step_whose_new_rows_are_all_bad(what):
     z.synchronize()
     assert st.item() == 0 and bool(torch.isnan(got[:T]).all()) and torch.equal(got[T:], want[0][T:])
     assert a.elapsed_time(z) < 20
+
+
+def test_a_refused_allocation_does_not_fail_the_calls_behind_it():
+    from paper_2609_03311_gb300 import synth
+
+    shape = synth.ModelShape("oom", n_layers=2, hidden=256, n_q_heads=4, n_kv_heads=2, head_dim=128, ffn=384, vocab=512)
+    b = Batch(4, 2, 64, HF, 16, [20], [(0, 5, 2)], seed=1)
+    want = b.run()
+    for call in (lambda: b.run(), lambda: dopr.Rope(64, 64)):
+        with pytest.raises(dopr.DoprError):
+            dopr.Store(dopr.make_config(shape, max_position=512), max_doc_id=15, pool_bytes=1 << 50)
+        got = call()
+    got = b.run()
+    assert torch.equal(got[0], want[0])

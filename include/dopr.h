@@ -583,6 +583,74 @@ DOPR_API int64_t dopr_shared_attention_workspace(const dopr_cache_layout *layout
                                                  int32_t max_tokens);
 
 /*
+ * RMSNorm of each query and key head, and rotary positions, in one pass (Sec. 4.1's backbone norms q and k so):
+ *   y_i = x_i g_i / sqrt(mean of x^2 over the head + eps), then dopr_rope_apply's turn of y.
+ * Arguments as there; rope NULL: no turn, positions is not read.  eps > 0.  Gains [head_dim] of gain_dtype, one for all
+ * heads of q, one for k; NULL: ones.  k, k_out NULL: q alone.  Computed in 32 bits, rounded once.  An output may be its input;
+ * otherwise outputs overlap nothing.  Rows with positions[t] < 0 are left as they were.  Device error: INVALID_ARG (a
+ * position >= max_position; its row is left).  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_head_norm_rope(const dopr_rope *rope, int32_t dtype, int32_t head_dim, int32_t n_tokens,
+                                         const int32_t *positions, float eps, int32_t gain_dtype, const dopr_heads *q,
+                                         const void *q_gain, const dopr_heads *q_out, const dopr_heads *k,
+                                         const void *k_gain, const dopr_heads *k_out, int32_t *status,
+                                         void *cuda_stream);
+
+/*
+ * Its gradients: from those of its outputs (dq_out, dk_out) and its inputs q, k, those of the inputs (dq, dk: views that may
+ * be dq_out, dk_out or q, k themselves) and, where asked for, of the gains: dq_gain, dk_gain [head_dim] float, overwritten (the
+ * sum over all rows with a position and all heads, in a fixed order).  An input that repeats a row (token_stride 0) gets a gradient
+ * for each token.  dk_out, k, dk NULL: q alone.
+ *   workspace dopr_head_norm_rope_workspace(head_dim) bytes, 16-byte aligned; NULL where no gain's gradient is asked for.
+ */
+DOPR_API dopr_status dopr_head_norm_rope_backward(const dopr_rope *rope, int32_t dtype, int32_t head_dim, int32_t n_tokens,
+                                                  const int32_t *positions, float eps, int32_t gain_dtype,
+                                                  const dopr_heads *dq_out, const dopr_heads *q, const void *q_gain,
+                                                  const dopr_heads *dq, float *dq_gain, const dopr_heads *dk_out,
+                                                  const dopr_heads *k, const void *k_gain, const dopr_heads *dk,
+                                                  float *dk_gain, void *workspace, int32_t *status, void *cuda_stream);
+/* Bytes of its workspace; -1 on a bad head_dim. */
+DOPR_API int64_t dopr_head_norm_rope_workspace(int32_t head_dim);
+
+/*
+ * The same cache in 4 bits: pools of 4.25 bits an element in place of 16.  layout, tables, slots, plan and workspace are those
+ * of the calls above; layout->dtype is the type of the rows (q, k, v and out).  32 elements of a head that follow one another
+ * (a group) share a scale s and are held as whole numbers c, -7 .. 7, an element as c s.  A scale is a byte, five bits of
+ * exponent above three of mantissa: s is the fp16 number of the bits byte << 7.  It is the smallest that is at least
+ * max |x| / 7, at most 9216 (byte 0xe1); c = x / s to the nearest whole number, ties away from zero: |x - c s| <= s / 2 for
+ * |x| <= 64512.  c s is exact in fp16 and bf16.  A group with a value that is not finite or above 65504 in magnitude is held as
+ * NaN (byte 0xff) and stores DOPR_ERR_RANGE in *status; bytes above 0xe1 stand for NaN.
+ * k_pool, v_pool: dopr_cache_4bit_pool_bytes(layout) bytes each, 16-byte aligned: [n_blocks][n_kv_heads] pages, each the codes
+ * of its rows [page][head_dim / 2 bytes], then their scales [page][head_dim / 32].  Of eight codes c + 8 in a 32-bit word, element
+ * 2 i is at bits 4 i and element 2 i + 1 at bits 16 + 4 i.  Memory that was never written must not be read as keys, so clear new pools.
+ */
+DOPR_API int64_t dopr_cache_4bit_pool_bytes(const dopr_cache_layout *layout);
+
+/*
+ * One layer's new rows into the pages at slots[t], as dopr_cache_append: v as it is; k, and q into q_out, normed where
+ * eps > 0 (gains as in dopr_head_norm_rope; eps 0: not normed, gains NULL) and turned where rope is not NULL.  k is rounded to
+ * layout->dtype, then held: the same bits as dopr_head_norm_rope and an append of its output.  q, q_out NULL: keys and
+ * values alone; q needs a norm or a rope.  Views are 16-byte aligned with strides multiples of 16 bytes; rotary_dim is a
+ * multiple of 16.  Rows with slots[t] < 0 are not stored; with positions[t] < 0 (and a rope) nothing of a row is written.  Slots
+ * are distinct.  Device errors: INVALID_ARG (a slot outside the pool, a position >= max_position; that row is left), RANGE.
+ * Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_cache_append_4bit(const dopr_cache_layout *layout, const dopr_rope *rope, int32_t n_tokens,
+                                            const int32_t *positions, const int64_t *slots, float eps, int32_t gain_dtype,
+                                            const dopr_heads *q, const void *q_gain, const dopr_heads *q_out,
+                                            const dopr_heads *k, const void *k_gain, const dopr_heads *v, void *k_pool,
+                                            void *v_pool, int32_t *status, void *cuda_stream);
+
+/*
+ * What the pages hold at slots[t], in layout->dtype (exact): k_out, v_out views of n_rows rows, 16-byte aligned with strides
+ * multiples of 16 bytes.  Rows with slots[t] < 0 are left as they were; slots may repeat.  Device error: INVALID_ARG (a slot
+ * outside the pool; its row is left).  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ */
+DOPR_API dopr_status dopr_cache_read_4bit(const dopr_cache_layout *layout, int32_t n_rows, const int64_t *slots,
+                                          const void *k_pool, const void *v_pool, const dopr_heads *k_out,
+                                          const dopr_heads *v_out, int32_t *status, void *cuda_stream);
+
+/*
  * Per-kernel accounting, for measurement.  Every dopr_score call counts its
  * kernel launches per kernel family (pack, embed, gemm_qkv, qknorm_rope,
  * attention, gemm_o, rmsnorm, gemm_gate_up, gemm_down, score, prefix_store;

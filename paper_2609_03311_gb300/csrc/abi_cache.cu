@@ -10,6 +10,7 @@
 
 #include "device_common.cuh"
 #include "internal.h"
+#include "pages4.cuh"
 
 struct dopr_rope : dopr::Rope {};
 
@@ -188,6 +189,41 @@ dopr_status check_attention(const dopr_cache_layout* l, int n_q_heads, int max_t
   return DOPR_OK;
 }
 
+// Arguments that a norm of heads has in common with its gradients and with the append.
+dopr_status check_norm(float eps, int gain_dtype, const void* q_gain, const void* k_gain) {
+  if (!(eps > 0.f) || !isfinite(eps)) return fail(DOPR_ERR_INVALID_ARG, "eps must be positive");
+  if (!q_gain && !k_gain) return DOPR_OK;
+  if (gain_dtype < DOPR_F16 || gain_dtype > DOPR_F32) return fail(DOPR_ERR_INVALID_ARG, "unknown gain_dtype %d", gain_dtype);
+  if (!aligned(q_gain, type_size(gain_dtype)) || !aligned(k_gain, type_size(gain_dtype)))
+    return fail(DOPR_ERR_INVALID_ARG, "a gain is not aligned to its type");
+  return DOPR_OK;
+}
+dopr_status check_head_dim(int head_dim) {
+  if (head_dim <= 0 || head_dim % 2 || head_dim > 256)
+    return fail(DOPR_ERR_UNSUPPORTED, "head_dim must be even, at most 256 (got %d)", head_dim);
+  return DOPR_OK;
+}
+HeadNormArgs norm_args(const dopr_rope* r, int n_tokens, int head_dim, const int32_t* positions, float eps, int gain_dtype,
+                       const void* q_gain, const void* k_gain, int32_t* status) {
+  HeadNormArgs a{};
+  a.n_tokens = n_tokens;
+  a.head_dim = head_dim;
+  a.eps = eps;
+  a.positions = positions;
+  a.gain_dtype = gain_dtype;
+  a.q_gain = q_gain;
+  a.k_gain = k_gain;
+  a.page = 1;
+  a.status = status;
+  if (r) {
+    a.rotary = r->cfg.rotary_dim;
+    a.interleaved = r->cfg.layout == DOPR_ROPE_INTERLEAVED;
+    a.table = r->table;
+    a.max_position = r->cfg.max_position;
+  }
+  return a;
+}
+
 // SMs of the current device.
 dopr_status sm_count(int* n) {
   int dev = -1;
@@ -335,6 +371,153 @@ dopr_status dopr_cache_append(const dopr_cache_layout* layout, const dopr_rope* 
   a.page = layout->page;
   a.n_slots = (int64_t)layout->n_blocks * layout->page;
   return cuda_status(launch_rope(layout->dtype, a, static_cast<cudaStream_t>(cuda_stream)), "dopr_cache_append");
+}
+
+dopr_status dopr_head_norm_rope(const dopr_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_tokens, const int32_t* positions,
+                                float eps, int32_t gain_dtype, const dopr_heads* q, const void* q_gain, const dopr_heads* q_out,
+                                const dopr_heads* k, const void* k_gain, const dopr_heads* k_out, int32_t* status,
+                                void* cuda_stream) {
+  if (dtype < DOPR_F16 || dtype > DOPR_F32) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (n_tokens < 0) return fail(DOPR_ERR_INVALID_ARG, "n_tokens is negative");
+  STATUS_TRY(check_head_dim(head_dim));
+  STATUS_TRY(check_norm(eps, gain_dtype, q_gain, k_gain));
+  if (!k != !k_out) return fail(DOPR_ERR_INVALID_ARG, "k and k_out belong together");
+  if (n_tokens == 0) return DOPR_OK;  // views of no rows have no data
+  if (rope) STATUS_TRY(check_rope_use(rope, head_dim, positions));
+  STATUS_TRY(check_words({rope ? positions : nullptr, status}));
+  const int size = type_size(dtype);
+  STATUS_TRY(check_view(q, "q", head_dim, size, false, 0));
+  STATUS_TRY(check_output(q_out, "q_out", head_dim, size, false, q->n_heads, n_tokens));
+  HeadNormArgs a = norm_args(rope, n_tokens, head_dim, positions, eps, gain_dtype, q_gain, k_gain, status);
+  a.q = rope_view(q, q_out);
+  if (k) {
+    STATUS_TRY(check_view(k, "k", head_dim, size, false, 0));
+    STATUS_TRY(check_output(k_out, "k_out", head_dim, size, false, k->n_heads, n_tokens));
+    a.k = rope_view(k, k_out);
+  }
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_head_norm(dtype, a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_head_norm_rope");
+}
+
+dopr_status dopr_head_norm_rope_backward(const dopr_rope* rope, int32_t dtype, int32_t head_dim, int32_t n_tokens,
+                                         const int32_t* positions, float eps, int32_t gain_dtype, const dopr_heads* dq_out,
+                                         const dopr_heads* q, const void* q_gain, const dopr_heads* dq, float* dq_gain,
+                                         const dopr_heads* dk_out, const dopr_heads* k, const void* k_gain, const dopr_heads* dk,
+                                         float* dk_gain, void* workspace, int32_t* status, void* cuda_stream) {
+  if (dtype < DOPR_F16 || dtype > DOPR_F32) return fail(DOPR_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+  if (n_tokens < 0) return fail(DOPR_ERR_INVALID_ARG, "n_tokens is negative");
+  STATUS_TRY(check_head_dim(head_dim));
+  STATUS_TRY(check_norm(eps, gain_dtype, q_gain, k_gain));
+  if (!k != !dk_out || !k != !dk) return fail(DOPR_ERR_INVALID_ARG, "dk_out, k and dk belong together");
+  if (!k && dk_gain) return fail(DOPR_ERR_INVALID_ARG, "dk_gain without k");
+  if ((dq_gain || dk_gain) && (!workspace || !aligned(workspace, 16)))
+    return fail(DOPR_ERR_INVALID_ARG, "the gains' gradients need a workspace, 16-byte aligned");
+  STATUS_TRY(check_words({rope ? positions : nullptr, status, dq_gain, dk_gain}));
+  HeadNormArgs a = norm_args(rope, n_tokens, head_dim, positions, eps, gain_dtype, q_gain, k_gain, status);
+  a.dq_gain = dq_gain;
+  a.dk_gain = dk_gain;
+  a.ws = static_cast<float*>(workspace);
+  if (n_tokens > 0) {  // views of no rows have no data; the gains' gradients are zero then
+    if (rope) STATUS_TRY(check_rope_use(rope, head_dim, positions));
+    const int size = type_size(dtype);
+    STATUS_TRY(check_view(q, "q", head_dim, size, false, 0));
+    STATUS_TRY(check_view(dq_out, "dq_out", head_dim, size, false, q->n_heads));
+    STATUS_TRY(check_output(dq, "dq", head_dim, size, false, q->n_heads, n_tokens));
+    a.q = rope_view(dq_out, dq);
+    a.qx = rope_view(q, nullptr);
+    if (k) {
+      STATUS_TRY(check_view(k, "k", head_dim, size, false, 0));
+      STATUS_TRY(check_view(dk_out, "dk_out", head_dim, size, false, k->n_heads));
+      STATUS_TRY(check_output(dk, "dk", head_dim, size, false, k->n_heads, n_tokens));
+      a.k = rope_view(dk_out, dk);
+      a.kx = rope_view(k, nullptr);
+    }
+  }
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_head_norm_backward(dtype, a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_head_norm_rope_backward");
+}
+
+int64_t dopr_head_norm_rope_workspace(int32_t head_dim) {
+  if (check_head_dim(head_dim) != DOPR_OK) return -1;
+  return static_cast<int64_t>(HEAD_NORM_MAX_BLOCKS) * 2 * head_dim * static_cast<int64_t>(sizeof(float));
+}
+
+int64_t dopr_cache_4bit_pool_bytes(const dopr_cache_layout* layout) {
+  if (check_layout(layout) != DOPR_OK) return -1;
+  return layout->n_blocks * static_cast<int64_t>(layout->n_kv_heads) * pages4::page_bytes(layout->page, layout->head_dim);
+}
+
+dopr_status dopr_cache_append_4bit(const dopr_cache_layout* layout, const dopr_rope* rope, int32_t n_tokens,
+                                   const int32_t* positions, const int64_t* slots, float eps, int32_t gain_dtype,
+                                   const dopr_heads* q, const void* q_gain, const dopr_heads* q_out, const dopr_heads* k,
+                                   const void* k_gain, const dopr_heads* v, void* k_pool, void* v_pool, int32_t* status,
+                                   void* cuda_stream) {
+  STATUS_TRY(check_layout(layout));
+  if (n_tokens < 0) return fail(DOPR_ERR_INVALID_ARG, "n_tokens is negative");
+  if (eps != 0.f) STATUS_TRY(check_norm(eps, gain_dtype, q_gain, k_gain));
+  else if (q_gain || k_gain) return fail(DOPR_ERR_INVALID_ARG, "a gain without a norm (eps 0)");
+  if (!q != !q_out) return fail(DOPR_ERR_INVALID_ARG, "q and q_out belong together");
+  if (q && !rope && eps == 0.f) return fail(DOPR_ERR_INVALID_ARG, "q without a norm or a rotary table");
+  if (n_tokens == 0) return DOPR_OK;  // views of no rows have no data
+  if (!slots || !k_pool || !v_pool) return fail(DOPR_ERR_INVALID_ARG, "slots, k_pool or v_pool is NULL");
+  if (!aligned(k_pool, 16) || !aligned(v_pool, 16)) return fail(DOPR_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+  if (!aligned(slots, 8)) return fail(DOPR_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+  STATUS_TRY(check_words({rope ? positions : nullptr, status}));
+  const int D = layout->head_dim;
+  if (rope) {
+    STATUS_TRY(check_rope_use(rope, D, positions));
+    if (rope->cfg.rotary_dim % 16) return fail(DOPR_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16 (got %d)", rope->cfg.rotary_dim);
+  }
+  STATUS_TRY(check_view(k, "k", D, 2, true, layout->n_kv_heads));
+  STATUS_TRY(check_view(v, "v", D, 2, true, layout->n_kv_heads));
+  HeadNormArgs a = norm_args(rope, n_tokens, D, positions, eps, gain_dtype, q_gain, k_gain, status);
+  if (q) {
+    STATUS_TRY(check_view(q, "q", D, 2, true, 0));
+    STATUS_TRY(check_output(q_out, "q_out", D, 2, true, q->n_heads, n_tokens));
+    a.q = rope_view(q, q_out);
+  }
+  a.k = rope_view(k, nullptr);
+  a.v = rope_view(v, nullptr);
+  a.slots = slots;
+  a.k_pool = static_cast<uint8_t*>(k_pool);
+  a.v_pool = static_cast<uint8_t*>(v_pool);
+  a.page = layout->page;
+  a.n_slots = (int64_t)layout->n_blocks * layout->page;
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_append_4bit(layout->dtype, a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_cache_append_4bit");
+}
+
+dopr_status dopr_cache_read_4bit(const dopr_cache_layout* layout, int32_t n_rows, const int64_t* slots, const void* k_pool,
+                                 const void* v_pool, const dopr_heads* k_out, const dopr_heads* v_out, int32_t* status,
+                                 void* cuda_stream) {
+  STATUS_TRY(check_layout(layout));
+  if (n_rows < 0) return fail(DOPR_ERR_INVALID_ARG, "n_rows is negative");
+  if (n_rows == 0) return DOPR_OK;  // views of no rows have no data
+  if (!slots || !k_pool || !v_pool) return fail(DOPR_ERR_INVALID_ARG, "slots, k_pool or v_pool is NULL");
+  if (!aligned(k_pool, 16) || !aligned(v_pool, 16)) return fail(DOPR_ERR_INVALID_ARG, "the pools must be 16-byte aligned");
+  if (!aligned(slots, 8)) return fail(DOPR_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+  STATUS_TRY(check_words({status}));
+  const int D = layout->head_dim;
+  STATUS_TRY(check_output(k_out, "k_out", D, 2, true, layout->n_kv_heads, n_rows));
+  STATUS_TRY(check_output(v_out, "v_out", D, 2, true, layout->n_kv_heads, n_rows));
+  Read4Args a{};
+  a.n_rows = n_rows;
+  a.head_dim = D;
+  a.n_kv_heads = layout->n_kv_heads;
+  a.page = layout->page;
+  a.n_slots = (int64_t)layout->n_blocks * layout->page;
+  a.slots = slots;
+  a.k_pool = static_cast<const uint8_t*>(k_pool);
+  a.v_pool = static_cast<const uint8_t*>(v_pool);
+  a.k = rope_view(k_out, k_out);
+  a.v = rope_view(v_out, v_out);
+  a.status = status;
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  return cuda_status(launch_read_4bit(layout->dtype, a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_cache_read_4bit");
 }
 
 dopr_status dopr_shared_attention_plan(const dopr_cache_layout* layout, int32_t n_q_heads, int32_t max_tokens,

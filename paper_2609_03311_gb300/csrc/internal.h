@@ -493,6 +493,42 @@ struct RopeArgs {
 };
 cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st);
 
+// Norms of heads with rotary positions, their gradients, and the same on the way into 4-bit pages.
+constexpr int HEAD_NORM_MAX_BLOCKS = 1024;  // of the backward kernel: partial sums of the gains' gradients, 2 x head_dim each
+struct HeadNormArgs {
+  int n_tokens, head_dim, rotary;  // rotary 0: nothing turns, positions is not read
+  bool interleaved;
+  float eps;                       // 0: rows are not normed
+  const float2* table;
+  int max_position;
+  const int32_t* positions;
+  int gain_dtype;
+  const void *q_gain, *k_gain;     // null: ones
+  RopeView q, k;                   // backward: the outputs' gradients, and where the inputs' go
+  RopeView qx, kx;                 // backward: the inputs (in only)
+  float *dq_gain, *dk_gain;        // backward, null: not wanted
+  float* ws;                       // backward: [HEAD_NORM_MAX_BLOCKS][2][head_dim]
+  // 4-bit pages: keys and values go there (slots null: no pages, k like q)
+  RopeView v;                      // in only
+  const int64_t* slots;
+  uint8_t *k_pool, *v_pool;
+  int page;
+  int64_t n_slots;
+  int32_t* status;
+};
+cudaError_t launch_head_norm(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_head_norm_backward(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_append_4bit(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st);
+struct Read4Args {
+  int n_rows, head_dim, n_kv_heads, page;
+  int64_t n_slots;
+  const int64_t* slots;
+  const uint8_t *k_pool, *v_pool;
+  RopeView k, v;  // out only
+  int32_t* status;
+};
+cudaError_t launch_read_4bit(int dtype, const Read4Args& a, int num_sms, cudaStream_t st);
+
 struct SharedAttnArgs {
   dopr_cache_layout lay;
   int Hq, max_tokens;

@@ -1,0 +1,57 @@
+// pages4.cuh -- rows of the paged cache in 4 bits: 32 elements of a head that follow one another (a group) share a scale s and
+// are held as whole numbers c from -7 to 7, an element as c s.
+//
+// A scale is a byte, five bits of exponent above three of mantissa: the upper bits of the fp16 number, so bits << 7 is that
+// number.  Its four bits and the three of |c| make seven: c s is exact in fp16 and in bf16, and products of the tensor cores
+// take the very values that are held.  Finer scales would hold the rows better by at most the 6 % that rounding a scale up
+// costs on the mean, and round every value on its way to a product.
+//
+// s is the smallest scale that is at least max |x| / 7, at most SCALE_MAX; then |x - c s| <= s / 2 up to 7 SCALE_MAX = 64512.
+//
+// A page of a kv head lies in one piece: its rows' codes, then their scales.  Codes are c + 8, in 32-bit words of eight: element
+// 2 i of the eight at bits 4 i, element 2 i + 1 at 16 + 4 i, so that a mask over a word takes out a pair of elements that follow
+// one another, each in its half of the word.
+#pragma once
+
+#include <type_traits>
+
+#include "device_common.cuh"
+
+namespace dopr {
+namespace pages4 {
+
+constexpr int GROUP = 32;
+constexpr uint32_t SCALE_LAST = 0xe1;      // the largest scale's byte; those above stand for NaN
+constexpr float SCALE_MAX = 9216.f;
+constexpr uint32_t SCALE_NAN = 0xff;
+constexpr float HELD_MAX = 65504.f;        // rows above are refused, as by the library's other fp16 stores
+
+template <int D>
+constexpr int CODE_BYTES = D / 2;          // of a row
+template <int D>
+constexpr int SCALE_BYTES = D / GROUP;
+__host__ __device__ inline int64_t page_bytes(int page, int head_dim) { return static_cast<int64_t>(page) * (head_dim / 2 + head_dim / GROUP); }
+
+// The scale of a group with the largest magnitude `most`: its byte.  `inverse`: what elements are multiplied by, a little more
+// than 1 / s: an element half way between two codes goes to the larger one, and no other crosses a border by it (x / s, x of 11
+// bits and s of 4, is half way or at least 2^-13 off; the factor is 2^-20 off).
+__device__ __forceinline__ uint32_t scale_byte(float most, float& inverse) {
+  const float want = __fdiv_rn(most, 7.f);
+  // steps of three bits of mantissa, of 2^-17 at the low end
+  const int e = max(static_cast<int>(__float_as_uint(want) >> 23) - 127 - 3, -17);
+  const float step = __uint_as_float(static_cast<uint32_t>(e + 127) << 23), per = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+  const float s = fminf(ceilf(__fmul_rn(want, per)) * step, SCALE_MAX);
+  if (!(most <= HELD_MAX)) {  // a NaN, an infinity, too large
+    inverse = 0.f;
+    return SCALE_NAN;
+  }
+  inverse = s > 0.f ? __fmul_rn(__frcp_rn(s), 1.f + 0x1p-20f) : 0.f;
+  return static_cast<uint32_t>(__half_as_ushort(__float2half_rn(s))) >> 7;
+}
+// c + 8 in the low four bits: the fused product with 2^23 + 2^22 + 8 is rounded to a whole number.
+__device__ __forceinline__ uint32_t code_of(float x, float inverse) {
+  return __float_as_uint(__fmaf_rn(x, inverse, 12582912.f + 8.f)) & 15u;
+}
+
+}  // namespace pages4
+}  // namespace dopr

@@ -89,6 +89,12 @@ def load():
         "dopr_rope_destroy": ([P], i32),
         "dopr_rope_apply": ([P, i32, i32, i32, P, P, P, P, P, i32, P, P], i32),
         "dopr_cache_append": ([P, P, i32] + [P] * 10, i32),
+        "dopr_head_norm_rope": ([P, i32, i32, i32, P, ctypes.c_float, i32] + [P] * 8, i32),
+        "dopr_head_norm_rope_backward": ([P, i32, i32, i32, P, ctypes.c_float, i32] + [P] * 13, i32),
+        "dopr_head_norm_rope_workspace": ([i32], i64),
+        "dopr_cache_4bit_pool_bytes": ([P], i64),
+        "dopr_cache_append_4bit": ([P, P, i32, P, P, ctypes.c_float, i32] + [P] * 10, i32),
+        "dopr_cache_read_4bit": ([P, i32] + [P] * 7, i32),
         "dopr_shared_attention_plan": ([P, i32, i32] + [P] * 6, i32),
         "dopr_shared_attention_plan_bytes": ([P, i32, i32], i64),
         "dopr_shared_attention": ([P, P, i32, P, P, P, P, ctypes.c_float] + [P] * 5, i32),
@@ -646,6 +652,143 @@ def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables,
         if guard is not None:
             guard.__exit__(None, None, None)
     return out
+
+
+# ------------------------------------------------------------------ norms of heads
+def _gains(q_gain, k_gain, head_dim, device):
+    """The two gains' pointers and type; each may be None."""
+    one = q_gain if q_gain is not None else k_gain
+    if one is None:
+        return None, None, 0
+    if one.dtype not in _DTYPES:
+        raise ValueError(f"gains are float16, bfloat16 or float32, got {one.dtype}")
+    for name, g in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if g is not None:
+            _no_grad(name, g)
+    return (_buf("q_gain", q_gain, one.dtype, head_dim, device), _buf("k_gain", k_gain, one.dtype, head_dim, device),
+            _DTYPES[one.dtype])
+
+
+def head_norm_rope(q, k=None, q_gain=None, k_gain=None, eps: float = 1e-6, rope: Rope | None = None, positions=None, q_out=None,
+                   k_out=None, status=None, stream=None):
+    """RMSNorm over each head of q and, with it, k ([tokens, heads, head_dim] views of float16, bfloat16 or float32), times a
+    gain [head_dim] each, then rotary positions.  Returns (q_out, k_out); pass q_out=q, k_out=k to work in place.  Its gradients:
+    head_norm_rope_backward, for a backward pass of the caller's own."""
+    (T, _, D), dt, dev = q.shape, q.dtype, q.device
+    if dt not in _DTYPES:
+        raise ValueError(f"head_norm_rope: float16, bfloat16 or float32, got {dt}")
+    handle = rope.handle() if rope is not None else None
+    st, guard, on = _on(dev, stream)
+    try:
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=dt, device=dev)
+        qg, kg, gain_dtype = _gains(q_gain, k_gain, D, on)
+        _check(load().dopr_head_norm_rope(
+            handle, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, on), eps, gain_dtype,
+            _heads("q", q, T, D, dt, on), qg, _heads("q_out", q_out, T, D, dt, on), _heads("k", k, T, D, dt, on), kg,
+            _heads("k_out", k_out if k is not None else None, T, D, dt, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
+    return q_out, k_out
+
+
+def head_norm_rope_workspace(head_dim: int, device="cuda") -> torch.Tensor:
+    n = load().dopr_head_norm_rope_workspace(head_dim)
+    if n < 0:
+        raise DoprError(ERR_UNSUPPORTED, load().dopr_last_error().decode())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def head_norm_rope_backward(dq_out, q, dk_out=None, k=None, q_gain=None, k_gain=None, eps: float = 1e-6, rope: Rope | None = None,
+                            positions=None, dq=None, dk=None, dq_gain=None, dk_gain=None, workspace=None, status=None, stream=None):
+    """Gradients of head_norm_rope, from those of its outputs and its inputs: (dq, dk, dq_gain, dk_gain).  dq and dk may be dq_out
+    and dk_out themselves.  Gains' gradients are float32 [head_dim], of the gains that are given.  workspace:
+    head_norm_rope_workspace(head_dim); without it each call allocates one."""
+    (T, _, D), dt, dev = q.shape, q.dtype, q.device
+    if dt not in _DTYPES:
+        raise ValueError(f"head_norm_rope_backward: float16, bfloat16 or float32, got {dt}")
+    handle = rope.handle() if rope is not None else None
+    st, guard, on = _on(dev, stream)
+    try:
+        if dq is None:
+            dq = torch.empty(q.shape, dtype=dt, device=dev)
+        if k is not None and dk is None:
+            dk = torch.empty(k.shape, dtype=dt, device=dev)
+        if q_gain is not None and dq_gain is None:
+            dq_gain = torch.empty(D, dtype=torch.float32, device=dev)
+        if k_gain is not None and dk_gain is None:
+            dk_gain = torch.empty(D, dtype=torch.float32, device=dev)
+        need = max(0, load().dopr_head_norm_rope_workspace(D))
+        if workspace is None and (dq_gain is not None or dk_gain is not None):
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        qg, kg, gain_dtype = _gains(q_gain, k_gain, D, on)
+        _check(load().dopr_head_norm_rope_backward(
+            handle, _DTYPES[dt], D, T, _buf("positions", positions, torch.int32, T, on), eps, gain_dtype,
+            _heads("dq_out", dq_out, T, D, dt, on), _heads("q", q, T, D, dt, on), qg, _heads("dq", dq, T, D, dt, on),
+            _buf("dq_gain", dq_gain, torch.float32, D, on), _heads("dk_out", dk_out, T, D, dt, on), _heads("k", k, T, D, dt, on),
+            kg, _heads("dk", dk if k is not None else None, T, D, dt, on), _buf("dk_gain", dk_gain, torch.float32, D, on),
+            _buf("workspace", workspace, torch.uint8, need, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
+    return dq, dk, dq_gain, dk_gain
+
+
+# ------------------------------------------------------------------ the paged cache in 4 bits
+# Layouts, tables, slots and plans are those of the cache above; the layout's dtype is that of the rows.
+
+def cache_pools_4bit(layout: CacheLayout, device="cuda"):
+    """One layer's pools of keys and values in 4 bits, cleared: uint8 [n_blocks, n_kv_heads, bytes of a page]."""
+    n = _sized(load().dopr_cache_4bit_pool_bytes, layout)
+    shape = (layout.n_blocks, layout.n_kv_heads, n // (layout.n_blocks * layout.n_kv_heads))
+    return torch.zeros(shape, dtype=torch.uint8, device=device), torch.zeros(shape, dtype=torch.uint8, device=device)
+
+
+def cache_append_4bit(layout: CacheLayout, slots, k, v, k_pool, v_pool, k_gain=None, eps: float = 0.0, rope: Rope | None = None,
+                      positions=None, q=None, q_gain=None, q_out=None, status=None, stream=None):
+    """One layer's new rows k and v [tokens, kv heads, head_dim] into the 4-bit pages at slots; k, and q where it is given,
+    are normed first where eps > 0 and turned where there is a rope.  Returns q_out.  Not recorded for autograd."""
+    T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
+    handle = rope.handle() if rope is not None else None
+    pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
+    st, guard, on = _on(dev, stream)
+    try:
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dt, device=dev)
+        qg, kg, gain_dtype = _gains(q_gain, k_gain, D, on)
+        _check(load().dopr_cache_append_4bit(
+            ctypes.byref(layout), handle, T, _buf("positions", positions, torch.int32, T, on),
+            _buf("slots", slots, torch.int64, T, on), eps, gain_dtype, _heads("q", q, T, D, dt, on), qg,
+            _heads("q_out", q_out if q is not None else None, T, D, dt, on), _heads("k", k, T, D, dt, on), kg,
+            _heads("v", v, T, D, dt, on), _buf("k_pool", k_pool, torch.uint8, pool, on),
+            _buf("v_pool", v_pool, torch.uint8, pool, on), _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
+    return q_out
+
+
+def cache_read_4bit(layout: CacheLayout, slots, k_pool, v_pool, k_out=None, v_out=None, status=None, stream=None):
+    """What the 4-bit pages hold at slots: (k_out, v_out) [rows, kv heads, head_dim] of the layout's type."""
+    T, D, dt, dev = slots.numel(), layout.head_dim, _TORCH_TYPES[layout.dtype], slots.device
+    pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
+    st, guard, on = _on(dev, stream)
+    try:
+        if k_out is None:
+            k_out = torch.empty((T, layout.n_kv_heads, D), dtype=dt, device=dev)
+        if v_out is None:
+            v_out = torch.empty((T, layout.n_kv_heads, D), dtype=dt, device=dev)
+        _check(load().dopr_cache_read_4bit(
+            ctypes.byref(layout), T, _buf("slots", slots, torch.int64, T, on), _buf("k_pool", k_pool, torch.uint8, pool, on),
+            _buf("v_pool", v_pool, torch.uint8, pool, on), _heads("k_out", k_out, T, D, dt, on), _heads("v_out", v_out, T, D, dt, on),
+            _buf("status", status, torch.int32, 1, on), st))
+    finally:
+        if guard is not None:
+            guard.__exit__(None, None, None)
+    return k_out, v_out
 
 
 def profile_enable(model: Model, on: bool = True):

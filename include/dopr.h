@@ -651,6 +651,15 @@ DOPR_API dopr_status dopr_cache_read_4bit(const dopr_cache_layout *layout, int32
                                           const dopr_heads *v_out, int32_t *status, void *cuda_stream);
 
 /*
+ * dopr_shared_attention over such pools: the same plan, arguments and arithmetic on the values that the pages hold.  A scale byte
+ * above 0xe1 among a row's keys counts as zero: device error RANGE.  Other errors as there.
+ */
+DOPR_API dopr_status dopr_shared_attention_4bit(const dopr_cache_layout *layout, const void *plan, int32_t max_tokens,
+                                                const dopr_heads *q, const void *k_pool, const void *v_pool,
+                                                const int32_t *block_tables, float scale, const dopr_heads *out, float *lse,
+                                                void *workspace, int32_t *status, void *cuda_stream);
+
+/*
  * Per-kernel accounting, for measurement.  Every dopr_score call counts its
  * kernel launches per kernel family (pack, embed, gemm_qkv, qknorm_rope,
  * attention, gemm_o, rmsnorm, gemm_gate_up, gemm_down, score, prefix_store;

@@ -231,6 +231,47 @@ dopr_status sm_count(int* n) {
   return cuda_status(cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev), "cudaDeviceGetAttribute");
 }
 
+// dopr_shared_attention over 16-bit pools and over those of the 4-bit cache.
+dopr_status attention(bool four, const dopr_cache_layout* layout, const void* plan, int32_t max_tokens, const dopr_heads* q, const void* k_pool,
+                      const void* v_pool, const int32_t* block_tables, float scale, const dopr_heads* out, float* lse, void* workspace,
+                      int32_t* status, void* cuda_stream) {
+  if (!q) return fail(DOPR_ERR_INVALID_ARG, "q is NULL");
+  STATUS_TRY(check_attention(layout, q->n_heads, max_tokens));
+  if (max_tokens == 0) return DOPR_OK;  // views of no rows have no data
+  if (!plan || !k_pool || !v_pool || !block_tables || !workspace)
+    return fail(DOPR_ERR_INVALID_ARG, "plan, k_pool, v_pool, block_tables or workspace is NULL");
+  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16))
+    return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned");
+  STATUS_TRY(check_words({block_tables, lse, status}));
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(DOPR_ERR_INVALID_ARG, "scale must be positive");
+  STATUS_TRY(check_view(q, "q", layout->head_dim, 2, true, 0));
+  STATUS_TRY(check_output(out, "out", layout->head_dim, 2, true, q->n_heads, max_tokens));
+  if (!aligned(workspace, 32)) return fail(DOPR_ERR_INVALID_ARG, "the workspace must be 32-byte aligned");
+  SharedAttnArgs a{};
+  a.lay = *layout;
+  a.Hq = q->n_heads;
+  a.max_tokens = max_tokens;
+  a.plan = plan;
+  a.q = q->data;
+  a.q_tok = q->token_stride;
+  a.q_head = q->head_stride;
+  a.k_pool = k_pool;
+  a.v_pool = v_pool;
+  a.tables = block_tables;
+  a.scale = scale;
+  a.out = out->data;
+  a.o_tok = out->token_stride;
+  a.o_head = out->head_stride;
+  a.lse = lse;
+  a.ws = static_cast<uint8_t*>(workspace);
+  a.status = status;
+  int sms = 0;
+  STATUS_TRY(sm_count(&sms));
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return four ? cuda_status(launch_shared_attention_4bit(a, sms, st), "dopr_shared_attention_4bit")
+              : cuda_status(launch_shared_attention(a, sms, st), "dopr_shared_attention");
+}
+
 }  // namespace
 }  // namespace dopr
 
@@ -549,39 +590,13 @@ int64_t dopr_shared_attention_plan_bytes(const dopr_cache_layout* layout, int32_
 dopr_status dopr_shared_attention(const dopr_cache_layout* layout, const void* plan, int32_t max_tokens, const dopr_heads* q,
                                   const void* k_pool, const void* v_pool, const int32_t* block_tables, float scale,
                                   const dopr_heads* out, float* lse, void* workspace, int32_t* status, void* cuda_stream) {
-  if (!q) return fail(DOPR_ERR_INVALID_ARG, "q is NULL");
-  STATUS_TRY(check_attention(layout, q->n_heads, max_tokens));
-  if (max_tokens == 0) return DOPR_OK;  // views of no rows have no data
-  if (!plan || !k_pool || !v_pool || !block_tables || !workspace)
-    return fail(DOPR_ERR_INVALID_ARG, "plan, k_pool, v_pool, block_tables or workspace is NULL");
-  if (!aligned(plan, 16) || !aligned(k_pool, 16) || !aligned(v_pool, 16))
-    return fail(DOPR_ERR_INVALID_ARG, "plan and pools must be 16-byte aligned");
-  STATUS_TRY(check_words({block_tables, lse, status}));
-  if (!(scale > 0.f) || !isfinite(scale)) return fail(DOPR_ERR_INVALID_ARG, "scale must be positive");
-  STATUS_TRY(check_view(q, "q", layout->head_dim, 2, true, 0));
-  STATUS_TRY(check_output(out, "out", layout->head_dim, 2, true, q->n_heads, max_tokens));
-  if (!aligned(workspace, 32)) return fail(DOPR_ERR_INVALID_ARG, "the workspace must be 32-byte aligned");
-  SharedAttnArgs a{};
-  a.lay = *layout;
-  a.Hq = q->n_heads;
-  a.max_tokens = max_tokens;
-  a.plan = plan;
-  a.q = q->data;
-  a.q_tok = q->token_stride;
-  a.q_head = q->head_stride;
-  a.k_pool = k_pool;
-  a.v_pool = v_pool;
-  a.tables = block_tables;
-  a.scale = scale;
-  a.out = out->data;
-  a.o_tok = out->token_stride;
-  a.o_head = out->head_stride;
-  a.lse = lse;
-  a.ws = static_cast<uint8_t*>(workspace);
-  a.status = status;
-  int sms = 0;
-  STATUS_TRY(sm_count(&sms));
-  return cuda_status(launch_shared_attention(a, sms, static_cast<cudaStream_t>(cuda_stream)), "dopr_shared_attention");
+  return attention(false, layout, plan, max_tokens, q, k_pool, v_pool, block_tables, scale, out, lse, workspace, status, cuda_stream);
+}
+
+dopr_status dopr_shared_attention_4bit(const dopr_cache_layout* layout, const void* plan, int32_t max_tokens, const dopr_heads* q,
+                                       const void* k_pool, const void* v_pool, const int32_t* block_tables, float scale,
+                                       const dopr_heads* out, float* lse, void* workspace, int32_t* status, void* cuda_stream) {
+  return attention(true, layout, plan, max_tokens, q, k_pool, v_pool, block_tables, scale, out, lse, workspace, status, cuda_stream);
 }
 
 int64_t dopr_shared_attention_workspace(const dopr_cache_layout* layout, int32_t n_q_heads, int32_t max_tokens) {

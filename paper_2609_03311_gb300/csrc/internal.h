@@ -556,6 +556,9 @@ int64_t shared_plan_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens);
 int64_t shared_workspace_bytes(const dopr_cache_layout& lay, int Hq, int max_tokens, int num_sms);
 cudaError_t launch_shared_plan(const SharedPlanArgs& a, int num_sms, cudaStream_t st);
 cudaError_t launch_shared_attention(const SharedAttnArgs& a, int num_sms, cudaStream_t st);
+// The same over 4-bit pools; and the second half of both, which joins partial results.
+cudaError_t launch_shared_attention_4bit(const SharedAttnArgs& a, int num_sms, cudaStream_t st);
+cudaError_t launch_shared_join(const SharedAttnArgs& a, int num_sms, cudaStream_t st);
 
 // Sets the message dopr_last_error() returns on this thread.
 void set_last_error_message(const std::string& msg);

@@ -53,5 +53,54 @@ __device__ __forceinline__ uint32_t code_of(float x, float inverse) {
   return __float_as_uint(__fmaf_rn(x, inverse, 12582912.f + 8.f)) & 15u;
 }
 
+// Codes to the products' type T.  A nibble n put into the mantissa of a power of two is the number 2^p + n; less 2^p + 8 and times s it
+// is c s, which a fused step gives exactly: 2^p + 8 times s fits the type where p is chosen so.  In f16 such a product with a large
+// scale leaves the range, so values come as 1 / 64 of what they are: s / 64 and all of its products are multiples of 2^-23.
+template <typename T>
+struct Widen;
+template <>
+struct Widen<__half> {
+  static constexpr float UNIT = 64.f;
+  __half2 s, from256, from16;
+  // bytes: the scale of the words' lower halves in bits 0 .. 7, of the upper in 16 .. 23
+  __device__ __forceinline__ explicit Widen(uint32_t bytes) {
+    const uint32_t h = bytes << 7;
+    s = __hmul2(reinterpret_cast<const __half2&>(h), __float2half2_rn(1.f / UNIT));
+    from256 = __hmul2(s, __float2half2_rn(-264.f));
+    from16 = __hmul2(s, __float2half2_rn(-24.f));
+  }
+  static __device__ __forceinline__ __half2 put(uint32_t w, uint32_t mask, uint32_t power) {
+    const uint32_t x = (w & mask) | power;
+    return reinterpret_cast<const __half2&>(x);
+  }
+  // v[k]: the pair of nibbles at 4 k and 16 + 4 k
+  __device__ __forceinline__ void operator()(uint32_t w, uint32_t (&v)[4]) const {
+    const uint32_t a = w << 2, b = w >> 6;  // nibbles at bits 2 and 6: beside powers 256 and 16
+    const __half2 r[4] = {__hfma2(put(a, 0x003c003cu, 0x5c005c00u), s, from256), __hfma2(put(a, 0x03c003c0u, 0x4c004c00u), s, from16),
+                          __hfma2(put(b, 0x003c003cu, 0x5c005c00u), s, from256), __hfma2(put(b, 0x03c003c0u, 0x4c004c00u), s, from16)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = reinterpret_cast<const uint32_t&>(r[k]);
+  }
+};
+template <>
+struct Widen<__nv_bfloat16> {
+  static constexpr float UNIT = 1.f;
+  __nv_bfloat162 s, from16;
+  __device__ __forceinline__ explicit Widen(uint32_t bytes) {
+    const uint32_t h = bytes << 4, up = 0x77807780u;  // the byte's exponent is 112 below; up: 2^112
+    s = __hmul2(reinterpret_cast<const __nv_bfloat162&>(h), reinterpret_cast<const __nv_bfloat162&>(up));
+    from16 = __hmul2(s, __float2bfloat162_rn(-24.f));
+  }
+  __device__ __forceinline__ void operator()(uint32_t w, uint32_t (&v)[4]) const {
+    const uint32_t at[4] = {w << 3, w >> 1, w >> 5, w >> 9};  // nibbles at bit 3: beside the power 16
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t x = (at[k] & 0x00780078u) | 0x41804180u;
+      const __nv_bfloat162 r = __hfma2(reinterpret_cast<const __nv_bfloat162&>(x), s, from16);
+      v[k] = reinterpret_cast<const uint32_t&>(r);
+    }
+  }
+};
+
 }  // namespace pages4
 }  // namespace dopr

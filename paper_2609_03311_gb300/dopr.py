@@ -98,6 +98,7 @@ def load():
         "dopr_shared_attention_plan": ([P, i32, i32] + [P] * 6, i32),
         "dopr_shared_attention_plan_bytes": ([P, i32, i32], i64),
         "dopr_shared_attention": ([P, P, i32, P, P, P, P, ctypes.c_float] + [P] * 5, i32),
+        "dopr_shared_attention_4bit": ([P, P, i32, P, P, P, P, ctypes.c_float] + [P] * 5, i32),
         "dopr_shared_attention_workspace": ([P, i32, i32], i64),
         "dopr_last_error": ([], ctypes.c_char_p),
         "dopr_version": ([], ctypes.c_char_p),
@@ -619,19 +620,13 @@ def shared_attention_workspace(layout: CacheLayout, n_q_heads: int, max_tokens: 
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None,
-                     lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
-    """Attention of q [max_tokens, q heads, head_dim], the plan's tokens, over their rows' prefixes and own keys.  lse:
-    float32 [max_tokens, q heads] to fill, or None.  workspace: shared_attention_workspace(...), for all layers; without
-    it each call allocates one, hundreds of megabytes for thousands of tokens.  Not recorded for autograd: it has no
-    backward pass."""
+def _attention(fn, layout, plan, q, k_pool, v_pool, pool, pool_type, block_tables, scale, out, lse, workspace, status, stream):
     _no_grad("k_pool", k_pool)
     _no_grad("v_pool", v_pool)
     T, hq, D = q.shape
     dt, dev = _TORCH_TYPES[layout.dtype], q.device
     if scale is None:
         scale = D ** -0.5
-    pool = layout.n_blocks * layout.n_kv_heads * layout.page * D
     lib = load()
     st, guard, on = _on(dev, stream)
     try:
@@ -640,11 +635,11 @@ def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables,
         need = _sized(lib.dopr_shared_attention_workspace, layout, hq, T)
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check(lib.dopr_shared_attention(
+        _check(fn(
             ctypes.byref(layout),
             _buf("plan", plan, torch.uint8, _sized(lib.dopr_shared_attention_plan_bytes, layout, hq, T), on), T,
-            _heads("q", q, T, layout.head_dim, dt, on), _buf("k_pool", k_pool, dt, pool, on),
-            _buf("v_pool", v_pool, dt, pool, on),
+            _heads("q", q, T, layout.head_dim, dt, on), _buf("k_pool", k_pool, pool_type, pool, on),
+            _buf("v_pool", v_pool, pool_type, pool, on),
             _buf("block_tables", block_tables, torch.int32, layout.n_seqs * layout.max_blocks, on), scale,
             _heads("out", out, T, layout.head_dim, dt, on), _buf("lse", lse, torch.float32, T * hq, on),
             _buf("workspace", workspace, torch.uint8, need, on), _buf("status", status, torch.int32, 1, on), st))
@@ -652,6 +647,17 @@ def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables,
         if guard is not None:
             guard.__exit__(None, None, None)
     return out
+
+
+def shared_attention(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None,
+                     lse=None, workspace=None, status=None, stream=None) -> torch.Tensor:
+    """Attention of q [max_tokens, q heads, head_dim], the plan's tokens, over their rows' prefixes and own keys.  lse:
+    float32 [max_tokens, q heads] to fill, or None.  workspace: shared_attention_workspace(...), for all layers; without
+    it each call allocates one, hundreds of megabytes for thousands of tokens.  Not recorded for autograd: it has no
+    backward pass."""
+    pool = layout.n_blocks * layout.n_kv_heads * layout.page * layout.head_dim
+    return _attention(load().dopr_shared_attention, layout, plan, q, k_pool, v_pool, pool, _TORCH_TYPES[layout.dtype], block_tables,
+                      scale, out, lse, workspace, status, stream)
 
 
 # ------------------------------------------------------------------ norms of heads
@@ -789,6 +795,14 @@ def cache_read_4bit(layout: CacheLayout, slots, k_pool, v_pool, k_out=None, v_ou
         if guard is not None:
             guard.__exit__(None, None, None)
     return k_out, v_out
+
+
+def shared_attention_4bit(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None, lse=None,
+                          workspace=None, status=None, stream=None) -> torch.Tensor:
+    """shared_attention over 4-bit pools: the same plan and workspace, q and out of the layout's type.  Not recorded for autograd."""
+    pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
+    return _attention(load().dopr_shared_attention_4bit, layout, plan, q, k_pool, v_pool, pool, torch.uint8, block_tables, scale, out,
+                      lse, workspace, status, stream)
 
 
 def profile_enable(model: Model, on: bool = True):

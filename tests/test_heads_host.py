@@ -150,3 +150,20 @@ def test_the_binding_takes_device_tensors_and_open_tables_only(lib):
             call()
     with pytest.raises(ValueError):
         dopr.head_norm_rope(x.long())
+
+
+def attention(**kw):
+    a = dict(l=ctypes.byref(layout()), plan=P, T=4, q=heads(), kp=P, vp=P, tables=P, scale=0.1, out=heads(), lse=None, ws=P, st=None)
+    a.update(kw)
+    return [a[x] for x in ("l", "plan", "T", "q", "kp", "vp", "tables", "scale", "out", "lse", "ws", "st")] + [None]
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(plan=None), 1), (dict(q=None), 1), (dict(kp=None), 1), (dict(vp=None), 1), (dict(tables=None), 1), (dict(out=None), 1),
+    (dict(ws=None), 1), (dict(T=-1), 1), (dict(T=2 ** 30), dopr.ERR_UNSUPPORTED), (dict(q=heads(n=3)), dopr.ERR_UNSUPPORTED),
+    (dict(out=heads(n=2)), 1), (dict(q=heads(data=4104)), 1), (dict(out=heads(tok=128)), 1), (dict(scale=0.0), 1),
+    (dict(scale=float("inf")), 1), (dict(kp=EIGHT), 1), (dict(ws=ctypes.c_void_p(4112)), 1), (dict(plan=EIGHT), 1), (dict(lse=ODD), 1),
+    (dict(l=ctypes.byref(layout(head_dim=96))), dopr.ERR_UNSUPPORTED)])
+def test_bad_attention_over_4_bits_is_refused(lib, kw, status):
+    assert lib.dopr_shared_attention_4bit(*attention(**kw)) == status
+    assert lib.dopr_last_error()

@@ -789,8 +789,7 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
       const int r = quad + 8 * i;
       float sum = l[i] + __shfl_xor_sync(0xffffffffu, l[i], 1);
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-      if (r >= rows) continue;
-      if (s.flags & SEG_WHOLE) {
+      if (r < rows && (s.flags & SEG_WHOLE)) {
         const int t = plan.order[s.tok + r / G], h = s.h * G + r % G;
         const float inv = sum == 0.f ? 0.f : inverse(sum) * HELD_UNIT<T, true>;
         uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head + 2 * NT * in_quad);
@@ -804,7 +803,7 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
             dst[(e * NT + d) / 8] = uint4{x[0], x[1], x[2], x[3]};
           }
         if (a.lse && in_quad == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m[i], sum);
-      } else {
+      } else if (r < rows) {
         float2* ml = reinterpret_cast<float2*>(a.ws);
         float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
         const int64_t row = static_cast<int64_t>(s.part_row) + r;
@@ -891,10 +890,12 @@ __device__ __forceinline__ void copy_4bit(const SharedAttnArgs& a, const Plan& p
       if (armed >> i & 1u) mbar_wait_warp(bar(L::RAW_FULL + stage0 + i), parity >> i & 1u, err, 100000000ull);
 }
 
-// Tiles: rows 64 `half` .. of each block of K or V from the raw ring into the products' ring, in the layout that copies of 16-bit rows
-// have there.  A lane a group: 16 bytes of codes to 64 of values.  Rows past a run's keys are zeros.
+// Tiles: each block of K or V, by two warps, from the raw ring into the products' ring, in the layout that copies of 16-bit rows have
+// there.  Warp `part` takes 32 rows of each half, so that both pass every stage of the ring: a warp that skipped some could take the
+// parity of a stage's phase before last for the one it waits for.  A lane a group: 16 bytes of codes to 64 of values.  Rows past a
+// run's keys are zeros.
 template <typename T, int D>
-__device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan& plan, uint8_t* smem, uint32_t s0, int2 work, bool is_v, int half,
+__device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan& plan, uint8_t* smem, uint32_t s0, int2 work, bool is_v, int part,
                                             int* err, int lane) {
   using L = Smem<D, true>;
   constexpr int ROW = D / 2, SROW = D / 32, AT_ONCE = 32 / SROW;
@@ -909,15 +910,14 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
   Ring r, raw;
   bool ok = true, bad = false;
   while (ok && walk.next(s)) {
-    for (uint32_t b = s.b0; b < s.b1; ++b) {
+    for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
       const int cols = min(page_blk, s.pages - static_cast<int>(b) * page_blk) * page;
-      if (half && cols > 64) raw.next(raw_stages);
       if (!mbar_wait_warp(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
         ok = false;
         break;
       }
-      if (64 * half < cols) {
-        const int rs = stage0 + raw.stage, n = min(64, cols - 64 * half);
+      for (int half = 0; 64 * half < cols; ++half) {
+        const int rs = stage0 + raw.stage, end = min(32 * part + 32, cols - 64 * half);
         if (!mbar_wait_warp(bar(L::RAW_FULL + rs), raw.phase, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
@@ -928,7 +928,7 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
         uint8_t* to = tiles + r.stage * L::TILE_BYTES + (D == 128 ? group >> 1 : 0) * HALF_BYTES + 64 * half * 128;
         const int place = (D == 128 ? group & 1 : group) * 4;
 #pragma unroll 2
-        for (int r0 = 0; r0 < n; r0 += AT_ONCE) {
+        for (int r0 = 32 * part; r0 < end; r0 += AT_ONCE) {
           const int row = r0 + lane / SROW, at = row >> bits, in = row & (piece - 1);
           const uint8_t* p = from + at * piece * (ROW + SROW);
           uint4 w = *reinterpret_cast<const uint4*>(p + in * ROW + 16 * group);
@@ -944,20 +944,19 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
             *reinterpret_cast<uint4*>(to + row * 128 + (((place + (j ^ swap)) ^ (row & 7)) << 4)) = uint4{x[0], x[1], x[2], x[3]};
           }
         }
-        fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(L::RAW_EMPTY + rs));
+        raw.next(raw_stages);
       }
+      if (!ok) break;
+      fence_proxy_async_shared();
+      __syncwarp();
       if (lane == 0) mbar_arrive(bar(full + r.stage));
       r.next(stages);
-      if (64 * half < cols) raw.next(raw_stages);
-      if (!half && cols > 64) raw.next(raw_stages);
-      if (half && cols <= 64) raw.next(raw_stages);
     }
   }
   if (bad && a.status) atomicCAS(a.status, 0, DOPR_ERR_RANGE);
 }
-
 
 // The CTA: its threads take their roles here.  FOUR: the pools are those of the 4-bit cache (tm_k and tm_v are not used).
 template <typename T, int D, bool FOUR>
@@ -984,8 +983,8 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     gave_up = 0;
     for (int i = 0; i < L::N_BARS; ++i)
       mbar_init(bar(i), (i >= L::P_FULL && i < L::P_FULL + 4) || i == L::ML_FULL || i == L::ML_EMPTY ? 4
-                        : FOUR && (i < L::K_EMPTY || (i >= L::V_FULL && i < L::V_EMPTY))             ? 2  // half a block each
-                                                                                                     : 1);
+                        : FOUR && (i < L::K_EMPTY || (i >= L::V_FULL && i < L::V_EMPTY) || i >= L::RAW_EMPTY) ? 2  // two warps expand
+                                                                                                              : 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q8);
     tma_prefetch_desc(&tm_q1);
@@ -1002,7 +1001,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  Segment s;
+  Segment s{};
   const bool good = made_for(head, a.lay, a.Hq, a.max_tokens, gridDim.x);
   const bool few = static_cast<int>(blockIdx.x) >= head.tile_ctas;
   if (!good && threadIdx.x == 0 && a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
@@ -1070,7 +1069,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
           if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
     }
   } else if (FOUR && warp >= 12) {
-    // ======================= 4 bits: K (warps 12, 13) and V (14, 15) to the products' type, half of each block each
+    // ======================= 4 bits: K (warps 12, 13) and V (14, 15) to the products' type
     regs_few<FOUR>();
     if constexpr (FOUR) expand_4bit<T, D>(a, plan, smem, s0, work, warp >= 14, warp & 1, err, lane);
   } else if (warp == 1) {

@@ -402,6 +402,26 @@ def test_two_streams_at_the_same_time():
         assert st.item() == 0 and all(torch.equal(x, out) for x in outs)
 
 
+@pytest.mark.parametrize("d,dt,page", [(128, HF, 16), (128, BF, 32), (64, BF, 16), (128, BF, 128)])
+def test_calls_one_after_another_give_the_same_bits(d, dt, page):
+    # tiles whose blocks end in their first half or in their second, so that the raw rings' stages change hands, beside few items
+    r = np.random.default_rng(page + d)
+    docs = [79, 724, 40, 200, 129, 16, 1000, 50]
+    reqs = [(i % 8, int(r.integers(1, 90)), 1) for i in range(100)] + [(2, 90, 30), (-1, 70, 70), (3, 20, 20)]
+    bs = [Batch4(16, 8, d, dt, page, docs, reqs, seed=s) for s in (1, 2)]
+    want = [b.run() for b in bs]
+    for b, w in zip(bs, want):
+        b.check(w)
+    jobs = [(b, dopr.shared_attention_plan(b.layout, b.hq, *b.args()), i32(b.tables), torch.empty_like(b.q),
+             dopr.shared_attention_workspace(b.layout, b.hq, b.T)) for b in bs]
+    same, st = torch.ones((), dtype=torch.bool, device=DEV), word()
+    for _ in range(1500):
+        for (b, plan, tables, out, ws), w in zip(jobs, want):
+            dopr.shared_attention_4bit(b.layout, plan, b.q, b.k4, b.v4, tables, out=out, workspace=ws, status=st)
+            same &= (out == w[0]).all()
+    assert bool(same) and st.item() == 0
+
+
 def test_thousands_of_rows_and_steps_of_no_tokens():
     r = np.random.default_rng(5)
     reqs = [(int(x), int(r.integers(0, 4)), int(r.choice([0, 1, 1, 2]))) for x in r.integers(-1, 40, 1500)]

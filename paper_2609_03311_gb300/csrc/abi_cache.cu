@@ -482,7 +482,7 @@ dopr_status dopr_head_norm_rope_backward(const dopr_rope* rope, int32_t dtype, i
 
 int64_t dopr_head_norm_rope_workspace(int32_t head_dim) {
   if (check_head_dim(head_dim) != DOPR_OK) return -1;
-  return static_cast<int64_t>(HEAD_NORM_MAX_BLOCKS) * 2 * head_dim * static_cast<int64_t>(sizeof(float));
+  return static_cast<int64_t>(HEAD_NORM_MAX_BLOCKS) * head_dim * static_cast<int64_t>(sizeof(float));
 }
 
 int64_t dopr_cache_4bit_pool_bytes(const dopr_cache_layout* layout) {

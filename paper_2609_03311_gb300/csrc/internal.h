@@ -494,7 +494,7 @@ struct RopeArgs {
 cudaError_t launch_rope(int dtype, const RopeArgs& a, cudaStream_t st);
 
 // Norms of heads with rotary positions, their gradients, and the same on the way into 4-bit pages.
-constexpr int HEAD_NORM_MAX_BLOCKS = 1024;  // of the backward kernel: partial sums of the gains' gradients, 2 x head_dim each
+constexpr int HEAD_NORM_MAX_BLOCKS = 1024;  // of the backward kernel: partial sums of a gain's gradient, head_dim each
 struct HeadNormArgs {
   int n_tokens, head_dim, rotary;  // rotary 0: nothing turns, positions is not read
   bool interleaved;
@@ -507,7 +507,7 @@ struct HeadNormArgs {
   RopeView q, k;                   // backward: the outputs' gradients, and where the inputs' go
   RopeView qx, kx;                 // backward: the inputs (in only)
   float *dq_gain, *dk_gain;        // backward, null: not wanted
-  float* ws;                       // backward: [HEAD_NORM_MAX_BLOCKS][2][head_dim]
+  float* ws;                       // backward: [HEAD_NORM_MAX_BLOCKS][head_dim]
   // 4-bit pages: keys and values go there (slots null: no pages, k like q)
   RopeView v;                      // in only
   const int64_t* slots;

@@ -135,14 +135,6 @@ struct Units {
       *reinterpret_cast<Pack<T, VEC>*>(row + ib[i]) = b;
     }
   }
-  __device__ __forceinline__ void gains(const float* from, float (&g)[NU][2 * VEC]) const {
-#pragma unroll
-    for (int i = 0; i < NU; ++i) {
-      if (!there[i]) continue;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) g[i][j] = from[ia[i] + j], g[i][VEC + j] = from[ib[i] + j];
-    }
-  }
 };
 
 // Adds up over the `lanes` (a power of two) lanes that hold a head.
@@ -151,112 +143,162 @@ __device__ __forceinline__ float head_sum(float v, int lanes) {
   return v;
 }
 
+// How the work is cut: a block takes one of the views (a role: q, k or, on the way into pages, v), so that a thread's gain stays with
+// it and sums of gradients have one place; a warp takes units, a slice of one token's heads each, and walks over the slice with
+// the token's cos and sin.
+struct Roles {
+  int end[3];     // blocks before the end of each
+  int slices[3];  // of a token's heads
+};
+struct Role {
+  int what, block, blocks, slices, per_slice;
+  __device__ __forceinline__ Role(const Roles& r, const HeadNormArgs& a, int per_warp) {
+    const int b = blockIdx.x;
+    what = b < r.end[0] ? 0 : b < r.end[1] ? 1 : 2;
+    const int from = what > 0 ? r.end[what - 1] : 0;
+    block = b - from;
+    blocks = r.end[what] - from;
+    slices = r.slices[what];
+    const int heads = view(a).n_heads, turns = (heads + per_warp - 1) / per_warp;
+    per_slice = (turns + slices - 1) / slices * per_warp;
+  }
+  __device__ __forceinline__ const RopeView& view(const HeadNormArgs& a) const { return what == 0 ? a.q : what == 1 ? a.k : a.v; }
+};
+
 // PAGES: keys and values go to 4-bit pages.
 template <typename T, int VEC, int NU, bool INTER, bool PAGES>
-__global__ void __launch_bounds__(THREADS) k_head_norm(const __grid_constant__ HeadNormArgs a, int lanes) {
-  __shared__ float gain[2][MAX_DIM];
+__global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles, int lanes) {
   __shared__ __align__(16) float most[PAGES ? THREADS / 4 : 1][16];  // of each head at work, the largest magnitudes of its runs of eight
   const int D = a.head_dim, lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes;
-  const int at_once = THREADS / lanes, h_first = blockIdx.y * at_once + (threadIdx.x >> 5) * per_warp;
-  const int heads = a.q.n_heads + a.k.n_heads + a.v.n_heads, step = at_once * gridDim.y;
   const Units<VEC, NU, INTER> units(sub, D, a.rotary);
+  const Role role(roles, a, per_warp);
+  const bool is_v = role.what == 2, normed = a.eps > 0.f && !is_v, turned = a.rotary > 0 && !is_v;
+  const RopeView view = role.view(a);
   const int page_bits = PAGES ? __ffs(a.page) - 1 : 0;
+  const float inv_d = 1.f / D;
   pdl_wait();
   pdl_trigger();
-  if (a.eps > 0.f) {
-    for (int i = threadIdx.x; i < D; i += THREADS) {
-      gain[0][i] = gain_at(a.q_gain, a.gain_dtype, i);
-      gain[1][i] = gain_at(a.k_gain, a.gain_dtype, i);
-    }
-    __syncthreads();
-  }
-  const float inv_d = 1.f / D;
-  for (int t = blockIdx.x; static_cast<uint32_t>(t) < static_cast<uint32_t>(a.n_tokens); t = static_cast<int>(t + gridDim.x)) {
+  const int64_t n = static_cast<int64_t>(a.n_tokens) * role.slices, step = static_cast<int64_t>(role.blocks) * (THREADS / 32);
+#pragma unroll 1
+  for (int64_t unit = static_cast<int64_t>(role.block) * (THREADS / 32) + (threadIdx.x >> 5); unit < n; unit += step) {
+    const int t = static_cast<int>(role.slices > 1 ? unit / role.slices : unit);
+    const int first = (role.slices > 1 ? static_cast<int>(unit - static_cast<int64_t>(t) * role.slices) : 0) * role.per_slice;
+    const int end = min(view.n_heads, first + role.per_slice);
     const int pos = a.rotary > 0 ? a.positions[t] : 0;
     const int64_t slot = PAGES ? a.slots[t] : 0;
+    // the first heads' elements are asked for beside the position and the table
+    const T* x0 = static_cast<const T*>(view.in) + t * view.in_tok;
     Pack<T, VEC> p0[NU], p1[NU];
-    auto load = [&](int h) {
-      const bool is_q = h < a.q.n_heads, is_v = h >= a.q.n_heads + a.k.n_heads;
-      const RopeView& view = is_q ? a.q : is_v ? a.v : a.k;
-      const int hh = is_q ? h : is_v ? h - a.q.n_heads - a.k.n_heads : h - a.q.n_heads;
-      units.load(static_cast<const T*>(view.in) + t * view.in_tok + hh * view.in_head, h < heads, p0, p1);
-    };
-    load(h_first + lane / lanes);
+    int h = first + lane / lanes;
+    units.load(x0 + h * view.in_head, h < end, p0, p1);
     if (pos < 0) continue;
-    float c[NU][VEC], s[NU][VEC];
-    if (a.rotary > 0) {
-      if (pos >= a.max_position) {
-        set_status(a.status, DOPR_ERR_INVALID_ARG);
-        continue;
-      }
-      units.angles(a.table, pos, a.rotary, sub, false, c, s);
-    }
-    if (PAGES && slot >= a.n_slots) {
+    if (a.rotary > 0 && pos >= a.max_position) {
       set_status(a.status, DOPR_ERR_INVALID_ARG);
       continue;
     }
-    float g[NU][2 * VEC];
-    int held = -1;  // whose gain g is
+    if constexpr (PAGES) {
+      if (slot >= a.n_slots) {
+        set_status(a.status, DOPR_ERR_INVALID_ARG);
+        continue;
+      }
+      if (role.what > 0 && slot < 0) continue;
+    }
+    // z_a = r (x_a ga c - x_b gb s), z_b = r (x_b gb c + x_a ga s): the gains go with cos and sin, once a token
+    float ac[NU][VEC], bs[NU][VEC], bc[NU][VEC], as[NU][VEC];
+    {
+      float g[NU][2 * VEC], c[NU][VEC], s[NU][VEC];
+      const void* gain = role.what == 0 ? a.q_gain : a.k_gain;
+#pragma unroll
+      for (int i = 0; i < NU; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          g[i][j] = normed && units.there[i] ? gain_at(gain, a.gain_dtype, units.ia[i] + j) : 1.f;
+          g[i][VEC + j] = normed && units.there[i] ? gain_at(gain, a.gain_dtype, units.ib[i] + j) : 1.f;
+          c[i][j] = 1.f, s[i][j] = 0.f;
+        }
+      if (turned) units.angles(a.table, pos, a.rotary, sub, false, c, s);
+#pragma unroll
+      for (int i = 0; i < NU; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          constexpr bool APART = !INTER || VEC == 1;
+          const bool pair = turned && units.turns[i];
+          const float ga = APART || !pair ? g[i][j] : g[i][2 * j], gb = APART || !pair ? g[i][VEC + j] : g[i][2 * j + 1];
+          ac[i][j] = __fmul_rn(ga, c[i][j]), as[i][j] = __fmul_rn(ga, s[i][j]);
+          bc[i][j] = __fmul_rn(gb, c[i][j]), bs[i][j] = __fmul_rn(gb, s[i][j]);
+        }
+    }
 #pragma unroll 1
-    for (int h0 = h_first; h0 < heads; h0 += step) {
-      const int h = h0 + lane / lanes;
-      const bool is_q = h < a.q.n_heads, is_v = h >= a.q.n_heads + a.k.n_heads, valid = h < heads;
-      const int hh = is_q ? h : is_v ? h - a.q.n_heads - a.k.n_heads : h - a.q.n_heads;
+    for (int h0 = first; h0 < end; h0 += per_warp) {
+      const bool valid = h < end;
+      const int hh = h;
       float x[NU][2 * VEC];
       units.widen(p0, p1, valid, x);
-      if (h0 + step < heads) load(h + step);
-      if (a.eps > 0.f) {
+      h += per_warp;
+      units.load(x0 + h * view.in_head, h < end, p0, p1);
+      float r = 1.f;
+      if (normed) {
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NU; ++i)
 #pragma unroll
           for (int j = 0; j < 2 * VEC; ++j) sum = __fmaf_rn(x[i][j], x[i][j], sum);
-        sum = head_sum(sum, lanes);
-        if (!is_v) {
-          if (held != (is_q ? 0 : 1)) units.gains(gain[held = is_q ? 0 : 1], g);
-          const float r = rsqrtf(__fmaf_rn(sum, inv_d, a.eps));
+        r = rsqrtf(__fmaf_rn(head_sum(sum, lanes), inv_d, a.eps));
+      }
+      if (normed || turned) {
 #pragma unroll
-          for (int i = 0; i < NU; ++i)
+        for (int i = 0; i < NU; ++i) {
+          const bool pair = turned && units.turns[i];
 #pragma unroll
-            for (int j = 0; j < 2 * VEC; ++j) x[i][j] = __fmul_rn(__fmul_rn(x[i][j], r), g[i][j]);
+          for (int j = 0; j < VEC; ++j) {
+            constexpr bool APART = !INTER || VEC == 1;
+            if (pair) {
+              float &xa = APART ? x[i][j] : x[i][2 * j], &xb = APART ? x[i][VEC + j] : x[i][2 * j + 1];
+              const float u = xa, v = xb;
+              xa = __fmul_rn(__fmaf_rn(u, ac[i][j], -__fmul_rn(v, bs[i][j])), r);
+              xb = __fmul_rn(__fmaf_rn(v, bc[i][j], __fmul_rn(u, as[i][j])), r);
+            } else {  // (c 1: ac and bc are the gains)
+              x[i][j] = __fmul_rn(__fmul_rn(x[i][j], ac[i][j]), r);
+              x[i][VEC + j] = __fmul_rn(__fmul_rn(x[i][VEC + j], bc[i][j]), r);
+            }
+          }
         }
       }
-      if (a.rotary > 0 && !is_v) units.turn(x, c, s);
-      if (!PAGES || is_q) {
-        const RopeView& view = is_q ? a.q : a.k;
+      if (!PAGES || role.what == 0) {
         if (valid) units.store(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head, x);
-      }
-      if constexpr (PAGES) {
-        static_assert(VEC == 8 && NU == 1, "runs of eight");
-        // what the row's type holds goes into the page: the same as a row stored and appended
-        float top[2] = {0.f, 0.f};
+      } else {
+        if constexpr (PAGES) {
+          static_assert(VEC == 8 && NU == 1, "runs of eight");
+          // what the row's type holds goes into the page: the same as a row stored and appended
+          float top[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) {
-          x[0][j] = to_f32(from_f32<T>(x[0][j]));
-          track_range(top[j / VEC], x[0][j]);
-        }
-        float* of_head = most[threadIdx.x / lanes];
-        __syncwarp();  // the head before has been read
-        if (units.there[0]) of_head[units.ia[0] / 8] = top[0], of_head[units.ib[0] / 8] = top[1];
-        __syncwarp();
-        if (valid && !is_q && slot >= 0 && units.there[0]) {
-          uint8_t* base = (is_v ? a.v_pool : a.k_pool) + ((slot >> page_bits) * a.k.n_heads + hh) * pages4::page_bytes(a.page, D);
-          const int row = static_cast<int>(slot) & (a.page - 1);
+          for (int j = 0; j < 2 * VEC; ++j) {
+            x[0][j] = to_f32(from_f32<T>(x[0][j]));
+            track_range(top[j / VEC], x[0][j]);
+          }
+          float* of_head = most[threadIdx.x / lanes];
+          __syncwarp();  // the head before has been read
+          if (units.there[0]) of_head[units.ia[0] / 8] = top[0], of_head[units.ib[0] / 8] = top[1];
+          __syncwarp();
+          if (valid && units.there[0]) {
+            uint8_t* base = (is_v ? a.v_pool : a.k_pool) + ((slot >> page_bits) * a.k.n_heads + hh) * pages4::page_bytes(a.page, D);
+            const int row = static_cast<int>(slot) & (a.page - 1);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int run = (k ? units.ib[0] : units.ia[0]) / 8;
-            const float4 m = *reinterpret_cast<const float4*>(of_head + (run & ~3));
-            float all = m.x, inverse;
-            track_range(all, m.y), track_range(all, m.z), track_range(all, m.w);
-            const uint32_t byte = pages4::scale_byte(all, inverse);
-            uint32_t word = 0;
+            for (int k = 0; k < 2; ++k) {
+              const int run = (k ? units.ib[0] : units.ia[0]) / 8;
+              const float4 m = *reinterpret_cast<const float4*>(of_head + (run & ~3));
+              float all = m.x, inverse;
+              track_range(all, m.y), track_range(all, m.z), track_range(all, m.w);
+              const uint32_t byte = pages4::scale_byte(all, inverse);
+              uint32_t word = 0;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) word |= pages4::code_of(x[0][8 * k + j], inverse) << (4 * (j / 2) + 16 * (j & 1));
-            if (byte == pages4::SCALE_NAN) word = 0x88888888u;
-            *reinterpret_cast<uint32_t*>(base + row * (D / 2) + 4 * run) = word;
-            if ((run & 3) == 0) {
-              base[a.page * (D / 2) + row * (D / 32) + run / 4] = static_cast<uint8_t>(byte);
-              if (byte == pages4::SCALE_NAN) set_status(a.status, DOPR_ERR_RANGE);
+              for (int j = 0; j < 8; ++j) word |= pages4::code_of(x[0][8 * k + j], inverse) << (4 * (j / 2) + 16 * (j & 1));
+              if (byte == pages4::SCALE_NAN) word = 0x88888888u;
+              *reinterpret_cast<uint32_t*>(base + row * (D / 2) + 4 * run) = word;
+              if ((run & 3) == 0) {
+                base[a.page * (D / 2) + row * (D / 32) + run / 4] = static_cast<uint8_t>(byte);
+                if (byte == pages4::SCALE_NAN) set_status(a.status, DOPR_ERR_RANGE);
+              }
             }
           }
         }
@@ -265,25 +307,33 @@ __global__ void __launch_bounds__(THREADS) k_head_norm(const __grid_constant__ H
   }
 }
 
-// Gradients of the inputs, and each block's part of the gains'.
+// Gradients of the inputs, and each block's part of its gain's.
 template <typename T, int VEC, int NU, bool INTER>
-__global__ void __launch_bounds__(THREADS) k_head_norm_back(const __grid_constant__ HeadNormArgs a, int lanes) {
-  __shared__ float gain[2][MAX_DIM];
-  __shared__ float part[THREADS / 32][2][MAX_DIM];
+__global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles, int lanes) {
+  __shared__ __align__(16) float gain[MAX_DIM];
+  __shared__ float part[THREADS / 32][MAX_DIM];
   const int D = a.head_dim, lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes, warp = threadIdx.x >> 5;
-  const int at_once = THREADS / lanes, h_first = warp * per_warp, heads = a.q.n_heads + a.k.n_heads;
   const Units<VEC, NU, INTER> units(sub, D, a.rotary);
+  const Role role(roles, a, per_warp);
+  const RopeView view = role.view(a), from = role.what == 0 ? a.qx : a.kx;
   pdl_wait();
   pdl_trigger();
-  for (int i = threadIdx.x; i < D; i += THREADS) {
-    gain[0][i] = gain_at(a.q_gain, a.gain_dtype, i);
-    gain[1][i] = gain_at(a.k_gain, a.gain_dtype, i);
-  }
+  for (int i = threadIdx.x; i < D; i += THREADS) gain[i] = gain_at(role.what == 0 ? a.q_gain : a.k_gain, a.gain_dtype, i);
   __syncthreads();
   const float inv_d = 1.f / D;
-  float dg[2][NU][2 * VEC] = {};
-  for (int t = blockIdx.x; static_cast<uint32_t>(t) < static_cast<uint32_t>(a.n_tokens); t = static_cast<int>(t + gridDim.x)) {
+  float dg[NU][2 * VEC] = {};
+  const int64_t n = static_cast<int64_t>(a.n_tokens) * role.slices, step = static_cast<int64_t>(role.blocks) * (THREADS / 32);
+#pragma unroll 1
+  for (int64_t unit = static_cast<int64_t>(role.block) * (THREADS / 32) + warp; unit < n; unit += step) {
+    const int t = static_cast<int>(role.slices > 1 ? unit / role.slices : unit);
+    const int first = (role.slices > 1 ? static_cast<int>(unit - static_cast<int64_t>(t) * role.slices) : 0) * role.per_slice;
+    const int end = min(view.n_heads, first + role.per_slice);
     const int pos = a.rotary > 0 ? a.positions[t] : 0;
+    const T *x0 = static_cast<const T*>(from.in) + t * from.in_tok, *z0 = static_cast<const T*>(view.in) + t * view.in_tok;
+    Pack<T, VEC> p0[NU], p1[NU], p2[NU], p3[NU];
+    int h = first + lane / lanes;
+    units.load(x0 + h * from.in_head, h < end, p0, p1);
+    units.load(z0 + h * view.in_head, h < end, p2, p3);
     if (pos < 0) continue;
     float c[NU][VEC], s[NU][VEC];
     if (a.rotary > 0) {
@@ -294,81 +344,83 @@ __global__ void __launch_bounds__(THREADS) k_head_norm_back(const __grid_constan
       units.angles(a.table, pos, a.rotary, sub, true, c, s);
     }
 #pragma unroll 1
-    for (int h0 = h_first; h0 < heads; h0 += at_once) {
-      const int h = h0 + lane / lanes;
-      const bool is_q = h < a.q.n_heads, valid = h < heads;
-      const int hh = is_q ? h : h - a.q.n_heads;
-      const RopeView &view = is_q ? a.q : a.k, &from = is_q ? a.qx : a.kx;
-      Pack<T, VEC> p0[NU], p1[NU], p2[NU], p3[NU];
-      units.load(static_cast<const T*>(from.in) + t * from.in_tok + hh * from.in_head, valid, p0, p1);
-      units.load(static_cast<const T*>(view.in) + t * view.in_tok + hh * view.in_head, valid, p2, p3);
-      float x[NU][2 * VEC], dy[NU][2 * VEC];
+    for (int h0 = first; h0 < end; h0 += per_warp) {
+      const bool valid = h < end;
+      const int hh = h;
+      float x[NU][2 * VEC], w[NU][2 * VEC];
       units.widen(p0, p1, valid, x);
-      units.widen(p2, p3, valid, dy);
-      if (a.rotary > 0) units.turn(dy, c, s);
-      const float* g = gain[is_q ? 0 : 1];
-      float sum = 0.f, dot = 0.f;
+      units.widen(p2, p3, valid, w);
+      h += per_warp;
+      units.load(x0 + h * from.in_head, h < end, p0, p1);
+      units.load(z0 + h * view.in_head, h < end, p2, p3);
+      if (a.rotary > 0) units.turn(w, c, s);
+      float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) {
-          const float w = units.there[i] ? dy[i][j] * g[(j < VEC ? units.ia[i] : units.ib[i] - VEC) + j] : 0.f;
-          sum = __fmaf_rn(x[i][j], x[i][j], sum);
-          dot = __fmaf_rn(x[i][j], w, dot);
+        for (int j = 0; j < 2 * VEC; ++j) sum = __fmaf_rn(x[i][j], x[i][j], sum);
+      const float r = rsqrtf(__fmaf_rn(head_sum(sum, lanes), inv_d, a.eps));
+      float dot = 0.f;
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        float g[2 * VEC];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          g[j] = units.there[i] ? gain[units.ia[i] + j] : 0.f;
+          g[VEC + j] = units.there[i] ? gain[units.ib[i] + j] : 0.f;
         }
-      sum = head_sum(sum, lanes);
-      dot = head_sum(dot, lanes);
-      const float r = rsqrtf(__fmaf_rn(sum, inv_d, a.eps)), by = dot * inv_d * r * r;
+#pragma unroll
+        for (int j = 0; j < 2 * VEC; ++j) {
+          dg[i][j] = __fmaf_rn(__fmul_rn(w[i][j], r), x[i][j], dg[i][j]);
+          w[i][j] = __fmul_rn(w[i][j], g[j]);
+          dot = __fmaf_rn(x[i][j], w[i][j], dot);
+        }
+      }
+      const float by = head_sum(dot, lanes) * inv_d * r * r;
 #pragma unroll
       for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) {
-          const float n = dy[i][j] * x[i][j] * r;
-          dg[0][i][j] += is_q ? n : 0.f;
-          dg[1][i][j] += is_q ? 0.f : n;
-          const float w = units.there[i] ? dy[i][j] * g[(j < VEC ? units.ia[i] : units.ib[i] - VEC) + j] : 0.f;
-          x[i][j] = r * (w - x[i][j] * by);
-        }
+        for (int j = 0; j < 2 * VEC; ++j) x[i][j] = __fmul_rn(__fmaf_rn(-x[i][j], by, w[i][j]), r);
       if (valid) units.store(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head, x);
     }
   }
-  if (!a.dq_gain && !a.dk_gain) return;
+  if (!(role.what == 0 ? a.dq_gain : a.dk_gain)) return;
   // the lanes of a warp that hold the same elements, then the warps, in a fixed order
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+  for (int i = 0; i < NU; ++i)
 #pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-      for (int j = 0; j < 2 * VEC; ++j) {
-        float v = dg[k][i][j];
-        for (int o = lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane < lanes && units.there[i]) part[warp][k][(j < VEC ? units.ia[i] : units.ib[i] - VEC) + j] = v;
-      }
+    for (int j = 0; j < 2 * VEC; ++j) {
+      float v = dg[i][j];
+      for (int o = lanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane < lanes && units.there[i]) part[warp][(j < VEC ? units.ia[i] : units.ib[i] - VEC) + j] = v;
+    }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += THREADS) {
+  for (int i = threadIdx.x; i < D; i += THREADS) {
     float v = 0.f;
 #pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) v += part[w][i / D][i % D];
-    a.ws[static_cast<int64_t>(blockIdx.x) * 2 * D + i] = v;
+    for (int w = 0; w < THREADS / 32; ++w) v += part[w][i];
+    a.ws[static_cast<int64_t>(blockIdx.x) * D + i] = v;
   }
 }
 
-// The blocks' parts of the gains' gradients, in a fixed order: 32 columns a block, a warp every eighth part.
-__global__ void __launch_bounds__(256) k_head_norm_gains(const float* ws, int parts, int D, float* dq_gain, float* dk_gain) {
-  __shared__ float sums[8][32];
+// The blocks' parts of the gains' gradients, in a fixed order: 32 columns of one gain a block, a warp every 32nd part.
+__global__ void __launch_bounds__(1024) k_head_norm_gains(const float* ws, int q_parts, int k_parts, int D, float* dq_gain, float* dk_gain) {
+  __shared__ float sums[32][33];
   const int i = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  const bool is_k = blockIdx.y > 0;
+  float* out = is_k ? dk_gain : dq_gain;
   pdl_wait();
   pdl_trigger();
+  if (!out) return;
   float v = 0.f;
-  if (i < 2 * D)
-    for (int p = warp; p < parts; p += 8) v += ws[static_cast<int64_t>(p) * 2 * D + i];
+  if (i < D)
+    for (int p = warp; p < (is_k ? k_parts : q_parts); p += 32) v += ws[static_cast<int64_t>(p + (is_k ? q_parts : 0)) * D + i];
   sums[warp][threadIdx.x & 31] = v;
   __syncthreads();
-  if (warp > 0 || i >= 2 * D) return;
-#pragma unroll
-  for (int w = 1; w < 8; ++w) v += sums[w][threadIdx.x];
-  float* out = i < D ? dq_gain : dk_gain;
-  if (out) out[i % D] = v;
+  // warp w adds up column w
+  v = sums[threadIdx.x & 31][warp];
+  v = warp_sum(v);
+  if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + warp < D) out[blockIdx.x * 32 + warp] = v;
 }
 
 bool aligned16(const void* p, int64_t s0, int64_t s1, int size) {
@@ -391,14 +443,33 @@ int lanes_of(int head_dim, int vec) {
   return lanes;
 }
 
+// Blocks for each role, by the heads: few tokens leave most SMs idle, so their heads go to several warps.
+Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks) {
+  const int heads[3] = {a.q.n_heads, a.k.n_heads, a.v.n_heads}, per_warp = 32 / lanes, warps = THREADS / 32;
+  const int all = heads[0] + heads[1] + heads[2];
+  Roles r{};
+  int at = 0;
+  for (int i = 0; i < 3; ++i) {
+    const int turns = (heads[i] + per_warp - 1) / per_warp;
+    const int64_t room = static_cast<int64_t>(most_blocks) * warps * heads[i] / (all > 0 ? all : 1);  // warps
+    int64_t slices = a.n_tokens > 0 ? room / a.n_tokens : 1;
+    slices = slices < 1 ? 1 : slices > turns ? (turns > 0 ? turns : 1) : slices;
+    // as many as are not empty
+    const int per = turns > 0 ? static_cast<int>((turns + slices - 1) / slices) : 1;
+    slices = turns > 0 ? (turns + per - 1) / per : 1;
+    const int64_t units = static_cast<int64_t>(a.n_tokens) * slices, need = (units + warps - 1) / warps, part = (room + warps - 1) / warps;
+    r.slices[i] = static_cast<int>(slices);
+    at += heads[i] > 0 ? static_cast<int>(need < part ? need : part > 0 ? part : 1) : 0;
+    r.end[i] = at;
+  }
+  return r;
+}
+
 template <typename T, int VEC, int NU, bool INTER, bool PAGES>
 cudaError_t launch(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const int lanes = lanes_of(a.head_dim, VEC), at_once = THREADS / lanes;
-  const int heads = a.q.n_heads + a.k.n_heads + a.v.n_heads;
-  // few tokens leave most SMs idle: a token's heads over several blocks
-  const int turns = (heads + at_once - 1) / at_once, spare = a.n_tokens < 4 * num_sms ? 4 * num_sms / a.n_tokens : 1;
-  const dim3 grid(a.n_tokens < 65536 ? a.n_tokens : 65536, turns < spare ? turns : spare);
-  return launch_dependent(k_head_norm<T, VEC, NU, INTER, PAGES>, grid, THREADS, 0, st, a, lanes);
+  const int lanes = lanes_of(a.head_dim, VEC);
+  const Roles r = roles_of(a, lanes, 12 * num_sms);
+  return launch_dependent(k_head_norm<T, VEC, NU, INTER, PAGES>, dim3(r.end[2]), THREADS, 0, st, a, r, lanes);
 }
 template <typename T>
 cudaError_t launch_type(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
@@ -409,14 +480,17 @@ cudaError_t launch_type(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
 }
 template <typename T, int VEC, int NU, bool INTER>
 cudaError_t launch_back(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  int blocks = 4 * num_sms < HEAD_NORM_MAX_BLOCKS ? 4 * num_sms : HEAD_NORM_MAX_BLOCKS;
-  if (a.n_tokens < blocks) blocks = a.n_tokens;
-  if (blocks > 0) {
-    const cudaError_t e = launch_dependent(k_head_norm_back<T, VEC, NU, INTER>, dim3(blocks), THREADS, 0, st, a, lanes_of(a.head_dim, VEC));
+  const int lanes = lanes_of(a.head_dim, VEC);
+  const int blocks = 4 * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? 4 * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
+  Roles r{};
+  if (a.n_tokens > 0) {
+    r = roles_of(a, lanes, blocks);
+    const cudaError_t e = launch_dependent(k_head_norm_back<T, VEC, NU, INTER>, dim3(r.end[1]), THREADS, 0, st, a, r, lanes);
     if (e != cudaSuccess) return e;
   }
   if (!a.dq_gain && !a.dk_gain) return cudaSuccess;
-  return launch_dependent(k_head_norm_gains, dim3((2 * a.head_dim + 31) / 32), 256, 0, st, a.ws, blocks, a.head_dim, a.dq_gain, a.dk_gain);
+  return launch_dependent(k_head_norm_gains, dim3((a.head_dim + 31) / 32, 2), 1024, 0, st, a.ws, r.end[0], r.end[1] - r.end[0], a.head_dim,
+                          a.dq_gain, a.dk_gain);
 }
 template <typename T>
 cudaError_t launch_back_type(const HeadNormArgs& a, int num_sms, cudaStream_t st) {

@@ -38,6 +38,55 @@ struct alignas(VEC > 1 ? 16 : sizeof(T)) Pack {
   T v[VEC];
 };
 
+// A run of VEC elements from and to memory.
+template <typename T, int VEC>
+__device__ __forceinline__ void widen_run(const Pack<T, VEC>& p, float* x) {
+  if constexpr (VEC > 1 && sizeof(T) == 2) {
+    const uint4 w = reinterpret_cast<const uint4&>(p);
+    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float2 f;
+      if constexpr (std::is_same_v<T, __half>) f = __half22float2(reinterpret_cast<const __half2&>(v[i]));
+      else f = __bfloat1622float2(reinterpret_cast<const __nv_bfloat162&>(v[i]));
+      x[2 * i] = f.x, x[2 * i + 1] = f.y;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) x[j] = to_f32(p.v[j]);
+  }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_run(T* to, const float* x) {
+  if constexpr (VEC > 1 && sizeof(T) == 2) {
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = std::is_same_v<T, __half> ? pack_f16x2(x[2 * i], x[2 * i + 1]) : pack_bf16x2(x[2 * i], x[2 * i + 1]);
+    *reinterpret_cast<uint4*>(to) = uint4{v[0], v[1], v[2], v[3]};
+  } else {
+    Pack<T, VEC> p;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) p.v[j] = from_f32<T>(x[j]);
+    *reinterpret_cast<Pack<T, VEC>*>(to) = p;
+  }
+}
+// Two at once: a * b + c, a * b.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 a, a, b, c;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
 __device__ __forceinline__ float gain_at(const void* gain, int dtype, int i) {
   if (!gain) return 1.f;
   if (dtype == DOPR_F32) return static_cast<const float*>(gain)[i];
@@ -104,36 +153,39 @@ struct Units {
       }
     }
   }
+  // (zeros where there is nothing)
   template <typename T>
   __device__ __forceinline__ void load(const T* row, bool valid, Pack<T, VEC> (&a)[NU], Pack<T, VEC> (&b)[NU]) const {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
+      a[i] = Pack<T, VEC>{}, b[i] = Pack<T, VEC>{};
       if (!there[i] || !valid) continue;
       a[i] = *reinterpret_cast<const Pack<T, VEC>*>(row + ia[i]);
       b[i] = *reinterpret_cast<const Pack<T, VEC>*>(row + ib[i]);
     }
   }
   template <typename T>
-  __device__ __forceinline__ void widen(const Pack<T, VEC> (&a)[NU], const Pack<T, VEC> (&b)[NU], bool valid, float (&x)[NU][2 * VEC]) const {
+  __device__ __forceinline__ void widen(const Pack<T, VEC> (&a)[NU], const Pack<T, VEC> (&b)[NU], float (&x)[NU][2 * VEC]) const {
 #pragma unroll
-    for (int i = 0; i < NU; ++i)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        x[i][j] = there[i] && valid ? to_f32(a[i].v[j]) : 0.f;
-        x[i][VEC + j] = there[i] && valid ? to_f32(b[i].v[j]) : 0.f;
-      }
+    for (int i = 0; i < NU; ++i) widen_run(a[i], x[i]), widen_run(b[i], x[i] + VEC);
   }
   template <typename T>
   __device__ __forceinline__ void store(T* row, const float (&x)[NU][2 * VEC]) const {
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       if (!there[i]) continue;
-      Pack<T, VEC> a, b;
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) a.v[j] = from_f32<T>(x[i][j]), b.v[j] = from_f32<T>(x[i][VEC + j]);
-      *reinterpret_cast<Pack<T, VEC>*>(row + ia[i]) = a;
-      *reinterpret_cast<Pack<T, VEC>*>(row + ib[i]) = b;
+      store_run<T, VEC>(row + ia[i], x[i]);
+      store_run<T, VEC>(row + ib[i], x[i] + VEC);
     }
+  }
+  // The sum of x y over this lane's units.
+  static __device__ __forceinline__ float dot(const float (&x)[NU][2 * VEC], const float (&y)[NU][2 * VEC]) {
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+#pragma unroll
+      for (int j = 0; j < 2 * VEC; j += 2) sum = fma2(make_float2(x[i][j], x[i][j + 1]), make_float2(y[i][j], y[i][j + 1]), sum);
+    return sum.x + sum.y;
   }
 };
 
@@ -233,33 +285,40 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
       const bool valid = h < end;
       const int hh = h;
       float x[NU][2 * VEC];
-      units.widen(p0, p1, valid, x);
+      units.widen(p0, p1, x);
       h += per_warp;
       units.load(x0 + h * view.in_head, h < end, p0, p1);
       float r = 1.f;
       if (normed) {
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < NU; ++i)
-#pragma unroll
-          for (int j = 0; j < 2 * VEC; ++j) sum = __fmaf_rn(x[i][j], x[i][j], sum);
-        r = rsqrtf(__fmaf_rn(head_sum(sum, lanes), inv_d, a.eps));
+        r = rsqrtf(__fmaf_rn(head_sum(units.dot(x, x), lanes), inv_d, a.eps));
       }
       if (normed || turned) {
+        constexpr bool APART = !INTER || VEC == 1;
+        const float2 rr = make_float2(r, r);
 #pragma unroll
         for (int i = 0; i < NU; ++i) {
-          const bool pair = turned && units.turns[i];
+          if (!(turned && units.turns[i])) {  // (c 1: ac and bc are the gains)
 #pragma unroll
-          for (int j = 0; j < VEC; ++j) {
-            constexpr bool APART = !INTER || VEC == 1;
-            if (pair) {
+            for (int j = 0; j < VEC; ++j) {
+              x[i][j] = __fmul_rn(__fmul_rn(x[i][j], ac[i][j]), r);
+              x[i][VEC + j] = __fmul_rn(__fmul_rn(x[i][VEC + j], bc[i][j]), r);
+            }
+          } else if constexpr (APART && VEC > 1) {
+#pragma unroll
+            for (int j = 0; j < VEC; j += 2) {
+              const float2 u = make_float2(x[i][j], x[i][j + 1]), v = make_float2(x[i][VEC + j], x[i][VEC + j + 1]);
+              const float2 y = mul2(v, make_float2(-bs[i][j], -bs[i][j + 1])), z = mul2(u, make_float2(as[i][j], as[i][j + 1]));
+              const float2 za = mul2(fma2(u, make_float2(ac[i][j], ac[i][j + 1]), y), rr);
+              const float2 zb = mul2(fma2(v, make_float2(bc[i][j], bc[i][j + 1]), z), rr);
+              x[i][j] = za.x, x[i][j + 1] = za.y, x[i][VEC + j] = zb.x, x[i][VEC + j + 1] = zb.y;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
               float &xa = APART ? x[i][j] : x[i][2 * j], &xb = APART ? x[i][VEC + j] : x[i][2 * j + 1];
               const float u = xa, v = xb;
               xa = __fmul_rn(__fmaf_rn(u, ac[i][j], -__fmul_rn(v, bs[i][j])), r);
               xb = __fmul_rn(__fmaf_rn(v, bc[i][j], __fmul_rn(u, as[i][j])), r);
-            } else {  // (c 1: ac and bc are the gains)
-              x[i][j] = __fmul_rn(__fmul_rn(x[i][j], ac[i][j]), r);
-              x[i][VEC + j] = __fmul_rn(__fmul_rn(x[i][VEC + j], bc[i][j]), r);
             }
           }
         }
@@ -271,11 +330,12 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
           static_assert(VEC == 8 && NU == 1, "runs of eight");
           // what the row's type holds goes into the page: the same as a row stored and appended
           float top[2] = {0.f, 0.f};
+          if (normed || turned) {
 #pragma unroll
-          for (int j = 0; j < 2 * VEC; ++j) {
-            x[0][j] = to_f32(from_f32<T>(x[0][j]));
-            track_range(top[j / VEC], x[0][j]);
+            for (int j = 0; j < 2 * VEC; ++j) x[0][j] = to_f32(from_f32<T>(x[0][j]));
           }
+#pragma unroll
+          for (int j = 0; j < 2 * VEC; ++j) track_range(top[j / VEC], x[0][j]);
           float* of_head = most[threadIdx.x / lanes];
           __syncwarp();  // the head before has been read
           if (units.there[0]) of_head[units.ia[0] / 8] = top[0], of_head[units.ib[0] / 8] = top[1];
@@ -290,9 +350,7 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
               float all = m.x, inverse;
               track_range(all, m.y), track_range(all, m.z), track_range(all, m.w);
               const uint32_t byte = pages4::scale_byte(all, inverse);
-              uint32_t word = 0;
-#pragma unroll
-              for (int j = 0; j < 8; ++j) word |= pages4::code_of(x[0][8 * k + j], inverse) << (4 * (j / 2) + 16 * (j & 1));
+              uint32_t word = pages4::codes_of(x[0] + 8 * k, inverse);
               if (byte == pages4::SCALE_NAN) word = 0x88888888u;
               *reinterpret_cast<uint32_t*>(base + row * (D / 2) + 4 * run) = word;
               if ((run & 3) == 0) {
@@ -310,7 +368,6 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
 // Gradients of the inputs, and each block's part of its gain's.
 template <typename T, int VEC, int NU, bool INTER>
 __global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles, int lanes) {
-  __shared__ __align__(16) float gain[MAX_DIM];
   __shared__ float part[THREADS / 32][MAX_DIM];
   const int D = a.head_dim, lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes, warp = threadIdx.x >> 5;
   const Units<VEC, NU, INTER> units(sub, D, a.rotary);
@@ -318,10 +375,13 @@ __global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_cons
   const RopeView view = role.view(a), from = role.what == 0 ? a.qx : a.kx;
   pdl_wait();
   pdl_trigger();
-  for (int i = threadIdx.x; i < D; i += THREADS) gain[i] = gain_at(role.what == 0 ? a.q_gain : a.k_gain, a.gain_dtype, i);
-  __syncthreads();
   const float inv_d = 1.f / D;
-  float dg[NU][2 * VEC] = {};
+  float dg[NU][2 * VEC] = {}, g[NU][2 * VEC];
+#pragma unroll
+  for (int i = 0; i < NU; ++i)
+#pragma unroll
+    for (int j = 0; j < 2 * VEC; ++j)
+      g[i][j] = units.there[i] ? gain_at(role.what == 0 ? a.q_gain : a.k_gain, a.gain_dtype, (j < VEC ? units.ia[i] : units.ib[i] - VEC) + j) : 0.f;
   const int64_t n = static_cast<int64_t>(a.n_tokens) * role.slices, step = static_cast<int64_t>(role.blocks) * (THREADS / 32);
 #pragma unroll 1
   for (int64_t unit = static_cast<int64_t>(role.block) * (THREADS / 32) + warp; unit < n; unit += step) {
@@ -348,39 +408,36 @@ __global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_cons
       const bool valid = h < end;
       const int hh = h;
       float x[NU][2 * VEC], w[NU][2 * VEC];
-      units.widen(p0, p1, valid, x);
-      units.widen(p2, p3, valid, w);
+      units.widen(p0, p1, x);
+      units.widen(p2, p3, w);
       h += per_warp;
       units.load(x0 + h * from.in_head, h < end, p0, p1);
       units.load(z0 + h * view.in_head, h < end, p2, p3);
       if (a.rotary > 0) units.turn(w, c, s);
-      float sum = 0.f;
+      // sum x^2 is there first; sum w x = sum dy x g too, so that dg's terms dy x serve both
+      const float r = rsqrtf(__fmaf_rn(head_sum(units.dot(x, x), lanes), inv_d, a.eps));
+      float2 dot = make_float2(0.f, 0.f);
+      const float2 rr = make_float2(r, r);
 #pragma unroll
       for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) sum = __fmaf_rn(x[i][j], x[i][j], sum);
-      const float r = rsqrtf(__fmaf_rn(head_sum(sum, lanes), inv_d, a.eps));
-      float dot = 0.f;
-#pragma unroll
-      for (int i = 0; i < NU; ++i) {
-        float g[2 * VEC];
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          g[j] = units.there[i] ? gain[units.ia[i] + j] : 0.f;
-          g[VEC + j] = units.there[i] ? gain[units.ib[i] + j] : 0.f;
+        for (int j = 0; j < 2 * VEC; j += 2) {
+          const float2 gg = make_float2(g[i][j], g[i][j + 1]), dy = make_float2(w[i][j], w[i][j + 1]);
+          const float2 yx = mul2(dy, make_float2(x[i][j], x[i][j + 1]));
+          const float2 sum = fma2(yx, rr, make_float2(dg[i][j], dg[i][j + 1]));
+          dg[i][j] = sum.x, dg[i][j + 1] = sum.y;
+          dot = fma2(yx, gg, dot);
         }
-#pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) {
-          dg[i][j] = __fmaf_rn(__fmul_rn(w[i][j], r), x[i][j], dg[i][j]);
-          w[i][j] = __fmul_rn(w[i][j], g[j]);
-          dot = __fmaf_rn(x[i][j], w[i][j], dot);
-        }
-      }
-      const float by = head_sum(dot, lanes) * inv_d * r * r;
+      // dx = (dy g - x by) r
+      const float by = head_sum(dot.x + dot.y, lanes) * inv_d * r * r;
 #pragma unroll
       for (int i = 0; i < NU; ++i)
 #pragma unroll
-        for (int j = 0; j < 2 * VEC; ++j) x[i][j] = __fmul_rn(__fmaf_rn(-x[i][j], by, w[i][j]), r);
+        for (int j = 0; j < 2 * VEC; j += 2) {
+          const float2 xb = mul2(make_float2(x[i][j], x[i][j + 1]), make_float2(-by, -by));
+          const float2 d = mul2(fma2(make_float2(w[i][j], w[i][j + 1]), make_float2(g[i][j], g[i][j + 1]), xb), rr);
+          x[i][j] = d.x, x[i][j + 1] = d.y;
+        }
       if (valid) units.store(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head, x);
     }
   }
@@ -504,8 +561,9 @@ cudaError_t launch_back_type(const HeadNormArgs& a, int num_sms, cudaStream_t st
 // A thread a run of eight elements: a word and its group's scale in, 16 bytes out.  c s is exact.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) k_read_4bit(const __grid_constant__ Read4Args a) {
-  const int D = a.head_dim, runs = D / 8, at_once = THREADS / runs, run = threadIdx.x % runs;
+  const int D = a.head_dim, runs = D / 8, at_once = THREADS / runs, run = threadIdx.x % runs, h0 = threadIdx.x / runs;
   const int page_bits = __ffs(a.page) - 1;
+  const int64_t page_bytes = pages4::page_bytes(a.page, D);
   pdl_wait();
   pdl_trigger();
   for (int t = blockIdx.x; static_cast<uint32_t>(t) < static_cast<uint32_t>(a.n_rows); t = static_cast<int>(t + gridDim.x)) {
@@ -516,18 +574,30 @@ __global__ void __launch_bounds__(THREADS) k_read_4bit(const __grid_constant__ R
       continue;
     }
     const int row = static_cast<int>(slot) & (a.page - 1);
-    for (int h = threadIdx.x / runs; h < 2 * a.n_kv_heads; h += at_once) {
-      const bool is_v = h >= a.n_kv_heads;
-      const int hh = is_v ? h - a.n_kv_heads : h;
-      const uint8_t* base = (is_v ? a.v_pool : a.k_pool) + ((slot >> page_bits) * a.n_kv_heads + hh) * pages4::page_bytes(a.page, D);
-      const uint32_t word = *reinterpret_cast<const uint32_t*>(base + row * (D / 2) + 4 * run);
-      const uint32_t byte = base[a.page * (D / 2) + row * (D / 32) + run / 4];
-      const float s = byte > pages4::SCALE_LAST ? __uint_as_float(0x7fc00000u) : __half2float(__ushort_as_half(static_cast<unsigned short>(byte << 7)));
-      Pack<T, 8> out;
+    const int64_t base = (slot >> page_bits) * a.n_kv_heads * page_bytes;
+    const uint8_t *k = a.k_pool + base, *v = a.v_pool + base;
+    const int code = row * (D / 2) + 4 * run, scale = a.page * (D / 2) + row * (D / 32) + run / 4;
+    T *ko = static_cast<T*>(a.k.out) + t * a.k.out_tok + 8 * run, *vo = static_cast<T*>(a.v.out) + t * a.v.out_tok + 8 * run;
+    for (int h = h0; h < a.n_kv_heads; h += at_once) {
+      const int64_t at = h * page_bytes;
+      // a key's and a value's at once
+      const uint32_t word[2] = {*reinterpret_cast<const uint32_t*>(k + at + code), *reinterpret_cast<const uint32_t*>(v + at + code)};
+      const uint32_t byte[2] = {k[at + scale], v[at + scale]};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) out.v[j] = from_f32<T>((static_cast<int>(word >> (4 * (j / 2) + 16 * (j & 1)) & 15u) - 8) * s);
-      const RopeView& view = is_v ? a.v : a.k;
-      *reinterpret_cast<Pack<T, 8>*>(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head + 8 * run) = out;
+      for (int i = 0; i < 2; ++i) {
+        uint32_t x[4];
+        const pages4::Widen<T> widen(byte[i] * 0x10001u);
+        widen(word[i], x);
+        if constexpr (std::is_same_v<T, __half>) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __half2 y = __hmul2(reinterpret_cast<const __half2&>(x[j]), __float2half2_rn(pages4::Widen<T>::UNIT));
+            x[j] = reinterpret_cast<const uint32_t&>(y);
+          }
+        }
+        if (byte[i] > pages4::SCALE_LAST) x[0] = x[1] = x[2] = x[3] = 0x7fff7fffu;  // NaN
+        *reinterpret_cast<uint4*>((i ? vo + h * a.v.out_head : ko + h * a.k.out_head)) = uint4{x[0], x[1], x[2], x[3]};
+      }
     }
   }
 }

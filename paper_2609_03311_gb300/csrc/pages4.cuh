@@ -34,23 +34,32 @@ __host__ __device__ inline int64_t page_bytes(int page, int head_dim) { return s
 
 // The scale of a group with the largest magnitude `most`: its byte.  `inverse`: what elements are multiplied by, a little more
 // than 1 / s: an element half way between two codes goes to the larger one, and no other crosses a border by it (x / s, x of 11
-// bits and s of 4, is half way or at least 2^-13 off; the factor is 2^-20 off).
+// bits and s of 4, is half way or at least 2^-13 off; the factor is 2^-20 off, give or take 2^-22).
 __device__ __forceinline__ uint32_t scale_byte(float most, float& inverse) {
-  const float want = __fdiv_rn(most, 7.f);
-  // steps of three bits of mantissa, of 2^-17 at the low end
+  // s = t steps, steps of three bits of mantissa, of 2^-17 at the low end: the smallest whole t with 7 t >= most / step.  The product
+  // with 1 / 7 is off by less than 2^-18, so its ceiling less that is t or one below.
+  const float want = __fmul_rn(most, 1.f / 7.f);
   const int e = max(static_cast<int>(__float_as_uint(want) >> 23) - 127 - 3, -17);
   const float step = __uint_as_float(static_cast<uint32_t>(e + 127) << 23), per = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-  const float s = fminf(ceilf(__fmul_rn(want, per)) * step, SCALE_MAX);
+  float t = fmaxf(ceilf(__fmaf_rn(want, per, -0x1p-18f)), 0.f);
+  if (__fmul_rn(7.f, t) < __fmul_rn(most, per)) t += 1.f;
+  const float s = fminf(t * step, SCALE_MAX);
   if (!(most <= HELD_MAX)) {  // a NaN, an infinity, too large
     inverse = 0.f;
     return SCALE_NAN;
   }
-  inverse = s > 0.f ? __fmul_rn(__frcp_rn(s), 1.f + 0x1p-20f) : 0.f;
+  inverse = s > 0.f ? __fmul_rn(__fdividef(1.f, s), 1.f + 0x1p-20f) : 0.f;
   return static_cast<uint32_t>(__half_as_ushort(__float2half_rn(s))) >> 7;
 }
-// c + 8 in the low four bits: the fused product with 2^23 + 2^22 + 8 is rounded to a whole number.
-__device__ __forceinline__ uint32_t code_of(float x, float inverse) {
-  return __float_as_uint(__fmaf_rn(x, inverse, 12582912.f + 8.f)) & 15u;
+// The word of eight elements.  The fused product with 2^23 + 2^22 + 8 is rounded to a whole number, c + 8 in its low bits; what stands
+// above them is zero in the lower 16 bits, where sums of four with 1, 16, 256, 4096 put the codes in order.
+__device__ __forceinline__ uint32_t codes_of(const float* x, float inverse) {
+  uint32_t n[8], half[2];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) n[j] = __float_as_uint(__fmaf_rn(x[j], inverse, 12582912.f + 8.f));
+#pragma unroll
+  for (int j = 0; j < 2; ++j) half[j] = n[j] + 16 * n[2 + j] + 256 * n[4 + j] + 4096 * n[6 + j];
+  return __byte_perm(half[0], half[1], 0x5410);
 }
 
 // Codes to the products' type T.  A nibble n put into the mantissa of a power of two is the number 2^p + n; less 2^p + 8 and times s it

@@ -19,6 +19,10 @@ namespace dopr {
 namespace {
 
 constexpr int THREADS = 128, MAX_DIM = 256;
+// Blocks an SM holds, by the registers that they get; and in the whole grid, for each SM, of many tokens: a view's blocks are not equally
+// long, so several rounds of them even out.  26,800 rows of 40 heads: 5 held, 40 in all 93.6 us; 6 and 12 115.7; 6 and 36 101;
+// 7 and 42 104 (registers run out).  Gradients of 8,192 rows: 4 held 60.8, 3 63.2, 5 74.2; their partial sums want few blocks.
+constexpr int HELD = 5, GRID = 40, BACK_HELD = 4;
 
 template <typename T>
 __device__ __forceinline__ float to_f32(T x) {
@@ -189,9 +193,17 @@ struct Units {
   }
 };
 
+// Lanes that hold a head: a power of two.
+__host__ __device__ constexpr int lanes_of(int head_dim, int vec) {
+  int lanes = 1;
+  while (lanes < 32 && lanes * 2 * vec < head_dim) lanes *= 2;
+  return lanes;
+}
 // Adds up over the `lanes` (a power of two) lanes that hold a head.
 __device__ __forceinline__ float head_sum(float v, int lanes) {
-  for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
@@ -217,11 +229,142 @@ struct Role {
   __device__ __forceinline__ const RopeView& view(const HeadNormArgs& a) const { return what == 0 ? a.q : what == 1 ? a.k : a.v; }
 };
 
-// PAGES: keys and values go to 4-bit pages.
-template <typename T, int VEC, int NU, bool INTER, bool PAGES>
-__global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles, int lanes) {
+// A warp's units, one ahead: the next one's position and slot, and its first heads' elements, are asked for before this one's work.
+struct Unit {
+  int t, first, end, pos;
+  int64_t slot;
+  bool there;
+};
+template <bool PAGES, bool POSITIONS = true>
+struct Walk {
+  const HeadNormArgs& a;
+  const Role& role;
+  const int n_heads;
+  int64_t unit, n, step;
+  __device__ __forceinline__ Walk(const HeadNormArgs& args, const Role& r, int heads)
+      : a(args), role(r), n_heads(heads), unit(static_cast<int64_t>(r.block) * (THREADS / 32) + (threadIdx.x >> 5)),
+        n(static_cast<int64_t>(args.n_tokens) * r.slices), step(static_cast<int64_t>(r.blocks) * (THREADS / 32)) {}
+  __device__ __forceinline__ Unit next() {
+    Unit u{};
+    u.there = unit < n;
+    if (!u.there) return u;
+    u.t = static_cast<int>(unit);
+    if (role.slices > 1) {
+      u.t = static_cast<int>(static_cast<uint32_t>(unit) / static_cast<uint32_t>(role.slices));  // (slices of few tokens: below 2^31)
+      u.first = (static_cast<int>(unit) - u.t * role.slices) * role.per_slice;
+    }
+    u.end = min(n_heads, u.first + role.per_slice);
+    if (POSITIONS && a.rotary > 0) u.pos = a.positions[u.t];
+    if (POSITIONS && PAGES) u.slot = a.slots[u.t];
+    unit += step;
+    return u;
+  }
+};
+
+// The next unit's cos and sin into L1.
+__device__ __forceinline__ void prefetch_angles(const HeadNormArgs& a, const Unit& u, int lane) {
+  if (u.pos < 0 || u.pos >= a.max_position) return;
+  const char* cs = reinterpret_cast<const char*>(a.table + static_cast<int64_t>(u.pos) * (a.rotary / 2));
+  for (int i = lane * 128; i < a.rotary * 4; i += 32 * 128) asm volatile("prefetch.global.L1 [%0];" ::"l"(cs + i));
+}
+
+// The elements of a warp's heads, turn after turn over its units, of one or two views (backward: the inputs and the outputs'
+// gradients).  What bounds these kernels is how much is on its way: 16-byte copies into shared memory run AHEAD turns before they
+// are taken (one turn in registers: a chunk of 26,800 rows 112 us).  A lane takes what it has copied itself.
+template <typename T, int VEC, int NU, bool INTER, int VIEWS, int AHEAD>
+struct Stream {
+  static constexpr bool RING = VEC > 1;
+  static constexpr int STAGES = AHEAD + 1, BYTES = RING ? (THREADS / 32) * STAGES * VIEWS * 1024 : 16;
+  using P = Pack<T, VEC>;
+  const Units<VEC, NU, INTER>& units;
+  const RopeView (&views)[VIEWS];
+  Walk<false, false> walk;
+  Unit u;
+  int h, stage = 0, lanes;
+  uint8_t* ring;
+  P p[RING ? 1 : VIEWS][2][NU];
+  __device__ __forceinline__ Stream(const Units<VEC, NU, INTER>& un, const HeadNormArgs& a, const Role& role, const RopeView (&v)[VIEWS],
+                                    uint8_t* smem, int lanes_)
+      : units(un), views(v), walk(a, role, v[0].n_heads), lanes(lanes_), ring(smem + (threadIdx.x >> 5) * STAGES * VIEWS * 1024) {
+    u = walk.next();
+    h = u.first;
+    if constexpr (RING) {
+#pragma unroll 1
+      for (int i = 0; i < AHEAD; ++i) put(i);
+    } else {
+      put(0);
+    }
+  }
+  __device__ __forceinline__ void put(int at) {
+    if (RING && !u.there) {
+      cp_async_commit();
+      return;
+    }
+    const int lane = threadIdx.x & 31, mine = h + lane / lanes;
+    const bool valid = u.there && mine < u.end;
+#pragma unroll
+    for (int i = 0; i < VIEWS; ++i) {
+      const T* row = static_cast<const T*>(views[i].in) + u.t * views[i].in_tok + mine * views[i].in_head;
+      if constexpr (RING) {
+        const uint32_t to = smem_u32(ring) + (at * VIEWS + i) * 1024 + lane * 16;
+        if (units.there[0]) {
+          cp_async16(to, row + units.ia[0], valid);
+          cp_async16(to + 512, row + units.ib[0], valid);
+        }
+      } else {
+        units.load(row, valid, p[i][0], p[i][1]);
+      }
+    }
+    if constexpr (RING) cp_async_commit();
+    if (u.there) {
+      h += 32 / lanes;
+      if (h >= u.end) {
+        u = walk.next();
+        h = u.first;
+      }
+    }
+  }
+  // The next turn's elements, in 32 bits; the one AHEAD turns behind it is asked for.
+  __device__ __forceinline__ void take(float (&x)[VIEWS][NU][2 * VEC]) {
+    if constexpr (RING) {
+      put(stage == 0 ? AHEAD : stage - 1);  // the stage taken last
+      asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD) : "memory");
+      const int lane = threadIdx.x & 31;
+#pragma unroll
+      for (int i = 0; i < VIEWS; ++i) {
+        const P* from = reinterpret_cast<const P*>(ring + (stage * VIEWS + i) * 1024) + lane;
+        if (units.there[0]) {
+          widen_run(from[0], x[i][0]);
+          widen_run(from[32], x[i][0] + VEC);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 2 * VEC; ++j) x[i][0][j] = 0.f;
+        }
+      }
+      stage = stage == AHEAD ? 0 : stage + 1;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VIEWS; ++i) units.widen(p[i][0], p[i][1], x[i]);
+      put(0);
+    }
+  }
+  // Goes past a unit.
+  __device__ __forceinline__ void skip(const Unit& past) {
+    for (int i = past.first; i < past.end; i += 32 / lanes) {
+      float x[VIEWS][NU][2 * VEC];
+      take(x);
+    }
+  }
+};
+
+// PAGES: keys and values go to 4-bit pages.  DIM: the head size, or 0: head_dim.
+template <typename T, int VEC, int NU, bool INTER, bool PAGES, int DIM>
+__global__ void __launch_bounds__(THREADS, HELD) k_head_norm(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles) {
+  using S = Stream<T, VEC, NU, INTER, 1, 4>;
+  __shared__ __align__(16) uint8_t ring[S::BYTES];
+  __shared__ __align__(16) float gains[MAX_DIM];
   __shared__ __align__(16) float most[PAGES ? THREADS / 4 : 1][16];  // of each head at work, the largest magnitudes of its runs of eight
-  const int D = a.head_dim, lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes;
+  const int D = DIM > 0 ? DIM : a.head_dim, lanes = lanes_of(D, VEC), lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes;
   const Units<VEC, NU, INTER> units(sub, D, a.rotary);
   const Role role(roles, a, per_warp);
   const bool is_v = role.what == 2, normed = a.eps > 0.f && !is_v, turned = a.rotary > 0 && !is_v;
@@ -230,64 +373,64 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
   const float inv_d = 1.f / D;
   pdl_wait();
   pdl_trigger();
-  const int64_t n = static_cast<int64_t>(a.n_tokens) * role.slices, step = static_cast<int64_t>(role.blocks) * (THREADS / 32);
+  if (normed) {
+    for (int i = threadIdx.x; i < D; i += THREADS) gains[i] = gain_at(role.what == 0 ? a.q_gain : a.k_gain, a.gain_dtype, i);
+    __syncthreads();
+  }
+  Walk<PAGES> walk(a, role, view.n_heads);
+  const RopeView views[1] = {view};
+  S stream(units, a, role, views, ring, lanes);
+  Unit next = walk.next();
 #pragma unroll 1
-  for (int64_t unit = static_cast<int64_t>(role.block) * (THREADS / 32) + (threadIdx.x >> 5); unit < n; unit += step) {
-    const int t = static_cast<int>(role.slices > 1 ? unit / role.slices : unit);
-    const int first = (role.slices > 1 ? static_cast<int>(unit - static_cast<int64_t>(t) * role.slices) : 0) * role.per_slice;
-    const int end = min(view.n_heads, first + role.per_slice);
-    const int pos = a.rotary > 0 ? a.positions[t] : 0;
-    const int64_t slot = PAGES ? a.slots[t] : 0;
-    // the first heads' elements are asked for beside the position and the table
-    const T* x0 = static_cast<const T*>(view.in) + t * view.in_tok;
-    Pack<T, VEC> p0[NU], p1[NU];
-    int h = first + lane / lanes;
-    units.load(x0 + h * view.in_head, h < end, p0, p1);
-    if (pos < 0) continue;
-    if (a.rotary > 0 && pos >= a.max_position) {
+  while (next.there) {
+    const Unit u = next;
+    next = walk.next();
+    int h = u.first + lane / lanes;
+    bool skip = u.pos < 0 || (PAGES && role.what > 0 && u.slot < 0);
+    if ((a.rotary > 0 && u.pos >= a.max_position) || (PAGES && u.pos >= 0 && u.slot >= a.n_slots)) {
       set_status(a.status, DOPR_ERR_INVALID_ARG);
-      continue;
+      skip = true;
     }
-    if constexpr (PAGES) {
-      if (slot >= a.n_slots) {
-        set_status(a.status, DOPR_ERR_INVALID_ARG);
-        continue;
-      }
-      if (role.what > 0 && slot < 0) continue;
+    if (skip) {
+      stream.skip(u);
+      continue;
     }
     // z_a = r (x_a ga c - x_b gb s), z_b = r (x_b gb c + x_a ga s): the gains go with cos and sin, once a token
     float ac[NU][VEC], bs[NU][VEC], bc[NU][VEC], as[NU][VEC];
     {
-      float g[NU][2 * VEC], c[NU][VEC], s[NU][VEC];
-      const void* gain = role.what == 0 ? a.q_gain : a.k_gain;
+      float c[NU][VEC], s[NU][VEC];
 #pragma unroll
       for (int i = 0; i < NU; ++i)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) c[i][j] = 1.f, s[i][j] = 0.f;
+      if (turned) units.angles(a.table, u.pos, a.rotary, sub, false, c, s);
+#pragma unroll
+      for (int i = 0; i < NU; ++i) {
+        float g[2 * VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          g[i][j] = normed && units.there[i] ? gain_at(gain, a.gain_dtype, units.ia[i] + j) : 1.f;
-          g[i][VEC + j] = normed && units.there[i] ? gain_at(gain, a.gain_dtype, units.ib[i] + j) : 1.f;
-          c[i][j] = 1.f, s[i][j] = 0.f;
+          g[j] = normed && units.there[i] ? gains[units.ia[i] + j] : 1.f;
+          g[VEC + j] = normed && units.there[i] ? gains[units.ib[i] + j] : 1.f;
         }
-      if (turned) units.angles(a.table, pos, a.rotary, sub, false, c, s);
-#pragma unroll
-      for (int i = 0; i < NU; ++i)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
           constexpr bool APART = !INTER || VEC == 1;
           const bool pair = turned && units.turns[i];
-          const float ga = APART || !pair ? g[i][j] : g[i][2 * j], gb = APART || !pair ? g[i][VEC + j] : g[i][2 * j + 1];
+          const float ga = APART || !pair ? g[j] : g[2 * j], gb = APART || !pair ? g[VEC + j] : g[2 * j + 1];
           ac[i][j] = __fmul_rn(ga, c[i][j]), as[i][j] = __fmul_rn(ga, s[i][j]);
-          bc[i][j] = __fmul_rn(gb, c[i][j]), bs[i][j] = __fmul_rn(gb, s[i][j]);
+          bc[i][j] = __fmul_rn(gb, c[i][j]), bs[i][j] = __fmul_rn(gb, -s[i][j]);
         }
+      }
     }
 #pragma unroll 1
-    for (int h0 = first; h0 < end; h0 += per_warp) {
-      const bool valid = h < end;
+    for (int h0 = u.first; h0 < u.end; h0 += per_warp) {
+      const bool valid = h < u.end;
       const int hh = h;
-      float x[NU][2 * VEC];
-      units.widen(p0, p1, x);
+      float taken[1][NU][2 * VEC];
+      stream.take(taken);
+      auto& x = taken[0];
       h += per_warp;
-      units.load(x0 + h * view.in_head, h < end, p0, p1);
+      if (h0 == u.first && turned && next.there) prefetch_angles(a, next, lane);
       float r = 1.f;
       if (normed) {
         r = rsqrtf(__fmaf_rn(head_sum(units.dot(x, x), lanes), inv_d, a.eps));
@@ -306,9 +449,9 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
           } else if constexpr (APART && VEC > 1) {
 #pragma unroll
             for (int j = 0; j < VEC; j += 2) {
-              const float2 u = make_float2(x[i][j], x[i][j + 1]), v = make_float2(x[i][VEC + j], x[i][VEC + j + 1]);
-              const float2 y = mul2(v, make_float2(-bs[i][j], -bs[i][j + 1])), z = mul2(u, make_float2(as[i][j], as[i][j + 1]));
-              const float2 za = mul2(fma2(u, make_float2(ac[i][j], ac[i][j + 1]), y), rr);
+              const float2 u2 = make_float2(x[i][j], x[i][j + 1]), v = make_float2(x[i][VEC + j], x[i][VEC + j + 1]);
+              const float2 y = mul2(v, make_float2(bs[i][j], bs[i][j + 1])), z = mul2(u2, make_float2(as[i][j], as[i][j + 1]));
+              const float2 za = mul2(fma2(u2, make_float2(ac[i][j], ac[i][j + 1]), y), rr);
               const float2 zb = mul2(fma2(v, make_float2(bc[i][j], bc[i][j + 1]), z), rr);
               x[i][j] = za.x, x[i][j + 1] = za.y, x[i][VEC + j] = zb.x, x[i][VEC + j + 1] = zb.y;
             }
@@ -316,15 +459,15 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
 #pragma unroll
             for (int j = 0; j < VEC; ++j) {
               float &xa = APART ? x[i][j] : x[i][2 * j], &xb = APART ? x[i][VEC + j] : x[i][2 * j + 1];
-              const float u = xa, v = xb;
-              xa = __fmul_rn(__fmaf_rn(u, ac[i][j], -__fmul_rn(v, bs[i][j])), r);
-              xb = __fmul_rn(__fmaf_rn(v, bc[i][j], __fmul_rn(u, as[i][j])), r);
+              const float ua = xa, ub = xb;
+              xa = __fmul_rn(__fmaf_rn(ua, ac[i][j], __fmul_rn(ub, bs[i][j])), r);
+              xb = __fmul_rn(__fmaf_rn(ub, bc[i][j], __fmul_rn(ua, as[i][j])), r);
             }
           }
         }
       }
       if (!PAGES || role.what == 0) {
-        if (valid) units.store(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head, x);
+        if (valid) units.store(static_cast<T*>(view.out) + u.t * view.out_tok + hh * view.out_head, x);
       } else {
         if constexpr (PAGES) {
           static_assert(VEC == 8 && NU == 1, "runs of eight");
@@ -341,8 +484,8 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
           if (units.there[0]) of_head[units.ia[0] / 8] = top[0], of_head[units.ib[0] / 8] = top[1];
           __syncwarp();
           if (valid && units.there[0]) {
-            uint8_t* base = (is_v ? a.v_pool : a.k_pool) + ((slot >> page_bits) * a.k.n_heads + hh) * pages4::page_bytes(a.page, D);
-            const int row = static_cast<int>(slot) & (a.page - 1);
+            uint8_t* base = (is_v ? a.v_pool : a.k_pool) + ((u.slot >> page_bits) * a.k.n_heads + hh) * pages4::page_bytes(a.page, D);
+            const int row = static_cast<int>(u.slot) & (a.page - 1);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const int run = (k ? units.ib[0] : units.ia[0]) / 8;
@@ -365,11 +508,81 @@ __global__ void __launch_bounds__(THREADS, PAGES ? 5 : 6) k_head_norm(const __gr
   }
 }
 
+// Rows into 4-bit pages as they are: a lane 16 elements that follow one another, two lanes a group.
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) k_append_4bit(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles) {
+  constexpr int LANES = D / 16, PER_WARP = 32 / LANES;
+  const int lane = threadIdx.x & 31, sub = lane % LANES, page_bits = __ffs(a.page) - 1;
+  const Role role(roles, a, PER_WARP);
+  const RopeView view = role.view(a);
+  uint8_t* const pool = role.what == 1 ? a.k_pool : a.v_pool;
+  const int64_t page_bytes = pages4::page_bytes(a.page, D);
+  pdl_wait();
+  pdl_trigger();
+  Walk<true> walk(a, role, view.n_heads);
+  uint4 p[2];
+  auto load = [&](const Unit& u, int h) {
+    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(view.in) + u.t * view.in_tok + h * view.in_head) + 2 * sub;
+    p[0] = p[1] = uint4{0, 0, 0, 0};
+    if (u.there && h < u.end) p[0] = from[0], p[1] = from[1];
+  };
+  Unit next = walk.next();
+  load(next, next.first + lane / LANES);
+#pragma unroll 1
+  while (next.there) {
+    const Unit u = next;
+    next = walk.next();
+    int h = u.first + lane / LANES;
+    if (u.slot < 0 || u.slot >= a.n_slots) {
+      if (u.slot >= 0) set_status(a.status, DOPR_ERR_INVALID_ARG);
+      load(next, next.first + lane / LANES);
+      continue;
+    }
+    const int row = static_cast<int>(u.slot) & (a.page - 1);
+    uint8_t* const base = pool + (u.slot >> page_bits) * a.k.n_heads * page_bytes;
+#pragma unroll 1
+    for (int h0 = u.first; h0 < u.end; h0 += PER_WARP) {
+      const bool valid = h < u.end;
+      uint8_t* to = base + h * page_bytes;
+      float x[16];
+      widen_run(reinterpret_cast<const Pack<T, 8>&>(p[0]), x);
+      widen_run(reinterpret_cast<const Pack<T, 8>&>(p[1]), x + 8);
+      h += PER_WARP;
+      const bool last = h0 + PER_WARP >= u.end;
+      load(last ? next : u, last ? next.first + lane / LANES : h);
+      float top[4] = {0.f, 0.f, 0.f, 0.f}, inverse;
+#pragma unroll
+      for (int j = 0; j < 16; ++j) track_range(top[j & 3], x[j]);
+      track_range(top[0], top[1]), track_range(top[2], top[3]), track_range(top[0], top[2]);
+      track_range(top[0], __shfl_xor_sync(0xffffffffu, top[0], 1));
+      const uint32_t byte = pages4::scale_byte(top[0], inverse);
+      uint2 words = make_uint2(pages4::codes_of(x, inverse), pages4::codes_of(x + 8, inverse));
+      if (byte == pages4::SCALE_NAN) words = make_uint2(0x88888888u, 0x88888888u);
+      // the head's scales to its first lane
+      uint32_t scales = byte << (8 * (sub >> 1));
+#pragma unroll
+      for (int o = 2; o < LANES; o <<= 1) scales |= __shfl_xor_sync(0xffffffffu, scales, o);
+      if (valid) {
+        *reinterpret_cast<uint2*>(to + row * (D / 2) + 8 * sub) = words;
+        if (sub == 0) {
+          uint8_t* s = to + a.page * (D / 2) + row * (D / 32);
+          if constexpr (D == 128) *reinterpret_cast<uint32_t*>(s) = scales;
+          else *reinterpret_cast<uint16_t*>(s) = static_cast<uint16_t>(scales);
+        }
+        if (byte == pages4::SCALE_NAN) set_status(a.status, DOPR_ERR_RANGE);
+      }
+    }
+  }
+}
+
 // Gradients of the inputs, and each block's part of its gain's.
-template <typename T, int VEC, int NU, bool INTER>
-__global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles, int lanes) {
+template <typename T, int VEC, int NU, bool INTER, int DIM>
+__global__ void __launch_bounds__(THREADS, BACK_HELD) k_head_norm_back(const __grid_constant__ HeadNormArgs a, const __grid_constant__ Roles roles) {
+  using S = Stream<T, VEC, NU, INTER, 2, 3>;
+  __shared__ __align__(16) uint8_t ring[S::BYTES];
   __shared__ float part[THREADS / 32][MAX_DIM];
-  const int D = a.head_dim, lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes, warp = threadIdx.x >> 5;
+  const int D = DIM > 0 ? DIM : a.head_dim, lanes = lanes_of(D, VEC), lane = threadIdx.x & 31, sub = lane & (lanes - 1), per_warp = 32 / lanes,
+            warp = threadIdx.x >> 5;
   const Units<VEC, NU, INTER> units(sub, D, a.rotary);
   const Role role(roles, a, per_warp);
   const RopeView view = role.view(a), from = role.what == 0 ? a.qx : a.kx;
@@ -382,37 +595,31 @@ __global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_cons
 #pragma unroll
     for (int j = 0; j < 2 * VEC; ++j)
       g[i][j] = units.there[i] ? gain_at(role.what == 0 ? a.q_gain : a.k_gain, a.gain_dtype, (j < VEC ? units.ia[i] : units.ib[i] - VEC) + j) : 0.f;
-  const int64_t n = static_cast<int64_t>(a.n_tokens) * role.slices, step = static_cast<int64_t>(role.blocks) * (THREADS / 32);
+  Walk<false> walk(a, role, view.n_heads);
+  const RopeView views[2] = {from, view};
+  S stream(units, a, role, views, ring, lanes);
+  Unit next = walk.next();
 #pragma unroll 1
-  for (int64_t unit = static_cast<int64_t>(role.block) * (THREADS / 32) + warp; unit < n; unit += step) {
-    const int t = static_cast<int>(role.slices > 1 ? unit / role.slices : unit);
-    const int first = (role.slices > 1 ? static_cast<int>(unit - static_cast<int64_t>(t) * role.slices) : 0) * role.per_slice;
-    const int end = min(view.n_heads, first + role.per_slice);
-    const int pos = a.rotary > 0 ? a.positions[t] : 0;
-    const T *x0 = static_cast<const T*>(from.in) + t * from.in_tok, *z0 = static_cast<const T*>(view.in) + t * view.in_tok;
-    Pack<T, VEC> p0[NU], p1[NU], p2[NU], p3[NU];
-    int h = first + lane / lanes;
-    units.load(x0 + h * from.in_head, h < end, p0, p1);
-    units.load(z0 + h * view.in_head, h < end, p2, p3);
-    if (pos < 0) continue;
-    float c[NU][VEC], s[NU][VEC];
-    if (a.rotary > 0) {
-      if (pos >= a.max_position) {
-        set_status(a.status, DOPR_ERR_INVALID_ARG);
-        continue;
-      }
-      units.angles(a.table, pos, a.rotary, sub, true, c, s);
+  while (next.there) {
+    const Unit u = next;
+    next = walk.next();
+    int h = u.first + lane / lanes;
+    if (u.pos < 0 || (a.rotary > 0 && u.pos >= a.max_position)) {
+      if (u.pos >= 0) set_status(a.status, DOPR_ERR_INVALID_ARG);
+      stream.skip(u);
+      continue;
     }
+    float c[NU][VEC], s[NU][VEC];
+    if (a.rotary > 0) units.angles(a.table, u.pos, a.rotary, sub, true, c, s);
 #pragma unroll 1
-    for (int h0 = first; h0 < end; h0 += per_warp) {
-      const bool valid = h < end;
+    for (int h0 = u.first; h0 < u.end; h0 += per_warp) {
+      const bool valid = h < u.end;
       const int hh = h;
-      float x[NU][2 * VEC], w[NU][2 * VEC];
-      units.widen(p0, p1, x);
-      units.widen(p2, p3, w);
+      float taken[2][NU][2 * VEC];
+      stream.take(taken);
+      auto &x = taken[0], &w = taken[1];
       h += per_warp;
-      units.load(x0 + h * from.in_head, h < end, p0, p1);
-      units.load(z0 + h * view.in_head, h < end, p2, p3);
+      if (h0 == u.first && a.rotary > 0 && next.there) prefetch_angles(a, next, lane);
       if (a.rotary > 0) units.turn(w, c, s);
       // sum x^2 is there first; sum w x = sum dy x g too, so that dg's terms dy x serve both
       const float r = rsqrtf(__fmaf_rn(head_sum(units.dot(x, x), lanes), inv_d, a.eps));
@@ -438,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 4) k_head_norm_back(const __grid_cons
           const float2 d = mul2(fma2(make_float2(w[i][j], w[i][j + 1]), make_float2(g[i][j], g[i][j + 1]), xb), rr);
           x[i][j] = d.x, x[i][j + 1] = d.y;
         }
-      if (valid) units.store(static_cast<T*>(view.out) + t * view.out_tok + hh * view.out_head, x);
+      if (valid) units.store(static_cast<T*>(view.out) + u.t * view.out_tok + hh * view.out_head, x);
     }
   }
   if (!(role.what == 0 ? a.dq_gain : a.dk_gain)) return;
@@ -494,109 +701,129 @@ bool wide(const HeadNormArgs& a, int size) {
   }
   return ok;
 }
-int lanes_of(int head_dim, int vec) {
-  int lanes = 1;
-  while (lanes < 32 && lanes * 2 * vec < head_dim) lanes *= 2;
-  return lanes;
-}
-
-// Blocks for each role, by the heads: few tokens leave most SMs idle, so their heads go to several warps.
+// Blocks for each role, by its work: turns of heads a warp, and about one for a token's cos and sin (gradients of 8,192 rows by the
+// heads alone: 60.3 us, the keys' blocks end last).  Few tokens leave most SMs idle, so their heads go to several warps.
 Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks) {
   const int heads[3] = {a.q.n_heads, a.k.n_heads, a.v.n_heads}, per_warp = 32 / lanes, warps = THREADS / 32;
-  const int all = heads[0] + heads[1] + heads[2];
+  int turns[3], all = 0;
+  for (int i = 0; i < 3; ++i) {
+    turns[i] = (heads[i] + per_warp - 1) / per_warp;
+    all += turns[i] > 0 ? turns[i] + 1 : 0;
+  }
   Roles r{};
   int at = 0;
   for (int i = 0; i < 3; ++i) {
-    const int turns = (heads[i] + per_warp - 1) / per_warp;
-    const int64_t room = static_cast<int64_t>(most_blocks) * warps * heads[i] / (all > 0 ? all : 1);  // warps
-    int64_t slices = a.n_tokens > 0 ? room / a.n_tokens : 1;
-    slices = slices < 1 ? 1 : slices > turns ? (turns > 0 ? turns : 1) : slices;
-    // as many as are not empty
-    const int per = turns > 0 ? static_cast<int>((turns + slices - 1) / slices) : 1;
-    slices = turns > 0 ? (turns + per - 1) / per : 1;
-    const int64_t units = static_cast<int64_t>(a.n_tokens) * slices, need = (units + warps - 1) / warps, part = (room + warps - 1) / warps;
-    r.slices[i] = static_cast<int>(slices);
-    at += heads[i] > 0 ? static_cast<int>(need < part ? need : part > 0 ? part : 1) : 0;
+    r.slices[i] = 1;
+    if (turns[i] > 0) {
+      const int64_t blocks = static_cast<int64_t>(most_blocks) * (turns[i] + 1) / all, part = blocks > 0 ? blocks : 1;
+      int64_t slices = a.n_tokens > 0 ? part * warps / a.n_tokens : 1;
+      slices = slices < 1 ? 1 : slices > turns[i] ? turns[i] : slices;
+      const int per = static_cast<int>((turns[i] + slices - 1) / slices);  // as many slices as are not empty
+      r.slices[i] = (turns[i] + per - 1) / per;
+      const int64_t need = (static_cast<int64_t>(a.n_tokens) * r.slices[i] + warps - 1) / warps;
+      at += static_cast<int>(need < part ? need : part);
+    }
     r.end[i] = at;
   }
   return r;
 }
 
-template <typename T, int VEC, int NU, bool INTER, bool PAGES>
+template <typename T, int VEC, int NU, bool INTER, bool PAGES, int DIM>
 cudaError_t launch(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const int lanes = lanes_of(a.head_dim, VEC);
-  const Roles r = roles_of(a, lanes, 12 * num_sms);
-  return launch_dependent(k_head_norm<T, VEC, NU, INTER, PAGES>, dim3(r.end[2]), THREADS, 0, st, a, r, lanes);
+  const Roles r = roles_of(a, lanes_of(a.head_dim, VEC), GRID * num_sms);
+  return launch_dependent(k_head_norm<T, VEC, NU, INTER, PAGES, DIM>, dim3(r.end[2]), THREADS, 0, st, a, r);
 }
-template <typename T>
+template <typename T, bool INTER>
 cudaError_t launch_type(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
-  if (wide(a, sizeof(T)))
-    return a.interleaved ? launch<T, VEC, 1, true, false>(a, num_sms, st) : launch<T, VEC, 1, false, false>(a, num_sms, st);
-  return a.interleaved ? launch<T, 1, 4, true, false>(a, num_sms, st) : launch<T, 1, 4, false, false>(a, num_sms, st);
+  if (!wide(a, sizeof(T))) return launch<T, 1, 4, INTER, false, 0>(a, num_sms, st);
+  return a.head_dim == 128 ? launch<T, VEC, 1, INTER, false, 128>(a, num_sms, st) : launch<T, VEC, 1, INTER, false, 0>(a, num_sms, st);
 }
-template <typename T, int VEC, int NU, bool INTER>
+template <typename T, bool INTER>
+cudaError_t launch_pages(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
+  return a.head_dim == 128 ? launch<T, 8, 1, INTER, true, 128>(a, num_sms, st) : launch<T, 8, 1, INTER, true, 64>(a, num_sms, st);
+}
+template <typename T, int D>
+cudaError_t launch_append(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
+  const Roles r = roles_of(a, D / 16, 16 * num_sms);
+  return launch_dependent(k_append_4bit<T, D>, dim3(r.end[2]), THREADS, 0, st, a, r);
+}
+template <typename T, int VEC, int NU, bool INTER, int DIM>
 cudaError_t launch_back(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const int lanes = lanes_of(a.head_dim, VEC);
-  const int blocks = 4 * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? 4 * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
+  const int blocks = BACK_HELD * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? 4 * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
   Roles r{};
   if (a.n_tokens > 0) {
-    r = roles_of(a, lanes, blocks);
-    const cudaError_t e = launch_dependent(k_head_norm_back<T, VEC, NU, INTER>, dim3(r.end[1]), THREADS, 0, st, a, r, lanes);
+    r = roles_of(a, lanes_of(a.head_dim, VEC), blocks);
+    const cudaError_t e = launch_dependent(k_head_norm_back<T, VEC, NU, INTER, DIM>, dim3(r.end[1]), THREADS, 0, st, a, r);
     if (e != cudaSuccess) return e;
   }
   if (!a.dq_gain && !a.dk_gain) return cudaSuccess;
   return launch_dependent(k_head_norm_gains, dim3((a.head_dim + 31) / 32, 2), 1024, 0, st, a.ws, r.end[0], r.end[1] - r.end[0], a.head_dim,
                           a.dq_gain, a.dk_gain);
 }
-template <typename T>
+template <typename T, bool INTER>
 cudaError_t launch_back_type(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   constexpr int VEC = 16 / sizeof(T);
-  if (wide(a, sizeof(T)))
-    return a.interleaved ? launch_back<T, VEC, 1, true>(a, num_sms, st) : launch_back<T, VEC, 1, false>(a, num_sms, st);
-  return a.interleaved ? launch_back<T, 1, 4, true>(a, num_sms, st) : launch_back<T, 1, 4, false>(a, num_sms, st);
+  if (!wide(a, sizeof(T))) return launch_back<T, 1, 4, INTER, 0>(a, num_sms, st);
+  return a.head_dim == 128 ? launch_back<T, VEC, 1, INTER, 128>(a, num_sms, st) : launch_back<T, VEC, 1, INTER, 0>(a, num_sms, st);
 }
 
 // ------------------------------------------------------------------ rows out of 4-bit pages
 // A thread a run of eight elements: a word and its group's scale in, 16 bytes out.  c s is exact.
-template <typename T>
+template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) k_read_4bit(const __grid_constant__ Read4Args a) {
-  const int D = a.head_dim, runs = D / 8, at_once = THREADS / runs, run = threadIdx.x % runs, h0 = threadIdx.x / runs;
+  constexpr int runs = D / 8, at_once = THREADS / runs;
+  const int run = threadIdx.x % runs, h0 = threadIdx.x / runs;
   const int page_bits = __ffs(a.page) - 1;
   const int64_t page_bytes = pages4::page_bytes(a.page, D);
   pdl_wait();
   pdl_trigger();
-  for (int t = blockIdx.x; static_cast<uint32_t>(t) < static_cast<uint32_t>(a.n_rows); t = static_cast<int>(t + gridDim.x)) {
-    const int64_t slot = a.slots[t];
-    if (slot < 0) continue;
-    if (slot >= a.n_slots) {
-      set_status(a.status, DOPR_ERR_INVALID_ARG);
-      continue;
+  // ROWS rows at once: their slots, then all their words and scales, then what these stand for
+  constexpr int ROWS = 4;
+  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * ROWS; t0 < a.n_rows; t0 += static_cast<int64_t>(gridDim.x) * ROWS) {
+    int64_t slot[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      slot[i] = t0 + i < a.n_rows ? a.slots[t0 + i] : -1;
+      if (slot[i] >= a.n_slots) {
+        set_status(a.status, DOPR_ERR_INVALID_ARG);
+        slot[i] = -1;
+      }
     }
-    const int row = static_cast<int>(slot) & (a.page - 1);
-    const int64_t base = (slot >> page_bits) * a.n_kv_heads * page_bytes;
-    const uint8_t *k = a.k_pool + base, *v = a.v_pool + base;
-    const int code = row * (D / 2) + 4 * run, scale = a.page * (D / 2) + row * (D / 32) + run / 4;
-    T *ko = static_cast<T*>(a.k.out) + t * a.k.out_tok + 8 * run, *vo = static_cast<T*>(a.v.out) + t * a.v.out_tok + 8 * run;
     for (int h = h0; h < a.n_kv_heads; h += at_once) {
-      const int64_t at = h * page_bytes;
-      // a key's and a value's at once
-      const uint32_t word[2] = {*reinterpret_cast<const uint32_t*>(k + at + code), *reinterpret_cast<const uint32_t*>(v + at + code)};
-      const uint32_t byte[2] = {k[at + scale], v[at + scale]};
+      uint32_t word[ROWS][2], byte[ROWS][2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        uint32_t x[4];
-        const pages4::Widen<T> widen(byte[i] * 0x10001u);
-        widen(word[i], x);
-        if constexpr (std::is_same_v<T, __half>) {
+      for (int i = 0; i < ROWS; ++i) {
+        if (slot[i] < 0) continue;
+        const int row = static_cast<int>(slot[i]) & (a.page - 1);
+        const int64_t at = ((slot[i] >> page_bits) * a.n_kv_heads + h) * page_bytes;
+        const int code = row * (D / 2) + 4 * run, scale = a.page * (D / 2) + row * (D / 32) + run / 4;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const __half2 y = __hmul2(reinterpret_cast<const __half2&>(x[j]), __float2half2_rn(pages4::Widen<T>::UNIT));
-            x[j] = reinterpret_cast<const uint32_t&>(y);
-          }
+        for (int k = 0; k < 2; ++k) {
+          const uint8_t* p = (k ? a.v_pool : a.k_pool) + at;
+          word[i][k] = *reinterpret_cast<const uint32_t*>(p + code);
+          byte[i][k] = p[scale];
         }
-        if (byte[i] > pages4::SCALE_LAST) x[0] = x[1] = x[2] = x[3] = 0x7fff7fffu;  // NaN
-        *reinterpret_cast<uint4*>((i ? vo + h * a.v.out_head : ko + h * a.k.out_head)) = uint4{x[0], x[1], x[2], x[3]};
+      }
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        if (slot[i] < 0) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          uint32_t x[4];
+          const pages4::Widen<T> widen(byte[i][k] * 0x10001u);
+          widen(word[i][k], x);
+          if constexpr (std::is_same_v<T, __half>) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __half2 y = __hmul2(reinterpret_cast<const __half2&>(x[j]), __float2half2_rn(pages4::Widen<T>::UNIT));
+              x[j] = reinterpret_cast<const uint32_t&>(y);
+            }
+          }
+          if (byte[i][k] > pages4::SCALE_LAST) x[0] = x[1] = x[2] = x[3] = 0x7fff7fffu;  // NaN
+          const RopeView& out = k ? a.v : a.k;
+          *reinterpret_cast<uint4*>(static_cast<T*>(out.out) + (t0 + i) * out.out_tok + h * out.out_head + 8 * run) = uint4{x[0], x[1], x[2], x[3]};
+        }
       }
     }
   }
@@ -607,32 +834,40 @@ __global__ void __launch_bounds__(THREADS) k_read_4bit(const __grid_constant__ R
 cudaError_t launch_head_norm(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   if (a.n_tokens == 0) return cudaSuccess;
   switch (dtype) {
-    case DOPR_F16: return launch_type<__half>(a, num_sms, st);
-    case DOPR_BF16: return launch_type<__nv_bfloat16>(a, num_sms, st);
-    default: return launch_type<float>(a, num_sms, st);
+    case DOPR_F16: return a.interleaved ? launch_type<__half, true>(a, num_sms, st) : launch_type<__half, false>(a, num_sms, st);
+    case DOPR_BF16: return a.interleaved ? launch_type<__nv_bfloat16, true>(a, num_sms, st) : launch_type<__nv_bfloat16, false>(a, num_sms, st);
+    default: return a.interleaved ? launch_type<float, true>(a, num_sms, st) : launch_type<float, false>(a, num_sms, st);
   }
 }
 
 cudaError_t launch_head_norm_backward(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   switch (dtype) {
-    case DOPR_F16: return launch_back_type<__half>(a, num_sms, st);
-    case DOPR_BF16: return launch_back_type<__nv_bfloat16>(a, num_sms, st);
-    default: return launch_back_type<float>(a, num_sms, st);
+    case DOPR_F16: return a.interleaved ? launch_back_type<__half, true>(a, num_sms, st) : launch_back_type<__half, false>(a, num_sms, st);
+    case DOPR_BF16: return a.interleaved ? launch_back_type<__nv_bfloat16, true>(a, num_sms, st) : launch_back_type<__nv_bfloat16, false>(a, num_sms, st);
+    default: return a.interleaved ? launch_back_type<float, true>(a, num_sms, st) : launch_back_type<float, false>(a, num_sms, st);
   }
 }
 
 cudaError_t launch_append_4bit(int dtype, const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   if (a.n_tokens == 0) return cudaSuccess;
-  if (dtype == DOPR_F16)
-    return a.interleaved ? launch<__half, 8, 1, true, true>(a, num_sms, st) : launch<__half, 8, 1, false, true>(a, num_sms, st);
-  return a.interleaved ? launch<__nv_bfloat16, 8, 1, true, true>(a, num_sms, st) : launch<__nv_bfloat16, 8, 1, false, true>(a, num_sms, st);
+  const bool half = dtype == DOPR_F16;
+  if (a.eps == 0.f && a.rotary == 0) {  // rows as they are, and no q
+    if (a.head_dim == 128) return half ? launch_append<__half, 128>(a, num_sms, st) : launch_append<__nv_bfloat16, 128>(a, num_sms, st);
+    return half ? launch_append<__half, 64>(a, num_sms, st) : launch_append<__nv_bfloat16, 64>(a, num_sms, st);
+  }
+  if (a.interleaved) return half ? launch_pages<__half, true>(a, num_sms, st) : launch_pages<__nv_bfloat16, true>(a, num_sms, st);
+  return half ? launch_pages<__half, false>(a, num_sms, st) : launch_pages<__nv_bfloat16, false>(a, num_sms, st);
 }
 
 cudaError_t launch_read_4bit(int dtype, const Read4Args& a, int num_sms, cudaStream_t st) {
   if (a.n_rows == 0) return cudaSuccess;
-  const dim3 grid(a.n_rows < 65536 ? a.n_rows : 65536);
-  return dtype == DOPR_F16 ? launch_dependent(k_read_4bit<__half>, grid, THREADS, 0, st, a)
-                           : launch_dependent(k_read_4bit<__nv_bfloat16>, grid, THREADS, 0, st, a);
+  const int blocks = a.n_rows / 4 + 1;
+  const dim3 grid(blocks < 16 * num_sms ? blocks : 16 * num_sms);
+  if (a.head_dim == 128)
+    return dtype == DOPR_F16 ? launch_dependent(k_read_4bit<__half, 128>, grid, THREADS, 0, st, a)
+                             : launch_dependent(k_read_4bit<__nv_bfloat16, 128>, grid, THREADS, 0, st, a);
+  return dtype == DOPR_F16 ? launch_dependent(k_read_4bit<__half, 64>, grid, THREADS, 0, st, a)
+                           : launch_dependent(k_read_4bit<__nv_bfloat16, 64>, grid, THREADS, 0, st, a);
 }
 
 }  // namespace dopr

@@ -46,9 +46,11 @@ struct Smem {
   static constexpr int OFF_KEYS = OFF_ML + 128 * 8;     // of each page of a V stage (4 bits: of each piece of a half): rows that hold keys
   static constexpr int OFF_BAR = OFF_KEYS + 64;
   // few items: from 0 on, pieces of 16 columns of K and V, F_STAGES of them a warp
-  static constexpr int F_STAGES = FOUR ? (D == 128 ? 8 : 16) : D == 128 ? 3 : 6;
+  static constexpr int F_STAGES = FOUR ? (D == 128 ? 8 : 12) : D == 128 ? 3 : 6;
   static constexpr int F_BYTES = FOUR ? 2 * PIECE * (D / 2 + D / 32) : 2 * HALVES * PIECE * 128;
-  static_assert(WORKERS * F_STAGES * F_BYTES <= OFF_ROW, "the few items' pieces");
+  static constexpr int F_SCALES = WORKERS * F_STAGES * F_BYTES;  // 4 bits: what each warp takes of 32 keys' scales
+  static constexpr int F_SCALE_BYTES = FOUR ? 32 * (D / 32) * (4 + 2) : 0;
+  static_assert(F_SCALES + WORKERS * F_SCALE_BYTES <= OFF_ROW, "the few items' pieces");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
                        O_FULL = P_FULL + 4, ML_FULL = O_FULL + 2, ML_EMPTY = ML_FULL + 1, DRAIN = ML_EMPTY + 1, RAW_FULL = DRAIN + 1,
@@ -590,6 +592,42 @@ __device__ __forceinline__ void few_items(const SharedAttnArgs& a, const Plan& p
 template <typename T, bool FOUR>
 constexpr float HELD_UNIT = FOUR ? pages4::Widen<T>::UNIT : 1.f;
 
+// Shared memory by its own addresses: what comes from a pointer made of a number is read and written as memory of any kind, with
+// addresses of 64 bits (64 conversations so: 139 us).
+__device__ __forceinline__ uint32_t lds32(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t at) {
+  uint16_t x;
+  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t at) {
+  uint32_t x;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(x) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 x;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t at) {
+  uint2 x;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(at));
+  return x;
+}
+__device__ __forceinline__ void sts16(uint32_t at, uint32_t x) {
+  asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(x)) : "memory");
+}
+__device__ __forceinline__ void sts64(uint32_t at, uint2 x) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x.x), "r"(x.y) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t at, uint4 x) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
 // n bytes of 16, zeros for the others.
 __device__ __forceinline__ void cp_async16_part(uint32_t dst, const void* src, int n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -599,98 +637,71 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "r"(bar)
                : "memory");
 }
+// D (16 x 8, 32-bit) = A (16 x 16) B (16 x 8) + C of fp16 by a warp.
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
+                                             float c1, float c2, float c3) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
+__device__ __forceinline__ void mma_f16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An 8 x 8 of 16-bit elements, row lane / 4 and columns 2 (lane % 4) and the next a lane, the other way round.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<const __half2&>(x); }
+__device__ __forceinline__ uint32_t as_bits(__half2 x) { return reinterpret_cast<const uint32_t&>(x); }
+// The four pairs of nibbles at 4 k and 16 + 4 k as fp16 numbers of the lowest bits: n 2^-24 for k = 0 and 2, 16 n 2^-24 for 1 and 3.
+__device__ __forceinline__ void as_subnormals(uint32_t w, uint32_t (&x)[4]) {
+  x[0] = w & 0x000f000fu, x[1] = w & 0x00f000f0u;
+  w >>= 8;
+  x[2] = w & 0x000f000fu, x[3] = w & 0x00f000f0u;
+}
+// The largest of a word's bytes.
+__device__ __forceinline__ uint32_t max_byte(uint32_t w) {
+  const uint32_t t = __vmaxu2(w & 0x00ff00ffu, w >> 8 & 0x00ff00ffu);
+  return max(t & 0xffffu, t >> 16);
+}
+
 // A scale's byte; one that stands for NaN counts as zero and is noted.
 __device__ __forceinline__ uint32_t scale_of(uint32_t byte, bool& bad) {
   bad |= byte > pages4::SCALE_LAST;
   return byte > pages4::SCALE_LAST ? 0u : byte;
 }
 
-// As few_items.  Of a piece a thread widens, in registers, what is its own of the products' operands: of K the 32 (head size 64: 16)
-// elements t of a key, in any order, as long as Q's are in the same; of V the pairs of two tokens' elements that two words hold.
-// Keys stand in the products' columns so that rows which lanes read at once lie in different banks: column n of eight is key n / 2,
-// of the odd ones 4 + (n / 2 ^ 1).  Scales of rows past the run's keys come as zeros, so such rows are zeros.
-template <typename T, int D>
-__device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, const uint8_t* smem, uint32_t s0, int wi, int2 work,
-                                               int lane) {
-  using L = Smem<D, true>;
-  constexpr int ROW = D / 2, SROW = D / 32, CODES = PIECE * ROW, SCALES = PIECE * SROW, STAGE = L::F_BYTES, WORDS = D / 32;
-  constexpr int CHUNKS = ROW / 16, SCALE_CHUNKS = SCALES / 16;
-  const uint32_t base = s0 + wi * L::F_STAGES * STAGE;
-  const uint8_t* pieces = smem + wi * L::F_STAGES * STAGE;
-  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
-  const int64_t page_bytes = pages4::page_bytes(page, D);
-  const float scale_log2 = a.scale * 1.4426950408889634f * HELD_UNIT<T, true>;
-  const int quad = lane >> 2, in_quad = lane & 3;
-  bool bad = false;
-  // copies run ahead of the products, over the ends of segments too
-  Walk copies(plan, work);
-  Segment c;
-  bool more = copies.next(c);
-  uint32_t next = more ? c.b0 : 0;
-  int stage = 0, ahead = 0;      // of the piece at hand, of the next one to be copied
-  int page_at = 0, key_at = 0;   // where the next 32 pieces lie: a lane a piece; its first row in the page, and 256 times its keys
-  auto find = [&](uint32_t b) {
-    if (b >= c.b1) return;
-    PageCursor cur(plan, c);
-    cur.go(b);
-    const Run& run = cur.run;
-    const int key = (static_cast<int>(b) - run.off) * PIECE;
-    int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
-    if (block < 0 || block >= a.lay.n_blocks) {
-      if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
-      block = 0;
-    }
-    page_at = block * Hkv + c.h;
-    key_at = key % page + 256 * min(PIECE, run.keys - key);
-  };
-  auto copy = [&] {
-    if (more && next == c.b1) {
-      more = copies.next(c);
-      next = c.b0;
-    }
-    if (more) {
-      const int at = (next - c.b0) & 31;
-      if (at == 0) find(next + lane);
-      const int64_t from = __shfl_sync(0xffffffffu, page_at, at) * page_bytes;
-      const int key = __shfl_sync(0xffffffffu, key_at, at), first = key & 255, valid = key >> 8;
-      const uint8_t *k = static_cast<const uint8_t*>(a.k_pool) + from, *v = static_cast<const uint8_t*>(a.v_pool) + from;
-      const uint32_t dst = base + ahead * STAGE;
-#pragma unroll
-      for (int i = 0; i < CODES / 512; ++i) {
-        const int x = lane + 32 * i, r = x / CHUNKS;
-        const uint32_t to = dst + r * ROW + (((x % CHUNKS) ^ (D == 128 ? r & 2 : 0)) << 4);
-        cp_async16(to, k + first * ROW + 16 * x, true);
-        cp_async16(to + CODES, v + first * ROW + 16 * x, true);
-      }
-      if (lane < 2 * SCALE_CHUNKS) {
-        const int x = lane % SCALE_CHUNKS;
-        cp_async16_part(dst + 2 * CODES + 16 * lane, (lane < SCALE_CHUNKS ? k : v) + page * ROW + first * SROW + 16 * x,
-                        min(16, max(0, valid * SROW - 16 * x)));
-      }
-      ++next;
-    }
-    cp_async_commit();
-    ahead = ahead + 1 == L::F_STAGES ? 0 : ahead + 1;
-  };
-#pragma unroll 1
-  for (int i = 0; i + 1 < L::F_STAGES; ++i) copy();
+// Where in a row of a piece its 16 bytes lie that are its c-th: at c ^ chunk_place, so that rows which lanes read at once lie in different banks.
+template <int D>
+__device__ __forceinline__ int chunk_place(int row) {
+  return D == 128 ? (row & 2) | (row >> 2 & 1) : row >> 2 & 1;
+}
 
-  const int key_col[2] = {in_quad, 4 + (in_quad ^ 1)};                         // the keys, of eight, of this thread's columns of scores
-  const int key_row = quad & 1 ? 4 + ((quad >> 1) ^ 1) : quad >> 1;            // the key that it widens
-  Walk walk(plan, work);
-  Segment s;
-  while (walk.next(s)) {
-    const int rows = s.n_tok * G;
-    uint32_t q[D / 16][4];
-    int own0[2], own1[2];
+// Up to 16 rows of a segment of few items by a warp, the rows on the products' long side: codes are widened in registers.  Of K a thread
+// widens a key's elements from D / 4 t on, of Q it has the same ones; of V it widens the elements from D / 8 g on of four keys.
+template <typename T, int D>
+struct Few16 {
+  static constexpr int ROW = D / 2, SROW = D / 32, CODES = PIECE * ROW, SCALES = PIECE * SROW, WORDS = D / 32, NT = D / 8;
+  uint32_t q[D / 16][4];
+  int own0[2], own1[2];
+  float o[NT][4], m[2], l[2], scale_log2;
+
+  __device__ __forceinline__ Few16(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int rows, int G, int lane) {
+    const int quad = lane >> 2, in_quad = lane & 3;
+    scale_log2 = a.scale * 1.4426950408889634f * HELD_UNIT<T, true>;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = quad + 8 * i;
       const bool valid = r < rows;
-      const int o = s.tok + (valid ? r / G : 0);
-      const int2 own = plan.own[o];
+      const int at = s.tok + (valid ? r / G : 0);
+      const int2 own = plan.own[at];
       own0[i] = valid ? own.x : 0, own1[i] = valid ? own.y : 0;
-      const uint2* src = reinterpret_cast<const uint2*>(static_cast<const T*>(a.q) + plan.order[o] * a.q_tok +
+      const uint2* src = reinterpret_cast<const uint2*>(static_cast<const T*>(a.q) + plan.order[at] * a.q_tok +
                                                         static_cast<int64_t>(s.h * G + (valid ? r % G : 0)) * a.q_head + in_quad * (D / 4));
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
@@ -698,92 +709,102 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
         q[k][i] = x.x;
         q[k][2 + i] = x.y;
       }
+      m[i] = -INFINITY, l[i] = 0.f;
     }
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    for (uint32_t b = s.b0; b < s.b1; ++b) {
-      copy();
-      asm volatile("cp.async.wait_group %0;" ::"n"(L::F_STAGES - 1) : "memory");
-      __syncwarp();
-      const uint8_t *kc = pieces + stage * STAGE, *vc = kc + CODES, *ks = kc + 2 * CODES, *vs = ks + SCALES;
-      const int col0 = b * PIECE;
-      float sc[2][4];
+    for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  }
+
+  // A piece of 16 keys, of which the first is column col0.
+  __device__ __forceinline__ void step(uint32_t piece, int prefix_keys, int col0, bool& bad, int lane) {
+    const int quad = lane >> 2, in_quad = lane & 3;
+    const int key_col[2] = {in_quad, 4 + (in_quad ^ 1)};               // the keys, of eight, of this thread's columns of scores
+    const int key_row = quad & 1 ? 4 + ((quad >> 1) ^ 1) : quad >> 1;  // the key that it widens
+    float sc[2][4];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+      const int row = 8 * t + key_row;
+      const uint32_t at = piece + row * ROW;
+      uint32_t w[WORDS];
+      if constexpr (D == 128) {
+        const uint4 x = lds128(at + ((in_quad ^ chunk_place<D>(row)) << 4));
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+      } else {
+        const uint2 x = lds64(at + (((in_quad >> 1) ^ chunk_place<D>(row)) << 4) + 8 * (in_quad & 1));
+        w[0] = x.x, w[1] = x.y;
+      }
+      const pages4::Widen<T> widen(scale_of(lds8(piece + 2 * CODES + row * SROW + in_quad * SROW / 4), bad) * 0x10001u);
+#pragma unroll
+      for (int j = 0; j < WORDS; ++j) {
+        uint32_t x[4];
+        widen(w[j], x);
+        mma16<T>(sc[t], q[2 * j], x[0], x[1]);
+        mma16<T>(sc[t], q[2 * j + 1], x[2], x[3]);
+      }
+    }
+    if (prefix_keys < col0 + PIECE) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = col0 + 8 * t + key_col[e & 1], i = e >> 1;
+          if (!(at < prefix_keys || (at >= own0[i] && at < own1[i]))) sc[t][e] = -INFINITY;
+        }
+    }
+    uint32_t p[4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2 - BELOW<T>;
+      if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
+      const bool grow = top > m[i] + RESCALE<T>;
+      if (__any_sync(0xffffffffu, grow)) {
+        const float by = grow ? ex2(m[i] - top) : 1.f;
+        if (grow) m[i] = top;
+        l[i] *= by;
+#pragma unroll
+        for (int d = 0; d < NT; ++d) o[d][2 * i] *= by, o[d][2 * i + 1] *= by;
+      }
+      const float at_m = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
-        const int row = 8 * t + key_row;
-        uint32_t w[WORDS];
-        if constexpr (D == 128) *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(kc + row * ROW + ((in_quad ^ (row & 2)) << 4));
-        else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(kc + row * ROW + 8 * in_quad);
-        const pages4::Widen<T> widen(scale_of(ks[row * SROW + in_quad * SROW / 4], bad) * 0x10001u);
-#pragma unroll
-        for (int j = 0; j < WORDS; ++j) {
-          uint32_t x[4];
-          widen(w[j], x);
-          mma16<T>(sc[t], q[2 * j], x[0], x[1]);
-          mma16<T>(sc[t], q[2 * j + 1], x[2], x[3]);
-        }
+        const float x = ex2(fmaf(sc[t][2 * i], scale_log2, -at_m)), y = ex2(fmaf(sc[t][2 * i + 1], scale_log2, -at_m));
+        l[i] += x + y;  // this thread's columns: the quad's four sums are added up at the end
+        p[2 * t + i] = pack2<T>(x, y);
       }
-      if (s.prefix_keys < col0 + PIECE) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int at = col0 + 8 * t + key_col[e & 1], i = e >> 1;
-            if (!(at < s.prefix_keys || (at >= own0[i] && at < own1[i]))) sc[t][e] = -INFINITY;
-          }
-      }
-      uint32_t p[4];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float top = fmaxf(fmaxf(sc[0][2 * i], sc[0][2 * i + 1]), fmaxf(sc[1][2 * i], sc[1][2 * i + 1]));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2)) * scale_log2 - BELOW<T>;
-        if (m[i] == -INFINITY) m[i] = top;  // nothing but zeros has been summed
-        const bool grow = top > m[i] + RESCALE<T>;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float by = grow ? ex2(m[i] - top) : 1.f;
-          if (grow) m[i] = top;
-          l[i] *= by;
-#pragma unroll
-          for (int d = 0; d < D / 8; ++d) o[d][2 * i] *= by, o[d][2 * i + 1] *= by;
-        }
-        const float at_m = m[i] == -INFINITY ? 0.f : m[i];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float x = ex2(fmaf(sc[t][2 * i], scale_log2, -at_m)), y = ex2(fmaf(sc[t][2 * i + 1], scale_log2, -at_m));
-          l[i] += x + y;  // this thread's columns: the quad's four sums are added up at the end
-          p[2 * t + i] = pack2<T>(x, y);
-        }
-      }
-      // V: tokens of the columns 2 t, 2 t + 1 (a, b) and 2 t + 8, 2 t + 9 (c, d); elements from D / 8 * quad on
-      uint32_t w[4][(WORDS + 1) / 2], by[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 8 * (i >> 1) + key_col[i & 1];
-        if constexpr (D == 128)
-          *reinterpret_cast<uint2*>(w[i]) = *reinterpret_cast<const uint2*>(vc + row * ROW + (((quad >> 1) ^ (row & 2)) << 4) + 8 * (quad & 1));
-        else
-          w[i][0] = *reinterpret_cast<const uint32_t*>(vc + row * ROW + 4 * quad);
-        by[i] = scale_of(vs[row * SROW + quad * SROW / 8], bad);
-      }
-      const pages4::Widen<T> ab(by[0] | by[1] << 16), cd(by[2] | by[3] << 16);
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-        for (int odd = 0; odd < 2; ++odd) {
-          uint32_t x[4], y[4];
-          ab(__byte_perm(w[0][j], w[1][j], odd ? 0x7632 : 0x5410), x);
-          cd(__byte_perm(w[2][j], w[3][j], odd ? 0x7632 : 0x5410), y);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mma16<T>(o[8 * j + 2 * k + odd], p, x[k], y[k]);
-        }
-      __syncwarp();  // every lane has read the stage
-      if (++stage == L::F_STAGES) stage = 0;
     }
-    // column n of the product d of O is element D / 8 * n + d: a thread has D / 4 elements that follow one another of each row
-    constexpr int NT = D / 8;
+    // V: tokens of the columns 2 t, 2 t + 1 (a, b) and 2 t + 8, 2 t + 9 (c, d)
+    uint32_t w[4][(WORDS + 1) / 2], by[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * (i >> 1) + key_col[i & 1];
+      const uint32_t at = piece + CODES + row * ROW;
+      if constexpr (D == 128) {
+        const uint2 x = lds64(at + (((quad >> 1) ^ chunk_place<D>(row)) << 4) + 8 * (quad & 1));
+        w[i][0] = x.x, w[i][1] = x.y;
+      } else {
+        w[i][0] = lds32(at + (((quad >> 2) ^ chunk_place<D>(row)) << 4) + 4 * (quad & 3));
+      }
+      by[i] = scale_of(lds8(piece + 2 * CODES + SCALES + row * SROW + quad * SROW / 8), bad);
+    }
+    const pages4::Widen<T> ab(by[0] | by[1] << 16), cd(by[2] | by[3] << 16);
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j)
+#pragma unroll
+      for (int odd = 0; odd < 2; ++odd) {
+        uint32_t x[4], y[4];
+        ab(__byte_perm(w[0][j], w[1][j], odd ? 0x7632 : 0x5410), x);
+        cd(__byte_perm(w[2][j], w[3][j], odd ? 0x7632 : 0x5410), y);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma16<T>(o[8 * j + 2 * k + odd], p, x[k], y[k]);
+      }
+  }
+
+  // Rows out: column n of the product d of O is element D / 8 * n + d, so a thread has D / 4 elements that follow one another of each row.
+  __device__ __forceinline__ void finish(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int rows, int G, int lane) {
+    const int quad = lane >> 2, in_quad = lane & 3;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = quad + 8 * i;
@@ -805,7 +826,7 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
         if (a.lse && in_quad == 0) a.lse[static_cast<int64_t>(t) * a.Hq + h] = lse_of(m[i], sum);
       } else if (r < rows) {
         float2* ml = reinterpret_cast<float2*>(a.ws);
-        float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, Hkv, G, a.max_tokens, gridDim.x));
+        float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, a.lay.n_kv_heads, G, a.max_tokens, gridDim.x));
         const int64_t row = static_cast<int64_t>(s.part_row) + r;
         if (in_quad == 0) ml[row] = make_float2(m[i], sum);
         if (sum != 0.f) {
@@ -819,6 +840,480 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
         }
       }
     }
+  }
+};
+
+// Up to 8 rows of a segment of few items, from row0 on, by a warp.  Thread (g, t) = (lane / 4, lane % 4) has scores of the keys g and g + 8 of a piece
+// with rows 2 t and 2 t + 1, as the products leave them, and of O the elements that its words of V hold.
+template <typename T, int D>
+struct Few8 {
+  static constexpr int GROUPS = D / 32, ROW = D / 2, SROW = D / 32, CODES = PIECE * ROW, SCALES = PIECE * SROW;
+  uint32_t q[GROUPS][4];           // row g: 8 elements from 8 t on of each group; the second and fourth pair 1 / 16
+  float start[GROUPS][4];          // -8 2^-24 times Q's sum over the group, rows 2 t and 2 t + 1, twice: as a product's sum begins
+  float unit[2];                   // what their scores are multiplied by
+  int own0[2], own1[2];
+  int all0, all1;                  // own columns that all rows see
+  float o[GROUPS][2][4], ones[GROUPS][4];
+  float m[2], l[2];
+  int top_scale;                   // the largest exponent of V's scales so far: they are taken times 2^(14 - top_scale)
+
+  __device__ __forceinline__ Few8(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int row0, int rows, int G, int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    const bool valid = g < rows;
+    const int token = plan.order[s.tok + (row0 + (valid ? g : 0)) / G];
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const T*>(a.q) + token * a.q_tok +
+                                                      static_cast<int64_t>(s.h * G + (row0 + (valid ? g : 0)) % G) * a.q_head) + t;
+    float x[GROUPS][8], most = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const uint4 w = valid ? src[4 * i] : uint4{0, 0, 0, 0};
+      const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 f = unpack2<T>(v[k]);
+        x[i][2 * k] = f.x, x[i][2 * k + 1] = f.y;
+        most = fmaxf(most, fmaxf(fabsf(f.x), fabsf(f.y)));
+      }
+    }
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    // the row's largest to 2^13 and above: what is rounded then lies 2^-35 below it
+    const int e = most > 0.f ? min(100, 13 + 127 - static_cast<int>(__float_as_uint(most) >> 23)) : 0;
+    const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
+    float sum[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      sum[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float by = k & 1 ? up / 16.f : up;
+        q[i][k] = pack_f16x2(x[i][2 * k] * by, x[i][2 * k + 1] * by);
+        const float2 f = __half22float2(as_half2(q[i][k]));
+        sum[i] += (f.x + f.y) * (k & 1 ? 16.f : 1.f);
+      }
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
+      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
+    }
+    const float scale = a.scale * 1.4426950408889634f * 0x1p12f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = 2 * t + j;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) start[i][j] = start[i][2 + j] = -8.f * 0x1p-24f * __shfl_sync(0xffffffffu, sum[i], 4 * row);
+      unit[j] = scale * __shfl_sync(0xffffffffu, down, 4 * row);
+      const int2 own = plan.own[s.tok + (row0 + (row < rows ? row : 0)) / G];
+      own0[j] = row < rows ? own.x : 0, own1[j] = row < rows ? own.y : 0;
+      m[j] = -INFINITY, l[j] = 0.f;
+    }
+    all0 = __reduce_max_sync(0xffffffffu, max(2 * t < rows ? own0[0] : 0, 2 * t + 1 < rows ? own0[1] : 0));
+    all1 = __reduce_min_sync(0xffffffffu, min(2 * t < rows ? own1[0] : INT_MAX, 2 * t + 1 < rows ? own1[1] : INT_MAX));
+    top_scale = 0;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[i][0][k] = o[i][1][k] = ones[i][k] = 0.f;
+  }
+
+  // Two pieces of 16 keys, of which the first is column col0; the second's address is the first's where there is one only.
+  __device__ __forceinline__ void step(const uint32_t (&piece)[2], uint32_t scales, int prefix_keys, int col0, bool& bad, int lane) {
+    constexpr int N = 2;
+    const bool two = piece[1] != piece[0];
+    const int g = lane >> 2, t = lane & 3;
+    // each lane looks at a key's scales: bytes that stand for NaN become zeros; the largest of V's; and what the products take, a key's
+    // four of K in 32 bits, and V's in fp16 by groups
+    {
+      const uint32_t ks = (lane < 16 ? piece[0] : piece[1]) + 2 * CODES + (lane & 15) * SROW;
+      uint32_t kw, vw;
+      if constexpr (D == 128) kw = lds32(ks), vw = lds32(ks + SCALES);
+      else kw = lds16(ks), vw = lds16(ks + SCALES);
+      if (lane >= 16 && !two) kw = vw = 0;
+      uint32_t most = max_byte(vw);
+      const bool odd = max(most, max_byte(kw)) > pages4::SCALE_LAST;
+      if (__any_sync(0xffffffffu, odd)) {
+        bad |= odd;
+#pragma unroll
+        for (int i = 0; i < SROW; ++i) {
+          if ((kw >> 8 * i & 0xffu) > pages4::SCALE_LAST) kw &= ~(0xffu << 8 * i);
+          if ((vw >> 8 * i & 0xffu) > pages4::SCALE_LAST) vw &= ~(0xffu << 8 * i);
+        }
+        most = max_byte(vw);
+      }
+      const int top = static_cast<int>(__reduce_max_sync(0xffffffffu, most)) >> 3;
+      if (top > top_scale) {
+        const float by = __uint_as_float(static_cast<uint32_t>(127 + top_scale - top) << 23);
+        top_scale = top;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            o[i][0][k] *= by, o[i][1][k] *= by, ones[i][k] *= by;
+          }
+      }
+      // a byte's exponent is 112 below as a 32-bit number's; and 2^24 of the codes, less 2^12 that are in `unit`
+      float f[GROUPS];
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p124f;
+      const __half2 norm = as_half2(static_cast<uint32_t>(29 - top_scale) << 10 | static_cast<uint32_t>(29 - top_scale) << 26);
+      const uint32_t even = as_bits(__hmul2(as_half2(vw << 7 & 0x7f807f80u), norm)), uneven = as_bits(__hmul2(as_half2(vw >> 1 & 0x7f807f80u), norm));
+      const uint32_t ks32 = scales + lane * (GROUPS * 4), vs16 = scales + 32 * GROUPS * 4 + 2 * lane;
+      if constexpr (GROUPS == 4) sts128(ks32, uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+      else sts64(ks32, uint2{__float_as_uint(f[0]), __float_as_uint(f[1])});
+      sts16(vs16, even), sts16(vs16 + 64, uneven);
+      if constexpr (GROUPS == 4) sts16(vs16 + 128, even >> 16), sts16(vs16 + 192, uneven >> 16);
+      __syncwarp();
+    }
+    float sc[N][4];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int place = chunk_place<D>(g);
+      const uint32_t kc = piece[n] + g * ROW + 4 * t, ks = scales + (16 * n + g) * (GROUPS * 4);
+      float f0[GROUPS], f1[GROUPS];  // scales of the keys g and g + 8
+      if constexpr (GROUPS == 4) {
+        const uint4 u = lds128(ks), v = lds128(ks + 8 * GROUPS * 4);
+        f0[0] = __uint_as_float(u.x), f0[1] = __uint_as_float(u.y), f0[2] = __uint_as_float(u.z), f0[3] = __uint_as_float(u.w);
+        f1[0] = __uint_as_float(v.x), f1[1] = __uint_as_float(v.y), f1[2] = __uint_as_float(v.z), f1[3] = __uint_as_float(v.w);
+      } else {
+        const uint2 u = lds64(ks), v = lds64(ks + 8 * GROUPS * 4);
+        f0[0] = __uint_as_float(u.x), f0[1] = __uint_as_float(u.y);
+        f1[0] = __uint_as_float(v.x), f1[1] = __uint_as_float(v.y);
+      }
+      sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+        uint32_t x[4], y[4];
+        as_subnormals(lds32(kc + ((i ^ place) << 4)), x);
+        as_subnormals(lds32(kc + ((i ^ place) << 4) + 8 * ROW), y);
+        float d[4];
+        mma_f16_from(d, x[0], y[0], x[1], y[1], q[i][0], q[i][1], start[i][0], start[i][1], start[i][2], start[i][3]);
+        mma_f16_add(d, x[2], y[2], x[3], y[3], q[i][2], q[i][3]);
+        sc[n][0] = fmaf(d[0], f0[i], sc[n][0]), sc[n][1] = fmaf(d[1], f0[i], sc[n][1]);
+        sc[n][2] = fmaf(d[2], f1[i], sc[n][2]), sc[n][3] = fmaf(d[3], f1[i], sc[n][3]);
+      }
+    }
+    const int end = col0 + (two ? 2 : 1) * PIECE;
+    if (!two || (prefix_keys < end && (col0 < all0 || end > all1))) {
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int at = col0 + PIECE * n + g + 8 * (e >> 1), j = e & 1;
+          if (at >= end || !(at < prefix_keys || (at >= own0[j] && at < own1[j]))) sc[n][e] = -INFINITY;
+        }
+    }
+    // a row's keys are those of this thread and of the lanes with the same t
+    float top[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      top[j] = fmaxf(fmaxf(sc[0][j], sc[0][2 + j]), fmaxf(sc[1][j], sc[1][2 + j]));
+    }
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      top[0] = fmaxf(top[0], __shfl_xor_sync(0xffffffffu, top[0], d));
+      top[1] = fmaxf(top[1], __shfl_xor_sync(0xffffffffu, top[1], d));
+    }
+    bool grow[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      top[j] = top[j] * unit[j] - BELOW<__half>;
+      if (m[j] == -INFINITY) m[j] = top[j];  // nothing but zeros has been summed
+      grow[j] = top[j] > m[j] + RESCALE<__half>;
+    }
+    if (__any_sync(0xffffffffu, grow[0] || grow[1])) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float by = grow[j] ? ex2(m[j] - top[j]) : 1.f;
+        if (grow[j]) m[j] = top[j];
+        l[j] *= by;
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+          o[i][0][j] *= by, o[i][0][2 + j] *= by, o[i][1][j] *= by, o[i][1][2 + j] *= by;
+          ones[i][j] *= by, ones[i][2 + j] *= by;
+        }
+      }
+    }
+    const float m0 = m[0] == -INFINITY ? 0.f : m[0], m1 = m[1] == -INFINITY ? 0.f : m[1];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float p0 = ex2(fmaf(sc[n][0], unit[0], -m0)), p1 = ex2(fmaf(sc[n][1], unit[1], -m1));
+      const float p2 = ex2(fmaf(sc[n][2], unit[0], -m0)), p3 = ex2(fmaf(sc[n][3], unit[1], -m1));
+      l[0] += p0 + p2, l[1] += p1 + p3;  // this thread's keys: the lanes' sums are added up at the end
+      // row g, keys 2 t and 2 t + 1, and 8 more
+      const __half2 pa = as_half2(transpose8(pack_f16x2(p0, p1))), pb = as_half2(transpose8(pack_f16x2(p2, p3)));
+      const uint32_t vc = piece[n] + CODES + 2 * t * ROW + 4 * (g >> 1);
+      const uint32_t vs = scales + 32 * GROUPS * 4 + 32 * n + 4 * t;  // two keys' of a group; 64 bytes a group
+      const int place = chunk_place<D>(2 * t);
+      const uint32_t half_word = g & 1 ? 0x7632u : 0x5410u;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i) {
+        const uint32_t ba = as_bits(__hmul2(pa, as_half2(lds32(vs + 64 * i)))), bb = as_bits(__hmul2(pb, as_half2(lds32(vs + 64 * i + 16))));
+        const uint32_t w = vc + ((i ^ place) << 4);
+        uint32_t x[4], y[4];
+        as_subnormals(__byte_perm(lds32(w), lds32(w + ROW), half_word), x);
+        as_subnormals(__byte_perm(lds32(w + 8 * ROW), lds32(w + 9 * ROW), half_word), y);
+        mma_f16_add(o[i][0], x[0], x[1], y[0], y[1], ba, bb);
+        mma_f16_add(o[i][1], x[2], x[3], y[2], y[3], ba, bb);
+        mma_f16_add(ones[i], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, ba, bb);  // 8 2^-24
+      }
+    }
+  }
+
+  // Rows out: of row 2 t + j thread (g, t) has elements 32 i + 8 (g / 2) + 2 k + g % 2; with its neighbour's it has 8 that follow one
+  // another, of row 2 t where g is even, else of 2 t + 1.
+  __device__ __forceinline__ void finish(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int row0, int rows, int G, int lane) {
+    const int g = lane >> 2, t = lane & 3, odd = g & 1, r = 2 * t + odd;
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      l[0] += __shfl_xor_sync(0xffffffffu, l[0], d);
+      l[1] += __shfl_xor_sync(0xffffffffu, l[1], d);
+    }
+    const float mm = odd ? m[1] : m[0], ll = odd ? l[1] : l[0];
+    const bool whole = s.flags & SEG_WHOLE;
+    float by = __uint_as_float(static_cast<uint32_t>(127 + 24 - 14 + top_scale) << 23);
+    if (whole) by = ll == 0.f ? 0.f : by * inverse(ll);
+    const int at = row0 + (r < rows ? r : 0), h = s.h * G + at % G, token = plan.order[s.tok + at / G];
+    float2* ml = reinterpret_cast<float2*>(a.ws);
+    const int64_t part = static_cast<int64_t>(s.part_row) + row0 + r;
+    float* part_o = reinterpret_cast<float*>(ml + max_part_rows(a.lay.n_seqs, a.lay.n_kv_heads, G, a.max_tokens, gridDim.x)) + part * D;
+    T* out = static_cast<T*>(a.out) + token * a.o_tok + h * a.o_head;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // O of code k: the second of each pair is 16 times what it is
+        const float(&x)[4] = o[i][k >> 1];
+        const float f = k & 1 ? 1.f / 16.f : 1.f;
+        const float e0 = fmaf(x[2 * (k & 1)], f, -ones[i][0]), e1 = fmaf(x[2 * (k & 1) + 1], f, -ones[i][1]);
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? e0 : e1, 4);
+        v[2 * k] = odd ? other : e0, v[2 * k + 1] = odd ? e1 : other;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] *= by;
+      const int d = 32 * i + 8 * (g >> 1);
+      if (r < rows) {
+        if (whole) {
+          *reinterpret_cast<uint4*>(out + d) = uint4{pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])};
+        } else if (ll != 0.f) {
+          *reinterpret_cast<float4*>(part_o + d) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4*>(part_o + d + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      }
+    }
+    if (r < rows && g < 2) {
+      if (!whole) ml[part] = make_float2(mm, ll);
+      else if (a.lse) a.lse[static_cast<int64_t>(token) * a.Hq + h] = lse_of(mm, ll);
+    }
+  }
+};
+
+// What a warp does at once of few items of the 4-bit cache: a segment, or where it has more than 8 rows and long runs, whose tokens alone
+// see them, a run of it.  Few8 takes 1.0 us a piece where Few16 takes 1.45 with eight warps at work, but its code beside Few16's no
+// longer stays in the instruction caches when jobs are short (a third of the warps' time then goes to waiting for instructions).  By
+// the pieces of a job from which Few8 takes it (runs: on average):
+//   runs       64 conversations of 2,000 to 6,000 keys   256 of 50 to 400, 4 and 8 rows a token   32 of 1,000 to 3,000, a row a token
+//     8                       111 us                                  75 and 76                                  52
+//    12                       113                                     61 and 66                                  53
+//    16                       118                                     48 and 51                                  56
+//    24                       126                                     47 and 50                                  55
+//    none                     162                                     50 and 51                                  58
+//   segments   one token of 32 heads on 8 over 32,768 keys   256 queries on 64 documents of 1 to 1,024 tokens, 16 heads on 8
+//     6                        33                                      56
+//    12                        35                                      53
+//    32                        40                                      51
+constexpr uint32_t LONG_RUN = 16, LONG_SEGMENT = 12;
+struct Job {
+  const Segment* s;
+  int row0, rows;
+  uint32_t from, to;  // pieces
+  bool eight;         // by Few8
+};
+struct Jobs {
+  const Plan& plan;
+  const Segment* s = nullptr;
+  int at, end, G, run = -1;
+  __device__ __forceinline__ Jobs(const Plan& p, int2 work, int G_) : plan(p), at(work.x), end(work.y), G(G_) {}
+  __device__ __forceinline__ bool apart() const {
+    const uint32_t n = s->b1 - s->b0, most = n / LONG_RUN;
+    if (most < 2) return false;
+    const Run* runs = plan.runs + s->run;
+    uint32_t of = 0;
+    for (int i0 = s->run_at; i0 < s->n_runs; i0 += 32) {  // a lane a run
+      const int i = i0 + static_cast<int>(threadIdx.x & 31u);
+      const bool in = i < s->n_runs && static_cast<uint32_t>(runs[i].off) < s->b1;
+      if (__any_sync(0xffffffffu, in && (runs[i].token < 0 || (runs[i].tok1 - runs[i].tok0) * G > 8))) return false;
+      of += __popc(__ballot_sync(0xffffffffu, in));
+    }
+    return of <= most;
+  }
+  // starts: the segment is a new one, and its runs are jobs of their own
+  __device__ __forceinline__ bool next(Job& j, bool& starts) {
+    starts = false;
+    for (;;) {
+      if (run >= 0) {
+        const Run* r = plan.runs + s->run + run;
+        if (run < s->n_runs && static_cast<uint32_t>(r->off) < s->b1) {
+          ++run;
+          j.from = max(s->b0, static_cast<uint32_t>(r->off)), j.to = min(s->b1, static_cast<uint32_t>(r->off + r->pages));
+          if (j.from >= j.to) continue;
+          j.row0 = r->tok0 * G, j.rows = (r->tok1 - r->tok0) * G;
+          return true;
+        }
+        run = -1;
+      }
+      if (at >= end) return false;
+      s = j.s = plan.segs + at++;
+      if (at < end) asm volatile("prefetch.global.L1 [%0];" ::"l"(plan.segs + at));
+      j.from = s->b0, j.to = s->b1;
+      j.row0 = 0, j.rows = s->n_tok * G;
+      j.eight = j.rows <= 8 && j.to - j.from >= LONG_SEGMENT;
+      if (j.rows <= 8 || !apart()) return true;
+      j.eight = true;
+      run = s->run_at;
+      starts = true;
+    }
+  }
+};
+
+// Results of rows of a segment whose runs are jobs of their own, but which have none in it.
+template <typename T, int D>
+__device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int G, int lane) {
+  const Run* runs = plan.runs + s.run;
+  uint32_t seen = 0;  // a bit a row; a lane a run
+  for (int i = s.run_at + lane; i < s.n_runs; i += 32) {
+    const Run run = runs[i];
+    const uint32_t off = run.off;
+    if (max(off, s.b0) < min(off + run.pages, s.b1)) seen |= (1u << run.tok1 * G) - (1u << run.tok0 * G);
+  }
+  seen = __reduce_or_sync(0xffffffffu, seen);
+  for (uint32_t none = ((1u << s.n_tok * G) - 1u) & ~seen; none != 0; none &= none - 1u) {
+    const int r = __ffs(none) - 1;
+    if (s.flags & SEG_WHOLE) {
+      const int t = plan.order[s.tok + r / G], h = s.h * G + r % G;
+      if (lane < D / 8) reinterpret_cast<uint4*>(static_cast<T*>(a.out) + t * a.o_tok + h * a.o_head)[lane] = uint4{0, 0, 0, 0};
+      if (lane == 0 && a.lse) a.lse[static_cast<int64_t>(t) * a.Hq + h] = -INFINITY;
+    } else if (lane == 0) {
+      reinterpret_cast<float2*>(a.ws)[static_cast<int64_t>(s.part_row) + r] = make_float2(-INFINITY, 0.f);
+    }
+  }
+}
+
+// Eight warps a CTA with a ring of pieces each, by 16-byte copies.  Scales of rows past a run's keys come as zeros, so such rows are zeros.
+//
+// Few16 has rows on the products' long side (16) and widens codes to 16 bits by masks, shifts and fused products.  Few8 has keys and
+// values there, 16 of them for 8 rows, and codes go into the products as they are, as fp16 numbers of the lowest bits (n 2^-24; 16 n 2^-24 where
+// they stand four bits up, against 1 / 16 of the other operand): a mask and a quarter of a shift a pair of codes.  What is left of
+// c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
+// -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
+// from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
+// 2^11 below its range's end.
+// Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
+// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 118 us (2.4 TB/s),
+// 168 by Few16 alone.
+template <typename T, int D>
+__device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {
+  using L = Smem<D, true>;
+  constexpr int ROW = D / 2, SROW = D / 32, CODES = PIECE * ROW, SCALES = PIECE * SROW, STAGE = L::F_BYTES, STAGES = L::F_STAGES;
+  constexpr int CHUNKS = ROW / 16, SCALE_CHUNKS = SCALES / 16;
+  const uint32_t base = s0 + warp * STAGES * STAGE, scales = s0 + L::F_SCALES + warp * L::F_SCALE_BYTES;
+  const int Hkv = a.lay.n_kv_heads, G = a.Hq / Hkv, page = a.lay.page;
+  const int64_t page_bytes = pages4::page_bytes(page, D);
+  bool bad = false;
+  // copies run ahead of the products, over the ends of jobs too; two stages are left to the products
+  Jobs copies(plan, work, G);
+  Job c{};
+  bool unused, more = copies.next(c, unused);
+  uint32_t k = 0;
+  int stage = 0, ahead = 0;      // of the piece at hand, of the next one to be copied
+  int64_t code_at = 0;           // where the next 32 pieces lie: a lane a piece; its codes,
+  int key_at = 0;                // its first row in the page, and 256 times its keys
+  auto find = [&](uint32_t b) {
+    if (b >= c.to) return;
+    PageCursor cur(plan, *c.s);
+    cur.go(b);
+    const Run& run = cur.run;
+    const int key = (static_cast<int>(b) - run.off) * PIECE;
+    int block = a.tables[static_cast<int64_t>(run.row) * a.lay.max_blocks + key / page];
+    if (block < 0 || block >= a.lay.n_blocks) {
+      if (a.status) atomicCAS(a.status, 0, DOPR_ERR_INVALID_ARG);
+      block = 0;
+    }
+    code_at = (block * Hkv + c.s->h) * page_bytes + key % page * ROW;
+    key_at = key % page + 256 * min(PIECE, run.keys - key);
+  };
+  const uint8_t *const k_lane = static_cast<const uint8_t*>(a.k_pool) + 16 * lane, *const v_lane = static_cast<const uint8_t*>(a.v_pool) + 16 * lane;
+  const uint8_t* const s_lane = static_cast<const uint8_t*>(lane < SCALE_CHUNKS ? a.k_pool : a.v_pool) + page * ROW + 16 * (lane % SCALE_CHUNKS);
+  uint32_t to_lane[CODES / 512];
+#pragma unroll
+  for (int i = 0; i < CODES / 512; ++i) {
+    const int x = lane + 32 * i, r = x / CHUNKS;
+    to_lane[i] = r * ROW + (((x % CHUNKS) ^ chunk_place<D>(r)) << 4);
+  }
+  auto copy = [&] {
+    if (more && c.from + k == c.to) {
+      more = copies.next(c, unused);
+      k = 0;
+    }
+    if (more) {
+      if ((k & 31u) == 0) find(c.from + k + lane);
+      const int64_t at = __shfl_sync(0xffffffffu, code_at, k & 31u);
+      const int key = __shfl_sync(0xffffffffu, key_at, k & 31u);
+      const uint32_t dst = base + ahead * STAGE;
+#pragma unroll
+      for (int i = 0; i < CODES / 512; ++i) {
+        cp_async16(dst + to_lane[i], k_lane + at + 512 * i, true);
+        cp_async16(dst + CODES + to_lane[i], v_lane + at + 512 * i, true);
+      }
+      if (lane < 2 * SCALE_CHUNKS)
+        cp_async16_part(dst + 2 * CODES + 16 * lane, s_lane + at - (key & 255) * (ROW - SROW),
+                        min(16, max(0, (key >> 8) * SROW - 16 * (lane % SCALE_CHUNKS))));
+      ++k;
+    }
+    cp_async_commit();
+    ahead = ahead + 1 == STAGES ? 0 : ahead + 1;
+  };
+#pragma unroll 1
+  for (int i = 0; i + 2 < STAGES; ++i) copy();
+
+  Jobs jobs(plan, work, G);
+  Job j{};
+  bool starts;
+#pragma unroll 1
+  while (jobs.next(j, starts)) {
+    if (starts) rows_without_keys<T, D>(a, plan, *j.s, G, lane);
+    const int prefix_keys = j.s->prefix_keys;
+    auto wait = [&] {
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+      __syncwarp();
+    };
+    auto stage_at = [&] {
+      const uint32_t at = base + stage * STAGE;
+      if (++stage == STAGES) stage = 0;
+      return at;
+    };
+    if (!j.eight) {
+      Few16<T, D> f(a, plan, *j.s, j.rows, G, lane);
+#pragma unroll 1
+      for (uint32_t b = j.from; b < j.to; ++b) {
+        copy();
+        wait();
+        f.step(stage_at(), prefix_keys, b * PIECE, bad, lane);
+        __syncwarp();  // every lane has read the stage
+      }
+      f.finish(a, plan, *j.s, j.rows, G, lane);
+      continue;
+    }
+    Few8<T, D> f(a, plan, *j.s, j.row0, j.rows, G, lane);
+#pragma unroll 1
+    for (uint32_t b = j.from; b < j.to; b += 2) {
+      const bool two = b + 1 < j.to;
+      copy();
+      if (two) copy();
+      wait();
+      const uint32_t first = stage_at(), at[2] = {first, two ? stage_at() : first};
+      f.step(at, scales, prefix_keys, b * PIECE, bad, lane);
+      __syncwarp();
+    }
+    f.finish(a, plan, *j.s, j.row0, j.rows, G, lane);
   }
   if (bad && a.status) atomicCAS(a.status, 0, DOPR_ERR_RANGE);
 }
@@ -895,14 +1390,14 @@ __device__ __forceinline__ void copy_4bit(const SharedAttnArgs& a, const Plan& p
 // parity of a stage's phase before last for the one it waits for.  A lane a group: 16 bytes of codes to 64 of values.  Rows past a
 // run's keys are zeros.
 template <typename T, int D>
-__device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan& plan, uint8_t* smem, uint32_t s0, int2 work, bool is_v, int part,
+__device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int2 work, bool is_v, int part,
                                             int* err, int lane) {
   using L = Smem<D, true>;
   constexpr int ROW = D / 2, SROW = D / 32, AT_ONCE = 32 / SROW;
   const int page = a.lay.page, page_blk = BLOCK / page, piece = min(page, 64), bits = __ffs(piece) - 1;
   const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
   const int raw_stages = is_v ? L::RAW_V : L::RAW_K, stage0 = is_v ? L::RAW_K : 0;
-  uint8_t* const tiles = smem + (is_v ? L::OFF_V : L::OFF_K);
+  const uint32_t tiles = s0 + (is_v ? L::OFF_V : L::OFF_K);
   auto bar = [&](int i) { return s0 + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
   const int group = lane % SROW, swap = D == 128 && group >= 2 ? 2 : 0;
   Walk walk(plan, work);
@@ -922,17 +1417,17 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
           ok = false;
           break;
         }
-        const uint8_t* from = smem + L::OFF_RAW + rs * L::RAW_BYTES;
-        const uint8_t* keys = smem + L::OFF_KEYS + rs * 4;
+        const uint32_t from = s0 + L::OFF_RAW + rs * L::RAW_BYTES, keys = s0 + L::OFF_KEYS + rs * 4;
         // the half of the head and the first of four 16-byte places in a row of it
-        uint8_t* to = tiles + r.stage * L::TILE_BYTES + (D == 128 ? group >> 1 : 0) * HALF_BYTES + 64 * half * 128;
+        const uint32_t to = tiles + r.stage * L::TILE_BYTES + (D == 128 ? group >> 1 : 0) * HALF_BYTES + 64 * half * 128;
         const int place = (D == 128 ? group & 1 : group) * 4;
 #pragma unroll 2
         for (int r0 = 32 * part; r0 < end; r0 += AT_ONCE) {
           const int row = r0 + lane / SROW, at = row >> bits, in = row & (piece - 1);
-          const uint8_t* p = from + at * piece * (ROW + SROW);
-          uint4 w = *reinterpret_cast<const uint4*>(p + in * ROW + 16 * group);
-          const uint32_t byte = in < keys[at] ? scale_of(p[piece * ROW + in * SROW + group], bad) : 0u;
+          const uint32_t p = from + at * piece * (ROW + SROW);
+          uint4 w = lds128(p + in * ROW + 16 * group);
+          const uint32_t got = lds8(p + piece * ROW + in * SROW + group);
+          const uint32_t byte = in < static_cast<int>(lds8(keys + at)) ? scale_of(got, bad) : 0u;
           const pages4::Widen<T> widen(byte * 0x10001u);
           // lanes of the upper half of the head begin with their third word, so that those that store at once meet all banks
           if (swap) w = uint4{w.z, w.w, w.x, w.y};
@@ -941,7 +1436,7 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
           for (int j = 0; j < 4; ++j) {
             uint32_t x[4];
             widen(words[j], x);
-            *reinterpret_cast<uint4*>(to + row * 128 + (((place + (j ^ swap)) ^ (row & 7)) << 4)) = uint4{x[0], x[1], x[2], x[3]};
+            sts128(to + row * 128 + (((place + (j ^ swap)) ^ (row & 7)) << 4), uint4{x[0], x[1], x[2], x[3]});
           }
         }
         __syncwarp();
@@ -1010,7 +1505,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
   } else if (few) {
     if (warp >= 4 && warp < 12) {
       regs_many<FOUR>();
-      if constexpr (FOUR) few_items_4bit<T, D>(a, plan, smem, s0, warp - 4, work, lane);
+      if constexpr (FOUR) few_items_4bit<T, D>(a, plan, s0, warp - 4, work, lane);
       else few_items<T, D>(a, plan, s0, warp - 4, work, &marked[warp - 4], lane);
     } else {
       regs_few<FOUR>();
@@ -1071,7 +1566,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
   } else if (FOUR && warp >= 12) {
     // ======================= 4 bits: K (warps 12, 13) and V (14, 15) to the products' type
     regs_few<FOUR>();
-    if constexpr (FOUR) expand_4bit<T, D>(a, plan, smem, s0, work, warp >= 14, warp & 1, err, lane);
+    if constexpr (FOUR) expand_4bit<T, D>(a, plan, s0, work, warp >= 14, warp & 1, err, lane);
   } else if (warp == 1) {
     // ======================= MMA issuer
     regs_few<FOUR>();

@@ -60,6 +60,22 @@ struct Smem {
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
+// A wait of the CTA's roles.  4 bits: by counts, some half a second, each role by itself; the clock's code and the atomic's, at twenty
+// places, took more of the instruction caches than they can spare beside the warps that expand (200 queries on 16 documents: 182 us
+// for 220 with the clock, 200 with the atomic; 2,048 rows on 16,384 keys: 420 for 427 and 433).
+__device__ __forceinline__ bool wait_by_counts(uint32_t bar, uint32_t parity, int* err) {
+#pragma unroll 1
+  for (int i = 0; i < 1 << 24; ++i)
+    if (mbar_try_wait(bar, parity)) return true;
+  *reinterpret_cast<volatile int*>(err) = DEV_ERR_TIMEOUT;
+  return false;
+}
+template <bool FOUR>
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int* err, uint64_t timeout_ns) {
+  if constexpr (FOUR) return __all_sync(0xffffffffu, wait_by_counts(bar, parity, err)) != 0;
+  return mbar_wait_warp(bar, parity, err, timeout_ns);
+}
+
 struct Ring {
   int stage = 0;
   uint32_t phase = 0;
@@ -1353,7 +1369,7 @@ __device__ __forceinline__ void copy_4bit(const SharedAttnArgs& a, const Plan& p
         src += (block * Hkv + s.h) * page_bytes;
       }
       for (int half = 0; half * 64 < cols; ++half) {
-        if (!mbar_wait_warp(bar(L::RAW_EMPTY + stage0 + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
+        if (!wait_warp<true>(bar(L::RAW_EMPTY + stage0 + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
         }
@@ -1382,24 +1398,30 @@ __device__ __forceinline__ void copy_4bit(const SharedAttnArgs& a, const Plan& p
   }
   if (!ok)  // copies in flight land before the CTA ends
     for (int i = 0; i < stages; ++i)
-      if (armed >> i & 1u) mbar_wait_warp(bar(L::RAW_FULL + stage0 + i), parity >> i & 1u, err, 100000000ull);
+      if (armed >> i & 1u) wait_warp<true>(bar(L::RAW_FULL + stage0 + i), parity >> i & 1u, err, 100000000ull);
 }
 
 // Tiles: each block of K or V, by two warps, from the raw ring into the products' ring, in the layout that copies of 16-bit rows have
-// there.  Warp `part` takes 32 rows of each half, so that both pass every stage of the ring: a warp that skipped some could take the
+// there.  Bound by what fetching and waiting for instructions cost a warp alone on its part of a scheduler: loads of 16 rows before
+// their stores took 2,048 rows on 16,384 keys from 482 us to 440, addresses once for 16 rows to 427; four such loads at once 450.
+// Warp `part` takes 32 rows of each half, so that both pass every stage of the ring: a warp that skipped some could take the
 // parity of a stage's phase before last for the one it waits for.  A lane a group: 16 bytes of codes to 64 of values.  Rows past a
 // run's keys are zeros.
 template <typename T, int D>
 __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int2 work, bool is_v, int part,
                                             int* err, int lane) {
   using L = Smem<D, true>;
-  constexpr int ROW = D / 2, SROW = D / 32, AT_ONCE = 32 / SROW;
+  constexpr int ROW = D / 2, SROW = D / 32, AT_ONCE = 32 / SROW, TIMES = 16 / AT_ONCE;
   const int page = a.lay.page, page_blk = BLOCK / page, piece = min(page, 64), bits = __ffs(piece) - 1;
   const int stages = is_v ? L::V_STAGES : L::K_STAGES, full = is_v ? L::V_FULL : L::K_FULL, empty = full + stages;
   const int raw_stages = is_v ? L::RAW_V : L::RAW_K, stage0 = is_v ? L::RAW_K : 0;
-  const uint32_t tiles = s0 + (is_v ? L::OFF_V : L::OFF_K);
   auto bar = [&](int i) { return s0 + L::OFF_BAR + 8u * static_cast<uint32_t>(i); };
-  const int group = lane % SROW, swap = D == 128 && group >= 2 ? 2 : 0;
+  const int group = lane % SROW, first = 32 * part + lane / SROW;
+  // the half of the head, the row, and the first of four 16-byte places in it; lanes of the upper half of the head begin with their
+  // third word, so that those that store at once meet all banks
+  const bool swap = D == 128 && group >= 2;
+  const uint32_t tile0 = s0 + (is_v ? L::OFF_V : L::OFF_K) + (D == 128 ? group >> 1 : 0) * HALF_BYTES + first * 128 +
+                         ((((D == 128 ? group & 1 : group) * 4 + (swap ? 2 : 0)) ^ (first & 7)) << 4);
   Walk walk(plan, work);
   Segment s;
   Ring r, raw;
@@ -1407,36 +1429,42 @@ __device__ __forceinline__ void expand_4bit(const SharedAttnArgs& a, const Plan&
   while (ok && walk.next(s)) {
     for (uint32_t b = s.b0; b < s.b1 && ok; ++b) {
       const int cols = min(page_blk, s.pages - static_cast<int>(b) * page_blk) * page;
-      if (!mbar_wait_warp(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
+      if (!wait_warp<true>(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
         ok = false;
         break;
       }
       for (int half = 0; 64 * half < cols; ++half) {
-        const int rs = stage0 + raw.stage, end = min(32 * part + 32, cols - 64 * half);
-        if (!mbar_wait_warp(bar(L::RAW_FULL + rs), raw.phase, err, WAIT_TIMEOUT_NS)) {
+        const int rs = stage0 + raw.stage, rows = cols - 64 * half - 32 * part;  // of this warp's 32; a multiple of 16
+        if (!wait_warp<true>(bar(L::RAW_FULL + rs), raw.phase, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
         }
-        const uint32_t from = s0 + L::OFF_RAW + rs * L::RAW_BYTES, keys = s0 + L::OFF_KEYS + rs * 4;
-        // the half of the head and the first of four 16-byte places in a row of it
-        const uint32_t to = tiles + r.stage * L::TILE_BYTES + (D == 128 ? group >> 1 : 0) * HALF_BYTES + 64 * half * 128;
-        const int place = (D == 128 ? group & 1 : group) * 4;
-#pragma unroll 2
-        for (int r0 = 32 * part; r0 < end; r0 += AT_ONCE) {
-          const int row = r0 + lane / SROW, at = row >> bits, in = row & (piece - 1);
-          const uint32_t p = from + at * piece * (ROW + SROW);
-          uint4 w = lds128(p + in * ROW + 16 * group);
-          const uint32_t got = lds8(p + piece * ROW + in * SROW + group);
-          const uint32_t byte = in < static_cast<int>(lds8(keys + at)) ? scale_of(got, bad) : 0u;
-          const pages4::Widen<T> widen(byte * 0x10001u);
-          // lanes of the upper half of the head begin with their third word, so that those that store at once meet all banks
-          if (swap) w = uint4{w.z, w.w, w.x, w.y};
-          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+        const uint32_t from = s0 + L::OFF_RAW + rs * L::RAW_BYTES, keys = lds32(s0 + L::OFF_KEYS + rs * 4);
+        const uint32_t to = tile0 + r.stage * L::TILE_BYTES + 64 * half * 128;
+        // 16 rows at a time, of one piece: codes and scales first, for the stores may not pass the loads, nor the other way round
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows && r0 < 32; r0 += 16) {
+          const int row = 32 * part + r0, at = row >> bits, in = row & (piece - 1);
+          const int left = static_cast<int>(keys >> 8 * at & 0xffu) - in - lane / SROW;  // keys of the run from this lane's row on
+          const uint32_t p = from + at * piece * (ROW + SROW), codes = p + in * ROW + 16 * lane, scales = p + piece * ROW + in * SROW + lane;
+          uint4 w[TIMES];
+          uint32_t byte[TIMES];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t x[4];
-            widen(words[j], x);
-            sts128(to + row * 128 + (((place + (j ^ swap)) ^ (row & 7)) << 4), uint4{x[0], x[1], x[2], x[3]});
+          for (int i = 0; i < TIMES; ++i) {
+            w[i] = lds128(codes + i * 512);
+            byte[i] = lds8(scales + i * 32);
+          }
+#pragma unroll
+          for (int i = 0; i < TIMES; ++i) {
+            const pages4::Widen<T> widen((i * AT_ONCE < left ? scale_of(byte[i], bad) : 0u) * 0x10001u);
+            if (swap) w[i] = uint4{w[i].z, w[i].w, w[i].x, w[i].y};
+            const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              uint32_t x[4];
+              widen(words[j], x);
+              sts128((to ^ (j << 4)) + (r0 + i * AT_ONCE) * 128, uint4{x[0], x[1], x[2], x[3]});
+            }
           }
         }
         __syncwarp();
@@ -1540,7 +1568,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
               block = 0;
             }
           }
-          if (!mbar_wait_warp(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
+          if (!wait_warp<FOUR>(bar(empty + r.stage), r.phase ^ 1u, err, WAIT_TIMEOUT_NS)) {
             ok = false;
             break;
           }
@@ -1561,7 +1589,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
       }
       if (!ok)  // copies in flight land before the CTA ends
         for (int i = 0; i < stages; ++i)
-          if (armed >> i & 1u) mbar_wait_warp(bar(full + i), parity >> i & 1u, err, 100000000ull);
+          if (armed >> i & 1u) wait_warp<FOUR>(bar(full + i), parity >> i & 1u, err, 100000000ull);
     }
   } else if (FOUR && warp >= 12) {
     // ======================= 4 bits: K (warps 12, 13) and V (14, 15) to the products' type
@@ -1576,7 +1604,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     Walk walk(plan, work);
     Groups groups;
     bool ok = true;
-    auto wait = [&](int b, uint32_t par) { return ok = ok && mbar_wait_warp(bar(b), par, err, WAIT_TIMEOUT_NS); };
+    auto wait = [&](int b, uint32_t par) { return ok = ok && wait_warp<FOUR>(bar(b), par, err, WAIT_TIMEOUT_NS); };
     constexpr uint32_t idesc_o = umma_idesc_f16_bmn(TILE, D) | type_bits<T>();
     const uint64_t v_desc0 = umma_desc_sw128_mn(sV, HALF_BYTES, 1024), k_desc0 = umma_desc_sw128(sK), q_desc0 = umma_desc_sw128(sQ);
     uint32_t p_par = 0, q_par = 0;  // a bit a group
@@ -1768,7 +1796,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     }
     commit_pv();
     if (one) umma_commit(bar(L::DRAIN));
-    mbar_wait_warp(bar(L::DRAIN), 0, err, ok ? WAIT_TIMEOUT_NS : 100000000ull);
+    wait_warp<FOUR>(bar(L::DRAIN), 0, err, ok ? WAIT_TIMEOUT_NS : 100000000ull);
   } else if (warp == 3) {
     // ======================= rows of Q: row r of a group's tile is token r / G of the tile, head r % G of the kv head's
     regs_few<FOUR>();
@@ -1795,7 +1823,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
         const uint32_t runs = __ballot_sync(0xffffffffu, run);
         for (int r = lane; !a.q_boxes && r < rows; r += 32) row[r] = tok[r / G];
         __syncwarp();
-        if ((used >> w & 1u) && !mbar_wait_warp(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
+        if ((used >> w & 1u) && !wait_warp<FOUR>(bar(L::Q_EMPTY + w), par >> w & 1u, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
         }
@@ -1843,7 +1871,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     }
     if (ld_volatile(err))  // copies in flight land before the CTA ends
       for (int w = 0; w < 2; ++w)
-        if (used >> w & 1u) mbar_wait_warp(bar(L::Q_FULL + w), (filled >> w & 1u) ^ 1u, err, 100000000ull);
+        if (used >> w & 1u) wait_warp<FOUR>(bar(L::Q_FULL + w), (filled >> w & 1u) ^ 1u, err, 100000000ull);
   } else {
     // ======================= softmax: thread r of group w has row r of its tile
     regs_many<FOUR>();
@@ -1860,7 +1888,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     bool ok = true;
     // (the first group that takes a block) rows of V past a page's keys count as zero: before any of P is given
     auto ready_v = [&](int stage, uint32_t phase, int cols) {
-      if (!mbar_wait_warp(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
+      if (!wait_warp<FOUR>(bar(L::V_FULL + stage), phase, err, WAIT_TIMEOUT_NS)) return false;
       const int page = a.lay.page;
 #pragma unroll 1
       for (int pg = 0; pg * page < cols; ++pg) {
@@ -1889,7 +1917,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
     constexpr uint32_t SUMS = 2, LEFT = 4;
     while (ok && walk.next(s)) {
       if (o_par & LEFT) {
-        if (!mbar_wait_warp(bar(L::ML_EMPTY), (o_par & SUMS) == 0, err, WAIT_TIMEOUT_NS)) break;
+        if (!wait_warp<FOUR>(bar(L::ML_EMPTY), (o_par & SUMS) == 0, err, WAIT_TIMEOUT_NS)) break;
         o_par &= ~LEFT;
       }
       const int t0 = s.flags & SEG_TWO ? w * TT : 0, n = min(TT, s.n_tok - t0);
@@ -1910,7 +1938,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
         const uint32_t v_phase = rv.phase;
         rv.next(L::V_STAGES);
         if (!(takes >> w & 1u)) continue;
-        if (!mbar_wait_warp(bar(L::S_FULL + w), s_par, err, WAIT_TIMEOUT_NS)) {
+        if (!wait_warp<FOUR>(bar(L::S_FULL + w), s_par, err, WAIT_TIMEOUT_NS)) {
           ok = false;
           break;
         }
@@ -2006,7 +2034,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
       }
       if (!ok) break;
       if (done > 0) {
-        if (!mbar_wait_warp(bar(L::O_FULL + w), o_par & 1u, err, WAIT_TIMEOUT_NS)) break;
+        if (!wait_warp<FOUR>(bar(L::O_FULL + w), o_par & 1u, err, WAIT_TIMEOUT_NS)) break;
         o_par ^= 1u;
         tc_fence_after();
       }
@@ -2022,7 +2050,7 @@ __device__ __forceinline__ void attend(const CUtensorMap& tm_q8, const CUtensorM
           if (lane == 0) mbar_arrive(bar(L::ML_FULL));
           o_par |= LEFT;
         } else if (both) {
-          if (!mbar_wait_warp(bar(L::ML_FULL), (o_par & SUMS) != 0, err, WAIT_TIMEOUT_NS)) break;
+          if (!wait_warp<FOUR>(bar(L::ML_FULL), (o_par & SUMS) != 0, err, WAIT_TIMEOUT_NS)) break;
           tc_fence_after();
           const float2 sum = add_other<D>(o_col, make_float2(m, l), ml[r]);
           m = sum.x, l = sum.y;

@@ -750,7 +750,7 @@ cudaError_t launch_append(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
 }
 template <typename T, int VEC, int NU, bool INTER, int DIM>
 cudaError_t launch_back(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const int blocks = BACK_HELD * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? 4 * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
+  const int blocks = BACK_HELD * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? BACK_HELD * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
   Roles r{};
   if (a.n_tokens > 0) {
     r = roles_of(a, lanes_of(a.head_dim, VEC), blocks);

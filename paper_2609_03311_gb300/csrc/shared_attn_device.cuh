@@ -60,12 +60,12 @@ struct Smem {
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
-// A wait of the CTA's roles.  4 bits: by counts, some half a second, each role by itself; the clock's code and the atomic's, at twenty
+// A wait of the CTA's roles.  4 bits: by counts, some two seconds, each role by itself; the clock's code and the atomic's, at twenty
 // places, took more of the instruction caches than they can spare beside the warps that expand (200 queries on 16 documents: 182 us
 // for 220 with the clock, 200 with the atomic; 2,048 rows on 16,384 keys: 420 for 427 and 433).
 __device__ __forceinline__ bool wait_by_counts(uint32_t bar, uint32_t parity, int* err) {
 #pragma unroll 1
-  for (int i = 0; i < 1 << 24; ++i)
+  for (int i = 0; i < 1 << 26; ++i)
     if (mbar_try_wait(bar, parity)) return true;
   *reinterpret_cast<volatile int*>(err) = DEV_ERR_TIMEOUT;
   return false;
@@ -1122,8 +1122,8 @@ struct Few8 {
   }
 };
 
-// What a warp does at once of few items of the 4-bit cache: a segment, or where it has more than 8 rows and long runs, whose tokens alone
-// see them, a run of it.  Few8 takes 1.0 us a piece where Few16 takes 1.45 with eight warps at work, but its code beside Few16's no
+// What a warp does at once of few items of the 4-bit cache: a segment, or where that has several long runs, whose tokens alone see
+// them, a run of it.  A part for Few8 is of one run: the scales of other tokens' values would cost its rows precision.  Few8 takes 1.0 us a piece where Few16 takes 1.45 with eight warps at work, but its code beside Few16's no
 // longer stays in the instruction caches when jobs are short (a third of the warps' time then goes to waiting for instructions).  By
 // the pieces of a job from which Few8 takes it (runs: on average):
 //   runs       64 conversations of 2,000 to 6,000 keys   256 of 50 to 400, 4 and 8 rows a token   32 of 1,000 to 3,000, a row a token
@@ -1148,18 +1148,18 @@ struct Jobs {
   const Segment* s = nullptr;
   int at, end, G, run = -1;
   __device__ __forceinline__ Jobs(const Plan& p, int2 work, int G_) : plan(p), at(work.x), end(work.y), G(G_) {}
-  __device__ __forceinline__ bool apart() const {
-    const uint32_t n = s->b1 - s->b0, most = n / LONG_RUN;
-    if (most < 2) return false;
+  // The segment's runs; own: none is a prefix, and none has more than 8 rows.
+  __device__ __forceinline__ uint32_t count(bool& own) const {
     const Run* runs = plan.runs + s->run;
     uint32_t of = 0;
+    own = true;
     for (int i0 = s->run_at; i0 < s->n_runs; i0 += 32) {  // a lane a run
       const int i = i0 + static_cast<int>(threadIdx.x & 31u);
       const bool in = i < s->n_runs && static_cast<uint32_t>(runs[i].off) < s->b1;
-      if (__any_sync(0xffffffffu, in && (runs[i].token < 0 || (runs[i].tok1 - runs[i].tok0) * G > 8))) return false;
+      if (__any_sync(0xffffffffu, in && (runs[i].token < 0 || (runs[i].tok1 - runs[i].tok0) * G > 8))) own = false;
       of += __popc(__ballot_sync(0xffffffffu, in));
     }
-    return of <= most;
+    return of;
   }
   // starts: the segment is a new one, and its runs are jobs of their own
   __device__ __forceinline__ bool next(Job& j, bool& starts) {
@@ -1181,8 +1181,16 @@ struct Jobs {
       if (at < end) asm volatile("prefetch.global.L1 [%0];" ::"l"(plan.segs + at));
       j.from = s->b0, j.to = s->b1;
       j.row0 = 0, j.rows = s->n_tok * G;
-      j.eight = j.rows <= 8 && j.to - j.from >= LONG_SEGMENT;
-      if (j.rows <= 8 || !apart()) return true;
+      j.eight = false;
+      const uint32_t n = j.to - j.from;
+      if (n < LONG_SEGMENT) return true;
+      bool own;
+      const uint32_t of = count(own);
+      if (of == 1 && j.rows <= 8) {
+        j.eight = true;
+        return true;
+      }
+      if (!own || n < LONG_RUN * of) return true;
       j.eight = true;
       run = s->run_at;
       starts = true;
@@ -1221,7 +1229,7 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
 // -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
 // from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
-// 2^11 below its range's end.
+// 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded twice to 11 bits.
 // Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
 // last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 118 us (2.4 TB/s),
 // 168 by Few16 alone.

@@ -176,6 +176,98 @@ def test_one_heavy_key_among_many_light_ones(tokens, d, dt):
         assert bool(((got[1].double() - lse).abs() <= 2.0 ** -12 + 2.0 ** -22 * lse.abs()).all())
 
 
+# Parts of few rows long enough that a warp takes 8 rows of one run at once, with codes as they are: some 16 pieces of 16 keys and more for
+# each of 8 warps an SM.  fp16 rounds P and then P times the scale, so a unit of 2^-11 more stands before A there (bf16's own is larger).
+LONG = {
+    "a row a token": (8, 8, 0, [(-1, 2100 + 37 * i, 1) for i in range(24)]),
+    "four rows a token": (32, 8, 0, [(-1, 1500 + 91 * i, 1) for i in range(24)]),
+    "five rows a token": (20, 4, 0, [(-1, 1900 + 53 * i, 1) for i in range(50)]),
+    "eight rows a token": (64, 8, 0, [(-1, 2400 + 29 * (i % 7), 1) for i in range(20)]),
+    "two tokens of each": (16, 8, 0, [(-1, 1700 + 111 * i, 2) for i in range(20)]),
+    "five of each, more than 8 rows": (16, 8, 0, [(-1, 2200 + 13 * i, 5) for i in range(20)]),
+    "long and short": (32, 8, 0, [(-1, [40, 5000, 3, 2600, 0, 16, 17][i % 7], 1) for i in range(49)]),
+    "one sequence": (8, 2, 0, [(-1, 250001, 1)]),
+    "two tokens of one": (8, 2, 0, [(-1, 250017, 2)]),
+    "three tokens of one": (8, 2, 0, [(-1, 250002, 3)]),
+    "two on a document": (8, 2, 230000, [(0, 25, 1), (0, 400, 1)]),
+}
+
+
+def check_long(b, got):
+    out, lse, avg = b.exact()
+    u = torch.finfo(b.dt).eps / 2
+    err, tol = (got[0].double() - out).abs(), (u + 2.0 ** -11 + (2.0 ** -11 if b.dt == HF else 0)) * avg + u * out.abs() + 2.0 ** -24
+    assert bool((err <= tol).all()), (float((err / tol).max()), int((~(err <= tol)).sum()))
+    empty = lse == -math.inf
+    assert torch.equal(got[1] == -math.inf, empty) and bool((got[0][empty] == 0).all())
+    e2 = (got[1].double() - lse).abs()[~empty]
+    assert bool((e2 <= 2.0 ** -12 + 2.0 ** -22 * lse.abs()[~empty]).all()), float(e2.max())
+
+
+@pytest.mark.parametrize("dt,d,page", [(BF, 128, 64), (HF, 128, 16), (HF, 64, 128), (BF, 64, 32)])
+@pytest.mark.parametrize("kind", list(LONG))
+def test_long_parts_of_few_rows(kind, dt, d, page):
+    hq, hkv, m, reqs = LONG[kind]
+    b = Batch4(hq, hkv, d, dt, page, [m] if m else [], reqs, seed=len(kind) + d)
+    got = b.run()
+    check_long(b, got)
+    again = b.run()
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, 1e30])
+def test_bad_queries_stay_in_their_rows_of_long_parts(bad):
+    hq, hkv, _, reqs = LONG["four rows a token"]
+    b = Batch4(hq, hkv, 128, BF, 64, [], reqs, seed=2)
+    clean = b.run()
+    b.q[3, 5] = bad
+    got = b.run()
+    rest = torch.ones(b.T, hq, dtype=torch.bool, device=DEV)
+    rest[3, 5] = False
+    assert not bool(torch.isfinite(got[0][3, 5]).all()) or bad == 1e30
+    assert torch.equal(got[0][rest], clean[0][rest]) and torch.equal(got[1][rest], clean[1][rest])
+
+
+@pytest.mark.parametrize("byte", [0xe2, 0xff])
+@pytest.mark.parametrize("pool", ["k", "v"])
+@pytest.mark.parametrize("kind", ["a row a token", "four rows a token", "one sequence"])
+def test_scales_that_stand_for_nan_in_long_parts(kind, pool, byte):
+    hq, hkv, _, reqs = LONG[kind]
+    b = Batch4(hq, hkv, 128, HF, 16, [], reqs, seed=5)
+    p = b.k4 if pool == "k" else b.v4
+    places = [(int(b.tables[i, at // 16]), i % hkv, 16 * 64 + at % 16 * 4 + i % 4)
+              for i in range(0, len(reqs), 2) for at in (0, 777, b.lens[i] - 1)]
+    for x in places:
+        p[x] = byte
+    got = b.run(want=dopr.ERR_RANGE)
+    for x in places:
+        p[x] = 0
+    again = b.run()
+    assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
+
+
+@pytest.mark.parametrize("dt", [BF, HF])
+def test_values_of_very_different_sizes_in_long_parts(dt):
+    # a sequence's values grow 2^16 times over its keys, one group of elements is 2^6 times the others, and every other sequence is larger
+    # still.  P's largest is 2^11 or more, the largest scale comes as 1 / 2 or more, and their products are rounded to 11 bits, or to
+    # steps of 2^-24: a key adds at most 7 2^-25 / (2^11 / 2) = 7 2^-35 of the run's largest scale.
+    hq, hkv, _, reqs = LONG["four rows a token"]
+    b = Batch4(hq, hkv, 128, dt, 64, [], reqs, seed=9)
+    for i, n in enumerate(b.lens):
+        grow = torch.exp2(torch.linspace(-16, 0, n, device=DEV))[:, None, None] * (16.0 if i % 2 else 1.0)
+        v = b.rows[i][1].float() * grow
+        v[:, :, 32:64] *= 64
+        b.rows[i][1] = v.to(dt)
+        b.write(i, torch.arange(n, device=DEV))
+    out, lse, avg = b.exact()
+    got = b.run()
+    u = torch.finfo(dt).eps / 2
+    largest = max(float(r[1].float().abs().max()) for r in b.rows) / 7 * 1.125
+    tol = (u + 2.0 ** -10) * avg + u * out.abs() + 7 * 2.0 ** -35 * largest * max(b.lens) + 2.0 ** -24
+    err = (got[0].double() - out).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+
+
 @pytest.mark.parametrize("bad", [math.nan, math.inf, 1e30])
 @pytest.mark.parametrize("tokens", [1, 30])
 def test_bad_queries_stay_in_their_rows(bad, tokens):

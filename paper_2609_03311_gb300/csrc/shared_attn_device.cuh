@@ -1123,20 +1123,20 @@ struct Few8 {
 };
 
 // What a warp does at once of few items of the 4-bit cache: a segment, or where that has several long runs, whose tokens alone see
-// them, a run of it.  A part for Few8 is of one run: the scales of other tokens' values would cost its rows precision.  Few8 takes 1.0 us a piece where Few16 takes 1.45 with eight warps at work, but its code beside Few16's no
-// longer stays in the instruction caches when jobs are short (a third of the warps' time then goes to waiting for instructions).  By
-// the pieces of a job from which Few8 takes it (runs: on average):
-//   runs       64 conversations of 2,000 to 6,000 keys   256 of 50 to 400, 4 and 8 rows a token   32 of 1,000 to 3,000, a row a token
-//     8                       111 us                                  75 and 76                                  52
-//    12                       113                                     61 and 66                                  53
-//    16                       118                                     48 and 51                                  56
-//    24                       126                                     47 and 50                                  55
-//    none                     162                                     50 and 51                                  58
-//   segments   one token of 32 heads on 8 over 32,768 keys   256 queries on 64 documents of 1 to 1,024 tokens, 16 heads on 8
-//     6                        33                                      56
-//    12                        35                                      53
-//    32                        40                                      51
-constexpr uint32_t LONG_RUN = 16, LONG_SEGMENT = 12;
+// them, a run of it.  A part for Few8 is of one run: the scales of other tokens' values would cost its rows precision.  Few8 takes
+// 0.9 us a piece where Few16 takes 1.4 with eight warps at work, but its code beside Few16's does not stay in the instruction
+// caches when parts are short (half of a warp's time then goes to waiting for instructions).  By the pieces from which Few8 takes a
+// run (on average over a segment's), in us:
+//           64 conversations of    256 of 50 to 400 keys,    32 of 1,000 to 3,000    8 of 16,000 keys,
+//           2,000 to 6,000 keys    4 and 8 rows a token      keys, a row a token     8 rows a token
+//      8          109                   75   76                     49                     63
+//     12          109                   64   71                     49                     63
+//     16          110                   48   54                     57                     65
+//     24          114                   48   50                     57                     69
+//   none          153                   48   50                     56                     83
+// and a segment of one run: one token of 32 heads on 8 over 32,768 keys, 256 queries on 64 documents of 1 to 1,024 tokens: from 6
+// pieces on 33.6 and 50.3, 12: 35.4 and 49.8, 24: 39.7 and 49.5, none: 39.7 and 48.7.
+constexpr uint32_t LONG_RUN = 16, LONG_SEGMENT = 6;
 struct Job {
   const Segment* s;
   int row0, rows;
@@ -1231,8 +1231,8 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
 // 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded twice to 11 bits.
 // Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
-// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 118 us (2.4 TB/s),
-// 168 by Few16 alone.
+// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 110 us (2.6 TB/s),
+// 153 by Few16 alone.
 template <typename T, int D>
 __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {
   using L = Smem<D, true>;

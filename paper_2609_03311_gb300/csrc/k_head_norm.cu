@@ -667,10 +667,12 @@ __global__ void __launch_bounds__(THREADS, BACK_HELD) k_head_norm_back(const __g
   }
 }
 
-// The blocks' parts of the gains' gradients, in a fixed order: 32 columns of one gain a block, a warp every 32nd part.
+// The blocks' parts of the gains' gradients, in a fixed order: 8 columns of one gain a block (a sector of a part's), eight threads
+// every 128th part.  Latency: gradients of 8,192 rows 42.9 us, with 32 columns and every 32nd part 43.4.
+constexpr int GAIN_COLS = 8;
 __global__ void __launch_bounds__(1024) k_head_norm_gains(const float* ws, int q_parts, int k_parts, int D, float* dq_gain, float* dk_gain) {
-  __shared__ float sums[32][33];
-  const int i = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+  __shared__ float sums[32][GAIN_COLS + 1];
+  const int col = threadIdx.x % GAIN_COLS, i = blockIdx.x * GAIN_COLS + col, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool is_k = blockIdx.y > 0;
   float* out = is_k ? dk_gain : dq_gain;
   pdl_wait();
@@ -678,13 +680,16 @@ __global__ void __launch_bounds__(1024) k_head_norm_gains(const float* ws, int q
   if (!out) return;
   float v = 0.f;
   if (i < D)
-    for (int p = warp; p < (is_k ? k_parts : q_parts); p += 32) v += ws[static_cast<int64_t>(p + (is_k ? q_parts : 0)) * D + i];
-  sums[warp][threadIdx.x & 31] = v;
+    for (int p = threadIdx.x / GAIN_COLS; p < (is_k ? k_parts : q_parts); p += 1024 / GAIN_COLS)
+      v += ws[static_cast<int64_t>(p + (is_k ? q_parts : 0)) * D + i];
+#pragma unroll
+  for (int o = GAIN_COLS; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane < GAIN_COLS) sums[warp][lane] = v;
   __syncthreads();
   // warp w adds up column w
-  v = sums[threadIdx.x & 31][warp];
-  v = warp_sum(v);
-  if ((threadIdx.x & 31) == 0 && blockIdx.x * 32 + warp < D) out[blockIdx.x * 32 + warp] = v;
+  if (warp >= GAIN_COLS) return;
+  v = warp_sum(sums[lane][warp]);
+  if (lane == 0 && blockIdx.x * GAIN_COLS + warp < D) out[blockIdx.x * GAIN_COLS + warp] = v;
 }
 
 bool aligned16(const void* p, int64_t s0, int64_t s1, int size) {
@@ -703,7 +708,9 @@ bool wide(const HeadNormArgs& a, int size) {
 }
 // Blocks for each role, by its work: turns of heads a warp, and about one for a token's cos and sin (gradients of 8,192 rows by the
 // heads alone: 60.3 us, the keys' blocks end last).  Few tokens leave most SMs idle, so their heads go to several warps.
-Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks) {
+// one_round: all blocks run at once, so what counts is the warp with most turns (1,021 rows of fp32, one slice a token: 14.2 us, by
+// this 13.7).
+Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks, bool one_round) {
   const int heads[3] = {a.q.n_heads, a.k.n_heads, a.v.n_heads}, per_warp = 32 / lanes, warps = THREADS / 32;
   int turns[3], all = 0;
   for (int i = 0; i < 3; ++i) {
@@ -718,6 +725,13 @@ Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks) {
       const int64_t blocks = static_cast<int64_t>(most_blocks) * (turns[i] + 1) / all, part = blocks > 0 ? blocks : 1;
       int64_t slices = a.n_tokens > 0 ? part * warps / a.n_tokens : 1;
       slices = slices < 1 ? 1 : slices > turns[i] ? turns[i] : slices;
+      if (one_round && slices < turns[i]) {
+        int64_t least = INT64_MAX;
+        for (int n = 1; n <= turns[i] && n <= 16 && static_cast<int64_t>(a.n_tokens) * n <= INT32_MAX; ++n) {
+          const int64_t units = (static_cast<int64_t>(a.n_tokens) * n + part * warps - 1) / (part * warps), took = units * ((turns[i] + n - 1) / n + 1);
+          if (took < least) least = took, slices = n;
+        }
+      }
       const int per = static_cast<int>((turns[i] + slices - 1) / slices);  // as many slices as are not empty
       r.slices[i] = (turns[i] + per - 1) / per;
       const int64_t need = (static_cast<int64_t>(a.n_tokens) * r.slices[i] + warps - 1) / warps;
@@ -730,7 +744,7 @@ Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks) {
 
 template <typename T, int VEC, int NU, bool INTER, bool PAGES, int DIM>
 cudaError_t launch(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const Roles r = roles_of(a, lanes_of(a.head_dim, VEC), GRID * num_sms);
+  const Roles r = roles_of(a, lanes_of(a.head_dim, VEC), GRID * num_sms, false);
   return launch_dependent(k_head_norm<T, VEC, NU, INTER, PAGES, DIM>, dim3(r.end[2]), THREADS, 0, st, a, r);
 }
 template <typename T, bool INTER>
@@ -745,7 +759,7 @@ cudaError_t launch_pages(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
 }
 template <typename T, int D>
 cudaError_t launch_append(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
-  const Roles r = roles_of(a, D / 16, 16 * num_sms);
+  const Roles r = roles_of(a, D / 16, 16 * num_sms, false);
   return launch_dependent(k_append_4bit<T, D>, dim3(r.end[2]), THREADS, 0, st, a, r);
 }
 template <typename T, int VEC, int NU, bool INTER, int DIM>
@@ -753,12 +767,12 @@ cudaError_t launch_back(const HeadNormArgs& a, int num_sms, cudaStream_t st) {
   const int blocks = BACK_HELD * num_sms < HEAD_NORM_MAX_BLOCKS - 2 ? BACK_HELD * num_sms : HEAD_NORM_MAX_BLOCKS - 2;  // (a part may be rounded up)
   Roles r{};
   if (a.n_tokens > 0) {
-    r = roles_of(a, lanes_of(a.head_dim, VEC), blocks);
+    r = roles_of(a, lanes_of(a.head_dim, VEC), blocks, true);
     const cudaError_t e = launch_dependent(k_head_norm_back<T, VEC, NU, INTER, DIM>, dim3(r.end[1]), THREADS, 0, st, a, r);
     if (e != cudaSuccess) return e;
   }
   if (!a.dq_gain && !a.dk_gain) return cudaSuccess;
-  return launch_dependent(k_head_norm_gains, dim3((a.head_dim + 31) / 32, 2), 1024, 0, st, a.ws, r.end[0], r.end[1] - r.end[0], a.head_dim,
+  return launch_dependent(k_head_norm_gains, dim3((a.head_dim + GAIN_COLS - 1) / GAIN_COLS, 2), 1024, 0, st, a.ws, r.end[0], r.end[1] - r.end[0], a.head_dim,
                           a.dq_gain, a.dk_gain);
 }
 template <typename T, bool INTER>

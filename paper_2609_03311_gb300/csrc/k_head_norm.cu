@@ -827,10 +827,13 @@ __global__ void __launch_bounds__(THREADS) k_read_4bit(const __grid_constant__ R
           uint32_t x[4];
           const pages4::Widen<T> widen(byte[i][k] * 0x10001u);
           widen(word[i][k], x);
-          if constexpr (std::is_same_v<T, __half>) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (std::is_same_v<T, __half>) {
               const __half2 y = __hmul2(reinterpret_cast<const __half2&>(x[j]), __float2half2_rn(pages4::Widen<T>::UNIT));
+              x[j] = reinterpret_cast<const uint32_t&>(y);
+            } else {
+              const __nv_bfloat162 y = __hmul2(reinterpret_cast<const __nv_bfloat162&>(x[j]), __float2bfloat162_rn(pages4::Widen<T>::UNIT));
               x[j] = reinterpret_cast<const uint32_t&>(y);
             }
           }

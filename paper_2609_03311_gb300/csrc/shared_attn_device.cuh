@@ -1231,7 +1231,7 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
 // 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded twice to 11 bits.
 // Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
-// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 110 us (2.6 TB/s),
+// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 107 us (2.7 TB/s),
 // 153 by Few16 alone.
 template <typename T, int D>
 __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {
@@ -1246,9 +1246,9 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
   Jobs copies(plan, work, G);
   Job c{};
   bool unused, more = copies.next(c, unused);
-  uint32_t k = 0;
+  uint32_t first = more ? c.from : 0, k = 0, found = 0;  // of c, pieces from `first` on have been found, and k of them copied
   int stage = 0, ahead = 0;      // of the piece at hand, of the next one to be copied
-  int64_t code_at = 0;           // where the next 32 pieces lie: a lane a piece; its codes,
+  int64_t code_at = 0;           // where they lie: a lane a piece; its codes,
   int key_at = 0;                // its first row in the page, and 256 times its keys
   auto find = [&](uint32_t b) {
     if (b >= c.to) return;
@@ -1273,14 +1273,19 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
     to_lane[i] = r * ROW + (((x % CHUNKS) ^ chunk_place<D>(r)) << 4);
   }
   auto copy = [&] {
-    if (more && c.from + k == c.to) {
-      more = copies.next(c, unused);
+    if (k == found && more) {
+      first += k;
       k = 0;
+      while (more && first == c.to) {
+        more = copies.next(c, unused);
+        first = c.from;
+      }
+      found = more ? min(32u, c.to - first) : 0;
+      if (more) find(first + lane);
     }
-    if (more) {
-      if ((k & 31u) == 0) find(c.from + k + lane);
-      const int64_t at = __shfl_sync(0xffffffffu, code_at, k & 31u);
-      const int key = __shfl_sync(0xffffffffu, key_at, k & 31u);
+    if (k < found) {
+      const int64_t at = __shfl_sync(0xffffffffu, code_at, k);
+      const int key = __shfl_sync(0xffffffffu, key_at, k);
       const uint32_t dst = base + ahead * STAGE;
 #pragma unroll
       for (int i = 0; i < CODES / 512; ++i) {

@@ -1276,7 +1276,7 @@ __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Pl
     if (k == found && more) {
       first += k;
       k = 0;
-      while (more && first == c.to) {
+      if (first == c.to) {  // (no segment is empty)
         more = copies.next(c, unused);
         first = c.from;
       }

@@ -526,6 +526,7 @@ struct Read4Args {
   const uint8_t *k_pool, *v_pool;
   RopeView k, v;  // out only
   int32_t* status;
+  int rows;       // of a block at once; the launch's
 };
 cudaError_t launch_read_4bit(int dtype, const Read4Args& a, int num_sms, cudaStream_t st);
 

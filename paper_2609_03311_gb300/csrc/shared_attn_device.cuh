@@ -130,11 +130,6 @@ template <bool FOUR>
 __device__ __forceinline__ void regs_few() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(REGS_FEW<FOUR>)); }
 template <bool FOUR>
 __device__ __forceinline__ void regs_many() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(REGS_MANY<FOUR>)); }
-__device__ __forceinline__ void st_global32(void* p, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
-               "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }

@@ -49,7 +49,7 @@ struct Smem {
   static constexpr int F_STAGES = FOUR ? (D == 128 ? 8 : 12) : D == 128 ? 3 : 6;
   static constexpr int F_BYTES = FOUR ? 2 * PIECE * (D / 2 + D / 32) : 2 * HALVES * PIECE * 128;
   static constexpr int F_SCALES = WORKERS * F_STAGES * F_BYTES;  // 4 bits: what each warp takes of 32 keys' scales
-  static constexpr int F_SCALE_BYTES = FOUR ? 32 * (D / 32) * (4 + 2) : 0;
+  static constexpr int F_SCALE_BYTES = FOUR ? 32 * (D / 32) * 8 : 0;
   static_assert(F_SCALES + WORKERS * F_SCALE_BYTES <= OFF_ROW, "the few items' pieces");
   static constexpr int K_FULL = 0, K_EMPTY = K_FULL + K_STAGES, V_FULL = K_EMPTY + K_STAGES, V_EMPTY = V_FULL + V_STAGES,
                        Q_FULL = V_EMPTY + V_STAGES, Q_EMPTY = Q_FULL + 2, S_FULL = Q_EMPTY + 2, P_FULL = S_FULL + 2,
@@ -630,9 +630,6 @@ __device__ __forceinline__ uint2 lds64(uint32_t at) {
   asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(at));
   return x;
 }
-__device__ __forceinline__ void sts16(uint32_t at, uint32_t x) {
-  asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"(static_cast<uint16_t>(x)) : "memory");
-}
 __device__ __forceinline__ void sts64(uint32_t at, uint2 x) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x.x), "r"(x.y) : "memory");
 }
@@ -668,7 +665,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<const __half2&>(x); }
-__device__ __forceinline__ uint32_t as_bits(__half2 x) { return reinterpret_cast<const uint32_t&>(x); }
 // The four pairs of nibbles at 4 k and 16 + 4 k as fp16 numbers of the lowest bits: n 2^-24 for k = 0 and 2, 16 n 2^-24 for 1 and 3.
 __device__ __forceinline__ void as_subnormals(uint32_t w, uint32_t (&x)[4]) {
   x[0] = w & 0x000f000fu, x[1] = w & 0x00f000f0u;
@@ -925,6 +921,19 @@ struct Few8 {
       for (int k = 0; k < 4; ++k) o[i][0][k] = o[i][1][k] = ones[i][k] = 0.f;
   }
 
+  static __device__ __forceinline__ void put_scales(uint32_t to, const float (&f)[GROUPS]) {
+    if constexpr (GROUPS == 4) sts128(to, uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
+    else sts64(to, uint2{__float_as_uint(f[0]), __float_as_uint(f[1])});
+  }
+  static __device__ __forceinline__ void get_scales(uint32_t from, float (&f)[GROUPS]) {
+    if constexpr (GROUPS == 4) {
+      const uint4 u = lds128(from);
+      f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y), f[2] = __uint_as_float(u.z), f[3] = __uint_as_float(u.w);
+    } else {
+      const uint2 u = lds64(from);
+      f[0] = __uint_as_float(u.x), f[1] = __uint_as_float(u.y);
+    }
+  }
   // Two pieces of 16 keys, of which the first is column col0; the second's address is the first's where there is one only.
   __device__ __forceinline__ void step(const uint32_t (&piece)[2], uint32_t scales, int prefix_keys, int col0, bool& bad, int lane) {
     constexpr int N = 2;
@@ -960,17 +969,17 @@ struct Few8 {
             o[i][0][k] *= by, o[i][1][k] *= by, ones[i][k] *= by;
           }
       }
-      // a byte's exponent is 112 below as a 32-bit number's; and 2^24 of the codes, less 2^12 that are in `unit`
-      float f[GROUPS];
+      // a byte's exponent is 112 below as a 32-bit number's; K: and 2^24 of the codes, less 2^12 that are in `unit`
+      const float norm = __uint_as_float(static_cast<uint32_t>(253 - top_scale) << 23);
+      float f[GROUPS], v[GROUPS];
 #pragma unroll
-      for (int i = 0; i < GROUPS; ++i) f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p124f;
-      const __half2 norm = as_half2(static_cast<uint32_t>(29 - top_scale) << 10 | static_cast<uint32_t>(29 - top_scale) << 26);
-      const uint32_t even = as_bits(__hmul2(as_half2(vw << 7 & 0x7f807f80u), norm)), uneven = as_bits(__hmul2(as_half2(vw >> 1 & 0x7f807f80u), norm));
-      const uint32_t ks32 = scales + lane * (GROUPS * 4), vs16 = scales + 32 * GROUPS * 4 + 2 * lane;
-      if constexpr (GROUPS == 4) sts128(ks32, uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-      else sts64(ks32, uint2{__float_as_uint(f[0]), __float_as_uint(f[1])});
-      sts16(vs16, even), sts16(vs16 + 64, uneven);
-      if constexpr (GROUPS == 4) sts16(vs16 + 128, even >> 16), sts16(vs16 + 192, uneven >> 16);
+      for (int i = 0; i < GROUPS; ++i) {
+        f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p124f;
+        v[i] = __uint_as_float((i < 3 ? vw << (20 - 8 * i) : vw >> 4) & 0x0ff00000u) * norm;
+      }
+      const uint32_t to = scales + lane * (GROUPS * 4);
+      put_scales(to, f);
+      put_scales(to + 32 * GROUPS * 4, v);
       __syncwarp();
     }
     float sc[N][4];
@@ -979,15 +988,8 @@ struct Few8 {
       const int place = chunk_place<D>(g);
       const uint32_t kc = piece[n] + g * ROW + 4 * t, ks = scales + (16 * n + g) * (GROUPS * 4);
       float f0[GROUPS], f1[GROUPS];  // scales of the keys g and g + 8
-      if constexpr (GROUPS == 4) {
-        const uint4 u = lds128(ks), v = lds128(ks + 8 * GROUPS * 4);
-        f0[0] = __uint_as_float(u.x), f0[1] = __uint_as_float(u.y), f0[2] = __uint_as_float(u.z), f0[3] = __uint_as_float(u.w);
-        f1[0] = __uint_as_float(v.x), f1[1] = __uint_as_float(v.y), f1[2] = __uint_as_float(v.z), f1[3] = __uint_as_float(v.w);
-      } else {
-        const uint2 u = lds64(ks), v = lds64(ks + 8 * GROUPS * 4);
-        f0[0] = __uint_as_float(u.x), f0[1] = __uint_as_float(u.y);
-        f1[0] = __uint_as_float(v.x), f1[1] = __uint_as_float(v.y);
-      }
+      get_scales(ks, f0);
+      get_scales(ks + 8 * GROUPS * 4, f1);
       sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
@@ -1048,15 +1050,17 @@ struct Few8 {
       const float p0 = ex2(fmaf(sc[n][0], unit[0], -m0)), p1 = ex2(fmaf(sc[n][1], unit[1], -m1));
       const float p2 = ex2(fmaf(sc[n][2], unit[0], -m0)), p3 = ex2(fmaf(sc[n][3], unit[1], -m1));
       l[0] += p0 + p2, l[1] += p1 + p3;  // this thread's keys: the lanes' sums are added up at the end
-      // row g, keys 2 t and 2 t + 1, and 8 more
-      const __half2 pa = as_half2(transpose8(pack_f16x2(p0, p1))), pb = as_half2(transpose8(pack_f16x2(p2, p3)));
+      float f0[GROUPS], f1[GROUPS];
+      const uint32_t vs = scales + (32 + 16 * n + g) * (GROUPS * 4);
+      get_scales(vs, f0);
+      get_scales(vs + 8 * GROUPS * 4, f1);
       const uint32_t vc = piece[n] + CODES + 2 * t * ROW + 4 * (g >> 1);
-      const uint32_t vs = scales + 32 * GROUPS * 4 + 32 * n + 4 * t;  // two keys' of a group; 64 bytes a group
       const int place = chunk_place<D>(2 * t);
       const uint32_t half_word = g & 1 ? 0x7632u : 0x5410u;
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
-        const uint32_t ba = as_bits(__hmul2(pa, as_half2(lds32(vs + 64 * i)))), bb = as_bits(__hmul2(pb, as_half2(lds32(vs + 64 * i + 16))));
+        // P times the scale, rounded once: row g, keys 2 t and 2 t + 1, and 8 more
+        const uint32_t ba = transpose8(pack_f16x2(p0 * f0[i], p1 * f0[i])), bb = transpose8(pack_f16x2(p2 * f1[i], p3 * f1[i]));
         const uint32_t w = vc + ((i ^ place) << 4);
         uint32_t x[4], y[4];
         as_subnormals(__byte_perm(lds32(w), lds32(w + ROW), half_word), x);
@@ -1224,9 +1228,10 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
 // -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
 // from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
-// 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded twice to 11 bits.
+// 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded to 11 bits,
+// once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
 // Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
-// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 107 us (2.7 TB/s),
+// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 110 us (2.6 TB/s),
 // 153 by Few16 alone.
 template <typename T, int D>
 __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {

@@ -940,7 +940,7 @@ struct Few8 {
     const bool two = piece[1] != piece[0];
     const int g = lane >> 2, t = lane & 3;
     // each lane looks at a key's scales: bytes that stand for NaN become zeros; the largest of V's; and what the products take, a key's
-    // four of K in 32 bits, and V's in fp16 by groups
+    // of K and of V in 32 bits
     {
       const uint32_t ks = (lane < 16 ? piece[0] : piece[1]) + 2 * CODES + (lane & 15) * SROW;
       uint32_t kw, vw;

@@ -861,8 +861,11 @@ struct Few8 {
   int own0[2], own1[2];
   int all0, all1;                  // own columns that all rows see
   float o[GROUPS][2][4], ones[GROUPS][4];
+  // P = 2^(score - m), m BELOW the largest sum of a score and its value's exponent e (scales below 2^e) among the keys that the row
+  // sees: what is rounded is P times a scale, at most 2^15, and no key's value takes from another's unless it weighs more.  (Scales
+  // taken relative to the largest of all keys so far: rows lost what they saw to large values at no weight, or that later tokens alone
+  // see.)
   float m[2], l[2];
-  int top_scale;                   // the largest exponent of V's scales so far: they are taken times 2^(14 - top_scale)
 
   __device__ __forceinline__ Few8(const SharedAttnArgs& a, const Plan& plan, const Segment& s, int row0, int rows, int G, int lane) {
     const int g = lane >> 2, t = lane & 3;
@@ -884,7 +887,8 @@ struct Few8 {
     }
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // the row's largest to 2^13 and above: what is rounded then lies 2^-35 below it
+    // the row's largest to 2^13 and above: elements below 2^-23 of it are rounded, by at most 2^-34 of it (the sixteenths; the others
+    // from 2^-27, by 2^-38)
     const int e = most > 0.f ? min(100, 13 + 127 - static_cast<int>(__float_as_uint(most) >> 23)) : 0;
     const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
     float sum[GROUPS];
@@ -914,7 +918,6 @@ struct Few8 {
     }
     all0 = __reduce_max_sync(0xffffffffu, max(2 * t < rows ? own0[0] : 0, 2 * t + 1 < rows ? own0[1] : 0));
     all1 = __reduce_min_sync(0xffffffffu, min(2 * t < rows ? own1[0] : INT_MAX, 2 * t + 1 < rows ? own1[1] : INT_MAX));
-    top_scale = 0;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
@@ -939,8 +942,9 @@ struct Few8 {
     constexpr int N = 2;
     const bool two = piece[1] != piece[0];
     const int g = lane >> 2, t = lane & 3;
-    // each lane looks at a key's scales: bytes that stand for NaN become zeros; the largest of V's; and what the products take, a key's
-    // of K and of V in 32 bits
+    // each lane looks at a key's scales: bytes that stand for NaN become zeros; the exponent of the largest of V's; and what the products
+    // take, a key's of K and of V in 32 bits
+    float exponent;
     {
       const uint32_t ks = (lane < 16 ? piece[0] : piece[1]) + 2 * CODES + (lane & 15) * SROW;
       uint32_t kw, vw;
@@ -958,24 +962,13 @@ struct Few8 {
         }
         most = max_byte(vw);
       }
-      const int top = static_cast<int>(__reduce_max_sync(0xffffffffu, most)) >> 3;
-      if (top > top_scale) {
-        const float by = __uint_as_float(static_cast<uint32_t>(127 + top_scale - top) << 23);
-        top_scale = top;
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            o[i][0][k] *= by, o[i][1][k] *= by, ones[i][k] *= by;
-          }
-      }
+      exponent = static_cast<float>(static_cast<int>(most >> 3) - 14);
       // a byte's exponent is 112 below as a 32-bit number's; K: and 2^24 of the codes, less 2^12 that are in `unit`
-      const float norm = __uint_as_float(static_cast<uint32_t>(253 - top_scale) << 23);
       float f[GROUPS], v[GROUPS];
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
         f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p124f;
-        v[i] = __uint_as_float((i < 3 ? vw << (20 - 8 * i) : vw >> 4) & 0x0ff00000u) * norm;
+        v[i] = __uint_as_float((i < 3 ? vw << (20 - 8 * i) : vw >> 4) & 0x0ff00000u) * 0x1p112f;
       }
       const uint32_t to = scales + lane * (GROUPS * 4);
       put_scales(to, f);
@@ -1015,9 +1008,16 @@ struct Few8 {
     }
     // a row's keys are those of this thread and of the lanes with the same t
     float top[2];
+    {
+      float e[N][2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      top[j] = fmaxf(fmaxf(sc[0][j], sc[0][2 + j]), fmaxf(sc[1][j], sc[1][2 + j]));
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) e[n][i] = __shfl_sync(0xffffffffu, exponent, 16 * n + 8 * i + g);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        top[j] = fmaxf(fmaxf(fmaf(sc[0][j], unit[j], e[0][0]), fmaf(sc[0][2 + j], unit[j], e[0][1])),
+                       fmaxf(fmaf(sc[1][j], unit[j], e[1][0]), fmaf(sc[1][2 + j], unit[j], e[1][1])));
     }
 #pragma unroll
     for (int d = 4; d < 32; d <<= 1) {
@@ -1027,7 +1027,7 @@ struct Few8 {
     bool grow[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      top[j] = top[j] * unit[j] - BELOW<__half>;
+      top[j] -= BELOW<__half>;
       if (m[j] == -INFINITY) m[j] = top[j];  // nothing but zeros has been summed
       grow[j] = top[j] > m[j] + RESCALE<__half>;
     }
@@ -1083,7 +1083,7 @@ struct Few8 {
     }
     const float mm = odd ? m[1] : m[0], ll = odd ? l[1] : l[0];
     const bool whole = s.flags & SEG_WHOLE;
-    float by = __uint_as_float(static_cast<uint32_t>(127 + 24 - 14 + top_scale) << 23);
+    float by = 0x1p24f;
     if (whole) by = ll == 0.f ? 0.f : by * inverse(ll);
     const int at = row0 + (r < rows ? r : 0), h = s.h * G + at % G, token = plan.order[s.tok + at / G];
     float2* ml = reinterpret_cast<float2*>(a.ws);
@@ -1122,7 +1122,7 @@ struct Few8 {
 };
 
 // What a warp does at once of few items of the 4-bit cache: a segment, or where that has several long runs, whose tokens alone see
-// them, a run of it.  A part for Few8 is of one run: the scales of other tokens' values would cost its rows precision.  Few8 takes
+// them, a run of it.  A part for Few8 is of one run: the rows of others would see none of it.  Few8 takes
 // 0.9 us a piece where Few16 takes 1.4 with eight warps at work, but its code beside Few16's does not stay in the instruction
 // caches when parts are short (half of a warp's time then goes to waiting for instructions).  By the pieces from which Few8 takes a
 // run (on average over a segment's), in us:
@@ -1227,9 +1227,8 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // they stand four bits up, against 1 / 16 of the other operand): a mask and a quarter of a shift a pair of codes.  What is left of
 // c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
 // -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
-// from a product with ones.  Q is brought to fp16 by a power of two for each row, V's scales by one for all keys so far, and P lies
-// 2^11 below its range's end: P times a scale lies on steps of 2^-34 of the largest of each, or is rounded to 11 bits,
-// once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
+// from a product with ones.  Q is brought to fp16 by a power of two for each row, P times a scale by the row's m: it is rounded to 11
+// bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
 // Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
 // last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 110 us (2.6 TB/s),
 // 153 by Few16 alone.

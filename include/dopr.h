@@ -643,8 +643,9 @@ DOPR_API dopr_status dopr_cache_append_4bit(const dopr_cache_layout *layout, con
 
 /*
  * What the pages hold at slots[t], in layout->dtype (exact): k_out, v_out views of n_rows rows, 16-byte aligned with strides
- * multiples of 16 bytes.  Rows with slots[t] < 0 are left as they were; slots may repeat.  Device error: INVALID_ARG (a slot
- * outside the pool; its row is left).  Errors: INVALID_ARG, UNSUPPORTED, CUDA.
+ * multiples of 16 bytes.  Rows with slots[t] < 0 are left as they were; slots may repeat.  Groups whose scale byte stands for NaN come
+ * as NaN, which is no error here.  Device error: INVALID_ARG (a slot outside the pool; its row is left).  Errors: INVALID_ARG,
+ * UNSUPPORTED, CUDA.
  */
 DOPR_API dopr_status dopr_cache_read_4bit(const dopr_cache_layout *layout, int32_t n_rows, const int64_t *slots,
                                           const void *k_pool, const void *v_pool, const dopr_heads *k_out,
@@ -652,7 +653,8 @@ DOPR_API dopr_status dopr_cache_read_4bit(const dopr_cache_layout *layout, int32
 
 /*
  * dopr_shared_attention over such pools: the same plan, arguments and arithmetic on the values that the pages hold.  A scale byte
- * above 0xe1 among a row's keys counts as zero: device error RANGE.  Other errors as there.  Where up to 8 rows share many keys, a
+ * above 0xe1 among a row's keys counts as zero: device error RANGE, which status alone tells: results stay finite.  Other errors as
+ * there.  Where up to 8 rows share many keys, a
  * probability times a value's scale is rounded to 11 bits, or to steps of 2^-34 of the largest such product among the keys that the row
  * sees (scales below 2^-15 count as 2^-15 there), and a query's elements below 2^-23 of its head's largest to steps of 2^-33 of that.
  */

@@ -20,8 +20,10 @@ namespace {
 
 constexpr int THREADS = 128, MAX_DIM = 256;
 // Blocks an SM holds, by the registers that they get; and in the whole grid, for each SM, of many tokens: a view's blocks are not equally
-// long, so several rounds of them even out.  26,800 rows of 40 heads: 5 held, 40 in all 93.6 us; 6 and 12 115.7; 6 and 36 101;
-// 7 and 42 104 (registers run out).  Gradients of 8,192 rows: 4 held 60.8, 3 63.2, 5 74.2; their partial sums want few blocks.
+// long, so several rounds of them even out.  26,800 rows of 40 heads: 5 held, 40 in all 89 us; 5 and 20 89, 5 and 12 95; 4 and 40
+// 95; 6 and 12 102; 6 and 36 90; 7 and 42 98 (registers run out).  With the keys and values on the way into pages: 5 and 40 133, 4 and
+// 40 132, 5 and 20 136, 6 and 36 144, 7 and 42 187 (five hold 96 registers a thread, of which these kernels spill up to eleven words
+// where pairs are halves apart; four hold 128).  Gradients of 8,192 rows: 4 held 43, 3 45, 5 63; their partial sums want few blocks.
 constexpr int HELD = 5, GRID = 40, BACK_HELD = 4;
 
 template <typename T>
@@ -270,7 +272,7 @@ __device__ __forceinline__ void prefetch_angles(const HeadNormArgs& a, const Uni
 
 // The elements of a warp's heads, turn after turn over its units, of one or two views (backward: the inputs and the outputs'
 // gradients).  What bounds these kernels is how much is on its way: 16-byte copies into shared memory run AHEAD turns before they
-// are taken (one turn in registers: a chunk of 26,800 rows 112 us).  A lane takes what it has copied itself.
+// are taken (one turn ahead, in registers, as these kernels were then: a chunk of 26,800 rows 112 us).  A lane takes what it has copied itself.
 template <typename T, int VEC, int NU, bool INTER, int VIEWS, int AHEAD>
 struct Stream {
   static constexpr bool RING = VEC > 1;
@@ -706,8 +708,8 @@ bool wide(const HeadNormArgs& a, int size) {
   }
   return ok;
 }
-// Blocks for each role, by its work: turns of heads a warp, and about one for a token's cos and sin (gradients of 8,192 rows by the
-// heads alone: 60.3 us, the keys' blocks end last).  Few tokens leave most SMs idle, so their heads go to several warps.
+// Blocks for each role, by its work: turns of heads a warp, and about one for a token's cos and sin (by the heads alone the keys'
+// blocks end last).  Few tokens leave most SMs idle, so their heads go to several warps.
 // one_round: all blocks run at once, so what counts is the warp with most turns (1,021 rows of fp32, one slice a token: 14.2 us, by
 // this 13.7).
 Roles roles_of(const HeadNormArgs& a, int lanes, int most_blocks, bool one_round) {

@@ -60,7 +60,9 @@ struct Smem {
   static_assert(BYTES <= 227 * 1024, "shared memory budget");
 };
 
-// A wait of the CTA's roles.  4 bits: by counts, some two seconds, each role by itself; the clock's code and the atomic's, at twenty
+// A wait of the CTA's roles.  4 bits: by counts, some two seconds whatever limit the caller gives (that is the clock's), each role by
+// itself: where copies stop, the roles give up within two seconds of one another and their drains two seconds later, and the
+// error is reported then; the clock's code and the atomic's, at twenty
 // places, took more of the instruction caches than they can spare beside the warps that expand (200 queries on 16 documents: 182 us
 // for 220 with the clock, 200 with the atomic; 2,048 rows on 16,384 keys: 420 for 427 and 433).
 __device__ __forceinline__ bool wait_by_counts(uint32_t bar, uint32_t parity, int* err) {
@@ -1128,13 +1130,13 @@ struct Few8 {
 // run (on average over a segment's), in us:
 //           64 conversations of    256 of 50 to 400 keys,    32 of 1,000 to 3,000    8 of 16,000 keys,
 //           2,000 to 6,000 keys    4 and 8 rows a token      keys, a row a token     8 rows a token
-//      8          109                   75   76                     49                     63
-//     12          109                   64   71                     49                     63
-//     16          110                   48   54                     57                     65
-//     24          114                   48   50                     57                     69
-//   none          153                   48   50                     56                     83
+//      8          110                   68   73                     49                     63
+//     12          109                   56   68                     49                     63
+//     16          110                   46   52                     54                     64
+//     24          111                   46   50                     54                     66
+//   none          145                   46   50                     54                     79
 // and a segment of one run: one token of 32 heads on 8 over 32,768 keys, 256 queries on 64 documents of 1 to 1,024 tokens: from 6
-// pieces on 33.6 and 50.3, 12: 35.4 and 49.8, 24: 39.7 and 49.5, none: 39.7 and 48.7.
+// pieces on 33.7 and 50.9, 12: 34.2 and 50.3, 24: 38.4 and 49.9, none: 38.5 and 48.8.
 constexpr uint32_t LONG_RUN = 16, LONG_SEGMENT = 6;
 struct Job {
   const Segment* s;
@@ -1229,9 +1231,9 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
 // from a product with ones.  Q is brought to fp16 by a power of two for each row, P times a scale by the row's m: it is rounded to 11
 // bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
-// Bound by instructions, 420 a piece of 16 keys: two warps a quarter of the SM issue in 45 % of its cycles, each waiting for its own
-// last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000 keys each: 110 us (2.6 TB/s),
-// 153 by Few16 alone.
+// Bound by instructions, 445 a piece of 16 keys with starts and ends: two warps a quarter of the SM issue in 47 % of its cycles, each
+// waiting for its own last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000
+// keys each: 110 us (2.6 TB/s), 144 by Few16 alone.
 template <typename T, int D>
 __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {
   using L = Smem<D, true>;

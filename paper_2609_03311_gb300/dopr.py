@@ -756,7 +756,8 @@ def cache_pools_4bit(layout: CacheLayout, device="cuda"):
 def cache_append_4bit(layout: CacheLayout, slots, k, v, k_pool, v_pool, k_gain=None, eps: float = 0.0, rope: Rope | None = None,
                       positions=None, q=None, q_gain=None, q_out=None, status=None, stream=None):
     """One layer's new rows k and v [tokens, kv heads, head_dim] into the 4-bit pages at slots; k, and q where it is given,
-    are normed first where eps > 0 and turned where there is a rope.  Returns q_out.  Not recorded for autograd."""
+    are normed first where eps > 0 and turned where there is a rope.  Returns q_out.  status, an int32 of the device, is what tells of
+    rows that could not be held.  Not recorded for autograd."""
     T, D, dt, dev = k.shape[0], layout.head_dim, _TORCH_TYPES[layout.dtype], k.device
     handle = rope.handle() if rope is not None else None
     pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
@@ -778,7 +779,8 @@ def cache_append_4bit(layout: CacheLayout, slots, k, v, k_pool, v_pool, k_gain=N
 
 
 def cache_read_4bit(layout: CacheLayout, slots, k_pool, v_pool, k_out=None, v_out=None, status=None, stream=None):
-    """What the 4-bit pages hold at slots: (k_out, v_out) [rows, kv heads, head_dim] of the layout's type."""
+    """What the 4-bit pages hold at slots: (k_out, v_out) [rows, kv heads, head_dim] of the layout's type; NaN where a group could not
+    be held."""
     T, D, dt, dev = slots.numel(), layout.head_dim, _TORCH_TYPES[layout.dtype], slots.device
     pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
     st, guard, on = _on(dev, stream)
@@ -799,7 +801,8 @@ def cache_read_4bit(layout: CacheLayout, slots, k_pool, v_pool, k_out=None, v_ou
 
 def shared_attention_4bit(layout: CacheLayout, plan, q, k_pool, v_pool, block_tables, scale: float | None = None, out=None, lse=None,
                           workspace=None, status=None, stream=None) -> torch.Tensor:
-    """shared_attention over 4-bit pools: the same plan and workspace, q and out of the layout's type.  Not recorded for autograd."""
+    """shared_attention over 4-bit pools: the same plan and workspace, q and out of the layout's type.  Groups that could not be held
+    count as zeros, so a program that may have stored some passes status (ERR_RANGE).  Not recorded for autograd."""
     pool = _sized(load().dopr_cache_4bit_pool_bytes, layout)
     return _attention(load().dopr_shared_attention_4bit, layout, plan, q, k_pool, v_pool, pool, torch.uint8, block_tables, scale, out,
                       lse, workspace, status, stream)

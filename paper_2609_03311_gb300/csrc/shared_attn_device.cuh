@@ -862,7 +862,7 @@ struct Few8 {
   float unit[2];                   // what their scores are multiplied by
   int own0[2], own1[2];
   int all0, all1;                  // own columns that all rows see
-  float o[GROUPS][2][4], ones[GROUPS][4];
+  float o[GROUPS][2][4];
   // P = 2^(score - m), m BELOW the largest sum of a score and its value's exponent e (scales below 2^e) among the keys that the row
   // sees: what is rounded is P times a scale, at most 2^15, and no key's value takes from another's unless it weighs more.  (Scales
   // taken relative to the largest of all keys so far: rows lost what they saw to large values at no weight, or that later tokens alone
@@ -923,7 +923,7 @@ struct Few8 {
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[i][0][k] = o[i][1][k] = ones[i][k] = 0.f;
+      for (int k = 0; k < 4; ++k) o[i][0][k] = o[i][1][k] = 0.f;
   }
 
   static __device__ __forceinline__ void put_scales(uint32_t to, const float (&f)[GROUPS]) {
@@ -1042,7 +1042,6 @@ struct Few8 {
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) {
           o[i][0][j] *= by, o[i][0][2 + j] *= by, o[i][1][j] *= by, o[i][1][2 + j] *= by;
-          ones[i][j] *= by, ones[i][2 + j] *= by;
         }
       }
     }
@@ -1067,9 +1066,11 @@ struct Few8 {
         uint32_t x[4], y[4];
         as_subnormals(__byte_perm(lds32(w), lds32(w + ROW), half_word), x);
         as_subnormals(__byte_perm(lds32(w + 8 * ROW), lds32(w + 9 * ROW), half_word), y);
+        // less 8 2^-24, and 16 times that, of each first
+        mma_f16_add(o[i][0], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, ba, bb);
+        mma_f16_add(o[i][1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, ba, bb);
         mma_f16_add(o[i][0], x[0], x[1], y[0], y[1], ba, bb);
         mma_f16_add(o[i][1], x[2], x[3], y[2], y[3], ba, bb);
-        mma_f16_add(ones[i], 0x00080008u, 0x00080008u, 0x00080008u, 0x00080008u, ba, bb);  // 8 2^-24
       }
     }
   }
@@ -1100,7 +1101,7 @@ struct Few8 {
         // O of code k: the second of each pair is 16 times what it is
         const float(&x)[4] = o[i][k >> 1];
         const float f = k & 1 ? 1.f / 16.f : 1.f;
-        const float e0 = fmaf(x[2 * (k & 1)], f, -ones[i][0]), e1 = fmaf(x[2 * (k & 1) + 1], f, -ones[i][1]);
+        const float e0 = x[2 * (k & 1)] * f, e1 = x[2 * (k & 1) + 1] * f;
         const float other = __shfl_xor_sync(0xffffffffu, odd ? e0 : e1, 4);
         v[2 * k] = odd ? other : e0, v[2 * k + 1] = odd ? e1 : other;
       }
@@ -1228,8 +1229,9 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // values there, 16 of them for 8 rows, and codes go into the products as they are, as fp16 numbers of the lowest bits (n 2^-24; 16 n 2^-24 where
 // they stand four bits up, against 1 / 16 of the other operand): a mask and a quarter of a shift a pair of codes.  What is left of
 // c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
-// -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the keys comes
-// from a product with ones.  Q is brought to fp16 by a power of two for each row, P times a scale by the row's m: it is rounded to 11
+// -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the piece's keys is
+// taken off by a product with -8 ahead of that with the codes.  (Added up over all keys beside the codes' sum and taken off at the end,
+// it made both grow and every step cut them off at their last bit: errors of 0.03 of the outputs' norm over 1,700 pieces.)  Q is brought to fp16 by a power of two for each row, P times a scale by the row's m: it is rounded to 11
 // bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
 // Bound by instructions, 445 a piece of 16 keys with starts and ends: two warps a quarter of the SM issue in 47 % of its cycles, each
 // waiting for its own last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000

@@ -135,3 +135,38 @@ def test_values_that_are_all_zero_and_ones_behind_them(dt):
     b.check(got)
     for i in range(2, len(b.lens), 4):
         assert bool((got[0][i] == 0).all())
+
+
+@pytest.mark.parametrize("S,n,hq,hkv,d,dt", [(128, 32768, 8, 8, 64, HF), (128, 32771, 8, 2, 128, HF), (128, 30001, 8, 8, 128, BF),
+                                             (256, 20011, 8, 4, 64, BF)])
+@pytest.mark.parametrize("mean", [0.0, 2.0])
+def test_many_long_sequences(S, n, hq, hkv, d, dt, mean):
+    # A warp's part has hundreds of pieces, of keys of about one weight.  Roundings are independent of one another and of the values: of
+    # P times a scale at most 2^-11 of each term, whose squares add up to those of the values' part that has no mean, and of the result u;
+    # uniform ones have a third of their bounds' squares on the mean.  32-bit sums add next to nothing.  Twice that is allowed.
+    page, pages = 64, -(-n // 64)
+    layout = dopr.make_cache_layout(S * pages, page, hkv, d, dt, S, pages)
+    k4, v4 = dopr.cache_pools_4bit(layout)
+    g = torch.Generator(DEV).manual_seed(n)
+    tables = torch.randperm(S * pages, generator=g, device=DEV).view(S, pages)
+    t = torch.arange(n, device=DEV)
+    slots = lambda i: tables[i][t // page] * page + t % page  # noqa: E731
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for i in range(S):
+        k, v = (torch.randn(n, hkv, d, generator=g, device=DEV) for _ in range(2))
+        dopr.cache_append_4bit(layout, slots(i), k.to(dt), (v + mean).to(dt), k4, v4, status=st)
+    q = (torch.randn(S, hq, d, generator=g, device=DEV) / 4).to(dt)
+    i32 = lambda x: torch.as_tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    plan = dopr.shared_attention_plan(layout, hq, i32(range(S + 1)), i32([n] * S), i32([-1] * S), S, status=st)
+    out = dopr.shared_attention_4bit(layout, plan, q, k4, v4, i32(tables), status=st)
+    assert st.item() == 0
+    G, err, room = hq // hkv, 0.0, 0.0
+    for i in range(0, S, 16):
+        k, v = dopr.cache_read_4bit(layout, slots(i), k4, v4)
+        for h in range(hkv):
+            a = (q[i, h * G:h * G + G].double() @ k[:, h].double().T * d ** -0.5).softmax(-1)
+            want = a @ v[:, h].double()
+            u = torch.finfo(dt).eps / 2
+            err += float((out[i, h * G:h * G + G].double() - want).square().sum())
+            room += float((2.0 ** -22 * (a.square() @ v[:, h].double().square()) + u ** 2 * want.square()).sum()) / 3
+    assert err <= 4 * room, math.sqrt(err / room)

@@ -656,7 +656,7 @@ DOPR_API dopr_status dopr_cache_read_4bit(const dopr_cache_layout *layout, int32
  * above 0xe1 among a row's keys counts as zero: device error RANGE, which status alone tells: results stay finite.  Other errors as
  * there.  Where up to 8 rows share many keys, a
  * probability times a value's scale is rounded to 11 bits, or to steps of 2^-34 of the largest such product among the keys that the row
- * sees (scales below 2^-15 count as 2^-15 there), and a query's elements below 2^-23 of its head's largest to steps of 2^-33 of that.
+ * sees (scales below 2^-15 count as 2^-15 there), and a query's elements below 2^-27 of its head's largest to steps of 2^-37 of that.
  */
 DOPR_API dopr_status dopr_shared_attention_4bit(const dopr_cache_layout *layout, const void *plan, int32_t max_tokens,
                                                 const dopr_heads *q, const void *k_pool, const void *v_pool,

@@ -5,7 +5,8 @@
 // the arithmetic is that of the 16-bit cache on those values.
 //   Tiles: 512 threads a CTA.  Blocks come as they are held, by bulk copies of a page each (codes and scales lie together), into a
 //   ring of halves of 64 rows; four warps widen them into the rings that the products read.
-//   Few items: a warp a part of one; codes go into the products as they are, or are widened in registers where parts are short.
+//   Few items: a warp a part of one; codes go into the products without their scales, or are widened in registers where
+//   parts are short.
 // Every finite scale gives finite values, and one that stands for NaN counts as zero and is an error, so a column that a row does
 // not see can add nothing to it, and no row is looked at again.
 #include "shared_attn_device.cuh"

@@ -647,14 +647,7 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                "r"(bar)
                : "memory");
 }
-// D (16 x 8, 32-bit) = A (16 x 16) B (16 x 8) + C of fp16 by a warp.
-__device__ __forceinline__ void mma_f16_from(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0,
-                                             float c1, float c2, float c3) {
-  asm(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
+// D (16 x 8, 32-bit) += A (16 x 16) B (16 x 8) of fp16 by a warp.
 __device__ __forceinline__ void mma_f16_add(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -667,11 +660,18 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 __device__ __forceinline__ __half2 as_half2(uint32_t x) { return reinterpret_cast<const __half2&>(x); }
-// The four pairs of nibbles at 4 k and 16 + 4 k as fp16 numbers of the lowest bits: n 2^-24 for k = 0 and 2, 16 n 2^-24 for 1 and 3.
-__device__ __forceinline__ void as_subnormals(uint32_t w, uint32_t (&x)[4]) {
-  x[0] = w & 0x000f000fu, x[1] = w & 0x00f000f0u;
-  w >>= 8;
-  x[2] = w & 0x000f000fu, x[3] = w & 0x00f000f0u;
+// The four pairs of codes at 4 k and 16 + 4 k as fp16 numbers c 2^-9: n 2^-24 or 16 n 2^-24 as they stand, the type's lowest, to n 2^-9 less
+// 8 2^-9, exactly.  (As they stand in the products, with 8 times the other operand taken off, is a fused step less for a pair, but the
+// sums are off by up to 2^-15 of their largest terms: lighter keys beside a heavy one whose code is zero were lost, and scores of hundreds
+// off by ten times what a product in 32 bits is.  It was no faster: 64 conversations 110 us for 106.)
+__device__ __forceinline__ void as_codes(uint32_t w, uint32_t (&x)[4]) {
+  const uint32_t n[4] = {w & 0x000f000fu, w & 0x00f000f0u, w >> 8 & 0x000f000fu, w >> 8 & 0x00f000f0u};
+  const uint32_t up = 0x78007800u, up16 = 0x68006800u, from = 0xa400a400u;  // 2^15, 2^11, -8 2^-9
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __half2 c = __hfma2(as_half2(n[k]), as_half2(k & 1 ? up16 : up), as_half2(from));
+    x[k] = reinterpret_cast<const uint32_t&>(c);
+  }
 }
 // The largest of a word's bytes.
 __device__ __forceinline__ uint32_t max_byte(uint32_t w) {
@@ -857,8 +857,7 @@ struct Few16 {
 template <typename T, int D>
 struct Few8 {
   static constexpr int GROUPS = D / 32, ROW = D / 2, SROW = D / 32, CODES = PIECE * ROW, SCALES = PIECE * SROW;
-  uint32_t q[GROUPS][4];           // row g: 8 elements from 8 t on of each group; the second and fourth pair 1 / 16
-  float start[GROUPS][4];          // -8 2^-24 times Q's sum over the group, rows 2 t and 2 t + 1, twice: as a product's sum begins
+  uint32_t q[GROUPS][4];           // row g: 8 elements from 8 t on of each group
   float unit[2];                   // what their scores are multiplied by
   int own0[2], own1[2];
   int all0, all1;                  // own columns that all rows see
@@ -889,30 +888,17 @@ struct Few8 {
     }
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
     most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-    // the row's largest to 2^13 and above: elements below 2^-23 of it are rounded, by at most 2^-34 of it (the sixteenths; the others
-    // from 2^-27, by 2^-38)
+    // the row's largest to 2^13 and above: elements below 2^-27 of it are rounded, by at most 2^-38 of it
     const int e = most > 0.f ? min(100, 13 + 127 - static_cast<int>(__float_as_uint(most) >> 23)) : 0;
     const float up = __uint_as_float(static_cast<uint32_t>(127 + e) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);
-    float sum[GROUPS];
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      sum[i] = 0.f;
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float by = k & 1 ? up / 16.f : up;
-        q[i][k] = pack_f16x2(x[i][2 * k] * by, x[i][2 * k + 1] * by);
-        const float2 f = __half22float2(as_half2(q[i][k]));
-        sum[i] += (f.x + f.y) * (k & 1 ? 16.f : 1.f);
-      }
-      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
-      sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-    }
-    const float scale = a.scale * 1.4426950408889634f * 0x1p12f;
+      for (int k = 0; k < 4; ++k) q[i][k] = pack_f16x2(x[i][2 * k] * up, x[i][2 * k + 1] * up);
+    const float scale = a.scale * 1.4426950408889634f * 0x1p9f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int row = 2 * t + j;
-#pragma unroll
-      for (int i = 0; i < GROUPS; ++i) start[i][j] = start[i][2 + j] = -8.f * 0x1p-24f * __shfl_sync(0xffffffffu, sum[i], 4 * row);
       unit[j] = scale * __shfl_sync(0xffffffffu, down, 4 * row);
       const int2 own = plan.own[s.tok + (row0 + (row < rows ? row : 0)) / G];
       own0[j] = row < rows ? own.x : 0, own1[j] = row < rows ? own.y : 0;
@@ -965,11 +951,11 @@ struct Few8 {
         most = max_byte(vw);
       }
       exponent = static_cast<float>(static_cast<int>(most >> 3) - 14);
-      // a byte's exponent is 112 below as a 32-bit number's; K: and 2^24 of the codes, less 2^12 that are in `unit`
+      // a byte's exponent is 112 below as a 32-bit number's
       float f[GROUPS], v[GROUPS];
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
-        f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p124f;
+        f[i] = __uint_as_float((i < 3 ? kw << (20 - 8 * i) : kw >> 4) & 0x0ff00000u) * 0x1p112f;
         v[i] = __uint_as_float((i < 3 ? vw << (20 - 8 * i) : vw >> 4) & 0x0ff00000u) * 0x1p112f;
       }
       const uint32_t to = scales + lane * (GROUPS * 4);
@@ -989,10 +975,10 @@ struct Few8 {
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
         uint32_t x[4], y[4];
-        as_subnormals(lds32(kc + ((i ^ place) << 4)), x);
-        as_subnormals(lds32(kc + ((i ^ place) << 4) + 8 * ROW), y);
-        float d[4];
-        mma_f16_from(d, x[0], y[0], x[1], y[1], q[i][0], q[i][1], start[i][0], start[i][1], start[i][2], start[i][3]);
+        as_codes(lds32(kc + ((i ^ place) << 4)), x);
+        as_codes(lds32(kc + ((i ^ place) << 4) + 8 * ROW), y);
+        float d[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_f16_add(d, x[0], y[0], x[1], y[1], q[i][0], q[i][1]);
         mma_f16_add(d, x[2], y[2], x[3], y[3], q[i][2], q[i][3]);
         sc[n][0] = fmaf(d[0], f0[i], sc[n][0]), sc[n][1] = fmaf(d[1], f0[i], sc[n][1]);
         sc[n][2] = fmaf(d[2], f1[i], sc[n][2]), sc[n][3] = fmaf(d[3], f1[i], sc[n][3]);
@@ -1064,11 +1050,8 @@ struct Few8 {
         const uint32_t ba = transpose8(pack_f16x2(p0 * f0[i], p1 * f0[i])), bb = transpose8(pack_f16x2(p2 * f1[i], p3 * f1[i]));
         const uint32_t w = vc + ((i ^ place) << 4);
         uint32_t x[4], y[4];
-        as_subnormals(__byte_perm(lds32(w), lds32(w + ROW), half_word), x);
-        as_subnormals(__byte_perm(lds32(w + 8 * ROW), lds32(w + 9 * ROW), half_word), y);
-        // less 8 2^-24, and 16 times that, of each first
-        mma_f16_add(o[i][0], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, ba, bb);
-        mma_f16_add(o[i][1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, ba, bb);
+        as_codes(__byte_perm(lds32(w), lds32(w + ROW), half_word), x);
+        as_codes(__byte_perm(lds32(w + 8 * ROW), lds32(w + 9 * ROW), half_word), y);
         mma_f16_add(o[i][0], x[0], x[1], y[0], y[1], ba, bb);
         mma_f16_add(o[i][1], x[2], x[3], y[2], y[3], ba, bb);
       }
@@ -1086,7 +1069,7 @@ struct Few8 {
     }
     const float mm = odd ? m[1] : m[0], ll = odd ? l[1] : l[0];
     const bool whole = s.flags & SEG_WHOLE;
-    float by = 0x1p24f;
+    float by = 0x1p9f;
     if (whole) by = ll == 0.f ? 0.f : by * inverse(ll);
     const int at = row0 + (r < rows ? r : 0), h = s.h * G + at % G, token = plan.order[s.tok + at / G];
     float2* ml = reinterpret_cast<float2*>(a.ws);
@@ -1098,10 +1081,8 @@ struct Few8 {
       float v[8];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        // O of code k: the second of each pair is 16 times what it is
-        const float(&x)[4] = o[i][k >> 1];
-        const float f = k & 1 ? 1.f / 16.f : 1.f;
-        const float e0 = x[2 * (k & 1)] * f, e1 = x[2 * (k & 1) + 1] * f;
+        const float(&x)[4] = o[i][k >> 1];  // O of code k
+        const float e0 = x[2 * (k & 1)], e1 = x[2 * (k & 1) + 1];
         const float other = __shfl_xor_sync(0xffffffffu, odd ? e0 : e1, 4);
         v[2 * k] = odd ? other : e0, v[2 * k + 1] = odd ? e1 : other;
       }
@@ -1226,13 +1207,11 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // Eight warps a CTA with a ring of pieces each, by 16-byte copies.  Scales of rows past a run's keys come as zeros, so such rows are zeros.
 //
 // Few16 has rows on the products' long side (16) and widens codes to 16 bits by masks, shifts and fused products.  Few8 has keys and
-// values there, 16 of them for 8 rows, and codes go into the products as they are, as fp16 numbers of the lowest bits (n 2^-24; 16 n 2^-24 where
-// they stand four bits up, against 1 / 16 of the other operand): a mask and a quarter of a shift a pair of codes.  What is left of
-// c s = (n - 8) s is added where there is less of it: a group's products with Q are scaled when its 32 elements are summed up, and
-// -8 times the sum of Q is where that sum starts; P times V's scale is made for each group, and 8 times its sum over the piece's keys is
-// taken off by a product with -8 ahead of that with the codes.  (Added up over all keys beside the codes' sum and taken off at the end,
-// it made both grow and every step cut them off at their last bit: errors of 0.03 of the outputs' norm over 1,700 pieces.)  Q is brought to fp16 by a power of two for each row, P times a scale by the row's m: it is rounded to 11
-// bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in fp16: 107 us, but errors of 0.00035 of the outputs' norm for 0.00028).
+// values there, 16 of them for 8 rows, and codes go into the products without their scales, as c 2^-9 (as_codes): a mask, a fused step and a
+// quarter of a shift a pair.  Scales come in where there is less of them: a group's products with Q are scaled when its 32 elements are
+// summed up, and P is multiplied by V's scale for each group.  Q is brought to fp16 by a power of two for each row, P times a scale by the
+// row's m: it is rounded to 11 bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in
+// fp16: errors of 0.00035 of the outputs' norm for 0.00028).
 // Bound by instructions, 445 a piece of 16 keys with starts and ends: two warps a quarter of the SM issue in 47 % of its cycles, each
 // waiting for its own last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000
 // keys each: 110 us (2.6 TB/s), 144 by Few16 alone.

@@ -170,3 +170,46 @@ def test_many_long_sequences(S, n, hq, hkv, d, dt, mean):
             err += float((out[i, h * G:h * G + G].double() - want).square().sum())
             room += float((2.0 ** -22 * (a.square() @ v[:, h].double().square()) + u ** 2 * want.square()).sum()) / 3
     assert err <= 4 * room, math.sqrt(err / room)
+
+
+@pytest.mark.parametrize("dt,d,page", FORMS)
+@pytest.mark.parametrize("kind", ["a row a token", "four rows a token", "eight rows a token"])
+def test_light_values_beside_a_heavy_key_whose_codes_are_zero(kind, dt, d, page):
+    # Every second element of the heavy key's value is zero, beside others of 4; the keys around it have 2^-18 of its weight and all that there
+    # is of those elements.  The heavy key has the largest product, so a key adds at most 7 2^-35 of 4 / 7.
+    hq, hkv, _, reqs = LONG[kind]
+    b = Sized(hq, hkv, d, dt, page, [], reqs, seed=len(kind) + d)
+    for i, n in enumerate(b.lens):
+        b.light_beside_heavy(i, n - 9)
+        v = b.rows[i][1]
+        v *= 16.0
+        v[:-16] = 0.0
+        v[n - 9, :, 1::2] = 4.0
+        b.write(i, torch.arange(n, device=DEV))
+    b.check(b.run())
+
+
+@pytest.mark.parametrize("dt,d,page", FORMS)
+@pytest.mark.parametrize("size", [1, 16, 256])
+def test_scores_are_as_good_as_a_product_in_32_bits(size, dt, d, page):
+    # A score is a sum of a head's products, exact in 32 bits, in 16 steps at most, each of which is off by a last bit of what has been
+    # added up, below 2^-23 of the sum M of the magnitudes; independent of one another (half of that on the root of the mean squares): the
+    # root of 16 half bits, and 2^-22 |score| of the last two products.  One key outweighs the others there, so its score is what is seen.
+    # Twice that is allowed on the root mean square over the rows, beside 2^-12 of the softmax's sum in the worst row.
+    hq, hkv, _, reqs = LONG["four rows a token"]
+    b = Sized(hq, hkv, d, dt, page, [], reqs, seed=size)
+    for i, n in enumerate(b.lens):
+        b.rows[i][0] = (b.rows[i][0].float() * size ** 0.5).to(dt)
+        b.write(i, torch.arange(n, device=DEV))
+    b.q = (b.q.float() * 4 * size ** 0.5).to(dt)
+    lse, got = b.exact()[1], b.run()[1].double()
+    bound = torch.zeros_like(lse)
+    for i in range(len(b.lens)):
+        k = b.rows[i][0].double().repeat_interleave(hq // hkv, 1)
+        a = torch.einsum("hd,khd->hk", b.q[i].double(), k) * d ** -0.5
+        at = a.argmax(-1)
+        M = (b.q[i].double().abs() * k[at, torch.arange(hq, device=DEV)].abs()).sum(-1) * d ** -0.5
+        bound[i] = M * 4 * 2.0 ** -24 + a.amax(-1).abs() * 2.0 ** -22 + 2.0 ** -20
+    err = (got - lse).abs()
+    assert float(err.square().mean().sqrt()) <= 2 * float(bound.square().mean().sqrt()), float(err.square().mean().sqrt() / bound.square().mean().sqrt())
+    assert bool((err <= 2.0 ** -12 + 8 * bound).all()), float((err / bound).max())

@@ -1112,13 +1112,13 @@ struct Few8 {
 // run (on average over a segment's), in us:
 //           64 conversations of    256 of 50 to 400 keys,    32 of 1,000 to 3,000    8 of 16,000 keys,
 //           2,000 to 6,000 keys    4 and 8 rows a token      keys, a row a token     8 rows a token
-//      8          110                   68   73                     49                     63
-//     12          109                   56   68                     49                     63
-//     16          110                   46   52                     54                     64
-//     24          111                   46   50                     54                     66
-//   none          145                   46   50                     54                     79
+//      8          104                   64   71                     48                     61
+//     12          104                   54   67                     48                     62
+//     16          106                   45   52                     54                     63
+//     24          108                   46   51                     54                     66
+//   none          142                   46   51                     54                     78
 // and a segment of one run: one token of 32 heads on 8 over 32,768 keys, 256 queries on 64 documents of 1 to 1,024 tokens: from 6
-// pieces on 33.7 and 50.9, 12: 34.2 and 50.3, 24: 38.4 and 49.9, none: 38.5 and 48.8.
+// pieces on 33.2 and 50.4, 12: 34.8 and 49.9, 24: 38.5 and 49.4, none: 38.5 and 48.6.
 constexpr uint32_t LONG_RUN = 16, LONG_SEGMENT = 6;
 struct Job {
   const Segment* s;
@@ -1212,9 +1212,9 @@ __device__ __forceinline__ void rows_without_keys(const SharedAttnArgs& a, const
 // summed up, and P is multiplied by V's scale for each group.  Q is brought to fp16 by a power of two for each row, P times a scale by the
 // row's m: it is rounded to 11 bits, or lies on steps of 2^-34 of the row's largest, once (P rounded first, and the product of both in
 // fp16: errors of 0.00035 of the outputs' norm for 0.00028).
-// Bound by instructions, 445 a piece of 16 keys with starts and ends: two warps a quarter of the SM issue in 47 % of its cycles, each
+// Bound by instructions, 476 a piece of 16 keys with starts and ends: two warps a quarter of the SM issue in 53 % of its cycles, each
 // waiting for its own last result otherwise; the registers (168 a thread) hold no third.  64 tokens of 32 heads on 8 over 2,000 to 6,000
-// keys each: 110 us (2.6 TB/s), 144 by Few16 alone.
+// keys each: 106 us (2.7 TB/s), 142 by Few16 alone.
 template <typename T, int D>
 __device__ __forceinline__ void few_items_4bit(const SharedAttnArgs& a, const Plan& plan, uint32_t s0, int warp, int2 work, int lane) {
   using L = Smem<D, true>;
